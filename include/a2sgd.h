@@ -365,6 +365,95 @@ int a2sgd_encode_noalloc(uint64_t n, uint32_t P, uint32_t mode, const float *gra
                          const float *err, int64_t err_stride, float *local_means, uint64_t *pos_counts,
                          void *stream);
 
+/* ======================================================================
+ * Training operators: what produces the gradients of a transformer block (layer norm, the gated
+ * feed-forward block) and what consumes the averaged ones (AdamW over a list of tensors).  They
+ * stand beside the A2SGD step and share its conventions: device memory owned by the caller, nothing
+ * allocated or retained except by a2sgd_adamw_create, kernels enqueued on `stream` of `device`,
+ * refusals by status before anything is launched, results bitwise reproducible (no floating-point
+ * atomics, fixed-order sums).  Calls without a plan keep no state between calls; calls that share a
+ * workspace or a plan must follow one another in stream order.  Sums and statistics are fp32 (the
+ * gradients' norm fp64); a 16-bit output is rounded once, to nearest, ties to even.
+ *
+ * Element types.  16-bit tensors are passed as void* with one of: */
+enum a2sgd_dtype { A2SGD_F32 = 0, A2SGD_BF16 = 1, A2SGD_F16 = 2 };
+
+/* AdamW (Loshchilov and Hutter) over S tensors at once, one launch a step.  For every element, with
+ * c = *grad_scale (1 without one) and t = step:
+ *     g = c * grad
+ *     m <- beta1 m + (1 - beta1) g          v <- beta2 v + (1 - beta2) g^2
+ *     w <- w (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, each product, sum, quotient and root rounded once, in that order; the coefficients are formed
+ * in fp64 and rounded once.  Weights are fp32; a 16-bit copy of them is written by the same pass when w16
+ * is given.
+ *
+ * State.  One buffer each for m and v, holding the tensors one after another, every tensor starting at a
+ * multiple of A2SGD_ADAMW_BLOCK elements; a2sgd_adamw_state_elements gives the length.  Zero it
+ * before the first step.
+ *   32 bits  float m[], v[].
+ *   8 bits   int8_t m[], uint8_t v[], and one float of m_scale[], v_scale[] a block:
+ *                m = sign(q) (q / 127)^2 m_scale,        sqrt(v) = (q / 255)^2 v_scale,
+ *            the scale being the block's largest value.  Squares spend the codes on small values: the
+ *            smallest one is 6e-5 of the scale, a step near the scale 1.6 % and 0.8 %.  Codes are rounded up
+ *            or down by a 12-bit dither, a hash of the step and of the element's place, so that their
+ *            expectation is the value: with beta2 = 0.999 a step moves sqrt(v) by at most 0.05 % when
+ *            gradients fall silent, and rounding to nearest would hold it still for ever.  v's code is at
+ *            least 2 (6e-5 of the scale), so that |m| / sqrt(v) stays within what exact states can reach.
+ *            A block that meets a gradient that is not finite holds NaN from then on, as 32-bit states do
+ *            element by element.
+ *
+ *   S, numel    number of tensors; HOST [S] element counts (each >= 1)
+ *   w, grad     HOST arrays of S DEVICE pointers: fp32 weights, gradients of grad_dtype
+ *   w16         HOST array of S DEVICE pointers to the copies of w16_dtype, or NULL
+ *   state_bits  32 or 8;  m, v 32-byte aligned;  m_scale, v_scale [state_elements / A2SGD_ADAMW_BLOCK]
+ *               (8 bits) or NULL (32)
+ * A tensor whose w is 32-byte and grad and w16 16-byte aligned takes the widest accesses; any alignment to
+ * the element type is right.  The plan keeps the pointers. */
+typedef struct a2sgd_adamw a2sgd_adamw;
+#define A2SGD_ADAMW_BLOCK 256
+uint64_t a2sgd_adamw_state_elements(uint32_t S, const uint64_t *numel);
+int a2sgd_adamw_create(a2sgd_adamw **out, uint32_t S, const uint64_t *numel, float *const *w,
+                       const void *const *grad, int grad_dtype, void *const *w16, int w16_dtype,
+                       int state_bits, void *m, void *v, float *m_scale, float *v_scale, int device);
+int a2sgd_adamw_destroy(a2sgd_adamw *plan);
+
+/* The step above.  lr, weight_decay >= 0, 0 <= beta1, beta2 < 1, eps > 0 (as fp32), step >= 1, counted by
+ * the caller.  grad_scale: DEVICE, one float, or NULL; a value that is not finite makes the whole step
+ * change nothing, so that a norm that overflowed needs no read-back. */
+int a2sgd_adamw_step(a2sgd_adamw *plan, double lr, double beta1, double beta2, double eps, double weight_decay,
+                     uint64_t step, const float *grad_scale, void *stream);
+
+/* The 2-norm of all the plan's gradients together and the factor that clips it:
+ *   norm_and_scale  DEVICE, out, [2] = {norm, min(1, max_norm / norm)}; the factor is NaN when the norm is
+ *                   not finite.  max_norm > 0 and finite. */
+int a2sgd_adamw_grad_norm(a2sgd_adamw *plan, float max_norm, float *norm_and_scale, void *stream);
+
+/* The state as fp32 m and v in the layout above, out of and into the plan's own format (8-bit codes are
+ * rounded to the nearer square; a copy for 32-bit states): for checkpoints, and to change the format.
+ * 32-byte aligned; read_state leaves out what is NULL. */
+int a2sgd_adamw_read_state(a2sgd_adamw *plan, float *m_out, float *v_out, void *stream);
+int a2sgd_adamw_write_state(a2sgd_adamw *plan, const float *m_in, const float *v_in, void *stream);
+
+/* Layer norm over rows of d elements:
+ *     y = (x - mean) * rstd * weight + bias,   rstd = 1 / sqrt(variance + eps)  (variance over d)
+ *   x, y        [rows] rows of `dtype`, stride in ELEMENTS (>= d); y may be x
+ *   weight, bias  [d] of param_dtype (A2SGD_F32, or dtype), or NULL (1 and 0)
+ *   mean, rstd  out, fp32 [rows], for the backward pass; may be NULL
+ * Rows whose bases and strides are multiples of 16 bytes, with d a multiple of 8, take 128-bit accesses. */
+int a2sgd_layer_norm_forward(const void *x, int64_t x_stride, int dtype, const void *weight, const void *bias,
+                             int param_dtype, void *y, int64_t y_stride, float *mean, float *rstd,
+                             uint64_t rows, uint32_t d, double eps, int device, void *stream);
+
+/* Its backward pass.  With xhat = (x - mean) rstd and g = dy weight:
+ *     dx = rstd (g - mean_c(g) - xhat mean_c(g xhat)),  dweight = sum_rows dy xhat,  dbias = sum_rows dy
+ * dx (may be dy or x), dweight, dbias (of param_dtype) may each be NULL; no rows give zero sums.
+ *   workspace   DEVICE, a2sgd_layer_norm_workspace bytes (needed for dweight or dbias) */
+uint64_t a2sgd_layer_norm_workspace(uint64_t rows, uint32_t d, int device);
+int a2sgd_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int dtype,
+                              const void *weight, int param_dtype, const float *mean, const float *rstd,
+                              void *dx, int64_t dx_stride, void *dweight, void *dbias, uint64_t rows, uint32_t d,
+                              void *workspace, uint64_t workspace_bytes, int device, void *stream);
+
 /* Static, never NULL. */
 const char *a2sgd_status_string(int status);
 

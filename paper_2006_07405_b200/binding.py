@@ -109,6 +109,30 @@ def lib() -> ctypes.CDLL:
         l.a2sgd_materialize_err.argtypes = [_vp, _vp, _i64, _vp]
         l.a2sgd_step_segments_lr.restype = ctypes.c_int
         l.a2sgd_step_segments_lr.argtypes = [_vp, _vp, _vp, _vp]
+        _dbl, _u64, _u32, _int = ctypes.c_double, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int
+        l.a2sgd_adamw_state_elements.restype = _u64
+        l.a2sgd_adamw_state_elements.argtypes = [_u32, ctypes.POINTER(_u64)]
+        l.a2sgd_adamw_create.restype = _int
+        l.a2sgd_adamw_create.argtypes = [ctypes.POINTER(_vp), _u32, ctypes.POINTER(_u64), ctypes.POINTER(_vp),
+                                         ctypes.POINTER(_vp), _int, ctypes.POINTER(_vp), _int, _int, _vp, _vp, _vp,
+                                         _vp, _int]
+        l.a2sgd_adamw_destroy.restype = _int
+        l.a2sgd_adamw_destroy.argtypes = [_vp]
+        l.a2sgd_adamw_step.restype = _int
+        l.a2sgd_adamw_step.argtypes = [_vp, _dbl, _dbl, _dbl, _dbl, _dbl, _u64, _vp, _vp]
+        l.a2sgd_adamw_grad_norm.restype = _int
+        l.a2sgd_adamw_grad_norm.argtypes = [_vp, ctypes.c_float, _vp, _vp]
+        for fn in (l.a2sgd_adamw_read_state, l.a2sgd_adamw_write_state):
+            fn.restype = _int
+            fn.argtypes = [_vp, _vp, _vp, _vp]
+        l.a2sgd_layer_norm_forward.restype = _int
+        l.a2sgd_layer_norm_forward.argtypes = [_vp, _i64, _int, _vp, _vp, _int, _vp, _i64, _vp, _vp, _u64, _u32, _dbl,
+                                               _int, _vp]
+        l.a2sgd_layer_norm_workspace.restype = _u64
+        l.a2sgd_layer_norm_workspace.argtypes = [_u64, _u32, _int]
+        l.a2sgd_layer_norm_backward.restype = _int
+        l.a2sgd_layer_norm_backward.argtypes = [_vp, _i64, _vp, _i64, _int, _vp, _int, _vp, _vp, _vp, _i64, _vp, _vp,
+                                                _u64, _u32, _vp, _u64, _int, _vp]
         l.a2sgd_status_string.restype = ctypes.c_char_p
         l.a2sgd_status_string.argtypes = [ctypes.c_int]
         _lib = l
@@ -460,3 +484,212 @@ def a2sgd_launch_info(ctx: Context, shared_w: bool = True) -> dict:
     _check(lib().a2sgd_launch_info(ctx.handle, 0 if shared_w else ctx.n, out), "a2sgd_launch_info")
     return {"encode_ctas": out[0], "decode_ctas": out[1], "threads": out[2], "single_launch": bool(out[3]),
             "sms": out[4]}
+
+
+# ---------------------------------------------------------------------------------------------
+# Training operators (AdamW over a list of tensors, layer norm, gated feed-forward block): see the
+# section of that name in include/a2sgd.h.  Argument checks and marshalling only, as above.
+
+F32, BF16, F16 = 0, 1, 2
+ADAMW_BLOCK = 256
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _dtype_code(t: torch.Tensor, name: str) -> int:
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: need float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _matrix(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.device) -> Tuple[int, int]:
+    """CUDA [rows, columns] with unit inner stride -> (address, row stride in elements)."""
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: need a {dtype} tensor {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    stride, inner = t.stride()
+    if shape[1] > 1 and inner != 1:
+        raise ValueError(f"{name}: need unit inner stride")
+    return t.data_ptr(), stride
+
+
+def _vector(t: Optional[torch.Tensor], name: str, numel: int, dtype, device: torch.device) -> Optional[int]:
+    """A contiguous CUDA tensor of ``numel`` elements (or None) -> address."""
+    if t is None:
+        return None
+    if (dtype is not None and t.dtype != dtype) or t.device != device or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous tensor of {numel} elements of {dtype} on {device}, got {t.dtype} "
+                         f"{list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _stream_on(device: torch.device, stream) -> int:
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return _stream(stream)
+
+
+def _cuda_device(t: torch.Tensor, name: str) -> torch.device:
+    if not t.is_cuda:
+        raise ValueError(f"{name}: need a CUDA tensor")
+    return t.device
+
+
+def a2sgd_adamw_state_elements(params) -> int:
+    """Elements of the m and the v buffer for tensors (or element counts): each tensor starts at a multiple of 256."""
+    numel = [int(p.numel()) if torch.is_tensor(p) else int(p) for p in params]
+    return int(lib().a2sgd_adamw_state_elements(len(numel), (ctypes.c_uint64 * len(numel))(*numel)))
+
+
+class AdamW:
+    """Owns an ``a2sgd_adamw`` plan and keeps the tensors it points at alive."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, w16=None):
+        params, grads = list(params), list(grads)
+        S = len(params)
+        if S == 0 or len(grads) != S or (w16 is not None and len(w16) != S):
+            raise ValueError("params, grads and w16: need lists of the same length, at least 1")
+        self.device = _cuda_device(params[0], "params")
+
+        def table(tensors, name, dtype):
+            for t, p in zip(tensors, params):
+                if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or t.numel() != p.numel():
+                    raise ValueError(f"{name}: need contiguous {dtype} tensors on {self.device}, as long as the parameters")
+            return (_vp * S)(*[t.data_ptr() for t in tensors])
+
+        w_tab = table(params, "params", torch.float32)
+        g_code = _dtype_code(grads[0], "grads")
+        g_tab = table(grads, "grads", grads[0].dtype)
+        w16_tab, w16_code = None, F32
+        if w16 is not None:
+            w16 = list(w16)
+            w16_code = _dtype_code(w16[0], "w16")
+            w16_tab = table(w16, "w16", w16[0].dtype)
+        self.state_elements = n = a2sgd_adamw_state_elements(params)
+        self.state_bits = 32 if m.dtype == torch.float32 else 8
+        m_type, v_type = (torch.float32, torch.float32) if self.state_bits == 32 else (torch.int8, torch.uint8)
+        scales = None if self.state_bits == 32 else n // ADAMW_BLOCK
+        if (scales is None) != (m_scale is None) or (scales is None) != (v_scale is None):
+            raise ValueError("m_scale, v_scale: needed with 8-bit states, and only there")
+        m_ptr = _vector(m, "m", n, m_type, self.device)
+        v_ptr = _vector(v, "v", n, v_type, self.device)
+        ms_ptr = _vector(m_scale, "m_scale", scales, torch.float32, self.device)
+        vs_ptr = _vector(v_scale, "v_scale", scales, torch.float32, self.device)
+        self._keep = (params, grads, m, v, m_scale, v_scale, w16)
+        numel = (ctypes.c_uint64 * S)(*[p.numel() for p in params])
+        self._h = _vp()
+        _check(lib().a2sgd_adamw_create(ctypes.byref(self._h), S, numel, w_tab, g_tab, g_code, w16_tab, w16_code,
+                                        self.state_bits, m_ptr, v_ptr, ms_ptr, vs_ptr, self.device.index),
+               "a2sgd_adamw_create")
+
+    @property
+    def handle(self):
+        if not self._h:
+            raise RuntimeError("AdamW plan destroyed")
+        return self._h
+
+    def destroy(self) -> None:
+        if self._h:
+            lib().a2sgd_adamw_destroy(self._h)
+            self._h = _vp()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def a2sgd_adamw_create(params, grads, m: torch.Tensor, v: torch.Tensor, m_scale: Optional[torch.Tensor] = None,
+                       v_scale: Optional[torch.Tensor] = None, w16=None) -> AdamW:
+    """params: float32 CUDA tensors; grads: as many of one type; w16: 16-bit tensors that receive copies, or None.
+    m, v: flat state of a2sgd_adamw_state_elements(params) elements, float32, or int8 and uint8 with one float32
+    scale for each 256 (m_scale, v_scale); zero them before the first step."""
+    return AdamW(params, grads, m, v, m_scale, v_scale, w16)
+
+
+def a2sgd_adamw_destroy(plan: AdamW) -> None:
+    plan.destroy()
+
+
+def a2sgd_adamw_step(plan: AdamW, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                     weight_decay: float = 0.0, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """grad_scale: float32 CUDA tensor of one element, a factor on every gradient; not finite: nothing changes."""
+    gs = _vector(grad_scale, "grad_scale", 1, torch.float32, plan.device)
+    if step < 1:
+        raise ValueError("step: counted from 1")
+    _check(lib().a2sgd_adamw_step(plan.handle, lr, beta1, beta2, eps, weight_decay, step, gs,
+                                  _stream_on(plan.device, stream)), "a2sgd_adamw_step")
+
+
+def a2sgd_adamw_grad_norm(plan: AdamW, max_norm: float, norm_and_scale: torch.Tensor, stream=None) -> None:
+    """norm_and_scale: float32 CUDA [2], out: the norm of all gradients, and min(1, max_norm / norm)."""
+    out = _vector(norm_and_scale, "norm_and_scale", 2, torch.float32, plan.device)
+    _check(lib().a2sgd_adamw_grad_norm(plan.handle, max_norm, out, _stream_on(plan.device, stream)),
+           "a2sgd_adamw_grad_norm")
+
+
+def a2sgd_adamw_read_state(plan: AdamW, m_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], stream=None) -> None:
+    """m_out, v_out: float32 CUDA tensors of plan.state_elements (either may be None)."""
+    _check(lib().a2sgd_adamw_read_state(plan.handle, _vector(m_out, "m_out", plan.state_elements, torch.float32, plan.device),
+                                        _vector(v_out, "v_out", plan.state_elements, torch.float32, plan.device),
+                                        _stream_on(plan.device, stream)), "a2sgd_adamw_read_state")
+
+
+def a2sgd_adamw_write_state(plan: AdamW, m_in: torch.Tensor, v_in: torch.Tensor, stream=None) -> None:
+    _check(lib().a2sgd_adamw_write_state(plan.handle, _vector(m_in, "m_in", plan.state_elements, torch.float32, plan.device),
+                                         _vector(v_in, "v_in", plan.state_elements, torch.float32, plan.device),
+                                         _stream_on(plan.device, stream)), "a2sgd_adamw_write_state")
+
+
+def _param_dtype(x: torch.Tensor, *vectors) -> torch.dtype:
+    for v in vectors:
+        if v is not None:
+            return v.dtype
+    return x.dtype
+
+
+def a2sgd_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor],
+                             y: torch.Tensor, mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor],
+                             eps: float = 1e-5, stream=None) -> None:
+    """x, y: CUDA [rows, d], unit inner stride (y may be x); weight, bias: [d] of float32 or x's type, or None;
+    mean, rstd: float32 [rows], out, or None."""
+    dev, code = _cuda_device(x, "x"), _dtype_code(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: need [rows, d]")
+    shape = rows, d = tuple(x.shape)
+    pt = _param_dtype(x, weight, bias)
+    xp, xs = _matrix(x, "x", shape, x.dtype, dev)
+    yp, ys = _matrix(y, "y", shape, x.dtype, dev)
+    _check(lib().a2sgd_layer_norm_forward(
+        xp, xs, code, _vector(weight, "weight", d, pt, dev), _vector(bias, "bias", d, pt, dev),
+        _DTYPE_CODES.get(pt, -1), yp, ys, _vector(mean, "mean", rows, torch.float32, dev),
+        _vector(rstd, "rstd", rows, torch.float32, dev), rows, d, eps, dev.index, _stream_on(dev, stream)),
+        "a2sgd_layer_norm_forward")
+
+
+def a2sgd_layer_norm_workspace(rows: int, d: int, device: Optional[int] = None) -> int:
+    """Bytes of workspace of a2sgd_layer_norm_backward."""
+    device = torch.cuda.current_device() if device is None else int(device)
+    return int(lib().a2sgd_layer_norm_workspace(int(rows), int(d), device))
+
+
+def a2sgd_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                              rstd: torch.Tensor, dx: Optional[torch.Tensor], dweight: Optional[torch.Tensor],
+                              dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx (may be dy or x), dweight, dbias: out, each may be None; workspace: uint8 CUDA tensor of
+    a2sgd_layer_norm_workspace bytes, needed for dweight or dbias."""
+    dev, code = _cuda_device(x, "x"), _dtype_code(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: need [rows, d]")
+    shape = rows, d = tuple(x.shape)
+    pt = _param_dtype(x, weight, dweight, dbias)
+    xp, xs = _matrix(x, "x", shape, x.dtype, dev)
+    gp, gs = _matrix(dy, "dy", shape, x.dtype, dev)
+    op, os_ = (None, 0) if dx is None else _matrix(dx, "dx", shape, x.dtype, dev)
+    wb = 0 if workspace is None else workspace.numel()
+    _check(lib().a2sgd_layer_norm_backward(
+        gp, gs, xp, xs, code, _vector(weight, "weight", d, pt, dev), _DTYPE_CODES.get(pt, -1),
+        _vector(mean, "mean", rows, torch.float32, dev), _vector(rstd, "rstd", rows, torch.float32, dev), op, os_,
+        _vector(dweight, "dweight", d, pt, dev), _vector(dbias, "dbias", d, pt, dev), rows, d,
+        _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev.index, _stream_on(dev, stream)),
+        "a2sgd_layer_norm_backward")

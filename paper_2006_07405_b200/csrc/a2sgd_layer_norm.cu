@@ -1,0 +1,640 @@
+// Layer norm, forward and backward, with the gradients of its weight and bias.
+//
+//   forward   mean = sum_c x / d,  rstd = 1 / sqrt(sum_c (x - mean)^2 / d + eps),  y = (x - mean) rstd w + b
+//   backward  xhat = (x - mean) rstd,  g = dy w,
+//             dx = rstd (g - sum_c g / d - xhat sum_c (g xhat) / d),
+//             dw = sum_rows dy xhat,  db = sum_rows dy
+//
+// Bound by HBM: x once and y once forward, x and dy once and dx once backward.  A group of TPR
+// threads owns the columns of a row, each thread the same columns of every row it meets, so that the
+// weight and the bias, and backward the two column sums, stay in its registers over all rows.  R rows
+// are in flight together: their loads are issued before any is used, and the threads of a group meet
+// at one barrier for the R rows' sums.  The squared deviations are summed in a second reduction over
+// the registers, not from a sum of squares, which cancels when the mean is large against the spread.
+// All sums are fp32 within a thread's few values and trees above; every order is fixed.
+//
+// Rows too long for registers (over kMostCols) take k_ln_*_long, which walk the row again instead.
+#include "a2sgd_train.cuh"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+using namespace a2sgd_train;
+
+namespace {
+
+constexpr int kMaxThreads = 1024;                       // of the long forms and the fold
+constexpr int kRowThreads = 512;                        // of the register forms: 128 registers each
+constexpr uint32_t kMostCols = kRowThreads * 16;        // 8192: at most 16 columns a thread
+constexpr uint32_t kFoldCols = 32;                   // columns of one CTA of the fold
+
+struct LnArgs {
+    const void *x, *dy, *w, *b;
+    void *y; // forward: y; backward: dx
+    float *mean, *rstd;
+    int64_t x_stride, dy_stride, y_stride;
+    uint64_t rows;
+    uint32_t d;
+    uint32_t tpr;    // threads of a row
+    uint32_t groups; // rows at a time / R
+    float inv_d, eps;
+    float *partials; // backward: [grid][2][d]
+    void *dw, *db;
+    uint32_t parts;
+};
+
+// N sums over the threads of a group, the same in each of them.  A group of up to 32 threads (a power
+// of two) is part of a warp; a larger one is a whole number of warps and takes one barrier of the CTA.
+// Two buffers in turn: a warp that runs ahead writes the other one, and meets the barrier before it
+// comes back to the first.
+template <int N>
+struct GroupSum {
+    float *sh; // [2][groups][warps of a group][N]
+    uint32_t tpr, warps, in_group, group;
+    int turn = 0;
+    __device__ __forceinline__ void operator()(float (&v)[N])
+    {
+        const uint32_t width = tpr < 32 ? tpr : 32;
+        for (uint32_t o = width / 2; o; o >>= 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        }
+        if (tpr <= 32) return;
+        float *slot = sh + (uint32_t)turn * (kMaxThreads / 32) * N + group * warps * N;
+        turn ^= 1;
+        if ((in_group & 31) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) slot[(in_group >> 5) * N + i] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.0f;
+        for (uint32_t k = 0; k < warps; ++k) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += slot[k * N + i];
+        }
+    }
+};
+
+// A thread's NC columns of one row.  VEC: eight consecutive ones at a time (column c0 = (k tpr + t) 8);
+// else every tpr-th one.
+template <typename T, int NC, bool VEC>
+struct RowPart {
+    Raw8<T> raw[VEC ? NC / 8 : 1];
+    T one[VEC ? 1 : NC];
+    __device__ __forceinline__ void load(const T *row, uint32_t d, uint32_t t, uint32_t tpr, bool live)
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int k = 0; k < NC / 8; ++k) {
+                const uint32_t c = (k * tpr + t) * 8;
+                if (live && c < d) raw[k].load(row + c);
+                else raw[k].zero();
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                const uint32_t c = k * tpr + t;
+                one[k] = live && c < d ? row[c] : from_f32<T>(0.0f);
+            }
+        }
+    }
+    __device__ __forceinline__ void unpack(float (&f)[NC]) const
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int k = 0; k < NC / 8; ++k) {
+                float e[8];
+                raw[k].unpack(e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[k * 8 + i] = e[i];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NC; ++k) f[k] = to_f32(one[k]);
+        }
+    }
+};
+
+template <int NC, bool VEC>
+__device__ __forceinline__ uint32_t column(int i, uint32_t t, uint32_t tpr)
+{
+    return VEC ? ((i / 8) * tpr + t) * 8 + (i & 7) : i * tpr + t;
+}
+
+template <typename T, int NC, bool VEC>
+__device__ __forceinline__ void store_part(T *row, uint32_t d, uint32_t t, uint32_t tpr, const float (&f)[NC])
+{
+    if constexpr (VEC) {
+#pragma unroll
+        for (int k = 0; k < NC / 8; ++k) {
+            const uint32_t c = (k * tpr + t) * 8;
+            if (c < d) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = f[k * 8 + i];
+                store8(row + c, e);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            const uint32_t c = k * tpr + t;
+            if (c < d) row[c] = from_f32<T>(f[k]);
+        }
+    }
+}
+
+template <typename T, typename W, int NC, int R, bool VEC>
+__global__ void __launch_bounds__(kRowThreads) k_ln_forward(const __grid_constant__ LnArgs a)
+{
+    extern __shared__ float sh[];
+    const uint32_t group = threadIdx.x / a.tpr, t = threadIdx.x - group * a.tpr;
+    GroupSum<R> sum{sh, a.tpr, a.tpr >> 5, t, group};
+    wait_prior_grid();
+    release_next_grid();
+    float w[NC], b[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const uint32_t c = column<NC, VEC>(i, t, a.tpr);
+        w[i] = c < a.d && a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
+        b[i] = c < a.d && a.b ? to_f32(static_cast<const W *>(a.b)[c]) : 0.0f;
+    }
+    const uint64_t at_once = (uint64_t)a.groups * R;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * at_once; r0 < a.rows; r0 += (uint64_t)gridDim.x * at_once) {
+        const uint64_t row = r0 + (uint64_t)group * R;
+        RowPart<T, NC, VEC> part[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            part[r].load(static_cast<const T *>(a.x) + (int64_t)(row + r) * a.x_stride, a.d, t, a.tpr, row + r < a.rows);
+        float mean[R], var[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float f[NC];
+            part[r].unpack(f);
+            mean[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) mean[r] += f[i];
+        }
+        sum(mean);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] *= a.inv_d;
+            float f[NC];
+            part[r].unpack(f);
+            var[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const float c = column<NC, VEC>(i, t, a.tpr) < a.d ? f[i] - mean[r] : 0.0f;
+                var[r] = fmaf(c, c, var[r]);
+            }
+        }
+        sum(var);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (row + r >= a.rows) break;
+            const float rstd = 1.0f / sqrtf(fmaf(var[r], a.inv_d, a.eps));
+            float f[NC];
+            part[r].unpack(f);
+#pragma unroll
+            for (int i = 0; i < NC; ++i) f[i] = fmaf((f[i] - mean[r]) * rstd, w[i], b[i]);
+            store_part<T, NC, VEC>(static_cast<T *>(a.y) + (int64_t)(row + r) * a.y_stride, a.d, t, a.tpr, f);
+            if (t == 0) {
+                if (a.mean) a.mean[row + r] = mean[r];
+                if (a.rstd) a.rstd[row + r] = rstd;
+            }
+        }
+    }
+}
+
+template <typename T, typename W, int NC, int R, bool VEC>
+__global__ void __launch_bounds__(kRowThreads) k_ln_backward(const __grid_constant__ LnArgs a)
+{
+    extern __shared__ float sh[];
+    const uint32_t group = threadIdx.x / a.tpr, t = threadIdx.x - group * a.tpr;
+    GroupSum<2 * R> sum{sh, a.tpr, a.tpr >> 5, t, group};
+    wait_prior_grid();
+    release_next_grid();
+    float w[NC], dw[NC], db[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const uint32_t c = column<NC, VEC>(i, t, a.tpr);
+        w[i] = c < a.d && a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
+        dw[i] = db[i] = 0.0f;
+    }
+    const uint64_t at_once = (uint64_t)a.groups * R;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * at_once; r0 < a.rows; r0 += (uint64_t)gridDim.x * at_once) {
+        const uint64_t row = r0 + (uint64_t)group * R;
+        RowPart<T, NC, VEC> px[R], pg[R];
+        float mean[R], rstd[R], s[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool live = row + r < a.rows;
+            px[r].load(static_cast<const T *>(a.x) + (int64_t)(row + r) * a.x_stride, a.d, t, a.tpr, live);
+            pg[r].load(static_cast<const T *>(a.dy) + (int64_t)(row + r) * a.dy_stride, a.d, t, a.tpr, live);
+            mean[r] = live ? __ldcg(a.mean + row + r) : 0.0f;
+            rstd[r] = live ? __ldcg(a.rstd + row + r) : 0.0f;
+        }
+        // columns past d and rows past the end hold dy = 0 and drop out of all four sums
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x[NC], g[NC];
+            px[r].unpack(x);
+            pg[r].unpack(g);
+            s[2 * r] = s[2 * r + 1] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const float xhat = (x[i] - mean[r]) * rstd[r];
+                db[i] += g[i];
+                dw[i] = fmaf(g[i], xhat, dw[i]);
+                const float u = g[i] * w[i];
+                s[2 * r] += u;
+                s[2 * r + 1] = fmaf(u, xhat, s[2 * r + 1]);
+            }
+        }
+        sum(s);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (row + r >= a.rows) break;
+            const float c1 = s[2 * r] * a.inv_d, c2 = s[2 * r + 1] * a.inv_d;
+            float x[NC], g[NC];
+            px[r].unpack(x);
+            pg[r].unpack(g);
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const float xhat = (x[i] - mean[r]) * rstd[r];
+                g[i] = rstd[r] * (fmaf(g[i], w[i], -c1) - xhat * c2);
+            }
+            if (a.y) store_part<T, NC, VEC>(static_cast<T *>(a.y) + (int64_t)(row + r) * a.y_stride, a.d, t, a.tpr, g);
+        }
+    }
+    if (!a.partials) return;
+    // the groups' column sums, in order, through shared memory: [groups][2][d]
+    if (a.groups > 1) {
+        __syncthreads();
+        float *mine = sh + (size_t)group * 2 * a.d;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const uint32_t c = column<NC, VEC>(i, t, a.tpr);
+            if (c < a.d) {
+                mine[c] = dw[i];
+                mine[a.d + c] = db[i];
+            }
+        }
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
+            float v = 0.0f;
+            for (uint32_t g = 0; g < a.groups; ++g) v += sh[(size_t)g * 2 * a.d + c];
+            a.partials[(size_t)blockIdx.x * 2 * a.d + c] = v;
+        }
+        return;
+    }
+    float *out = a.partials + (size_t)blockIdx.x * 2 * a.d;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const uint32_t c = column<NC, VEC>(i, t, a.tpr);
+        if (c < a.d) {
+            out[c] = dw[i];
+            out[a.d + c] = db[i];
+        }
+    }
+}
+
+// The CTAs' column sums, added up in order: 32 columns a CTA, 32 slices of the CTAs side by side.
+template <typename W>
+__global__ void __launch_bounds__(kMaxThreads) k_ln_fold(const __grid_constant__ LnArgs a)
+{
+    __shared__ float sh[kMaxThreads / kFoldCols][kFoldCols + 1];
+    wait_prior_grid();
+    release_next_grid();
+    const uint32_t lane = threadIdx.x % kFoldCols, slice = threadIdx.x / kFoldCols;
+    const uint32_t c = blockIdx.x * kFoldCols + lane; // of the 2 d columns dw | db
+    float v = 0.0f;
+    if (c < 2 * a.d) {
+        for (uint32_t p = slice; p < a.parts; p += kMaxThreads / kFoldCols) v += __ldcg(a.partials + (size_t)p * 2 * a.d + c);
+    }
+    sh[slice][lane] = v;
+    __syncthreads();
+    if (slice == 0 && c < 2 * a.d) {
+        v = 0.0f;
+        for (uint32_t k = 0; k < kMaxThreads / kFoldCols; ++k) v += sh[k][lane];
+        W *out = static_cast<W *>(c < a.d ? a.dw : a.db);
+        if (out) out[c < a.d ? c : c - a.d] = from_f32<W>(v);
+    }
+}
+
+// ------------------------------------------------------------------ rows of any length
+__device__ __forceinline__ float block_sum(float v, float *sh)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads(); // the last sum has been read
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0f;
+    for (uint32_t k = 0; k < blockDim.x / 32; ++k) v += sh[k];
+    return v;
+}
+
+template <typename T, typename W>
+__global__ void __launch_bounds__(kMaxThreads) k_ln_forward_long(const __grid_constant__ LnArgs a)
+{
+    __shared__ float sh[kMaxThreads / 32];
+    wait_prior_grid();
+    release_next_grid();
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.x_stride;
+        T *y = static_cast<T *>(a.y) + (int64_t)row * a.y_stride;
+        float v = 0.0f;
+        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) v += to_f32(x[c]);
+        const float mean = block_sum(v, sh) * a.inv_d;
+        v = 0.0f;
+        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+            const float e = to_f32(x[c]) - mean;
+            v = fmaf(e, e, v);
+        }
+        const float rstd = 1.0f / sqrtf(fmaf(block_sum(v, sh), a.inv_d, a.eps));
+        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+            const float w = a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
+            const float b = a.b ? to_f32(static_cast<const W *>(a.b)[c]) : 0.0f;
+            y[c] = from_f32<T>(fmaf((to_f32(x[c]) - mean) * rstd, w, b));
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+// Column sums of a slice of the rows: one thread a column.
+template <typename T>
+__global__ void __launch_bounds__(256) k_ln_columns_long(const __grid_constant__ LnArgs a)
+{
+    wait_prior_grid();
+    release_next_grid();
+    const uint32_t c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.d) return;
+    float dw = 0.0f, db = 0.0f;
+    for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float g = to_f32((static_cast<const T *>(a.dy) + (int64_t)row * a.dy_stride)[c]);
+        const float x = to_f32((static_cast<const T *>(a.x) + (int64_t)row * a.x_stride)[c]);
+        db += g;
+        dw = fmaf(g, (x - a.mean[row]) * a.rstd[row], dw);
+    }
+    a.partials[(size_t)blockIdx.y * 2 * a.d + c] = dw;
+    a.partials[(size_t)blockIdx.y * 2 * a.d + a.d + c] = db;
+}
+
+template <typename T, typename W>
+__global__ void __launch_bounds__(kMaxThreads) k_ln_backward_long(const __grid_constant__ LnArgs a)
+{
+    __shared__ float sh[kMaxThreads / 32];
+    wait_prior_grid();
+    release_next_grid();
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.x_stride;
+        const T *dy = static_cast<const T *>(a.dy) + (int64_t)row * a.dy_stride;
+        T *dx = static_cast<T *>(a.y) + (int64_t)row * a.y_stride;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+            const float u = to_f32(dy[c]) * (a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f);
+            s1 += u;
+            s2 = fmaf(u, (to_f32(x[c]) - mean) * rstd, s2);
+        }
+        const float c1 = block_sum(s1, sh) * a.inv_d, c2 = block_sum(s2, sh) * a.inv_d;
+        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+            const float w = a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
+            const float xhat = (to_f32(x[c]) - mean) * rstd;
+            dx[c] = from_f32<T>(rstd * (fmaf(to_f32(dy[c]), w, -c1) - xhat * c2));
+        }
+    }
+}
+
+// ------------------------------------------------------------------ host
+struct Plan {
+    const void *fn = nullptr;
+    bool long_row = false;
+    uint32_t tpr = 0, groups = 0;
+    int nc = 0, r = 0;
+    unsigned threads = 0, grid = 0;
+    size_t smem = 0;
+};
+
+template <typename T, typename W, bool BWD>
+const void *pick(int nc, int r, bool vec)
+{
+#define A2_LN(NC, R, V)                                                                       \
+    if (nc == NC && r == R && vec == V)                                                       \
+        return BWD ? reinterpret_cast<const void *>(&k_ln_backward<T, W, NC, R, V>)           \
+                   : reinterpret_cast<const void *>(&k_ln_forward<T, W, NC, R, V>);
+    A2_LN(8, 1, true)
+    A2_LN(8, 4, true)
+    A2_LN(16, 1, true)
+    A2_LN(8, 1, false)
+    A2_LN(8, 4, false)
+    A2_LN(16, 1, false)
+#undef A2_LN
+    return nullptr;
+}
+
+template <bool BWD>
+const void *pick_types(int dtype, int param, int nc, int r, bool vec)
+{
+    if (dtype == A2SGD_F32) return pick<float, float, BWD>(nc, r, vec);
+    if (dtype == A2SGD_BF16)
+        return param == A2SGD_F32 ? pick<__nv_bfloat16, float, BWD>(nc, r, vec)
+                                  : pick<__nv_bfloat16, __nv_bfloat16, BWD>(nc, r, vec);
+    return param == A2SGD_F32 ? pick<__half, float, BWD>(nc, r, vec) : pick<__half, __half, BWD>(nc, r, vec);
+}
+
+#define A2_LN_LONG(name)                                                                                         \
+    const void *name##_of(int dtype, int param)                                                                  \
+    {                                                                                                            \
+        if (dtype == A2SGD_F32) return reinterpret_cast<const void *>(&name<float, float>);                      \
+        if (dtype == A2SGD_BF16)                                                                                 \
+            return param == A2SGD_F32 ? reinterpret_cast<const void *>(&name<__nv_bfloat16, float>)              \
+                                      : reinterpret_cast<const void *>(&name<__nv_bfloat16, __nv_bfloat16>);     \
+        return param == A2SGD_F32 ? reinterpret_cast<const void *>(&name<__half, float>)                         \
+                                  : reinterpret_cast<const void *>(&name<__half, __half>);                       \
+    }
+A2_LN_LONG(k_ln_forward_long)
+A2_LN_LONG(k_ln_backward_long)
+#undef A2_LN_LONG
+
+// Column slices of the long form's column sums.
+inline uint32_t long_parts(uint64_t rows) { return (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, rows / 16)); }
+
+constexpr int kCtasPerSm = 4; // at most: the partial sums of the backward pass are sized by it
+
+Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int dtype, int param)
+{
+    Plan p;
+    if (d > kMostCols) {
+        p.long_row = true;
+        p.threads = kMaxThreads;
+        p.grid = (unsigned)std::min<uint64_t>(rows, (uint64_t)sms * 2);
+        p.fn = backward ? k_ln_backward_long_of(dtype, param) : k_ln_forward_long_of(dtype, param);
+        return p;
+    }
+    p.nc = d <= (uint32_t)kRowThreads * 8 ? 8 : 16;
+    const uint32_t need = (d + p.nc - 1) / p.nc; // threads that have columns
+    if (need <= 32) {
+        p.tpr = 1;
+        while (p.tpr < need) p.tpr *= 2;
+    } else {
+        p.tpr = (need + 31) / 32 * 32;
+    }
+    // short rows share a CTA of up to 256 threads
+    p.groups = p.tpr <= 128 ? 256 / p.tpr : 1;
+    p.groups = std::max(1u, std::min<uint32_t>(p.groups, 64));
+    if ((uint64_t)p.groups > rows) p.groups = (uint32_t)std::max<uint64_t>(1, rows);
+    // whole warps
+    while (p.tpr * p.groups % 32) ++p.groups;
+    p.threads = p.tpr * p.groups;
+    // four rows in flight where there are rows enough to keep every SM busy with them
+    p.r = p.nc == 8 && rows >= (uint64_t)sms * p.groups * 8 ? 4 : 1;
+    const size_t sums = sizeof(float) * 2 * (kMaxThreads / 32) * (backward ? 2 : 1) * p.r;
+    p.smem = std::max(sums, backward && p.groups > 1 ? sizeof(float) * 2 * d * p.groups : (size_t)0);
+    p.fn = backward ? pick_types<true>(dtype, param, p.nc, p.r, vec) : pick_types<false>(dtype, param, p.nc, p.r, vec);
+    // every CTA resident at once: the rows are dealt out evenly
+    const uint64_t trips = (rows + (uint64_t)p.groups * p.r - 1) / ((uint64_t)p.groups * p.r);
+    const uint64_t slots = (uint64_t)sms * std::min(kCtasPerSm, resident_ctas(p.fn, p.threads, p.smem));
+    p.grid = (unsigned)std::min<uint64_t>(trips, slots);
+    return p;
+}
+
+int check(const void *x, int64_t x_stride, int dtype, int param, uint64_t rows, uint32_t d)
+{
+    if (!known(dtype) || (param != A2SGD_F32 && param != dtype) || d == 0 || d >= (1u << 30) || rows >= (1ull << 40))
+        return A2SGD_ERR_ARG;
+    if (rows == 0) return A2SGD_OK;
+    if (!x || (rows > 1 && x_stride < (int64_t)d)) return A2SGD_ERR_ARG;
+    return aligned(x, size_of(dtype)) ? A2SGD_OK : A2SGD_ERR_ALIGN;
+}
+
+inline bool rows_vector(const void *p, int64_t stride, uint64_t rows, int dtype)
+{
+    return aligned(p, 16) && (rows <= 1 || (size_t)stride * size_of(dtype) % 16 == 0);
+}
+
+int run(const Plan &p, LnArgs &a, cudaStream_t s)
+{
+    void *params[] = {&a};
+    A2_TRAIN_CUDA(launch(p.fn, dim3(p.grid), p.threads, p.smem, params, s));
+    return A2SGD_OK;
+}
+
+} // namespace
+
+extern "C" int a2sgd_layer_norm_forward(const void *x, int64_t x_stride, int dtype, const void *weight, const void *bias,
+                                        int param_dtype, void *y, int64_t y_stride, float *mean, float *rstd,
+                                        uint64_t rows, uint32_t d, double eps, int device, void *stream)
+{
+    int rc = check(x, x_stride, dtype, param_dtype, rows, d);
+    if (rc == A2SGD_OK && rows) rc = check(y, y_stride, dtype, param_dtype, rows, d);
+    if (rc != A2SGD_OK) return rc;
+    if (!std::isfinite(eps) || !(eps >= 0.0)) return A2SGD_ERR_ARG;
+    if (!aligned(weight, size_of(param_dtype)) || !aligned(bias, size_of(param_dtype)) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return A2SGD_ERR_ALIGN;
+    if (rows == 0) return A2SGD_OK;
+    DeviceGuard guard(device);
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms == 0) return A2SGD_ERR_CUDA;
+    const bool vec = d % 8 == 0 && rows_vector(x, x_stride, rows, dtype) && rows_vector(y, y_stride, rows, dtype);
+    const Plan p = make_plan(rows, d, vec, false, sms, dtype, param_dtype);
+    LnArgs a{};
+    a.x = x;
+    a.w = weight;
+    a.b = bias;
+    a.y = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.x_stride = x_stride;
+    a.y_stride = y_stride;
+    a.rows = rows;
+    a.d = d;
+    a.tpr = p.tpr;
+    a.groups = p.groups;
+    a.inv_d = 1.0f / (float)d;
+    a.eps = (float)eps;
+    return run(p, a, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" uint64_t a2sgd_layer_norm_workspace(uint64_t rows, uint32_t d, int device)
+{
+    (void)rows;
+    const int sms = sm_count(device);
+    // the partial sums of dw and db: one pair of rows a CTA (or a slice, for long rows)
+    return sizeof(float) * 2 * (uint64_t)d * (uint64_t)(d > kMostCols ? 64 : std::max(1, sms) * kCtasPerSm);
+}
+
+extern "C" int a2sgd_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int dtype,
+                                         const void *weight, int param_dtype, const float *mean, const float *rstd,
+                                         void *dx, int64_t dx_stride, void *dweight, void *dbias, uint64_t rows, uint32_t d,
+                                         void *workspace, uint64_t workspace_bytes, int device, void *stream)
+{
+    int rc = check(x, x_stride, dtype, param_dtype, rows, d);
+    if (rc == A2SGD_OK && rows) rc = check(dy, dy_stride, dtype, param_dtype, rows, d);
+    if (rc == A2SGD_OK && rows && dx) rc = check(dx, dx_stride, dtype, param_dtype, rows, d);
+    if (rc != A2SGD_OK) return rc;
+    if (rows && (!mean || !rstd)) return A2SGD_ERR_ARG;
+    const size_t pe = size_of(param_dtype);
+    if (!aligned(weight, pe) || !aligned(dweight, pe) || !aligned(dbias, pe) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+        !aligned(workspace, 4))
+        return A2SGD_ERR_ALIGN;
+    DeviceGuard guard(device);
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms == 0) return A2SGD_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rows == 0) { // no rows: the sums are zero
+        if (dweight) A2_TRAIN_CUDA(cudaMemsetAsync(dweight, 0, pe * d, s));
+        if (dbias) A2_TRAIN_CUDA(cudaMemsetAsync(dbias, 0, pe * d, s));
+        return A2SGD_OK;
+    }
+    const bool columns = dweight || dbias;
+    if (!columns && !dx) return A2SGD_OK;
+    const bool vec = d % 8 == 0 && rows_vector(x, x_stride, rows, dtype) && rows_vector(dy, dy_stride, rows, dtype) &&
+                     (!dx || rows_vector(dx, dx_stride, rows, dtype));
+    const Plan p = make_plan(rows, d, vec, true, sms, dtype, param_dtype);
+    LnArgs a{};
+    a.x = x;
+    a.dy = dy;
+    a.w = weight;
+    a.y = dx;
+    a.mean = const_cast<float *>(mean);
+    a.rstd = const_cast<float *>(rstd);
+    a.x_stride = x_stride;
+    a.dy_stride = dy_stride;
+    a.y_stride = dx_stride;
+    a.rows = rows;
+    a.d = d;
+    a.tpr = p.tpr;
+    a.groups = p.groups;
+    a.inv_d = 1.0f / (float)d;
+    a.dw = dweight;
+    a.db = dbias;
+    a.parts = p.long_row ? long_parts(rows) : p.grid;
+    a.partials = columns ? static_cast<float *>(workspace) : nullptr;
+    if (columns && (!workspace || workspace_bytes < sizeof(float) * 2 * (uint64_t)d * a.parts)) return A2SGD_ERR_ARG;
+    if (p.long_row) {
+        if (columns) { // before dx, which may take the place of x or dy
+            const void *fn = dtype == A2SGD_F32    ? reinterpret_cast<const void *>(&k_ln_columns_long<float>)
+                             : dtype == A2SGD_BF16 ? reinterpret_cast<const void *>(&k_ln_columns_long<__nv_bfloat16>)
+                                                   : reinterpret_cast<const void *>(&k_ln_columns_long<__half>);
+            void *params[] = {&a};
+            A2_TRAIN_CUDA(launch(fn, dim3((d + 255) / 256, a.parts), 256, 0, params, s));
+        }
+        if (dx) rc = run(p, a, s);
+    } else {
+        rc = run(p, a, s);
+    }
+    if (rc != A2SGD_OK || !columns) return rc;
+    const void *fold = param_dtype == A2SGD_F32    ? reinterpret_cast<const void *>(&k_ln_fold<float>)
+                       : param_dtype == A2SGD_BF16 ? reinterpret_cast<const void *>(&k_ln_fold<__nv_bfloat16>)
+                                                   : reinterpret_cast<const void *>(&k_ln_fold<__half>);
+    void *params[] = {&a};
+    A2_TRAIN_CUDA(launch(fold, dim3((2 * d + kFoldCols - 1) / kFoldCols), kMaxThreads, 0, params, s));
+    return A2SGD_OK;
+}

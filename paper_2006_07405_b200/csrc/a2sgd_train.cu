@@ -1,0 +1,50 @@
+// Host helpers of the training operators.
+#include "a2sgd_train.cuh"
+
+#include <map>
+#include <mutex>
+#include <tuple>
+
+namespace a2sgd_train {
+
+int sm_count(int device)
+{
+    static std::mutex lock;
+    static std::map<int, int> known_counts;
+    std::lock_guard<std::mutex> hold(lock);
+    auto it = known_counts.find(device);
+    if (it != known_counts.end()) return it->second;
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    try {
+        known_counts[device] = n;
+    } catch (...) { // no memory for the note: ask again next time
+    }
+    return n;
+}
+
+int resident_ctas(const void *fn, unsigned threads, size_t smem)
+{
+    static std::mutex lock;
+    static std::map<std::tuple<const void *, unsigned, size_t>, int> known_counts;
+    std::lock_guard<std::mutex> hold(lock);
+    const auto key = std::make_tuple(fn, threads, smem);
+    auto it = known_counts.find(key);
+    if (it != known_counts.end()) return it->second;
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, (int)threads, smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 1;
+    }
+    n = n > 0 ? n : 1;
+    try {
+        known_counts[key] = n;
+    } catch (...) { // as above
+    }
+    return n;
+}
+
+} // namespace a2sgd_train
