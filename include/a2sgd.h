@@ -454,6 +454,49 @@ int a2sgd_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, 
                               void *dx, int64_t dx_stride, void *dweight, void *dbias, uint64_t rows, uint32_t d,
                               void *workspace, uint64_t workspace_bytes, int device, void *stream);
 
+/* The gated feed-forward block (both projections, the activation, their product and the projection back):
+ *     a = x w_gate^T,   b = x w_up^T,   hidden = act(a) b,   y = hidden w_down^T
+ *   x, y      [tokens, d];  w_gate, w_up [f, d];  w_down [d, f];  hidden, gate (a), up (b) [tokens, f]
+ * All of one 16-bit type, rows with unit inner stride and their own row stride in ELEMENTS (>= the row's
+ * length).  Products are accumulated in fp32 on the tensor cores; a and b meet in fp32, hidden is rounded once
+ * and then read by the last product.  hidden is always written; gate and up, for the backward pass,
+ * when both are given.  Matrices whose address is a multiple of 16 bytes and whose row stride is a multiple
+ * of 8 elements are read where they are; others are first copied to padded rows in the workspace.
+ *   activation  A2SGD_ACT_SILU: a / (1 + exp(-a));  A2SGD_ACT_GELU_TANH: a (1 + tanh(k (a + 0.044715 a^3))) / 2,
+ *               k = sqrt(2 / pi)
+ *   workspace   DEVICE, 256-byte aligned, a2sgd_gated_ffn_workspace bytes: flags A2SGD_FFN_BACKWARD for the
+ *               backward pass, A2SGD_FFN_ALIGNED when every matrix that is read (and hidden) is laid out as above
+ * y and the other outputs must not overlap an input. */
+enum a2sgd_activation { A2SGD_ACT_SILU = 0, A2SGD_ACT_GELU_TANH = 1 };
+#define A2SGD_FFN_BACKWARD 1u
+#define A2SGD_FFN_ALIGNED 2u
+uint64_t a2sgd_gated_ffn_workspace(uint64_t tokens, uint32_t d, uint32_t f, uint32_t flags);
+int a2sgd_gated_ffn_forward(const void *x, int64_t x_stride, const void *w_gate, int64_t w_gate_stride,
+                            const void *w_up, int64_t w_up_stride, const void *w_down, int64_t w_down_stride,
+                            void *y, int64_t y_stride, void *hidden, int64_t hidden_stride, void *gate,
+                            int64_t gate_stride, void *up, int64_t up_stride, int dtype, int activation,
+                            uint64_t tokens, uint32_t d, uint32_t f, void *workspace, uint64_t workspace_bytes,
+                            int device, void *stream);
+
+/* Its backward pass, from dy [tokens, d] and what the forward pass left (hidden, gate, up):
+ *     dh = dy w_down,   da = dh b act'(a),   db = dh act(a)      (da, db rounded once, in the workspace)
+ *     dx = da w_gate + db w_up,   dw_gate = da^T x,   dw_up = db^T x,   dw_down = dy^T hidden
+ * dx [tokens, d], dw_gate, dw_up [f, d], dw_down [d, f]: each may be NULL, and what only it needs is then not
+ * computed.  No tokens give zero weight gradients. */
+int a2sgd_gated_ffn_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *w_gate,
+                             int64_t w_gate_stride, const void *w_up, int64_t w_up_stride, const void *w_down,
+                             int64_t w_down_stride, const void *hidden, int64_t hidden_stride, const void *gate,
+                             int64_t gate_stride, const void *up, int64_t up_stride, void *dx, int64_t dx_stride,
+                             void *dw_gate, int64_t dw_gate_stride, void *dw_up, int64_t dw_up_stride,
+                             void *dw_down, int64_t dw_down_stride, int dtype, int activation, uint64_t tokens,
+                             uint32_t d, uint32_t f, void *workspace, uint64_t workspace_bytes, int device,
+                             void *stream);
+
+/* Synchronises `stream` and returns the status that the block's kernels latched on the device
+ * (A2SGD_OK, or A2SGD_ERR_TIMEOUT: a bounded wait inside a kernel ran out and that call's outputs are undefined),
+ * clearing it. */
+int a2sgd_gated_ffn_status(int device, int *device_status, void *stream);
+
 /* Static, never NULL. */
 const char *a2sgd_status_string(int status);
 

@@ -133,6 +133,14 @@ def lib() -> ctypes.CDLL:
         l.a2sgd_layer_norm_backward.restype = _int
         l.a2sgd_layer_norm_backward.argtypes = [_vp, _i64, _vp, _i64, _int, _vp, _int, _vp, _vp, _vp, _i64, _vp, _vp,
                                                 _u64, _u32, _vp, _u64, _int, _vp]
+        l.a2sgd_gated_ffn_workspace.restype = _u64
+        l.a2sgd_gated_ffn_workspace.argtypes = [_u64, _u32, _u32, _u32]
+        l.a2sgd_gated_ffn_forward.restype = _int
+        l.a2sgd_gated_ffn_forward.argtypes = [_vp, _i64] * 8 + [_int, _int, _u64, _u32, _u32, _vp, _u64, _int, _vp]
+        l.a2sgd_gated_ffn_backward.restype = _int
+        l.a2sgd_gated_ffn_backward.argtypes = [_vp, _i64] * 12 + [_int, _int, _u64, _u32, _u32, _vp, _u64, _int, _vp]
+        l.a2sgd_gated_ffn_status.restype = _int
+        l.a2sgd_gated_ffn_status.argtypes = [_int, ctypes.POINTER(_int), _vp]
         l.a2sgd_status_string.restype = ctypes.c_char_p
         l.a2sgd_status_string.argtypes = [ctypes.c_int]
         _lib = l
@@ -693,3 +701,76 @@ def a2sgd_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optiona
         _vector(dweight, "dweight", d, pt, dev), _vector(dbias, "dbias", d, pt, dev), rows, d,
         _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev.index, _stream_on(dev, stream)),
         "a2sgd_layer_norm_backward")
+
+
+FFN_BACKWARD, FFN_ALIGNED = 1, 2
+_ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
+
+
+def a2sgd_gated_ffn_workspace(tokens: int, d: int, f: int, backward: bool = False, aligned: bool = False) -> int:
+    """Bytes of workspace of a2sgd_gated_ffn_forward (or _backward).  aligned: every matrix that is read, and hidden,
+    starts at a multiple of 16 bytes with a row stride that is a multiple of 8 elements."""
+    flags = (FFN_BACKWARD if backward else 0) | (FFN_ALIGNED if aligned else 0)
+    return int(lib().a2sgd_gated_ffn_workspace(int(tokens), int(d), int(f), flags))
+
+
+def _ffn_sizes(x: torch.Tensor, w_gate: torch.Tensor, activation: str):
+    dev = _cuda_device(x, "x")
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"x: need bfloat16 or float16, got {x.dtype}")
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise ValueError("x, w_gate: need matrices")
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation: need one of {sorted(_ACTIVATIONS)}, got {activation!r}")
+    return dev, x.dtype, x.shape[0], x.shape[1], w_gate.shape[0]
+
+
+def _optional_matrix(t, name, shape, dtype, dev):
+    return (None, 0) if t is None else _matrix(t, name, shape, dtype, dev)
+
+
+def a2sgd_gated_ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                            y: torch.Tensor, hidden: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                            up: Optional[torch.Tensor] = None, activation: str = "silu",
+                            workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """x, y: [tokens, d]; w_gate, w_up: [f, d]; w_down: [d, f]; hidden, gate, up: [tokens, f], out (gate and up, for the
+    backward pass, may both be None).  One 16-bit type, unit inner stride.  workspace: uint8 CUDA tensor of
+    a2sgd_gated_ffn_workspace bytes."""
+    dev, dt, t, d, f = _ffn_sizes(x, w_gate, activation)
+    wb = 0 if workspace is None else workspace.numel()
+    _check(lib().a2sgd_gated_ffn_forward(
+        *_matrix(x, "x", (t, d), dt, dev), *_matrix(w_gate, "w_gate", (f, d), dt, dev),
+        *_matrix(w_up, "w_up", (f, d), dt, dev), *_matrix(w_down, "w_down", (d, f), dt, dev),
+        *_matrix(y, "y", (t, d), dt, dev), *_matrix(hidden, "hidden", (t, f), dt, dev),
+        *_optional_matrix(gate, "gate", (t, f), dt, dev), *_optional_matrix(up, "up", (t, f), dt, dev),
+        _DTYPE_CODES[dt], _ACTIVATIONS[activation], t, d, f, _vector(workspace, "workspace", wb, torch.uint8, dev), wb,
+        dev.index, _stream_on(dev, stream)), "a2sgd_gated_ffn_forward")
+
+
+def a2sgd_gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                             w_down: torch.Tensor, hidden: torch.Tensor, gate: torch.Tensor, up: torch.Tensor,
+                             dx: Optional[torch.Tensor], dw_gate: Optional[torch.Tensor], dw_up: Optional[torch.Tensor],
+                             dw_down: Optional[torch.Tensor], activation: str = "silu",
+                             workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dy: [tokens, d]; hidden, gate, up: what the forward pass left; dx [tokens, d], dw_gate, dw_up [f, d], dw_down [d, f]:
+    out, each may be None; workspace: uint8 CUDA tensor of a2sgd_gated_ffn_workspace(..., backward=True) bytes."""
+    dev, dt, t, d, f = _ffn_sizes(x, w_gate, activation)
+    wb = 0 if workspace is None else workspace.numel()
+    _check(lib().a2sgd_gated_ffn_backward(
+        *_matrix(dy, "dy", (t, d), dt, dev), *_matrix(x, "x", (t, d), dt, dev),
+        *_matrix(w_gate, "w_gate", (f, d), dt, dev), *_matrix(w_up, "w_up", (f, d), dt, dev),
+        *_matrix(w_down, "w_down", (d, f), dt, dev), *_matrix(hidden, "hidden", (t, f), dt, dev),
+        *_matrix(gate, "gate", (t, f), dt, dev), *_matrix(up, "up", (t, f), dt, dev),
+        *_optional_matrix(dx, "dx", (t, d), dt, dev), *_optional_matrix(dw_gate, "dw_gate", (f, d), dt, dev),
+        *_optional_matrix(dw_up, "dw_up", (f, d), dt, dev), *_optional_matrix(dw_down, "dw_down", (d, f), dt, dev),
+        _DTYPE_CODES[dt], _ACTIVATIONS[activation], t, d, f, _vector(workspace, "workspace", wb, torch.uint8, dev), wb,
+        dev.index, _stream_on(dev, stream)), "a2sgd_gated_ffn_backward")
+
+
+def a2sgd_gated_ffn_status(device: Optional[int] = None, stream=None) -> int:
+    """Synchronises the stream; the status that the block's kernels latched on the device (OK or ERR_TIMEOUT), cleared."""
+    device = torch.cuda.current_device() if device is None else int(device)
+    st = ctypes.c_int(0)
+    _check(lib().a2sgd_gated_ffn_status(device, ctypes.byref(st), _stream_on(torch.device("cuda", device), stream)),
+           "a2sgd_gated_ffn_status")
+    return st.value

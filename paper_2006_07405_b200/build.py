@@ -13,10 +13,10 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liba2sgd.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("a2sgd.cu", "a2sgd_checked.cu", "a2sgd_noalloc.cu", "a2sgd_train.cu",
-                                               "a2sgd_adamw.cu", "a2sgd_layer_norm.cu")]
+                                               "a2sgd_adamw.cu", "a2sgd_layer_norm.cu", "a2sgd_gated_ffn.cu")]
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("a2sgd_kernels.cuh", "a2sgd_segments.cuh", "a2sgd_select.cuh",
                                                      "a2sgd_kernel_table.h", "a2sgd_debug_check.h",
-                                                     "a2sgd_train.cuh")] \
+                                                     "a2sgd_train.cuh", "a2sgd_tcgen05.cuh")] \
     + [os.path.join(ROOT, "include", "a2sgd.h")]
 
 COMPILE_FLAGS = [
