@@ -393,7 +393,8 @@ enum a2sgd_dtype { A2SGD_F32 = 0, A2SGD_BF16 = 1, A2SGD_F16 = 2 };
  *   32 bits  float m[], v[].
  *   8 bits   int8_t m[], uint8_t v[], and one float of m_scale[], v_scale[] a block:
  *                m = sign(q) (q / 127)^2 m_scale,        sqrt(v) = (q / 255)^2 v_scale,
- *            the scale being the block's largest value.  Squares spend the codes on small values: the
+ *            the scale being the block's largest value (formed as q |q| * (scale * fl(1 / 127^2)), and the
+ *            code's square as |m| * (fl(1 / scale) * 127^2), each product rounded once).  Squares spend the codes on small values: the
  *            smallest one is 6e-5 of the scale, a step near the scale 1.6 % and 0.8 %.  Codes are rounded up
  *            or down by a 12-bit dither, a hash of the step and of the element's place, so that their
  *            expectation is the value: with beta2 = 0.999 a step moves sqrt(v) by at most 0.05 % when

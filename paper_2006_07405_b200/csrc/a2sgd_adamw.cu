@@ -28,6 +28,7 @@ static_assert(kStateBlock == 256, "a block of the 8-bit states is one warp of 8 
 constexpr int kNormCtas = 2048; // partial sums of the norm at most
 // Blocks whose largest state is below 2^-100 are held as zeros: the gain 127^2 / scale stays finite.
 constexpr float kSmallestScale = 7.888609052210118e-31f;
+constexpr float kPerM = 1.0f / 16129.0f, kPerV = 1.0f / 65025.0f; // rounded once, then factors
 
 struct __align__(32) Tile {
     float *w;
@@ -96,7 +97,7 @@ __device__ __forceinline__ Gain gain_of(uint32_t largest_bits, float top_squared
     Gain r;
     r.scale = __uint_as_float(largest_bits);
     if (r.scale < kSmallestScale) r.scale = 0.0f; // false for NaN, which stays and shows
-    r.gain = r.scale == 0.0f ? 0.0f : __fdiv_rn(top_squared, r.scale);
+    r.gain = r.scale == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(r.scale), top_squared);
     return r;
 }
 
@@ -177,7 +178,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
         }
     }
     if constexpr (EIGHT) {
-        const float cm = __fdiv_rn(ms, 16129.0f), cr = __fdiv_rn(vs, 65025.0f);
+        const float cm = __fmul_rn(ms, kPerM), cr = __fmul_rn(vs, kPerV);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             // two's complement byte with its top bit flipped is the code plus 128
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(kThreads) k_read_state(const int8_t *mq, const
     if (block >= blocks) return;
     const uint64_t at = block * kStateBlock + (threadIdx.x & 31) * 8;
     const uint2 mw = *reinterpret_cast<const uint2 *>(mq + at), vw = *reinterpret_cast<const uint2 *>(vq + at);
-    const float cm = __fdiv_rn(m_scale[block], 16129.0f), cr = __fdiv_rn(v_scale[block], 65025.0f);
+    const float cm = __fmul_rn(m_scale[block], kPerM), cr = __fmul_rn(v_scale[block], kPerV);
     float m[8], v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

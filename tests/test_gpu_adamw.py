@@ -127,7 +127,7 @@ def _codes(x, top, u):
     scale = x.max(axis=1, keepdims=True)
     scale = np.where(scale < F32(2.0 ** -100), F32(0), scale)
     with np.errstate(divide="ignore"):
-        gain = np.where(scale > 0, F32(top * top) / scale, F32(0)).astype(F32)
+        gain = np.where(scale > 0, (F32(1) / scale) * F32(top * top), F32(0)).astype(F32)
     s = x * gain
     q = np.floor(np.sqrt(s))
     q = q + (s - q * q > u.reshape(x.shape) * F32(1 / 4096) * (F32(2) * q + F32(1))).astype(F32)
@@ -137,9 +137,9 @@ def _codes(x, top, u):
 def _step8(w, g, mq, vq, ms, vs, step, lr, beta1, beta2, eps, weight_decay):
     """The header's sequence of single-precision operations."""
     q, a, b = mq.astype(F32).reshape(-1, 256), ms.reshape(-1, 1), vs.reshape(-1, 1)
-    m = (q * np.abs(q)) * (a / F32(16129))
+    m = (q * np.abs(q)) * (a * F32(1 / 16129))
     q = vq.astype(F32).reshape(-1, 256)
-    r = (q * q) * (b / F32(65025))
+    r = (q * q) * (b * F32(1 / 65025))
     v = r * r
     g, w = g.reshape(-1, 256), w.reshape(-1, 256)
     m = m * F32(beta1) + g * F32(1 - beta1)
