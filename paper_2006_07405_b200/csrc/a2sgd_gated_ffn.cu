@@ -37,42 +37,50 @@ constexpr int kBM = 256;                  // rows of a tile, 128 a CTA
 constexpr int kBK = 64;                   // depth of a slice: 128 bytes a row
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
-constexpr uint32_t kABytes = 128 * kBK * 2; // A's slice in one CTA
+constexpr uint32_t kABytes = 128 * kBK * 2;  // A's slice in one CTA
+constexpr uint32_t kChunk = 64 * kBK * 2;    // 64 columns of an MN-major slice
 constexpr uint32_t kTmemColumns = 512;
+constexpr uint32_t kStaging = 32 * 128;      // 32 rows of 64 columns on their way out: two for each epilogue warp
+constexpr uint32_t kSmem = 227 * 1024;
+constexpr int kMostStages = 8;
+constexpr uint32_t kOperands = kSmem - 1024 - 512 - kEpilogueWarps * 2 * kStaging; // room for the slices
 
 enum Epilogue { kStore = 0, kGate = 1, kGateGrad = 2 };
 
 // Latched when a kernel's bounded wait ran out; read and cleared by a2sgd_gated_ffn_status.
 __device__ int g_status = 0;
 
+// 16-bit rows that the epilogue writes or reads: by TMA where `map` could be made, else element by element.
+struct Rows {
+    CUtensorMap map; // boxes of 32 rows and 64 columns
+    void *p;
+    int64_t ld;
+    int tma;
+};
+
 struct Problem {
-    int m, n;          // rows and columns of the output
-    int tiles_m, first; // tiles down, and this problem's first tile
-    int seg, segs;     // operand pairs that are added up: a[seg], b[seg], ...
-    void *out;
-    int64_t ldo;
+    int m, n;           // rows and columns of the output
+    int tiles_m, tiles_n, first; // tiles down and across, and this problem's first tile
+    int seg, segs;      // operand pairs that are added up: a[seg], b[seg], ...
+    int k_blocks;       // slices of all its pairs together
 };
 
 struct GemmArgs {
     CUtensorMap a[3], b[3];
-    int k_blocks[3];
+    Rows out[3];        // by problem; kGate: h; kGateGrad: da
+    Rows out2;          // kGate: a second copy of h, when p is set; kGateGrad: db
+    Rows gate, up;      // kGate: written when p is set; kGateGrad: read
+    int seg_blocks[3];  // slices of an operand pair
     Problem problem[3];
-    int problems, tiles;
+    int problems;
+    int bn;             // columns of a tile
+    int box;            // B's rows in one box (K-major B)
+    int stages;
+    uint32_t stage_bytes;
     int act;
-    // kGate: out is h; these are optional.  kGateGrad: out is da, out2 db, gate and up are read.
-    void *out2;       // kGate: a second copy of h (padded rows)
-    int64_t ldo2;
-    void *gate, *up;
-    int64_t ld_gate, ld_up;
-};
-
-template <int BN>
-struct Shape {
-    static constexpr uint32_t kBBytes = (BN / 2) * kBK * 2;
-    static constexpr uint32_t kStage = kABytes + kBBytes;
-    static constexpr int kStages = BN == 256 ? 6 : 8;
-    static constexpr uint32_t kBarriers = kStage * kStages;
-    static constexpr uint32_t kSmem = kBarriers + 256 + 1024; // and the alignment of the first stage
+    // Work: `whole` tiles, then the remaining ones in `splits` parts of their depth each
+    int whole, items, splits;
+    float *partials;    // [items - whole][bn / 4][256][4]
 };
 
 // ------------------------------------------------------------------ activations
@@ -93,64 +101,114 @@ __device__ __forceinline__ void activation(int act, float a, float &value, float
     }
 }
 
-// ------------------------------------------------------------------ global rows, 32 columns at a time
+// ------------------------------------------------------------------ staged rows
+// A warp's 32 rows of 64 columns, 128 bytes a row, the 16-byte pieces of a row permuted by the row's number
+// as the TMA's 128-byte swizzle does: lanes that hold a row each meet no bank twice.
+__device__ __forceinline__ uint32_t piece(uint32_t buf, uint32_t row, uint32_t i) { return buf + row * 128 + ((i ^ (row & 7)) << 4); }
+
 template <typename T>
-__device__ __forceinline__ void store32(T *row, int column, int n, const float (&v)[32], bool vec)
+__device__ __forceinline__ uint4 pack8(const float *v)
 {
-    if (vec && column + 32 <= n) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<uint4 *>(row + column + 8 * i) =
-                make_uint4(pack2(v[8 * i], v[8 * i + 1], T()), pack2(v[8 * i + 2], v[8 * i + 3], T()),
-                           pack2(v[8 * i + 4], v[8 * i + 5], T()), pack2(v[8 * i + 6], v[8 * i + 7], T()));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            if (column + i < n) row[column + i] = from_f32<T>(v[i]);
-        }
-    }
+    return make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()), pack2(v[6], v[7], T()));
 }
 template <typename T>
-__device__ __forceinline__ void load32(const T *row, int column, int n, float (&v)[32], bool vec)
+__device__ __forceinline__ void unpack8(uint4 q, float (&v)[8])
 {
-    if (vec && column + 32 <= n) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(row + column + 8 * i);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[8 * i + 2 * j] = lo_f32(w[j], T());
-                v[8 * i + 2 * j + 1] = hi_f32(w[j], T());
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = column + i < n ? to_f32(row[column + i]) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = lo_f32(w[j], T());
+        v[2 * j + 1] = hi_f32(w[j], T());
     }
 }
-__device__ __forceinline__ bool rows_vector(const void *p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && ld % 8 == 0; }
+
+// Staged rows out: one TMA store, or any alignment, 32 consecutive elements of a row at a time.  The whole warp.
+__device__ __forceinline__ void rows_out(const Rows &o, uint32_t buf, int row0, int col0, int m, int n, uint32_t lane)
+{
+    if (o.tma) {
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store(&o.map, col0, row0, buf);
+            tma_store_commit();
+        }
+    } else {
+        __syncwarp();
+        const int rows = min(32, m - row0);
+        for (int r = 0; r < rows; ++r) {
+            uint16_t *p = static_cast<uint16_t *>(o.p) + (int64_t)(row0 + r) * o.ld + col0;
+            for (int c = lane; c < min(64, n - col0); c += 32) p[c] = ld_shared16(piece(buf, r, c >> 3) + (c & 7) * 2);
+        }
+        __syncwarp();
+        if (lane == 0) tma_store_commit(); // an empty group: the buffers' turns are counted in groups
+    }
+}
+__device__ __forceinline__ void rows_in(const Rows &o, uint32_t buf, int row0, int col0, int m, int n, uint32_t lane)
+{
+    for (int r = 0; r < min(32, m - row0); ++r) {
+        const uint16_t *p = static_cast<const uint16_t *>(o.p) + (int64_t)(row0 + r) * o.ld + col0;
+        for (int c = lane; c < 64; c += 32) st_shared16(piece(buf, r, c >> 3) + (c & 7) * 2, c < n - col0 ? p[c] : (uint16_t)0);
+    }
+}
 
 // ------------------------------------------------------------------ the product
-template <typename T, int EPI, bool A_MN, bool B_MN, int BN>
+// One piece of work: a tile, all of its depth or a part of it.
+struct Item {
+    int p, tm, tn;      // problem, tile
+    int k0, k1;         // slices
+    int cols;           // columns of the product, a multiple of 32 (64 beyond 256), the tile's or less at the edge
+    int mmas, n_mma;    // products side by side and their width
+    int slot;           // of the partial sums; -1: the whole depth
+};
+
+// Tiles are walked in groups of 8 tiles down, so that the pairs at work share slices of both operands in L2.
+__device__ __forceinline__ Item item_at(const GemmArgs &g, int i)
+{
+    Item t;
+    int tile = i, part = 0;
+    t.slot = -1;
+    if (i >= g.whole) {
+        t.slot = i - g.whole;
+        tile = g.whole + t.slot / g.splits;
+        part = t.slot % g.splits;
+    }
+    t.p = 0;
+    while (t.p + 1 < g.problems && tile >= g.problem[t.p + 1].first) ++t.p;
+    const Problem &q = g.problem[t.p];
+    tile -= q.first;
+    const int per_group = 8 * q.tiles_n, group = tile / per_group, rest = tile - group * per_group;
+    const int down = min(8, q.tiles_m - group * 8);
+    t.tm = group * 8 + rest % down;
+    t.tn = rest / down;
+    t.k0 = t.slot < 0 ? 0 : (int)((int64_t)q.k_blocks * part / g.splits);
+    t.k1 = t.slot < 0 ? q.k_blocks : (int)((int64_t)q.k_blocks * (part + 1) / g.splits);
+    t.cols = min(g.bn, (q.n - t.tn * g.bn + 31) / 32 * 32);
+    t.mmas = t.cols > 256 ? 2 : 1;
+    t.n_mma = t.cols > 256 ? (t.cols / 2 + 31) / 32 * 32 : t.cols;
+    t.cols = t.mmas * t.n_mma;
+    return t;
+}
+
+template <typename T, int EPI, bool A_MN, bool B_MN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(const __grid_constant__ GemmArgs g)
 {
-    using S = Shape<BN>;
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = base + S::kBarriers;
-    const auto full = [&](int s) { return bars + 8u * s; };
-    const auto empty = [&](int s) { return bars + 8u * (S::kStages + s); };
-    const auto acc_full = [&](int i) { return bars + 8u * (2 * S::kStages + i); };
-    const auto acc_empty = [&](int i) { return bars + 8u * (2 * S::kStages + 2 + i); };
+    const uint32_t staging = base + kOperands / 1024 * 1024;
+    __shared__ __align__(8) uint64_t bars[2 * kMostStages + 4 + kEpilogueWarps];
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 8u * s; };
+    const auto empty = [&](int s) { return bar0 + 8u * (kMostStages + s); };
+    const auto acc_full = [&](int i) { return bar0 + 8u * (2 * kMostStages + i); };
+    const auto acc_empty = [&](int i) { return bar0 + 8u * (2 * kMostStages + 2 + i); };
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
 
     const uint32_t rank = cluster_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int accs = EPI == kGate || g.bn <= 256 ? 2 : 1; // accumulators of up to 256 columns alternate
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) {
+        for (int s = 0; s < kMostStages; ++s) {
             bar_init(full(s), 1);
             bar_init(empty(s), 1);
         }
@@ -158,12 +216,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
             bar_init(acc_full(i), 1);
             bar_init(acc_empty(i), 2 * kEpilogueWarps);
         }
+        for (int i = 0; i < kEpilogueWarps; ++i) bar_init(bar0 + 8u * (2 * kMostStages + 4 + i), 1);
         gave_up = 0;
         bar_init_fence();
-        for (int i = 0; i < 3; ++i) {
-            tma_prefetch_map(&g.a[i]);
-            tma_prefetch_map(&g.b[i]);
-        }
     }
     if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_at), kTmemColumns);
     fence_before();
@@ -174,90 +229,98 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     wait_prior_grid();
     release_next_grid();
 
-    const auto problem_of = [&](int tile) {
-        int p = 0;
-        while (p + 1 < g.problems && tile >= g.problem[p + 1].first) ++p;
-        return p;
-    };
-
     if (warp == 0 && lane == 0) {
         // ---------------------------------------------------------- operands in
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int tile = pair; ok && tile < g.tiles; tile += pairs) {
-            const Problem &q = g.problem[problem_of(tile)];
-            const int local = tile - q.first, tm = local % q.tiles_m, tn = local / q.tiles_m;
-            const int row = tm * kBM + (int)rank * 128;
-            const int col = EPI == kGate ? tn * 128 : tn * BN + (int)rank * (BN / 2);
-            for (int seg = q.seg; ok && seg < q.seg + q.segs; ++seg) {
+        const uint32_t leader = map_to(full(0), 0);
+        for (int i = pair; ok && i < g.items; i += pairs) {
+            const Item t = item_at(g, i);
+            const Problem &q = g.problem[t.p];
+            const int row = t.tm * kBM + (int)rank * 128;
+            const int mine = EPI == kGate ? 128 : t.n_mma / 2;                   // columns of B in this CTA, a product
+            const int loads = B_MN ? (mine + 63) / 64 : (mine + g.box - 1) / g.box;
+            const uint32_t load_bytes = B_MN ? kChunk : g.box * 128u;
+            const int step = B_MN ? 64 : g.box;
+            const int mmas = EPI == kGate ? 1 : t.mmas;
+            const int col = EPI == kGate ? t.tn * 128 : t.tn * g.bn + (int)rank * mine;
+            const uint32_t bytes = 2 * (kABytes + (uint32_t)(mmas * loads) * load_bytes); // of both CTAs
+            int seg = q.seg, kb = t.k0;
+            while (kb >= g.seg_blocks[seg]) kb -= g.seg_blocks[seg++];
+            for (int k = t.k0; k < t.k1; ++k, ++kb) {
+                if (kb == g.seg_blocks[seg]) {
+                    kb = 0;
+                    ++seg;
+                }
+                ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
+                if (!ok) break;
                 const CUtensorMap *ma = &g.a[seg], *mb = EPI == kGate ? &g.b[rank] : &g.b[seg];
-                for (int kb = 0; kb < g.k_blocks[seg]; ++kb) {
-                    ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
-                    if (!ok) break;
-                    if (rank == 0) bar_expect(full(stage), 2 * S::kStage);
-                    const uint32_t bar = map_to(full(stage), 0);
-                    const uint32_t sa = base + stage * S::kStage, sb = sa + kABytes;
-                    if constexpr (A_MN) {
-                        tma_load_pair(sa, ma, row, kb * kBK, bar);
-                        tma_load_pair(sa + 64 * kBK * 2, ma, row + 64, kb * kBK, bar);
-                    } else {
-                        tma_load_pair(sa, ma, kb * kBK, row, bar);
+                if (rank == 0) bar_expect(full(stage), bytes);
+                const uint32_t bar = leader + 8u * stage;
+                const uint32_t sa = base + stage * g.stage_bytes;
+                uint32_t sb = sa + kABytes;
+                if constexpr (A_MN) {
+                    tma_load_pair(sa, ma, row, kb * kBK, bar);
+                    tma_load_pair(sa + kChunk, ma, row + 64, kb * kBK, bar);
+                } else {
+                    tma_load_pair(sa, ma, kb * kBK, row, bar);
+                }
+                for (int h = 0; h < mmas; ++h) {
+                    for (int j = 0; j < loads; ++j, sb += load_bytes) {
+                        const int c = col + h * t.n_mma + j * step;
+                        if constexpr (B_MN) tma_load_pair(sb, mb, c, kb * kBK, bar);
+                        else tma_load_pair(sb, mb, kb * kBK, c, bar);
                     }
-                    if constexpr (B_MN) {
-#pragma unroll
-                        for (int j = 0; j < BN / 128; ++j) tma_load_pair(sb + j * 64 * kBK * 2, mb, col + 64 * j, kb * kBK, bar);
-                    } else {
-                        tma_load_pair(sb, mb, kb * kBK, col, bar);
-                    }
-                    if (++stage == S::kStages) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                }
+                if (++stage == g.stages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
         }
         // every slice has been consumed: nothing is in flight towards this CTA any more
-        for (int s = 0; ok && s < S::kStages; ++s) {
+        for (int s = 0; ok && s < g.stages; ++s) {
             ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
-            if (++stage == S::kStages) {
+            if (++stage == g.stages) {
                 stage = 0;
                 phase ^= 1u;
             }
         }
     } else if (warp == 1 && lane == 0 && rank == 0) {
         // ---------------------------------------------------------- products
-        constexpr uint32_t kType = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-        constexpr uint32_t kDesc = instruction_desc(kType, A_MN, B_MN, kBM, BN);
+        constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         constexpr uint32_t kStepA = A_MN ? 16 * 128 : 32, kStepB = B_MN ? 16 * 128 : 32; // 16 of k further
         int stage = 0, turn = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int tile = pair; ok && tile < g.tiles; tile += pairs, ++turn) {
-            const Problem &q = g.problem[problem_of(tile)];
-            const int acc = turn & 1;
-            ok = bar_wait(acc_empty(acc), ((turn >> 1) & 1) ^ 1, &gave_up);
+        for (int i = pair; ok && i < g.items; i += pairs, ++turn) {
+            const Item t = item_at(g, i);
+            const int acc = turn % accs;
+            ok = bar_wait(acc_empty(acc), ((turn / accs) & 1) ^ 1, &gave_up);
             if (!ok) break;
             fence_after();
+            const int n_mma = EPI == kGate ? 256 : t.n_mma, mmas = EPI == kGate ? 1 : t.mmas;
+            const uint32_t desc = instruction_desc(kType, A_MN, B_MN, kBM, 0) | (uint32_t)(n_mma >> 3) << 17;
+            const uint32_t second = EPI == kGate ? 0
+                                    : B_MN       ? (uint32_t)(n_mma / 2 + 63) / 64 * kChunk
+                                                 : (uint32_t)((n_mma / 2 + g.box - 1) / g.box * g.box) * 128;
             const uint32_t d = tmem + acc * 256;
-            bool add = false;
-            for (int seg = q.seg; ok && seg < q.seg + q.segs; ++seg) {
-                for (int kb = 0; kb < g.k_blocks[seg]; ++kb) {
-                    ok = bar_wait(full(stage), phase, &gave_up);
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t sa = base + stage * S::kStage, sb = sa + kABytes;
+            for (int k = t.k0; k < t.k1; ++k) {
+                ok = bar_wait(full(stage), phase, &gave_up);
+                if (!ok) break;
+                fence_after();
+                const uint32_t sa = base + stage * g.stage_bytes;
+                const uint64_t da = operand_desc(sa, A_MN ? kChunk : 16), db = operand_desc(sa + kABytes, B_MN ? kChunk : 16);
+                for (int h = 0; h < mmas; ++h) {
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k) {
-                        mma_pair(d, operand_desc(sa + k * kStepA, A_MN ? 64 * kBK * 2 : 16),
-                                 operand_desc(sb + k * kStepB, B_MN ? 64 * kBK * 2 : 16), kDesc, add);
-                        add = true;
-                    }
-                    commit_pair(empty(stage));
-                    if (++stage == S::kStages) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                    for (int j = 0; j < kBK / 16; ++j)
+                        mma_pair(d + h * n_mma, da + j * (kStepA >> 4), db + ((h * second + j * kStepB) >> 4), desc, k > t.k0 || j > 0);
+                }
+                commit_pair(empty(stage));
+                if (++stage == g.stages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
             commit_pair(acc_full(acc));
@@ -265,87 +328,153 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     } else if (warp >= 2) {
         // ---------------------------------------------------------- accumulators out
         const uint32_t quarter = warp & 3, half = (warp - 2) >> 2; // a warp reads the TMEM lanes of its quarter
+        const uint32_t buf0 = staging + (warp - 2) * 2 * kStaging, buf1 = buf0 + kStaging;
+        const uint32_t loaded = bar0 + 8u * (2 * kMostStages + 4 + (warp - 2));
         int turn = 0;
-        for (int tile = pair; tile < g.tiles; tile += pairs, ++turn) {
-            const Problem &q = g.problem[problem_of(tile)];
-            const int local = tile - q.first, tm = local % q.tiles_m, tn = local / q.tiles_m;
-            const int acc = turn & 1;
-            const int row = tm * kBM + (int)rank * 128 + quarter * 32 + lane;
-            const bool live = row < q.m;
-            if (!bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
-            fence_after();
+        uint32_t loads = 0, stores = 0;
+        for (int i = pair; i < g.items; i += pairs, ++turn) {
+            const Item t = item_at(g, i);
+            const Problem &q = g.problem[t.p];
+            const int acc = turn % accs;
+            const int row0 = t.tm * kBM + (int)rank * 128 + quarter * 32; // this warp's 32 rows
+            const bool live = row0 < q.m;
             const uint32_t d = tmem + acc * 256 + (quarter * 32u << 16);
             if constexpr (EPI == kGate) {
-                T *h = static_cast<T *>(q.out) + (int64_t)row * q.ldo;
-                T *h2 = static_cast<T *>(g.out2) + (int64_t)row * g.ldo2;
-                T *ga = static_cast<T *>(g.gate) + (int64_t)row * g.ld_gate;
-                T *up = static_cast<T *>(g.up) + (int64_t)row * g.ld_up;
-                const bool vh = rows_vector(q.out, q.ldo), vg = rows_vector(g.gate, g.ld_gate), vu = rows_vector(g.up, g.ld_up);
-#pragma unroll 1
-                for (int c = half * 64; c < (int)half * 64 + 64; c += 32) {
+                if (!bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up)) break;
+                fence_after();
+                const int c = half * 64, col0 = t.tn * 128 + c;
+                if (lane == 0) tma_store_read<0>();
+                __syncwarp();
+                uint4 h[8];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
                     float a[32], b[32];
-                    tmem_ld32(d + c, a);
-                    tmem_ld32(d + 128 + c, b);
+                    tmem_ld32(d + c + 32 * j, a);
+                    tmem_ld32(d + 128 + c + 32 * j, b);
                     tmem_wait_ld();
-                    const int column = tn * 128 + c;
-                    if (live && g.gate) {
-                        store32(ga, column, q.n, a, vg);
-                        store32(up, column, q.n, b, vu);
+                    if (g.gate.p) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            st_shared(piece(buf0, lane, 4 * j + k), pack8<T>(a + 8 * k));
+                            st_shared(piece(buf1, lane, 4 * j + k), pack8<T>(b + 8 * k));
+                        }
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int k = 0; k < 32; ++k) {
                         float value, slope;
-                        activation(g.act, a[i], value, slope);
-                        a[i] = value * b[i];
+                        activation(g.act, a[k], value, slope);
+                        a[k] = value * b[k];
                     }
-                    if (live) {
-                        if (q.out) store32(h, column, q.n, a, vh);
-                        if (g.out2) store32(h2, column, q.n, a, true);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) h[4 * j + k] = pack8<T>(a + 8 * k);
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
+                if (live && col0 < q.n) {
+                    if (g.gate.p) {
+                        rows_out(g.gate, buf0, row0, col0, q.m, q.n, lane);
+                        rows_out(g.up, buf1, row0, col0, q.m, q.n, lane);
+                        if (lane == 0) tma_store_read<0>();
+                        __syncwarp();
                     }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) st_shared(piece(buf0, lane, k), h[k]);
+                    rows_out(g.out[0], buf0, row0, col0, q.m, q.n, lane);
+                    if (g.out2.p) rows_out(g.out2, buf0, row0, col0, q.m, q.n, lane);
                 }
             } else if constexpr (EPI == kGateGrad) {
-                T *da = static_cast<T *>(q.out) + (int64_t)row * q.ldo;
-                T *db = static_cast<T *>(g.out2) + (int64_t)row * g.ldo2;
-                const T *ga = static_cast<const T *>(g.gate) + (int64_t)row * g.ld_gate;
-                const T *up = static_cast<const T *>(g.up) + (int64_t)row * g.ld_up;
-                const bool vg = rows_vector(g.gate, g.ld_gate), vu = rows_vector(g.up, g.ld_up);
-#pragma unroll 1
-                for (int c = half * (BN / 2); c < (int)(half + 1) * (BN / 2); c += 32) {
-                    float dh[32], a[32], b[32];
-                    const int column = tn * BN + c;
-                    tmem_ld32(d + c, dh);
-                    if (live) {
-                        load32(ga, column, q.n, a, vg);
-                        load32(up, column, q.n, b, vu);
-                    }
-                    tmem_wait_ld();
-                    if (live) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float value, slope;
-                            activation(g.act, a[i], value, slope);
-                            a[i] = dh[i] * b[i] * slope;
-                            b[i] = dh[i] * value;
+                // a and b arrive where da and db leave from
+                const int subs = (t.cols + 63) / 64;
+                bool waited = false, ok = true;
+                for (int sub = half; sub < subs; sub += 2) {
+                    const int col0 = t.tn * g.bn + sub * 64;
+                    const bool here = live && col0 < q.n;
+                    if (here) {
+                        if (lane == 0) tma_store_read<0>();
+                        __syncwarp();
+                        const uint32_t bytes = (g.gate.tma ? kStaging : 0u) + (g.up.tma ? kStaging : 0u);
+                        if (lane == 0 && bytes) {
+                            bar_expect(loaded, bytes);
+                            if (g.gate.tma) tma_load(buf0, &g.gate.map, col0, row0, loaded);
+                            if (g.up.tma) tma_load(buf1, &g.up.map, col0, row0, loaded);
                         }
-                        store32(da, column, q.n, a, true);
-                        store32(db, column, q.n, b, true);
+                        if (!g.gate.tma) rows_in(g.gate, buf0, row0, col0, q.m, q.n, lane);
+                        if (!g.up.tma) rows_in(g.up, buf1, row0, col0, q.m, q.n, lane);
+                        __syncwarp();
+                        if (bytes) ok = ok && bar_wait(loaded, loads++ & 1, &gave_up);
                     }
+                    if (!waited) {
+                        ok = ok && bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up);
+                        fence_after();
+                        waited = true;
+                    }
+                    if (!__all_sync(0xffffffffu, ok)) break;
+                    if (!here) continue;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float dh[32];
+                        tmem_ld32(d + sub * 64 + 32 * j, dh);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float a[8], b[8];
+                            unpack8<T>(ld_shared(piece(buf0, lane, 4 * j + k)), a);
+                            unpack8<T>(ld_shared(piece(buf1, lane, 4 * j + k)), b);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                float value, slope;
+                                activation(g.act, a[e], value, slope);
+                                a[e] = dh[8 * k + e] * b[e] * slope;
+                                b[e] = dh[8 * k + e] * value;
+                            }
+                            st_shared(piece(buf0, lane, 4 * j + k), pack8<T>(a));
+                            st_shared(piece(buf1, lane, 4 * j + k), pack8<T>(b));
+                        }
+                    }
+                    rows_out(g.out[0], buf0, row0, col0, q.m, q.n, lane);
+                    rows_out(g.out2, buf1, row0, col0, q.m, q.n, lane);
                 }
+                if (!__all_sync(0xffffffffu, ok)) break;
+                if (!waited && !bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up)) break;
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
             } else {
-                T *out = static_cast<T *>(q.out) + (int64_t)row * q.ldo;
-                const bool vo = rows_vector(q.out, q.ldo);
-#pragma unroll 1
-                for (int c = half * (BN / 2); c < (int)(half + 1) * (BN / 2); c += 32) {
-                    float v[32];
-                    tmem_ld32(d + c, v);
-                    tmem_wait_ld();
-                    if (live) store32(out, tn * BN + c, q.n, v, vo);
+                if (!bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up)) break;
+                fence_after();
+                const int subs = (min(t.cols, q.n - t.tn * g.bn) + 63) / 64;
+                for (int sub = half; live && sub < subs; sub += 2) {
+                    const int col0 = t.tn * g.bn + sub * 64;
+                    const uint32_t buf = stores++ & 1 ? buf1 : buf0;
+                    if (t.slot < 0) {
+                        if (lane == 0) tma_store_read<1>();
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float v[32];
+                        tmem_ld32(d + sub * 64 + 32 * j, v);
+                        tmem_wait_ld();
+                        if (t.slot < 0) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) st_shared(piece(buf, lane, 4 * j + k), pack8<T>(v + 8 * k));
+                        } else if (sub * 64 + 32 * j < g.bn) {
+                            // rows side by side: 512 consecutive bytes a warp and store
+                            float4 *part = reinterpret_cast<float4 *>(g.partials) +
+                                           ((int64_t)t.slot * (g.bn / 4) + sub * 16 + 8 * j) * kBM + rank * 128 + quarter * 32 + lane;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) part[k * kBM] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        }
+                    }
+                    if (t.slot < 0) rows_out(g.out[t.p], buf, row0, col0, q.m, q.n, lane);
                 }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
             }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
         }
+        if (lane == 0) tma_store_done();
     }
     __syncwarp();
     __syncthreads();
@@ -357,6 +486,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     }
     cluster_sync();
     if (warp == 1) tmem_free_pair(tmem, kTmemColumns);
+}
+
+// The parts of the tiles that were split, added up in order.  One thread: a row, 8 columns.
+template <typename T>
+__global__ void __launch_bounds__(kBM) k_join(const __grid_constant__ GemmArgs g)
+{
+    wait_prior_grid();
+    release_next_grid();
+    const Item t = item_at(g, g.whole + (int)blockIdx.x * g.splits);
+    const Problem &q = g.problem[t.p];
+    const int row = t.tm * kBM + threadIdx.x, col = t.tn * g.bn + blockIdx.y * 8;
+    if (row >= q.m || col >= q.n) return;
+    float v[8] = {};
+    const float4 *part = reinterpret_cast<const float4 *>(g.partials) + ((int64_t)t.slot * (g.bn / 4) + blockIdx.y * 2) * kBM + threadIdx.x;
+    for (int s = 0; s < g.splits; ++s, part += (int64_t)(g.bn / 4) * kBM) {
+        const float4 x = __ldcg(part), y = __ldcg(part + kBM);
+        v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+    }
+    T *out = static_cast<T *>(g.out[t.p].p) + (int64_t)row * g.out[t.p].ld + col;
+    if (g.out[t.p].tma && col + 8 <= q.n) {
+        *reinterpret_cast<uint4 *>(out) = pack8<T>(v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (col + i < q.n) out[i] = from_f32<T>(v[i]);
+        }
+    }
 }
 
 // ------------------------------------------------------------------ rows that TMA cannot read
@@ -429,63 +586,143 @@ inline bool tma_ok(const Matrix &m) { return aligned(m.p, 16) && (m.rows <= 1 ||
 inline uint64_t room(int64_t rows, int64_t cols) { return ((uint64_t)rows * padded(cols) * 2 + 255) / 256 * 256; }
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-template <typename T, int EPI, bool A_MN, bool B_MN, int BN>
-int launch_gemm(GemmArgs &g, int sms, cudaStream_t s)
+// What the epilogue writes or reads: by TMA where rows allow it.  A TMA store leaves out what lies past the end of a
+// row in pieces of 16 bytes only, so that rows of other lengths are written element by element.
+bool set_rows(Rows &r, const Matrix &m, int dtype, bool written = true)
 {
-    const void *fn = reinterpret_cast<const void *>(&k_gemm<T, EPI, A_MN, B_MN, BN>);
+    r.p = const_cast<void *>(m.p);
+    r.ld = m.ld;
+    r.tma = m.p && tma_ok(m) && (!written || m.cols % 8 == 0);
+    return !r.tma || make_map(&r.map, m, dtype, 32);
+}
+
+// Rows of the workspace with their padding, which may be written.
+Matrix whole_rows(Matrix m)
+{
+    m.cols = (int)m.ld;
+    return m;
+}
+
+// ---- the shape of a launch ---------------------------------------------------------------------------
+// What a product's tiles cost, in clocks of a slice: the tensor cores take 2 a column, the way from L2 about
+// 42 bytes a clock and SM (measured: every shape of this kernel met 10 to 11 TB/s there), so that narrow
+// tiles, which bring in more for what they compute, are bound by the latter.
+inline double slice_clocks(int bn) { return std::max(2.0 * bn, (16384.0 + 64.0 * bn) / 42.0); }
+
+constexpr int kMostPairs = 80;  // pairs that take part in splitting: bounds the workspace
+constexpr int kLeastSlices = 8; // of a part of a tile
+
+struct Shape {
+    int bn = 256, splits = 1;
+    double cost = 1e30;
+};
+
+inline int64_t tiles_of(const Problem &q, int bn) { return (int64_t)ceil_div(q.m, kBM) * ceil_div(q.n, bn); }
+
+// Tiles that do not fill a last round over the pairs of SMs are split in depth, as evenly as the pairs allow.
+inline int splits_of(int64_t tiles, int pairs, int k_blocks)
+{
+    const int64_t rest = tiles % pairs;
+    if (rest == 0) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(pairs, kMostPairs) / rest, k_blocks / kLeastSlices));
+}
+
+// One problem, plain output: the width and the splitting with the least cost.
+Shape choose(const Problem &q, bool b_mn, int pairs, bool may_split)
+{
+    Shape best;
+    for (int bn : {64, 128, 192, 256, 320, 384, 448, 512}) { // whole staged blocks of 64 columns
+        if (b_mn && bn != 128 && bn != 256 && bn != 512) continue; // whole chunks of 64 columns in either CTA
+        if (bn > 128 && bn - 64 >= q.n) continue;
+        const int64_t tiles = tiles_of(q, bn);
+        const int splits = may_split ? splits_of(tiles, pairs, q.k_blocks) : 1;
+        const double rounds = (double)(tiles / pairs) + (tiles % pairs ? 1.0 / splits : 0.0);
+        // what is not overlapped: the last tile's way out, or every tile's beyond 256 columns; joining the parts
+        const double out = bn > 256 ? 12.0 * bn * std::ceil(rounds) : 12.0 * bn;
+        const double cost = rounds * q.k_blocks * slice_clocks(bn) + out + (splits > 1 ? 4000.0 + 20.0 * bn : 0.0);
+        if (cost < best.cost) {
+            best.bn = bn;
+            best.splits = splits;
+            best.cost = cost;
+        }
+    }
+    return best;
+}
+
+inline uint64_t partial_bytes(int64_t slots, int bn) { return (uint64_t)slots * kBM * bn * sizeof(float); }
+
+template <typename T, int EPI, bool A_MN, bool B_MN>
+int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
+{
+    const void *fn = reinterpret_cast<const void *>(&k_gemm<T, EPI, A_MN, B_MN>);
     static std::atomic<uint64_t> allowed{0}; // devices on which this kernel may use its shared memory
     int device = 0;
     A2_TRAIN_CUDA(cudaGetDevice(&device));
     const uint64_t bit = 1ull << (device & 63);
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        A2_TRAIN_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<BN>::kSmem));
+        A2_TRAIN_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024)));
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    const unsigned pairs = (unsigned)std::min(g.tiles, sms / 2);
+    const int pairs = std::max(1, sms / 2);
+    g.whole = g.splits > 1 ? tiles / pairs * pairs : tiles;
+    g.items = g.whole + (tiles - g.whole) * g.splits;
+    g.stage_bytes = kABytes + (EPI == kGate ? 128u : (uint32_t)g.bn / 2) * 128u;
+    g.stages = (int)std::min<uint32_t>(kMostStages, kOperands / g.stage_bytes);
     void *params[] = {&g};
-    A2_TRAIN_CUDA(launch(fn, dim3(2 * pairs), kThreads, Shape<BN>::kSmem, params, s));
+    A2_TRAIN_CUDA(launch(fn, dim3(2 * (unsigned)std::min(g.items, pairs)), kThreads, kSmem - 1024, params, s));
+    if (EPI == kStore && g.splits > 1)
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / 8)), kBM, 0,
+                             params, s));
     return A2SGD_OK;
 }
 
 // The maps of one operand pair.  An operand that is not transposed lies as [rows, k], a transposed one as [k, rows].
-template <bool A_MN, bool B_MN, int BN>
-bool add_operands(GemmArgs &g, int i, const Matrix &a, const Matrix &b, int64_t k, int dtype)
+template <bool A_MN, bool B_MN>
+bool add_operands(GemmArgs &g, int i, const Matrix &a, const Matrix &b, int dtype)
 {
-    g.k_blocks[i] = ceil_div(k, kBK);
-    return make_map(&g.a[i], a, dtype, A_MN ? kBK : 128) && make_map(&g.b[i], b, dtype, B_MN ? kBK : BN / 2);
+    return make_map(&g.a[i], a, dtype, A_MN ? kBK : 128) && make_map(&g.b[i], b, dtype, B_MN ? kBK : g.box);
 }
 
-void add_problem(GemmArgs &g, int64_t m, int n, int tile_n, int seg, int segs, void *out, int64_t ldo)
+// Adds a product of `segs` operand pairs, each `k` deep, from pair `seg` on.
+int add_problem(GemmArgs &g, int64_t m, int n, int tile_n, int seg, int segs, int64_t k, int tiles)
 {
     Problem &q = g.problem[g.problems++];
     q.m = (int)m;
     q.n = n;
     q.tiles_m = ceil_div(m, kBM);
-    q.first = g.tiles;
+    q.tiles_n = ceil_div(n, tile_n);
+    q.first = tiles;
     q.seg = seg;
     q.segs = segs;
-    q.out = out;
-    q.ldo = ldo;
-    g.tiles += q.tiles_m * ceil_div(n, tile_n);
+    q.k_blocks = segs * ceil_div(k, kBK);
+    for (int i = seg; i < seg + segs; ++i) g.seg_blocks[i] = ceil_div(k, kBK);
+    return tiles + q.tiles_m * q.tiles_n;
 }
 
-// Columns of a tile of a plain product: the width that leaves the tensor cores least idle, counting whole
-// rounds of tiles over the pairs of SMs.
-int tile_columns(int64_t m, int n, int sms)
+void set_shape(GemmArgs &g, const Shape &shape, float *partials)
 {
-    const int pairs = std::max(1, sms / 2);
-    const int64_t rows = ceil_div(m, kBM);
-    const int64_t wide = (rows * ceil_div(n, 256) + pairs - 1) / pairs * 256;
-    const int64_t narrow = (rows * ceil_div(n, 128) + pairs - 1) / pairs * 128;
-    return narrow < wide ? 128 : 256;
+    g.bn = shape.bn;
+    g.box = shape.bn > 256 ? shape.bn / 4 : shape.bn / 2;
+    g.splits = shape.splits;
+    g.partials = partials;
+}
+
+// Shapes of the two products with plain outputs of [tokens, d]: they may need room for partial sums.
+Shape shape_of(int64_t m, int n, int64_t k, int segs, bool b_mn, int sms)
+{
+    Problem q{};
+    q.m = (int)m;
+    q.n = n;
+    q.k_blocks = segs * ceil_div(k, kBK);
+    return choose(q, b_mn, std::max(1, sms / 2), true);
 }
 
 struct Packer {
     PackArgs args{};
     int jobs = 0;
     int64_t most_rows = 0;
-    char *at;
-    explicit Packer(void *workspace) : at(static_cast<char *>(workspace)) {}
+    char *begin, *at;
+    explicit Packer(void *workspace) : begin(static_cast<char *>(workspace)), at(begin) {}
     void *take(int64_t rows, int64_t cols)
     {
         void *p = at;
@@ -503,6 +740,14 @@ struct Packer {
                                    m.rows, m.cols};
         most_rows = std::max(most_rows, m.rows);
         return c;
+    }
+    uint64_t used() const { return (uint64_t)(at - begin); }
+    bool fits(uint64_t bytes) const { return used() == 0 || (begin && used() <= bytes); }
+    // The shape, without its splitting where the rest of the workspace has no room for the partial sums.
+    Shape fit(Shape shape, uint64_t bytes) const
+    {
+        if (shape.splits > 1 && (!begin || used() + partial_bytes(kMostPairs, shape.bn) > bytes)) shape.splits = 1;
+        return shape;
     }
     int run(int sms, cudaStream_t s)
     {
@@ -536,6 +781,8 @@ template <typename T>
 int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &wd, Matrix y, Matrix h, Matrix gate, Matrix up, int act,
             int dtype, void *workspace, uint64_t workspace_bytes, int sms, cudaStream_t s)
 {
+    const int64_t t = x.rows;
+    const int d = x.cols, f = h.cols;
     Packer pack(workspace);
     const Matrix px = pack.usable(x), pg = pack.usable(wg), pu = pack.usable(wu), pd = pack.usable(wd);
     Matrix ph = h; // what the second product reads
@@ -543,48 +790,26 @@ int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &w
         ph.ld = padded(h.cols);
         ph.p = pack.take(h.rows, h.cols);
     }
-    const uint64_t need = (uint64_t)(pack.at - static_cast<char *>(workspace));
-    if (need && (!workspace || workspace_bytes < need)) return A2SGD_ERR_ARG;
+    const Shape shape = pack.fit(shape_of(t, d, f, 1, false, sms), workspace_bytes);
+    if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
     int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
-    const int64_t t = x.rows;
-    const int d = x.cols, f = h.cols;
 
     GemmArgs g{};
     g.act = act;
-    if (!add_operands<false, false, 256>(g, 0, px, pg, d, dtype) || !make_map(&g.b[1], pu, dtype, 128)) return A2SGD_ERR_CUDA;
-    add_problem(g, t, f, 128, 0, 1, const_cast<void *>(h.p), h.ld);
-    if (ph.p != h.p) {
-        g.out2 = const_cast<void *>(ph.p);
-        g.ldo2 = ph.ld;
-    }
-    g.gate = const_cast<void *>(gate.p);
-    g.ld_gate = gate.ld;
-    g.up = const_cast<void *>(up.p);
-    g.ld_up = up.ld;
-    rc = launch_gemm<T, kGate, false, false, 256>(g, sms, s);
+    g.bn = 256;
+    g.box = 128;
+    g.splits = 1;
+    if (!add_operands<false, false>(g, 0, px, pg, dtype) || !make_map(&g.b[1], pu, dtype, 128) || !set_rows(g.out[0], h, dtype) ||
+        (ph.p != h.p && !set_rows(g.out2, whole_rows(ph), dtype)) || !set_rows(g.gate, gate, dtype) || !set_rows(g.up, up, dtype))
+        return A2SGD_ERR_CUDA;
+    rc = launch_gemm<T, kGate, false, false>(g, add_problem(g, t, f, 128, 0, 1, d, 0), sms, s);
     if (rc != A2SGD_OK) return rc;
 
     g = GemmArgs{};
-    if (tile_columns(t, d, sms) == 256) {
-        if (!add_operands<false, false, 256>(g, 0, ph, pd, f, dtype)) return A2SGD_ERR_CUDA;
-        add_problem(g, t, d, 256, 0, 1, const_cast<void *>(y.p), y.ld);
-        return launch_gemm<T, kStore, false, false, 256>(g, sms, s);
-    }
-    if (!add_operands<false, false, 128>(g, 0, ph, pd, f, dtype)) return A2SGD_ERR_CUDA;
-    add_problem(g, t, d, 128, 0, 1, const_cast<void *>(y.p), y.ld);
-    return launch_gemm<T, kStore, false, false, 128>(g, sms, s);
-}
-
-template <typename T, int BN>
-int input_gradient(const Matrix &da, const Matrix &db, const Matrix &wg, const Matrix &wu, const Matrix &dx, int dtype, int sms,
-                   cudaStream_t s)
-{
-    GemmArgs g{};
-    if (!add_operands<false, true, BN>(g, 0, da, wg, da.cols, dtype) || !add_operands<false, true, BN>(g, 1, db, wu, db.cols, dtype))
-        return A2SGD_ERR_CUDA;
-    add_problem(g, dx.rows, dx.cols, BN, 0, 2, const_cast<void *>(dx.p), dx.ld);
-    return launch_gemm<T, kStore, false, true, BN>(g, sms, s);
+    set_shape(g, shape, reinterpret_cast<float *>(pack.at));
+    if (!add_operands<false, false>(g, 0, ph, pd, dtype) || !set_rows(g.out[0], y, dtype)) return A2SGD_ERR_CUDA;
+    return launch_gemm<T, kStore, false, false>(g, add_problem(g, t, d, g.bn, 0, 1, f, 0), sms, s);
 }
 
 template <typename T>
@@ -612,42 +837,43 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
     }
     if (dwg.p || dwu.p) px = pack.usable(x);
     if (dwd.p) ph = pack.usable(h);
-    const uint64_t need = (uint64_t)(pack.at - static_cast<char *>(workspace));
-    if (need && (!workspace || workspace_bytes < need)) return A2SGD_ERR_ARG;
+    const Shape shape = dx.p ? pack.fit(shape_of(t, d, f, 2, true, sms), workspace_bytes) : Shape();
+    if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
     int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
 
     if (inner) {
         GemmArgs g{};
         g.act = act;
-        if (!add_operands<false, true, 256>(g, 0, pdy, pwd, d, dtype)) return A2SGD_ERR_CUDA;
-        add_problem(g, t, f, 256, 0, 1, const_cast<void *>(da.p), da.ld);
-        g.out2 = const_cast<void *>(db.p);
-        g.ldo2 = db.ld;
-        g.gate = const_cast<void *>(gate.p);
-        g.ld_gate = gate.ld;
-        g.up = const_cast<void *>(up.p);
-        g.ld_up = up.ld;
-        rc = launch_gemm<T, kGateGrad, false, true, 256>(g, sms, s);
+        set_shape(g, Shape(), nullptr);
+        if (!add_operands<false, true>(g, 0, pdy, pwd, dtype) || !set_rows(g.out[0], whole_rows(da), dtype) || !set_rows(g.out2, whole_rows(db), dtype) ||
+            !set_rows(g.gate, gate, dtype, false) || !set_rows(g.up, up, dtype, false))
+            return A2SGD_ERR_CUDA;
+        rc = launch_gemm<T, kGateGrad, false, true>(g, add_problem(g, t, f, g.bn, 0, 1, d, 0), sms, s);
         if (rc != A2SGD_OK) return rc;
     }
     if (dx.p) {
-        rc = tile_columns(t, d, sms) == 256 ? input_gradient<T, 256>(da, db, pwg, pwu, dx, dtype, sms, s)
-                                            : input_gradient<T, 128>(da, db, pwg, pwu, dx, dtype, sms, s);
+        GemmArgs g{};
+        set_shape(g, shape, reinterpret_cast<float *>(pack.at));
+        if (!add_operands<false, true>(g, 0, da, pwg, dtype) || !add_operands<false, true>(g, 1, db, pwu, dtype) ||
+            !set_rows(g.out[0], dx, dtype))
+            return A2SGD_ERR_CUDA;
+        rc = launch_gemm<T, kStore, false, true>(g, add_problem(g, t, d, g.bn, 0, 2, f, 0), sms, s);
         if (rc != A2SGD_OK) return rc;
     }
     if (dwg.p || dwu.p || dwd.p) {
         GemmArgs g{};
-        int i = 0;
+        set_shape(g, Shape(), nullptr);
+        int i = 0, tiles = 0;
         const auto add = [&](const Matrix &a, const Matrix &b, const Matrix &out) {
             if (!out.p) return true;
-            if (!add_operands<true, true, 256>(g, i, a, b, t, dtype)) return false;
-            add_problem(g, out.rows, out.cols, 256, i, 1, const_cast<void *>(out.p), out.ld);
+            if (!add_operands<true, true>(g, i, a, b, dtype) || !set_rows(g.out[i], out, dtype)) return false;
+            tiles = add_problem(g, out.rows, out.cols, g.bn, i, 1, t, tiles);
             ++i;
             return true;
         };
         if (!add(da, px, dwg) || !add(db, px, dwu) || !add(pdy, ph, dwd)) return A2SGD_ERR_CUDA;
-        rc = launch_gemm<T, kStore, true, true, 256>(g, sms, s);
+        rc = launch_gemm<T, kStore, true, true>(g, tiles, sms, s);
     }
     return rc;
 }
@@ -668,6 +894,8 @@ extern "C" uint64_t a2sgd_gated_ffn_workspace(uint64_t tokens, uint32_t d, uint3
         bytes += 2 * room(f, d) + room(d, f) + room(t, f) + room(t, d); // Wg, Wu, Wd, h, x
         if (flags & A2SGD_FFN_BACKWARD) bytes += room(t, d);            // dy
     }
+    // partial sums of the product that ends in [tokens, d], at the widest tile
+    if (tokens) bytes += partial_bytes(kMostPairs, d > 256 ? 512 : 256);
     return bytes;
 }
 

@@ -142,6 +142,25 @@ def test_forward_and_backward(t, d, f, dtype, act, pad, skew):
     p.check_edges()
 
 
+@pytest.mark.parametrize("t,d,f,pad", [(70, 777, 1001, 7), (300, 1601, 321, 7), (1, 9, 17, 7), (5, 1, 1, 7), (260, 130, 66, 6), (3, 61, 2045, 3)])
+def test_rows_of_odd_length_at_aligned_addresses(t, d, f, pad):
+    p = Block(t, d, f, torch.bfloat16, pad, 8)
+    p.forward("silu")
+    _check_forward(p, "silu")
+    _check_backward(p, "silu", p.backward("silu"))
+    p.check_edges()
+
+
+@pytest.mark.parametrize("t,d,f", [(1300, 1600, 640), (2500, 1344, 256), (9600, 512, 128), (4736, 1024, 192), (3000, 2048, 64),
+                                   (40, 1600, 4096), (700, 200, 8192)])
+def test_every_tile_width_and_split(t, d, f):
+    """Sizes whose best tiles are 64 to 512 columns wide, whole and split in depth."""
+    p = Block(t, d, f, torch.bfloat16)
+    p.forward("silu")
+    _check_forward(p, "silu")
+    _check_backward(p, "silu", p.backward("silu"))
+
+
 @pytest.mark.parametrize("dtype,act", [(torch.bfloat16, "gelu_tanh"), (torch.float16, "silu")])
 @pytest.mark.parametrize("t", [1, 2, 7, 8, 9, 16, 17, 33, 64, 65])
 def test_few_tokens_without_what_the_backward_pass_needs(t, dtype, act):
