@@ -36,14 +36,18 @@ namespace {
 constexpr int kBM = 256;                  // rows of a tile, 128 a CTA
 constexpr int kBK = 64;                   // depth of a slice: 128 bytes a row
 constexpr int kEpilogueWarps = 8;
-constexpr int kThreads = 64 + 32 * kEpilogueWarps;
+constexpr int kFirstEpilogueWarp = 3; // after A's loads, the products and B's loads
+constexpr int kThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
 constexpr uint32_t kABytes = 128 * kBK * 2;  // A's slice in one CTA
 constexpr uint32_t kChunk = 64 * kBK * 2;    // 64 columns of an MN-major slice
 constexpr uint32_t kTmemColumns = 512;
 constexpr uint32_t kStaging = 32 * 128;      // 32 rows of 64 columns on their way out: two for each epilogue warp
 constexpr uint32_t kSmem = 227 * 1024;
 constexpr int kMostStages = 8;
-constexpr uint32_t kOperands = kSmem - 1024 - 512 - kEpilogueWarps * 2 * kStaging; // room for the slices
+// Staging buffers of an epilogue warp: a plain output takes one, so that its slices have six stages.
+__host__ __device__ constexpr uint32_t staging_bytes(int epilogue) { return kEpilogueWarps * (epilogue == 0 ? 1 : 2) * kStaging; }
+// Room for the slices.
+__host__ __device__ constexpr uint32_t operand_bytes(int epilogue) { return (kSmem - 1024 - 512 - staging_bytes(epilogue)) / 1024 * 1024; }
 
 enum Epilogue { kStore = 0, kGate = 1, kGateGrad = 2 };
 
@@ -140,7 +144,6 @@ __device__ __forceinline__ void rows_out(const Rows &o, uint32_t buf, int row0, 
             for (int c = lane; c < min(64, n - col0); c += 32) p[c] = ld_shared16(piece(buf, r, c >> 3) + (c & 7) * 2);
         }
         __syncwarp();
-        if (lane == 0) tma_store_commit(); // an empty group: the buffers' turns are counted in groups
     }
 }
 __device__ __forceinline__ void rows_in(const Rows &o, uint32_t buf, int row0, int col0, int m, int n, uint32_t lane)
@@ -194,7 +197,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
 {
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t staging = base + kOperands / 1024 * 1024;
+    constexpr uint32_t kOperands = operand_bytes(EPI);
+    const uint32_t staging = base + kOperands;
     __shared__ __align__(8) uint64_t bars[2 * kMostStages + 4 + kEpilogueWarps];
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
@@ -229,71 +233,84 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     wait_prior_grid();
     release_next_grid();
 
-    if (warp == 0 && lane == 0) {
-        // ---------------------------------------------------------- operands in
+    if (warp == 0 || warp == 2) {
+        // ---------------------------------------------------------- operands in: warp 0 A's, warp 2 B's
+        // The warp walks the slices together, so that addresses stay in uniform registers; one thread issues.
+        const bool chosen = elect_one();
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        const uint32_t leader = map_to(full(0), 0);
+        const uint32_t leader = map_to(full(0), 0), stage_bytes = g.stage_bytes;
+        const int stages = g.stages;
         for (int i = pair; ok && i < g.items; i += pairs) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
-            const int row = t.tm * kBM + (int)rank * 128;
-            const int mine = EPI == kGate ? 128 : t.n_mma / 2;                   // columns of B in this CTA, a product
+            const int mine = EPI == kGate ? 128 : t.n_mma / 2; // columns of B in this CTA, a product
             const int loads = B_MN ? (mine + 63) / 64 : (mine + g.box - 1) / g.box;
             const uint32_t load_bytes = B_MN ? kChunk : g.box * 128u;
-            const int step = B_MN ? 64 : g.box;
-            const int mmas = EPI == kGate ? 1 : t.mmas;
-            const int col = EPI == kGate ? t.tn * 128 : t.tn * g.bn + (int)rank * mine;
-            const uint32_t bytes = 2 * (kABytes + (uint32_t)(mmas * loads) * load_bytes); // of both CTAs
-            int seg = q.seg, kb = t.k0;
-            while (kb >= g.seg_blocks[seg]) kb -= g.seg_blocks[seg++];
-            for (int k = t.k0; k < t.k1; ++k, ++kb) {
-                if (kb == g.seg_blocks[seg]) {
-                    kb = 0;
-                    ++seg;
-                }
-                ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
-                if (!ok) break;
+            const int total = (EPI == kGate ? 1 : t.mmas) * loads;
+            const uint32_t bytes = 2 * (kABytes + (uint32_t)total * load_bytes); // of both CTAs
+            const int row = t.tm * kBM + (int)rank * 128;
+            int at[4]; // B's columns, a load
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                at[j] = EPI == kGate ? t.tn * 128
+                                     : t.tn * g.bn + (int)rank * mine + (j / loads) * t.n_mma + (j % loads) * (B_MN ? 64 : g.box);
+            int k = t.k0, before = 0; // slices of the operand pairs before this one
+            for (int seg = q.seg; ok && k < t.k1; before += g.seg_blocks[seg++]) {
+                const int last = min(t.k1, before + g.seg_blocks[seg]);
                 const CUtensorMap *ma = &g.a[seg], *mb = EPI == kGate ? &g.b[rank] : &g.b[seg];
-                if (rank == 0) bar_expect(full(stage), bytes);
-                const uint32_t bar = leader + 8u * stage;
-                const uint32_t sa = base + stage * g.stage_bytes;
-                uint32_t sb = sa + kABytes;
-                if constexpr (A_MN) {
-                    tma_load_pair(sa, ma, row, kb * kBK, bar);
-                    tma_load_pair(sa + kChunk, ma, row + 64, kb * kBK, bar);
-                } else {
-                    tma_load_pair(sa, ma, kb * kBK, row, bar);
-                }
-                for (int h = 0; h < mmas; ++h) {
-                    for (int j = 0; j < loads; ++j, sb += load_bytes) {
-                        const int c = col + h * t.n_mma + j * step;
-                        if constexpr (B_MN) tma_load_pair(sb, mb, c, kb * kBK, bar);
-                        else tma_load_pair(sb, mb, kb * kBK, c, bar);
+                for (; k < last; ++k) {
+                    ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
+                    if (!ok) break;
+                    const uint32_t bar = leader + 8u * stage;
+                    const uint32_t sa = base + stage * stage_bytes, sb = sa + kABytes;
+                    const int depth = (k - before) * kBK;
+                    if (chosen) {
+                        if (warp == 0) {
+                            if (rank == 0) bar_expect(full(stage), bytes);
+                            if constexpr (A_MN) {
+                                tma_load_pair(sa, ma, row, depth, bar);
+                                tma_load_pair(sa + kChunk, ma, row + 64, depth, bar);
+                            } else {
+                                tma_load_pair(sa, ma, depth, row, bar);
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < (EPI == kGate ? 1 : 4); ++j) {
+                                if (j < total) {
+                                    if constexpr (B_MN) tma_load_pair(sb + j * kChunk, mb, at[j], depth, bar);
+                                    else tma_load_pair(sb + j * load_bytes, mb, depth, at[j], bar);
+                                }
+                            }
+                        }
                     }
-                }
-                if (++stage == g.stages) {
-                    stage = 0;
-                    phase ^= 1u;
+                    __syncwarp();
+                    if (++stage == stages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
                 }
             }
         }
         // every slice has been consumed: nothing is in flight towards this CTA any more
-        for (int s = 0; ok && s < g.stages; ++s) {
+        for (int s = 0; ok && s < stages; ++s) {
             ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
-            if (++stage == g.stages) {
+            if (++stage == stages) {
                 stage = 0;
                 phase ^= 1u;
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         // ---------------------------------------------------------- products
         constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         constexpr uint32_t kStepA = A_MN ? 16 * 128 : 32, kStepB = B_MN ? 16 * 128 : 32; // 16 of k further
+        const bool chosen = elect_one();
         int stage = 0, turn = 0;
         uint32_t phase = 0;
         bool ok = true;
+        const uint32_t stage_bytes = g.stage_bytes;
+        const int stages = g.stages;
         for (int i = pair; ok && i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
             const int acc = turn % accs;
@@ -310,28 +327,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                 ok = bar_wait(full(stage), phase, &gave_up);
                 if (!ok) break;
                 fence_after();
-                const uint32_t sa = base + stage * g.stage_bytes;
-                const uint64_t da = operand_desc(sa, A_MN ? kChunk : 16), db = operand_desc(sa + kABytes, B_MN ? kChunk : 16);
-                for (int h = 0; h < mmas; ++h) {
+                if (chosen) {
+                    const uint32_t sa = base + stage * stage_bytes;
+                    const uint64_t da = operand_desc(sa, A_MN ? kChunk : 16), db = operand_desc(sa + kABytes, B_MN ? kChunk : 16);
 #pragma unroll
                     for (int j = 0; j < kBK / 16; ++j)
-                        mma_pair(d + h * n_mma, da + j * (kStepA >> 4), db + ((h * second + j * kStepB) >> 4), desc, k > t.k0 || j > 0);
+                        mma_pair(d, da + j * (kStepA >> 4), db + j * (kStepB >> 4), desc, k > t.k0 || j > 0);
+                    if (mmas == 2) {
+#pragma unroll
+                        for (int j = 0; j < kBK / 16; ++j)
+                            mma_pair(d + n_mma, da + j * (kStepA >> 4), db + (second >> 4) + j * (kStepB >> 4), desc, k > t.k0 || j > 0);
+                    }
+                    commit_pair(empty(stage));
+                    if (k + 1 == t.k1) commit_pair(acc_full(acc));
                 }
-                commit_pair(empty(stage));
-                if (++stage == g.stages) {
+                __syncwarp();
+                if (++stage == stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
             }
-            commit_pair(acc_full(acc));
         }
-    } else if (warp >= 2) {
+    } else if (warp >= kFirstEpilogueWarp) {
         // ---------------------------------------------------------- accumulators out
-        const uint32_t quarter = warp & 3, half = (warp - 2) >> 2; // a warp reads the TMEM lanes of its quarter
-        const uint32_t buf0 = staging + (warp - 2) * 2 * kStaging, buf1 = buf0 + kStaging;
-        const uint32_t loaded = bar0 + 8u * (2 * kMostStages + 4 + (warp - 2));
+        const uint32_t quarter = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2; // a warp reads the TMEM lanes of its quarter
+        const uint32_t buf0 = staging + (warp - kFirstEpilogueWarp) * (EPI == kStore ? 1 : 2) * kStaging, buf1 = buf0 + kStaging;
+        const uint32_t loaded = bar0 + 8u * (2 * kMostStages + 4 + (warp - kFirstEpilogueWarp));
         int turn = 0;
-        uint32_t loads = 0, stores = 0;
+        uint32_t loads = 0;
         for (int i = pair; i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
@@ -446,9 +469,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                 const int subs = (min(t.cols, q.n - t.tn * g.bn) + 63) / 64;
                 for (int sub = half; live && sub < subs; sub += 2) {
                     const int col0 = t.tn * g.bn + sub * 64;
-                    const uint32_t buf = stores++ & 1 ? buf1 : buf0;
                     if (t.slot < 0) {
-                        if (lane == 0) tma_store_read<1>();
+                        if (lane == 0) tma_store_read<0>();
                         __syncwarp();
                     }
 #pragma unroll
@@ -458,7 +480,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                         tmem_wait_ld();
                         if (t.slot < 0) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) st_shared(piece(buf, lane, 4 * j + k), pack8<T>(v + 8 * k));
+                            for (int k = 0; k < 4; ++k) st_shared(piece(buf0, lane, 4 * j + k), pack8<T>(v + 8 * k));
                         } else if (sub * 64 + 32 * j < g.bn) {
                             // rows side by side: 512 consecutive bytes a warp and store
                             float4 *part = reinterpret_cast<float4 *>(g.partials) +
@@ -467,7 +489,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                             for (int k = 0; k < 8; ++k) part[k * kBM] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                         }
                     }
-                    if (t.slot < 0) rows_out(g.out[t.p], buf, row0, col0, q.m, q.n, lane);
+                    if (t.slot < 0) rows_out(g.out[t.p], buf0, row0, col0, q.m, q.n, lane);
                 }
                 fence_before();
                 __syncwarp();
@@ -667,7 +689,8 @@ int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
     g.whole = g.splits > 1 ? tiles / pairs * pairs : tiles;
     g.items = g.whole + (tiles - g.whole) * g.splits;
     g.stage_bytes = kABytes + (EPI == kGate ? 128u : (uint32_t)g.bn / 2) * 128u;
-    g.stages = (int)std::min<uint32_t>(kMostStages, kOperands / g.stage_bytes);
+    g.stages = (int)std::min<uint32_t>(kMostStages, operand_bytes(EPI) / g.stage_bytes);
+
     void *params[] = {&g};
     A2_TRAIN_CUDA(launch(fn, dim3(2 * (unsigned)std::min(g.items, pairs)), kThreads, kSmem - 1024, params, s));
     if (EPI == kStore && g.splits > 1)
