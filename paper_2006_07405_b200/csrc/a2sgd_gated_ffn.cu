@@ -159,8 +159,7 @@ __device__ __forceinline__ void rows_in(const Rows &o, uint32_t buf, int row0, i
 struct Item {
     int p, tm, tn;      // problem, tile
     int k0, k1;         // slices
-    int cols;           // columns of the product, a multiple of 32 (64 beyond 256), the tile's or less at the edge
-    int mmas, n_mma;    // products side by side and their width
+    int cols;           // columns of the product, a multiple of 32, the tile's or less at the edge
     int slot;           // of the partial sums; -1: the whole depth
 };
 
@@ -186,9 +185,6 @@ __device__ __forceinline__ Item item_at(const GemmArgs &g, int i)
     t.k0 = t.slot < 0 ? 0 : (int)((int64_t)q.k_blocks * part / g.splits);
     t.k1 = t.slot < 0 ? q.k_blocks : (int)((int64_t)q.k_blocks * (part + 1) / g.splits);
     t.cols = min(g.bn, (q.n - t.tn * g.bn + 31) / 32 * 32);
-    t.mmas = t.cols > 256 ? 2 : 1;
-    t.n_mma = t.cols > 256 ? (t.cols / 2 + 31) / 32 * 32 : t.cols;
-    t.cols = t.mmas * t.n_mma;
     return t;
 }
 
@@ -210,7 +206,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
 
     const uint32_t rank = cluster_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int accs = EPI == kGate || g.bn <= 256 ? 2 : 1; // accumulators of up to 256 columns alternate
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMostStages; ++s) {
             bar_init(full(s), 1);
@@ -245,17 +240,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         for (int i = pair; ok && i < g.items; i += pairs) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
-            const int mine = EPI == kGate ? 128 : t.n_mma / 2; // columns of B in this CTA, a product
-            const int loads = B_MN ? (mine + 63) / 64 : (mine + g.box - 1) / g.box;
+            const int mine = EPI == kGate ? 128 : t.cols / 2; // columns of B in this CTA
+            const int loads = B_MN && mine > 64 ? 2 : 1;
             const uint32_t load_bytes = B_MN ? kChunk : g.box * 128u;
-            const int total = (EPI == kGate ? 1 : t.mmas) * loads;
-            const uint32_t bytes = 2 * (kABytes + (uint32_t)total * load_bytes); // of both CTAs
+            const uint32_t bytes = 2 * (kABytes + (uint32_t)loads * load_bytes); // of both CTAs
             const int row = t.tm * kBM + (int)rank * 128;
-            int at[4]; // B's columns, a load
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                at[j] = EPI == kGate ? t.tn * 128
-                                     : t.tn * g.bn + (int)rank * mine + (j / loads) * t.n_mma + (j % loads) * (B_MN ? 64 : g.box);
+            const int col = EPI == kGate ? t.tn * 128 : t.tn * g.bn + (int)rank * mine;
             int k = t.k0, before = 0; // slices of the operand pairs before this one
             for (int seg = q.seg; ok && k < t.k1; before += g.seg_blocks[seg++]) {
                 const int last = min(t.k1, before + g.seg_blocks[seg]);
@@ -276,12 +266,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                                 tma_load_pair(sa, ma, depth, row, bar);
                             }
                         } else {
-#pragma unroll
-                            for (int j = 0; j < (EPI == kGate ? 1 : 4); ++j) {
-                                if (j < total) {
-                                    if constexpr (B_MN) tma_load_pair(sb + j * kChunk, mb, at[j], depth, bar);
-                                    else tma_load_pair(sb + j * load_bytes, mb, depth, at[j], bar);
-                                }
+                            if constexpr (B_MN) {
+                                tma_load_pair(sb, mb, col, depth, bar);
+                                if (loads == 2) tma_load_pair(sb + kChunk, mb, col + 64, depth, bar);
+                            } else {
+                                tma_load_pair(sb, mb, depth, col, bar);
                             }
                         }
                     }
@@ -313,15 +302,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         const int stages = g.stages;
         for (int i = pair; ok && i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
-            const int acc = turn % accs;
-            ok = bar_wait(acc_empty(acc), ((turn / accs) & 1) ^ 1, &gave_up);
+            const int acc = turn & 1;
+            ok = bar_wait(acc_empty(acc), ((turn >> 1) & 1) ^ 1, &gave_up);
             if (!ok) break;
             fence_after();
-            const int n_mma = EPI == kGate ? 256 : t.n_mma, mmas = EPI == kGate ? 1 : t.mmas;
-            const uint32_t desc = instruction_desc(kType, A_MN, B_MN, kBM, 0) | (uint32_t)(n_mma >> 3) << 17;
-            const uint32_t second = EPI == kGate ? 0
-                                    : B_MN       ? (uint32_t)(n_mma / 2 + 63) / 64 * kChunk
-                                                 : (uint32_t)((n_mma / 2 + g.box - 1) / g.box * g.box) * 128;
+            const uint32_t desc = EPI == kGate ? instruction_desc(kType, A_MN, B_MN, kBM, 256)
+                                               : instruction_desc(kType, A_MN, B_MN, kBM, 0) | (uint32_t)(t.cols >> 3) << 17;
             const uint32_t d = tmem + acc * 256;
             for (int k = t.k0; k < t.k1; ++k) {
                 ok = bar_wait(full(stage), phase, &gave_up);
@@ -333,11 +319,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
 #pragma unroll
                     for (int j = 0; j < kBK / 16; ++j)
                         mma_pair(d, da + j * (kStepA >> 4), db + j * (kStepB >> 4), desc, k > t.k0 || j > 0);
-                    if (mmas == 2) {
-#pragma unroll
-                        for (int j = 0; j < kBK / 16; ++j)
-                            mma_pair(d + n_mma, da + j * (kStepA >> 4), db + (second >> 4) + j * (kStepB >> 4), desc, k > t.k0 || j > 0);
-                    }
                     commit_pair(empty(stage));
                     if (k + 1 == t.k1) commit_pair(acc_full(acc));
                 }
@@ -358,12 +339,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         for (int i = pair; i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
-            const int acc = turn % accs;
+            const int acc = turn & 1;
             const int row0 = t.tm * kBM + (int)rank * 128 + quarter * 32; // this warp's 32 rows
             const bool live = row0 < q.m;
             const uint32_t d = tmem + acc * 256 + (quarter * 32u << 16);
             if constexpr (EPI == kGate) {
-                if (!bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up)) break;
+                if (!bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
                 fence_after();
                 const int c = half * 64, col0 = t.tn * 128 + c;
                 if (lane == 0) tma_store_read<0>();
@@ -428,7 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                         if (bytes) ok = ok && bar_wait(loaded, loads++ & 1, &gave_up);
                     }
                     if (!waited) {
-                        ok = ok && bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up);
+                        ok = ok && bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up);
                         fence_after();
                         waited = true;
                     }
@@ -459,12 +440,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                     rows_out(g.out2, buf1, row0, col0, q.m, q.n, lane);
                 }
                 if (!__all_sync(0xffffffffu, ok)) break;
-                if (!waited && !bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up)) break;
+                if (!waited && !bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
             } else {
-                if (!bar_wait(acc_full(acc), (turn / accs) & 1, &gave_up)) break;
+                if (!bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
                 fence_after();
                 const int subs = (min(t.cols, q.n - t.tn * g.bn) + 63) / 64;
                 for (int sub = half; live && sub < subs; sub += 2) {
@@ -481,7 +462,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                         if (t.slot < 0) {
 #pragma unroll
                             for (int k = 0; k < 4; ++k) st_shared(piece(buf0, lane, 4 * j + k), pack8<T>(v + 8 * k));
-                        } else if (sub * 64 + 32 * j < g.bn) {
+                        } else {
                             // rows side by side: 512 consecutive bytes a warp and store
                             float4 *part = reinterpret_cast<float4 *>(g.partials) +
                                            ((int64_t)t.slot * (g.bn / 4) + sub * 16 + 8 * j) * kBM + rank * 128 + quarter * 32 + lane;
@@ -510,7 +491,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     if (warp == 1) tmem_free_pair(tmem, kTmemColumns);
 }
 
-// The parts of the tiles that were split, added up in order.  One thread: a row, 8 columns.
+// The parts of the tiles that were split, added up in order.  One thread: a row, 4 columns.
 template <typename T>
 __global__ void __launch_bounds__(kBM) k_join(const __grid_constant__ GemmArgs g)
 {
@@ -518,21 +499,22 @@ __global__ void __launch_bounds__(kBM) k_join(const __grid_constant__ GemmArgs g
     release_next_grid();
     const Item t = item_at(g, g.whole + (int)blockIdx.x * g.splits);
     const Problem &q = g.problem[t.p];
-    const int row = t.tm * kBM + threadIdx.x, col = t.tn * g.bn + blockIdx.y * 8;
+    const int row = t.tm * kBM + threadIdx.x, col = t.tn * g.bn + blockIdx.y * 4;
     if (row >= q.m || col >= q.n) return;
-    float v[8] = {};
-    const float4 *part = reinterpret_cast<const float4 *>(g.partials) + ((int64_t)t.slot * (g.bn / 4) + blockIdx.y * 2) * kBM + threadIdx.x;
-    for (int s = 0; s < g.splits; ++s, part += (int64_t)(g.bn / 4) * kBM) {
-        const float4 x = __ldcg(part), y = __ldcg(part + kBM);
+    const int64_t next = (int64_t)(g.bn / 4) * kBM;
+    const float4 *part = reinterpret_cast<const float4 *>(g.partials) + (int64_t)t.slot * next + blockIdx.y * kBM + threadIdx.x;
+    float v[4] = {};
+#pragma unroll 8
+    for (int s = 0; s < g.splits; ++s) {
+        const float4 x = __ldcg(part + s * next);
         v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-        v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
     }
     T *out = static_cast<T *>(g.out[t.p].p) + (int64_t)row * g.out[t.p].ld + col;
-    if (g.out[t.p].tma && col + 8 <= q.n) {
-        *reinterpret_cast<uint4 *>(out) = pack8<T>(v);
+    if (g.out[t.p].tma && col + 4 <= q.n) {
+        *reinterpret_cast<uint2 *>(out) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (col + i < q.n) out[i] = from_f32<T>(v[i]);
         }
     }
@@ -626,20 +608,18 @@ Matrix whole_rows(Matrix m)
 }
 
 // ---- the shape of a launch ---------------------------------------------------------------------------
-// What a product's tiles cost, in clocks of a slice: the tensor cores take 2 a column, the way from L2 about
-// 42 bytes a clock and SM (measured: every shape of this kernel met 10 to 11 TB/s there), so that narrow
-// tiles, which bring in more for what they compute, are bound by the latter.
-inline double slice_clocks(int bn) { return std::max(2.0 * bn, (16384.0 + 64.0 * bn) / 42.0); }
+// What a slice of a tile costs, in clocks: the tensor cores take 2 a column, the way from L2 about 56 bytes a clock
+// and SM.  With [8192, 6400] x [1600, 6400]^T a round of tiles took 27, 33 and 37 us at 128, 192 and 256
+// columns: 459, 559, 624 clocks a slice against 439, 512 and 585 by this rule.
+inline double slice_clocks(int bn) { return std::max(2.0 * bn, (16384.0 + 64.0 * bn) / 56.0); }
 
 constexpr int kMostPairs = 80;  // pairs that take part in splitting: bounds the workspace
-constexpr int kLeastSlices = 8; // of a part of a tile
+constexpr int kLeastSlices = 4; // of a part of a tile
 
 struct Shape {
     int bn = 256, splits = 1;
     double cost = 1e30;
 };
-
-inline int64_t tiles_of(const Problem &q, int bn) { return (int64_t)ceil_div(q.m, kBM) * ceil_div(q.n, bn); }
 
 // Tiles that do not fill a last round over the pairs of SMs are split in depth, as evenly as the pairs allow.
 inline int splits_of(int64_t tiles, int pairs, int k_blocks)
@@ -649,23 +629,31 @@ inline int splits_of(int64_t tiles, int pairs, int k_blocks)
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(pairs, kMostPairs) / rest, k_blocks / kLeastSlices));
 }
 
-// One problem, plain output: the width and the splitting with the least cost.
-Shape choose(const Problem &q, bool b_mn, int pairs, bool may_split)
+// Products with plain outputs, all of the same depth: the width and the splitting with the least cost.
+struct Extent {
+    int64_t m;
+    int n;
+};
+Shape choose(const Extent *outs, int count, int k_blocks, bool b_mn, int pairs)
 {
     Shape best;
-    for (int bn : {64, 128, 192, 256, 320, 384, 448, 512}) { // whole staged blocks of 64 columns
-        if (b_mn && bn != 128 && bn != 256 && bn != 512) continue; // whole chunks of 64 columns in either CTA
-        if (bn > 128 && bn - 64 >= q.n) continue;
-        const int64_t tiles = tiles_of(q, bn);
-        const int splits = may_split ? splits_of(tiles, pairs, q.k_blocks) : 1;
-        const double rounds = (double)(tiles / pairs) + (tiles % pairs ? 1.0 / splits : 0.0);
-        // what is not overlapped: the last tile's way out, or every tile's beyond 256 columns; joining the parts
-        const double out = bn > 256 ? 12.0 * bn * std::ceil(rounds) : 12.0 * bn;
-        const double cost = rounds * q.k_blocks * slice_clocks(bn) + out + (splits > 1 ? 4000.0 + 20.0 * bn : 0.0);
-        if (cost < best.cost) {
-            best.bn = bn;
-            best.splits = splits;
-            best.cost = cost;
+    int widest = 0;
+    for (int i = 0; i < count; ++i) widest = std::max(widest, outs[i].n);
+    for (int bn : {64, 128, 192, 256}) {             // whole staged blocks of 64 columns
+        if (b_mn && bn != 128 && bn != 256) continue; // whole chunks of 64 columns in either CTA
+        if (bn > 128 && bn - 64 >= widest) continue;
+        int64_t tiles = 0;
+        for (int i = 0; i < count; ++i) tiles += (int64_t)ceil_div(outs[i].m, kBM) * ceil_div(outs[i].n, bn);
+        for (int splits : {1, splits_of(tiles, pairs, k_blocks)}) {
+            const double rounds = (double)(tiles / pairs) + (tiles % pairs ? 1.0 / splits : 0.0);
+            // and the last tile's way out, and joining the parts: a launch, and their bytes through L2
+            const double join = splits > 1 ? 6000.0 + (double)(tiles % pairs) * splits * 2.0 * kBM * bn * 4 / (148 * 40.0) : 0.0;
+            const double cost = rounds * k_blocks * slice_clocks(bn) + 12.0 * bn + join;
+            if (cost < best.cost) {
+                best.bn = bn;
+                best.splits = splits;
+                best.cost = cost;
+            }
         }
     }
     return best;
@@ -685,7 +673,7 @@ int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
         A2_TRAIN_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024)));
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    const int pairs = std::max(1, sms / 2);
+    const int pairs = sms / 2;
     g.whole = g.splits > 1 ? tiles / pairs * pairs : tiles;
     g.items = g.whole + (tiles - g.whole) * g.splits;
     g.stage_bytes = kABytes + (EPI == kGate ? 128u : (uint32_t)g.bn / 2) * 128u;
@@ -694,7 +682,7 @@ int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
     void *params[] = {&g};
     A2_TRAIN_CUDA(launch(fn, dim3(2 * (unsigned)std::min(g.items, pairs)), kThreads, kSmem - 1024, params, s));
     if (EPI == kStore && g.splits > 1)
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / 8)), kBM, 0,
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / 4)), kBM, 0,
                              params, s));
     return A2SGD_OK;
 }
@@ -725,19 +713,9 @@ int add_problem(GemmArgs &g, int64_t m, int n, int tile_n, int seg, int segs, in
 void set_shape(GemmArgs &g, const Shape &shape, float *partials)
 {
     g.bn = shape.bn;
-    g.box = shape.bn > 256 ? shape.bn / 4 : shape.bn / 2;
+    g.box = shape.bn / 2;
     g.splits = shape.splits;
     g.partials = partials;
-}
-
-// Shapes of the two products with plain outputs of [tokens, d]: they may need room for partial sums.
-Shape shape_of(int64_t m, int n, int64_t k, int segs, bool b_mn, int sms)
-{
-    Problem q{};
-    q.m = (int)m;
-    q.n = n;
-    q.k_blocks = segs * ceil_div(k, kBK);
-    return choose(q, b_mn, std::max(1, sms / 2), true);
 }
 
 struct Packer {
@@ -813,7 +791,8 @@ int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &w
         ph.ld = padded(h.cols);
         ph.p = pack.take(h.rows, h.cols);
     }
-    const Shape shape = pack.fit(shape_of(t, d, f, 1, false, sms), workspace_bytes);
+    const Extent out{t, d};
+    const Shape shape = pack.fit(choose(&out, 1, ceil_div(f, kBK), false, sms / 2), workspace_bytes);
     if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
     int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
@@ -860,7 +839,15 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
     }
     if (dwg.p || dwu.p) px = pack.usable(x);
     if (dwd.p) ph = pack.usable(h);
-    const Shape shape = dx.p ? pack.fit(shape_of(t, d, f, 2, true, sms), workspace_bytes) : Shape();
+    const Extent out{t, d};
+    const Shape shape = dx.p ? pack.fit(choose(&out, 1, 2 * ceil_div(f, kBK), true, sms / 2), workspace_bytes) : Shape();
+    Extent weights[3];
+    int weight_count = 0;
+    for (const Matrix *w : {&dwg, &dwu, &dwd}) {
+        if (w->p) weights[weight_count++] = Extent{w->rows, w->cols};
+    }
+    const Shape weight_shape =
+        weight_count ? pack.fit(choose(weights, weight_count, ceil_div(t, kBK), true, sms / 2), workspace_bytes) : Shape();
     if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
     int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
@@ -884,9 +871,9 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
         rc = launch_gemm<T, kStore, false, true>(g, add_problem(g, t, d, g.bn, 0, 2, f, 0), sms, s);
         if (rc != A2SGD_OK) return rc;
     }
-    if (dwg.p || dwu.p || dwd.p) {
+    if (weight_count) {
         GemmArgs g{};
-        set_shape(g, Shape(), nullptr);
+        set_shape(g, weight_shape, reinterpret_cast<float *>(pack.at));
         int i = 0, tiles = 0;
         const auto add = [&](const Matrix &a, const Matrix &b, const Matrix &out) {
             if (!out.p) return true;
@@ -917,8 +904,7 @@ extern "C" uint64_t a2sgd_gated_ffn_workspace(uint64_t tokens, uint32_t d, uint3
         bytes += 2 * room(f, d) + room(d, f) + room(t, f) + room(t, d); // Wg, Wu, Wd, h, x
         if (flags & A2SGD_FFN_BACKWARD) bytes += room(t, d);            // dy
     }
-    // partial sums of the product that ends in [tokens, d], at the widest tile
-    if (tokens) bytes += partial_bytes(kMostPairs, d > 256 ? 512 : 256);
+    if (tokens) bytes += partial_bytes(kMostPairs, 256); // partial sums of tiles that are split, at the widest
     return bytes;
 }
 
@@ -943,7 +929,7 @@ extern "C" int a2sgd_gated_ffn_forward(const void *x, int64_t x_stride, const vo
     if (!aligned(workspace, 256)) return A2SGD_ERR_ALIGN;
     DeviceGuard guard(device);
     const int sms = guard.ok ? sm_count(device) : 0;
-    if (sms == 0) return A2SGD_ERR_CUDA;
+    if (sms < 2) return A2SGD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return dtype == A2SGD_BF16
                ? forward<__nv_bfloat16>(mx, mg, mu, md, my, mh, ma, mb, activation, dtype, workspace, workspace_bytes, sms, s)
@@ -977,7 +963,7 @@ extern "C" int a2sgd_gated_ffn_backward(const void *dy, int64_t dy_stride, const
     if (!aligned(workspace, 256)) return A2SGD_ERR_ALIGN;
     DeviceGuard guard(device);
     const int sms = guard.ok ? sm_count(device) : 0;
-    if (sms == 0) return A2SGD_ERR_CUDA;
+    if (sms < 2) return A2SGD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (tokens == 0) { // no tokens: the weights' gradients are zero
         for (const Matrix *m : {&odg, &odu, &odd}) {
