@@ -543,6 +543,174 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
     }
 }
 
+// ------------------------------------------------------------------ few tokens
+// Up to 32 tokens the block is bound by the weights' bytes, and tiles of 256 rows would be nearly empty.  Here
+// the weights are the left operand, 16 of their rows a CTA, and stream from memory straight into the
+// registers of mma.sync (m16n8k16): a lane loads 16 bytes, 8 consecutive k of one row, and since the order of k
+// within a product is free as long as both operands share it, those 8 are the lane's part of two products; the
+// tokens' 8 k lie the same way.  Eight warps, and the CTAs of a cluster, share the depth; their sums meet in shared
+// memory, in order, where the gate, the activation and the product are applied.
+constexpr int kFewTokens = 32;
+constexpr int kFewWarps = 8;
+constexpr int kFewUnroll = 4; // steps of 32 k whose loads are in flight together
+
+struct FewArgs {
+    const void *w0, *w1; // w1: the second projection, side by side with w0
+    const void *x;
+    int64_t ld0, ld1, ldx;
+    int rows, depth, tokens; // rows of the weights = columns of the output
+    int act;
+    void *out, *gate, *up;
+    int64_t ldo, ld_gate, ld_up;
+    int parts; // CTAs of a cluster
+};
+
+template <typename T>
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 8 elements of a row from k on; zeros past its end and where the row does not exist.
+template <bool VEC>
+__device__ __forceinline__ uint4 few_load(const uint16_t *row, int k, int depth, bool live)
+{
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (!live || k >= depth) return q;
+    if (VEC && k + 8 <= depth) return ld_stream(row + k);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (k + i < depth) w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T, bool DUAL, int NT, bool VEC>
+__global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ FewArgs g)
+{
+    constexpr int kSides = DUAL ? 2 : 1;
+    constexpr int kCols = 8 * NT;
+    __shared__ float sums[kFewWarps][kSides][16][kCols + 1];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, c = lane & 3;
+    const int part = blockIdx.x % g.parts, row0 = blockIdx.x / g.parts * 16;
+    const int steps = (g.depth + 31) / 32, share = part * kFewWarps + warp, shares = g.parts * kFewWarps;
+    const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
+
+    if constexpr (DUAL) {
+        wait_prior_grid();
+        release_next_grid();
+    }
+    float acc[kSides][NT][4] = {};
+    const bool live0 = row0 + (int)quad < g.rows, live1 = row0 + 8 + (int)quad < g.rows;
+    const uint16_t *wr[kSides][2];
+    wr[0][0] = static_cast<const uint16_t *>(g.w0) + (int64_t)(row0 + quad) * g.ld0;
+    wr[0][1] = wr[0][0] + 8 * g.ld0;
+    if constexpr (DUAL) {
+        wr[1][0] = static_cast<const uint16_t *>(g.w1) + (int64_t)(row0 + quad) * g.ld1;
+        wr[1][1] = wr[1][0] + 8 * g.ld1;
+    }
+    const uint16_t *xr = static_cast<const uint16_t *>(g.x) + (int64_t)quad * g.ldx;
+    bool waited = false;
+    for (int s = s0; s < s1 || !waited; s += kFewUnroll) {
+        uint4 w[kFewUnroll][kSides][2], x[kFewUnroll][NT];
+#pragma unroll
+        for (int u = 0; u < kFewUnroll; ++u) {
+            const int k = (s + u) * 32 + (int)c * 8;
+            const bool in = s + u < s1;
+#pragma unroll
+            for (int e = 0; e < kSides; ++e) {
+                w[u][e][0] = few_load<VEC>(wr[e][0], k, g.depth, in && live0);
+                w[u][e][1] = few_load<VEC>(wr[e][1], k, g.depth, in && live1);
+            }
+        }
+        if (!waited) {
+            // Weights are not written by the launch before this one, which is the block's own (or, for the first
+            // launch of a call, has been waited for): they are on their way while it ends.
+            if constexpr (!DUAL) {
+                wait_prior_grid();
+                release_next_grid();
+            }
+            waited = true;
+        }
+#pragma unroll
+        for (int u = 0; u < kFewUnroll; ++u) {
+            const int k = (s + u) * 32 + (int)c * 8;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                x[u][n] = few_load<VEC>(xr + (int64_t)n * 8 * g.ldx, k, g.depth, s + u < s1 && n * 8 + (int)quad < g.tokens);
+        }
+#pragma unroll
+        for (int u = 0; u < kFewUnroll; ++u) {
+#pragma unroll
+            for (int e = 0; e < kSides; ++e) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 a = w[u][e][0], b = w[u][e][1];
+                    mma_16816<T>(acc[e][n], a.x, b.x, a.y, b.y, x[u][n].x, x[u][n].y);
+                    mma_16816<T>(acc[e][n], a.z, b.z, a.w, b.w, x[u][n].z, x[u][n].w);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < kSides; ++e) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[warp][e][quad + 8 * (i >> 1)][n * 8 + 2 * c + (i & 1)] = acc[e][n][i];
+        }
+    }
+    __syncthreads();
+    // this CTA's sums into its first warp's places
+    for (int i = threadIdx.x; i < kSides * 16 * kCols; i += 32 * kFewWarps) {
+        const int e = i / (16 * kCols), r = i / kCols % 16, n = i % kCols;
+        float v = sums[0][e][r][n];
+#pragma unroll
+        for (int k = 1; k < kFewWarps; ++k) v += sums[k][e][r][n];
+        sums[0][e][r][n] = v;
+    }
+    if (g.parts > 1) cluster_sync();
+    else __syncthreads();
+    // every CTA of the cluster finishes its share of the outputs
+    for (int i = part * 32 * kFewWarps + threadIdx.x; i < 16 * kCols; i += g.parts * 32 * kFewWarps) {
+        const int r = i % 16, n = i / 16;
+        if (n >= g.tokens || row0 + r >= g.rows) continue;
+        float v[kSides];
+#pragma unroll
+        for (int e = 0; e < kSides; ++e) {
+            v[e] = 0.0f;
+            const uint32_t at = smem_u32(&sums[0][e][r][n]);
+            for (int p = 0; p < g.parts; ++p) {
+                float y;
+                if (g.parts > 1) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(map_to(at, p)) : "memory");
+                else y = sums[0][e][r][n];
+                v[e] += y;
+            }
+        }
+        const int col = row0 + r;
+        if constexpr (DUAL) {
+            float value, slope;
+            activation(g.act, v[0], value, slope);
+            static_cast<T *>(g.out)[(int64_t)n * g.ldo + col] = from_f32<T>(value * v[1]);
+            if (g.gate) {
+                static_cast<T *>(g.gate)[(int64_t)n * g.ld_gate + col] = from_f32<T>(v[0]);
+                static_cast<T *>(g.up)[(int64_t)n * g.ld_up + col] = from_f32<T>(v[1]);
+            }
+        } else {
+            static_cast<T *>(g.out)[(int64_t)n * g.ldo + col] = from_f32<T>(v[0]);
+        }
+    }
+    if (g.parts > 1) cluster_sync(); // no CTA leaves while another reads its sums
+}
+
 // ------------------------------------------------------------------ host
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -778,6 +946,54 @@ int check_sizes(uint64_t tokens, uint32_t d, uint32_t f, int dtype, int act)
     return A2SGD_OK;
 }
 
+template <typename T, bool DUAL, bool VEC>
+const void *pick_few(int tokens)
+{
+    return tokens <= 8    ? reinterpret_cast<const void *>(&k_few<T, DUAL, 1, VEC>)
+           : tokens <= 16 ? reinterpret_cast<const void *>(&k_few<T, DUAL, 2, VEC>)
+                          : reinterpret_cast<const void *>(&k_few<T, DUAL, 4, VEC>);
+}
+
+template <typename T, bool DUAL>
+int launch_few(FewArgs &g, bool vec, int sms, cudaStream_t s)
+{
+    const void *fn = vec ? pick_few<T, DUAL, true>(g.tokens) : pick_few<T, DUAL, false>(g.tokens);
+    // the depth is shared out over a cluster until there are two CTAs an SM, as long as a warp keeps two steps
+    const int groups = ceil_div(g.rows, 16), steps = ceil_div(g.depth, 32);
+    g.parts = 1;
+    while (g.parts < 8 && groups * g.parts < 2 * sms && steps >= g.parts * 2 * kFewWarps * 2) g.parts *= 2;
+    void *params[] = {&g};
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(groups * g.parts)), 32 * kFewWarps, 0, params, s, (unsigned)g.parts));
+    return A2SGD_OK;
+}
+
+template <typename T>
+int forward_few(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &wd, const Matrix &y, const Matrix &h,
+                const Matrix &gate, const Matrix &up, int act, int sms, cudaStream_t s)
+{
+    FewArgs g{};
+    g.w0 = wg.p, g.ld0 = wg.ld;
+    g.w1 = wu.p, g.ld1 = wu.ld;
+    g.x = x.p, g.ldx = x.ld;
+    g.rows = h.cols;
+    g.depth = x.cols;
+    g.tokens = (int)x.rows;
+    g.act = act;
+    g.out = const_cast<void *>(h.p), g.ldo = h.ld;
+    g.gate = const_cast<void *>(gate.p), g.ld_gate = gate.ld;
+    g.up = const_cast<void *>(up.p), g.ld_up = up.ld;
+    const int rc = launch_few<T, true>(g, tma_ok(wg) && tma_ok(wu) && tma_ok(x), sms, s);
+    if (rc != A2SGD_OK) return rc;
+    g = FewArgs{};
+    g.w0 = wd.p, g.ld0 = wd.ld;
+    g.x = h.p, g.ldx = h.ld;
+    g.rows = y.cols;
+    g.depth = h.cols;
+    g.tokens = (int)x.rows;
+    g.out = const_cast<void *>(y.p), g.ldo = y.ld;
+    return launch_few<T, false>(g, tma_ok(wd) && tma_ok(h), sms, s);
+}
+
 template <typename T>
 int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &wd, Matrix y, Matrix h, Matrix gate, Matrix up, int act,
             int dtype, void *workspace, uint64_t workspace_bytes, int sms, cudaStream_t s)
@@ -793,7 +1009,8 @@ int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &w
     }
     const Extent out{t, d};
     const Shape shape = pack.fit(choose(&out, 1, ceil_div(f, kBK), false, sms / 2), workspace_bytes);
-    if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
+    if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG; // for few tokens too, so that what is refused does not go by their number
+    if (t <= kFewTokens) return forward_few<T>(x, wg, wu, wd, y, h, gate, up, act, sms, s);
     int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
 

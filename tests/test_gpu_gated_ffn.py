@@ -164,9 +164,11 @@ def test_every_tile_width_and_split(t, d, f):
 @pytest.mark.parametrize("dtype,act", [(torch.bfloat16, "gelu_tanh"), (torch.float16, "silu")])
 @pytest.mark.parametrize("t", [1, 2, 7, 8, 9, 16, 17, 33, 64, 65])
 def test_few_tokens_without_what_the_backward_pass_needs(t, dtype, act):
-    p = Block(t, 328, 1100, dtype, seed=t)
-    p.forward(act, train=False)
-    _check_forward(p, act)
+    for pad in (0, 1):
+        p = Block(t, 328, 1100, dtype, pad, seed=t)
+        p.forward(act, train=False)
+        _check_forward(p, act)
+        p.check_edges()
 
 
 @pytest.mark.parametrize("only", [("dx",), ("dwg",), ("dwu", "dwd"), ("dwd",), ()])
