@@ -510,36 +510,42 @@ def _dtype_code(t: torch.Tensor, name: str) -> int:
     return code
 
 
-def _matrix(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.device) -> Tuple[int, int]:
+# The calls below are short enough for the host's share to count (a layer norm of few rows takes less time on the
+# device than its launch): one pass over each tensor's properties, devices as indices.
+
+def _matrix(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> Tuple[int, int]:
     """CUDA [rows, columns] with unit inner stride -> (address, row stride in elements)."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
-        raise ValueError(f"{name}: need a {dtype} tensor {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        raise ValueError(f"{name}: need a {dtype} tensor {list(shape)} on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
     stride, inner = t.stride()
-    if shape[1] > 1 and inner != 1:
+    if inner != 1 and shape[1] > 1:
         raise ValueError(f"{name}: need unit inner stride")
     return t.data_ptr(), stride
 
 
-def _vector(t: Optional[torch.Tensor], name: str, numel: int, dtype, device: torch.device) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], name: str, numel: int, dtype, index: int) -> Optional[int]:
     """A contiguous CUDA tensor of ``numel`` elements (or None) -> address."""
     if t is None:
         return None
-    if (dtype is not None and t.dtype != dtype) or t.device != device or t.numel() != numel or not t.is_contiguous():
-        raise ValueError(f"{name}: need a contiguous tensor of {numel} elements of {dtype} on {device}, got {t.dtype} "
+    if t.dtype is not dtype or t.get_device() != index or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous tensor of {numel} elements of {dtype} on cuda:{index}, got {t.dtype} "
                          f"{list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _stream_on(device: torch.device, stream) -> int:
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # torch.cuda.current_stream without its wrapper: 0.1 us
+
+
+def _stream_on(index: int, stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream
+        return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
     return _stream(stream)
 
 
-def _cuda_device(t: torch.Tensor, name: str) -> torch.device:
+def _cuda_index(t: torch.Tensor, name: str) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name}: need a CUDA tensor")
-    return t.device
+    return t.get_device()
 
 
 def a2sgd_adamw_state_elements(params) -> int:
@@ -556,12 +562,12 @@ class AdamW:
         S = len(params)
         if S == 0 or len(grads) != S or (w16 is not None and len(w16) != S):
             raise ValueError("params, grads and w16: need lists of the same length, at least 1")
-        self.device = _cuda_device(params[0], "params")
+        self.device = _cuda_index(params[0], "params")
 
         def table(tensors, name, dtype):
             for t, p in zip(tensors, params):
-                if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or t.numel() != p.numel():
-                    raise ValueError(f"{name}: need contiguous {dtype} tensors on {self.device}, as long as the parameters")
+                if t.dtype != dtype or t.get_device() != self.device or not t.is_contiguous() or t.numel() != p.numel():
+                    raise ValueError(f"{name}: need contiguous {dtype} tensors on cuda:{self.device}, as long as the parameters")
             return (_vp * S)(*[t.data_ptr() for t in tensors])
 
         w_tab = table(params, "params", torch.float32)
@@ -586,7 +592,7 @@ class AdamW:
         numel = (ctypes.c_uint64 * S)(*[p.numel() for p in params])
         self._h = _vp()
         _check(lib().a2sgd_adamw_create(ctypes.byref(self._h), S, numel, w_tab, g_tab, g_code, w16_tab, w16_code,
-                                        self.state_bits, m_ptr, v_ptr, ms_ptr, vs_ptr, self.device.index),
+                                        self.state_bits, m_ptr, v_ptr, ms_ptr, vs_ptr, self.device),
                "a2sgd_adamw_create")
 
     @property
@@ -661,17 +667,17 @@ def a2sgd_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bi
                              eps: float = 1e-5, stream=None) -> None:
     """x, y: CUDA [rows, d], unit inner stride (y may be x); weight, bias: [d] of float32 or x's type, or None;
     mean, rstd: float32 [rows], out, or None."""
-    dev, code = _cuda_device(x, "x"), _dtype_code(x, "x")
+    dev, code = _cuda_index(x, "x"), _dtype_code(x, "x")
     if x.dim() != 2:
         raise ValueError("x: need [rows, d]")
-    shape = rows, d = tuple(x.shape)
+    shape = rows, d = x.shape
     pt = _param_dtype(x, weight, bias)
     xp, xs = _matrix(x, "x", shape, x.dtype, dev)
     yp, ys = _matrix(y, "y", shape, x.dtype, dev)
     _check(lib().a2sgd_layer_norm_forward(
         xp, xs, code, _vector(weight, "weight", d, pt, dev), _vector(bias, "bias", d, pt, dev),
         _DTYPE_CODES.get(pt, -1), yp, ys, _vector(mean, "mean", rows, torch.float32, dev),
-        _vector(rstd, "rstd", rows, torch.float32, dev), rows, d, eps, dev.index, _stream_on(dev, stream)),
+        _vector(rstd, "rstd", rows, torch.float32, dev), rows, d, eps, dev, _stream_on(dev, stream)),
         "a2sgd_layer_norm_forward")
 
 
@@ -686,10 +692,10 @@ def a2sgd_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optiona
                               dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """dx (may be dy or x), dweight, dbias: out, each may be None; workspace: uint8 CUDA tensor of
     a2sgd_layer_norm_workspace bytes, needed for dweight or dbias."""
-    dev, code = _cuda_device(x, "x"), _dtype_code(x, "x")
+    dev, code = _cuda_index(x, "x"), _dtype_code(x, "x")
     if x.dim() != 2:
         raise ValueError("x: need [rows, d]")
-    shape = rows, d = tuple(x.shape)
+    shape = rows, d = x.shape
     pt = _param_dtype(x, weight, dweight, dbias)
     xp, xs = _matrix(x, "x", shape, x.dtype, dev)
     gp, gs = _matrix(dy, "dy", shape, x.dtype, dev)
@@ -699,7 +705,7 @@ def a2sgd_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optiona
         gp, gs, xp, xs, code, _vector(weight, "weight", d, pt, dev), _DTYPE_CODES.get(pt, -1),
         _vector(mean, "mean", rows, torch.float32, dev), _vector(rstd, "rstd", rows, torch.float32, dev), op, os_,
         _vector(dweight, "dweight", d, pt, dev), _vector(dbias, "dbias", d, pt, dev), rows, d,
-        _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev.index, _stream_on(dev, stream)),
+        _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev, _stream_on(dev, stream)),
         "a2sgd_layer_norm_backward")
 
 
@@ -715,8 +721,8 @@ def a2sgd_gated_ffn_workspace(tokens: int, d: int, f: int, backward: bool = Fals
 
 
 def _ffn_sizes(x: torch.Tensor, w_gate: torch.Tensor, activation: str):
-    dev = _cuda_device(x, "x")
-    if x.dtype not in (torch.bfloat16, torch.float16):
+    dev = _cuda_index(x, "x")
+    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float16:
         raise ValueError(f"x: need bfloat16 or float16, got {x.dtype}")
     if x.dim() != 2 or w_gate.dim() != 2:
         raise ValueError("x, w_gate: need matrices")
@@ -744,7 +750,7 @@ def a2sgd_gated_ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.T
         *_matrix(y, "y", (t, d), dt, dev), *_matrix(hidden, "hidden", (t, f), dt, dev),
         *_optional_matrix(gate, "gate", (t, f), dt, dev), *_optional_matrix(up, "up", (t, f), dt, dev),
         _DTYPE_CODES[dt], _ACTIVATIONS[activation], t, d, f, _vector(workspace, "workspace", wb, torch.uint8, dev), wb,
-        dev.index, _stream_on(dev, stream)), "a2sgd_gated_ffn_forward")
+        dev, _stream_on(dev, stream)), "a2sgd_gated_ffn_forward")
 
 
 def a2sgd_gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
@@ -764,13 +770,13 @@ def a2sgd_gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Te
         *_optional_matrix(dx, "dx", (t, d), dt, dev), *_optional_matrix(dw_gate, "dw_gate", (f, d), dt, dev),
         *_optional_matrix(dw_up, "dw_up", (f, d), dt, dev), *_optional_matrix(dw_down, "dw_down", (d, f), dt, dev),
         _DTYPE_CODES[dt], _ACTIVATIONS[activation], t, d, f, _vector(workspace, "workspace", wb, torch.uint8, dev), wb,
-        dev.index, _stream_on(dev, stream)), "a2sgd_gated_ffn_backward")
+        dev, _stream_on(dev, stream)), "a2sgd_gated_ffn_backward")
 
 
 def a2sgd_gated_ffn_status(device: Optional[int] = None, stream=None) -> int:
     """Synchronises the stream; the status that the block's kernels latched on the device (OK or ERR_TIMEOUT), cleared."""
     device = torch.cuda.current_device() if device is None else int(device)
     st = ctypes.c_int(0)
-    _check(lib().a2sgd_gated_ffn_status(device, ctypes.byref(st), _stream_on(torch.device("cuda", device), stream)),
+    _check(lib().a2sgd_gated_ffn_status(device, ctypes.byref(st), _stream_on(device, stream)),
            "a2sgd_gated_ffn_status")
     return st.value
