@@ -44,63 +44,91 @@ struct LnArgs {
     uint32_t parts;
 };
 
-// N sums over the threads of a group, the same in each of them.  A group of up to 32 threads (a power
-// of two) is part of a warp; a larger one is a whole number of warps and takes one barrier of the CTA.
-// Two buffers in turn: a warp that runs ahead writes the other one, and meets the barrier before it
-// comes back to the first.
+// N sums (a power of two) over the threads of a group, the same in each of them.  A group of up to 32 threads
+// (a power of two) is part of a warp; a larger one is a whole number of warps and takes one barrier of the CTA.
+// Within a warp the values are folded across lanes, half of them going each way, until a lane holds one: N = 8
+// takes 9 shuffles in place of 40.  Two buffers in turn: a warp that runs ahead writes the other one, and meets the
+// barrier before it comes back to the first.
 template <int N>
 struct GroupSum {
-    float *sh; // [2][groups][warps of a group][N]
+    float *sh; // [2][warps of the CTA][N]
     uint32_t tpr, warps, in_group, group;
     int turn = 0;
-    __device__ __forceinline__ void operator()(float (&v)[N])
+    // v <- finish(sums).  With a whole warp or more, a lane holds sum number lane % N (or lane / (32 / N)) before they
+    // are handed round, and `finish` is applied to that one only.
+    template <typename F>
+    __device__ __forceinline__ void operator()(float (&v)[N], F finish)
     {
-        const uint32_t width = tpr < 32 ? tpr : 32;
-        for (uint32_t o = width / 2; o; o >>= 1) {
+        const uint32_t lane = threadIdx.x & 31;
+        if (tpr < 32) {
+            for (uint32_t o = tpr / 2; o; o >>= 1) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+                for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = finish(v[i]);
+            return;
         }
-        if (tpr <= 32) return;
-        float *slot = sh + (uint32_t)turn * (kMaxThreads / 32) * N + group * warps * N;
+        int o = 16;
+#pragma unroll
+        for (int n = N / 2; n; n >>= 1, o >>= 1) {
+            const bool upper = lane & o;
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const float send = upper ? v[i] : v[n + i];
+                v[i] = (upper ? v[n + i] : v[i]) + __shfl_xor_sync(0xffffffffu, send, o);
+            }
+        }
+        float x = v[0];
+#pragma unroll
+        for (; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        // x: sum number lane / (32 / N)
+        if (tpr == 32) {
+            x = finish(x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x, i * (32 / N));
+            return;
+        }
+        float *slot = sh + ((uint32_t)turn * (kRowThreads / 32) + group * warps) * N;
         turn ^= 1;
-        if ((in_group & 31) == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) slot[(in_group >> 5) * N + i] = v[i];
-        }
+        if (lane % (32 / N) == 0) slot[(in_group >> 5) * N + lane / (32 / N)] = x;
         __syncthreads();
+        x = lane < warps * N ? slot[lane] : 0.0f;
+        for (uint32_t k = lane + 32; k < warps * N; k += 32) x += slot[k];
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.0f;
-        for (uint32_t k = 0; k < warps; ++k) {
+        for (int q = N; q < 32; q <<= 1) x += __shfl_xor_sync(0xffffffffu, x, q);
+        x = finish(x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += slot[k * N + i];
-        }
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x, i);
     }
 };
 
-// A thread's NC columns of one row.  VEC: eight consecutive ones at a time (column c0 = (k tpr + t) 8);
-// else every tpr-th one.
+// The columns of a thread.  VEC: eight consecutive ones at a time, from (k tpr + t) 8 on; else every tpr-th one from t on.
+template <int NC, bool VEC>
+__device__ __forceinline__ uint32_t column(int i, uint32_t t, uint32_t tpr)
+{
+    return VEC ? ((i / 8) * tpr + t) * 8 + (i & 7) : i * tpr + t;
+}
+
+// A thread's columns of one row; `row` points at its first one, `left` is the number of columns from there on.
 template <typename T, int NC, bool VEC>
 struct RowPart {
     Raw8<T> raw[VEC ? NC / 8 : 1];
     T one[VEC ? 1 : NC];
-    __device__ __forceinline__ void load(const T *row, uint32_t d, uint32_t t, uint32_t tpr, bool live)
+    __device__ __forceinline__ void load(const T *row, int left, uint32_t tpr, bool live)
     {
         if constexpr (VEC) {
 #pragma unroll
             for (int k = 0; k < NC / 8; ++k) {
-                const uint32_t c = (k * tpr + t) * 8;
-                if (live && c < d) raw[k].load(row + c);
+                if (live && (int)(k * tpr * 8) < left) raw[k].load(row + k * tpr * 8);
                 else raw[k].zero();
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                const uint32_t c = k * tpr + t;
-                one[k] = live && c < d ? row[c] : from_f32<T>(0.0f);
-            }
+            for (int k = 0; k < NC; ++k) one[k] = live && (int)(k * tpr) < left ? row[k * tpr] : from_f32<T>(0.0f);
         }
     }
-    __device__ __forceinline__ void unpack(float (&f)[NC]) const
+    __device__ __forceinline__ void unpack(f32x2 (&p)[NC / 2]) const
     {
         if constexpr (VEC) {
 #pragma unroll
@@ -108,166 +136,221 @@ struct RowPart {
                 float e[8];
                 raw[k].unpack(e);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[k * 8 + i] = e[i];
+                for (int i = 0; i < 4; ++i) p[k * 4 + i] = pair(e[2 * i], e[2 * i + 1]);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < NC; ++k) f[k] = to_f32(one[k]);
+            for (int k = 0; k < NC / 2; ++k) p[k] = pair(to_f32(one[2 * k]), to_f32(one[2 * k + 1]));
         }
     }
 };
 
-template <int NC, bool VEC>
-__device__ __forceinline__ uint32_t column(int i, uint32_t t, uint32_t tpr)
-{
-    return VEC ? ((i / 8) * tpr + t) * 8 + (i & 7) : i * tpr + t;
-}
-
 template <typename T, int NC, bool VEC>
-__device__ __forceinline__ void store_part(T *row, uint32_t d, uint32_t t, uint32_t tpr, const float (&f)[NC])
+__device__ __forceinline__ void store_part(T *row, int left, uint32_t tpr, const f32x2 (&p)[NC / 2])
 {
+    float f[NC];
+#pragma unroll
+    for (int i = 0; i < NC / 2; ++i) unpair(p[i], f[2 * i], f[2 * i + 1]);
     if constexpr (VEC) {
 #pragma unroll
         for (int k = 0; k < NC / 8; ++k) {
-            const uint32_t c = (k * tpr + t) * 8;
-            if (c < d) {
+            if ((int)(k * tpr * 8) < left) {
                 float e[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) e[i] = f[k * 8 + i];
-                store8(row + c, e);
+                store8(row + k * tpr * 8, e);
             }
         }
     } else {
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            const uint32_t c = k * tpr + t;
-            if (c < d) row[c] = from_f32<T>(f[k]);
+            if ((int)(k * tpr) < left) row[k * tpr] = from_f32<T>(f[k]);
         }
     }
+}
+
+__device__ __forceinline__ float half_of(f32x2 p, int which)
+{
+    float lo, hi;
+    unpair(p, lo, hi);
+    return which ? hi : lo;
+}
+
+// Rows of a group from `row` on, at most r.
+__device__ __forceinline__ int rows_left(uint64_t row, int r, uint64_t rows)
+{
+    return row + r <= rows ? r : row < rows ? (int)(rows - row) : 0;
+}
+
+// Columns of a vector of W, or the value that stands for a missing vector.
+template <typename W, int NC, bool VEC>
+__device__ __forceinline__ void load_vector(const void *v, float missing, uint32_t t, uint32_t tpr, uint32_t d, f32x2 (&out)[NC / 2])
+{
+    float f[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const uint32_t c = column<NC, VEC>(i, t, tpr);
+        f[i] = c < d && v ? to_f32(static_cast<const W *>(v)[c]) : missing;
+    }
+#pragma unroll
+    for (int i = 0; i < NC / 2; ++i) out[i] = pair(f[2 * i], f[2 * i + 1]);
 }
 
 template <typename T, typename W, int NC, int R, bool VEC>
 __global__ void __launch_bounds__(kRowThreads) k_ln_forward(const __grid_constant__ LnArgs a)
 {
+    constexpr int kPairs = NC / 2;
     extern __shared__ float sh[];
     const uint32_t group = threadIdx.x / a.tpr, t = threadIdx.x - group * a.tpr;
+    const int left = (int)a.d - (int)(VEC ? t * 8 : t); // columns from this thread's first one on
     GroupSum<R> sum{sh, a.tpr, a.tpr >> 5, t, group};
     wait_prior_grid();
     release_next_grid();
-    float w[NC], b[NC];
+    f32x2 w[kPairs], b[kPairs];
+    load_vector<W, NC, VEC>(a.w, 1.0f, t, a.tpr, a.d, w);
+    load_vector<W, NC, VEC>(a.b, 0.0f, t, a.tpr, a.d, b);
+    const uint64_t at_once = (uint64_t)a.groups * R, step = gridDim.x * at_once;
+    uint64_t row = blockIdx.x * at_once + group * R;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.x_stride + (VEC ? t * 8 : t);
+    T *y = static_cast<T *>(a.y) + (int64_t)row * a.y_stride + (VEC ? t * 8 : t);
+    RowPart<T, NC, VEC> next[R]; // the loads of the next rows are on their way while these are worked on
+    int rows = rows_left(row, R, a.rows);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const uint32_t c = column<NC, VEC>(i, t, a.tpr);
-        w[i] = c < a.d && a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
-        b[i] = c < a.d && a.b ? to_f32(static_cast<const W *>(a.b)[c]) : 0.0f;
-    }
-    const uint64_t at_once = (uint64_t)a.groups * R;
-    for (uint64_t r0 = (uint64_t)blockIdx.x * at_once; r0 < a.rows; r0 += (uint64_t)gridDim.x * at_once) {
-        const uint64_t row = r0 + (uint64_t)group * R;
-        RowPart<T, NC, VEC> part[R];
+    for (int r = 0; r < R; ++r) next[r].load(x + r * a.x_stride, left, a.tpr, r < rows);
+    for (uint64_t r0 = blockIdx.x * at_once; r0 < a.rows; r0 += step) {
+        f32x2 v[R][kPairs];
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            part[r].load(static_cast<const T *>(a.x) + (int64_t)(row + r) * a.x_stride, a.d, t, a.tpr, row + r < a.rows);
-        float mean[R], var[R];
+        for (int r = 0; r < R; ++r) next[r].unpack(v[r]);
+        x += step * a.x_stride;
+        const int next_rows = rows_left(row + step, R, a.rows);
+#pragma unroll
+        for (int r = 0; r < R; ++r) next[r].load(x + r * a.x_stride, left, a.tpr, r < next_rows);
+        float mean[R], rstd[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float f[NC];
-            part[r].unpack(f);
-            mean[r] = 0.0f;
+            f32x2 s = v[r][0];
 #pragma unroll
-            for (int i = 0; i < NC; ++i) mean[r] += f[i];
+            for (int i = 1; i < kPairs; ++i) s = add2(s, v[r][i]);
+            mean[r] = sum2(s);
         }
-        sum(mean);
+        sum(mean, [&](float s) { return s * a.inv_d; });
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            mean[r] *= a.inv_d;
-            float f[NC];
-            part[r].unpack(f);
-            var[r] = 0.0f;
+            const f32x2 m = pair(-mean[r]);
+            rstd[r] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const float c = column<NC, VEC>(i, t, a.tpr) < a.d ? f[i] - mean[r] : 0.0f;
-                var[r] = fmaf(c, c, var[r]);
+            for (int k = 0; k < (VEC ? NC / 8 : 1); ++k) { // pieces that are there as a whole, or not at all
+                f32x2 s = pair(0.0f);
+#pragma unroll
+                for (int i = k * 4; i < (VEC ? k * 4 + 4 : kPairs); ++i) {
+                    v[r][i] = add2(v[r][i], m);
+                    f32x2 q = v[r][i];
+                    if (!VEC) // each column for itself
+                        q = mul2(q, pair((int)(2 * i * a.tpr) < left ? 1.0f : 0.0f, (int)((2 * i + 1) * a.tpr) < left ? 1.0f : 0.0f));
+                    s = fma2(q, q, s);
+                }
+                rstd[r] += !VEC || (int)(k * a.tpr * 8) < left ? sum2(s) : 0.0f;
             }
         }
-        sum(var);
+        sum(rstd, [&](float s) { return 1.0f / sqrtf(fmaf(s, a.inv_d, a.eps)); });
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (row + r >= a.rows) break;
-            const float rstd = 1.0f / sqrtf(fmaf(var[r], a.inv_d, a.eps));
-            float f[NC];
-            part[r].unpack(f);
+            const f32x2 p = pair(rstd[r]);
 #pragma unroll
-            for (int i = 0; i < NC; ++i) f[i] = fmaf((f[i] - mean[r]) * rstd, w[i], b[i]);
-            store_part<T, NC, VEC>(static_cast<T *>(a.y) + (int64_t)(row + r) * a.y_stride, a.d, t, a.tpr, f);
-            if (t == 0) {
-                if (a.mean) a.mean[row + r] = mean[r];
-                if (a.rstd) a.rstd[row + r] = rstd;
+            for (int i = 0; i < kPairs; ++i) v[r][i] = fma2(mul2(v[r][i], p), w[i], b[i]);
+            if (r < rows) {
+                store_part<T, NC, VEC>(y + r * a.y_stride, left, a.tpr, v[r]);
+                if (t == 0) {
+                    if (a.mean) a.mean[row + r] = mean[r];
+                    if (a.rstd) a.rstd[row + r] = rstd[r];
+                }
             }
         }
+        row += step;
+        y += step * a.y_stride;
+        rows = next_rows;
     }
 }
 
 template <typename T, typename W, int NC, int R, bool VEC>
 __global__ void __launch_bounds__(kRowThreads) k_ln_backward(const __grid_constant__ LnArgs a)
 {
+    constexpr int kPairs = NC / 2;
     extern __shared__ float sh[];
     const uint32_t group = threadIdx.x / a.tpr, t = threadIdx.x - group * a.tpr;
+    const int left = (int)a.d - (int)(VEC ? t * 8 : t);
     GroupSum<2 * R> sum{sh, a.tpr, a.tpr >> 5, t, group};
     wait_prior_grid();
     release_next_grid();
-    float w[NC], dw[NC], db[NC];
+    f32x2 w[kPairs], dw[kPairs], db[kPairs];
+    load_vector<W, NC, VEC>(a.w, 1.0f, t, a.tpr, a.d, w);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const uint32_t c = column<NC, VEC>(i, t, a.tpr);
-        w[i] = c < a.d && a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
-        dw[i] = db[i] = 0.0f;
-    }
-    const uint64_t at_once = (uint64_t)a.groups * R;
-    for (uint64_t r0 = (uint64_t)blockIdx.x * at_once; r0 < a.rows; r0 += (uint64_t)gridDim.x * at_once) {
-        const uint64_t row = r0 + (uint64_t)group * R;
-        RowPart<T, NC, VEC> px[R], pg[R];
-        float mean[R], rstd[R], s[2 * R];
+    for (int i = 0; i < kPairs; ++i) dw[i] = db[i] = pair(0.0f);
+    const uint64_t at_once = (uint64_t)a.groups * R, step = gridDim.x * at_once;
+    uint64_t row = blockIdx.x * at_once + group * R;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.x_stride + (VEC ? t * 8 : t);
+    const T *dy = static_cast<const T *>(a.dy) + (int64_t)row * a.dy_stride + (VEC ? t * 8 : t);
+    T *dx = static_cast<T *>(a.y) + (int64_t)row * a.y_stride + (VEC ? t * 8 : t);
+    RowPart<T, NC, VEC> px[R], pg[R], nx[R], ng[R];
+    float mean[R], rstd[R], next_mean[R], next_rstd[R];
+    int rows = rows_left(row, R, a.rows);
+    const auto fetch = [&](uint64_t first, int count) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool live = row + r < a.rows;
-            px[r].load(static_cast<const T *>(a.x) + (int64_t)(row + r) * a.x_stride, a.d, t, a.tpr, live);
-            pg[r].load(static_cast<const T *>(a.dy) + (int64_t)(row + r) * a.dy_stride, a.d, t, a.tpr, live);
-            mean[r] = live ? __ldcg(a.mean + row + r) : 0.0f;
-            rstd[r] = live ? __ldcg(a.rstd + row + r) : 0.0f;
+            nx[r].load(x + r * a.x_stride, left, a.tpr, r < count);
+            ng[r].load(dy + r * a.dy_stride, left, a.tpr, r < count);
+            next_mean[r] = r < count ? __ldcg(a.mean + first + r) : 0.0f;
+            next_rstd[r] = r < count ? __ldcg(a.rstd + first + r) : 0.0f;
         }
+    };
+    fetch(row, rows);
+    for (uint64_t r0 = blockIdx.x * at_once; r0 < a.rows; r0 += step) {
+        float s[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            px[r] = nx[r];
+            pg[r] = ng[r];
+            mean[r] = -next_mean[r];
+            rstd[r] = next_rstd[r];
+        }
+        x += step * a.x_stride;
+        dy += step * a.dy_stride;
+        const int next_rows = rows_left(row + step, R, a.rows);
+        fetch(row + step, next_rows);
         // columns past d and rows past the end hold dy = 0 and drop out of all four sums
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float x[NC], g[NC];
-            px[r].unpack(x);
+            f32x2 v[kPairs], g[kPairs];
+            px[r].unpack(v);
             pg[r].unpack(g);
-            s[2 * r] = s[2 * r + 1] = 0.0f;
+            const f32x2 m = pair(mean[r]), p = pair(rstd[r]);
+            f32x2 s1 = pair(0.0f), s2 = pair(0.0f);
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const float xhat = (x[i] - mean[r]) * rstd[r];
-                db[i] += g[i];
-                dw[i] = fmaf(g[i], xhat, dw[i]);
-                const float u = g[i] * w[i];
-                s[2 * r] += u;
-                s[2 * r + 1] = fmaf(u, xhat, s[2 * r + 1]);
+            for (int i = 0; i < kPairs; ++i) {
+                const f32x2 xhat = mul2(add2(v[i], m), p), u = mul2(g[i], w[i]);
+                db[i] = add2(db[i], g[i]);
+                dw[i] = fma2(g[i], xhat, dw[i]);
+                s1 = add2(s1, u);
+                s2 = fma2(u, xhat, s2);
             }
+            s[2 * r] = sum2(s1);
+            s[2 * r + 1] = sum2(s2);
         }
-        sum(s);
+        sum(s, [&](float q) { return -q * a.inv_d; });
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (row + r >= a.rows) break;
-            const float c1 = s[2 * r] * a.inv_d, c2 = s[2 * r + 1] * a.inv_d;
-            float x[NC], g[NC];
-            px[r].unpack(x);
+            if (!a.y || r >= rows) break;
+            f32x2 v[kPairs], g[kPairs];
+            px[r].unpack(v);
             pg[r].unpack(g);
+            const f32x2 m = pair(mean[r]), p = pair(rstd[r]), c1 = pair(s[2 * r]), c2 = pair(s[2 * r + 1]);
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const float xhat = (x[i] - mean[r]) * rstd[r];
-                g[i] = rstd[r] * (fmaf(g[i], w[i], -c1) - xhat * c2);
-            }
-            if (a.y) store_part<T, NC, VEC>(static_cast<T *>(a.y) + (int64_t)(row + r) * a.y_stride, a.d, t, a.tpr, g);
+            for (int i = 0; i < kPairs; ++i) g[i] = mul2(p, fma2(mul2(add2(v[i], m), p), c2, fma2(g[i], w[i], c1)));
+            store_part<T, NC, VEC>(dx + r * a.y_stride, left, a.tpr, g);
         }
+        row += step;
+        dx += step * a.y_stride;
+        rows = next_rows;
     }
     if (!a.partials) return;
     // the groups' column sums, in order, through shared memory: [groups][2][d]
@@ -278,8 +361,8 @@ __global__ void __launch_bounds__(kRowThreads) k_ln_backward(const __grid_consta
         for (int i = 0; i < NC; ++i) {
             const uint32_t c = column<NC, VEC>(i, t, a.tpr);
             if (c < a.d) {
-                mine[c] = dw[i];
-                mine[a.d + c] = db[i];
+                mine[c] = half_of(dw[i / 2], i & 1);
+                mine[a.d + c] = half_of(db[i / 2], i & 1);
             }
         }
         __syncthreads();
@@ -295,8 +378,8 @@ __global__ void __launch_bounds__(kRowThreads) k_ln_backward(const __grid_consta
     for (int i = 0; i < NC; ++i) {
         const uint32_t c = column<NC, VEC>(i, t, a.tpr);
         if (c < a.d) {
-            out[c] = dw[i];
-            out[a.d + c] = db[i];
+            out[c] = half_of(dw[i / 2], i & 1);
+            out[a.d + c] = half_of(db[i / 2], i & 1);
         }
     }
 }
@@ -422,6 +505,11 @@ struct Plan {
     size_t smem = 0;
 };
 
+// Rows in flight of a group (and as many being worked on), where there are rows enough: the backward pass has twice
+// the registers of a row to hold, rows without vector accesses hold an element a register.
+template <bool BWD>
+constexpr int kRows = BWD ? 2 : 4;
+
 template <typename T, typename W, bool BWD>
 const void *pick(int nc, int r, bool vec)
 {
@@ -430,10 +518,10 @@ const void *pick(int nc, int r, bool vec)
         return BWD ? reinterpret_cast<const void *>(&k_ln_backward<T, W, NC, R, V>)           \
                    : reinterpret_cast<const void *>(&k_ln_forward<T, W, NC, R, V>);
     A2_LN(8, 1, true)
-    A2_LN(8, 4, true)
+    A2_LN(8, kRows<BWD>, true)
     A2_LN(16, 1, true)
     A2_LN(8, 1, false)
-    A2_LN(8, 4, false)
+    A2_LN(8, 2, false)
     A2_LN(16, 1, false)
 #undef A2_LN
     return nullptr;
@@ -493,9 +581,9 @@ Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int 
     // whole warps
     while (p.tpr * p.groups % 32) ++p.groups;
     p.threads = p.tpr * p.groups;
-    // four rows in flight where there are rows enough to keep every SM busy with them
-    p.r = p.nc == 8 && rows >= (uint64_t)sms * p.groups * 8 ? 4 : 1;
-    const size_t sums = sizeof(float) * 2 * (kMaxThreads / 32) * (backward ? 2 : 1) * p.r;
+    // several rows in flight where there are enough to keep every SM busy with them
+    p.r = p.nc == 8 && rows >= (uint64_t)sms * p.groups * 8 ? (vec && !backward ? 4 : 2) : 1;
+    const size_t sums = sizeof(float) * 2 * (kRowThreads / 32) * (backward ? 2 : 1) * p.r;
     p.smem = std::max(sums, backward && p.groups > 1 ? sizeof(float) * 2 * d * p.groups : (size_t)0);
     p.fn = backward ? pick_types<true>(dtype, param, p.nc, p.r, vec) : pick_types<false>(dtype, param, p.nc, p.r, vec);
     // every CTA resident at once: the rows are dealt out evenly

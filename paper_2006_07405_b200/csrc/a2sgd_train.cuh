@@ -110,6 +110,49 @@ __device__ __forceinline__ void store8<float>(float *p, const float (&f)[8])
     st_stream(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
 }
 
+// ------------------------------------------------------------------ two fp32 operations in one instruction
+// sm_100's packed fp32 arithmetic: each half is the single operation, rounded to nearest.  It halves what
+// the element-wise kernels have to issue.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ f32x2 pair(float both) { return pair(both, both); }
+__device__ __forceinline__ void unpair(f32x2 p, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2_down(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rm.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float sum2(f32x2 p)
+{
+    float lo, hi;
+    unpair(p, lo, hi);
+    return lo + hi;
+}
+
 // 256-bit accesses of fp32 data (32-byte alignment), marked evict-first in L2 as in the gradient
 // path's kernels: a training step touches these bytes once, with gigabytes in between.
 __device__ __forceinline__ void ld256(const float *p, float (&f)[8])
