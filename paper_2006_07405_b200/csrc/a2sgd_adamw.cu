@@ -63,30 +63,66 @@ __device__ __forceinline__ uint32_t dither_bits(uint32_t place, uint32_t step_ke
     return h;
 }
 
-// byte -> float without the conversion unit, which issues a quarter as often as the adder: the byte
-// becomes the low mantissa of 2^23.
-__device__ __forceinline__ float byte_to_f32(uint32_t word, int byte)
-{
-    return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540u | byte)) - 8388608.0f;
-}
+// Bytes become floats and floats bytes without the conversion unit, which issues a quarter as often as the adder:
+// a byte is the low mantissa of 2^23.
 
-// The code q of s = (value / scale) * top^2, q in [0, top], rounded so that the expectation of q^2 over
+// The codes q of two s = (value / scale) * top^2, q in [0, top], rounded so that the expectation of q^2 over
 // the dither u in [0, 1) is s: q = floor(sqrt(s)), plus one when s - q^2 > u (2q + 1).  The approximate
 // root may be off by an ulp and so pick the neighbour of an exact floor only where s is within 2^-16
-// of a square's distance from it, where the second test gives the same sum: u ends at 4095/4096.
-__device__ __forceinline__ float encode(float s, uint32_t u12, float top)
+// of a square's distance from it, where the second test gives the same sum: u ends at 4095/4096.  q^2,
+// 2q + 1 and its product with u are exact.  u comes as 1 + u, 12 bits on top of a mantissa.
+__device__ __forceinline__ void encode2(f32x2 s, uint32_t one_plus_u0, uint32_t one_plus_u1, float top, float least, float &q0, float &q1)
 {
-    float root;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(s));
-    const float q = __fadd_rd(root, 8388608.0f) - 8388608.0f;
-    const float u = __fmul_rn(__uint_as_float(0x4B000000u | u12) - 8388608.0f, 1.0f / 4096.0f);
-    const bool up = __fsub_rn(s, __fmul_rn(q, q)) > __fmul_rn(u, __fadd_rn(__fmul_rn(2.0f, q), 1.0f));
-    return fminf(up ? q + 1.0f : q, top);
+    float s0, s1, r0, r1;
+    unpair(s, s0, s1);
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(s0));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(s1));
+    const f32x2 q = add2(add2_down(pair(r0, r1), pair(8388608.0f)), pair(-8388608.0f));
+    const f32x2 over = fma2(mul2(q, pair(-1.0f)), q, s); // s - q^2
+    const f32x2 u = add2(pair(__uint_as_float(one_plus_u0), __uint_as_float(one_plus_u1)), pair(-1.0f));
+    const f32x2 limit = mul2(u, fma2(pair(2.0f), q, pair(1.0f)));
+    float o0, o1, l0, l1;
+    unpair(over, o0, o1);
+    unpair(limit, l0, l1);
+    unpair(q, q0, q1);
+    if (o0 > l0) q0 += 1.0f;
+    if (o1 > l1) q1 += 1.0f;
+    q0 = fminf(q0, top);
+    q1 = fminf(q1, top);
+    if (least > 0.0f) {
+        q0 = fmaxf(q0, least);
+        q1 = fmaxf(q1, least);
+    }
 }
+// 12 bits of the dither as 1 + u: bits 31..20 for m's code, bits 19..8 for v's.
+__device__ __forceinline__ uint32_t dither_m(uint32_t h) { return 0x3F800000u | (h >> 9 & 0x007FF800u); }
+__device__ __forceinline__ uint32_t dither_v(uint32_t h) { return 0x3F800000u | (h << 3 & 0x007FF800u); }
 
-__device__ __forceinline__ uint32_t code_byte(float q) // q a whole number in [0, 255]
+// Codes to bytes: a whole number plus 1.5 * 2^23 has its two's complement in the low byte.
+__device__ __forceinline__ uint32_t bytes4(float a, float b, float c, float d)
 {
-    return __float_as_uint(q + 8388608.0f) & 0xffu;
+    float x, y, z, w;
+    unpair(add2(pair(a, b), pair(12582912.0f)), x, y);
+    unpair(add2(pair(c, d), pair(12582912.0f)), z, w);
+    const uint32_t lo = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x0040);
+    const uint32_t hi = __byte_perm(__float_as_uint(z), __float_as_uint(w), 0x0040);
+    return __byte_perm(lo, hi, 0x5410);
+}
+// Bytes to the values they stand for, two at a time: m = q |q| cm from two's complement with the top bit flipped
+// (q + 128), and sqrt(v) = q^2 cr.
+__device__ __forceinline__ f32x2 m_of(uint32_t flipped, int byte, f32x2 cm)
+{
+    const f32x2 q = add2(pair(__uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | byte)),
+                              __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7541u + byte))), pair(-8388736.0f));
+    float a, b;
+    unpair(q, a, b);
+    return mul2(mul2(q, pair(fabsf(a), fabsf(b))), cm);
+}
+__device__ __forceinline__ f32x2 root_of(uint32_t word, int byte, f32x2 cr)
+{
+    const f32x2 q = add2(pair(__uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540u | byte)),
+                              __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7541u + byte))), pair(-8388608.0f));
+    return mul2(mul2(q, q), cr);
 }
 
 struct Gain {
@@ -101,14 +137,36 @@ __device__ __forceinline__ Gain gain_of(uint32_t largest_bits, float top_squared
     return r;
 }
 
-// One element of the step.  r is sqrt(v), which the update needs and the 8-bit state holds.
-__device__ __forceinline__ void adamw_element(const StepArgs &a, float g, float &w, float &m, float &v, float &r)
+// sqrt(v) and m / d for two elements each, correctly rounded.  Within the range that `plain_range` tests this is
+// Markstein's method (IBM J. Res. Dev. 34, 1990): an approximate root or reciprocal, and the exact residual by a fused
+// multiply-add.  It has no special cases and runs on pairs; outside of the range the library functions are called.
+__device__ __forceinline__ f32x2 root2(f32x2 v)
 {
-    m = __fadd_rn(__fmul_rn(m, a.beta1), __fmul_rn(g, a.one_minus_beta1));
-    v = __fadd_rn(__fmul_rn(v, a.beta2), __fmul_rn(__fmul_rn(g, g), a.one_minus_beta2));
-    r = __fsqrt_rn(v);
-    const float d = __fadd_rn(__fmul_rn(r, a.root), a.eps);
-    w = __fsub_rn(__fmul_rn(w, a.decay), __fmul_rn(__fdiv_rn(m, d), a.rate));
+    float a, b, x, y;
+    unpair(v, a, b);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(a));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
+    const f32x2 y2 = pair(x, y), g = mul2(v, y2), h = mul2(y2, pair(0.5f));
+    const f32x2 left = fma2(mul2(g, pair(-1.0f)), g, v); // v - g^2
+    return fma2(left, h, g);
+}
+__device__ __forceinline__ f32x2 quotient2(f32x2 m, f32x2 d)
+{
+    float a, b, x, y;
+    unpair(d, a, b);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(a));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
+    const f32x2 minus = mul2(d, pair(-1.0f));
+    f32x2 y2 = pair(x, y);
+    y2 = fma2(y2, fma2(minus, y2, pair(1.0f)), y2);
+    const f32x2 q = mul2(m, y2);
+    return fma2(fma2(minus, q, m), y2, q);
+}
+// v of a lane within 2^-80..2^80 and |m| up to 2^80: d = sqrt(v) root + eps lies between 2^-40 and 2^100 and no residual
+// leaves the normal range, but that of an m below 2^-100, whose quotient may be an ulp off.
+__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, uint32_t largest_m)
+{
+    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x67800000u;
 }
 
 // GT: gradient type.  CT: type of the 16-bit copy of the weights, float when there is none.
@@ -137,7 +195,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
     // places inside the block: 8 consecutive ones a lane, or (any alignment) every 32nd
     const uint32_t base = vector ? lane * 8 : lane, step = vector ? 1 : 32;
 
-    float w[8], g[8], m[8], v[8], r[8];
+    float w[8], g[8], m[8], v[8];
     float *wp = t.w + first;
     const GT *gp = static_cast<const GT *>(t.grad) + first;
     const uint64_t at = block * kStateBlock + base;
@@ -177,20 +235,60 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
             }
         }
     }
+    // m, v and sqrt(v) after the step
+    f32x2 m2[4], v2[4], r2[4];
     if constexpr (EIGHT) {
-        const float cm = __fmul_rn(ms, kPerM), cr = __fmul_rn(vs, kPerV);
+        const f32x2 cm = pair(__fmul_rn(ms, kPerM)), cr = pair(__fmul_rn(vs, kPerV));
+        mw.x ^= 0x80808080u, mw.y ^= 0x80808080u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // two's complement byte with its top bit flipped is the code plus 128
-            const float qm = byte_to_f32((i < 4 ? mw.x : mw.y) ^ 0x80808080u, i & 3) - 128.0f;
-            const float qv = byte_to_f32(i < 4 ? vw.x : vw.y, i & 3);
-            m[i] = __fmul_rn(__fmul_rn(qm, fabsf(qm)), cm);
-            const float root = __fmul_rn(__fmul_rn(qv, qv), cr);
-            v[i] = __fmul_rn(root, root);
+        for (int i = 0; i < 4; ++i) {
+            m2[i] = m_of(i < 2 ? mw.x : mw.y, 2 * (i & 1), cm);
+            const f32x2 root = root_of(i < 2 ? vw.x : vw.y, 2 * (i & 1), cr);
+            v2[i] = mul2(root, root);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m2[i] = pair(m[2 * i], m[2 * i + 1]);
+            v2[i] = pair(v[2 * i], v[2 * i + 1]);
         }
     }
+    uint32_t big_m = 0, big_v = 0, least_v = 0xffffffffu; // bit patterns order like the floats, NaN above infinity
 #pragma unroll
-    for (int i = 0; i < 8; ++i) adamw_element(a, __fmul_rn(g[i], scale), w[i], m[i], v[i], r[i]);
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 gi = mul2(pair(g[2 * i], g[2 * i + 1]), pair(scale));
+        m2[i] = add2_of_products(mul2(m2[i], pair(a.beta1)), mul2(gi, pair(a.one_minus_beta1)));
+        v2[i] = add2_of_products(mul2(v2[i], pair(a.beta2)), mul2(mul2(gi, gi), pair(a.one_minus_beta2)));
+        unpair(m2[i], m[2 * i], m[2 * i + 1]);
+        unpair(v2[i], v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int k = 2 * i; k < 2 * i + 2; ++k) {
+            big_m = max(big_m, __float_as_uint(m[k]) & 0x7fffffffu);
+            big_v = max(big_v, __float_as_uint(v[k]));
+            least_v = min(least_v, __float_as_uint(v[k]));
+        }
+    }
+    if (plain_range(least_v, big_v, big_m)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r2[i] = root2(v2[i]);
+            const f32x2 q = quotient2(m2[i], add2_of_products(mul2(r2[i], pair(a.root)), pair(a.eps)));
+            unpair(add2_of_products(mul2(pair(w[2 * i], w[2 * i + 1]), pair(a.decay)), mul2(q, pair(-a.rate))), w[2 * i], w[2 * i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float r[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int e = 2 * i + k;
+                r[k] = __fsqrt_rn(v[e]);
+                const float q = __fdiv_rn(m[e], __fadd_rn(__fmul_rn(r[k], a.root), a.eps));
+                w[e] = __fsub_rn(__fmul_rn(w[e], a.decay), __fmul_rn(q, a.rate));
+            }
+            r2[i] = pair(r[0], r[1]);
+        }
+    }
 
     if (vector) {
         st256(wp + base, w);
@@ -217,35 +315,36 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
             }
         }
     } else {
-        // bit patterns of non-negative floats order like the floats, NaN above infinity
-        uint32_t big_m = 0, big_r = 0;
+        uint32_t big_r = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            big_m = max(big_m, __float_as_uint(m[i]) & 0x7fffffffu);
-            big_r = max(big_r, __float_as_uint(r[i]) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) {
+            float x, y;
+            unpair(r2[i], x, y);
+            big_r = max(big_r, max(__float_as_uint(x) & 0x7fffffffu, __float_as_uint(y) & 0x7fffffffu));
         }
         const Gain gm = gain_of(__reduce_max_sync(0xffffffffu, big_m), 16129.0f);
         const Gain gr = gain_of(__reduce_max_sync(0xffffffffu, big_r), 65025.0f);
-        uint32_t mo[8], vo[8];
+        float qm[8], qr[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t h = dither_bits((uint32_t)at + i * step, a.dither);
-            const float qm = encode(__fmul_rn(fabsf(m[i]), gm.gain), h >> 20, 127.0f);
-            const float qr = fmaxf(encode(__fmul_rn(r[i], gr.gain), (h >> 8) & 0xfffu, 255.0f), 2.0f);
-            const uint32_t b = code_byte(qm);
-            mo[i] = (m[i] < 0.0f ? 0u - b : b) & 0xffu;
-            vo[i] = code_byte(qr);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t h0 = dither_bits((uint32_t)at + 2 * i * step, a.dither);
+            const uint32_t h1 = dither_bits((uint32_t)at + (2 * i + 1) * step, a.dither);
+            const float m0 = m[2 * i], m1 = m[2 * i + 1];
+            encode2(mul2(pair(fabsf(m0), fabsf(m1)), pair(gm.gain)), dither_m(h0), dither_m(h1), 127.0f, 0.0f, qm[2 * i], qm[2 * i + 1]);
+            encode2(mul2(r2[i], pair(gr.gain)), dither_v(h0), dither_v(h1), 255.0f, 2.0f, qr[2 * i], qr[2 * i + 1]);
+            qm[2 * i] = copysignf(qm[2 * i], m0);
+            qm[2 * i + 1] = copysignf(qm[2 * i + 1], m1);
         }
+        const uint2 mo = make_uint2(bytes4(qm[0], qm[1], qm[2], qm[3]), bytes4(qm[4], qm[5], qm[6], qm[7]));
+        const uint2 vo = make_uint2(bytes4(qr[0], qr[1], qr[2], qr[3]), bytes4(qr[4], qr[5], qr[6], qr[7]));
         if (vector) {
-            *reinterpret_cast<uint2 *>(a.mq + at) = make_uint2(mo[0] | mo[1] << 8 | mo[2] << 16 | mo[3] << 24,
-                                                               mo[4] | mo[5] << 8 | mo[6] << 16 | mo[7] << 24);
-            *reinterpret_cast<uint2 *>(a.vq + at) = make_uint2(vo[0] | vo[1] << 8 | vo[2] << 16 | vo[3] << 24,
-                                                               vo[4] | vo[5] << 8 | vo[6] << 16 | vo[7] << 24);
+            *reinterpret_cast<uint2 *>(a.mq + at) = mo;
+            *reinterpret_cast<uint2 *>(a.vq + at) = vo;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                a.mq[at + i * 32] = (int8_t)mo[i];
-                a.vq[at + i * 32] = (uint8_t)vo[i];
+                a.mq[at + i * 32] = (int8_t)((i < 4 ? mo.x : mo.y) >> (8 * (i & 3)));
+                a.vq[at + i * 32] = (uint8_t)((i < 4 ? vo.x : vo.y) >> (8 * (i & 3)));
             }
         }
         if (lane == 0) {
@@ -326,15 +425,14 @@ __global__ void __launch_bounds__(kThreads) k_read_state(const int8_t *mq, const
     if (block >= blocks) return;
     const uint64_t at = block * kStateBlock + (threadIdx.x & 31) * 8;
     const uint2 mw = *reinterpret_cast<const uint2 *>(mq + at), vw = *reinterpret_cast<const uint2 *>(vq + at);
-    const float cm = __fmul_rn(m_scale[block], kPerM), cr = __fmul_rn(v_scale[block], kPerV);
+    const f32x2 cm = pair(__fmul_rn(m_scale[block], kPerM)), cr = pair(__fmul_rn(v_scale[block], kPerV));
+    const uint32_t flipped[2] = {mw.x ^ 0x80808080u, mw.y ^ 0x80808080u}, word[2] = {vw.x, vw.y};
     float m[8], v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float qm = byte_to_f32((i < 4 ? mw.x : mw.y) ^ 0x80808080u, i & 3) - 128.0f;
-        const float qv = byte_to_f32(i < 4 ? vw.x : vw.y, i & 3);
-        m[i] = __fmul_rn(__fmul_rn(qm, fabsf(qm)), cm);
-        const float root = __fmul_rn(__fmul_rn(qv, qv), cr);
-        v[i] = __fmul_rn(root, root);
+    for (int i = 0; i < 4; ++i) {
+        unpair(m_of(flipped[i / 2], 2 * (i & 1), cm), m[2 * i], m[2 * i + 1]);
+        const f32x2 root = root_of(word[i / 2], 2 * (i & 1), cr);
+        unpair(mul2(root, root), v[2 * i], v[2 * i + 1]);
     }
     if (m_out) st256(m_out + at, m);
     if (v_out) st256(v_out + at, v);
@@ -360,18 +458,17 @@ __global__ void __launch_bounds__(kThreads) k_write_state(const float *m_in, con
     }
     const Gain gm = gain_of(__reduce_max_sync(0xffffffffu, big_m), 16129.0f);
     const Gain gr = gain_of(__reduce_max_sync(0xffffffffu, big_r), 65025.0f);
-    constexpr uint32_t kHalf = 2048; // u = 1/2: to the nearer square
-    uint32_t mo[8], vo[8];
+    constexpr uint32_t kHalf = 0x3FC00000u; // u = 1/2: to the nearer square
+    float qm[8], qr[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t b = code_byte(encode(__fmul_rn(fabsf(m[i]), gm.gain), kHalf, 127.0f));
-        mo[i] = (m[i] < 0.0f ? 0u - b : b) & 0xffu;
-        vo[i] = code_byte(fmaxf(encode(__fmul_rn(r[i], gr.gain), kHalf, 255.0f), 2.0f));
+    for (int i = 0; i < 8; i += 2) {
+        encode2(mul2(pair(fabsf(m[i]), fabsf(m[i + 1])), pair(gm.gain)), kHalf, kHalf, 127.0f, 0.0f, qm[i], qm[i + 1]);
+        encode2(mul2(pair(r[i], r[i + 1]), pair(gr.gain)), kHalf, kHalf, 255.0f, 2.0f, qr[i], qr[i + 1]);
+        qm[i] = copysignf(qm[i], m[i]);
+        qm[i + 1] = copysignf(qm[i + 1], m[i + 1]);
     }
-    *reinterpret_cast<uint2 *>(mq + at) = make_uint2(mo[0] | mo[1] << 8 | mo[2] << 16 | mo[3] << 24,
-                                                     mo[4] | mo[5] << 8 | mo[6] << 16 | mo[7] << 24);
-    *reinterpret_cast<uint2 *>(vq + at) = make_uint2(vo[0] | vo[1] << 8 | vo[2] << 16 | vo[3] << 24,
-                                                     vo[4] | vo[5] << 8 | vo[6] << 16 | vo[7] << 24);
+    *reinterpret_cast<uint2 *>(mq + at) = make_uint2(bytes4(qm[0], qm[1], qm[2], qm[3]), bytes4(qm[4], qm[5], qm[6], qm[7]));
+    *reinterpret_cast<uint2 *>(vq + at) = make_uint2(bytes4(qr[0], qr[1], qr[2], qr[3]), bytes4(qr[4], qr[5], qr[6], qr[7]));
     if ((threadIdx.x & 31) == 0) {
         m_scale[block] = gm.scale;
         v_scale[block] = gr.scale;

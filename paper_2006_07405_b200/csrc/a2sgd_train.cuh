@@ -140,6 +140,16 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+// A sum of products that each have to be rounded for themselves: the compiler fuses a packed product and a packed sum
+// into a fused multiply-add even where both name their rounding (a x + (-0) in the product's place as well), so the
+// sum is made of two single ones.
+__device__ __forceinline__ f32x2 add2_of_products(f32x2 a, f32x2 b)
+{
+    float a0, a1, b0, b1;
+    unpair(a, a0, a1);
+    unpair(b, b0, b1);
+    return pair(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
+}
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
 {
     f32x2 r;
