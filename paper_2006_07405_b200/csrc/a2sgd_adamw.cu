@@ -164,15 +164,15 @@ __device__ __forceinline__ f32x2 quotient2(f32x2 m, f32x2 d)
 }
 // v of a lane within 2^-80..2^80 and |m| up to 2^80: d = sqrt(v) root + eps lies between 2^-40 and 2^100 and no residual
 // leaves the normal range, but that of an m below 2^-100, whose quotient may be an ulp off.
-__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, uint32_t largest_m)
+__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, float largest_m)
 {
-    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x67800000u;
+    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x1p80f;
 }
 
 // GT: gradient type.  CT: type of the 16-bit copy of the weights, float when there is none.
 // EIGHT: 8-bit states.
 template <typename GT, typename CT, bool EIGHT>
-__global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ StepArgs a)
+__global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ StepArgs a)
 {
     constexpr bool kCopy = sizeof(CT) == 2;
     const Tile *entry = a.tiles + blockIdx.x; // the plan's own table, written before any step
@@ -253,7 +253,9 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
             v2[i] = pair(v[2 * i], v[2 * i + 1]);
         }
     }
-    uint32_t big_m = 0, big_v = 0, least_v = 0xffffffffu; // bit patterns order like the floats, NaN above infinity
+    // v's bit patterns order like its values, NaN above infinity; an m that is not finite comes with such a v
+    uint32_t big_v = 0, least_v = 0xffffffffu;
+    float big_m = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const f32x2 gi = mul2(pair(g[2 * i], g[2 * i + 1]), pair(scale));
@@ -263,7 +265,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
         unpair(v2[i], v[2 * i], v[2 * i + 1]);
 #pragma unroll
         for (int k = 2 * i; k < 2 * i + 2; ++k) {
-            big_m = max(big_m, __float_as_uint(m[k]) & 0x7fffffffu);
+            big_m = fmaxf(big_m, fabsf(m[k]));
             big_v = max(big_v, __float_as_uint(v[k]));
             least_v = min(least_v, __float_as_uint(v[k]));
         }
@@ -315,15 +317,11 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
             }
         }
     } else {
-        uint32_t big_r = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float x, y;
-            unpair(r2[i], x, y);
-            big_r = max(big_r, max(__float_as_uint(x) & 0x7fffffffu, __float_as_uint(y) & 0x7fffffffu));
-        }
-        const Gain gm = gain_of(__reduce_max_sync(0xffffffffu, big_m), 16129.0f);
-        const Gain gr = gain_of(__reduce_max_sync(0xffffffffu, big_r), 65025.0f);
+        // the largest root is the root of the largest v: a correctly rounded root is monotonic
+        const float top_v = __uint_as_float(__reduce_max_sync(0xffffffffu, big_v));
+        const uint32_t top_m = __reduce_max_sync(0xffffffffu, __float_as_uint(big_m));
+        const Gain gr = gain_of(__float_as_uint(__fsqrt_rn(top_v)), 65025.0f);
+        const Gain gm = gain_of(top_v == top_v ? top_m : __float_as_uint(top_v), 16129.0f);
         float qm[8], qr[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
