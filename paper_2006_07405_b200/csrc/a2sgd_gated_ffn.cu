@@ -44,10 +44,8 @@ constexpr uint32_t kTmemColumns = 512;
 constexpr uint32_t kStaging = 32 * 128;      // 32 rows of 64 columns on their way out: two for each epilogue warp
 constexpr uint32_t kSmem = 227 * 1024;
 constexpr int kMostStages = 8;
-// Staging buffers of an epilogue warp: a plain output takes one, so that its slices have six stages.
-__host__ __device__ constexpr uint32_t staging_bytes(int epilogue) { return kEpilogueWarps * (epilogue == 0 ? 1 : 2) * kStaging; }
-// Room for the slices.
-__host__ __device__ constexpr uint32_t operand_bytes(int epilogue) { return (kSmem - 1024 - 512 - staging_bytes(epilogue)) / 1024 * 1024; }
+// Room for the slices: 160 KB, five stages of the widest tile.
+constexpr uint32_t kOperands = (kSmem - 1024 - 512 - kEpilogueWarps * 2 * kStaging) / 1024 * 1024;
 
 enum Epilogue { kStore = 0, kGate = 1, kGateGrad = 2 };
 
@@ -144,16 +142,9 @@ __device__ __forceinline__ void rows_out(const Rows &o, uint32_t buf, int row0, 
             for (int c = lane; c < min(64, n - col0); c += 32) p[c] = ld_shared16(piece(buf, r, c >> 3) + (c & 7) * 2);
         }
         __syncwarp();
+        if (lane == 0) tma_store_commit(); // an empty group: the buffers' turns are counted in groups
     }
 }
-__device__ __forceinline__ void rows_in(const Rows &o, uint32_t buf, int row0, int col0, int m, int n, uint32_t lane)
-{
-    for (int r = 0; r < min(32, m - row0); ++r) {
-        const uint16_t *p = static_cast<const uint16_t *>(o.p) + (int64_t)(row0 + r) * o.ld + col0;
-        for (int c = lane; c < 64; c += 32) st_shared16(piece(buf, r, c >> 3) + (c & 7) * 2, c < n - col0 ? p[c] : (uint16_t)0);
-    }
-}
-
 // ------------------------------------------------------------------ the product
 // One piece of work: a tile, all of its depth or a part of it.
 struct Item {
@@ -193,7 +184,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
 {
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    constexpr uint32_t kOperands = operand_bytes(EPI);
     const uint32_t staging = base + kOperands;
     __shared__ __align__(8) uint64_t bars[2 * kMostStages + 4 + kEpilogueWarps];
     const uint32_t bar0 = smem_u32(bars);
@@ -332,10 +322,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     } else if (warp >= kFirstEpilogueWarp) {
         // ---------------------------------------------------------- accumulators out
         const uint32_t quarter = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2; // a warp reads the TMEM lanes of its quarter
-        const uint32_t buf0 = staging + (warp - kFirstEpilogueWarp) * (EPI == kStore ? 1 : 2) * kStaging, buf1 = buf0 + kStaging;
+        const uint32_t buf0 = staging + (warp - kFirstEpilogueWarp) * 2 * kStaging, buf1 = buf0 + kStaging;
         const uint32_t loaded = bar0 + 8u * (2 * kMostStages + 4 + (warp - kFirstEpilogueWarp));
         int turn = 0;
-        uint32_t loads = 0;
+        uint32_t loads = 0, stores = 0;
         for (int i = pair; i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
@@ -397,16 +387,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                     if (here) {
                         if (lane == 0) tma_store_read<0>();
                         __syncwarp();
-                        const uint32_t bytes = (g.gate.tma ? kStaging : 0u) + (g.up.tma ? kStaging : 0u);
-                        if (lane == 0 && bytes) {
-                            bar_expect(loaded, bytes);
-                            if (g.gate.tma) tma_load(buf0, &g.gate.map, col0, row0, loaded);
-                            if (g.up.tma) tma_load(buf1, &g.up.map, col0, row0, loaded);
+                        if (lane == 0) {
+                            bar_expect(loaded, 2 * kStaging);
+                            tma_load(buf0, &g.gate.map, col0, row0, loaded);
+                            tma_load(buf1, &g.up.map, col0, row0, loaded);
                         }
-                        if (!g.gate.tma) rows_in(g.gate, buf0, row0, col0, q.m, q.n, lane);
-                        if (!g.up.tma) rows_in(g.up, buf1, row0, col0, q.m, q.n, lane);
                         __syncwarp();
-                        if (bytes) ok = ok && bar_wait(loaded, loads++ & 1, &gave_up);
+                        ok = ok && bar_wait(loaded, loads++ & 1, &gave_up);
                     }
                     if (!waited) {
                         ok = ok && bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up);
@@ -450,8 +437,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                 const int subs = (min(t.cols, q.n - t.tn * g.bn) + 63) / 64;
                 for (int sub = half; live && sub < subs; sub += 2) {
                     const int col0 = t.tn * g.bn + sub * 64;
-                    if (t.slot < 0) {
-                        if (lane == 0) tma_store_read<0>();
+                    const uint32_t buf = stores++ & 1 ? buf1 : buf0;
+                    if (t.slot < 0) { // the store before the last one has been read out of this buffer
+                        if (lane == 0) tma_store_read<1>();
                         __syncwarp();
                     }
 #pragma unroll
@@ -461,7 +449,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                         tmem_wait_ld();
                         if (t.slot < 0) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) st_shared(piece(buf0, lane, 4 * j + k), pack8<T>(v + 8 * k));
+                            for (int k = 0; k < 4; ++k) st_shared(piece(buf, lane, 4 * j + k), pack8<T>(v + 8 * k));
                         } else {
                             // rows side by side: 512 consecutive bytes a warp and store
                             float4 *part = reinterpret_cast<float4 *>(g.partials) +
@@ -470,7 +458,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                             for (int k = 0; k < 8; ++k) part[k * kBM] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                         }
                     }
-                    if (t.slot < 0) rows_out(g.out[t.p], buf0, row0, col0, q.m, q.n, lane);
+                    if (t.slot < 0) rows_out(g.out[t.p], buf, row0, col0, q.m, q.n, lane);
                 }
                 fence_before();
                 __syncwarp();
@@ -491,32 +479,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     if (warp == 1) tmem_free_pair(tmem, kTmemColumns);
 }
 
-// The parts of the tiles that were split, added up in order.  One thread: a row, 4 columns.
+// The parts of the tiles that were split, added up in order.  A CTA takes 32 rows of 32 columns: its warps read 32 rows
+// of 4 columns each, 512 bytes in a row, and write rows of 32 columns.
+constexpr int kJoinCols = 32;
 template <typename T>
-__global__ void __launch_bounds__(kBM) k_join(const __grid_constant__ GemmArgs g)
+__global__ void __launch_bounds__(256) k_join(const __grid_constant__ GemmArgs g)
 {
+    __shared__ T sums[32][kJoinCols + 2];
     wait_prior_grid();
     release_next_grid();
     const Item t = item_at(g, g.whole + (int)blockIdx.x * g.splits);
     const Problem &q = g.problem[t.p];
-    const int row = t.tm * kBM + threadIdx.x, col = t.tn * g.bn + blockIdx.y * 4;
-    if (row >= q.m || col >= q.n) return;
+    const int row0 = t.tm * kBM + blockIdx.z * 32, col0 = t.tn * g.bn + blockIdx.y * kJoinCols;
+    if (row0 >= q.m || col0 >= q.n) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t next = (int64_t)(g.bn / 4) * kBM;
-    const float4 *part = reinterpret_cast<const float4 *>(g.partials) + (int64_t)t.slot * next + blockIdx.y * kBM + threadIdx.x;
     float v[4] = {};
+    if (col0 + warp * 4 < q.n) { // rows past the end were not written: not stored below
+        const float4 *part = reinterpret_cast<const float4 *>(g.partials) + (int64_t)t.slot * next +
+                             (blockIdx.y * (kJoinCols / 4) + warp) * kBM + blockIdx.z * 32 + lane;
 #pragma unroll 8
-    for (int s = 0; s < g.splits; ++s) {
-        const float4 x = __ldcg(part + s * next);
-        v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-    }
-    T *out = static_cast<T *>(g.out[t.p].p) + (int64_t)row * g.out[t.p].ld + col;
-    if (g.out[t.p].tma && col + 4 <= q.n) {
-        *reinterpret_cast<uint2 *>(out) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (col + i < q.n) out[i] = from_f32<T>(v[i]);
+        for (int s = 0; s < g.splits; ++s) {
+            const float4 x = __ldcg(part + s * next);
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
         }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[lane][warp * 4 + i] = from_f32<T>(v[i]);
+    __syncthreads();
+    const int rows = min(32, q.m - row0);
+    T *out = static_cast<T *>(g.out[t.p].p) + (int64_t)row0 * g.out[t.p].ld + col0;
+    for (int r = warp; r < rows; r += 8) {
+        if (col0 + lane < q.n) out[(int64_t)r * g.out[t.p].ld + lane] = sums[r][lane];
     }
 }
 
@@ -529,17 +523,25 @@ struct PackJob {
     int cols;
 };
 struct PackArgs {
-    PackJob job[6];
+    PackJob job[8];
 };
 __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a)
 {
     wait_prior_grid();
     release_next_grid();
     const PackJob &j = a.job[blockIdx.y];
-    for (int64_t r = blockIdx.x; r < j.rows; r += gridDim.x) {
-        const uint16_t *s = j.src + r * j.ld_src;
-        uint16_t *d = j.dst + r * j.ld_dst;
-        for (int c = threadIdx.x; c < j.cols; c += 256) d[c] = s[c];
+    const int pieces = (j.cols + 7) / 8; // 16 bytes of a padded row each
+    const int64_t all = j.rows * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces;
+        const int c = (int)(i - r * pieces) * 8;
+        const uint16_t *s = j.src + r * j.ld_src + c;
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (c + k < j.cols) w[k / 2] |= (uint32_t)s[k] << (16 * (k & 1));
+        }
+        *reinterpret_cast<uint4 *>(j.dst + r * j.ld_dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -845,12 +847,12 @@ int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
     g.whole = g.splits > 1 ? tiles / pairs * pairs : tiles;
     g.items = g.whole + (tiles - g.whole) * g.splits;
     g.stage_bytes = kABytes + (EPI == kGate ? 128u : (uint32_t)g.bn / 2) * 128u;
-    g.stages = (int)std::min<uint32_t>(kMostStages, operand_bytes(EPI) / g.stage_bytes);
+    g.stages = (int)std::min<uint32_t>(kMostStages, kOperands / g.stage_bytes);
 
     void *params[] = {&g};
     A2_TRAIN_CUDA(launch(fn, dim3(2 * (unsigned)std::min(g.items, pairs)), kThreads, kSmem - 1024, params, s));
     if (EPI == kStore && g.splits > 1)
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / 4)), kBM, 0,
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / kJoinCols), kBM / 32), 256, 0,
                              params, s));
     return A2SGD_OK;
 }
@@ -889,7 +891,7 @@ void set_shape(GemmArgs &g, const Shape &shape, float *partials)
 struct Packer {
     PackArgs args{};
     int jobs = 0;
-    int64_t most_rows = 0;
+    int64_t most_pieces = 0;
     char *begin, *at;
     explicit Packer(void *workspace) : begin(static_cast<char *>(workspace)), at(begin) {}
     void *take(int64_t rows, int64_t cols)
@@ -907,7 +909,7 @@ struct Packer {
         c.p = take(m.rows, m.cols);
         args.job[jobs++] = PackJob{static_cast<const uint16_t *>(m.p), static_cast<uint16_t *>(const_cast<void *>(c.p)), m.ld, c.ld,
                                    m.rows, m.cols};
-        most_rows = std::max(most_rows, m.rows);
+        most_pieces = std::max(most_pieces, m.rows * (padded(m.cols) / 8));
         return c;
     }
     uint64_t used() const { return (uint64_t)(at - begin); }
@@ -923,7 +925,7 @@ struct Packer {
         if (!jobs) return A2SGD_OK;
         void *params[] = {&args};
         A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_pack),
-                             dim3((unsigned)std::min<int64_t>(most_rows, (int64_t)sms * 8), jobs), 256, 0, params, s));
+                             dim3((unsigned)std::min<int64_t>((most_pieces + 255) / 256, (int64_t)sms * 8), jobs), 256, 0, params, s));
         return A2SGD_OK;
     }
 };
@@ -1040,10 +1042,12 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
     const int d = x.cols, f = h.cols;
     const bool inner = dx.p || dwg.p || dwu.p; // da and db are needed
     Packer pack(workspace);
-    Matrix da, db, pdy, pwd, pwg, pwu, px, ph;
+    Matrix da, db, pdy, pwd, pwg, pwu, px, ph, pgate, pup;
     pdy = pack.usable(dy);
     if (inner) {
         pwd = pack.usable(wd);
+        pgate = pack.usable(gate);
+        pup = pack.usable(up);
         da.rows = db.rows = t;
         da.cols = db.cols = f;
         da.ld = db.ld = padded(f);
@@ -1074,7 +1078,7 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
         g.act = act;
         set_shape(g, Shape(), nullptr);
         if (!add_operands<false, true>(g, 0, pdy, pwd, dtype) || !set_rows(g.out[0], whole_rows(da), dtype) || !set_rows(g.out2, whole_rows(db), dtype) ||
-            !set_rows(g.gate, gate, dtype, false) || !set_rows(g.up, up, dtype, false))
+            !set_rows(g.gate, pgate, dtype, false) || !set_rows(g.up, pup, dtype, false))
             return A2SGD_ERR_CUDA;
         rc = launch_gemm<T, kGateGrad, false, true>(g, add_problem(g, t, f, g.bn, 0, 1, d, 0), sms, s);
         if (rc != A2SGD_OK) return rc;
@@ -1119,7 +1123,7 @@ extern "C" uint64_t a2sgd_gated_ffn_workspace(uint64_t tokens, uint32_t d, uint3
     uint64_t bytes = flags & A2SGD_FFN_BACKWARD ? 2 * room(t, f) : 0;
     if (!(flags & A2SGD_FFN_ALIGNED)) {
         bytes += 2 * room(f, d) + room(d, f) + room(t, f) + room(t, d); // Wg, Wu, Wd, h, x
-        if (flags & A2SGD_FFN_BACKWARD) bytes += room(t, d);            // dy
+        if (flags & A2SGD_FFN_BACKWARD) bytes += room(t, d) + 2 * room(t, f); // dy, gate, up
     }
     if (tokens) bytes += partial_bytes(kMostPairs, 256); // partial sums of tiles that are split, at the widest
     return bytes;

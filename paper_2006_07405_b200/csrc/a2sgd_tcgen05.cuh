@@ -135,11 +135,6 @@ __device__ __forceinline__ uint16_t ld_shared16(uint32_t addr)
     asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
     return v;
 }
-__device__ __forceinline__ void st_shared16(uint32_t addr, uint16_t v)
-{
-    asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
-}
-
 // ------------------------------------------------------------------ tcgen05
 // Shared memory operand: 128-byte rows swizzled over 8 rows (1024 bytes), as the TMA writes them.
 // K-major (a row holds 64 consecutive k): 8-row groups 1024 bytes apart; the leading offset is unused.
