@@ -79,27 +79,66 @@ struct GemmArgs {
     int box;            // B's rows in one box (K-major B)
     int stages;
     uint32_t stage_bytes;
-    int act;
     // Work: `whole` tiles, then the remaining ones in `splits` parts of their depth each
     int whole, items, splits;
     float *partials;    // [items - whole][bn / 4][256][4]
 };
 
 // ------------------------------------------------------------------ activations
-// value and slope share p = the sigmoid: silu(a) = a s(a); gelu in its tanh form is a s(2 k (a + c a^3)).
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
-__device__ __forceinline__ void activation(int act, float a, float &value, float &slope)
+// value and slope of two preactivations, through p = the sigmoid of z: silu(a) = a p(a); gelu in its tanh form is
+// a p(2 k (a + c a^3)).  Both saturate without a special case: exp2 overflows to infinity, whose reciprocal is 0.
+// Packed arithmetic throughout, 2 special functions an element: the ends of the tiles would else take
+// longer than their products (17500 clocks a tile of 256 columns when each element was computed alone,
+// with the choice of the activation inside, against 14600 for 25 slices).
+__device__ __forceinline__ f32x2 sigmoid_of_minus(f32x2 z_log2) // 1 / (1 + 2^z)
 {
-    if (act == A2SGD_ACT_SILU) {
-        const float p = sigmoid(a);
-        value = a * p;
-        slope = p * (1.0f + a * (1.0f - p));
+    float a, b, x, y;
+    unpair(z_log2, a, b);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(a));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
+    unpair(add2(pair(x, y), pair(1.0f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(a));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
+    return pair(x, y);
+}
+template <int ACT>
+__device__ __forceinline__ void activation2(f32x2 a, f32x2 &value, f32x2 &slope)
+{
+    constexpr float kLog2e = 1.4426950408889634f;
+    if constexpr (ACT == A2SGD_ACT_SILU) {
+        const f32x2 p = sigmoid_of_minus(mul2(a, pair(-kLog2e)));
+        value = mul2(a, p);
+        slope = fma2(value, fma2(p, pair(-1.0f), pair(1.0f)), p);
     } else {
         constexpr float k2 = 1.5957691216057308f, c = 0.044715f;
-        const float p = sigmoid(k2 * (a + c * a * a * a));
-        value = a * p;
-        const float pq = p * (1.0f - p);
-        slope = pq == 0.0f ? p : p + a * pq * (k2 * (1.0f + 3.0f * c * a * a));
+        float x, y;
+        unpair(mul2(a, a), x, y);
+        const f32x2 square = pair(fminf(x, 1e20f), fminf(y, 1e20f)); // beyond, p is 0 or 1 and the slope's last term 0 times this
+        const f32x2 p = sigmoid_of_minus(mul2(mul2(a, pair(-k2 * kLog2e)), fma2(square, pair(c), pair(1.0f))));
+        value = mul2(a, p);
+        slope = fma2(mul2(value, fma2(p, pair(-1.0f), pair(1.0f))), fma2(square, pair(3.0f * c * k2), pair(k2)), p);
+    }
+}
+template <int ACT>
+__device__ __forceinline__ void gate_columns(float (&a)[32], const float (&b)[32]) // a <- act(a) b
+{
+#pragma unroll
+    for (int k = 0; k < 32; k += 2) {
+        f32x2 value, slope;
+        activation2<ACT>(pair(a[k], a[k + 1]), value, slope);
+        unpair(mul2(value, pair(b[k], b[k + 1])), a[k], a[k + 1]);
+    }
+}
+template <int ACT>
+__device__ __forceinline__ void gate_gradient(const float *dh, float (&a)[8], float (&b)[8]) // a <- dh b act'(a), b <- dh act(a)
+{
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        f32x2 value, slope;
+        activation2<ACT>(pair(a[k], a[k + 1]), value, slope);
+        const f32x2 g = pair(dh[k], dh[k + 1]);
+        unpair(mul2(mul2(g, pair(b[k], b[k + 1])), slope), a[k], a[k + 1]);
+        unpair(mul2(g, value), b[k], b[k + 1]);
     }
 }
 
@@ -142,7 +181,6 @@ __device__ __forceinline__ void rows_out(const Rows &o, uint32_t buf, int row0, 
             for (int c = lane; c < min(64, n - col0); c += 32) p[c] = ld_shared16(piece(buf, r, c >> 3) + (c & 7) * 2);
         }
         __syncwarp();
-        if (lane == 0) tma_store_commit(); // an empty group: the buffers' turns are counted in groups
     }
 }
 // ------------------------------------------------------------------ the product
@@ -179,7 +217,7 @@ __device__ __forceinline__ Item item_at(const GemmArgs &g, int i)
     return t;
 }
 
-template <typename T, int EPI, bool A_MN, bool B_MN>
+template <typename T, int EPI, bool A_MN, bool B_MN, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(const __grid_constant__ GemmArgs g)
 {
     extern __shared__ char smem_raw[];
@@ -208,6 +246,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         for (int i = 0; i < kEpilogueWarps; ++i) bar_init(bar0 + 8u * (2 * kMostStages + 4 + i), 1);
         gave_up = 0;
         bar_init_fence();
+    }
+    if (threadIdx.x >= 64 && threadIdx.x < 64 + 6) { // the maps are parameters: no need to wait for the launch before
+        const int i = threadIdx.x - 64;
+        if (i < 3) tma_prefetch_map(&g.a[i]);
+        else tma_prefetch_map(&g.b[i - 3]);
     }
     if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_at), kTmemColumns);
     fence_before();
@@ -325,7 +368,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         const uint32_t buf0 = staging + (warp - kFirstEpilogueWarp) * 2 * kStaging, buf1 = buf0 + kStaging;
         const uint32_t loaded = bar0 + 8u * (2 * kMostStages + 4 + (warp - kFirstEpilogueWarp));
         int turn = 0;
-        uint32_t loads = 0, stores = 0;
+        uint32_t loads = 0;
         for (int i = pair; i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
@@ -353,12 +396,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                             st_shared(piece(buf1, lane, 4 * j + k), pack8<T>(b + 8 * k));
                         }
                     }
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        float value, slope;
-                        activation(g.act, a[k], value, slope);
-                        a[k] = value * b[k];
-                    }
+                    gate_columns<ACT>(a, b);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) h[4 * j + k] = pack8<T>(a + 8 * k);
                 }
@@ -412,13 +450,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                             float a[8], b[8];
                             unpack8<T>(ld_shared(piece(buf0, lane, 4 * j + k)), a);
                             unpack8<T>(ld_shared(piece(buf1, lane, 4 * j + k)), b);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                float value, slope;
-                                activation(g.act, a[e], value, slope);
-                                a[e] = dh[8 * k + e] * b[e] * slope;
-                                b[e] = dh[8 * k + e] * value;
-                            }
+                            gate_gradient<ACT>(dh + 8 * k, a, b);
                             st_shared(piece(buf0, lane, 4 * j + k), pack8<T>(a));
                             st_shared(piece(buf1, lane, 4 * j + k), pack8<T>(b));
                         }
@@ -435,34 +467,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                 if (!bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
                 fence_after();
                 const int subs = (min(t.cols, q.n - t.tn * g.bn) + 63) / 64;
-                for (int sub = half; live && sub < subs; sub += 2) {
-                    const int col0 = t.tn * g.bn + sub * 64;
-                    const uint32_t buf = stores++ & 1 ? buf1 : buf0;
-                    if (t.slot < 0) { // the store before the last one has been read out of this buffer
-                        if (lane == 0) tma_store_read<1>();
-                        __syncwarp();
+                if (t.slot < 0) { // the last tile's stores have been read out of the buffers
+                    if (lane == 0) tma_store_read<0>();
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int turn2 = 0; turn2 < 2; ++turn2) { // a warp has two blocks of 64 columns at most
+                    const int sub = half + 2 * turn2;
+                    if (!live || sub >= subs) break;
+                    float v[64];
+                    tmem_ld32(d + sub * 64, reinterpret_cast<float(&)[32]>(v));
+                    tmem_ld32(d + sub * 64 + 32, reinterpret_cast<float(&)[32]>(v[32]));
+                    tmem_wait_ld();
+                    if (t.slot < 0) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) st_shared(piece(turn2 ? buf1 : buf0, lane, k), pack8<T>(v + 8 * k));
+                    } else {
+                        // rows side by side: 512 consecutive bytes a warp and store
+                        float4 *part = reinterpret_cast<float4 *>(g.partials) +
+                                       ((int64_t)t.slot * (g.bn / 4) + sub * 16) * kBM + rank * 128 + quarter * 32 + lane;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) part[k * kBM] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float v[32];
-                        tmem_ld32(d + sub * 64 + 32 * j, v);
-                        tmem_wait_ld();
-                        if (t.slot < 0) {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) st_shared(piece(buf, lane, 4 * j + k), pack8<T>(v + 8 * k));
-                        } else {
-                            // rows side by side: 512 consecutive bytes a warp and store
-                            float4 *part = reinterpret_cast<float4 *>(g.partials) +
-                                           ((int64_t)t.slot * (g.bn / 4) + sub * 16 + 8 * j) * kBM + rank * 128 + quarter * 32 + lane;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) part[k * kBM] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-                        }
-                    }
-                    if (t.slot < 0) rows_out(g.out[t.p], buf, row0, col0, q.m, q.n, lane);
                 }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
+                if (t.slot < 0 && live) {
+                    const int col0 = t.tn * g.bn + half * 64;
+                    if ((int)half < subs) rows_out(g.out[t.p], buf0, row0, col0, q.m, q.n, lane);
+                    if ((int)half + 2 < subs) rows_out(g.out[t.p], buf1, row0, col0 + 128, q.m, q.n, lane);
+                }
             }
         }
         if (lane == 0) tma_store_done();
@@ -699,9 +734,12 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
         }
         const int col = row0 + r;
         if constexpr (DUAL) {
-            float value, slope;
-            activation(g.act, v[0], value, slope);
-            static_cast<T *>(g.out)[(int64_t)n * g.ldo + col] = from_f32<T>(value * v[1]);
+            f32x2 value, slope;
+            if (g.act == A2SGD_ACT_SILU) activation2<A2SGD_ACT_SILU>(pair(v[0], 0.0f), value, slope);
+            else activation2<A2SGD_ACT_GELU_TANH>(pair(v[0], 0.0f), value, slope);
+            float h, other;
+            unpair(value, h, other);
+            static_cast<T *>(g.out)[(int64_t)n * g.ldo + col] = from_f32<T>(h * v[1]);
             if (g.gate) {
                 static_cast<T *>(g.gate)[(int64_t)n * g.ld_gate + col] = from_f32<T>(v[0]);
                 static_cast<T *>(g.up)[(int64_t)n * g.ld_up + col] = from_f32<T>(v[1]);
@@ -831,10 +869,10 @@ Shape choose(const Extent *outs, int count, int k_blocks, bool b_mn, int pairs)
 
 inline uint64_t partial_bytes(int64_t slots, int bn) { return (uint64_t)slots * kBM * bn * sizeof(float); }
 
-template <typename T, int EPI, bool A_MN, bool B_MN>
+template <typename T, int EPI, bool A_MN, bool B_MN, int ACT = 0>
 int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
 {
-    const void *fn = reinterpret_cast<const void *>(&k_gemm<T, EPI, A_MN, B_MN>);
+    const void *fn = reinterpret_cast<const void *>(&k_gemm<T, EPI, A_MN, B_MN, ACT>);
     static std::atomic<uint64_t> allowed{0}; // devices on which this kernel may use its shared memory
     int device = 0;
     A2_TRAIN_CUDA(cudaGetDevice(&device));
@@ -1017,14 +1055,15 @@ int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &w
     if (rc != A2SGD_OK) return rc;
 
     GemmArgs g{};
-    g.act = act;
     g.bn = 256;
     g.box = 128;
     g.splits = 1;
     if (!add_operands<false, false>(g, 0, px, pg, dtype) || !make_map(&g.b[1], pu, dtype, 128) || !set_rows(g.out[0], h, dtype) ||
         (ph.p != h.p && !set_rows(g.out2, whole_rows(ph), dtype)) || !set_rows(g.gate, gate, dtype) || !set_rows(g.up, up, dtype))
         return A2SGD_ERR_CUDA;
-    rc = launch_gemm<T, kGate, false, false>(g, add_problem(g, t, f, 128, 0, 1, d, 0), sms, s);
+    const int tiles = add_problem(g, t, f, 128, 0, 1, d, 0);
+    rc = act == A2SGD_ACT_SILU ? launch_gemm<T, kGate, false, false, A2SGD_ACT_SILU>(g, tiles, sms, s)
+                               : launch_gemm<T, kGate, false, false, A2SGD_ACT_GELU_TANH>(g, tiles, sms, s);
     if (rc != A2SGD_OK) return rc;
 
     g = GemmArgs{};
@@ -1075,12 +1114,13 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
 
     if (inner) {
         GemmArgs g{};
-        g.act = act;
         set_shape(g, Shape(), nullptr);
         if (!add_operands<false, true>(g, 0, pdy, pwd, dtype) || !set_rows(g.out[0], whole_rows(da), dtype) || !set_rows(g.out2, whole_rows(db), dtype) ||
             !set_rows(g.gate, pgate, dtype, false) || !set_rows(g.up, pup, dtype, false))
             return A2SGD_ERR_CUDA;
-        rc = launch_gemm<T, kGateGrad, false, true>(g, add_problem(g, t, f, g.bn, 0, 1, d, 0), sms, s);
+        const int tiles = add_problem(g, t, f, g.bn, 0, 1, d, 0);
+        rc = act == A2SGD_ACT_SILU ? launch_gemm<T, kGateGrad, false, true, A2SGD_ACT_SILU>(g, tiles, sms, s)
+                                   : launch_gemm<T, kGateGrad, false, true, A2SGD_ACT_GELU_TANH>(g, tiles, sms, s);
         if (rc != A2SGD_OK) return rc;
     }
     if (dx.p) {
