@@ -105,6 +105,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, i
                  "l"(map), "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
+// The same tile into L2 only.
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int y)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 // A tile out of shared memory; what lies outside the matrix is not written.
 __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src)
 {
