@@ -23,9 +23,9 @@
 #include "a2sgd_train.cuh"
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <mutex>
 #include <type_traits>
 
 using namespace a2sgd_train;
@@ -596,14 +596,16 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
 
 // ------------------------------------------------------------------ few tokens
 // Up to 32 tokens the block is bound by the weights' bytes, and tiles of 256 rows would be nearly empty.  Here
-// the weights are the left operand, 16 of their rows a CTA, and stream from memory straight into the
-// registers of mma.sync (m16n8k16): a lane loads 16 bytes, 8 consecutive k of one row, and since the order of k
-// within a product is free as long as both operands share it, those 8 are the lane's part of two products; the
-// tokens' 8 k lie the same way.  Eight warps, and the CTAs of a cluster, share the depth; their sums meet in shared
-// memory, in order, where the gate, the activation and the product are applied.
+// the weights are the left operand of mma.sync (m16n8k16), 16 of their rows a CTA.  A lane copies 16 bytes, 8 consecutive
+// k of one row, into a place of shared memory that it alone reads, several steps ahead (cp.async: no registers held, no
+// barrier); since the order of k within a product is free as long as both operands share it, those 8 are the lane's part
+// of two products, and the tokens' 8 k lie the same way.  Four warps, and the CTAs of a cluster, share the depth; their
+// sums meet in shared memory, in order, where the gate, the activation and the product are applied.
 constexpr int kFewTokens = 32;
-constexpr int kFewWarps = 8;
-constexpr int kFewUnroll = 4; // steps of 32 k whose loads are in flight together
+constexpr int kFewWarps = 4;
+constexpr uint32_t kFewPiece = 32 * 16; // what a warp copies at once
+// Steps of 32 k on their way: as many as leave room for three CTAs an SM.
+__host__ __device__ constexpr int few_steps_ahead(bool dual, int nt) { return 70 * 1024 / (kFewWarps * ((dual ? 4 : 2) + nt) * (int)kFewPiece) < 12 ? 70 * 1024 / (kFewWarps * ((dual ? 4 : 2) + nt) * (int)kFewPiece) : 12; }
 
 struct FewArgs {
     const void *w0, *w1; // w1: the second projection, side by side with w0
@@ -629,87 +631,100 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 8 elements of a row from k on; zeros past its end and where the row does not exist.
+// 8 elements of a row from k on into a lane's own place; zeros past the row's end and where the row does not exist.
 template <bool VEC>
-__device__ __forceinline__ uint4 few_load(const uint16_t *row, int k, int depth, bool live)
+__device__ __forceinline__ void few_copy(uint32_t place, const uint16_t *row, int k, int depth, bool live)
 {
-    uint4 q = make_uint4(0, 0, 0, 0);
-    if (!live || k >= depth) return q;
-    if (VEC && k + 8 <= depth) return ld_stream(row + k);
-    uint32_t w[4] = {0, 0, 0, 0};
+    const int there = live && k < depth ? min(8, depth - k) : 0;
+    if constexpr (VEC) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place), "l"(there ? row + k : row), "r"(2 * there) : "memory");
+    } else {
+        uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (k + i < depth) w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+        for (int i = 0; i < 8; ++i) {
+            if (i < there) w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+        }
+        st_shared(place, make_uint4(w[0], w[1], w[2], w[3]));
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ void few_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void few_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T, bool DUAL, int NT, bool VEC>
 __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ FewArgs g)
 {
-    constexpr int kSides = DUAL ? 2 : 1;
-    constexpr int kCols = 8 * NT;
+    constexpr int kSides = DUAL ? 2 : 1, kCols = 8 * NT, kAhead = few_steps_ahead(DUAL, NT), kPieces = 2 * kSides + NT;
+    extern __shared__ __align__(16) char ring[]; // [warps][kAhead][kPieces][32 lanes][16 bytes]
     __shared__ float sums[kFewWarps][kSides][16][kCols + 1];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, c = lane & 3;
     const int part = blockIdx.x % g.parts, row0 = blockIdx.x / g.parts * 16;
     const int steps = (g.depth + 31) / 32, share = part * kFewWarps + warp, shares = g.parts * kFewWarps;
     const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
+    const uint32_t mine = smem_u32(ring) + warp * kAhead * kPieces * kFewPiece + lane * 16;
+    const auto place = [&](int s, int p) { return mine + (uint32_t)((s - s0) % kAhead * kPieces + p) * kFewPiece; };
 
+    // rows that do not exist are not read: their copies have no bytes, from the matrix's first row
+    const bool live[2] = {row0 + (int)quad < g.rows, row0 + 8 + (int)quad < g.rows};
+    const uint16_t *w[kSides][2], *x[NT];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        w[0][r] = static_cast<const uint16_t *>(g.w0) + (live[r] ? (int64_t)(row0 + 8 * r + quad) * g.ld0 : 0);
+        if constexpr (DUAL) w[1][r] = static_cast<const uint16_t *>(g.w1) + (live[r] ? (int64_t)(row0 + 8 * r + quad) * g.ld1 : 0);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x[n] = static_cast<const uint16_t *>(g.x) + (n * 8 + (int)quad < g.tokens ? (int64_t)(n * 8 + quad) * g.ldx : 0);
+    const auto copy_weights = [&](int s) {
+#pragma unroll
+        for (int e = 0; e < kSides; ++e) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) few_copy<VEC>(place(s, 2 * e + r), w[e][r], s * 32 + (int)c * 8, g.depth, live[r]);
+        }
+    };
+    const auto copy_tokens = [&](int s) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            few_copy<VEC>(place(s, 2 * kSides + n), x[n], s * 32 + (int)c * 8, g.depth, n * 8 + (int)quad < g.tokens);
+    };
+    // The second launch of a call may start on its weights at once: the one before it, which wrote its tokens, does not
+    // write them, and had itself waited for what was before the call.
     if constexpr (DUAL) {
         wait_prior_grid();
         release_next_grid();
     }
-    float acc[kSides][NT][4] = {};
-    const bool live0 = row0 + (int)quad < g.rows, live1 = row0 + 8 + (int)quad < g.rows;
-    const uint16_t *wr[kSides][2];
-    wr[0][0] = static_cast<const uint16_t *>(g.w0) + (int64_t)(row0 + quad) * g.ld0;
-    wr[0][1] = wr[0][0] + 8 * g.ld0;
-    if constexpr (DUAL) {
-        wr[1][0] = static_cast<const uint16_t *>(g.w1) + (int64_t)(row0 + quad) * g.ld1;
-        wr[1][1] = wr[1][0] + 8 * g.ld1;
+    for (int s = s0; s < min(s1, s0 + kAhead); ++s) copy_weights(s);
+    if constexpr (!DUAL) {
+        wait_prior_grid();
+        release_next_grid();
     }
-    const uint16_t *xr = static_cast<const uint16_t *>(g.x) + (int64_t)quad * g.ldx;
-    bool waited = false;
-    for (int s = s0; s < s1 || !waited; s += kFewUnroll) {
-        uint4 w[kFewUnroll][kSides][2], x[kFewUnroll][NT];
+    for (int s = s0; s < s0 + kAhead; ++s) {
+        if (s < s1) copy_tokens(s);
+        few_commit();
+    }
+    float acc[kSides][NT][4] = {};
+    for (int s = s0; s < s1; ++s) {
+        few_wait<kAhead - 1>();
+        uint4 a[kSides][2], b[NT];
 #pragma unroll
-        for (int u = 0; u < kFewUnroll; ++u) {
-            const int k = (s + u) * 32 + (int)c * 8;
-            const bool in = s + u < s1;
+        for (int e = 0; e < kSides; ++e) {
 #pragma unroll
-            for (int e = 0; e < kSides; ++e) {
-                w[u][e][0] = few_load<VEC>(wr[e][0], k, g.depth, in && live0);
-                w[u][e][1] = few_load<VEC>(wr[e][1], k, g.depth, in && live1);
+            for (int r = 0; r < 2; ++r) a[e][r] = ld_shared(place(s, 2 * e + r));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) b[n] = ld_shared(place(s, 2 * kSides + n));
+#pragma unroll
+        for (int e = 0; e < kSides; ++e) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma_16816<T>(acc[e][n], a[e][0].x, a[e][1].x, a[e][0].y, a[e][1].y, b[n].x, b[n].y);
+                mma_16816<T>(acc[e][n], a[e][0].z, a[e][1].z, a[e][0].w, a[e][1].w, b[n].z, b[n].w);
             }
         }
-        if (!waited) {
-            // Weights are not written by the launch before this one, which is the block's own (or, for the first
-            // launch of a call, has been waited for): they are on their way while it ends.
-            if constexpr (!DUAL) {
-                wait_prior_grid();
-                release_next_grid();
-            }
-            waited = true;
+        if (s + kAhead < s1) {
+            copy_weights(s + kAhead);
+            copy_tokens(s + kAhead);
         }
-#pragma unroll
-        for (int u = 0; u < kFewUnroll; ++u) {
-            const int k = (s + u) * 32 + (int)c * 8;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                x[u][n] = few_load<VEC>(xr + (int64_t)n * 8 * g.ldx, k, g.depth, s + u < s1 && n * 8 + (int)quad < g.tokens);
-        }
-#pragma unroll
-        for (int u = 0; u < kFewUnroll; ++u) {
-#pragma unroll
-            for (int e = 0; e < kSides; ++e) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint4 a = w[u][e][0], b = w[u][e][1];
-                    mma_16816<T>(acc[e][n], a.x, b.x, a.y, b.y, x[u][n].x, x[u][n].y);
-                    mma_16816<T>(acc[e][n], a.z, b.z, a.w, b.w, x[u][n].z, x[u][n].w);
-                }
-            }
-        }
+        few_commit();
     }
 #pragma unroll
     for (int e = 0; e < kSides; ++e) {
@@ -883,18 +898,33 @@ Shape choose(const Extent *outs, int count, int k_blocks, bool b_mn, int pairs)
 
 inline uint64_t partial_bytes(int64_t slots, int bn) { return (uint64_t)slots * kBM * bn * sizeof(float); }
 
+// Lets a kernel use more than 48 KB of shared memory; once a kernel and device.
+int allow_smem(const void *fn, size_t bytes)
+{
+    struct Allowed {
+        const void *fn;
+        int device;
+    };
+    static std::mutex lock;
+    static Allowed allowed[256];
+    static int count = 0;
+    int device = 0;
+    A2_TRAIN_CUDA(cudaGetDevice(&device));
+    std::lock_guard<std::mutex> hold(lock);
+    for (int i = 0; i < count; ++i) {
+        if (allowed[i].fn == fn && allowed[i].device == device) return A2SGD_OK;
+    }
+    A2_TRAIN_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (count < 256) allowed[count++] = Allowed{fn, device};
+    return A2SGD_OK;
+}
+
 template <typename T, int EPI, bool A_MN, bool B_MN, int ACT = 0>
 int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
 {
     const void *fn = reinterpret_cast<const void *>(&k_gemm<T, EPI, A_MN, B_MN, ACT>);
-    static std::atomic<uint64_t> allowed{0}; // devices on which this kernel may use its shared memory
-    int device = 0;
-    A2_TRAIN_CUDA(cudaGetDevice(&device));
-    const uint64_t bit = 1ull << (device & 63);
-    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        A2_TRAIN_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024)));
-        allowed.fetch_or(bit, std::memory_order_relaxed);
-    }
+    const int rc = allow_smem(fn, kSmem - 1024);
+    if (rc != A2SGD_OK) return rc;
     const int pairs = sms / 2;
     g.whole = g.splits > 1 ? tiles / pairs * pairs : tiles;
     g.items = g.whole + (tiles - g.whole) * g.splits;
@@ -1012,12 +1042,16 @@ template <typename T, bool DUAL>
 int launch_few(FewArgs &g, bool vec, int sms, cudaStream_t s)
 {
     const void *fn = vec ? pick_few<T, DUAL, true>(g.tokens) : pick_few<T, DUAL, false>(g.tokens);
+    const int nt = g.tokens <= 8 ? 1 : g.tokens <= 16 ? 2 : 4;
+    const size_t smem = (size_t)kFewWarps * few_steps_ahead(DUAL, nt) * ((DUAL ? 4 : 2) + nt) * kFewPiece;
+    const int rc = allow_smem(fn, smem);
+    if (rc != A2SGD_OK) return rc;
     // the depth is shared out over a cluster until there are two CTAs an SM, as long as a warp keeps two steps
     const int groups = ceil_div(g.rows, 16), steps = ceil_div(g.depth, 32);
     g.parts = 1;
     while (g.parts < 8 && groups * g.parts < 2 * sms && steps >= g.parts * 2 * kFewWarps * 2) g.parts *= 2;
     void *params[] = {&g};
-    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(groups * g.parts)), 32 * kFewWarps, 0, params, s, (unsigned)g.parts));
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(groups * g.parts)), 32 * kFewWarps, smem, params, s, (unsigned)g.parts));
     return A2SGD_OK;
 }
 
