@@ -192,6 +192,17 @@ struct Item {
     int slot;           // of the partial sums; -1: the whole depth
 };
 
+// a / b and its remainder for a < 2^24 and quotients below 2^20: by the approximate reciprocal, put right by one.  Every
+// role works out every tile, and the compiler's divisions took 1000 clocks of it, as long as a tile of two slices.
+__device__ __forceinline__ int quick_div(int a, int b, int &rest)
+{
+    int q = __float2int_rz(__fdividef((float)a, (float)b));
+    rest = a - q * b;
+    if (rest < 0) --q, rest += b;
+    if (rest >= b) ++q, rest -= b;
+    return q;
+}
+
 // Tiles are walked in groups of 8 tiles down, so that the pairs at work share slices of both operands in L2.
 __device__ __forceinline__ Item item_at(const GemmArgs &g, int i)
 {
@@ -200,19 +211,23 @@ __device__ __forceinline__ Item item_at(const GemmArgs &g, int i)
     t.slot = -1;
     if (i >= g.whole) {
         t.slot = i - g.whole;
-        tile = g.whole + t.slot / g.splits;
-        part = t.slot % g.splits;
+        tile = g.whole + quick_div(t.slot, g.splits, part);
     }
     t.p = 0;
-    while (t.p + 1 < g.problems && tile >= g.problem[t.p + 1].first) ++t.p;
+    if (g.problems > 1 && tile >= g.problem[1].first) t.p = g.problems > 2 && tile >= g.problem[2].first ? 2 : 1;
     const Problem &q = g.problem[t.p];
     tile -= q.first;
-    const int per_group = 8 * q.tiles_n, group = tile / per_group, rest = tile - group * per_group;
-    const int down = min(8, q.tiles_m - group * 8);
-    t.tm = group * 8 + rest % down;
-    t.tn = rest / down;
-    t.k0 = t.slot < 0 ? 0 : (int)((int64_t)q.k_blocks * part / g.splits);
-    t.k1 = t.slot < 0 ? q.k_blocks : (int)((int64_t)q.k_blocks * (part + 1) / g.splits);
+    int rest, row;
+    const int group = quick_div(tile, 8 * q.tiles_n, rest);
+    t.tn = quick_div(rest, min(8, q.tiles_m - group * 8), row);
+    t.tm = group * 8 + row;
+    t.k0 = 0;
+    t.k1 = q.k_blocks;
+    if (t.slot >= 0) {
+        int unused;
+        t.k0 = quick_div(q.k_blocks * part, g.splits, unused);
+        t.k1 = quick_div(q.k_blocks * (part + 1), g.splits, unused);
+    }
     t.cols = min(g.bn, (q.n - t.tn * g.bn + 31) / 32 * 32);
     return t;
 }
@@ -1024,8 +1039,11 @@ int check_sizes(uint64_t tokens, uint32_t d, uint32_t f, int dtype, int act)
     if ((dtype != A2SGD_BF16 && dtype != A2SGD_F16) || (act != A2SGD_ACT_SILU && act != A2SGD_ACT_GELU_TANH)) return A2SGD_ERR_ARG;
     if (d == 0 || f == 0) return A2SGD_ERR_ARG;
     if (tokens >= (1ull << 30) || d >= (1u << 24) || f >= (1u << 24)) return A2SGD_ERR_TOO_LARGE;
-    // tiles are counted in 32 bits
-    if ((tokens / kBM + 1) * (std::max(d, f) / 128 + 1) >= (1ull << 30) || ((uint64_t)d / 128 + 1) * (f / 128 + 1) >= (1ull << 28))
+    // tiles and slices are counted in 24 bits, what a tile's place in them is worked out from
+    constexpr uint64_t kMost = 1ull << 24;
+    const uint64_t wide = std::max(d, f) / 64 + 1;
+    if ((tokens / kBM + 1) * wide >= kMost || 3 * ((uint64_t)d / 64 + 1) * ((uint64_t)f / 64 + 1) >= kMost ||
+        std::max<uint64_t>(tokens, 2 * std::max(d, f)) / kBK * kMostPairs >= kMost)
         return A2SGD_ERR_TOO_LARGE;
     return A2SGD_OK;
 }
