@@ -25,7 +25,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <mutex>
 #include <type_traits>
 
 using namespace a2sgd_train;
@@ -82,6 +81,10 @@ struct GemmArgs {
     // Work: `whole` tiles, then the remaining ones in `splits` parts of their depth each
     int whole, items, splits;
     float *partials;    // [items - whole][bn / 4][256][4]
+    // Rows that the next launch will read, brought into L2 once this one's own loads are on their way (rows 0: none)
+    const void *ahead[2];
+    int64_t ahead_ld;
+    int ahead_rows, ahead_bytes;
 };
 
 // ------------------------------------------------------------------ activations
@@ -328,6 +331,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                         phase ^= 1u;
                     }
                 }
+            }
+        }
+        if (warp == 2 && chosen) {
+            for (int r = blockIdx.x; r < g.ahead_rows; r += gridDim.x) {
+                const int64_t at = r * g.ahead_ld * 2;
+                l2_prefetch(static_cast<const char *>(g.ahead[0]) + at, g.ahead_bytes);
+                if (g.ahead[1]) l2_prefetch(static_cast<const char *>(g.ahead[1]) + at, g.ahead_bytes);
             }
         }
         // every slice has been consumed: nothing is in flight towards this CTA any more
@@ -913,33 +923,11 @@ Shape choose(const Extent *outs, int count, int k_blocks, bool b_mn, int pairs)
 
 inline uint64_t partial_bytes(int64_t slots, int bn) { return (uint64_t)slots * kBM * bn * sizeof(float); }
 
-// Lets a kernel use more than 48 KB of shared memory; once a kernel and device.
-int allow_smem(const void *fn, size_t bytes)
-{
-    struct Allowed {
-        const void *fn;
-        int device;
-    };
-    static std::mutex lock;
-    static Allowed allowed[256];
-    static int count = 0;
-    int device = 0;
-    A2_TRAIN_CUDA(cudaGetDevice(&device));
-    std::lock_guard<std::mutex> hold(lock);
-    for (int i = 0; i < count; ++i) {
-        if (allowed[i].fn == fn && allowed[i].device == device) return A2SGD_OK;
-    }
-    A2_TRAIN_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    if (count < 256) allowed[count++] = Allowed{fn, device};
-    return A2SGD_OK;
-}
-
 template <typename T, int EPI, bool A_MN, bool B_MN, int ACT = 0>
 int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
 {
     const void *fn = reinterpret_cast<const void *>(&k_gemm<T, EPI, A_MN, B_MN, ACT>);
-    const int rc = allow_smem(fn, kSmem - 1024);
-    if (rc != A2SGD_OK) return rc;
+    A2_TRAIN_CUDA(allow_smem(fn, kSmem - 1024));
     const int pairs = sms / 2;
     g.whole = g.splits > 1 ? tiles / pairs * pairs : tiles;
     g.items = g.whole + (tiles - g.whole) * g.splits;
@@ -952,6 +940,18 @@ int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
         A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / kJoinCols), kBM / 32), 256, 0,
                              params, s));
     return A2SGD_OK;
+}
+
+// The weights of the next product, for launches of no more than one round of tiles: their ends and the next launch's
+// start would leave the memory idle.  Rows that bulk copies can read (the pointers are TMA operands': 16-byte rows).
+void bring_ahead(GemmArgs &g, int tiles, int sms, const Matrix &w0, const Matrix *w1)
+{
+    if (tiles > sms / 2 * 2 || (w1 && w1->ld != w0.ld)) return;
+    g.ahead[0] = w0.p;
+    g.ahead[1] = w1 ? w1->p : nullptr;
+    g.ahead_ld = w0.ld;
+    g.ahead_bytes = w0.cols / 8 * 16;
+    g.ahead_rows = g.ahead_bytes ? (int)w0.rows : 0;
 }
 
 // The maps of one operand pair.  An operand that is not transposed lies as [rows, k], a transposed one as [k, rows].
@@ -1062,8 +1062,7 @@ int launch_few(FewArgs &g, bool vec, int sms, cudaStream_t s)
     const void *fn = vec ? pick_few<T, DUAL, true>(g.tokens) : pick_few<T, DUAL, false>(g.tokens);
     const int nt = g.tokens <= 8 ? 1 : g.tokens <= 16 ? 2 : 4;
     const size_t smem = (size_t)kFewWarps * few_steps_ahead(DUAL, nt) * ((DUAL ? 4 : 2) + nt) * kFewPiece;
-    const int rc = allow_smem(fn, smem);
-    if (rc != A2SGD_OK) return rc;
+    A2_TRAIN_CUDA(allow_smem(fn, smem));
     // the depth is shared out over a cluster until there are two CTAs an SM, as long as a warp keeps two steps
     const int groups = ceil_div(g.rows, 16), steps = ceil_div(g.depth, 32);
     g.parts = 1;
@@ -1128,6 +1127,7 @@ int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &w
         (ph.p != h.p && !set_rows(g.out2, whole_rows(ph), dtype)) || !set_rows(g.gate, gate, dtype) || !set_rows(g.up, up, dtype))
         return A2SGD_ERR_CUDA;
     const int tiles = add_problem(g, t, f, 128, 0, 1, d, 0);
+    bring_ahead(g, tiles, sms, pd, nullptr);
     rc = act == A2SGD_ACT_SILU ? launch_gemm<T, kGate, false, false, A2SGD_ACT_SILU>(g, tiles, sms, s)
                                : launch_gemm<T, kGate, false, false, A2SGD_ACT_GELU_TANH>(g, tiles, sms, s);
     if (rc != A2SGD_OK) return rc;
@@ -1185,6 +1185,7 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
             !set_rows(g.gate, pgate, dtype, 32, false) || !set_rows(g.up, pup, dtype, 32, false))
             return A2SGD_ERR_CUDA;
         const int tiles = add_problem(g, t, f, g.bn, 0, 1, d, 0);
+        if (dx.p) bring_ahead(g, tiles, sms, pwg, &pwu);
         rc = act == A2SGD_ACT_SILU ? launch_gemm<T, kGateGrad, false, true, A2SGD_ACT_SILU>(g, tiles, sms, s)
                                    : launch_gemm<T, kGateGrad, false, true, A2SGD_ACT_GELU_TANH>(g, tiles, sms, s);
         if (rc != A2SGD_OK) return rc;

@@ -110,6 +110,11 @@ __device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int 
 {
     asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
 }
+// Consecutive bytes into L2 only: address and size multiples of 16.
+__device__ __forceinline__ void l2_prefetch(const void *p, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
 // A tile out of shared memory; what lies outside the matrix is not written.
 __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src)
 {

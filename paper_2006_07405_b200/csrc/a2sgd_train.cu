@@ -4,6 +4,7 @@
 #include <map>
 #include <mutex>
 #include <tuple>
+#include <utility>
 
 namespace a2sgd_train {
 
@@ -45,6 +46,26 @@ int resident_ctas(const void *fn, unsigned threads, size_t smem)
     } catch (...) { // as above
     }
     return n;
+}
+
+cudaError_t allow_smem(const void *fn, size_t bytes)
+{
+    static std::mutex lock;
+    static std::map<std::pair<const void *, int>, size_t> allowed;
+    int device = 0;
+    const cudaError_t err = cudaGetDevice(&device);
+    if (err != cudaSuccess) return err;
+    std::lock_guard<std::mutex> hold(lock);
+    const auto key = std::make_pair(fn, device);
+    const auto it = allowed.find(key);
+    if (it != allowed.end() && it->second >= bytes) return cudaSuccess;
+    const cudaError_t set = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (set != cudaSuccess) return set;
+    try {
+        allowed[key] = bytes;
+    } catch (...) { // no memory for the note: set again next time
+    }
+    return cudaSuccess;
 }
 
 } // namespace a2sgd_train

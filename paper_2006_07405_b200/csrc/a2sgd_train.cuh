@@ -230,6 +230,9 @@ int sm_count(int device);
 // CTAs of a kernel that an SM of the current device holds at once, at least 1; asked once a kernel and shape.
 int resident_ctas(const void *fn, unsigned threads, size_t smem);
 
+// Lets a kernel use that much dynamic shared memory on the current device; once a kernel, device and amount.
+cudaError_t allow_smem(const void *fn, size_t bytes);
+
 } // namespace a2sgd_train
 
 #define A2_TRAIN_CUDA(call)              \
