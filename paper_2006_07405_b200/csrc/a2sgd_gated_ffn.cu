@@ -1180,7 +1180,9 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
 
     if (inner) {
         GemmArgs g{};
-        set_shape(g, Shape(), nullptr);
+        Shape narrow; // half the columns where that still makes one round of tiles: twice the SMs bring in Wd
+        if ((int64_t)ceil_div(t, kBM) * ceil_div(f, 128) <= sms / 2) narrow.bn = 128;
+        set_shape(g, narrow, nullptr);
         if (!add_operands<false, true>(g, 0, pdy, pwd, dtype) || !set_rows(g.out[0], whole_rows(da), dtype, 32) || !set_rows(g.out2, whole_rows(db), dtype, 32) ||
             !set_rows(g.gate, pgate, dtype, 32, false) || !set_rows(g.up, pup, dtype, 32, false))
             return A2SGD_ERR_CUDA;
