@@ -178,14 +178,26 @@ __device__ __forceinline__ void rows_out(const Rows &o, uint32_t buf, int row0, 
         }
     } else {
         __syncwarp();
-        const int rows = min(32, m - row0);
-        for (int r = 0; r < rows; ++r) {
-            uint16_t *p = static_cast<uint16_t *>(o.p) + (int64_t)(row0 + r) * o.ld + col0;
-            for (int c = lane; c < min(64, n - col0); c += 32) p[c] = ld_shared16(piece(buf, r, c >> 3) + (c & 7) * 2);
+        const int rows = min(32, m - row0), cols = min(64, n - col0), c0 = lane, c1 = lane + 32;
+        uint16_t *p = static_cast<uint16_t *>(o.p) + (int64_t)row0 * o.ld + col0;
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += 8) { // eight rows' reads before their writes
+            uint16_t v[8][2];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                v[r][0] = ld_shared16(piece(buf, r0 + r, c0 >> 3) + (c0 & 7) * 2);
+                v[r][1] = ld_shared16(piece(buf, r0 + r, c1 >> 3) + (c1 & 7) * 2);
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r, p += o.ld) {
+                if (r0 + r < rows && c0 < cols) p[c0] = v[r][0];
+                if (r0 + r < rows && c1 < cols) p[c1] = v[r][1];
+            }
         }
         __syncwarp();
     }
 }
+
 // ------------------------------------------------------------------ the product
 // One piece of work: a tile, all of its depth or a part of it.
 struct Item {
