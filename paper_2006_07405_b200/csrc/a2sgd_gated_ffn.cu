@@ -51,9 +51,9 @@ enum Epilogue { kStore = 0, kGate = 1, kGateGrad = 2 };
 // Latched when a kernel's bounded wait ran out; read and cleared by a2sgd_gated_ffn_status.
 __device__ int g_status = 0;
 
-// 16-bit rows that the epilogue writes or reads: by TMA where `map` could be made, else element by element.
+// 16-bit rows that the epilogue writes, by TMA where `map` could be made, else element by element; or reads.
 struct Rows {
-    CUtensorMap map; // boxes of 32 rows and 64 columns (kGateGrad: 32)
+    CUtensorMap map; // boxes of 32 rows and 64 columns
     void *p;
     int64_t ld;
     int tma;
@@ -253,7 +253,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t staging = base + kOperands;
-    __shared__ __align__(8) uint64_t bars[2 * kMostStages + 4 + 2 * kEpilogueWarps];
+    __shared__ __align__(8) uint64_t bars[2 * kMostStages + 4];
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
     const auto empty = [&](int s) { return bar0 + 8u * (kMostStages + s); };
@@ -273,7 +273,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
             bar_init(acc_full(i), 1);
             bar_init(acc_empty(i), 2 * kEpilogueWarps);
         }
-        for (int i = 0; i < 2 * kEpilogueWarps; ++i) bar_init(bar0 + 8u * (2 * kMostStages + 4 + i), 1);
         gave_up = 0;
         bar_init_fence();
     }
@@ -403,9 +402,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         // ---------------------------------------------------------- accumulators out
         const uint32_t quarter = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2; // a warp reads the TMEM lanes of its quarter
         const uint32_t buf0 = staging + (warp - kFirstEpilogueWarp) * 2 * kStaging, buf1 = buf0 + kStaging;
-        const uint32_t loaded = bar0 + 8u * (2 * kMostStages + 4 + 2 * (warp - kFirstEpilogueWarp)); // and the one after it
         int turn = 0;
-        uint32_t blocks = 0; // of a and b that have been asked for (kGateGrad)
         for (int i = pair; i < g.items; i += pairs, ++turn) {
             const Item t = item_at(g, i);
             const Problem &q = g.problem[t.p];
@@ -453,43 +450,50 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                     if (g.out2.p) rows_out(g.out2, buf0, row0, col0, q.m, q.n, lane);
                 }
             } else if constexpr (EPI == kGateGrad) {
-                // Blocks of 32 columns.  a and b arrive where da and db leave from; there are two such places, so
-                // that one block is brought in while another is worked on.  The first two of a tile are asked for
-                // before its products are done, the others brought into L2.  (With one place of 64 columns the
-                // waits for the store out and the load in made 10000 clocks a tile, for 14600 of products.)
+                // Blocks of 32 columns, two in turn: one is brought in while another is worked on, and da and db leave from
+                // where a and b arrived, by cp.async and plain stores, 64 consecutive bytes a row (TMA boxes with a
+                // barrier a block measured the same).
                 const int count = (min(t.cols, q.n - t.tn * g.bn) + 31) / 32, rounds = live ? (count - (int)half + 1) / 2 : 0;
-                const int first = t.tn * g.bn + half * 32; // this warp's blocks: every second one
-                const auto ask = [&](int k) {
-                    const uint32_t place = blocks++ & 1;
-                    if (lane == 0) {
-                        bar_expect(loaded + 8u * place, kStaging);
-                        tma_load(buf0 + place * kStaging, &g.gate.map, first + 64 * k, row0, loaded + 8u * place);
-                        tma_load(buf0 + place * kStaging + kStaging / 2, &g.up.map, first + 64 * k, row0, loaded + 8u * place);
-                    }
+                const int first = t.tn * g.bn + half * 32;       // this warp's blocks: every second one
+                const int copy_row = lane >> 2, copy_piece = lane & 3; // rows copy_row + 8 i, 16 bytes of each
+                const auto place = [&](int k, uint32_t row, uint32_t e) {
+                    return buf0 + (k & 1) * kStaging + row * 64 + ((e ^ (row >> 1 & 3)) << 4); // swizzled; b 2 KB on
                 };
-                if (lane == 0) {
-                    for (int k = 2; k < rounds; ++k) {
-                        tma_prefetch(&g.gate.map, first + 64 * k, row0);
-                        tma_prefetch(&g.up.map, first + 64 * k, row0);
+                const auto bring = [&](int k) {
+                    const int col = first + 64 * k + copy_piece * 8;
+                    const uint32_t bytes = max(0, min(8, q.n - col)) * 2;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = copy_row + 8 * i, row = row0 + r;
+                        const bool there = k < rounds && row < q.m && bytes;
+                        const int64_t at_gate = there ? (int64_t)row * g.gate.ld + col : 0, at_up = there ? (int64_t)row * g.up.ld + col : 0;
+                        async_copy16(place(k, r, copy_piece), static_cast<const T *>(g.gate.p) + at_gate, there ? bytes : 0);
+                        async_copy16(place(k, r, copy_piece) + kStaging / 2, static_cast<const T *>(g.up.p) + at_up, there ? bytes : 0);
                     }
-                    tma_store_read<0>(); // the last tile's stores have been read out of both places
+                    async_commit();
+                };
+                if (row0 + (int)lane < q.m) { // the later blocks into L2: a row's 128 bytes for both halves' warps
+                    const Rows &o = half ? g.up : g.gate;
+                    for (int k = 2; k < rounds; ++k) l2_prefetch_line(static_cast<const T *>(o.p) + (int64_t)(row0 + lane) * o.ld + t.tn * g.bn + 64 * k);
                 }
-                __syncwarp();
-                const uint32_t begin = blocks;
-                for (int k = 0; k < min(rounds, 2); ++k) ask(k);
+                bring(0);
+                bring(1);
                 if (!bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
                 fence_after();
-                bool ok = true;
                 for (int k = 0; k < rounds; ++k) {
-                    const uint32_t use = begin + k, place = use & 1, at = buf0 + place * kStaging;
-                    ok = bar_wait(loaded + 8u * place, (use >> 1) & 1, &gave_up);
-                    if (!__all_sync(0xffffffffu, ok)) break;
                     float dh[32];
                     tmem_ld32(d + half * 32 + 64 * k, dh);
+                    async_wait<1>();
+                    __syncwarp();
                     tmem_wait_ld();
+                    if (k + 1 == rounds) { // all that this warp reads has been read
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint32_t pa = at + lane * 64 + ((e ^ (lane >> 1 & 3)) << 4), pb = pa + kStaging / 2; // 64-byte rows, swizzled
+                        const uint32_t pa = place(k, lane, e), pb = pa + kStaging / 2;
                         float a[8], b[8];
                         unpack8<T>(ld_shared(pa), a);
                         unpack8<T>(ld_shared(pb), b);
@@ -497,23 +501,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
                         st_shared(pa, pack8<T>(a));
                         st_shared(pb, pack8<T>(b));
                     }
-                    if (k > 0 && k + 1 < rounds) { // the block before this one has left by now: its place is free
-                        if (lane == 0) tma_store_read<0>();
-                        __syncwarp();
-                        ask(k + 1);
-                    }
-                    fence_async();
                     __syncwarp();
-                    if (lane == 0) {
-                        tma_store(&g.out[0].map, first + 64 * k, row0, at);
-                        tma_store(&g.out2.map, first + 64 * k, row0, at + kStaging / 2);
-                        tma_store_commit();
+                    const int col = first + 64 * k + copy_piece * 8;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { // da and db have padded rows: whole pieces
+                        const int r = copy_row + 8 * i, row = row0 + r;
+                        const uint4 va = ld_shared(place(k, r, copy_piece)), vb = ld_shared(place(k, r, copy_piece) + kStaging / 2);
+                        if (row < q.m && col < q.n) {
+                            *reinterpret_cast<uint4 *>(static_cast<T *>(g.out[0].p) + (int64_t)row * g.out[0].ld + col) = va;
+                            *reinterpret_cast<uint4 *>(static_cast<T *>(g.out2.p) + (int64_t)row * g.out2.ld + col) = vb;
+                        }
                     }
+                    __syncwarp();
+                    bring(k + 2);
                 }
-                if (!__all_sync(0xffffffffu, ok)) break;
-                fence_before();
+                if (rounds == 0) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
+                }
+                async_wait<0>();
                 __syncwarp();
-                if (lane == 0) bar_arrive_cluster(map_to(acc_empty(acc), 0));
             } else {
                 if (!bar_wait(acc_full(acc), (turn >> 1) & 1, &gave_up)) break;
                 fence_after();
@@ -674,7 +682,7 @@ __device__ __forceinline__ void few_copy(uint32_t place, const uint16_t *row, in
 {
     const int there = live && k < depth ? min(8, depth - k) : 0;
     if constexpr (VEC) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place), "l"(there ? row + k : row), "r"(2 * there) : "memory");
+        async_copy16(place, there ? row + k : row, 2 * there);
     } else {
         uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -684,10 +692,6 @@ __device__ __forceinline__ void few_copy(uint32_t place, const uint16_t *row, in
         st_shared(place, make_uint4(w[0], w[1], w[2], w[3]));
     }
 }
-__device__ __forceinline__ void few_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void few_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 template <typename T, bool DUAL, int NT, bool VEC>
 __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ FewArgs g)
 {
@@ -736,11 +740,11 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     }
     for (int s = s0; s < s0 + kAhead; ++s) {
         if (s < s1) copy_tokens(s);
-        few_commit();
+        async_commit();
     }
     float acc[kSides][NT][4] = {};
     for (int s = s0; s < s1; ++s) {
-        few_wait<kAhead - 1>();
+        async_wait<kAhead - 1>();
         uint4 a[kSides][2], b[NT];
 #pragma unroll
         for (int e = 0; e < kSides; ++e) {
@@ -761,7 +765,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
             copy_weights(s + kAhead);
             copy_tokens(s + kAhead);
         }
-        few_commit();
+        async_commit();
     }
 #pragma unroll
     for (int e = 0; e < kSides; ++e) {
@@ -846,17 +850,17 @@ struct Matrix {
 
 inline int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-// Tiles of `box_rows` rows and 64 or 32 columns, 128 or 64 bytes a row, swizzled.
-bool make_map(CUtensorMap *map, const Matrix &m, int dtype, int box_rows, int box_cols = 64)
+// Tiles of `box_rows` rows and 64 columns, 128 bytes a row, swizzled.
+bool make_map(CUtensorMap *map, const Matrix &m, int dtype, int box_rows)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(m.rows > 1 ? m.ld : padded(m.cols)) * 2}; // one row: any stride is right
-    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
     return encode(map, dtype == A2SGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
                   const_cast<void *>(m.p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -864,14 +868,21 @@ inline bool tma_ok(const Matrix &m) { return aligned(m.p, 16) && (m.rows <= 1 ||
 inline uint64_t room(int64_t rows, int64_t cols) { return ((uint64_t)rows * padded(cols) * 2 + 255) / 256 * 256; }
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// What the epilogue writes or reads: by TMA where rows allow it.  A TMA store leaves out what lies past the end of a
-// row in pieces of 16 bytes only, so that rows of other lengths are written element by element.
-bool set_rows(Rows &r, const Matrix &m, int dtype, int box_cols = 64, bool written = true)
+// What the epilogue writes: by TMA where rows allow it.  A TMA store leaves out what lies past the end of a row in pieces
+// of 16 bytes only, so that rows of other lengths are written element by element.
+bool set_rows(Rows &r, const Matrix &m, int dtype)
 {
     r.p = const_cast<void *>(m.p);
     r.ld = m.ld;
-    r.tma = m.p && tma_ok(m) && (!written || m.cols % 8 == 0);
-    return !r.tma || make_map(&r.map, m, dtype, 32, box_cols);
+    r.tma = m.p && tma_ok(m) && m.cols % 8 == 0;
+    return !r.tma || make_map(&r.map, m, dtype, 32);
+}
+
+// Rows that are read or written without TMA.
+void set_plain(Rows &r, const Matrix &m)
+{
+    r.p = const_cast<void *>(m.p);
+    r.ld = m.ld;
 }
 
 // Rows of the workspace with their padding, which may be written.
@@ -1195,9 +1206,11 @@ int backward(const Matrix &dy, const Matrix &x, const Matrix &wg, const Matrix &
         Shape narrow; // half the columns where that still makes one round of tiles: twice the SMs bring in Wd
         if ((int64_t)ceil_div(t, kBM) * ceil_div(f, 128) <= sms / 2) narrow.bn = 128;
         set_shape(g, narrow, nullptr);
-        if (!add_operands<false, true>(g, 0, pdy, pwd, dtype) || !set_rows(g.out[0], whole_rows(da), dtype, 32) || !set_rows(g.out2, whole_rows(db), dtype, 32) ||
-            !set_rows(g.gate, pgate, dtype, 32, false) || !set_rows(g.up, pup, dtype, 32, false))
-            return A2SGD_ERR_CUDA;
+        if (!add_operands<false, true>(g, 0, pdy, pwd, dtype)) return A2SGD_ERR_CUDA;
+        set_plain(g.out[0], da);
+        set_plain(g.out2, db);
+        set_plain(g.gate, pgate);
+        set_plain(g.up, pup);
         const int tiles = add_problem(g, t, f, g.bn, 0, 1, d, 0);
         if (dx.p) bring_ahead(g, tiles, sms, pwg, &pwu);
         rc = act == A2SGD_ACT_SILU ? launch_gemm<T, kGateGrad, false, true, A2SGD_ACT_SILU>(g, tiles, sms, s)

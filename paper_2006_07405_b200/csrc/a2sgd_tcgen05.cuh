@@ -46,10 +46,11 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// bar: a shared::cluster address, of either CTA
+// bar: a shared::cluster address, of either CTA.  For what has been read out of TMEM only: no memory that the other side
+// reads is released (with a release for the cluster the arrival waited 2000 clocks for the tile's stores).
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
@@ -97,24 +98,20 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *m
                  : "memory");
 }
 
-// A tile for this CTA alone.
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes "
-                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
-                 : "memory");
-}
-// The same tile into L2 only.
-__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int y)
-{
-    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
-}
 // Consecutive bytes into L2 only: address and size multiples of 16.
 __device__ __forceinline__ void l2_prefetch(const void *p, uint32_t bytes)
 {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void l2_prefetch_line(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+// 16 bytes into shared memory, the first `bytes` of them from global memory, zeros after.
+__device__ __forceinline__ void async_copy16(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // A tile out of shared memory; what lies outside the matrix is not written.
 __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src)
 {
