@@ -640,13 +640,15 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
 }
 
 // ------------------------------------------------------------------ few tokens
-// Up to 32 tokens the block is bound by the weights' bytes, and tiles of 256 rows would be nearly empty.  Here
+// Up to 16 tokens the block is bound by the weights' bytes, and tiles of 256 rows would be nearly empty.  Here
 // the weights are the left operand of mma.sync (m16n8k16), 16 of their rows a CTA.  A lane copies 16 bytes, 8 consecutive
 // k of one row, into a place of shared memory that it alone reads, several steps ahead (cp.async: no registers held, no
 // barrier); since the order of k within a product is free as long as both operands share it, those 8 are the lane's part
 // of two products, and the tokens' 8 k lie the same way.  Four warps, and the CTAs of a cluster, share the depth; their
 // sums meet in shared memory, in order, where the gate, the activation and the product are applied.
-constexpr int kFewTokens = 32;
+// One call with d = 1600, f = 6400, its weights from memory: 8 tokens 16.8 us, 16 tokens 19.0; 24 and 32 tokens, with four
+// blocks of 8, 30.9 and 31.9 against 28.8 and 29.0 of the tiles above.
+constexpr int kFewTokens = 16;
 constexpr int kFewWarps = 4;
 constexpr uint32_t kFewPiece = 32 * 16; // what a warp copies at once
 // Steps of 32 k on their way: as many as leave room for three CTAs an SM.
@@ -1074,16 +1076,14 @@ int check_sizes(uint64_t tokens, uint32_t d, uint32_t f, int dtype, int act)
 template <typename T, bool DUAL, bool VEC>
 const void *pick_few(int tokens)
 {
-    return tokens <= 8    ? reinterpret_cast<const void *>(&k_few<T, DUAL, 1, VEC>)
-           : tokens <= 16 ? reinterpret_cast<const void *>(&k_few<T, DUAL, 2, VEC>)
-                          : reinterpret_cast<const void *>(&k_few<T, DUAL, 4, VEC>);
+    return tokens <= 8 ? reinterpret_cast<const void *>(&k_few<T, DUAL, 1, VEC>) : reinterpret_cast<const void *>(&k_few<T, DUAL, 2, VEC>);
 }
 
 template <typename T, bool DUAL>
 int launch_few(FewArgs &g, bool vec, int sms, cudaStream_t s)
 {
     const void *fn = vec ? pick_few<T, DUAL, true>(g.tokens) : pick_few<T, DUAL, false>(g.tokens);
-    const int nt = g.tokens <= 8 ? 1 : g.tokens <= 16 ? 2 : 4;
+    const int nt = g.tokens <= 8 ? 1 : 2;
     const size_t smem = (size_t)kFewWarps * few_steps_ahead(DUAL, nt) * ((DUAL ? 4 : 2) + nt) * kFewPiece;
     A2_TRAIN_CUDA(allow_smem(fn, smem));
     // the depth is shared out over a cluster until there are two CTAs an SM, as long as a warp keeps two steps
