@@ -383,8 +383,8 @@ enum a2sgd_dtype { A2SGD_F32 = 0, A2SGD_BF16 = 1, A2SGD_F16 = 2 };
  *     g = c * grad
  *     m <- beta1 m + (1 - beta1) g          v <- beta2 v + (1 - beta2) g^2
  *     w <- w (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, each product, sum, quotient and root rounded once, in that order; the coefficients are formed
- * in fp64 and rounded once.  Weights are fp32; a 16-bit copy of them is written by the same pass when w16
+ * in fp32, each product, sum, quotient and root rounded once, in that order (a quotient of an |m| below 2^-100
+ * to within one unit in the last place); the coefficients are formed in fp64 and rounded once.  Weights are fp32; a 16-bit copy of them is written by the same pass when w16
  * is given.
  *
  * State.  One buffer each for m and v, holding the tensors one after another, every tensor starting at a
