@@ -400,7 +400,7 @@ enum a2sgd_dtype { A2SGD_F32 = 0, A2SGD_BF16 = 1, A2SGD_F16 = 2 };
  *            expectation is the value: with beta2 = 0.999 a step moves sqrt(v) by at most 0.05 % when
  *            gradients fall silent, and rounding to nearest would hold it still for ever.  v's code is at
  *            least 2 (6e-5 of the scale), so that |m| / sqrt(v) stays within what exact states can reach.
- *            A block that meets a gradient that is not finite holds NaN from then on, as 32-bit states do
+ *            A block that meets a gradient that is not finite is not finite from then on, as 32-bit states are
  *            element by element.
  *
  *   S, numel    number of tensors; HOST [S] element counts (each >= 1)

@@ -164,9 +164,9 @@ __device__ __forceinline__ f32x2 quotient2(f32x2 m, f32x2 d)
 }
 // v of a lane within 2^-80..2^80 and |m| up to 2^80: d = sqrt(v) root + eps lies between 2^-40 and 2^100 and no residual
 // leaves the normal range, but that of an m below 2^-100, whose quotient may be an ulp off.
-__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, float largest_m)
+__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, uint32_t largest_m)
 {
-    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x1p80f;
+    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x67800000u;
 }
 
 // GT: gradient type.  CT: type of the 16-bit copy of the weights, float when there is none.
@@ -192,10 +192,10 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
     const uint64_t block = (uint64_t)t.block + warp;
     const uint32_t live = min((uint32_t)t.count - first, kStateBlock);
     const bool vector = t.vector && live == kStateBlock;
-    // places inside the block: 8 consecutive ones a lane, or (any alignment) every 32nd
-    const uint32_t base = vector ? lane * 8 : lane, step = vector ? 1 : 32;
+    const uint32_t base = lane * 8; // a lane's 8 consecutive places inside the block
 
-    float w[8], g[8], m[8], v[8];
+    __align__(16) float w[8], g[8];
+    float m[8], v[8];
     float *wp = t.w + first;
     const GT *gp = static_cast<const GT *>(t.grad) + first;
     const uint64_t at = block * kStateBlock + base;
@@ -205,14 +205,16 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
     if constexpr (EIGHT) {
         ms = __ldcg(a.m_scale + block);
         vs = __ldcg(a.v_scale + block);
-        if (vector) {
-            mw = *reinterpret_cast<const uint2 *>(a.mq + at);
-            vw = *reinterpret_cast<const uint2 *>(a.vq + at);
-        }
-    } else if (vector) {
+        mw = *reinterpret_cast<const uint2 *>(a.mq + at);
+        vw = *reinterpret_cast<const uint2 *>(a.vq + at);
+    } else {
         ld256(a.m + at, m);
         ld256(a.v + at, v);
     }
+    // Tensors that wide accesses cannot read, and their last blocks, go through shared memory: every 32nd element of
+    // the block a lane in memory, 8 consecutive ones in the arithmetic.
+    __shared__ __align__(16) float turn[kThreads / 32][2][kStateBlock];
+    float(*mine)[kStateBlock] = turn[warp];
     if (vector) {
         Raw8<GT> graw;
         ld256(wp + base, w);
@@ -221,18 +223,20 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t p = base + i * 32;
-            const bool in = p < live;
-            w[i] = in ? wp[p] : 0.0f;
-            g[i] = in ? to_f32(gp[p]) : 0.0f;
-            if constexpr (EIGHT) {
-                const uint32_t mb = (uint8_t)a.mq[at + i * 32], vb = a.vq[at + i * 32];
-                (i < 4 ? mw.x : mw.y) |= mb << (8 * (i & 3));
-                (i < 4 ? vw.x : vw.y) |= vb << (8 * (i & 3));
-            } else {
-                m[i] = a.m[at + i * 32];
-                v[i] = a.v[at + i * 32];
-            }
+            const uint32_t p = lane + i * 32;
+            w[i] = p < live ? wp[p] : 0.0f;
+            g[i] = p < live ? to_f32(gp[p]) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            mine[0][lane + i * 32] = w[i];
+            mine[1][lane + i * 32] = g[i];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            *reinterpret_cast<float4 *>(w + i) = *reinterpret_cast<const float4 *>(&mine[0][base + i]);
+            *reinterpret_cast<float4 *>(g + i) = *reinterpret_cast<const float4 *>(&mine[1][base + i]);
         }
     }
     // m, v and sqrt(v) after the step
@@ -253,9 +257,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
             v2[i] = pair(v[2 * i], v[2 * i + 1]);
         }
     }
-    // v's bit patterns order like its values, NaN above infinity; an m that is not finite comes with such a v
-    uint32_t big_v = 0, least_v = 0xffffffffu;
-    float big_m = 0.0f;
+    uint32_t big_m = 0, big_v = 0, least_v = 0xffffffffu; // bit patterns order like the values, NaN above infinity
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const f32x2 gi = mul2(pair(g[2 * i], g[2 * i + 1]), pair(scale));
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
         unpair(v2[i], v[2 * i], v[2 * i + 1]);
 #pragma unroll
         for (int k = 2 * i; k < 2 * i + 2; ++k) {
-            big_m = fmaxf(big_m, fabsf(m[k]));
+            big_m = max(big_m, __float_as_uint(m[k]) & 0x7fffffffu);
             big_v = max(big_v, __float_as_uint(v[k]));
             least_v = min(least_v, __float_as_uint(v[k]));
         }
@@ -296,37 +298,33 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
         st256(wp + base, w);
         if constexpr (kCopy) store8(static_cast<CT *>(t.w16) + first + base, w);
     } else {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(&mine[0][base + i]) = *reinterpret_cast<const float4 *>(w + i);
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t p = base + i * 32;
+            const uint32_t p = lane + i * 32;
             if (p < live) {
-                wp[p] = w[i];
-                if constexpr (kCopy) static_cast<CT *>(t.w16)[first + p] = from_f32<CT>(w[i]);
+                const float x = mine[0][p];
+                wp[p] = x;
+                if constexpr (kCopy) static_cast<CT *>(t.w16)[first + p] = from_f32<CT>(x);
             }
         }
     }
     if constexpr (!EIGHT) {
-        if (vector) {
-            st256(a.m + at, m);
-            st256(a.v + at, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                a.m[at + i * 32] = m[i];
-                a.v[at + i * 32] = v[i];
-            }
-        }
+        st256(a.m + at, m);
+        st256(a.v + at, v);
     } else {
         // the largest root is the root of the largest v: a correctly rounded root is monotonic
         const float top_v = __uint_as_float(__reduce_max_sync(0xffffffffu, big_v));
-        const uint32_t top_m = __reduce_max_sync(0xffffffffu, __float_as_uint(big_m));
         const Gain gr = gain_of(__float_as_uint(__fsqrt_rn(top_v)), 65025.0f);
-        const Gain gm = gain_of(top_v == top_v ? top_m : __float_as_uint(top_v), 16129.0f);
+        const Gain gm = gain_of(__reduce_max_sync(0xffffffffu, big_m), 16129.0f);
         float qm[8], qr[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t h0 = dither_bits((uint32_t)at + 2 * i * step, a.dither);
-            const uint32_t h1 = dither_bits((uint32_t)at + (2 * i + 1) * step, a.dither);
+            const uint32_t h0 = dither_bits((uint32_t)at + 2 * i, a.dither);
+            const uint32_t h1 = dither_bits((uint32_t)at + 2 * i + 1, a.dither);
             const float m0 = m[2 * i], m1 = m[2 * i + 1];
             encode2(mul2(pair(fabsf(m0), fabsf(m1)), pair(gm.gain)), dither_m(h0), dither_m(h1), 127.0f, 0.0f, qm[2 * i], qm[2 * i + 1]);
             encode2(mul2(r2[i], pair(gr.gain)), dither_v(h0), dither_v(h1), 255.0f, 2.0f, qr[2 * i], qr[2 * i + 1]);
@@ -335,16 +333,8 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
         }
         const uint2 mo = make_uint2(bytes4(qm[0], qm[1], qm[2], qm[3]), bytes4(qm[4], qm[5], qm[6], qm[7]));
         const uint2 vo = make_uint2(bytes4(qr[0], qr[1], qr[2], qr[3]), bytes4(qr[4], qr[5], qr[6], qr[7]));
-        if (vector) {
-            *reinterpret_cast<uint2 *>(a.mq + at) = mo;
-            *reinterpret_cast<uint2 *>(a.vq + at) = vo;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                a.mq[at + i * 32] = (int8_t)((i < 4 ? mo.x : mo.y) >> (8 * (i & 3)));
-                a.vq[at + i * 32] = (uint8_t)((i < 4 ? vo.x : vo.y) >> (8 * (i & 3)));
-            }
-        }
+        *reinterpret_cast<uint2 *>(a.mq + at) = mo;
+        *reinterpret_cast<uint2 *>(a.vq + at) = vo;
         if (lane == 0) {
             a.m_scale[block] = gm.scale;
             a.v_scale[block] = gr.scale;
