@@ -647,14 +647,15 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
 // the weights are the left operand of mma.sync (m16n8k16), 16 of their rows a CTA.  A lane copies 16 bytes, 8 consecutive
 // k of one row, into a place of shared memory that it alone reads, several steps ahead (cp.async: no registers held, no
 // barrier); since the order of k within a product is free as long as both operands share it, those 8 are the lane's part
-// of two products, and the tokens' 8 k lie the same way.  Four warps, and the CTAs of a cluster, share the depth; their
+// of two products, and the tokens' 8 k lie the same way.  Eight warps, and the CTAs of a cluster, share the depth; their
 // sums meet in shared memory, in order, where the gate, the activation and the product are applied.
 // One call with d = 1600, f = 6400, its weights from memory: 8 tokens 16.8 us, 16 tokens 19.0; 24 and 32 tokens, with four
 // blocks of 8, 30.9 and 31.9 against 28.8 and 29.0 of the tiles above.
 constexpr int kFewTokens = 16;
-constexpr int kFewWarps = 4;
+constexpr int kFewWarps = 8;
 constexpr uint32_t kFewPiece = 32 * 16; // what a warp copies at once
-// Steps of 32 k on their way: as many as leave room for three CTAs an SM.
+// Steps of 32 k on their way: as many as leave room for three CTAs an SM.  One token, 1600 x 6400, weights from memory, in a
+// graph: 14.5 us (4.2 TB/s; 4096 x 11008: 50 us, 5.4 TB/s); 15.1 and 60 us with four warps, 20 us with two CTAs an SM.
 __host__ __device__ constexpr int few_steps_ahead(bool dual, int nt) { return 70 * 1024 / (kFewWarps * ((dual ? 4 : 2) + nt) * (int)kFewPiece) < 12 ? 70 * 1024 / (kFewWarps * ((dual ? 4 : 2) + nt) * (int)kFewPiece) : 12; }
 
 struct FewArgs {
@@ -708,7 +709,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     const int steps = (g.depth + 31) / 32, share = part * kFewWarps + warp, shares = g.parts * kFewWarps;
     const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
     const uint32_t mine = smem_u32(ring) + warp * kAhead * kPieces * kFewPiece + lane * 16;
-    const auto place = [&](int s, int p) { return mine + (uint32_t)((s - s0) % kAhead * kPieces + p) * kFewPiece; };
+    const auto place = [&](int slot, int p) { return mine + (uint32_t)(slot * kPieces + p) * kFewPiece; };
 
     // rows that do not exist are not read: their copies have no bytes, from the matrix's first row
     const bool live[2] = {row0 + (int)quad < g.rows, row0 + 8 + (int)quad < g.rows};
@@ -720,17 +721,17 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) x[n] = static_cast<const uint16_t *>(g.x) + (n * 8 + (int)quad < g.tokens ? (int64_t)(n * 8 + quad) * g.ldx : 0);
-    const auto copy_weights = [&](int s) {
+    const auto copy_weights = [&](int s, int slot) {
 #pragma unroll
         for (int e = 0; e < kSides; ++e) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) few_copy<VEC>(place(s, 2 * e + r), w[e][r], s * 32 + (int)c * 8, g.depth, live[r]);
+            for (int r = 0; r < 2; ++r) few_copy<VEC>(place(slot, 2 * e + r), w[e][r], s * 32 + (int)c * 8, g.depth, live[r]);
         }
     };
-    const auto copy_tokens = [&](int s) {
+    const auto copy_tokens = [&](int s, int slot) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-            few_copy<VEC>(place(s, 2 * kSides + n), x[n], s * 32 + (int)c * 8, g.depth, n * 8 + (int)quad < g.tokens);
+            few_copy<VEC>(place(slot, 2 * kSides + n), x[n], s * 32 + (int)c * 8, g.depth, n * 8 + (int)quad < g.tokens);
     };
     // The second launch of a call may start on its weights at once: the one before it, which wrote its tokens, does not
     // write them, and had itself waited for what was before the call.
@@ -738,26 +739,26 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
         wait_prior_grid();
         release_next_grid();
     }
-    for (int s = s0; s < min(s1, s0 + kAhead); ++s) copy_weights(s);
+    for (int s = s0; s < min(s1, s0 + kAhead); ++s) copy_weights(s, s - s0);
     if constexpr (!DUAL) {
         wait_prior_grid();
         release_next_grid();
     }
     for (int s = s0; s < s0 + kAhead; ++s) {
-        if (s < s1) copy_tokens(s);
+        if (s < s1) copy_tokens(s, s - s0);
         async_commit();
     }
     float acc[kSides][NT][4] = {};
-    for (int s = s0; s < s1; ++s) {
+    for (int s = s0, slot = 0; s < s1; ++s, slot = slot + 1 == kAhead ? 0 : slot + 1) {
         async_wait<kAhead - 1>();
         uint4 a[kSides][2], b[NT];
 #pragma unroll
         for (int e = 0; e < kSides; ++e) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) a[e][r] = ld_shared(place(s, 2 * e + r));
+            for (int r = 0; r < 2; ++r) a[e][r] = ld_shared(place(slot, 2 * e + r));
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) b[n] = ld_shared(place(s, 2 * kSides + n));
+        for (int n = 0; n < NT; ++n) b[n] = ld_shared(place(slot, 2 * kSides + n));
 #pragma unroll
         for (int e = 0; e < kSides; ++e) {
 #pragma unroll
@@ -767,8 +768,8 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
             }
         }
         if (s + kAhead < s1) {
-            copy_weights(s + kAhead);
-            copy_tokens(s + kAhead);
+            copy_weights(s + kAhead, slot);
+            copy_tokens(s + kAhead, slot);
         }
         async_commit();
     }
