@@ -506,6 +506,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_ln_fold(const __grid_constant__
     const uint32_t c = blockIdx.x * kFoldCols + lane; // of the 2 d columns dw | db
     float v = 0.0f;
     if (c < 2 * a.d) {
+#pragma unroll 4
         for (uint32_t p = slice; p < a.parts; p += kMaxThreads / kFoldCols) v += __ldcg(a.partials + (size_t)p * 2 * a.d + c);
     }
     sh[slice][lane] = v;
