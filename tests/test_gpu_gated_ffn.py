@@ -247,6 +247,44 @@ def test_same_bits_every_time_and_on_another_stream():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("t", [12, 40, 300])
+def test_less_workspace_means_no_splitting(t):
+    """Aligned matrices need no workspace forward, and only da and db backward; what is then not split is as right."""
+    p = Block(t, 1600, 2048, torch.bfloat16)
+    p.y, p.h, p.a, p.b = p.out("y", t, 1600), p.out("h", t, 2048), p.out("a", t, 2048), p.out("b", t, 2048)
+    B.a2sgd_gated_ffn_forward(p.x, p.wg, p.wu, p.wd, p.y, p.h, p.a, p.b)
+    _check_forward(p, "silu")
+    got = {"dx": p.out("dx", t, 1600), "dwg": p.out("dwg", 2048, 1600), "dwu": p.out("dwu", 2048, 1600), "dwd": p.out("dwd", 1600, 2048)}
+    room = -(-t * 2048 * 2 // 256) * 256
+    work = torch.empty(2 * room, dtype=torch.uint8, device="cuda")
+    B.a2sgd_gated_ffn_backward(p.dy, p.x, p.wg, p.wu, p.wd, p.h, p.a, p.b, *got.values(), workspace=work)
+    assert B.a2sgd_gated_ffn_status() == B.OK
+    _check_backward(p, "silu", got)
+
+
+def test_calls_can_be_captured_in_a_graph():
+    """A captured forward and backward pass replays to the same bits."""
+    p = Block(200, 264, 520, torch.bfloat16)
+    p.forward("silu")
+    got = p.backward("silu")
+    want = [t.clone() for t in (p.y, p.h, *got.values())]
+    y, h, a, b = p.out("y", 200, 264), p.out("h", 200, 520), p.out("a", 200, 520), p.out("b", 200, 520)
+    grads = [torch.zeros_like(g) for g in got.values()]
+    work = torch.empty(B.a2sgd_gated_ffn_workspace(200, 264, 520, backward=True), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.a2sgd_gated_ffn_forward(p.x, p.wg, p.wu, p.wd, y, h, a, b, workspace=work)
+        B.a2sgd_gated_ffn_backward(p.dy, p.x, p.wg, p.wu, p.wd, h, a, b, *grads, workspace=work)
+    for _ in range(2):
+        for t in (y, h, a, b, *grads):
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, ref in zip((y, h, *grads), want):
+            assert torch.equal(x, ref)
+
+
 def test_no_tokens_and_refusals():
     p = Block(0, 64, 128, torch.bfloat16)
     p.forward("silu")
