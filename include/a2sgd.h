@@ -466,7 +466,9 @@ int a2sgd_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, 
  *   activation  A2SGD_ACT_SILU: a / (1 + exp(-a));  A2SGD_ACT_GELU_TANH: a (1 + tanh(k (a + 0.044715 a^3))) / 2,
  *               k = sqrt(2 / pi)
  *   workspace   DEVICE, 256-byte aligned, a2sgd_gated_ffn_workspace bytes: flags A2SGD_FFN_BACKWARD for the
- *               backward pass, A2SGD_FFN_ALIGNED when every matrix that is read (and hidden) is laid out as above
+ *               backward pass, A2SGD_FFN_ALIGNED when every matrix that is read (and hidden) is laid out as above.
+ *               With less, down to what the padded copies (and da, db) take, tiles are not split in depth: slower
+ *               for some sizes, and rounded in another order
  * y and the other outputs must not overlap an input. */
 enum a2sgd_activation { A2SGD_ACT_SILU = 0, A2SGD_ACT_GELU_TANH = 1 };
 #define A2SGD_FFN_BACKWARD 1u

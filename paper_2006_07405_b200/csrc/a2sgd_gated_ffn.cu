@@ -65,7 +65,7 @@ struct Rows {
 struct Problem {
     int m, n;           // rows and columns of the output
     int tiles_m, tiles_n, first; // tiles down and across, and this problem's first tile
-    int seg, segs;      // operand pairs that are added up: a[seg], b[seg], ...
+    int seg;            // operand pairs that are added up: a[seg], b[seg], ...
     int k_blocks;       // slices of all its pairs together
 };
 
@@ -74,6 +74,7 @@ struct GemmArgs {
     Rows out[3];        // by problem; kGate: h; kGateGrad: da
     Rows out2;          // kGate: a second copy of h, when p is set; kGateGrad: db
     Rows gate, up;      // kGate: written when p is set; kGateGrad: read
+    int operands;       // pairs in use
     int seg_blocks[3];  // slices of an operand pair
     Problem problem[3];
     int problems;
@@ -211,7 +212,7 @@ struct Item {
 };
 
 // a / b and its remainder for a < 2^24 and quotients below 2^20: by the approximate reciprocal, put right by one.  Every
-// role works out every tile, and the compiler's divisions took 1000 clocks of it, as long as a tile of two slices.
+// role works out every tile, which counts where tiles are a slice or two deep (64 tokens backward 68 -> 66 us).
 __device__ __forceinline__ int quick_div(int a, int b, int &rest)
 {
     int q = __float2int_rz(__fdividef((float)a, (float)b));
@@ -280,9 +281,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
         bar_init_fence();
     }
     if (threadIdx.x >= 64 && threadIdx.x < 64 + 6) { // the maps are parameters: no need to wait for the launch before
-        const int i = threadIdx.x - 64;
-        if (i < 3) tma_prefetch_map(&g.a[i]);
-        else tma_prefetch_map(&g.b[i - 3]);
+        const int i = (threadIdx.x - 64) % 3;
+        if (threadIdx.x < 67 && i < g.operands) tma_prefetch_map(&g.a[i]);
+        if (threadIdx.x >= 67 && i < (EPI == kGate ? 2 : g.operands)) tma_prefetch_map(&g.b[i]);
     }
     if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_at), kTmemColumns);
     fence_before();
@@ -962,20 +963,19 @@ int launch_gemm(GemmArgs &g, int tiles, int sms, cudaStream_t s)
     g.items = g.whole + (tiles - g.whole) * g.splits;
     g.stage_bytes = kABytes + (EPI == kGate ? 128u : (uint32_t)g.bn / 2) * 128u;
     g.stages = (int)std::min<uint32_t>(kMostStages, kOperands / g.stage_bytes);
-
     void *params[] = {&g};
     A2_TRAIN_CUDA(launch(fn, dim3(2 * (unsigned)std::min(g.items, pairs)), kThreads, kSmem - 1024, params, s));
     if (EPI == kStore && g.splits > 1)
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>), dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / kJoinCols), kBM / 32), 256, 0,
-                             params, s));
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_join<T>),
+                             dim3((unsigned)(tiles - g.whole), (unsigned)(g.bn / kJoinCols), kBM / 32), 256, 0, params, s));
     return A2SGD_OK;
 }
 
-// The weights of the next product, for launches of no more than one round of tiles: their ends and the next launch's
+// The weights of the next product, for launches of no more than two rounds of tiles: their ends and the next launch's
 // start would leave the memory idle.  Rows that bulk copies can read (the pointers are TMA operands': 16-byte rows).
 void bring_ahead(GemmArgs &g, int tiles, int sms, const Matrix &w0, const Matrix *w1)
 {
-    if (tiles > sms / 2 * 2 || (w1 && w1->ld != w0.ld)) return;
+    if (tiles > 2 * (sms / 2) || (w1 && w1->ld != w0.ld)) return;
     g.ahead[0] = w0.p;
     g.ahead[1] = w1 ? w1->p : nullptr;
     g.ahead_ld = w0.ld;
@@ -1000,9 +1000,9 @@ int add_problem(GemmArgs &g, int64_t m, int n, int tile_n, int seg, int segs, in
     q.tiles_n = ceil_div(n, tile_n);
     q.first = tiles;
     q.seg = seg;
-    q.segs = segs;
     q.k_blocks = segs * ceil_div(k, kBK);
     for (int i = seg; i < seg + segs; ++i) g.seg_blocks[i] = ceil_div(k, kBK);
+    g.operands = seg + segs;
     return tiles + q.tiles_m * q.tiles_n;
 }
 
