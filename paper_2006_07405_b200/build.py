@@ -16,7 +16,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("a2sgd.cu", "a2sgd_checked.cu", "a2sg
                                                "a2sgd_adamw.cu", "a2sgd_layer_norm.cu", "a2sgd_gated_ffn.cu")]
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("a2sgd_kernels.cuh", "a2sgd_segments.cuh", "a2sgd_select.cuh",
                                                      "a2sgd_kernel_table.h", "a2sgd_debug_check.h",
-                                                     "a2sgd_train.cuh", "a2sgd_tcgen05.cuh")] \
+                                                     "a2sgd_train.cuh", "a2sgd_tcgen05.cuh", "a2sgd_adamw_arith.cuh")] \
     + [os.path.join(ROOT, "include", "a2sgd.h")]
 
 COMPILE_FLAGS = [

@@ -9,7 +9,7 @@
 //
 // Every operation is a single IEEE rounding in the order the header gives (no contraction to a
 // fused multiply-add), so that a step is defined to the bit, and with it the 8-bit codes.
-#include "a2sgd_train.cuh"
+#include "a2sgd_adamw_arith.cuh"
 
 #include <algorithm>
 #include <cmath>
@@ -66,34 +66,6 @@ __device__ __forceinline__ uint32_t dither_bits(uint32_t place, uint32_t step_ke
 // Bytes become floats and floats bytes without the conversion unit, which issues a quarter as often as the adder:
 // a byte is the low mantissa of 2^23.
 
-// The codes q of two s = (value / scale) * top^2, q in [0, top], rounded so that the expectation of q^2 over
-// the dither u in [0, 1) is s: q = floor(sqrt(s)), plus one when s - q^2 > u (2q + 1).  The approximate
-// root may be off by an ulp and so pick the neighbour of an exact floor only where s is within 2^-16
-// of a square's distance from it, where the second test gives the same sum: u ends at 4095/4096.  q^2,
-// 2q + 1 and its product with u are exact.  u comes as 1 + u, 12 bits on top of a mantissa.
-__device__ __forceinline__ void encode2(f32x2 s, uint32_t one_plus_u0, uint32_t one_plus_u1, float top, float least, float &q0, float &q1)
-{
-    float s0, s1, r0, r1;
-    unpair(s, s0, s1);
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(s0));
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(s1));
-    const f32x2 q = add2(add2_down(pair(r0, r1), pair(8388608.0f)), pair(-8388608.0f));
-    const f32x2 over = fma2(mul2(q, pair(-1.0f)), q, s); // s - q^2
-    const f32x2 u = add2(pair(__uint_as_float(one_plus_u0), __uint_as_float(one_plus_u1)), pair(-1.0f));
-    const f32x2 limit = mul2(u, fma2(pair(2.0f), q, pair(1.0f)));
-    float o0, o1, l0, l1;
-    unpair(over, o0, o1);
-    unpair(limit, l0, l1);
-    unpair(q, q0, q1);
-    if (o0 > l0) q0 += 1.0f;
-    if (o1 > l1) q1 += 1.0f;
-    q0 = fminf(q0, top);
-    q1 = fminf(q1, top);
-    if (least > 0.0f) {
-        q0 = fmaxf(q0, least);
-        q1 = fmaxf(q1, least);
-    }
-}
 // 12 bits of the dither as 1 + u: bits 31..20 for m's code, bits 19..8 for v's.
 __device__ __forceinline__ uint32_t dither_m(uint32_t h) { return 0x3F800000u | (h >> 9 & 0x007FF800u); }
 __device__ __forceinline__ uint32_t dither_v(uint32_t h) { return 0x3F800000u | (h << 3 & 0x007FF800u); }
@@ -135,38 +107,6 @@ __device__ __forceinline__ Gain gain_of(uint32_t largest_bits, float top_squared
     if (r.scale < kSmallestScale) r.scale = 0.0f; // false for NaN, which stays and shows
     r.gain = r.scale == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(r.scale), top_squared);
     return r;
-}
-
-// sqrt(v) and m / d for two elements each, correctly rounded.  Within the range that `plain_range` tests this is
-// Markstein's method (IBM J. Res. Dev. 34, 1990): an approximate root or reciprocal, and the exact residual by a fused
-// multiply-add.  It has no special cases and runs on pairs; outside of the range the library functions are called.
-__device__ __forceinline__ f32x2 root2(f32x2 v)
-{
-    float a, b, x, y;
-    unpair(v, a, b);
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(a));
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
-    const f32x2 y2 = pair(x, y), g = mul2(v, y2), h = mul2(y2, pair(0.5f));
-    const f32x2 left = fma2(mul2(g, pair(-1.0f)), g, v); // v - g^2
-    return fma2(left, h, g);
-}
-__device__ __forceinline__ f32x2 quotient2(f32x2 m, f32x2 d)
-{
-    float a, b, x, y;
-    unpair(d, a, b);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(a));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
-    const f32x2 minus = mul2(d, pair(-1.0f));
-    f32x2 y2 = pair(x, y);
-    y2 = fma2(y2, fma2(minus, y2, pair(1.0f)), y2);
-    const f32x2 q = mul2(m, y2);
-    return fma2(fma2(minus, q, m), y2, q);
-}
-// v of a lane within 2^-80..2^80 and |m| up to 2^80: d = sqrt(v) root + eps lies between 2^-40 and 2^100 and no residual
-// leaves the normal range, but that of an m below 2^-100, whose quotient may be an ulp off.
-__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, uint32_t largest_m)
-{
-    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x67800000u;
 }
 
 // GT: gradient type.  CT: type of the 16-bit copy of the weights, float when there is none.
