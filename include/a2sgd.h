@@ -383,9 +383,9 @@ enum a2sgd_dtype { A2SGD_F32 = 0, A2SGD_BF16 = 1, A2SGD_F16 = 2 };
  *     g = c * grad
  *     m <- beta1 m + (1 - beta1) g          v <- beta2 v + (1 - beta2) g^2
  *     w <- w (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, each product, sum, quotient and root rounded once, in that order (a quotient of an |m| below 2^-100
- * to within one unit in the last place); the coefficients are formed in fp64 and rounded once.  Weights are fp32; a 16-bit copy of them is written by the same pass when w16
- * is given.
+ * in fp32, each product, sum, quotient and root rounded once, in that order (a quotient below 2^-125, or of
+ * an |m| below 2^-100, to within one unit in the last place); the coefficients are formed in fp64 and rounded once.  Weights are
+ * fp32; a 16-bit copy of them is written by the same pass when w16 is given.
  *
  * State.  One buffer each for m and v, holding the tensors one after another, every tensor starting at a
  * multiple of A2SGD_ADAMW_BLOCK elements; a2sgd_adamw_state_elements gives the length.  Zero it
@@ -419,7 +419,8 @@ int a2sgd_adamw_create(a2sgd_adamw **out, uint32_t S, const uint64_t *numel, flo
 int a2sgd_adamw_destroy(a2sgd_adamw *plan);
 
 /* The step above.  lr, weight_decay >= 0, 0 <= beta1, beta2 < 1, eps > 0 (as fp32), step >= 1, counted by
- * the caller.  grad_scale: DEVICE, one float, or NULL; a value that is not finite makes the whole step
+ * the caller; eps and the coefficients 1 - lr wd and lr / (1 - beta1^t) have to be finite as fp32.  grad_scale:
+ * DEVICE, one float, or NULL; a value that is not finite makes the whole step
  * change nothing, so that a norm that overflowed needs no read-back. */
 int a2sgd_adamw_step(a2sgd_adamw *plan, double lr, double beta1, double beta2, double eps, double weight_decay,
                      uint64_t step, const float *grad_scale, void *stream);

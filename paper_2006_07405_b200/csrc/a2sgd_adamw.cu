@@ -12,6 +12,7 @@
 #include "a2sgd_adamw_arith.cuh"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -48,6 +49,7 @@ struct StepArgs {
     const float *grad_scale;           // nullptr: 1
     float beta1, one_minus_beta1, beta2, one_minus_beta2, decay, rate, root, eps;
     uint32_t dither;
+    uint32_t least_plain; // of v, for plain_range
 };
 
 // Two 12-bit numbers from the element's place in the state and the step: a counter (Weyl sequence,
@@ -212,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ S
             least_v = min(least_v, __float_as_uint(v[k]));
         }
     }
-    if (plain_range(least_v, big_v, big_m)) {
+    if (plain_range(least_v, a.least_plain, big_v, big_m)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             r2[i] = root2(v2[i]);
@@ -551,8 +553,10 @@ extern "C" int a2sgd_adamw_step(a2sgd_adamw *p, double lr, double beta1, double 
 {
     if (!p || step == 0) return A2SGD_ERR_ARG;
     if (!std::isfinite(lr) || !(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
-        !std::isfinite(eps) || !((float)eps > 0.0f) || !std::isfinite(weight_decay) || !(weight_decay >= 0.0))
+        !(eps <= FLT_MAX) || !((float)eps > 0.0f) || !std::isfinite(weight_decay) || !(weight_decay >= 0.0))
         return A2SGD_ERR_ARG;
+    const double decay = 1.0 - lr * weight_decay, rate = lr / (1.0 - std::pow(beta1, (double)step));
+    if (!(std::fabs(decay) <= FLT_MAX) || !(rate <= FLT_MAX)) return A2SGD_ERR_ARG; // not finite as fp32
     if (!aligned(grad_scale, 4)) return A2SGD_ERR_ALIGN;
     DeviceGuard guard(p->device);
     if (!guard.ok) return A2SGD_ERR_CUDA;
@@ -572,11 +576,12 @@ extern "C" int a2sgd_adamw_step(a2sgd_adamw *p, double lr, double beta1, double 
     a.one_minus_beta1 = (float)(1.0 - beta1);
     a.beta2 = (float)beta2;
     a.one_minus_beta2 = (float)(1.0 - beta2);
-    a.decay = (float)(1.0 - lr * weight_decay);
-    a.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    a.decay = (float)decay;
+    a.rate = (float)rate;
     a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
     a.eps = (float)eps;
     a.dither = (uint32_t)step * 0x85A308D3u + 0x243F6A89u;
+    a.least_plain = eps <= kMostPlainEps ? kLeastPlain : 0xffffffffu; // no v passes: the library path
     const void *fn = p->eight ? pick_step<true>(p->grad_dtype, p->w16_dtype) : pick_step<false>(p->grad_dtype, p->w16_dtype);
     void *params[] = {&a};
     A2_TRAIN_CUDA(launch(fn, dim3((unsigned)p->n_tiles), kThreads, 0, params, static_cast<cudaStream_t>(stream)));

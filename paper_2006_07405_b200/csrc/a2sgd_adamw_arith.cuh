@@ -62,11 +62,14 @@ __device__ __forceinline__ f32x2 quotient2(f32x2 m, f32x2 d)
     const f32x2 q = mul2(m, y2);
     return fma2(fma2(minus, q, m), y2, q);
 }
-// v of a lane within 2^-80..2^80 and |m| up to 2^80: d = sqrt(v) root + eps lies between 2^-40 and 2^100 and no residual
-// leaves the normal range, but that of an m below 2^-100, whose quotient may be an ulp off.
-__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t largest_v, uint32_t largest_m)
+// v of a lane within least..2^80 and |m| up to 2^80; least is 2^-80 for eps up to 2^60 and lets nothing through beyond.  With a
+// root's factor below 2^27, d = sqrt(v) root + eps lies between 2^-40 and 2^68, its reciprocal is a normal number, and no
+// residual leaves the normal range but that of an m below 2^-100 or of a quotient below 2^-125, which may be an ulp off.
+constexpr uint32_t kLeastPlain = 0x17800000u;           // 2^-80
+constexpr double kMostPlainEps = 1152921504606846976.0; // 2^60
+__device__ __forceinline__ bool plain_range(uint32_t least_v, uint32_t least, uint32_t largest_v, uint32_t largest_m)
 {
-    return least_v >= 0x17800000u && largest_v <= 0x67800000u && largest_m <= 0x67800000u;
+    return least_v >= least && largest_v <= 0x67800000u && largest_m <= 0x67800000u;
 }
 
 } // namespace a2sgd_train
