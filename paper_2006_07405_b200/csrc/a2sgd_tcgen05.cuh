@@ -69,15 +69,18 @@ __device__ __forceinline__ uint64_t now_ns()
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-// Every wait ends: after kWaitLimitNs, or once another thread of the CTA has given up, it returns false.
+// Every wait ends: after kWaitLimitNs, or once another warp of the CTA has given up, it returns false.  The whole warp waits, and
+// its lanes go on together with one answer: if one lane gave up while another saw the barrier complete, the two would
+// meet at different barriers from there on, and for good.  No barrier here moves on by a second phase before each of
+// its waiting warps has been let through, so that lanes may ask again until all have seen it.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
-    if (bar_try(bar, parity)) return true;
+    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
     const uint64_t begin = now_ns();
     for (uint32_t polls = 1;; ++polls) {
-        if (bar_try(bar, parity)) return true;
-        if ((polls & 255u) == 0u && (*gave_up || now_ns() - begin > kWaitLimitNs)) {
+        if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+        if ((polls & 255u) == 0u && __any_sync(0xffffffffu, *gave_up || now_ns() - begin > kWaitLimitNs)) {
             *gave_up = 1;
             return false;
         }
