@@ -825,6 +825,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
             static_cast<T *>(g.out)[(int64_t)n * g.ldo + col] = from_f32<T>(v[0]);
         }
     }
+    __syncwarp(); // lanes past the last token have left the loop's body early, and the barrier wants whole warps
     if (g.parts > 1) cluster_sync(); // no CTA leaves while another reads its sums
 }
 
