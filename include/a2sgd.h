@@ -496,9 +496,10 @@ int a2sgd_gated_ffn_backward(const void *dy, int64_t dy_stride, const void *x, i
                              uint32_t d, uint32_t f, void *workspace, uint64_t workspace_bytes, int device,
                              void *stream);
 
-/* Synchronises `stream` and returns the status that the block's kernels latched on the device
- * (A2SGD_OK, or A2SGD_ERR_TIMEOUT: a bounded wait inside a kernel ran out and that call's outputs are undefined),
- * clearing it. */
+/* Synchronises `stream` and says whether a bounded wait inside one of the block's kernels has run out on the device since this
+ * was last asked with the same stream (before the first time: since the library was loaded): A2SGD_OK, or A2SGD_ERR_TIMEOUT, and
+ * the outputs of the calls since then are undefined.  The kernels count such waits for the device as a whole; asking takes
+ * nothing away from other streams, each of which is told once, whichever stream the call ran on. */
 int a2sgd_gated_ffn_status(int device, int *device_status, void *stream);
 
 /* Static, never NULL. */

@@ -774,7 +774,8 @@ def a2sgd_gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Te
 
 
 def a2sgd_gated_ffn_status(device: Optional[int] = None, stream=None) -> int:
-    """Synchronises the stream; the status that the block's kernels latched on the device (OK or ERR_TIMEOUT), cleared."""
+    """Synchronises the stream; ERR_TIMEOUT if a wait inside one of the block's kernels has run out on the device since this
+    was last asked with the same stream, else OK."""
     device = torch.cuda.current_device() if device is None else int(device)
     st = ctypes.c_int(0)
     _check(lib().a2sgd_gated_ffn_status(device, ctypes.byref(st), _stream_on(device, stream)),

@@ -51,8 +51,9 @@ constexpr uint32_t kOperands = (kSmem - 1024 - 512 - kEpilogueWarps * 2 * kStagi
 
 enum Epilogue { kStore = 0, kGate = 1, kGateGrad = 2 };
 
-// Latched when a kernel's bounded wait ran out; read and cleared by a2sgd_gated_ffn_status.
-__device__ int g_status = 0;
+// CTAs whose bounded wait ran out, since the library was loaded: only ever counted up, so that no reader takes the news
+// from another.  a2sgd_gated_ffn_status compares it with what was last seen from a stream.
+__device__ unsigned int g_waits_run_out = 0;
 
 // 16-bit rows that the epilogue writes, by TMA where `map` could be made, else element by element; or reads.
 struct Rows {
@@ -569,7 +570,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_gemm(
     __syncthreads();
     if (gave_up) {
         // leave the copies and products in flight a bounded time to end, and say so
-        if (threadIdx.x == 0) atomicExch(&g_status, A2SGD_ERR_TIMEOUT);
+        if (threadIdx.x == 0) atomicAdd(&g_waits_run_out, 1u);
         const uint64_t begin = now_ns();
         while (now_ns() - begin < 5000000ull) __nanosleep(1000);
     }
@@ -1344,9 +1345,9 @@ extern "C" int a2sgd_gated_ffn_status(int device, int *device_status, void *stre
     DeviceGuard guard(device);
     if (!guard.ok) return A2SGD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int zero = 0;
+    unsigned int count = 0;
+    A2_TRAIN_CUDA(cudaMemcpyFromSymbolAsync(&count, g_waits_run_out, sizeof count, 0, cudaMemcpyDeviceToHost, s));
     A2_TRAIN_CUDA(cudaStreamSynchronize(s));
-    A2_TRAIN_CUDA(cudaMemcpyFromSymbol(device_status, g_status, sizeof(int)));
-    A2_TRAIN_CUDA(cudaMemcpyToSymbol(g_status, &zero, sizeof(int)));
+    *device_status = count_moved(device, s, count) ? A2SGD_ERR_TIMEOUT : A2SGD_OK;
     return A2SGD_OK;
 }

@@ -3,6 +3,7 @@
 
 #include <map>
 #include <mutex>
+#include <thread>
 #include <tuple>
 #include <utility>
 
@@ -66,6 +67,23 @@ cudaError_t allow_smem(const void *fn, size_t bytes)
     } catch (...) { // no memory for the note: set again next time
     }
     return cudaSuccess;
+}
+
+bool count_moved(int device, cudaStream_t stream, unsigned int count)
+{
+    static std::mutex lock;
+    static std::map<std::tuple<int, cudaStream_t, std::thread::id>, unsigned int> seen;
+    if (count == 0) return false;
+    const std::thread::id thread = stream == cudaStreamPerThread ? std::this_thread::get_id() : std::thread::id();
+    std::lock_guard<std::mutex> hold(lock);
+    const auto key = std::make_tuple(device, stream, thread);
+    const auto it = seen.find(key);
+    if (it != seen.end() && it->second == count) return false;
+    try {
+        seen[key] = count;
+    } catch (...) { // no memory for the note: told again next time
+    }
+    return true;
 }
 
 } // namespace a2sgd_train

@@ -233,6 +233,10 @@ int resident_ctas(const void *fn, unsigned threads, size_t smem);
 // Lets a kernel use that much dynamic shared memory on the current device; once a kernel, device and amount.
 cudaError_t allow_smem(const void *fn, size_t bytes);
 
+// Whether a device's count has moved since this was last asked with the same stream (before the first time: since 0).
+// Each stream is told for itself, and each thread for its own per-thread default stream.
+bool count_moved(int device, cudaStream_t stream, unsigned int count);
+
 } // namespace a2sgd_train
 
 #define A2_TRAIN_CUDA(call)              \
