@@ -27,3 +27,7 @@ def _run(program, part):
 def test_every_stream_is_told_of_a_wait_that_ran_out(program):
     """One that another stream's caller asks about, or that runs out between two questions, is lost to nobody."""
     _run(program, "count")
+
+
+def test_what_fits_on_an_sm_is_noted_for_each_device(program):
+    _run(program, "occupancy")
