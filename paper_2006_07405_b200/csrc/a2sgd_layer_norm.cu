@@ -11,7 +11,8 @@
 // are in flight together: their loads are issued before any is used, and the threads of a group meet
 // at one barrier for the R rows' sums.  The squared deviations are summed in a second reduction over
 // the registers, not from a sum of squares, which cancels when the mean is large against the spread.
-// All sums are fp32 within a thread's few values and trees above; every order is fixed.
+// All sums are fp32, in runs of at most kRun terms a thread (the columns of a long row, the rows of a column), the runs one after
+// another, and trees or short chains over the threads, groups and CTAs; every order is fixed.
 //
 // B200, 65536 x 1600 bfloat16: forward 76 us (5.5 TB/s), a warp a row; backward 133 us (4.7 TB/s), two rows in flight, bound by
 // instruction issue and the barrier of a row's sums (with one row 277 us; four do not fit the registers).
@@ -31,6 +32,9 @@ constexpr int kMaxThreads = 1024;                       // of the long forms and
 constexpr int kRowThreads = 512;                        // of the register forms: 128 registers each
 constexpr uint32_t kMostCols = kRowThreads * 16;        // 8192: at most 16 columns a thread
 constexpr uint32_t kFoldCols = 32;                   // columns of one CTA of the fold
+// Terms of a running sum.  7812 equal terms in one chain were off by 1.2e-4 of their sum, in runs of 512 by 7e-7; a chain
+// of n fp32 additions may be off by n 2^-24.
+constexpr uint32_t kRun = 512;
 
 struct LnArgs {
     const void *x, *dy, *w, *b;
@@ -45,7 +49,10 @@ struct LnArgs {
     float *partials; // backward: [grid][2][d]
     void *dw, *db;
     uint32_t parts;
+    bool add; // to the partial sums of the rows before
 };
+
+__device__ __forceinline__ void keep_partial(const LnArgs &a, float *at, float v) { *at = a.add ? __ldcg(at) + v : v; }
 
 // N sums (a power of two) over the threads of a group, the same in each of them.  A group of up to 32 threads
 // (a power of two) is part of a warp; a larger one is a whole number of warps and takes one barrier of the CTA.
@@ -372,17 +379,30 @@ __global__ void __launch_bounds__(kRowThreads) k_ln_backward(const __grid_consta
         for (uint32_t c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
             float v = 0.0f;
             for (uint32_t g = 0; g < a.groups; ++g) v += sh[(size_t)g * 2 * a.d + c];
-            a.partials[(size_t)blockIdx.x * 2 * a.d + c] = v;
+            keep_partial(a, a.partials + (size_t)blockIdx.x * 2 * a.d + c, v);
         }
         return;
     }
     float *out = a.partials + (size_t)blockIdx.x * 2 * a.d;
+    if (VEC && a.add) { // beforehand, all reads side by side (element forms have no registers left for it)
+#pragma unroll
+        for (int i = 0; i < NC; i += 2) {
+            const uint32_t c = column<NC, VEC>(i, t, a.tpr), e = column<NC, VEC>(i + 1, t, a.tpr);
+            dw[i / 2] = add2(dw[i / 2], pair(c < a.d ? __ldcg(out + c) : 0.0f, e < a.d ? __ldcg(out + e) : 0.0f));
+            db[i / 2] = add2(db[i / 2], pair(c < a.d ? __ldcg(out + a.d + c) : 0.0f, e < a.d ? __ldcg(out + a.d + e) : 0.0f));
+        }
+    }
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         const uint32_t c = column<NC, VEC>(i, t, a.tpr);
         if (c < a.d) {
-            out[c] = half_of(dw[i / 2], i & 1);
-            out[a.d + c] = half_of(db[i / 2], i & 1);
+            if (VEC) {
+                out[c] = half_of(dw[i / 2], i & 1);
+                out[a.d + c] = half_of(db[i / 2], i & 1);
+            } else {
+                keep_partial(a, out + c, half_of(dw[i / 2], i & 1));
+                keep_partial(a, out + a.d + c, half_of(db[i / 2], i & 1));
+            }
         }
     }
 }
@@ -532,6 +552,24 @@ __device__ __forceinline__ float block_sum(float v, float *sh)
     return v;
 }
 
+// N sums over a thread's columns of a row, in runs of kRun terms: term(c, run) adds a column's.  Unrolled as measured: at
+// 4096 x 12288 bf16 forward 152 and 175 us by four and by two, backward 361 and 295 (registers: 44 and 32 a thread).
+template <int N, typename F>
+__device__ __forceinline__ void strided_sums(uint32_t d, float (&total)[N], F term)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) total[i] = 0.0f;
+    uint32_t c = threadIdx.x;
+    do {
+        const uint32_t end = min(d, c + kRun * kMaxThreads);
+        float run[N] = {};
+#pragma unroll (N == 1 ? 4 : 2)
+        for (; c < end; c += kMaxThreads) term(c, run);
+#pragma unroll
+        for (int i = 0; i < N; ++i) total[i] += run[i];
+    } while (c < d);
+}
+
 template <typename T, typename W>
 __global__ void __launch_bounds__(kMaxThreads) k_ln_forward_long(const __grid_constant__ LnArgs a)
 {
@@ -541,15 +579,14 @@ __global__ void __launch_bounds__(kMaxThreads) k_ln_forward_long(const __grid_co
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.x_stride;
         T *y = static_cast<T *>(a.y) + (int64_t)row * a.y_stride;
-        float v = 0.0f;
-        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) v += to_f32(x[c]);
-        const float mean = block_sum(v, sh) * a.inv_d;
-        v = 0.0f;
-        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+        float sum[1];
+        strided_sums(a.d, sum, [&](uint32_t c, float (&v)[1]) { v[0] += to_f32(x[c]); });
+        const float mean = block_sum(sum[0], sh) * a.inv_d;
+        strided_sums(a.d, sum, [&](uint32_t c, float (&v)[1]) {
             const float e = to_f32(x[c]) - mean;
-            v = fmaf(e, e, v);
-        }
-        const float rstd = 1.0f / sqrtf(fmaf(block_sum(v, sh), a.inv_d, a.eps));
+            v[0] = fmaf(e, e, v[0]);
+        });
+        const float rstd = 1.0f / sqrtf(fmaf(block_sum(sum[0], sh), a.inv_d, a.eps));
         for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
             const float w = a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
             const float b = a.b ? to_f32(static_cast<const W *>(a.b)[c]) : 0.0f;
@@ -577,8 +614,8 @@ __global__ void __launch_bounds__(256) k_ln_columns_long(const __grid_constant__
         db += g;
         dw = fmaf(g, (x - a.mean[row]) * a.rstd[row], dw);
     }
-    a.partials[(size_t)blockIdx.y * 2 * a.d + c] = dw;
-    a.partials[(size_t)blockIdx.y * 2 * a.d + a.d + c] = db;
+    keep_partial(a, a.partials + (size_t)blockIdx.y * 2 * a.d + c, dw);
+    keep_partial(a, a.partials + (size_t)blockIdx.y * 2 * a.d + a.d + c, db);
 }
 
 template <typename T, typename W>
@@ -592,13 +629,13 @@ __global__ void __launch_bounds__(kMaxThreads) k_ln_backward_long(const __grid_c
         const T *dy = static_cast<const T *>(a.dy) + (int64_t)row * a.dy_stride;
         T *dx = static_cast<T *>(a.y) + (int64_t)row * a.y_stride;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float s1 = 0.0f, s2 = 0.0f;
-        for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+        float s[2];
+        strided_sums(a.d, s, [&](uint32_t c, float (&v)[2]) {
             const float u = to_f32(dy[c]) * (a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f);
-            s1 += u;
-            s2 = fmaf(u, (to_f32(x[c]) - mean) * rstd, s2);
-        }
-        const float c1 = block_sum(s1, sh) * a.inv_d, c2 = block_sum(s2, sh) * a.inv_d;
+            v[0] += u;
+            v[1] = fmaf(u, (to_f32(x[c]) - mean) * rstd, v[1]);
+        });
+        const float c1 = block_sum(s[0], sh) * a.inv_d, c2 = block_sum(s[1], sh) * a.inv_d;
         for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
             const float w = a.w ? to_f32(static_cast<const W *>(a.w)[c]) : 1.0f;
             const float xhat = (to_f32(x[c]) - mean) * rstd;
@@ -846,17 +883,39 @@ extern "C" int a2sgd_layer_norm_backward(const void *dy, int64_t dy_stride, cons
     a.parts = p.long_row ? long_parts(rows) : p.grid;
     a.partials = columns ? static_cast<float *>(workspace) : nullptr;
     if (columns && (!workspace || workspace_bytes < sizeof(float) * 2 * (uint64_t)d * a.parts)) return A2SGD_ERR_ARG;
+    // Rows whose column sums take more than kRun terms a thread are taken in as many launches as that makes runs.
+    const auto launch_runs = [&](uint64_t most, auto &&go) {
+        if (rows <= most) {
+            rc = go();
+            return;
+        }
+        const LnArgs whole = a;
+        for (uint64_t first = 0; rc == A2SGD_OK && first < rows; first += most) {
+            a.rows = std::min(most, rows - first);
+            a.x = static_cast<const char *>(x) + (int64_t)first * x_stride * (int64_t)size_of(dtype);
+            a.dy = static_cast<const char *>(dy) + (int64_t)first * dy_stride * (int64_t)size_of(dtype);
+            if (dx) a.y = static_cast<char *>(dx) + (int64_t)first * dx_stride * (int64_t)size_of(dtype);
+            a.mean = whole.mean + first;
+            a.rstd = whole.rstd + first;
+            a.add = first != 0;
+            rc = go();
+        }
+        a = whole;
+    };
     if (p.long_row) {
         if (columns) { // before dx, which may take the place of x or dy
             const void *fn = dtype == A2SGD_F32    ? reinterpret_cast<const void *>(&k_ln_columns_long<float>)
                              : dtype == A2SGD_BF16 ? reinterpret_cast<const void *>(&k_ln_columns_long<__nv_bfloat16>)
                                                    : reinterpret_cast<const void *>(&k_ln_columns_long<__half>);
-            void *params[] = {&a};
-            A2_TRAIN_CUDA(launch(fn, dim3((d + 255) / 256, a.parts), 256, 0, params, s));
+            launch_runs((uint64_t)kRun * a.parts, [&]() -> int {
+                void *params[] = {&a};
+                A2_TRAIN_CUDA(launch(fn, dim3((d + 255) / 256, a.parts), 256, 0, params, s));
+                return A2SGD_OK;
+            });
         }
-        if (dx) rc = run(p, a, s);
+        if (rc == A2SGD_OK && dx) rc = run(p, a, s);
     } else {
-        rc = run(p, a, s);
+        launch_runs(columns ? (uint64_t)kRun * p.grid * p.groups : rows, [&] { return run(p, a, s); });
     }
     if (rc != A2SGD_OK || !columns) return rc;
     const void *fold = param_dtype == A2SGD_F32    ? reinterpret_cast<const void *>(&k_ln_fold<float>)
