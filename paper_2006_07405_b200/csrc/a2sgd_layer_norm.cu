@@ -721,7 +721,7 @@ inline uint32_t long_parts(uint64_t rows) { return (uint32_t)std::min<uint64_t>(
 
 constexpr int kCtasPerSm = 4; // at most: the partial sums of the backward pass are sized by it
 
-Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int dtype, int param)
+Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int device, int dtype, int param)
 {
     Plan p;
     if (d > kMostCols) {
@@ -735,7 +735,7 @@ Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int 
         // A warp a row wins by its few instructions once a warp has rows enough to hide its start: at d = 1600,
         // bf16, 76 against 83 us for 65536 rows (37 a warp), 16.2 against 13.0 us for 8192 (5 a warp).
         const void *fn = pick_warp_types(dtype, param, (int)(d + 255) / 256);
-        const uint64_t resident = (uint64_t)sms * resident_ctas(fn, kWarpThreads, 0);
+        const uint64_t resident = (uint64_t)sms * resident_ctas(fn, kWarpThreads, 0, device);
         if (rows >= resident * (kWarpThreads / 32) * 10) {
             p.threads = kWarpThreads;
             p.fn = fn;
@@ -765,7 +765,7 @@ Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int 
     p.fn = backward ? pick_types<true>(dtype, param, p.nc, p.r, vec) : pick_types<false>(dtype, param, p.nc, p.r, vec);
     // every CTA resident at once: the rows are dealt out evenly
     const uint64_t trips = (rows + (uint64_t)p.groups * p.r - 1) / ((uint64_t)p.groups * p.r);
-    const uint64_t slots = (uint64_t)sms * std::min(kCtasPerSm, resident_ctas(p.fn, p.threads, p.smem));
+    const uint64_t slots = (uint64_t)sms * std::min(kCtasPerSm, resident_ctas(p.fn, p.threads, p.smem, device));
     p.grid = (unsigned)std::min<uint64_t>(trips, slots);
     return p;
 }
@@ -808,7 +808,7 @@ extern "C" int a2sgd_layer_norm_forward(const void *x, int64_t x_stride, int dty
     const int sms = guard.ok ? sm_count(device) : 0;
     if (sms == 0) return A2SGD_ERR_CUDA;
     const bool vec = d % 8 == 0 && rows_vector(x, x_stride, rows, dtype) && rows_vector(y, y_stride, rows, dtype);
-    const Plan p = make_plan(rows, d, vec, false, sms, dtype, param_dtype);
+    const Plan p = make_plan(rows, d, vec, false, sms, device, dtype, param_dtype);
     LnArgs a{};
     a.x = x;
     a.w = weight;
@@ -862,7 +862,7 @@ extern "C" int a2sgd_layer_norm_backward(const void *dy, int64_t dy_stride, cons
     if (!columns && !dx) return A2SGD_OK;
     const bool vec = d % 8 == 0 && rows_vector(x, x_stride, rows, dtype) && rows_vector(dy, dy_stride, rows, dtype) &&
                      (!dx || rows_vector(dx, dx_stride, rows, dtype));
-    const Plan p = make_plan(rows, d, vec, true, sms, dtype, param_dtype);
+    const Plan p = make_plan(rows, d, vec, true, sms, device, dtype, param_dtype);
     LnArgs a{};
     a.x = x;
     a.dy = dy;

@@ -28,15 +28,10 @@ int sm_count(int device)
     return n;
 }
 
-int resident_ctas(const void *fn, unsigned threads, size_t smem)
+int resident_ctas(const void *fn, unsigned threads, size_t smem, int device)
 {
     static std::mutex lock;
     static std::map<std::tuple<const void *, int, unsigned, size_t>, int> known_counts;
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return 1;
-    }
     std::lock_guard<std::mutex> hold(lock);
     const auto key = std::make_tuple(fn, device, threads, smem);
     auto it = known_counts.find(key);

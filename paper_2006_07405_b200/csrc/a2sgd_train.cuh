@@ -227,8 +227,8 @@ inline bool known(int dtype) { return dtype == A2SGD_F32 || dtype == A2SGD_BF16 
 
 // SMs of a device; asked once a device.
 int sm_count(int device);
-// CTAs of a kernel that an SM of the current device holds at once, at least 1; asked once a kernel, device and shape.
-int resident_ctas(const void *fn, unsigned threads, size_t smem);
+// CTAs of a kernel that an SM of `device`, the current one, holds at once, at least 1; asked once a kernel, device and shape.
+int resident_ctas(const void *fn, unsigned threads, size_t smem, int device);
 
 // Lets a kernel use that much dynamic shared memory on the current device; once a kernel, device and amount.
 cudaError_t allow_smem(const void *fn, size_t bytes);

@@ -35,12 +35,12 @@ int main(int argc, char **argv)
     } else { // occupancy
         EXPECT(sm_count(0) == 100 && sm_count(1) == 101);
         const void *fn = &failures;
-        EXPECT(resident_ctas(fn, 128, 0) == 2 && resident_ctas(fn, 128, 0) == 2 && occupancy_questions == 1);
+        EXPECT(resident_ctas(fn, 128, 0, 0) == 2 && resident_ctas(fn, 128, 0, 0) == 2 && occupancy_questions == 1);
         current_device = 1;
-        EXPECT(resident_ctas(fn, 128, 0) == 3 && resident_ctas(fn, 128, 0) == 3 && occupancy_questions == 2);
+        EXPECT(resident_ctas(fn, 128, 0, 1) == 3 && resident_ctas(fn, 128, 0, 1) == 3 && occupancy_questions == 2);
         current_device = 0;
-        EXPECT(resident_ctas(fn, 128, 0) == 2 && occupancy_questions == 2);
-        EXPECT(resident_ctas(fn, 128, 1024) == 2 && occupancy_questions == 3);
+        EXPECT(resident_ctas(fn, 128, 0, 0) == 2 && occupancy_questions == 2);
+        EXPECT(resident_ctas(fn, 128, 1024, 0) == 2 && occupancy_questions == 3);
     }
     std::printf("%s\n", failures ? "FAILED" : "ok");
     return failures ? 1 : 0;
