@@ -659,31 +659,32 @@ const void *pick_warp(int k)
 {
 #define A2_LNW(K) \
     if (k == K) return reinterpret_cast<const void *>(&k_ln_forward_warp<T, W, K>);
-    A2_LNW(1) A2_LNW(2) A2_LNW(3) A2_LNW(4) A2_LNW(5) A2_LNW(6) A2_LNW(7) A2_LNW(8)
+    A2_LNW(2) A2_LNW(3) A2_LNW(4) A2_LNW(5) A2_LNW(6) A2_LNW(7) A2_LNW(8)
 #undef A2_LNW
     return nullptr;
 }
 
 // Rows in flight of a group (and as many being worked on), where there are rows enough: the backward pass has twice
 // the registers of a row to hold, rows without vector accesses hold an element a register.
-template <bool BWD>
-constexpr int kRows = BWD ? 2 : 4;
+template <bool BWD, bool VEC>
+constexpr int kRows = VEC && !BWD ? 4 : 2;
 
+template <typename T, typename W, bool BWD, int NC, int R, bool VEC>
+const void *row_kernel()
+{
+    if constexpr (BWD) return reinterpret_cast<const void *>(&k_ln_backward<T, W, NC, R, VEC>);
+    else return reinterpret_cast<const void *>(&k_ln_forward<T, W, NC, R, VEC>);
+}
+template <typename T, typename W, bool BWD, bool VEC>
+const void *pick_rows(int nc, int r)
+{
+    if (nc == 16) return row_kernel<T, W, BWD, 16, 1, VEC>();
+    return r == 1 ? row_kernel<T, W, BWD, 8, 1, VEC>() : row_kernel<T, W, BWD, 8, kRows<BWD, VEC>, VEC>();
+}
 template <typename T, typename W, bool BWD>
 const void *pick(int nc, int r, bool vec)
 {
-#define A2_LN(NC, R, V)                                                                       \
-    if (nc == NC && r == R && vec == V)                                                       \
-        return BWD ? reinterpret_cast<const void *>(&k_ln_backward<T, W, NC, R, V>)           \
-                   : reinterpret_cast<const void *>(&k_ln_forward<T, W, NC, R, V>);
-    A2_LN(8, 1, true)
-    A2_LN(8, kRows<BWD>, true)
-    A2_LN(16, 1, true)
-    A2_LN(8, 1, false)
-    A2_LN(8, 2, false)
-    A2_LN(16, 1, false)
-#undef A2_LN
-    return nullptr;
+    return vec ? pick_rows<T, W, BWD, true>(nc, r) : pick_rows<T, W, BWD, false>(nc, r);
 }
 
 template <bool BWD>
@@ -759,7 +760,8 @@ Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int 
     while (p.tpr * p.groups % 32) ++p.groups;
     p.threads = p.tpr * p.groups;
     // several rows in flight where there are enough to keep every SM busy with them
-    p.r = p.nc == 8 && rows >= (uint64_t)sms * p.groups * 8 ? (vec && !backward ? 4 : 2) : 1;
+    const bool several = p.nc == 8 && rows >= (uint64_t)sms * p.groups * 8;
+    p.r = !several ? 1 : backward ? (vec ? kRows<true, true> : kRows<true, false>) : vec ? kRows<false, true> : kRows<false, false>;
     const size_t sums = sizeof(float) * 2 * (kRowThreads / 32) * (backward ? 2 : 1) * p.r;
     p.smem = std::max(sums, backward && p.groups > 1 ? sizeof(float) * 2 * d * p.groups : (size_t)0);
     p.fn = backward ? pick_types<true>(dtype, param, p.nc, p.r, vec) : pick_types<false>(dtype, param, p.nc, p.r, vec);
