@@ -651,9 +651,15 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
 // barrier); since the order of k within a product is free as long as both operands share it, those 8 are the lane's part
 // of two products, and the tokens' 8 k lie the same way.  Eight warps, and the CTAs of a cluster, share the depth; their
 // sums meet in shared memory, in order, where the gate, the activation and the product are applied.
-// One call with d = 1600, f = 6400, its weights from memory: 8 tokens 16.8 us, 16 tokens 19.0; 24 and 32 tokens, with four
-// blocks of 8, 30.9 and 31.9 against 28.8 and 29.0 of the tiles above.
+// One call, its weights from memory, this form against the tiles above: aligned matrices, 16 tokens, 512 x 1408 13.1 and 15.7 us, 1024 x 4096
+// 20.5 and 21.3, 1600 x 6400 18.5 and 30.9, 4096 x 11008 58.4 and 78.8; with four blocks of 8 tokens, at 17 to 32, 13.1 and 15.7, 26 and 21.4,
+// 27 and 28.8, 78 and 79.4 (another set of kernels for a tenth at most: left out).
 constexpr int kFewTokens = 16;
+// Rows that are not aligned come in element by element, here for every token block, in the tiles' way once into padded copies:
+// this form wins for small matrices.  8 tokens: 512 x 1408 12.3 and 19.3 us, 777 x 2051 23.2 and 23.9, 1024 x 4096 35.3 and 34.3, 1600 x 6400
+// 67.5 and 56.8, 4096 x 11008 337 and 201; 1 token: 777 x 2051 20.6 and 24.0, 1024 x 4096 30.9 and 35.6, 1600 x 6400 61.5 and 59.9; 16 tokens:
+// 512 x 1408 12.5 and 19.6, 777 x 2051 26.8 and 23.9.
+inline bool few_elements(int64_t tokens, int d, int f) { return (int64_t)d * f * (tokens + 7) <= 1 << 25; }
 constexpr int kFewWarps = 8;
 constexpr uint32_t kFewPiece = 32 * 16; // what a warp copies at once
 // Steps of 32 k on their way: as many as leave room for three CTAs an SM.  One token, 1600 x 6400, weights from memory, in a
@@ -941,7 +947,7 @@ Shape choose(const Extent *outs, int count, int k_blocks, bool b_mn, int pairs)
         for (int splits : {1, splits_of(tiles, pairs, k_blocks)}) {
             const double rounds = (double)(tiles / pairs) + (tiles % pairs ? 1.0 / splits : 0.0);
             // and the last tile's way out, and joining the parts: a launch, and their bytes through L2
-            const double join = splits > 1 ? 6000.0 + (double)(tiles % pairs) * splits * 2.0 * kBM * bn * 4 / (148 * 40.0) : 0.0;
+            const double join = splits > 1 ? 6000.0 + (double)(tiles % pairs) * splits * 2.0 * kBM * bn * 4 / (2 * pairs * 40.0) : 0.0;
             const double cost = rounds * k_blocks * slice_clocks(bn) + 12.0 * bn + join;
             if (cost < best.cost) {
                 best.bn = bn;
@@ -1144,7 +1150,8 @@ int forward(const Matrix &x, const Matrix &wg, const Matrix &wu, const Matrix &w
     const Extent out{t, d};
     const Shape shape = pack.fit(choose(&out, 1, ceil_div(f, kBK), false, sms / 2), workspace_bytes);
     if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG; // for few tokens too, so that what is refused does not go by their number
-    if (t <= kFewTokens) return forward_few<T>(x, wg, wu, wd, y, h, gate, up, act, sms, s);
+    const bool whole = tma_ok(x) && tma_ok(wg) && tma_ok(wu) && tma_ok(wd) && tma_ok(h);
+    if (t <= kFewTokens && (whole || few_elements(t, d, f))) return forward_few<T>(x, wg, wu, wd, y, h, gate, up, act, sms, s);
     int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
 

@@ -732,9 +732,13 @@ Plan make_plan(uint64_t rows, uint32_t d, bool vec, bool backward, int sms, int 
         p.fn = backward ? k_ln_backward_long_of(dtype, param) : k_ln_forward_long_of(dtype, param);
         return p;
     }
-    if (vec && !backward && d > 256 && d <= kWarpCols) {
-        // A warp a row wins by its few instructions once a warp has rows enough to hide its start: at d = 1600,
-        // bf16, 76 against 83 us for 65536 rows (37 a warp), 16.2 against 13.0 us for 8192 (5 a warp).
+    if (vec && !backward && d > 256 && d <= kWarpCols && (dtype == A2SGD_F32 || d % 256)) {
+        // A warp a row wins by its few instructions once a warp has rows enough to hide its start, ten or more here, and
+        // where a row's threads of 8 columns each would not be whole warps, or read fp32.  This form against the other, us: bf16, 1600
+        // columns, 65536 rows (37 a warp) 75 and 82, 32768 42 and 43, 16384 25.5 and 23.2, 8192 (5 a warp) 17.1 and 13.0; 264 columns, 65536
+        // and 32768 rows 20.0 and 23.5, 11.5 and 12.9; fp32, 65536 rows, 512, 1024 and 2048 columns 51 and 57, 101 and 106, 200 and 210, 8192
+        // rows 10.2 and 10.0, 18.5 and 18.1, 36 and 29.  Whole warps in 16 bits, 65536 rows, 512, 1024 and 2048 columns: 27.0
+        // and 25.9, 48.9 and 48.2, 93.3 and 92.5, and worse for fewer: the other form.
         const void *fn = pick_warp_types(dtype, param, (int)(d + 255) / 256);
         const uint64_t resident = (uint64_t)sms * resident_ctas(fn, kWarpThreads, 0, device);
         if (rows >= resident * (kWarpThreads / 32) * 10) {

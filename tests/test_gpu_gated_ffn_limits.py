@@ -32,6 +32,15 @@ def test_small_float16_gradients(scale):
     _check_backward(p, "silu", p.backward("silu"))
 
 
+@pytest.mark.parametrize("t,d,f", [(1, 1603, 6401), (9, 1603, 6401), (16, 777, 2051), (8, 2048, 4099), (13, 2051, 4096), (2, 4096, 1025)])
+def test_few_tokens_with_large_matrices_that_are_not_aligned(t, d, f):
+    for pad, skew in ((3, 1), (0, 8)):
+        p = Block(t, d, f, torch.bfloat16, pad, skew)
+        p.forward("silu")
+        _check_forward(p, "silu")
+        p.check_edges()
+
+
 class Rows(Block):
     """Some rows of a block's matrices."""
 
