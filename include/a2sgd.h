@@ -492,7 +492,8 @@ int a2sgd_gated_ffn_forward(const void *x, int64_t x_stride, const void *w_gate,
  *     dh = dy w_down,   da = dh b act'(a),   db = dh act(a)      (da, db rounded once, in the workspace)
  *     dx = da w_gate + db w_up,   dw_gate = da^T x,   dw_up = db^T x,   dw_down = dy^T hidden
  * dx [tokens, d], dw_gate, dw_up [f, d], dw_down [d, f]: each may be NULL, and what only it needs is then not
- * computed.  No tokens give zero weight gradients. */
+ * computed.  No tokens give zero weight gradients.  da and db have the type's range as well as its precision: with float16, scale dy
+ * so that dh b act'(a) and dh act(a) stay between 2^-14, below which their unit is 2^-24, and 65504. */
 int a2sgd_gated_ffn_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *w_gate,
                              int64_t w_gate_stride, const void *w_up, int64_t w_up_stride, const void *w_down,
                              int64_t w_down_stride, const void *hidden, int64_t hidden_stride, const void *gate,

@@ -17,8 +17,12 @@
 // (Wd, Wg, Wu in the backward pass, everything in the weight gradients) are read as they lie, as
 // MN-major operands; nothing is transposed in memory.
 //
-// B200, bfloat16, 8192 x 1600 x 6400: forward 340 us (1480 TFLOP/s), with the outputs for the backward pass 363, backward 748 us
-// (1345 TFLOP/s); at the power cap 395, 426 and 883, where the library's products alone take 412 and 892.
+// B200, bfloat16, 8192 x 1600 x 6400, in a loop at the power cap: forward 400 us, with the outputs for the backward pass 429
+// (1170 TFLOP/s), backward 902 (1115); the library's products alone take 415 and 897.  In short bursts 343, 368 and 756.
+//
+// hidden, da and db are held in the 16-bit type between the products: they are operands of the next ones, which take 16-bit
+// numbers (hidden is the caller's tensor besides).  Each is rounded once, from fp32; the outputs after them are 1.4 times as far from the
+// 64-bit result as with fp32 in between (bfloat16 0.0023 in place of 0.0017, float16 0.00029 in place of 0.00021, as 2-norms).
 //
 // Rows whose address or stride is not a multiple of 16 bytes cannot be read by TMA; they are first
 // copied to padded rows in the workspace.
