@@ -49,6 +49,50 @@ def test_column_sums_of_many_rows(d):
     assert torch.all((dw.double().abs() - s).abs() <= (_bound(7812 / 512 + 1) + 4 * U) * s)
 
 
+@pytest.mark.parametrize("d", [8, 9, 72, 777, 1600])
+def test_several_runs_of_rows_in_several_groups(d):
+    """More than 512 rows for each group of four CTAs an SM, so that the second launch adds to the first one's sums: with and without
+    vector accesses, one group a CTA (1600) and up to 64 (8), in place and beside it.  The groups' and CTAs' sums take at most 64 + 19 + 32
+    roundings more; a term's own three are 4 u of (|x| + |mean|) rstd |dy|."""
+    need = -(-d // 8)
+    tpr = 1 << (need - 1).bit_length() if need <= 32 else -(-need // 32) * 32
+    groups = min(64, max(1, 256 // tpr if tpr <= 128 else 1))
+    rows = 512 * _sms() * 4 * groups + 12_345
+    gen = torch.Generator("cuda").manual_seed(d)
+    x = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda").normal_(0.5, 1.0, generator=gen)
+    dy = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda").normal_(0.25, 1.0, generator=gen)
+    mean = torch.empty(rows, device="cuda").normal_(0.5, 0.1, generator=gen)
+    rstd = torch.empty(rows, device="cuda").uniform_(0.5, 1.5, generator=gen)
+    w = torch.linspace(0.5, 1.5, d, device="cuda")
+    dw, db = torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+    work = torch.empty(B.a2sgd_layer_norm_workspace(rows, d), dtype=torch.uint8, device="cuda")
+    dx = torch.empty_like(x)
+    B.a2sgd_layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db, work)
+    want_w, want_b, mag_w, mag_b, own = (torch.zeros(d, dtype=torch.float64, device="cuda") for _ in range(5))
+    step = max(1, (1 << 26) // d)
+    for lo in range(0, rows, step):
+        p = slice(lo, min(rows, lo + step))
+        g, m, r = dy[p].double(), mean[p].double()[:, None], rstd[p].double()[:, None]
+        xhat = (x[p].double() - m) * r
+        want_w += (g * xhat).sum(0)
+        mag_w += (g * xhat).abs().sum(0)
+        own += ((x[p].double().abs() + m.abs()) * r * g.abs()).sum(0)
+        want_b += g.sum(0)
+        mag_b += g.abs().sum(0)
+    bound = (512 + 4 + 64 + 19 + 32) * U
+    assert torch.all((dw.double() - want_w).abs() <= bound * mag_w + 4 * U * own)
+    assert torch.all((db.double() - want_b).abs() <= bound * mag_b)
+    # rows of the later launches are as a few rows alone
+    for lo in (0, rows // 2, rows - 100):
+        p, few = slice(lo, lo + 100), torch.empty((100, d), dtype=torch.bfloat16, device="cuda")
+        B.a2sgd_layer_norm_backward(dy[p], x[p], w, mean[p], rstd[p], few, None, None)
+        err = (dx[p].double() - few.double()).abs()        # the same sums in another order, then half a unit each
+        assert torch.all(err <= 2.02 * HALF_ULP[torch.bfloat16] * few.double().abs() + 1e-4)
+    first = dx.clone()
+    B.a2sgd_layer_norm_backward(dy, x, w, mean, rstd, dy, dw, None, work)
+    assert torch.equal(dy, first)
+
+
 def test_sums_of_long_rows():
     d, c = 1 << 24, 1.9697274
     runs = d / 1024 / 512
