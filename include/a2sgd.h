@@ -509,6 +509,133 @@ int a2sgd_gated_ffn_backward(const void *dy, int64_t dy_stride, const void *x, i
  * nothing away from other streams, each of which is told once, whichever stream the call ran on. */
 int a2sgd_gated_ffn_status(int device, int *device_status, void *stream);
 
+/* ----------------------------------------------------------------------
+ * The attention half of a block: attention, rotary positions, and the residual connection with the norms around it.
+ * The conventions above hold.
+ *
+ * A tensor of heads: element c of head h in row t of sequence b is at p[b sequence_stride + t row_stride + h head_stride + c],
+ * strides in ELEMENTS.  Packed sequences share one plane: sequence_stride 0, and ranges say which rows are whose. */
+typedef struct a2sgd_heads {
+    void *p;
+    int64_t sequence_stride, row_stride, head_stride;
+} a2sgd_heads;
+
+/* Attention with a sliding window and first tokens that stay visible.  Query i of a sequence with Lq queries and Lk keys stands at
+ * place p = i + Lk - Lq (the last query at the last key) and sees key j where
+ *     j <= p   and   (j > p - window   or   j < sinks)
+ *     o = sum_j P_j v_j,   P = softmax over the visible j of scale (q . k_j),   lse = log sum exp of the same
+ * Query head h reads key head h / (q_heads / kv_heads).  A query that sees nothing (it stands before the first key, or there are no keys)
+ * has o = 0 and lse = -infinity.  Scores, sums and the output are accumulated in fp32; P is rounded once to the 16-bit type, as the
+ * operand of its product with v.
+ *   sequences, q_heads, kv_heads, head_dim   kv_heads divides q_heads; head_dim 1 to A2SGD_ATTENTION_MAX_HEAD_DIM
+ *   q_rows, k_rows   rows of a sequence's plane of the q and of the k tensors (packed: of the one plane)
+ *   q_ranges, k_ranges   DEVICE, [sequences][2] or NULL: first row and number of rows of each sequence in its plane.  NULL: all rows of
+ *               its own plane.  Rows outside are neither read into a result nor written; what they hold does not matter.  Ranges of
+ *               different sequences in one plane must not overlap where they are written, and are clipped to the plane.
+ *   window      at least 1; 2^31 and more: every key up to the query's own place
+ *   scale       finite, > 0;   dtype  A2SGD_BF16 or A2SGD_F16
+ *   lse         fp32 [sequences][q_heads][q_rows] (packed: [q_heads][q_rows]), out, for the backward pass; may be NULL
+ * Tensors whose address is a multiple of 16 bytes and whose strides are multiples of 8 elements are read where they are; others are
+ * first copied to the workspace.  A key or value that is not finite reaches every query whose tile of keys it is in, masked or not,
+ * as long as it lies in its sequence's range.
+ *   workspace   DEVICE, 256-byte aligned, a2sgd_window_attention_workspace bytes: flags A2SGD_ATTENTION_BACKWARD, and
+ *               A2SGD_ATTENTION_ALIGNED when every tensor that is read is laid out as above
+ * Outputs must not overlap an input or one another. */
+#define A2SGD_ATTENTION_MAX_HEAD_DIM 128
+#define A2SGD_ATTENTION_BACKWARD 1u
+#define A2SGD_ATTENTION_ALIGNED 2u
+typedef struct a2sgd_attention {
+    uint32_t sequences, q_heads, kv_heads, head_dim;
+    uint64_t q_rows, k_rows;
+    const int32_t *q_ranges, *k_ranges;
+    uint64_t window;
+    uint32_t sinks;
+    int32_t dtype;
+    double scale;
+} a2sgd_attention;
+uint64_t a2sgd_window_attention_workspace(const a2sgd_attention *shape, uint32_t flags);
+int a2sgd_window_attention_forward(const a2sgd_attention *shape, const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *v,
+                                   const a2sgd_heads *o, float *lse, void *workspace, uint64_t workspace_bytes, int device,
+                                   void *stream);
+
+/* Its backward pass, from dout and what the forward pass left (o, lse):
+ *     delta = sum_c dout o,   P = exp(scale q . k - lse),   dS = P (dout . v - delta)
+ *     dq = scale sum_j dS k,   dk = scale sum_i dS q,   dv = sum_i P dout      (dk, dv over the query heads of the key head, too)
+ * P and dS are rounded once to the 16-bit type, as operands of the products; with float16 scale dout so that dS stays between 2^-14 and
+ * 65504.  dq, dk, dv may each be NULL, and what only they need is then not computed.  Rows in a range that no query sees get zeros. */
+int a2sgd_window_attention_backward(const a2sgd_attention *shape, const a2sgd_heads *dout, const a2sgd_heads *q, const a2sgd_heads *k,
+                                    const a2sgd_heads *v, const a2sgd_heads *o, const float *lse, const a2sgd_heads *dq,
+                                    const a2sgd_heads *dk, const a2sgd_heads *dv, void *workspace, uint64_t workspace_bytes, int device,
+                                    void *stream);
+
+/* Rotary positions with several axes.  The first 2 n elements of a head, n = sum of sections, are n pairs; pair j belongs to the axis a whose
+ * section it lies in (the first sections[0] pairs to axis 0, and so on) and is turned by the angle positions[a][t] * omega_j:
+ *     (u, v) <- (u cos - v sin, u sin + v cos)      (A2SGD_ROTARY_INVERSE: by the opposite angle, which is the backward pass)
+ *     omega_j = base^(-j / n);   A2SGD_ROTARY_LADDER_PER_AXIS: base^(-l / sections[a]), l counted from the axis' first pair
+ * Pair j is the elements j and j + n; A2SGD_ROTARY_INTERLEAVED: 2 j and 2 j + 1.  Elements past the pairs are copied.  Angles are kept as
+ * 64-bit fractions of a turn (pos times a 64-bit frequency, modulo one turn), so that far positions lose nothing.
+ *   q, k        [tokens] rows of q_heads and k_heads heads (sequence_stride is not read); outputs q_out, k_out the same; an output may be its
+ *               input.  k_heads may be 0
+ *   positions   DEVICE, int32 [axes][tokens];   sections  HOST [axes], each at least 1;   axes 1 to A2SGD_ROTARY_MAX_AXES
+ *   head_dim    1 to A2SGD_ROTARY_MAX_HEAD_DIM, >= 2 n;   base  finite, > 0;   dtype  any
+ * Heads that start at multiples of 16 bytes, with n a multiple of 16 bytes too where pairs are not interleaved, take 128-bit accesses. */
+#define A2SGD_ROTARY_MAX_AXES 4
+#define A2SGD_ROTARY_MAX_HEAD_DIM 512
+#define A2SGD_ROTARY_INTERLEAVED 1u
+#define A2SGD_ROTARY_LADDER_PER_AXIS 2u
+#define A2SGD_ROTARY_INVERSE 4u
+int a2sgd_rotary(const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *q_out, const a2sgd_heads *k_out, const int32_t *positions,
+                 uint32_t axes, const uint32_t *sections, double base, uint32_t flags, uint64_t tokens, uint32_t q_heads,
+                 uint32_t k_heads, uint32_t head_dim, int dtype, int device, void *stream);
+
+/* The residual connection of a block with its gate, its scale, the norm after the block and the norm before the next one, over rows of d:
+ *     n = norm(y) post_weight + post_bias     (without A2SGD_RESIDUAL_POST_NORM: n = y)
+ *     z = x + alpha gate n                    (gate: row / gate_rows of it, or 1)
+ *     u = norm(z) pre_weight + pre_bias
+ *     norm(a) = (a - mean) rstd, rstd = 1 / sqrt(variance + eps);  A2SGD_RESIDUAL_RMS: a rstd, rstd = 1 / sqrt(mean of a^2 + eps)
+ * in fp32; z and u are each rounded once (u from z as it was before its rounding).
+ *   y, u        [rows] rows of `dtype`, stride in ELEMENTS (>= d);   x, z  the same of residual_dtype (A2SGD_F32, or dtype)
+ *   gate        [ceil(rows / gate_rows)][d], contiguous, or NULL;  gate_rows >= 1 with a gate
+ *   weights, biases  [d] or NULL (1 and 0), and gate: of param_dtype (A2SGD_F32, or dtype)
+ *   post_mean, post_rstd, pre_mean, pre_rstd  out, fp32 [rows], for the backward pass; each may be NULL
+ *   d           up to A2SGD_RESIDUAL_MAX_COLUMNS;   z may be x, u may be y (where the types agree, with the same stride) */
+#define A2SGD_RESIDUAL_MAX_COLUMNS 8192
+#define A2SGD_RESIDUAL_RMS 1u
+#define A2SGD_RESIDUAL_POST_NORM 2u
+typedef struct a2sgd_rows {
+    void *p;
+    int64_t stride;
+} a2sgd_rows;
+typedef struct a2sgd_residual {
+    uint64_t rows, gate_rows;
+    uint32_t d, flags;
+    int32_t dtype, residual_dtype, param_dtype, reserved;
+    double alpha, eps;
+    const void *post_weight, *post_bias, *gate, *pre_weight, *pre_bias;
+    float *post_mean, *post_rstd, *pre_mean, *pre_rstd;
+} a2sgd_residual;
+int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2sgd_rows *x, const a2sgd_rows *y, const a2sgd_rows *z,
+                                const a2sgd_rows *u, int device, void *stream);
+
+/* Its backward pass, from dz (what reaches z beside u; p NULL: nothing), du, y, z and the statistics (the means are not read for RMS):
+ *     t = dz + back(du pre_weight; z),   dx = t,   dn = alpha gate t,   dy = back(dn post_weight; y)  (no norm: dn)
+ *     back(g; a) = rstd (g - mean_c(g) - hat mean_c(g hat)),  hat = norm(a);  RMS: without mean_c(g)
+ *     dpre_weight = sum du norm(z),  dpre_bias = sum du,  dpost_weight = sum dn norm(y),  dpost_bias = sum dn,
+ *     dgate = sum over its rows of alpha t n
+ * dx may be dz, dy may be du or y (where the types agree, with the same stride).  dx.p and dy.p may be NULL, and so may each of the sums, which are of param_dtype
+ * and are zero when there are no rows.  shape->pre_bias and eps are not read.
+ *   workspace   DEVICE, 256-byte aligned, a2sgd_residual_norm_workspace bytes (needed for any of the sums) */
+typedef struct a2sgd_residual_sums {
+    void *dpost_weight, *dpost_bias, *dgate, *dpre_weight, *dpre_bias;
+} a2sgd_residual_sums;
+uint64_t a2sgd_residual_norm_workspace(uint64_t rows, uint32_t d, uint64_t gate_rows, int device);
+int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a2sgd_rows *dz, const a2sgd_rows *du, const a2sgd_rows *y,
+                                 const a2sgd_rows *z, const a2sgd_rows *dx, const a2sgd_rows *dy, const a2sgd_residual_sums *sums,
+                                 void *workspace, uint64_t workspace_bytes, int device, void *stream);
+
+/* As a2sgd_gated_ffn_status, for the attention's kernels. */
+int a2sgd_window_attention_status(int device, int *device_status, void *stream);
+
 /* Static, never NULL. */
 const char *a2sgd_status_string(int status);
 

@@ -125,6 +125,22 @@ def lib() -> ctypes.CDLL:
         for fn in (l.a2sgd_adamw_read_state, l.a2sgd_adamw_write_state):
             fn.restype = _int
             fn.argtypes = [_vp, _vp, _vp, _vp]
+        l.a2sgd_window_attention_workspace.restype = _u64
+        l.a2sgd_window_attention_workspace.argtypes = [_vp, _u32]
+        l.a2sgd_window_attention_forward.restype = _int
+        l.a2sgd_window_attention_forward.argtypes = [_vp] * 7 + [_u64, _int, _vp]
+        l.a2sgd_window_attention_backward.restype = _int
+        l.a2sgd_window_attention_backward.argtypes = [_vp] * 11 + [_u64, _int, _vp]
+        l.a2sgd_window_attention_status.restype = _int
+        l.a2sgd_window_attention_status.argtypes = [_int, ctypes.POINTER(_int), _vp]
+        l.a2sgd_rotary.restype = _int
+        l.a2sgd_rotary.argtypes = [_vp] * 5 + [_u32, _vp, _dbl, _u32, _u64, _u32, _u32, _u32, _int, _int, _vp]
+        l.a2sgd_residual_norm_forward.restype = _int
+        l.a2sgd_residual_norm_forward.argtypes = [_vp] * 5 + [_int, _vp]
+        l.a2sgd_residual_norm_workspace.restype = _u64
+        l.a2sgd_residual_norm_workspace.argtypes = [_u64, _u32, _u64, _int]
+        l.a2sgd_residual_norm_backward.restype = _int
+        l.a2sgd_residual_norm_backward.argtypes = [_vp] * 9 + [_u64, _int, _vp]
         l.a2sgd_layer_norm_forward.restype = _int
         l.a2sgd_layer_norm_forward.argtypes = [_vp, _i64, _int, _vp, _vp, _int, _vp, _i64, _vp, _vp, _u64, _u32, _dbl,
                                                _int, _vp]
@@ -781,3 +797,254 @@ def a2sgd_gated_ffn_status(device: Optional[int] = None, stream=None) -> int:
     _check(lib().a2sgd_gated_ffn_status(device, ctypes.byref(st), _stream_on(device, stream)),
            "a2sgd_gated_ffn_status")
     return st.value
+
+
+# ---- the attention half of a block: attention, rotary positions, the residual connection with its norms
+
+ATTENTION_BACKWARD, ATTENTION_ALIGNED = 1, 2
+ROTARY_INTERLEAVED, ROTARY_LADDER_PER_AXIS, ROTARY_INVERSE = 1, 2, 4
+RESIDUAL_RMS, RESIDUAL_POST_NORM = 1, 2
+NO_WINDOW = 1 << 31
+
+
+class _AttentionShape(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_uint32), ("q_heads", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32), ("q_rows", ctypes.c_uint64), ("k_rows", ctypes.c_uint64), ("q_ranges", _vp),
+                ("k_ranges", _vp), ("window", ctypes.c_uint64), ("sinks", ctypes.c_uint32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_double)]
+
+
+class _ResidualShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("gate_rows", ctypes.c_uint64), ("d", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+                ("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("alpha", ctypes.c_double), ("eps", ctypes.c_double)] \
+        + [(name, _vp) for name in ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias", "post_mean", "post_rstd",
+                                    "pre_mean", "pre_rstd")]
+
+
+def _heads(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int):
+    """CUDA [sequences, rows, heads, head_dim], or [rows, heads, head_dim] of packed sequences, unit inner stride ->
+    (address, sequence stride, row stride, head stride)."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        raise ValueError(f"{name}: need a {dtype} tensor {list(shape)} on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: need unit inner stride")
+    return (t.data_ptr(), 0, stride[0], stride[1]) if len(shape) == 3 else (t.data_ptr(), *stride[:3])
+
+
+def _ranges(t: Optional[torch.Tensor], name: str, sequences: int, index: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.get_device() != index or t.shape != (sequences, 2) or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous int32 tensor [{sequences}, 2] on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _attention_shape(q, k, window, sinks, scale, q_ranges, k_ranges):
+    dev = _cuda_index(q, "q")
+    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float16:
+        raise ValueError(f"q: need bfloat16 or float16, got {q.dtype}")
+    if q.dim() not in (3, 4) or k.dim() not in (3, 4):
+        raise ValueError("q, k: need [sequences, rows, heads, head_dim], or [rows, heads, head_dim] of packed sequences")
+    sequences = None
+    for t, ranges, name in ((q, q_ranges, "q"), (k, k_ranges, "k")):
+        if t.dim() == 3 and ranges is None:
+            raise ValueError(f"{name}: packed sequences need {name}_ranges")
+        n = t.shape[0] if t.dim() == 4 else ranges.shape[0]
+        if sequences is not None and n != sequences:
+            raise ValueError(f"q, k: {sequences} and {n} sequences")
+        sequences = n
+    if q.shape[-1] != k.shape[-1]:
+        raise ValueError("q, k: head_dim differs")
+    window = NO_WINDOW if window is None else int(window)
+    if window < 1 or sinks < 0:
+        raise ValueError("window: at least 1 (None: all keys up to the query's own place); sinks: at least 0")
+    d = q.shape[-1]
+    shape = _AttentionShape(sequences, q.shape[-2], k.shape[-2], d, q.shape[-3], k.shape[-3], _ranges(q_ranges, "q_ranges", sequences, dev),
+                            _ranges(k_ranges, "k_ranges", sequences, dev), window, min(int(sinks), NO_WINDOW), _DTYPE_CODES[q.dtype],
+                            d ** -0.5 if scale is None else scale)
+    return dev, shape
+
+
+def _lse(t, q, dev):
+    if t is None:
+        return None
+    want = (q.shape[1], q.shape[0]) if q.dim() == 3 else (q.shape[0], q.shape[2], q.shape[1])
+    if t.shape != want:
+        raise ValueError(f"lse: need {list(want)}, got {list(t.shape)}")
+    return _vector(t, "lse", t.numel(), torch.float32, dev)
+
+
+def _table(*heads):
+    """The tensors' (address, strides) one after another in memory, as the header's structures, and where each begins."""
+    flat = [x for h in heads for x in (h if h is not None else (0, 0, 0, 0))]
+    table = (_i64 * len(flat))(*flat)
+    at = ctypes.addressof(table)
+    return table, [at + 32 * i for i in range(len(heads))]
+
+
+def a2sgd_window_attention_workspace(q: torch.Tensor, k: torch.Tensor, window: Optional[int], sinks: int, sequences: int,
+                                     backward: bool = False, aligned: bool = False) -> int:
+    """Bytes of workspace of a2sgd_window_attention_forward (or _backward).  aligned: every tensor that is read starts at a multiple
+    of 16 bytes and has strides that are multiples of 8 elements."""
+    shape = _AttentionShape(int(sequences), q.shape[-2], k.shape[-2], q.shape[-1], q.shape[-3], k.shape[-3], None, None,
+                            NO_WINDOW if window is None else int(window), min(int(sinks), NO_WINDOW), _DTYPE_CODES.get(q.dtype, -1), 1.0)
+    flags = (ATTENTION_BACKWARD if backward else 0) | (ATTENTION_ALIGNED if aligned else 0)
+    return int(lib().a2sgd_window_attention_workspace(ctypes.addressof(shape), flags))
+
+
+def a2sgd_window_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+                                   lse: Optional[torch.Tensor] = None, window: Optional[int] = None, sinks: int = 0,
+                                   scale: Optional[float] = None, q_ranges: Optional[torch.Tensor] = None,
+                                   k_ranges: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                   stream=None) -> None:
+    """q, o: [sequences, q_rows, q_heads, head_dim]; k, v: [sequences, k_rows, kv_heads, head_dim]; without the first dimension
+    for packed sequences.  One 16-bit type, unit inner stride.  lse: float32 [sequences, q_heads, q_rows] (packed: [q_heads, q_rows]),
+    out, or None.  window: None for every key up to the query's own place; scale: None for head_dim ** -0.5.  q_ranges, k_ranges: int32
+    [sequences, 2], first row and number of rows, or None for all.  workspace: uint8 CUDA tensor of
+    a2sgd_window_attention_workspace bytes."""
+    dev, shape = _attention_shape(q, k, window, sinks, scale, q_ranges, k_ranges)
+    dt, wb = q.dtype, 0 if workspace is None else workspace.numel()
+    table, (qa, ka, va, oa) = _table(_heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev),
+                                     _heads(v, "v", k.shape, dt, dev), _heads(o, "o", q.shape, dt, dev))
+    _check(lib().a2sgd_window_attention_forward(
+        ctypes.addressof(shape), qa, ka, va, oa, _lse(lse, q, dev), _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev,
+        _stream_on(dev, stream)), "a2sgd_window_attention_forward")
+
+
+def a2sgd_window_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+                                    lse: torch.Tensor, dq: Optional[torch.Tensor], dk: Optional[torch.Tensor],
+                                    dv: Optional[torch.Tensor], window: Optional[int] = None, sinks: int = 0,
+                                    scale: Optional[float] = None, q_ranges: Optional[torch.Tensor] = None,
+                                    k_ranges: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                    stream=None) -> None:
+    """dout: as o; o, lse: what the forward pass left; dq, dk, dv: out, as q, k, v, each may be None; the rest as in the forward pass,
+    workspace of a2sgd_window_attention_workspace(..., backward=True) bytes."""
+    dev, shape = _attention_shape(q, k, window, sinks, scale, q_ranges, k_ranges)
+    dt, wb = q.dtype, 0 if workspace is None else workspace.numel()
+    maybe = lambda t, name, like: None if t is None else _heads(t, name, like.shape, dt, dev)  # noqa: E731
+    table, at = _table(_heads(dout, "dout", q.shape, dt, dev), _heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev),
+                       _heads(v, "v", k.shape, dt, dev), _heads(o, "o", q.shape, dt, dev), maybe(dq, "dq", q), maybe(dk, "dk", k),
+                       maybe(dv, "dv", k))
+    _check(lib().a2sgd_window_attention_backward(
+        ctypes.addressof(shape), *at[:5], _lse(lse, q, dev), *at[5:], _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev,
+        _stream_on(dev, stream)), "a2sgd_window_attention_backward")
+
+
+def a2sgd_window_attention_status(device: Optional[int] = None, stream=None) -> int:
+    """Synchronises the stream; ERR_TIMEOUT if a wait inside one of the attention's kernels has run out on the device since this
+    was last asked with the same stream, else OK."""
+    device = torch.cuda.current_device() if device is None else int(device)
+    st = ctypes.c_int(0)
+    _check(lib().a2sgd_window_attention_status(device, ctypes.byref(st), _stream_on(device, stream)),
+           "a2sgd_window_attention_status")
+    return st.value
+
+
+def a2sgd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor, k_out: Optional[torch.Tensor],
+                 positions: torch.Tensor, sections, base: float = 10000.0, interleaved: bool = False,
+                 ladder_per_axis: bool = False, inverse: bool = False, stream=None) -> None:
+    """q, q_out: [tokens, q_heads, head_dim], unit inner stride; k, k_out: [tokens, k_heads, head_dim], or None; an output may be its
+    input.  positions: int32 [axes, tokens], contiguous; sections: pairs of each axis.  inverse: the opposite angles, which is the
+    backward pass."""
+    dev, code = _cuda_index(q, "q"), _dtype_code(q, "q")
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q, k: need [tokens, heads, head_dim]")
+    tokens, heads, d = q.shape
+    if (k is None) != (k_out is None) or (k is not None and (k.shape[0] != tokens or k.shape[2] != d)):
+        raise ValueError("k, k_out: need as many tokens and elements as q, or neither")
+    axes = len(sections)
+    if positions.shape != (axes, tokens):
+        raise ValueError(f"positions: need {[axes, tokens]}, got {list(positions.shape)}")
+    pos = _vector(positions, "positions", axes * tokens, torch.int32, dev)
+    if axes and min(sections) < 1:
+        raise ValueError("sections: need at least one pair each")
+    none = (0, 0, 0, 0)
+    table, at = _table(_heads(q, "q", q.shape, q.dtype, dev), none if k is None else _heads(k, "k", k.shape, q.dtype, dev),
+                       _heads(q_out, "q_out", q.shape, q.dtype, dev), none if k is None else _heads(k_out, "k_out", k.shape, q.dtype, dev))
+    flags = (ROTARY_INTERLEAVED if interleaved else 0) | (ROTARY_LADDER_PER_AXIS if ladder_per_axis else 0) | (ROTARY_INVERSE if inverse else 0)
+    _check(lib().a2sgd_rotary(*at, pos, axes, (ctypes.c_uint32 * axes)(*sections), base, flags, tokens, heads,
+                              0 if k is None else k.shape[1], d, code, dev, _stream_on(dev, stream)), "a2sgd_rotary")
+
+
+_NORM_KINDS = {"layer": 0, "rms": RESIDUAL_RMS}
+
+
+def _residual_shape(y, residual, kind, post, post_weight, post_bias, gate, gate_rows, alpha, pre_weight, pre_bias, stats, eps, *params):
+    dev, code = _cuda_index(y, "y"), _dtype_code(y, "y")
+    if y.dim() != 2:
+        raise ValueError("y: need [rows, d]")
+    if kind not in _NORM_KINDS:
+        raise ValueError(f"kind: need one of {sorted(_NORM_KINDS)}, got {kind!r}")
+    rows, d = y.shape
+    pt = _param_dtype(y, post_weight, post_bias, gate, pre_weight, pre_bias, *params)
+    groups = 0
+    if gate is not None:
+        if gate_rows < 1:
+            raise ValueError("gate_rows: at least 1 with a gate")
+        groups = -(-rows // gate_rows)
+    rest = [_vector(t, name, n, dtype, dev) for t, name, n, dtype in
+            ((post_weight, "post_weight", d, pt), (post_bias, "post_bias", d, pt), (gate, "gate", groups * d, pt),
+             (pre_weight, "pre_weight", d, pt), (pre_bias, "pre_bias", d, pt))]
+    rest += [_vector(t, name, rows, torch.float32, dev) for t, name in zip(stats, ("post_mean", "post_rstd", "pre_mean", "pre_rstd"))]
+    shape = _ResidualShape(rows, gate_rows if gate is not None else 0, d, _NORM_KINDS[kind] | (RESIDUAL_POST_NORM if post else 0), code,
+                           _dtype_code(residual, "x or z"), _DTYPE_CODES.get(pt, -1), 0, alpha, eps, *rest)
+    return dev, shape, pt, groups
+
+
+def _rows_table(dev, shape, *tensors):
+    flat = [x for t, name, dtype in tensors for x in ((0, 0) if t is None else _matrix(t, name, shape, dtype, dev))]
+    table = (_i64 * len(flat))(*flat)
+    at = ctypes.addressof(table)
+    return table, [at + 16 * i for i in range(len(tensors))]
+
+
+def a2sgd_residual_norm_forward(x: torch.Tensor, y: torch.Tensor, z: torch.Tensor, u: torch.Tensor, kind: str = "rms",
+                                post: bool = True, post_weight: Optional[torch.Tensor] = None,
+                                post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                                alpha: float = 1.0, pre_weight: Optional[torch.Tensor] = None,
+                                pre_bias: Optional[torch.Tensor] = None, post_mean: Optional[torch.Tensor] = None,
+                                post_rstd: Optional[torch.Tensor] = None, pre_mean: Optional[torch.Tensor] = None,
+                                pre_rstd: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """z = x + alpha * gate * norm(y), u = norm(z).  y, u: [rows, d]; x, z: the same in float32 or y's type, unit inner stride; z
+    may be x, u may be y.  kind: "rms" or "layer"; post False: y is not normed.  weights, biases: [d]; gate: [ceil(rows / gate_rows), d];
+    of float32 or y's type, each may be None.  post_mean ... pre_rstd: float32 [rows], out, or None."""
+    dev, shape, _, _ = _residual_shape(y, x, kind, post, post_weight, post_bias, gate, gate_rows, alpha, pre_weight, pre_bias,
+                                       (post_mean, post_rstd, pre_mean, pre_rstd), eps)
+    table, at = _rows_table(dev, y.shape, (x, "x", x.dtype), (y, "y", y.dtype), (z, "z", x.dtype), (u, "u", y.dtype))
+    _check(lib().a2sgd_residual_norm_forward(ctypes.addressof(shape), *at, dev, _stream_on(dev, stream)), "a2sgd_residual_norm_forward")
+
+
+def a2sgd_residual_norm_workspace(rows: int, d: int, gate_rows: int = 0, device: Optional[int] = None) -> int:
+    """Bytes of workspace of a2sgd_residual_norm_backward (gate_rows: 0 without a gate)."""
+    device = torch.cuda.current_device() if device is None else int(device)
+    return int(lib().a2sgd_residual_norm_workspace(int(rows), int(d), int(gate_rows), device))
+
+
+def a2sgd_residual_norm_backward(dz: Optional[torch.Tensor], du: torch.Tensor, y: torch.Tensor, z: torch.Tensor,
+                                 dx: Optional[torch.Tensor], dy: Optional[torch.Tensor], kind: str = "rms", post: bool = True,
+                                 post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                                 gate: Optional[torch.Tensor] = None, gate_rows: int = 0, alpha: float = 1.0,
+                                 pre_weight: Optional[torch.Tensor] = None, post_mean: Optional[torch.Tensor] = None,
+                                 post_rstd: Optional[torch.Tensor] = None, pre_mean: Optional[torch.Tensor] = None,
+                                 pre_rstd: Optional[torch.Tensor] = None, dpost_weight: Optional[torch.Tensor] = None,
+                                 dpost_bias: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                                 dpre_weight: Optional[torch.Tensor] = None, dpre_bias: Optional[torch.Tensor] = None,
+                                 workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dz: what reaches z beside u (None: nothing); du, y, z and the statistics as the forward pass left them; dx (may be dz), dy (may be
+    du or y) and the sums over the rows: out, each may be None.  workspace: uint8 CUDA tensor of a2sgd_residual_norm_workspace bytes,
+    needed for any of the sums."""
+    dev, shape, pt, groups = _residual_shape(y, z, kind, post, post_weight, post_bias, gate, gate_rows, alpha, pre_weight, None,
+                                             (post_mean, post_rstd, pre_mean, pre_rstd), 0.0, dpost_weight, dpost_bias, dgate,
+                                             dpre_weight, dpre_bias)
+    d = y.shape[1]
+    table, at = _rows_table(dev, y.shape, (dz, "dz", z.dtype), (du, "du", y.dtype), (y, "y", y.dtype), (z, "z", z.dtype),
+                            (dx, "dx", z.dtype), (dy, "dy", y.dtype))
+    sums = (_vp * 5)(_vector(dpost_weight, "dpost_weight", d, pt, dev), _vector(dpost_bias, "dpost_bias", d, pt, dev),
+                     _vector(dgate, "dgate", groups * d, pt, dev), _vector(dpre_weight, "dpre_weight", d, pt, dev),
+                     _vector(dpre_bias, "dpre_bias", d, pt, dev))
+    wb = 0 if workspace is None else workspace.numel()
+    _check(lib().a2sgd_residual_norm_backward(ctypes.addressof(shape), *at, ctypes.addressof(sums),
+                                              _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev, _stream_on(dev, stream)),
+           "a2sgd_residual_norm_backward")

@@ -1,0 +1,646 @@
+// The residual connection of a block with its gate, its scale, the norm after the block and the norm before the next one.
+//
+//   forward   n = norm(y) w1 + b1,  z = x + alpha gate n,  u = norm(z) w2 + b2
+//   backward  t = dz + back(du w2; z),  dx = t,  dn = alpha gate t,  dy = back(dn w1; y),  and the columns' sums
+//
+// Bound by memory: forward reads x, y and writes z, u; backward reads dz, du, y, z and writes dx, dy.  A CTA takes a run of
+// consecutive rows, one after another, a row's elements in its threads' registers; the next row's are on their way while the present
+// one is worked on.  Each norm costs one barrier: a warp forms its own mean and sum of squares about it by shuffles, and
+// the warps' are joined from shared memory (Chan's formula), so that no element is squared about anything but a mean near its own.
+//
+// The columns' sums: t hat1 and t (from which the gate's, the post weight's and the post bias' gradients follow, a gate at a time), du hat2
+// and du.  A CTA adds its rows up in registers or shared memory, leaves one partial sum a column, and a second kernel adds the CTAs' in order.
+#include "a2sgd_train.cuh"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+using namespace a2sgd_train;
+
+namespace {
+
+constexpr int kMostThreads = 512;
+constexpr int kSums = 4; // t hat1, t, du hat2, du
+
+struct Rows {
+    void *p;
+    int64_t ld;
+};
+struct Args {
+    Rows x, y, z, u, dz, du, dx, dy;
+    const void *w1, *b1, *gate, *w2, *b2;
+    float *mean1, *rstd1, *mean2, *rstd2;
+    int64_t rows, gate_rows, run; // rows of a CTA
+    int d, param, rms, post;
+    float alpha, eps;
+    // backward
+    void *dw1, *db1, *dgate, *dw2, *db2;
+    float *partials;      // [CTAs][4][d]: dw1, db1, dw2, db2
+    float *gate_partials; // [CTAs][2][d]
+    int ctas;
+};
+
+__device__ __forceinline__ float param_at(const void *p, int type, int64_t i)
+{
+    if (type == A2SGD_F32) return static_cast<const float *>(p)[i];
+    if (type == A2SGD_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    return __half2float(static_cast<const __half *>(p)[i]);
+}
+__device__ __forceinline__ void param_put(void *p, int type, int64_t i, float v)
+{
+    if (type == A2SGD_F32) static_cast<float *>(p)[i] = v;
+    else if (type == A2SGD_BF16) static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+    else static_cast<__half *>(p)[i] = __float2half_rn(v);
+}
+
+// Eight elements of a thread: consecutive ones, or ones a CTA's threads apart (any alignment).
+template <typename T, int VEC>
+struct Eight;
+template <typename T>
+struct Eight<T, 8> {
+    Raw8<T> raw;
+    __device__ __forceinline__ void load(const T *row, int chunk, int d)
+    {
+        const int c = (chunk * (int)blockDim.x + (int)threadIdx.x) * 8;
+        if (c < d) raw.load(row + c);
+        else raw.zero();
+    }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const { raw.unpack(f); }
+    __device__ static __forceinline__ void store(T *row, int chunk, int d, const float (&f)[8])
+    {
+        const int c = (chunk * (int)blockDim.x + (int)threadIdx.x) * 8;
+        if (c < d) store8(row + c, f);
+    }
+};
+template <typename T>
+struct Eight<T, 1> {
+    T v[8];
+    __device__ __forceinline__ void load(const T *row, int chunk, int d)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = (chunk * 8 + i) * (int)blockDim.x + (int)threadIdx.x;
+            v[i] = c < d ? row[c] : from_f32<T>(0.0f);
+        }
+    }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = to_f32(v[i]);
+    }
+    __device__ static __forceinline__ void store(T *row, int chunk, int d, const float (&f)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = (chunk * 8 + i) * (int)blockDim.x + (int)threadIdx.x;
+            if (c < d) row[c] = from_f32<T>(f[i]);
+        }
+    }
+};
+template <int VEC>
+__device__ __forceinline__ int column(int chunk, int i)
+{
+    return VEC == 8 ? (chunk * (int)blockDim.x + (int)threadIdx.x) * 8 + i : (chunk * 8 + i) * (int)blockDim.x + (int)threadIdx.x;
+}
+// Eight columns of a vector of parameters, or `other` without one.
+template <int VEC>
+__device__ __forceinline__ void params8(float (&f)[8], const void *p, int type, int64_t base, int chunk, int d, float other)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int c = column<VEC>(chunk, i);
+        f[i] = p && c < d ? param_at(p, type, base + c) : other;
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int s = 16; s; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+    return v;
+}
+
+// Two sums over the CTA's threads, in a fixed order.  slot: [2][warps] floats, not in use since the barrier before the last.
+__device__ __forceinline__ void cta_sums(float &a, float &b, float *slot)
+{
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if (warps > 1) {
+        if ((threadIdx.x & 31) == 0) {
+            slot[warp] = a;
+            slot[16 + warp] = b;
+        }
+        __syncthreads();
+        a = b = 0.0f;
+        for (int w = 0; w < warps; ++w) {
+            a += slot[w];
+            b += slot[16 + w];
+        }
+    }
+}
+
+// The mean (0 for RMS) and 1 / sqrt(variance or mean square + eps) of a row whose elements the threads hold.
+template <int VEC, int C>
+__device__ __forceinline__ void moments(const float (&v)[C][8], const Args &a, float *slot, float &mean, float &rstd)
+{
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+    float sum = 0.0f, square = 0.0f;
+    if (a.rms) {
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) square = fmaf(v[k][i], v[k][i], square); // zeros past the row's end
+        cta_sums(sum, square, slot);
+        mean = 0.0f;
+        rstd = 1.0f / sqrtf(square / (float)a.d + a.eps);
+        return;
+    }
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < C; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sum += v[k][i];
+            count += column<VEC>(k, i) < a.d;
+        }
+    sum = warp_sum(sum);
+    const float n = (float)__reduce_add_sync(0xffffffffu, count), own = n > 0.0f ? sum / n : 0.0f;
+#pragma unroll
+    for (int k = 0; k < C; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = column<VEC>(k, i) < a.d ? v[k][i] - own : 0.0f;
+            square = fmaf(e, e, square);
+        }
+    square = warp_sum(square);
+    mean = own;
+    if (warps > 1) {
+        if ((threadIdx.x & 31) == 0) {
+            slot[warp] = sum;
+            slot[16 + warp] = square;
+            slot[32 + warp] = n;
+        }
+        __syncthreads();
+        sum = square = 0.0f;
+        for (int w = 0; w < warps; ++w) sum += slot[w];
+        mean = sum / (float)a.d;
+        for (int w = 0; w < warps; ++w) {
+            const float m = slot[32 + w], off = m > 0.0f ? slot[w] / m - mean : 0.0f;
+            square += slot[16 + w] + m * off * off;
+        }
+    }
+    rstd = 1.0f / sqrtf(square / (float)a.d + a.eps);
+}
+
+template <typename T, typename R, int VEC, int C>
+__global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant__ Args a)
+{
+    __shared__ float slots[2][48];
+    wait_prior_grid();
+    release_next_grid();
+    const int64_t row0 = (int64_t)blockIdx.x * a.run, end = min(a.rows, row0 + a.run);
+    if (row0 >= end) return;
+    Eight<T, VEC> y[C];
+    Eight<R, VEC> x[C];
+    const auto bring = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            y[k].load(static_cast<const T *>(a.y.p) + r * a.y.ld, k, a.d);
+            x[k].load(static_cast<const R *>(a.x.p) + r * a.x.ld, k, a.d);
+        }
+    };
+    bring(row0);
+    for (int64_t r = row0; r < end; ++r) {
+        float n[C][8], z[C][8];
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            y[k].unpack(n[k]);
+            x[k].unpack(z[k]);
+        }
+        if (r + 1 < end) bring(r + 1);
+        float mean = 0.0f, rstd = 1.0f;
+        if (a.post) {
+            moments<VEC, C>(n, a, slots[0], mean, rstd);
+            if (threadIdx.x == 0) {
+                if (a.mean1) a.mean1[r] = mean;
+                if (a.rstd1) a.rstd1[r] = rstd;
+            }
+        }
+        const int64_t gate = a.gate ? r / a.gate_rows * a.d : 0;
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            float w[8], b[8], g[8];
+            params8<VEC>(g, a.gate, a.param, gate, k, a.d, 1.0f);
+            if (a.post) {
+                params8<VEC>(w, a.w1, a.param, 0, k, a.d, 1.0f);
+                params8<VEC>(b, a.b1, a.param, 0, k, a.d, 0.0f);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (a.post) n[k][i] = fmaf((n[k][i] - mean) * rstd, w[i], b[i]);
+                z[k][i] = column<VEC>(k, i) < a.d ? fmaf(a.alpha * g[i], n[k][i], z[k][i]) : 0.0f;
+            }
+            Eight<R, VEC>::store(static_cast<R *>(a.z.p) + r * a.z.ld, k, a.d, z[k]);
+        }
+        moments<VEC, C>(z, a, slots[1], mean, rstd);
+        if (threadIdx.x == 0) {
+            if (a.mean2) a.mean2[r] = mean;
+            if (a.rstd2) a.rstd2[r] = rstd;
+        }
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            float w[8], b[8], u[8];
+            params8<VEC>(w, a.w2, a.param, 0, k, a.d, 1.0f);
+            params8<VEC>(b, a.b2, a.param, 0, k, a.d, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = fmaf((z[k][i] - mean) * rstd, w[i], b[i]);
+            Eight<T, VEC>::store(static_cast<T *>(a.u.p) + r * a.u.ld, k, a.d, u);
+        }
+    }
+}
+
+template <typename T, typename R, int VEC, int C>
+__global__ void __launch_bounds__(kMostThreads) k_backward(const __grid_constant__ Args a)
+{
+    extern __shared__ float sums[]; // [4][columns of the CTA], for C > 1
+    __shared__ float slots[2][48];
+    wait_prior_grid();
+    release_next_grid();
+    const int64_t row0 = (int64_t)blockIdx.x * a.run, end = min(a.rows, row0 + a.run);
+    if (row0 >= end) return;
+    const int span = C * 8 * (int)blockDim.x;
+    const bool want = a.partials != nullptr;
+    float acc[kSums][8] = {};
+    const auto sum_at = [&](int s, int k, int i) -> float & { return sums[s * span + (k * 8 + i) * (int)blockDim.x + (int)threadIdx.x]; };
+    if constexpr (C > 1) {
+        for (int s = 0; s < kSums; ++s)
+            for (int k = 0; k < C; ++k)
+                for (int i = 0; i < 8; ++i) sum_at(s, k, i) = 0.0f;
+    }
+    Eight<T, VEC> y[C], du[C];
+    Eight<R, VEC> z[C], dz[C];
+    const auto bring = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            y[k].load(static_cast<const T *>(a.y.p) + r * a.y.ld, k, a.d);
+            du[k].load(static_cast<const T *>(a.du.p) + r * a.du.ld, k, a.d);
+            z[k].load(static_cast<const R *>(a.z.p) + r * a.z.ld, k, a.d);
+            if (a.dz.p) dz[k].load(static_cast<const R *>(a.dz.p) + r * a.dz.ld, k, a.d);
+        }
+    };
+    bring(row0);
+    bool flushed = false; // this CTA's partial sums hold earlier gates' rows
+    for (int64_t r = row0; r < end; ++r) {
+        const float mean2 = a.rms ? 0.0f : a.mean2[r], rstd2 = a.rstd2[r];
+        const float mean1 = a.rms || !a.post ? 0.0f : a.mean1[r], rstd1 = a.post ? a.rstd1[r] : 1.0f;
+        const int64_t group = a.gate ? r / a.gate_rows : 0;
+        float h1[C][8], t[C][8], s0 = 0.0f, s1 = 0.0f;
+        Eight<T, VEC> g2[C];
+        Eight<R, VEC> zz[C], res[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            y[k].unpack(h1[k]);
+            g2[k] = du[k];
+            zz[k] = z[k];
+            res[k] = dz[k];
+        }
+        if (r + 1 < end) bring(r + 1);
+        // the norm before the next block
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            float w[8], g[8], h[8];
+            params8<VEC>(w, a.w2, a.param, 0, k, a.d, 1.0f);
+            g2[k].unpack(g);
+            zz[k].unpack(h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = column<VEC>(k, i) < a.d;
+                h[i] = in ? (h[i] - mean2) * rstd2 : 0.0f;
+                if (want) {
+                    if constexpr (C == 1) {
+                        acc[2][i] = fmaf(g[i], h[i], acc[2][i]);
+                        acc[3][i] += g[i];
+                    } else {
+                        sum_at(2, k, i) += g[i] * h[i];
+                        sum_at(3, k, i) += g[i];
+                    }
+                }
+                const float gw = in ? g[i] * w[i] : 0.0f;
+                s0 += gw;
+                s1 = fmaf(gw, h[i], s1);
+            }
+        }
+        cta_sums(s0, s1, slots[0]);
+        s0 = a.rms ? 0.0f : s0 / (float)a.d;
+        s1 /= (float)a.d;
+        float p0 = 0.0f, p1 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            float w[8], g[8], h[8], e[8];
+            params8<VEC>(w, a.w2, a.param, 0, k, a.d, 1.0f);
+            g2[k].unpack(g);
+            zz[k].unpack(h);
+            if (a.dz.p) res[k].unpack(e);
+            float w1[8], gt[8];
+            if (a.post) params8<VEC>(w1, a.w1, a.param, 0, k, a.d, 1.0f);
+            params8<VEC>(gt, a.gate, a.param, group * a.d, k, a.d, 1.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = column<VEC>(k, i) < a.d;
+                const float hat = (h[i] - mean2) * rstd2;
+                const float v = (g[i] * w[i] - s0 - hat * s1) * rstd2;
+                t[k][i] = in ? v + (a.dz.p ? e[i] : 0.0f) : 0.0f;
+                h1[k][i] = in ? (h1[k][i] - mean1) * rstd1 : 0.0f;
+                if (want) {
+                    if constexpr (C == 1) {
+                        acc[0][i] = fmaf(t[k][i], h1[k][i], acc[0][i]);
+                        acc[1][i] += t[k][i];
+                    } else {
+                        sum_at(0, k, i) += t[k][i] * h1[k][i];
+                        sum_at(1, k, i) += t[k][i];
+                    }
+                }
+            }
+            if (a.dx.p) Eight<R, VEC>::store(static_cast<R *>(a.dx.p) + r * a.dx.ld, k, a.d, t[k]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                t[k][i] *= a.alpha * gt[i];
+                if (a.post) {
+                    t[k][i] *= w1[i];
+                    p0 += t[k][i];
+                    p1 = fmaf(t[k][i], h1[k][i], p1);
+                }
+            }
+        }
+        if (a.post) {
+            cta_sums(p0, p1, slots[1]);
+            p0 = a.rms ? 0.0f : p0 / (float)a.d;
+            p1 /= (float)a.d;
+        }
+        if (a.dy.p) {
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[k][i] = a.post ? (t[k][i] - p0 - h1[k][i] * p1) * rstd1 : t[k][i];
+                Eight<T, VEC>::store(static_cast<T *>(a.dy.p) + r * a.dy.ld, k, a.d, t[k]);
+            }
+        }
+        // a gate's last row in this CTA: what its rows give to the gate, the post weight and the post bias
+        const bool last = r + 1 == end;
+        if (want && (last || (a.gate && (r + 1) / a.gate_rows != group))) {
+            const bool whole = a.gate && group * a.gate_rows >= row0 && min(a.rows, (group + 1) * a.gate_rows) <= end;
+            const int slot = a.gate && group != row0 / a.gate_rows;
+            float *mine = a.partials + (int64_t)blockIdx.x * kSums * a.d;
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                float w1[8], b1[8], gt[8];
+                params8<VEC>(w1, a.post ? a.w1 : nullptr, a.param, 0, k, a.d, 1.0f);
+                params8<VEC>(b1, a.post ? a.b1 : nullptr, a.param, 0, k, a.d, 0.0f);
+                params8<VEC>(gt, a.gate, a.param, group * a.d, k, a.d, 1.0f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = column<VEC>(k, i);
+                    if (c >= a.d) continue;
+                    float hat, one;
+                    if constexpr (C == 1) hat = acc[0][i], one = acc[1][i], acc[0][i] = acc[1][i] = 0.0f;
+                    else hat = sum_at(0, k, i), one = sum_at(1, k, i), sum_at(0, k, i) = sum_at(1, k, i) = 0.0f;
+                    if (a.dgate) {
+                        const float v = a.alpha * fmaf(w1[i], hat, b1[i] * one);
+                        if (whole) param_put(a.dgate, a.param, group * a.d + c, v);
+                        else a.gate_partials[((int64_t)blockIdx.x * 2 + slot) * a.d + c] = v;
+                    }
+                    const float f = a.alpha * gt[i];
+                    mine[c] = (flushed ? mine[c] : 0.0f) + f * hat;
+                    mine[a.d + c] = (flushed ? mine[a.d + c] : 0.0f) + f * one;
+                    if (last) {
+                        if constexpr (C == 1) mine[2 * a.d + c] = acc[2][i], mine[3 * a.d + c] = acc[3][i];
+                        else mine[2 * a.d + c] = sum_at(2, k, i), mine[3 * a.d + c] = sum_at(3, k, i);
+                    }
+                }
+            }
+            flushed = true;
+        }
+    }
+}
+
+// The CTAs' sums, added up in order: blocks of 32 columns, eight strips of CTAs each.  blockIdx.y: dw1, db1, dw2, db2, then the gates.
+__global__ void __launch_bounds__(256) k_fold(const __grid_constant__ Args a)
+{
+    __shared__ float part[8][32];
+    wait_prior_grid();
+    release_next_grid();
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), strip = threadIdx.x >> 5;
+    const int64_t groups = a.gate ? (a.rows + a.gate_rows - 1) / a.gate_rows : 0;
+    for (int64_t job = blockIdx.y; job < kSums + groups; job += gridDim.y) {
+        void *out;
+        int64_t at = c;
+        int first = 0, last = a.ctas - 1;
+        if (job < kSums) {
+            out = job == 0 ? a.dw1 : job == 1 ? a.db1 : job == 2 ? a.dw2 : a.db2;
+        } else {
+            const int64_t g = job - kSums;
+            out = a.dgate;
+            at += g * a.d;
+            first = (int)(g * a.gate_rows / a.run);
+            last = (int)((min(a.rows, (g + 1) * a.gate_rows) - 1) / a.run);
+            if (first == last) out = nullptr; // written by the one CTA that had all of its rows
+        }
+        if (!out) continue;
+        float sum = 0.0f;
+        if (c < a.d) {
+            const int count = last - first + 1, lo = first + count * strip / 8, hi = first + count * (strip + 1) / 8;
+#pragma unroll 4
+            for (int k = lo; k < hi; ++k) {
+                if (job < kSums) sum += __ldcg(a.partials + ((int64_t)k * kSums + job) * a.d + c);
+                else sum += __ldcg(a.gate_partials + ((int64_t)k * 2 + (k * a.run / a.gate_rows != job - kSums)) * a.d + c);
+            }
+        }
+        part[strip][threadIdx.x & 31] = sum;
+        __syncthreads();
+        if (strip == 0 && c < a.d) {
+            for (int k = 1; k < 8; ++k) sum += part[k][threadIdx.x];
+            param_put(out, a.param, at, sum);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ host
+struct Plan {
+    int threads, chunks, vec;
+};
+Plan plan_of(uint32_t d, bool vec)
+{
+    Plan p;
+    p.vec = vec ? 8 : 1;
+    p.chunks = d > 8u * kMostThreads ? 2 : 1;
+    const int pieces = (int)(d + 8 * p.chunks - 1) / (8 * p.chunks);
+    p.threads = (pieces + 31) / 32 * 32;
+    return p;
+}
+
+template <typename T, typename R>
+const void *pick(const Plan &p, bool backward)
+{
+#define A2_PICK(V, K)                                                                                         \
+    if (p.vec == V && p.chunks == K)                                                                          \
+        return backward ? reinterpret_cast<const void *>(&k_backward<T, R, V, K>) : reinterpret_cast<const void *>(&k_forward<T, R, V, K>);
+    A2_PICK(8, 1)
+    A2_PICK(8, 2)
+    A2_PICK(1, 1)
+    A2_PICK(1, 2)
+#undef A2_PICK
+    return nullptr;
+}
+const void *pick_types(int dtype, int residual, const Plan &p, bool backward)
+{
+    if (dtype == A2SGD_F32) return pick<float, float>(p, backward);
+    if (dtype == A2SGD_BF16) return residual == A2SGD_F32 ? pick<__nv_bfloat16, float>(p, backward) : pick<__nv_bfloat16, __nv_bfloat16>(p, backward);
+    return residual == A2SGD_F32 ? pick<__half, float>(p, backward) : pick<__half, __half>(p, backward);
+}
+size_t smem_of(const Plan &p, bool backward) { return backward && p.chunks > 1 ? (size_t)kSums * p.chunks * 8 * p.threads * 4 : 0; }
+
+int check_shape(const a2sgd_residual *s)
+{
+    if (!s || !known(s->dtype) || (s->residual_dtype != A2SGD_F32 && s->residual_dtype != s->dtype) ||
+        (s->param_dtype != A2SGD_F32 && s->param_dtype != s->dtype) || s->d == 0 || (s->flags & ~3u) || !std::isfinite(s->alpha) ||
+        (s->gate && s->gate_rows == 0))
+        return A2SGD_ERR_ARG;
+    if (s->d > A2SGD_RESIDUAL_MAX_COLUMNS || s->rows >= (1ull << 40) || s->gate_rows >= (1ull << 62)) return A2SGD_ERR_TOO_LARGE;
+    for (const void *p : {s->post_weight, s->post_bias, s->gate, s->pre_weight, s->pre_bias})
+        if (!aligned(p, size_of(s->param_dtype))) return A2SGD_ERR_ALIGN;
+    for (const float *p : {s->post_mean, s->post_rstd, s->pre_mean, s->pre_rstd})
+        if (!aligned(p, 4)) return A2SGD_ERR_ALIGN;
+    return A2SGD_OK;
+}
+int check_rows(const a2sgd_rows *r, const a2sgd_residual *s, int dtype, bool needed)
+{
+    if (!r || !r->p) return needed ? A2SGD_ERR_ARG : A2SGD_OK;
+    if (s->rows > 1 && r->stride < (int64_t)s->d) return A2SGD_ERR_ARG;
+    return aligned(r->p, size_of(dtype)) ? A2SGD_OK : A2SGD_ERR_ALIGN;
+}
+Rows rows_of(const a2sgd_rows *r) { return r && r->p ? Rows{r->p, r->stride} : Rows{nullptr, 0}; }
+bool wide(const a2sgd_rows *r, const a2sgd_residual *s, int dtype)
+{
+    if (!r || !r->p) return true;
+    return aligned(r->p, 16) && (s->rows <= 1 || r->stride * (int64_t)size_of(dtype) % 16 == 0);
+}
+
+Args common(const a2sgd_residual *s)
+{
+    Args a{};
+    a.w1 = s->post_weight, a.b1 = s->post_bias, a.gate = s->gate, a.w2 = s->pre_weight, a.b2 = s->pre_bias;
+    a.mean1 = s->post_mean, a.rstd1 = s->post_rstd, a.mean2 = s->pre_mean, a.rstd2 = s->pre_rstd;
+    a.rows = (int64_t)s->rows;
+    a.gate_rows = s->gate ? (int64_t)s->gate_rows : 1;
+    a.d = (int)s->d;
+    a.param = s->param_dtype;
+    a.rms = (s->flags & A2SGD_RESIDUAL_RMS) != 0;
+    a.post = (s->flags & A2SGD_RESIDUAL_POST_NORM) != 0;
+    a.alpha = (float)s->alpha;
+    a.eps = (float)s->eps;
+    return a;
+}
+
+constexpr int kMostCtas = 1024; // that leave partial sums
+inline uint64_t sums_bytes(int64_t ctas, uint32_t d, bool gate) { return (uint64_t)ctas * (kSums + (gate ? 2 : 0)) * d * 4; }
+int64_t most_ctas(uint64_t rows) { return (int64_t)std::min<uint64_t>(rows, kMostCtas); }
+
+} // namespace
+
+extern "C" int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2sgd_rows *x, const a2sgd_rows *y, const a2sgd_rows *z,
+                                           const a2sgd_rows *u, int device, void *stream)
+{
+    int rc = check_shape(shape);
+    if (rc != A2SGD_OK) return rc;
+    if (!std::isfinite(shape->eps) || shape->eps < 0.0) return A2SGD_ERR_ARG;
+    if (shape->rows == 0) return A2SGD_OK;
+    const int t = shape->dtype, r = shape->residual_dtype;
+    if ((rc = check_rows(x, shape, r, true)) != A2SGD_OK || (rc = check_rows(y, shape, t, true)) != A2SGD_OK ||
+        (rc = check_rows(z, shape, r, true)) != A2SGD_OK || (rc = check_rows(u, shape, t, true)) != A2SGD_OK)
+        return rc;
+    DeviceGuard guard(device);
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms < 1) return A2SGD_ERR_CUDA;
+    Args a = common(shape);
+    a.x = rows_of(x), a.y = rows_of(y), a.z = rows_of(z), a.u = rows_of(u);
+    const Plan p = plan_of(shape->d, shape->d % 8 == 0 && wide(x, shape, r) && wide(y, shape, t) && wide(z, shape, r) && wide(u, shape, t));
+    const void *fn = pick_types(t, r, p, false);
+    const int64_t most = (int64_t)sms * resident_ctas(fn, (unsigned)p.threads, 0, device);
+    a.run = (a.rows + most - 1) / most;
+    void *params[] = {&a};
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)((a.rows + a.run - 1) / a.run)), (unsigned)p.threads, 0, params, static_cast<cudaStream_t>(stream)));
+    return A2SGD_OK;
+}
+
+extern "C" uint64_t a2sgd_residual_norm_workspace(uint64_t rows, uint32_t d, uint64_t gate_rows, int device)
+{
+    (void)device;
+    return sums_bytes(most_ctas(rows), d, gate_rows != 0);
+}
+
+extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a2sgd_rows *dz, const a2sgd_rows *du, const a2sgd_rows *y,
+                                            const a2sgd_rows *z, const a2sgd_rows *dx, const a2sgd_rows *dy,
+                                            const a2sgd_residual_sums *sums, void *workspace, uint64_t workspace_bytes, int device,
+                                            void *stream)
+{
+    int rc = check_shape(shape);
+    if (rc != A2SGD_OK) return rc;
+    const int t = shape->dtype, r = shape->residual_dtype;
+    const bool rms = shape->flags & A2SGD_RESIDUAL_RMS, post = shape->flags & A2SGD_RESIDUAL_POST_NORM, some = shape->rows != 0;
+    if ((rc = check_rows(dz, shape, r, false)) != A2SGD_OK || (rc = check_rows(du, shape, t, some)) != A2SGD_OK ||
+        (rc = check_rows(y, shape, t, some)) != A2SGD_OK || (rc = check_rows(z, shape, r, some)) != A2SGD_OK ||
+        (rc = check_rows(dx, shape, r, false)) != A2SGD_OK || (rc = check_rows(dy, shape, t, false)) != A2SGD_OK)
+        return rc;
+    if (some && (!shape->pre_rstd || (!rms && !shape->pre_mean) || (post && (!shape->post_rstd || (!rms && !shape->post_mean)))))
+        return A2SGD_ERR_ARG;
+    const a2sgd_residual_sums none{};
+    if (!sums) sums = &none;
+    const void *outs[] = {sums->dpost_weight, sums->dpost_bias, sums->dgate, sums->dpre_weight, sums->dpre_bias};
+    bool want = false;
+    for (const void *p : outs) {
+        if (!aligned(p, size_of(shape->param_dtype))) return A2SGD_ERR_ALIGN;
+        want = want || p;
+    }
+    if ((sums->dgate && !shape->gate) || (!post && (sums->dpost_weight || sums->dpost_bias))) return A2SGD_ERR_ARG;
+    if (!aligned(workspace, 256)) return A2SGD_ERR_ALIGN;
+    if (want && some && (!workspace || workspace_bytes < a2sgd_residual_norm_workspace(shape->rows, shape->d, shape->gate ? shape->gate_rows : 0, device)))
+        return A2SGD_ERR_ARG;
+    DeviceGuard guard(device);
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms < 1) return A2SGD_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (!some) {
+        for (const void *p : outs)
+            if (p && p != sums->dgate) A2_TRAIN_CUDA(cudaMemsetAsync(const_cast<void *>(p), 0, (size_t)shape->d * size_of(shape->param_dtype), s));
+        return A2SGD_OK;
+    }
+    Args a = common(shape);
+    a.dz = rows_of(dz), a.du = rows_of(du), a.y = rows_of(y), a.z = rows_of(z), a.dx = rows_of(dx), a.dy = rows_of(dy);
+    a.dw1 = sums->dpost_weight, a.db1 = sums->dpost_bias, a.dgate = sums->dgate, a.dw2 = sums->dpre_weight, a.db2 = sums->dpre_bias;
+    bool vec = shape->d % 8 == 0;
+    for (const a2sgd_rows *m : {dz, z, dx}) vec = vec && wide(m, shape, r);
+    for (const a2sgd_rows *m : {du, y, dy}) vec = vec && wide(m, shape, t);
+    const Plan p = plan_of(shape->d, vec);
+    const void *fn = pick_types(t, r, p, true);
+    const size_t smem = smem_of(p, true);
+    A2_TRAIN_CUDA(allow_smem(fn, smem));
+    const int64_t most = std::min<int64_t>((int64_t)sms * resident_ctas(fn, (unsigned)p.threads, smem, device), kMostCtas);
+    a.run = (a.rows + most - 1) / most;
+    a.ctas = (int)((a.rows + a.run - 1) / a.run);
+    if (want) {
+        a.partials = static_cast<float *>(workspace);
+        a.gate_partials = a.partials + (int64_t)a.ctas * kSums * a.d;
+    }
+    void *params[] = {&a};
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)a.ctas), (unsigned)p.threads, smem, params, s));
+    if (want) {
+        const int64_t groups = a.dgate ? (a.rows + a.gate_rows - 1) / a.gate_rows : 0;
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold), dim3((unsigned)(a.d + 31) / 32, (unsigned)std::min<int64_t>(kSums + groups, 1024)),
+                             256, 0, params, s));
+    }
+    return A2SGD_OK;
+}
