@@ -538,12 +538,15 @@ typedef struct a2sgd_heads {
  * Tensors whose address is a multiple of 16 bytes and whose strides are multiples of 8 elements are read where they are; others are
  * first copied to the workspace.  A key or value that is not finite reaches every query whose tile of keys it is in, masked or not,
  * as long as it lies in its sequence's range.
- *   workspace   DEVICE, 256-byte aligned, a2sgd_window_attention_workspace bytes: flags A2SGD_ATTENTION_BACKWARD, and
- *               A2SGD_ATTENTION_ALIGNED when every tensor that is read is laid out as above
+ *   workspace   DEVICE, 256-byte aligned, a2sgd_window_attention_workspace bytes: flags A2SGD_ATTENTION_BACKWARD,
+ *               A2SGD_ATTENTION_ALIGNED when every tensor that is read is laid out as above, and A2SGD_ATTENTION_PACKED_Q, _PACKED_K
+ *               when the q and the k tensors hold packed sequences (else room is needed for each sequence's plane)
  * Outputs must not overlap an input or one another. */
 #define A2SGD_ATTENTION_MAX_HEAD_DIM 128
 #define A2SGD_ATTENTION_BACKWARD 1u
 #define A2SGD_ATTENTION_ALIGNED 2u
+#define A2SGD_ATTENTION_PACKED_Q 4u
+#define A2SGD_ATTENTION_PACKED_K 8u
 typedef struct a2sgd_attention {
     uint32_t sequences, q_heads, kv_heads, head_dim;
     uint64_t q_rows, k_rows;

@@ -801,7 +801,7 @@ def a2sgd_gated_ffn_status(device: Optional[int] = None, stream=None) -> int:
 
 # ---- the attention half of a block: attention, rotary positions, the residual connection with its norms
 
-ATTENTION_BACKWARD, ATTENTION_ALIGNED = 1, 2
+ATTENTION_BACKWARD, ATTENTION_ALIGNED, ATTENTION_PACKED_Q, ATTENTION_PACKED_K = 1, 2, 4, 8
 ROTARY_INTERLEAVED, ROTARY_LADDER_PER_AXIS, ROTARY_INVERSE = 1, 2, 4
 RESIDUAL_RMS, RESIDUAL_POST_NORM = 1, 2
 NO_WINDOW = 1 << 31
@@ -890,7 +890,8 @@ def a2sgd_window_attention_workspace(q: torch.Tensor, k: torch.Tensor, window: O
     of 16 bytes and has strides that are multiples of 8 elements."""
     shape = _AttentionShape(int(sequences), q.shape[-2], k.shape[-2], q.shape[-1], q.shape[-3], k.shape[-3], None, None,
                             NO_WINDOW if window is None else int(window), min(int(sinks), NO_WINDOW), _DTYPE_CODES.get(q.dtype, -1), 1.0)
-    flags = (ATTENTION_BACKWARD if backward else 0) | (ATTENTION_ALIGNED if aligned else 0)
+    flags = (ATTENTION_BACKWARD if backward else 0) | (ATTENTION_ALIGNED if aligned else 0) \
+        | (ATTENTION_PACKED_Q if q.dim() == 3 else 0) | (ATTENTION_PACKED_K if k.dim() == 3 else 0)
     return int(lib().a2sgd_window_attention_workspace(ctypes.addressof(shape), flags))
 
 

@@ -1,11 +1,14 @@
 // Attention with a sliding window and first tokens that stay visible, forward and backward.
+#include "a2sgd_tcgen05.cuh"
 #include "a2sgd_train.cuh"
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 using namespace a2sgd_train;
+using namespace a2sgd_tc;
 
 namespace {
 
@@ -45,6 +48,485 @@ __device__ __forceinline__ int64_t lse_at(const Args &a, int b, int head, int64_
 __device__ __forceinline__ bool sees(int place, int key, int window, int sinks)
 {
     return key <= place && (key > place - window || key < sinks);
+}
+
+
+// CTAs whose bounded wait ran out, since the library was loaded: only ever counted up.
+__device__ unsigned int g_waits_run_out = 0;
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------------ forward
+// A CTA takes kTiles tiles of 128 queries of one head and walks the blocks of 128 keys that any of them sees: the first tokens' blocks, then
+// those of the window.  One warp brings tiles in by TMA, one issues the products, four warps a tile hold the softmax, a thread a query.
+//   S = Q K^T into TMEM;  the tile's threads read their rows, form P and write it to TMEM in 16 bits;  O += P V, P read from TMEM.
+// O stays in TMEM.  P is taken about a reference that follows the running maximum: it is moved, and O and the sum with it, only once the
+// maximum has risen by more than 2^8 above it, so that P stays below 2^8 and nearly no block touches O.
+// kEarly (P beside S): the next block's S is formed while the present one's P is; else P lies over S, and the next S is issued after P V.
+struct ForwardArgs {
+    CUtensorMap q, k, v;
+    Heads o;
+    float *lse;
+    const int32_t *q_ranges, *k_ranges;
+    int q_heads, group, d, q_rows, k_rows, window, sinks;
+    int packed_q, q_planes, k_planes, v_planes; // planes: more than one: by sequence
+    int sequences, tiles;                       // tiles of a sequence, or of all packed ones
+    int wide_o;                                 // 16-byte stores
+    float scale_log2;
+};
+
+template <int D, int TILES>
+struct ForwardShape {
+    static constexpr bool kEarly = D == 64 && TILES == 1;
+    static constexpr int kThreads = 128 * (TILES + 1);
+    // registers a thread: 128 or 168 at launch, 200 or 208 for the softmax, whose threads hold a row of 128 scores, 56 or 88 for the rest
+    static constexpr int kMore = TILES == 1 ? 200 : 208, kFewer = TILES == 1 ? 56 : 88;
+    static constexpr uint32_t kTile = (D / 64) * 16384u; // 128 rows
+    static constexpr int kStages = TILES == 1 ? (D == 64 ? 5 : 2) : (D == 64 ? 8 : 5);
+    static constexpr uint32_t kSmem = TILES * kTile + kStages * kTile + 1024;
+    static constexpr uint32_t kColumns = TILES == 1 ? 256 : 512;
+};
+
+// The sequence and the tile of `unit` rows that a CTA has among packed sequences; count 0: none.  One warp.
+__device__ __forceinline__ void locate(const int32_t *ranges, int sequences, int rows, int unit, int target, int &seq, int &tile)
+{
+    const int lane = threadIdx.x & 31;
+    seq = -1, tile = 0;
+    for (int b0 = 0; b0 < sequences; b0 += 32) {
+        const int b = b0 + lane;
+        const int mine = b < sequences ? (range_of(ranges, b, rows).count + unit - 1) / unit : 0;
+        int sum = mine;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, s);
+            if (lane >= s) sum += v;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, sum > target);
+        if (hit) {
+            const int who = __ffs(hit) - 1;
+            seq = b0 + who;
+            tile = target - __shfl_sync(0xffffffffu, sum - mine, who);
+            return;
+        }
+        target -= __shfl_sync(0xffffffffu, sum, 31);
+    }
+}
+
+// The blocks of keys that a run of queries at places p0 to p1 (its last) sees, in order: sink_blocks first ones, then from first_block on.
+struct Blocks {
+    int sink_blocks, first_block, count;
+    __device__ __forceinline__ Blocks(int p0, int p1, int window, int sinks, int block)
+    {
+        const int end = p1 < 0 ? 0 : p1 / block + 1, lo = max(0, p0 - window + 1);
+        first_block = min(lo / block, end);
+        sink_blocks = sinks > 0 ? min((sinks - 1) / block + 1, first_block) : 0;
+        count = sink_blocks + end - first_block;
+    }
+    __device__ __forceinline__ int operator[](int n) const { return n < sink_blocks ? n : first_block + n - sink_blocks; }
+};
+
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Rows `valid` on of a tile of `rows` rows in shared memory are cleared: what lies behind a sequence may be anything, and zero times that
+// is not zero.  The whole warp.
+__device__ __forceinline__ void clear_rows(uint32_t tile, int chunks, int rows, int valid)
+{
+    for (int c = 0; c < chunks; ++c)
+        for (int i = valid * 8 + (int)(threadIdx.x & 31); i < rows * 8; i += 32)
+            st_shared(tile + (uint32_t)(c * rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
+    fence_async();
+    __syncwarp();
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(T *p, const float *v, int count, bool wide) // up to 32 elements
+{
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (8 * i < count)
+                *reinterpret_cast<uint4 *>(p + 8 * i) = make_uint4(pack2(v[8 * i], v[8 * i + 1], T()), pack2(v[8 * i + 2], v[8 * i + 3], T()),
+                                                                   pack2(v[8 * i + 4], v[8 * i + 5], T()), pack2(v[8 * i + 6], v[8 * i + 7], T()));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < count) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+template <typename T>
+__host__ __device__ constexpr uint32_t type_bits() { return std::is_same<T, __nv_bfloat16>::value ? 1u : 0u; }
+
+template <typename T, int D, int TILES>
+__global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ? 2 : 1) k_forward(const __grid_constant__ ForwardArgs a)
+{
+    using Shape = ForwardShape<D, TILES>;
+    constexpr bool kEarly = Shape::kEarly;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64;
+    constexpr uint32_t kTile = Shape::kTile;
+    extern __shared__ char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + TILES * kTile;
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 + 4 * TILES];
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int gave_up;
+    __shared__ int place_of[2];
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 8u * s; };
+    const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+    const uint32_t q_full = bar0 + 8u * (2 * kStages), tail = bar0 + 8u * (2 * kStages + 1);
+    const auto s_full = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + t); };
+    const auto s_free = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + TILES + t); };
+    const auto p_full = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + 2 * TILES + t); };
+    const auto pv_done = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + 3 * TILES + t); };
+    constexpr uint32_t kS = 0, kO = kEarly ? 192 : 128 * TILES; // columns; P: beside S, or over it
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full(s), 1);
+            bar_init(empty(s), 1);
+        }
+        bar_init(q_full, 1);
+        bar_init(tail, 1);
+        for (int t = 0; t < TILES; ++t) {
+            bar_init(s_full(t), 1);
+            bar_init(s_free(t), 4);
+            bar_init(p_full(t), 4);
+            bar_init(pv_done(t), 1);
+        }
+        gave_up = 0;
+        bar_init_fence();
+    }
+    if (warp == 4 * TILES + 1) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
+    wait_prior_grid();
+    // the CTA's head, sequence and queries: the longest tiles of a sequence first
+    int seq, tile, head;
+    if (a.packed_q) {
+        head = blockIdx.x / a.tiles;
+        if (warp == 0) {
+            locate(a.q_ranges, a.sequences, a.q_rows, 128 * TILES, a.tiles - 1 - (int)(blockIdx.x % a.tiles), seq, tile);
+            if (lane == 0) place_of[0] = seq, place_of[1] = tile;
+        }
+    } else {
+        tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);
+        head = blockIdx.x / a.tiles % a.q_heads;
+        seq = blockIdx.x / a.tiles / a.q_heads;
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    release_next_grid(); // not before this CTA has its TMEM: the next kernel's CTAs may want some, and wait for this one's end
+    const uint32_t tmem = tmem_at;
+    if (a.packed_q) seq = place_of[0], tile = place_of[1];
+    Range qr{0, 0}, kr{0, 0};
+    if (seq >= 0) qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
+    const int i0 = tile * 128 * TILES, ahead = kr.count - qr.count;
+    const int rows = min(128 * TILES, qr.count - i0); // of this CTA
+    const int p0 = i0 + ahead;
+    const Blocks blocks(p0, rows > 0 ? p0 + rows - 1 : -1, a.window, a.sinks, 128);
+    const int steps = (a.d + 15) / 16; // of 16 elements of the head
+    // a tile's last query's place, below 0 where it sees nothing; and whether the tile sees a block
+    const auto last_place = [&](int t) { return 128 * t < rows ? p0 + min(rows, 128 * t + 128) - 1 : -1; };
+    const auto sees_block = [&](int t, int block) {
+        const int k0 = block * 128;
+        return k0 <= last_place(t) && (TILES == 1 || k0 + 127 > p0 + 128 * t - a.window || k0 < a.sinks);
+    };
+
+    if (warp >= 4 * TILES) {
+    fewer_registers<Shape::kFewer>();
+    if (rows > 0 && warp == 4 * TILES) {
+        // ---------------------------------------------------------- tiles in
+        const bool chosen = elect_one();
+        int stage = 0;
+        uint32_t phase = 0, tails = 0;
+        bool ok = true;
+        if (blocks.count > 0 && chosen) {
+            bar_expect(q_full, TILES * kTile);
+            for (int t = 0; t < TILES; ++t)
+                for (int c = 0; c < kChunks; ++c)
+                    tma_load4(base + t * kTile + c * 16384u, &a.q, 64 * c, qr.first + i0 + 128 * t, head, a.q_planes > 1 ? seq : 0, q_full);
+        }
+        const auto bring = [&](const CUtensorMap *map, int planes, int block, bool clear) {
+            ok = ok && bar_wait(empty(stage), phase ^ 1u, &gave_up);
+            if (!ok) return;
+            const uint32_t dst = ring + stage * kTile;
+            const int valid = kr.count - block * 128;
+            clear = clear && a.k_ranges && valid < 128;
+            const uint32_t bar = clear ? tail : full(stage);
+            if (chosen) {
+                bar_expect(bar, kTile);
+                for (int c = 0; c < kChunks; ++c)
+                    tma_load4(dst + c * 16384u, map, 64 * c, kr.first + block * 128, head / a.group, planes > 1 ? seq : 0, bar);
+            }
+            __syncwarp();
+            if (clear) {
+                ok = bar_wait(tail, tails & 1u, &gave_up);
+                ++tails;
+                if (!ok) return;
+                clear_rows(dst, kChunks, 128, valid);
+                if (chosen) bar_arrive(full(stage));
+                __syncwarp();
+            }
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+        };
+        if (blocks.count > 0) bring(&a.k, a.k_planes, blocks[0], false);
+        for (int n = 0; ok && n < blocks.count; ++n) {
+            if (kEarly && n + 1 < blocks.count) bring(&a.k, a.k_planes, blocks[n + 1], false);
+            bring(&a.v, a.v_planes, blocks[n], true);
+            if (!kEarly && n + 1 < blocks.count) bring(&a.k, a.k_planes, blocks[n + 1], false);
+        }
+        // every tile has been consumed: nothing is in flight towards this CTA any more
+        for (int s = 0; ok && s < kStages; ++s) {
+            ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+        }
+    } else if (rows > 0 && warp == 4 * TILES + 1) {
+        // ---------------------------------------------------------- products
+        const bool chosen = elect_one();
+        const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, 128);
+        const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
+        int stage = 0;
+        uint32_t phase = 0;
+        int done[TILES] = {};
+        bool ok = blocks.count > 0 && bar_wait(q_full, 0, &gave_up);
+        const auto next = [&] {
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+        };
+        const auto form_s = [&](int t, uint32_t k) { // one thread
+            const uint64_t dq = operand_desc(base + t * kTile, 16), dk = operand_desc(k, 16);
+            for (int j = 0; j < steps; ++j) { // 64 elements a chunk of 16 KB
+                const uint32_t off = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4;
+                mma_ss(tmem + kS + 128 * t, dq + off, dk + off, desc_s, j > 0);
+            }
+            commit(s_full(t));
+        };
+        const auto add_pv = [&](int t, uint32_t v, bool first) { // one thread
+            const uint64_t dv = operand_desc(v, 16384);
+            const uint32_t p = tmem + (kEarly ? 128 : 128 * t);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mma_ts(tmem + kO + D * t, p + 8 * j, dv + j * (2048 >> 4), desc_o, !first || j > 0);
+        };
+        if (ok) ok = bar_wait(full(stage), phase, &gave_up);
+        if (ok) {
+            fence_after();
+            if (chosen) {
+                for (int t = 0; t < TILES; ++t)
+                    if (sees_block(t, blocks[0])) form_s(t, ring + stage * kTile);
+                commit(empty(stage));
+            }
+            __syncwarp();
+            next();
+        }
+        for (int n = 0; ok && n < blocks.count; ++n) {
+            const bool more = n + 1 < blocks.count;
+            if constexpr (kEarly) {
+                if (more) {
+                    ok = bar_wait(full(stage), phase, &gave_up) && bar_wait(s_free(0), n & 1, &gave_up);
+                    if (!ok) break;
+                    fence_after();
+                    if (chosen) {
+                        form_s(0, ring + stage * kTile);
+                        commit(empty(stage));
+                    }
+                    __syncwarp();
+                    next();
+                }
+                ok = bar_wait(full(stage), phase, &gave_up) && bar_wait(p_full(0), n & 1, &gave_up);
+                if (!ok) break;
+                fence_after();
+                if (chosen) {
+                    add_pv(0, ring + stage * kTile, n == 0);
+                    commit(empty(stage));
+                    commit(pv_done(0));
+                }
+                __syncwarp();
+                next();
+            } else {
+                ok = bar_wait(full(stage), phase, &gave_up);
+                if (!ok) break;
+                const uint32_t v = ring + stage * kTile, v_empty = empty(stage);
+                next();
+                const uint32_t k = ring + stage * kTile, k_empty = empty(stage);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    if (sees_block(t, blocks[n])) {
+                        ok = bar_wait(p_full(t), done[t] & 1, &gave_up);
+                        if (!ok) break;
+                        fence_after();
+                        if (chosen) {
+                            add_pv(t, v, done[t] == 0);
+                            if (blocks[n] == last_place(t) / 128) commit(pv_done(t));
+                        }
+                        ++done[t];
+                    }
+                    if (t == TILES - 1 && chosen) commit(v_empty);
+                    __syncwarp();
+                    if (more) {
+                        if (t == 0) ok = bar_wait(full(stage), phase, &gave_up);
+                        if (!ok) break;
+                        fence_after();
+                        if (chosen) {
+                            if (sees_block(t, blocks[n + 1])) form_s(t, k); // behind P V in the order of issue, which reads P where S goes
+                            if (t == TILES - 1) commit(k_empty);
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (more) next();
+            }
+        }
+    }
+    } else {
+        more_registers<Shape::kMore>();
+        if (rows > 0) {
+        // ---------------------------------------------------------- softmax, a thread a query
+        const int t = TILES == 1 ? 0 : warp >> 2, quarter = warp & 3;
+        const int row = 128 * t + quarter * 32 + lane, place = p0 + row;
+        const int w0 = p0 + 128 * t + quarter * 32, w1 = w0 + 31; // the warp's places
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t ts = lanes + kS + 128 * t, tp = kEarly ? lanes + 128 : ts, to = lanes + kO + D * t;
+        const float c = a.scale_log2;
+        float ref = -INFINITY, total = 0.0f;
+        int done = 0;
+        bool ok = true;
+        for (int n = 0; n < blocks.count; ++n) {
+            const int k0 = blocks[n] * 128;
+            if (!sees_block(t, blocks[n])) continue;
+            ok = bar_wait(s_full(t), done & 1, &gave_up);
+            if (!ok) break;
+            fence_after();
+            // groups of 32 keys that some row of the warp sees, and those that every row does
+            bool some[4], all[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int g0 = k0 + 32 * e, g1 = g0 + 31;
+                some[e] = g0 <= w1 && (g1 > w0 - a.window || g0 < a.sinks);
+                all[e] = g1 <= w0 && (g0 > w1 - a.window || g1 < a.sinks);
+            }
+            float s[128];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (some[e]) tmem_ld32(ts + 32 * e, reinterpret_cast<float(&)[32]>(s[32 * e]));
+            tmem_wait_ld();
+            if (kEarly) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(s_free(t));
+            }
+            float top0 = -INFINITY, top1 = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!some[e]) continue;
+                float(&x)[32] = reinterpret_cast<float(&)[32]>(s[32 * e]);
+                if (!all[e]) {
+                    const int g0 = k0 + 32 * e;
+                    const uint32_t seen = below(place + 1 - g0) & (~below(place - a.window + 1 - g0) | below(a.sinks - g0));
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = seen >> i & 1u ? x[i] : -INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    top0 = fmaxf(top0, x[i]);
+                    top1 = fmaxf(top1, x[i + 1]);
+                }
+            }
+            const float top = fmaxf(top0, top1);
+            const bool moves = top > ref && (top - ref) * c > 8.0f; // from -infinity, too
+            float shrink = 1.0f;
+            if (moves) {
+                shrink = exp2_approx((ref - top) * c);
+                ref = top;
+                total *= shrink;
+            }
+            const float off = ref == -INFINITY ? 0.0f : -ref * c;
+            const f32x2 c2 = pair(c), off2 = pair(off);
+            if (kEarly && done > 0) { // the product before has read P, and O is at rest
+                ok = bar_wait(pv_done(t), (done - 1) & 1, &gave_up);
+                if (!ok) break;
+                fence_after();
+            }
+            if (done > 0 && __any_sync(0xffffffffu, moves)) {
+#pragma unroll 1
+                for (int e = 0; 16 * e < a.d; ++e) {
+                    uint32_t r[16];
+                    tmem_ld16(to + 16 * e, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * shrink);
+                    tmem_st16(to + 16 * e, r);
+                }
+            }
+            f32x2 sum0 = pair(0.0f), sum1 = pair(0.0f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t p[16];
+                if (some[e]) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        float x0, x1, x2, x3;
+                        unpair(fma2(pair(s[32 * e + i], s[32 * e + i + 1]), c2, off2), x0, x1);
+                        unpair(fma2(pair(s[32 * e + i + 2], s[32 * e + i + 3]), c2, off2), x2, x3);
+                        x0 = exp2_approx(x0), x1 = exp2_approx(x1), x2 = exp2_approx(x2), x3 = exp2_approx(x3);
+                        sum0 = add2(sum0, pair(x0, x1));
+                        sum1 = add2(sum1, pair(x2, x3));
+                        p[i / 2] = pack2(x0, x1, T());
+                        p[i / 2 + 1] = pack2(x2, x3, T());
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[i] = 0;
+                }
+                tmem_st16(tp + 16 * e, p);
+            }
+            total += sum2(add2(sum0, sum1));
+            tmem_wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(p_full(t));
+            ++done;
+        }
+        if (ok && done > 0) {
+            ok = bar_wait(pv_done(t), kEarly ? (done - 1) & 1 : 0, &gave_up);
+            fence_after();
+        }
+        if (ok) {
+            const bool live = row < rows;
+            const int64_t out_row = qr.first + i0 + row;
+            const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
+            T *p = live ? at<T>(a.o, seq, out_row, head) : nullptr;
+#pragma unroll 1
+            for (int e = 0; 32 * e < a.d; ++e) {
+                float o[32];
+                if (done > 0) {
+                    tmem_ld32(to + 32 * e, o);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = total > 0.0f || total != total ? o[i] * (total != total ? total : inverse) : 0.0f;
+                if (live) store_row(p + 32 * e, o, a.d - 32 * e, a.wide_o);
+            }
+            if (live && a.lse)
+                a.lse[((int64_t)(a.packed_q ? 0 : seq) * a.q_heads + head) * a.q_rows + out_row] =
+                    total > 0.0f ? ref * (c * kLn2) + logf(total) : total != total ? total : -INFINITY;
+        }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (gave_up) {
+        // leave the copies and products in flight a bounded time to end, and say so
+        if (threadIdx.x == 0) atomicAdd(&g_waits_run_out, 1u);
+        const uint64_t begin = now_ns();
+        while (now_ns() - begin < 5000000ull) __nanosleep(1000);
+    }
+    if (warp == 4 * TILES + 1) tmem_free(tmem, Shape::kColumns);
 }
 
 // A warp a query: 32 keys at a time, a lane each, then the lanes share out the head's elements.
@@ -163,6 +645,36 @@ __global__ void __launch_bounds__(128) k_key(const __grid_constant__ Args a)
     }
 }
 
+// ------------------------------------------------------------------ tensors that TMA cannot read
+struct PackJob {
+    Heads src;
+    uint16_t *dst;
+    int64_t rows; // of all planes
+    int plane_rows, heads;
+};
+struct PackArgs {
+    PackJob job[4];
+    int d, padded;
+};
+__global__ void __launch_bounds__(256) k_pack_heads(const __grid_constant__ PackArgs a)
+{
+    wait_prior_grid();
+    release_next_grid();
+    const PackJob &j = a.job[blockIdx.y];
+    const int pieces = a.padded / 8; // 16 bytes of a padded head each
+    const int64_t all = j.rows * j.heads * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t head_row = i / pieces, row = head_row / j.heads, plane = row / j.plane_rows;
+        const int c = (int)(i - head_row * pieces) * 8, head = (int)(head_row - row * j.heads);
+        const uint16_t *s = static_cast<const uint16_t *>(j.src.p) + plane * j.src.seq + (row - plane * j.plane_rows) * j.src.row + (int64_t)head * j.src.head + c;
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c + k < a.d) w[k / 2] |= (uint32_t)s[k] << (16 * (k & 1));
+        *reinterpret_cast<uint4 *>(j.dst + i * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
 // ------------------------------------------------------------------ host
 int check_shape(const a2sgd_attention *s)
 {
@@ -192,6 +704,146 @@ Heads heads_of(const a2sgd_heads *h)
     return h && h->p ? Heads{h->p, h->sequence_stride, h->row_stride, h->head_stride} : Heads{nullptr, 0, 0, 0};
 }
 
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// A tensor of heads with its extents; planes: 1 where all sequences lie in one, or read the same.
+struct Tensor {
+    Heads h;
+    int64_t rows;
+    int heads, d, planes;
+};
+inline int padded(int d) { return (d + 7) / 8 * 8; }
+inline uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
+inline uint64_t room(int64_t planes, int64_t rows, int heads, int d) { return up256((uint64_t)planes * rows * heads * padded(d) * 2); }
+
+Tensor tensor_of(const a2sgd_attention *s, const a2sgd_heads *h, bool keys)
+{
+    Tensor t;
+    t.h = heads_of(h);
+    t.rows = (int64_t)(keys ? s->k_rows : s->q_rows);
+    t.heads = (int)(keys ? s->kv_heads : s->q_heads);
+    t.d = (int)s->head_dim;
+    t.planes = t.h.seq == 0 ? 1 : (int)s->sequences;
+    return t;
+}
+bool tma_ok(const Tensor &t)
+{
+    const auto step = [](int64_t extent, int64_t stride) { return extent <= 1 || (stride > 0 && stride % 8 == 0); };
+    return aligned(t.h.p, 16) && step(t.rows, t.h.row) && step(t.heads, t.h.head) && step(t.planes, t.h.seq);
+}
+// Tiles of `box` rows and 64 elements of one head, 128 bytes a row, swizzled.
+bool make_map(CUtensorMap *map, const Tensor &t, int dtype, int box)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const auto step = [](int64_t extent, int64_t stride) { return (cuuint64_t)(extent > 1 ? stride : 8) * 2; }; // one: any stride is right
+    const cuuint64_t dims[4] = {(cuuint64_t)t.d, (cuuint64_t)t.rows, (cuuint64_t)t.heads, (cuuint64_t)t.planes};
+    const cuuint64_t strides[3] = {step(t.rows, t.h.row), step(t.heads, t.h.head), step(t.planes, t.h.seq)};
+    const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, steps[4] = {1, 1, 1, 1};
+    return encode(map, dtype == A2SGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.h.p, dims, strides,
+                  boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// 16-byte accesses to whole rows of heads
+bool wide(const Tensor &t) { return t.d % 8 == 0 && tma_ok(t); }
+
+struct Packer {
+    PackArgs args{};
+    int jobs = 0;
+    int64_t most = 0;
+    char *begin, *at;
+    explicit Packer(void *workspace) : begin(static_cast<char *>(workspace)), at(begin) {}
+    void *take(uint64_t bytes)
+    {
+        void *p = at;
+        at += up256(bytes);
+        return p;
+    }
+    // The tensor itself, or where its padded copy will be.
+    Tensor usable(const Tensor &t)
+    {
+        if (t.rows == 0 || tma_ok(t)) return t;
+        Tensor c = t;
+        const int p = padded(t.d);
+        c.h.head = p;
+        c.h.row = (int64_t)t.heads * p;
+        c.h.seq = t.planes > 1 ? t.rows * c.h.row : 0;
+        c.h.p = take(room(t.planes, t.rows, t.heads, t.d));
+        args.job[jobs++] = PackJob{t.h, static_cast<uint16_t *>(c.h.p), t.planes * t.rows, (int)t.rows, t.heads};
+        args.d = t.d, args.padded = p;
+        most = std::max(most, t.planes * t.rows * t.heads * (p / 8));
+        return c;
+    }
+    bool fits(uint64_t bytes) const { return at == begin || (begin && (uint64_t)(at - begin) <= bytes); }
+    int run(int sms, cudaStream_t s)
+    {
+        if (!jobs) return A2SGD_OK;
+        void *params[] = {&args};
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_pack_heads),
+                             dim3((unsigned)std::min<int64_t>((most + 255) / 256, (int64_t)sms * 16), (unsigned)jobs), 256, 0, params, s));
+        return A2SGD_OK;
+    }
+};
+
+template <typename T, int D, int TILES>
+int launch_forward(ForwardArgs &f, int64_t rows, cudaStream_t s)
+{
+    using Shape = ForwardShape<D, TILES>;
+    const int unit = 128 * TILES;
+    f.tiles = (int)(f.packed_q ? rows / unit + f.sequences : (rows + unit - 1) / unit);
+    const int64_t ctas = (int64_t)f.tiles * f.q_heads * (f.packed_q ? 1 : f.sequences);
+    if (ctas > 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
+    const void *fn = reinterpret_cast<const void *>(&k_forward<T, D, TILES>);
+    A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
+    void *params[] = {&f};
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)ctas), Shape::kThreads, Shape::kSmem, params, s));
+    return A2SGD_OK;
+}
+
+template <typename T>
+int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &o, float *lse, void *workspace,
+            uint64_t workspace_bytes, int sms, cudaStream_t s)
+{
+    Packer pack(workspace);
+    const Tensor pq = pack.usable(q), pk = pack.usable(k), pv = pack.usable(v);
+    if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
+    const int rc = pack.run(sms, s);
+    if (rc != A2SGD_OK) return rc;
+    ForwardArgs f{};
+    const int box = 128;
+    if (!make_map(&f.q, pq, shape->dtype, 128)) return A2SGD_ERR_CUDA;
+    if (k.rows && (!make_map(&f.k, pk, shape->dtype, box) || !make_map(&f.v, pv, shape->dtype, box))) return A2SGD_ERR_CUDA;
+    f.o = o.h;
+    f.lse = lse;
+    f.q_ranges = shape->q_ranges, f.k_ranges = shape->k_ranges;
+    f.q_heads = q.heads, f.group = q.heads / k.heads, f.d = q.d;
+    f.q_rows = (int)q.rows, f.k_rows = (int)k.rows;
+    f.window = (int)std::min<uint64_t>(shape->window, 1u << 30);
+    f.sinks = (int)std::min<uint64_t>(shape->sinks, 1u << 30);
+    f.packed_q = shape->q_ranges && q.h.seq == 0;
+    f.q_planes = pq.planes, f.k_planes = pk.planes, f.v_planes = pv.planes;
+    f.sequences = (int)shape->sequences;
+    f.wide_o = wide(o);
+    f.scale_log2 = (float)(shape->scale * 1.4426950408889634);
+    return q.d <= 64 ? launch_forward<T, 64, 1>(f, q.rows, s) : launch_forward<T, 128, 2>(f, q.rows, s);
+}
+
 Args common(const a2sgd_attention *s, const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *v, const a2sgd_heads *o)
 {
     Args a{};
@@ -205,15 +857,6 @@ Args common(const a2sgd_attention *s, const a2sgd_heads *q, const a2sgd_heads *k
     a.packed_q = s->q_ranges && q->sequence_stride == 0;
     a.scale = (float)s->scale;
     return a;
-}
-
-template <typename T>
-int forward(Args &a, cudaStream_t s)
-{
-    void *params[] = {&a};
-    A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_query<T, false>),
-                         dim3((unsigned)(a.q_rows + 3) / 4, (unsigned)a.q_heads, (unsigned)a.sequences), 128, 0, params, s));
-    return A2SGD_OK;
 }
 
 template <typename T>
@@ -233,8 +876,15 @@ int backward(Args &a, cudaStream_t s)
 
 extern "C" uint64_t a2sgd_window_attention_workspace(const a2sgd_attention *shape, uint32_t flags)
 {
-    if (!shape || !(flags & A2SGD_ATTENTION_BACKWARD)) return 0;
-    return (uint64_t)shape->sequences * shape->q_heads * shape->q_rows * 4;
+    if (!shape || shape->head_dim > A2SGD_ATTENTION_MAX_HEAD_DIM) return 0;
+    const int64_t q_planes = flags & A2SGD_ATTENTION_PACKED_Q ? 1 : shape->sequences, k_planes = flags & A2SGD_ATTENTION_PACKED_K ? 1 : shape->sequences;
+    const int d = (int)shape->head_dim;
+    uint64_t bytes = 0;
+    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4);
+    if (!(flags & A2SGD_ATTENTION_ALIGNED))
+        bytes += (flags & A2SGD_ATTENTION_BACKWARD ? 2 : 1) * room(q_planes, (int64_t)shape->q_rows, (int)shape->q_heads, d) +
+                 2 * room(k_planes, (int64_t)shape->k_rows, (int)shape->kv_heads, d);
+    return bytes;
 }
 
 extern "C" int a2sgd_window_attention_forward(const a2sgd_attention *shape, const a2sgd_heads *q, const a2sgd_heads *k,
@@ -249,13 +899,13 @@ extern "C" int a2sgd_window_attention_forward(const a2sgd_attention *shape, cons
         (rc = check_heads(shape, o, shape->q_heads, shape->q_rows, shape->q_ranges, true, true)) != A2SGD_OK)
         return rc;
     if (!aligned(workspace, 256) || !aligned(lse, 4)) return A2SGD_ERR_ALIGN;
-    (void)workspace_bytes;
     DeviceGuard guard(device);
-    if (!guard.ok) return A2SGD_ERR_CUDA;
-    Args a = common(shape, q, k, v, o);
-    a.lse = lse;
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms < 1) return A2SGD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return shape->dtype == A2SGD_BF16 ? forward<__nv_bfloat16>(a, s) : forward<__half>(a, s);
+    const Tensor tq = tensor_of(shape, q, false), tk = tensor_of(shape, k, true), tv = tensor_of(shape, v, true), to = tensor_of(shape, o, false);
+    return shape->dtype == A2SGD_BF16 ? forward<__nv_bfloat16>(shape, tq, tk, tv, to, lse, workspace, workspace_bytes, sms, s)
+                                      : forward<__half>(shape, tq, tk, tv, to, lse, workspace, workspace_bytes, sms, s);
 }
 
 extern "C" int a2sgd_window_attention_backward(const a2sgd_attention *shape, const a2sgd_heads *dout, const a2sgd_heads *q,
@@ -274,7 +924,8 @@ extern "C" int a2sgd_window_attention_backward(const a2sgd_attention *shape, con
     if ((rc = check_heads(shape, dq, shape->q_heads, shape->q_rows, shape->q_ranges, false, true)) != A2SGD_OK) return rc;
     if (!lse && shape->q_rows) return A2SGD_ERR_ARG;
     if (!aligned(workspace, 256) || !aligned(lse, 4)) return A2SGD_ERR_ALIGN;
-    if (workspace_bytes < a2sgd_window_attention_workspace(shape, A2SGD_ATTENTION_BACKWARD | A2SGD_ATTENTION_ALIGNED))
+    if (workspace_bytes < a2sgd_window_attention_workspace(shape, A2SGD_ATTENTION_BACKWARD | A2SGD_ATTENTION_ALIGNED |
+                                                                      (shape->q_ranges && q->sequence_stride == 0 ? A2SGD_ATTENTION_PACKED_Q : 0)))
         return A2SGD_ERR_ARG;
     DeviceGuard guard(device);
     if (!guard.ok) return A2SGD_ERR_CUDA;
@@ -291,7 +942,10 @@ extern "C" int a2sgd_window_attention_status(int device, int *device_status, voi
     if (!device_status) return A2SGD_ERR_ARG;
     DeviceGuard guard(device);
     if (!guard.ok) return A2SGD_ERR_CUDA;
-    A2_TRAIN_CUDA(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
-    *device_status = A2SGD_OK;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    unsigned int count = 0;
+    A2_TRAIN_CUDA(cudaMemcpyFromSymbolAsync(&count, g_waits_run_out, sizeof count, 0, cudaMemcpyDeviceToHost, s));
+    A2_TRAIN_CUDA(cudaStreamSynchronize(s));
+    *device_status = count_moved(device, s, count) ? A2SGD_ERR_TIMEOUT : A2SGD_OK;
     return A2SGD_OK;
 }
