@@ -198,6 +198,42 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ bool bar_try_cta(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return done != 0;
+}
+// bar_wait for a barrier that only this CTA's threads, copies and products arrive on.
+__device__ __forceinline__ bool bar_wait_cta(uint32_t bar, uint32_t parity, volatile int *gave_up)
+{
+    if (__all_sync(0xffffffffu, bar_try_cta(bar, parity))) return true;
+    const uint64_t begin = now_ns();
+    for (uint32_t polls = 1;; ++polls) {
+        if (__all_sync(0xffffffffu, bar_try_cta(bar, parity))) return true;
+        if ((polls & 255u) == 0u && __any_sync(0xffffffffu, *gave_up || now_ns() - begin > kWaitLimitNs)) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+}
+// Whether any of the 64 threads of two warps says yes; they meet at the CTA's barrier `id`.
+__device__ __forceinline__ bool pair_any(int id, bool yes)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\t"
+                 "barrier.cta.red.or.pred.aligned q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any)
+                 : "r"(id), "r"((uint32_t)yes)
+                 : "memory");
+    return any != 0;
+}
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(id) : "memory"); }
 // A tile of a tensor of four dimensions, its bytes counted on `bar`.
 __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
 {

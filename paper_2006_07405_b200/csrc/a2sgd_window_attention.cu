@@ -57,12 +57,12 @@ __device__ unsigned int g_waits_run_out = 0;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ forward
-// A CTA takes kTiles tiles of 128 queries of one head and walks the blocks of 128 keys that any of them sees: the first tokens' blocks, then
-// those of the window.  One warp brings tiles in by TMA, one issues the products, four warps a tile hold the softmax, a thread a query.
-//   S = Q K^T into TMEM;  the tile's threads read their rows, form P and write it to TMEM in 16 bits;  O += P V, P read from TMEM.
+// A CTA takes a tile of 128 queries of one head and walks the blocks of 64 keys that any of them sees: the first tokens' blocks, then those
+// of the window.  One warp brings tiles in by TMA, one issues the products, four hold the softmax, a thread a query.
+//   S = Q K^T into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  O += P V, P read from TMEM.
+// The next S that goes where P is, is issued behind P V: a CTA's products execute in the order of issue.
 // O stays in TMEM.  P is taken about a reference that follows the running maximum: it is moved, and O and the sum with it, only once the
 // maximum has risen by more than 2^8 above it, so that P stays below 2^8 and nearly no block touches O.
-// kEarly (P beside S): the next block's S is formed while the present one's P is; else P lies over S, and the next S is issued after P V.
 struct ForwardArgs {
     CUtensorMap q, k, v;
     Heads o;
@@ -75,16 +75,14 @@ struct ForwardArgs {
     float scale_log2;
 };
 
-template <int D, int TILES>
+constexpr int kBlock = 64; // keys
+template <int D>
 struct ForwardShape {
-    static constexpr bool kEarly = D == 64 && TILES == 1;
-    static constexpr int kThreads = 128 * (TILES + 1);
-    // registers a thread: 128 or 168 at launch, 200 or 208 for the softmax, whose threads hold a row of 128 scores, 56 or 88 for the rest
-    static constexpr int kMore = TILES == 1 ? 200 : 208, kFewer = TILES == 1 ? 56 : 88;
-    static constexpr uint32_t kTile = (D / 64) * 16384u; // 128 rows
-    static constexpr int kStages = TILES == 1 ? (D == 64 ? 5 : 2) : (D == 64 ? 8 : 5);
-    static constexpr uint32_t kSmem = TILES * kTile + kStages * kTile + 1024;
-    static constexpr uint32_t kColumns = TILES == 1 ? 256 : 512;
+    static constexpr int kBuffers = D == 64 ? 1 : 2; // of S
+    static constexpr int kThreads = 192, kCtas = D == 64 ? 4 : 2, kStages = 4;
+    static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u; // 128 rows, 64 rows
+    static constexpr uint32_t kSmem = kTile + kStages * kSlice + 1024;
+    static constexpr uint32_t kColumns = D == 64 ? 128 : 256, kO = kBuffers * 64;
 };
 
 // The sequence and the tile of `unit` rows that a CTA has among packed sequences; count 0: none.  One warp.
@@ -164,28 +162,61 @@ __device__ __forceinline__ void store_row(T *p, const float *v, int count, bool 
 template <typename T>
 __host__ __device__ constexpr uint32_t type_bits() { return std::is_same<T, __nv_bfloat16>::value ? 1u : 0u; }
 
-template <typename T, int D, int TILES>
-__global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ? 2 : 1) k_forward(const __grid_constant__ ForwardArgs a)
+// The largest of N numbers; those that are not numbers do not count.
+template <int N>
+__device__ __forceinline__ float most_of(const float *x)
 {
-    using Shape = ForwardShape<D, TILES>;
-    constexpr bool kEarly = Shape::kEarly;
-    constexpr int kStages = Shape::kStages, kChunks = D / 64;
-    constexpr uint32_t kTile = Shape::kTile;
+    float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int i = 4; i < N; i += 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (i + j + 4 < N) asm("max.f32 %0, %0, %1, %2;" : "+f"(top[j]) : "f"(x[i + j]), "f"(x[i + j + 4]));
+            else top[j] = fmaxf(top[j], x[i + j]);
+        }
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+__device__ __forceinline__ void hide(float (&x)[32], uint32_t seen)
+{
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = seen >> i & 1u ? x[i] : -INFINITY;
+}
+// 2^(x c + off), added to `sum` and packed in 16 bits.
+template <typename T>
+__device__ __forceinline__ void exponentials(const float (&x)[32], float c, float off, f32x2 &sum, uint32_t (&p)[16])
+{
+    const f32x2 c2 = pair(c), off2 = pair(off);
+    f32x2 sums[4] = {sum, pair(0.0f), pair(0.0f), pair(0.0f)};
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        float x0, x1;
+        unpair(fma2(pair(x[i], x[i + 1]), c2, off2), x0, x1);
+        x0 = exp2_approx(x0), x1 = exp2_approx(x1);
+        sums[i / 2 & 3] = add2(sums[i / 2 & 3], pair(x0, x1));
+        p[i / 2] = pack2(x0, x1, T());
+    }
+    sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kCtas) k_forward(const __grid_constant__ ForwardArgs a)
+{
+    using Shape = ForwardShape<D>;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers;
+    constexpr uint32_t kSlice = Shape::kSlice;
     extern __shared__ char smem_raw[];
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + TILES * kTile;
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 + 4 * TILES];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + Shape::kTile;
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kBuffers];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
     __shared__ int place_of[2];
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
     const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
-    const uint32_t q_full = bar0 + 8u * (2 * kStages), tail = bar0 + 8u * (2 * kStages + 1);
-    const auto s_full = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + t); };
-    const auto s_free = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + TILES + t); };
-    const auto p_full = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + 2 * TILES + t); };
-    const auto pv_done = [&](int t) { return bar0 + 8u * (2 * kStages + 2 + 3 * TILES + t); };
-    constexpr uint32_t kS = 0, kO = kEarly ? 192 : 128 * TILES; // columns; P: beside S, or over it
+    const uint32_t q_full = bar0 + 8u * (2 * kStages), tail = bar0 + 8u * (2 * kStages + 1), pv_done = bar0 + 8u * (2 * kStages + 2), o_full = bar0 + 8u * (2 * kStages + 3);
+    const auto s_full = [&](int i) { return bar0 + 8u * (2 * kStages + 4 + i); };
+    const auto p_full = [&](int i) { return bar0 + 8u * (2 * kStages + 4 + kBuffers + i); };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -195,23 +226,25 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
         }
         bar_init(q_full, 1);
         bar_init(tail, 1);
-        for (int t = 0; t < TILES; ++t) {
-            bar_init(s_full(t), 1);
-            bar_init(s_free(t), 4);
-            bar_init(p_full(t), 4);
-            bar_init(pv_done(t), 1);
+        bar_init(pv_done, 1);
+        bar_init(o_full, 1);
+        for (int i = 0; i < kBuffers; ++i) {
+            bar_init(s_full(i), 1);
+            bar_init(p_full(i), 4);
         }
         gave_up = 0;
         bar_init_fence();
     }
-    if (warp == 4 * TILES + 1) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
+    if (warp == 5) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
+    const int beyond = (int)threadIdx.x - 128;
+    if (beyond >= 0 && beyond < 3) tma_prefetch_map(beyond == 0 ? &a.q : beyond == 1 ? &a.k : &a.v); // parameters: no need to wait for the launch before
     wait_prior_grid();
     // the CTA's head, sequence and queries: the longest tiles of a sequence first
     int seq, tile, head;
     if (a.packed_q) {
         head = blockIdx.x / a.tiles;
         if (warp == 0) {
-            locate(a.q_ranges, a.sequences, a.q_rows, 128 * TILES, a.tiles - 1 - (int)(blockIdx.x % a.tiles), seq, tile);
+            locate(a.q_ranges, a.sequences, a.q_rows, 128, a.tiles - 1 - (int)(blockIdx.x % a.tiles), seq, tile);
             if (lane == 0) place_of[0] = seq, place_of[1] = tile;
         }
     } else {
@@ -227,217 +260,129 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
     if (a.packed_q) seq = place_of[0], tile = place_of[1];
     Range qr{0, 0}, kr{0, 0};
     if (seq >= 0) qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
-    const int i0 = tile * 128 * TILES, ahead = kr.count - qr.count;
-    const int rows = min(128 * TILES, qr.count - i0); // of this CTA
-    const int p0 = i0 + ahead;
-    const Blocks blocks(p0, rows > 0 ? p0 + rows - 1 : -1, a.window, a.sinks, 128);
-    const int steps = (a.d + 15) / 16; // of 16 elements of the head
-    // a tile's last query's place, below 0 where it sees nothing; and whether the tile sees a block
-    const auto last_place = [&](int t) { return 128 * t < rows ? p0 + min(rows, 128 * t + 128) - 1 : -1; };
-    const auto sees_block = [&](int t, int block) {
-        const int k0 = block * 128;
-        return k0 <= last_place(t) && (TILES == 1 || k0 + 127 > p0 + 128 * t - a.window || k0 < a.sinks);
-    };
+    const int i0 = tile * 128, p0 = i0 + kr.count - qr.count;
+    const int rows = min(128, qr.count - i0); // of this CTA
+    const Blocks blocks(p0, rows > 0 ? p0 + rows - 1 : -1, a.window, a.sinks, kBlock);
 
-    if (warp >= 4 * TILES) {
-    fewer_registers<Shape::kFewer>();
-    if (rows > 0 && warp == 4 * TILES) {
+    if (warp == 4) {
         // ---------------------------------------------------------- tiles in
         const bool chosen = elect_one();
         int stage = 0;
         uint32_t phase = 0, tails = 0;
         bool ok = true;
         if (blocks.count > 0 && chosen) {
-            bar_expect(q_full, TILES * kTile);
-            for (int t = 0; t < TILES; ++t)
-                for (int c = 0; c < kChunks; ++c)
-                    tma_load4(base + t * kTile + c * 16384u, &a.q, 64 * c, qr.first + i0 + 128 * t, head, a.q_planes > 1 ? seq : 0, q_full);
+            bar_expect(q_full, Shape::kTile);
+            for (int c = 0; c < kChunks; ++c) tma_load4(base + c * 16384u, &a.q, 64 * c, qr.first + i0, head, a.q_planes > 1 ? seq : 0, q_full);
         }
         const auto bring = [&](const CUtensorMap *map, int planes, int block, bool clear) {
-            ok = ok && bar_wait(empty(stage), phase ^ 1u, &gave_up);
+            ok = ok && bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
             if (!ok) return;
-            const uint32_t dst = ring + stage * kTile;
-            const int valid = kr.count - block * 128;
-            clear = clear && a.k_ranges && valid < 128;
+            const uint32_t dst = ring + stage * kSlice;
+            const int valid = kr.count - block * kBlock;
+            clear = clear && a.k_ranges && valid < kBlock;
             const uint32_t bar = clear ? tail : full(stage);
             if (chosen) {
-                bar_expect(bar, kTile);
+                bar_expect(bar, kSlice);
                 for (int c = 0; c < kChunks; ++c)
-                    tma_load4(dst + c * 16384u, map, 64 * c, kr.first + block * 128, head / a.group, planes > 1 ? seq : 0, bar);
+                    tma_load4(dst + c * 8192u, map, 64 * c, kr.first + block * kBlock, head / a.group, planes > 1 ? seq : 0, bar);
             }
             __syncwarp();
             if (clear) {
-                ok = bar_wait(tail, tails & 1u, &gave_up);
+                ok = bar_wait_cta(tail, tails & 1u, &gave_up);
                 ++tails;
                 if (!ok) return;
-                clear_rows(dst, kChunks, 128, valid);
+                clear_rows(dst, kChunks, kBlock, valid);
                 if (chosen) bar_arrive(full(stage));
                 __syncwarp();
             }
             if (++stage == kStages) stage = 0, phase ^= 1u;
         };
-        if (blocks.count > 0) bring(&a.k, a.k_planes, blocks[0], false);
+        for (int n = 0; ok && n < min(kBuffers, blocks.count); ++n) bring(&a.k, a.k_planes, blocks[n], false);
         for (int n = 0; ok && n < blocks.count; ++n) {
-            if (kEarly && n + 1 < blocks.count) bring(&a.k, a.k_planes, blocks[n + 1], false);
             bring(&a.v, a.v_planes, blocks[n], true);
-            if (!kEarly && n + 1 < blocks.count) bring(&a.k, a.k_planes, blocks[n + 1], false);
+            if (n + kBuffers < blocks.count) bring(&a.k, a.k_planes, blocks[n + kBuffers], false);
         }
         // every tile has been consumed: nothing is in flight towards this CTA any more
         for (int s = 0; ok && s < kStages; ++s) {
-            ok = bar_wait(empty(stage), phase ^ 1u, &gave_up);
+            ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
             if (++stage == kStages) stage = 0, phase ^= 1u;
         }
-    } else if (rows > 0 && warp == 4 * TILES + 1) {
+    } else if (warp == 5) {
         // ---------------------------------------------------------- products
         const bool chosen = elect_one();
-        const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, 128);
+        const int steps = (a.d + 15) / 16; // of 16 elements of the head
+        const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
         const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
         int stage = 0;
         uint32_t phase = 0;
-        int done[TILES] = {};
-        bool ok = blocks.count > 0 && bar_wait(q_full, 0, &gave_up);
-        const auto next = [&] {
-            if (++stage == kStages) stage = 0, phase ^= 1u;
-        };
-        const auto form_s = [&](int t, uint32_t k) { // one thread
-            const uint64_t dq = operand_desc(base + t * kTile, 16), dk = operand_desc(k, 16);
-            for (int j = 0; j < steps; ++j) { // 64 elements a chunk of 16 KB
-                const uint32_t off = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4;
-                mma_ss(tmem + kS + 128 * t, dq + off, dk + off, desc_s, j > 0);
-            }
-            commit(s_full(t));
-        };
-        const auto add_pv = [&](int t, uint32_t v, bool first) { // one thread
-            const uint64_t dv = operand_desc(v, 16384);
-            const uint32_t p = tmem + (kEarly ? 128 : 128 * t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) mma_ts(tmem + kO + D * t, p + 8 * j, dv + j * (2048 >> 4), desc_o, !first || j > 0);
-        };
-        if (ok) ok = bar_wait(full(stage), phase, &gave_up);
-        if (ok) {
+        bool ok = blocks.count > 0 && bar_wait_cta(q_full, 0, &gave_up);
+        const auto form_s = [&](int n) {
+            ok = ok && bar_wait_cta(full(stage), phase, &gave_up);
+            if (!ok) return;
             fence_after();
             if (chosen) {
-                for (int t = 0; t < TILES; ++t)
-                    if (sees_block(t, blocks[0])) form_s(t, ring + stage * kTile);
+                const uint64_t dq = operand_desc(base, 16), dk = operand_desc(ring + stage * kSlice, 16);
+                for (int j = 0; j < steps; ++j) // 64 elements a chunk
+                    mma_ss(tmem + 64 * (n % kBuffers), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc_s, j > 0);
                 commit(empty(stage));
+                commit(s_full(n % kBuffers));
             }
             __syncwarp();
-            next();
-        }
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+        };
+        for (int n = 0; ok && n < min(kBuffers, blocks.count); ++n) form_s(n);
         for (int n = 0; ok && n < blocks.count; ++n) {
-            const bool more = n + 1 < blocks.count;
-            if constexpr (kEarly) {
-                if (more) {
-                    ok = bar_wait(full(stage), phase, &gave_up) && bar_wait(s_free(0), n & 1, &gave_up);
-                    if (!ok) break;
-                    fence_after();
-                    if (chosen) {
-                        form_s(0, ring + stage * kTile);
-                        commit(empty(stage));
-                    }
-                    __syncwarp();
-                    next();
-                }
-                ok = bar_wait(full(stage), phase, &gave_up) && bar_wait(p_full(0), n & 1, &gave_up);
-                if (!ok) break;
-                fence_after();
-                if (chosen) {
-                    add_pv(0, ring + stage * kTile, n == 0);
-                    commit(empty(stage));
-                    commit(pv_done(0));
-                }
-                __syncwarp();
-                next();
-            } else {
-                ok = bar_wait(full(stage), phase, &gave_up);
-                if (!ok) break;
-                const uint32_t v = ring + stage * kTile, v_empty = empty(stage);
-                next();
-                const uint32_t k = ring + stage * kTile, k_empty = empty(stage);
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    if (sees_block(t, blocks[n])) {
-                        ok = bar_wait(p_full(t), done[t] & 1, &gave_up);
-                        if (!ok) break;
-                        fence_after();
-                        if (chosen) {
-                            add_pv(t, v, done[t] == 0);
-                            if (blocks[n] == last_place(t) / 128) commit(pv_done(t));
-                        }
-                        ++done[t];
-                    }
-                    if (t == TILES - 1 && chosen) commit(v_empty);
-                    __syncwarp();
-                    if (more) {
-                        if (t == 0) ok = bar_wait(full(stage), phase, &gave_up);
-                        if (!ok) break;
-                        fence_after();
-                        if (chosen) {
-                            if (sees_block(t, blocks[n + 1])) form_s(t, k); // behind P V in the order of issue, which reads P where S goes
-                            if (t == TILES - 1) commit(k_empty);
-                        }
-                        __syncwarp();
-                    }
-                }
-                if (more) next();
-            }
-        }
-    }
-    } else {
-        more_registers<Shape::kMore>();
-        if (rows > 0) {
-        // ---------------------------------------------------------- softmax, a thread a query
-        const int t = TILES == 1 ? 0 : warp >> 2, quarter = warp & 3;
-        const int row = 128 * t + quarter * 32 + lane, place = p0 + row;
-        const int w0 = p0 + 128 * t + quarter * 32, w1 = w0 + 31; // the warp's places
-        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t ts = lanes + kS + 128 * t, tp = kEarly ? lanes + 128 : ts, to = lanes + kO + D * t;
-        const float c = a.scale_log2;
-        float ref = -INFINITY, total = 0.0f;
-        int done = 0;
-        bool ok = true;
-        for (int n = 0; n < blocks.count; ++n) {
-            const int k0 = blocks[n] * 128;
-            if (!sees_block(t, blocks[n])) continue;
-            ok = bar_wait(s_full(t), done & 1, &gave_up);
+            ok = bar_wait_cta(full(stage), phase, &gave_up) && bar_wait_cta(p_full(n % kBuffers), n / kBuffers & 1, &gave_up);
             if (!ok) break;
             fence_after();
-            // groups of 32 keys that some row of the warp sees, and those that every row does
-            bool some[4], all[4];
+            if (chosen) {
+                const uint64_t dv = operand_desc(ring + stage * kSlice, 8192);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int g0 = k0 + 32 * e, g1 = g0 + 31;
-                some[e] = g0 <= w1 && (g1 > w0 - a.window || g0 < a.sinks);
-                all[e] = g1 <= w0 && (g0 > w1 - a.window || g1 < a.sinks);
+                for (int j = 0; j < kBlock / 16; ++j)
+                    mma_ts(tmem + Shape::kO, tmem + 64 * (n % kBuffers) + 8 * j, dv + j * (2048 >> 4), desc_o, n > 0 || j > 0);
+                commit(empty(stage));
+                commit(pv_done);
+                if (n + 1 == blocks.count) commit(o_full);
             }
-            float s[128];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (some[e]) tmem_ld32(ts + 32 * e, reinterpret_cast<float(&)[32]>(s[32 * e]));
-            tmem_wait_ld();
-            if (kEarly) {
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(s_free(t));
+            __syncwarp();
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+            if (n + kBuffers < blocks.count) {
+                ok = bar_wait_cta(pv_done, n & 1, &gave_up);
+                form_s(n + kBuffers);
             }
-            float top0 = -INFINITY, top1 = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (!some[e]) continue;
-                float(&x)[32] = reinterpret_cast<float(&)[32]>(s[32 * e]);
-                if (!all[e]) {
-                    const int g0 = k0 + 32 * e;
-                    const uint32_t seen = below(place + 1 - g0) & (~below(place - a.window + 1 - g0) | below(a.sinks - g0));
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] = seen >> i & 1u ? x[i] : -INFINITY;
-                }
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    top0 = fmaxf(top0, x[i]);
-                    top1 = fmaxf(top1, x[i + 1]);
-                }
+        }
+    } else if (rows > 0) {
+        // ---------------------------------------------------------- softmax, a thread a query
+        const int row = warp * 32 + lane, place = p0 + row;
+        const int w0 = p0 + warp * 32, w1 = w0 + 31; // the warp's places
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16), to = lanes + Shape::kO;
+        const float c = a.scale_log2;
+        float ref = -INFINITY, total = 0.0f;
+        bool ok = true;
+        const auto some_seen = [&](int g0) { return g0 <= w1 && (g0 + 31 > w0 - a.window || g0 < a.sinks); }; // of 32 keys, by the warp
+        const auto seen_by = [&](int g0) { return below(place + 1 - g0) & (~below(place - a.window + 1 - g0) | below(a.sinks - g0)); };
+        for (int n = 0; n < blocks.count; ++n) {
+            const int k0 = blocks[n] * kBlock;
+            const uint32_t ts = lanes + 64 * (n % kBuffers); // S, and P over it
+            ok = bar_wait_cta(s_full(n % kBuffers), n / kBuffers & 1, &gave_up);
+            if (!ok) break;
+            fence_after();
+            const bool inside = k0 + 63 <= w0 && (k0 > w1 - a.window || k0 + 63 < a.sinks); // every row sees all 64
+            const bool first = inside || some_seen(k0), second = inside || some_seen(k0 + 32);
+            // 32 keys at a time; the second 32 are read for the maximum, and again for P: four CTAs an SM leave 80 registers
+            float x[32], top = -INFINITY;
+            if (second) {
+                tmem_ld32(ts + 32, x);
+                tmem_wait_ld();
+                if (!inside) hide(x, seen_by(k0 + 32));
+                top = most_of<32>(x);
             }
-            const float top = fmaxf(top0, top1);
+            if (first) {
+                tmem_ld32(ts, x);
+                tmem_wait_ld();
+                if (!inside) hide(x, seen_by(k0));
+                top = fmaxf(top, most_of<32>(x));
+            }
             const bool moves = top > ref && (top - ref) * c > 8.0f; // from -infinity, too
             float shrink = 1.0f;
             if (moves) {
@@ -445,14 +390,12 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
                 ref = top;
                 total *= shrink;
             }
-            const float off = ref == -INFINITY ? 0.0f : -ref * c;
-            const f32x2 c2 = pair(c), off2 = pair(off);
-            if (kEarly && done > 0) { // the product before has read P, and O is at rest
-                ok = bar_wait(pv_done(t), (done - 1) & 1, &gave_up);
-                if (!ok) break;
-                fence_after();
-            }
-            if (done > 0 && __any_sync(0xffffffffu, moves)) {
+            if (n > 0 && __any_sync(0xffffffffu, moves)) {
+                if (kBuffers > 1) { // O is at rest
+                    ok = bar_wait_cta(pv_done, (n - 1) & 1, &gave_up);
+                    if (!ok) break;
+                    fence_after();
+                }
 #pragma unroll 1
                 for (int e = 0; 16 * e < a.d; ++e) {
                     uint32_t r[16];
@@ -463,37 +406,29 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
                     tmem_st16(to + 16 * e, r);
                 }
             }
-            f32x2 sum0 = pair(0.0f), sum1 = pair(0.0f);
+            const float off = ref == -INFINITY ? 0.0f : -ref * c;
+            f32x2 sum = pair(0.0f);
+            uint32_t p[16] = {};
+            if (first) exponentials<T>(x, c, off, sum, p);
+            tmem_st16(ts, p);
+            if (second) {
+                tmem_ld32(ts + 32, x);
+                tmem_wait_ld();
+                if (!inside) hide(x, seen_by(k0 + 32));
+                exponentials<T>(x, c, off, sum, p);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t p[16];
-                if (some[e]) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        float x0, x1, x2, x3;
-                        unpair(fma2(pair(s[32 * e + i], s[32 * e + i + 1]), c2, off2), x0, x1);
-                        unpair(fma2(pair(s[32 * e + i + 2], s[32 * e + i + 3]), c2, off2), x2, x3);
-                        x0 = exp2_approx(x0), x1 = exp2_approx(x1), x2 = exp2_approx(x2), x3 = exp2_approx(x3);
-                        sum0 = add2(sum0, pair(x0, x1));
-                        sum1 = add2(sum1, pair(x2, x3));
-                        p[i / 2] = pack2(x0, x1, T());
-                        p[i / 2 + 1] = pack2(x2, x3, T());
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) p[i] = 0;
-                }
-                tmem_st16(tp + 16 * e, p);
+                for (int i = 0; i < 16; ++i) p[i] = 0;
             }
-            total += sum2(add2(sum0, sum1));
+            tmem_st16(ts + 16, p);
+            total += sum2(sum);
             tmem_wait_st();
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(p_full(t));
-            ++done;
+            if (lane == 0) bar_arrive(p_full(n % kBuffers));
         }
-        if (ok && done > 0) {
-            ok = bar_wait(pv_done(t), kEarly ? (done - 1) & 1 : 0, &gave_up);
+        if (ok && blocks.count > 0) {
+            ok = bar_wait_cta(o_full, 0, &gave_up);
             fence_after();
         }
         if (ok) {
@@ -504,7 +439,7 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
 #pragma unroll 1
             for (int e = 0; 32 * e < a.d; ++e) {
                 float o[32];
-                if (done > 0) {
+                if (blocks.count > 0) {
                     tmem_ld32(to + 32 * e, o);
                     tmem_wait_ld();
                 }
@@ -516,7 +451,6 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
                 a.lse[((int64_t)(a.packed_q ? 0 : seq) * a.q_heads + head) * a.q_rows + out_row] =
                     total > 0.0f ? ref * (c * kLn2) + logf(total) : total != total ? total : -INFINITY;
         }
-        }
     }
     __syncwarp();
     __syncthreads();
@@ -526,7 +460,7 @@ __global__ void __launch_bounds__(ForwardShape<D, TILES>::kThreads, TILES == 1 ?
         const uint64_t begin = now_ns();
         while (now_ns() - begin < 5000000ull) __nanosleep(1000);
     }
-    if (warp == 4 * TILES + 1) tmem_free(tmem, Shape::kColumns);
+    if (warp == 5) tmem_free(tmem, Shape::kColumns);
 }
 
 // A warp a query: 32 keys at a time, a lane each, then the lanes share out the head's elements.
@@ -801,15 +735,14 @@ struct Packer {
     }
 };
 
-template <typename T, int D, int TILES>
+template <typename T, int D>
 int launch_forward(ForwardArgs &f, int64_t rows, cudaStream_t s)
 {
-    using Shape = ForwardShape<D, TILES>;
-    const int unit = 128 * TILES;
-    f.tiles = (int)(f.packed_q ? rows / unit + f.sequences : (rows + unit - 1) / unit);
+    using Shape = ForwardShape<D>;
+    f.tiles = (int)(f.packed_q ? rows / 128 + f.sequences : (rows + 127) / 128);
     const int64_t ctas = (int64_t)f.tiles * f.q_heads * (f.packed_q ? 1 : f.sequences);
     if (ctas > 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
-    const void *fn = reinterpret_cast<const void *>(&k_forward<T, D, TILES>);
+    const void *fn = reinterpret_cast<const void *>(&k_forward<T, D>);
     A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
     void *params[] = {&f};
     A2_TRAIN_CUDA(launch(fn, dim3((unsigned)ctas), Shape::kThreads, Shape::kSmem, params, s));
@@ -826,9 +759,8 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     const int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
     ForwardArgs f{};
-    const int box = 128;
     if (!make_map(&f.q, pq, shape->dtype, 128)) return A2SGD_ERR_CUDA;
-    if (k.rows && (!make_map(&f.k, pk, shape->dtype, box) || !make_map(&f.v, pv, shape->dtype, box))) return A2SGD_ERR_CUDA;
+    if (k.rows && (!make_map(&f.k, pk, shape->dtype, kBlock) || !make_map(&f.v, pv, shape->dtype, kBlock))) return A2SGD_ERR_CUDA;
     f.o = o.h;
     f.lse = lse;
     f.q_ranges = shape->q_ranges, f.k_ranges = shape->k_ranges;
@@ -841,7 +773,7 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     f.sequences = (int)shape->sequences;
     f.wide_o = wide(o);
     f.scale_log2 = (float)(shape->scale * 1.4426950408889634);
-    return q.d <= 64 ? launch_forward<T, 64, 1>(f, q.rows, s) : launch_forward<T, 128, 2>(f, q.rows, s);
+    return q.d <= 64 ? launch_forward<T, 64>(f, q.rows, s) : launch_forward<T, 128>(f, q.rows, s);
 }
 
 Args common(const a2sgd_attention *s, const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *v, const a2sgd_heads *o)
