@@ -222,18 +222,21 @@ __device__ __forceinline__ bool bar_wait_cta(uint32_t bar, uint32_t parity, vola
         }
     }
 }
-// Whether any of the 64 threads of two warps says yes; they meet at the CTA's barrier `id`.
-__device__ __forceinline__ bool pair_any(int id, bool yes)
+// The same without an answer, for warps that go on either way: after a wait that ran out, what they compute is given up, and their later
+// waits end at once.  No vote: each lane waits for itself, and they meet again behind it.
+__device__ __forceinline__ void bar_pass_cta(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
-    uint32_t any;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\t"
-                 "barrier.cta.red.or.pred.aligned q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(any)
-                 : "r"(id), "r"((uint32_t)yes)
-                 : "memory");
-    return any != 0;
+    if (!bar_try_cta(bar, parity)) {
+        const uint64_t begin = now_ns();
+        for (uint32_t polls = 1; !bar_try_cta(bar, parity); ++polls) {
+            if ((polls & 63u) == 0u && (*gave_up || now_ns() - begin > kWaitLimitNs)) {
+                *gave_up = 1;
+                break;
+            }
+        }
+    }
+    __syncwarp();
 }
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(id) : "memory"); }
 // A tile of a tensor of four dimensions, its bytes counted on `bar`.
 __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
 {

@@ -57,12 +57,13 @@ __device__ unsigned int g_waits_run_out = 0;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ forward
-// A CTA takes a tile of 128 queries of one head and walks the blocks of 64 keys that any of them sees: the first tokens' blocks, then those
-// of the window.  One warp brings tiles in by TMA, one issues the products, four hold the softmax, a thread a query.
+// Persistent CTAs, two an SM, deal out the tiles of 128 queries of one head, the longest first.  For each tile a CTA walks the blocks of 64
+// keys that any of its queries sees: the first tokens' blocks, then those of the window.  One warp brings tiles in by TMA, one issues the
+// products, four hold the softmax, a thread a query.
 //   S = Q K^T into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  O += P V, P read from TMEM.
-// The next S that goes where P is, is issued behind P V: a CTA's products execute in the order of issue.
-// O stays in TMEM.  P is taken about a reference that follows the running maximum: it is moved, and O and the sum with it, only once the
-// maximum has risen by more than 2^8 above it, so that P stays below 2^8 and nearly no block touches O.
+// Two buffers of S: the next block's, be it the next tile's, is formed while the present one's P is.
+// P is taken about a reference that is moved, and O and the sum with it, only where P would grow beyond 2^13: nearly no
+// block touches O, and blocks without a mask need no maximum.
 struct ForwardArgs {
     CUtensorMap q, k, v;
     Heads o;
@@ -71,6 +72,7 @@ struct ForwardArgs {
     int q_heads, group, d, q_rows, k_rows, window, sinks;
     int packed_q, q_planes, k_planes, v_planes; // planes: more than one: by sequence
     int sequences, tiles;                       // tiles of a sequence, or of all packed ones
+    int items, lanes, together;                 // tiles of all heads; heads, times sequences that are not packed; of them at a time
     int wide_o;                                 // 16-byte stores
     float scale_log2;
 };
@@ -78,11 +80,10 @@ struct ForwardArgs {
 constexpr int kBlock = 64; // keys
 template <int D>
 struct ForwardShape {
-    static constexpr int kBuffers = D == 64 ? 1 : 2; // of S
-    static constexpr int kThreads = 192, kCtas = D == 64 ? 4 : 2, kStages = 4;
+    static constexpr int kThreads = 192, kCtas = 2, kStages = D == 64 ? 8 : 4;
     static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u; // 128 rows, 64 rows
     static constexpr uint32_t kSmem = kTile + kStages * kSlice + 1024;
-    static constexpr uint32_t kColumns = D == 64 ? 128 : 256, kO = kBuffers * 64;
+    static constexpr uint32_t kColumns = 256, kO = 128;
 };
 
 // The sequence and the tile of `unit` rows that a CTA has among packed sequences; count 0: none.  One warp.
@@ -113,6 +114,7 @@ __device__ __forceinline__ void locate(const int32_t *ranges, int sequences, int
 // The blocks of keys that a run of queries at places p0 to p1 (its last) sees, in order: sink_blocks first ones, then from first_block on.
 struct Blocks {
     int sink_blocks, first_block, count;
+    Blocks() = default;
     __device__ __forceinline__ Blocks(int p0, int p1, int window, int sinks, int block)
     {
         const int end = p1 < 0 ? 0 : p1 / block + 1, lo = max(0, p0 - window + 1);
@@ -182,12 +184,12 @@ __device__ __forceinline__ void hide(float (&x)[32], uint32_t seen)
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = seen >> i & 1u ? x[i] : -INFINITY;
 }
-// 2^(x c + off), added to `sum` and packed in 16 bits.
+// 2^(x c + off) packed in 16 bits; returns their sum.
 template <typename T>
-__device__ __forceinline__ void exponentials(const float (&x)[32], float c, float off, f32x2 &sum, uint32_t (&p)[16])
+__device__ __forceinline__ float exponentials(const float (&x)[32], float c, float off, uint32_t (&p)[16])
 {
     const f32x2 c2 = pair(c), off2 = pair(off);
-    f32x2 sums[4] = {sum, pair(0.0f), pair(0.0f), pair(0.0f)};
+    f32x2 sums[4] = {};
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
         float x0, x1;
@@ -196,95 +198,107 @@ __device__ __forceinline__ void exponentials(const float (&x)[32], float c, floa
         sums[i / 2 & 3] = add2(sums[i / 2 & 3], pair(x0, x1));
         p[i / 2] = pack2(x0, x1, T());
     }
-    sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
+    return sum2(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])));
+}
+
+// A tile: whose it is, its queries and the blocks of keys that they see.  The loading warp works them out and leaves them in shared memory.
+struct Tile {
+    int seq, head, p0, rows;     // place of the first query; queries, at least 1
+    int q_row, k_row, k_count;   // rows of the plane, keys
+    Blocks blocks;
+};
+constexpr int kTiles = 4; // kept in shared memory, in turn
+// The whole warp (packed sequences are searched through by its lanes).  False where there are no queries.
+__device__ __forceinline__ bool find_tile(const ForwardArgs &a, int item, Tile &t)
+{
+    const int part = item / (a.together * a.tiles), rest = item - part * a.together * a.tiles;
+    const int wide = min(a.together, a.lanes - part * a.together), lane = part * a.together + rest % wide;
+    int tile = a.tiles - 1 - rest / wide;
+    t.head = lane % a.q_heads;
+    if (a.packed_q) {
+        locate(a.q_ranges, a.sequences, a.q_rows, 128, tile, t.seq, tile);
+        if (t.seq < 0) return false;
+    } else {
+        t.seq = lane / a.q_heads;
+    }
+    const Range qr = range_of(a.q_ranges, t.seq, a.q_rows), kr = range_of(a.k_ranges, t.seq, a.k_rows);
+    t.rows = min(128, qr.count - tile * 128);
+    if (t.rows <= 0) return false;
+    t.p0 = tile * 128 + kr.count - qr.count;
+    t.q_row = qr.first + tile * 128;
+    t.k_row = kr.first;
+    t.k_count = kr.count;
+    t.blocks = Blocks(t.p0, t.p0 + t.rows - 1, a.window, a.sinks, kBlock);
+    return true;
+}
+__device__ __forceinline__ int64_t lse_of(const ForwardArgs &a, const Tile &t, int row)
+{
+    return ((int64_t)(a.packed_q ? 0 : t.seq) * a.q_heads + t.head) * a.q_rows + t.q_row + row;
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kCtas) k_forward(const __grid_constant__ ForwardArgs a)
 {
     using Shape = ForwardShape<D>;
-    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64;
     constexpr uint32_t kSlice = Shape::kSlice;
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + Shape::kTile;
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 * kBuffers];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 10];
+    __shared__ Tile tiles[kTiles];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
-    __shared__ int place_of[2];
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
     const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
-    const uint32_t q_full = bar0 + 8u * (2 * kStages), tail = bar0 + 8u * (2 * kStages + 1), pv_done = bar0 + 8u * (2 * kStages + 2), o_full = bar0 + 8u * (2 * kStages + 3);
-    const auto s_full = [&](int i) { return bar0 + 8u * (2 * kStages + 4 + i); };
-    const auto p_full = [&](int i) { return bar0 + 8u * (2 * kStages + 4 + kBuffers + i); };
+    const uint32_t tile0 = bar0 + 16u * kStages, more0 = tile0 + 16u * kTiles;
+    const auto tile_full = [&](int t) { return tile0 + 8u * (t % kTiles); };
+    const auto tile_empty = [&](int t) { return tile0 + 8u * (kTiles + t % kTiles); };
+    const uint32_t q_full = more0, q_empty = more0 + 8, tail = more0 + 16, pv_done = more0 + 24, o_full = more0 + 32, o_empty = more0 + 40;
+    const auto s_full = [&](int g) { return more0 + 48 + 8u * (g & 1); };
+    const auto p_full = [&](int g) { return more0 + 64 + 8u * (g & 1); };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            bar_init(full(s), 1);
-            bar_init(empty(s), 1);
+        for (int s = 0; s < 2 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
+        for (int t = 0; t < kTiles; ++t) {
+            bar_init(tile_full(t), 1);
+            bar_init(tile_empty(t), 5);
         }
-        bar_init(q_full, 1);
-        bar_init(tail, 1);
-        bar_init(pv_done, 1);
-        bar_init(o_full, 1);
-        for (int i = 0; i < kBuffers; ++i) {
-            bar_init(s_full(i), 1);
-            bar_init(p_full(i), 4);
-        }
+        for (uint32_t b : {q_full, q_empty, tail, pv_done, o_full, s_full(0), s_full(1)}) bar_init(b, 1);
+        for (uint32_t b : {o_empty, p_full(0), p_full(1)}) bar_init(b, 4);
         gave_up = 0;
         bar_init_fence();
     }
     if (warp == 5) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
     const int beyond = (int)threadIdx.x - 128;
     if (beyond >= 0 && beyond < 3) tma_prefetch_map(beyond == 0 ? &a.q : beyond == 1 ? &a.k : &a.v); // parameters: no need to wait for the launch before
-    wait_prior_grid();
-    // the CTA's head, sequence and queries: the longest tiles of a sequence first
-    int seq, tile, head;
-    if (a.packed_q) {
-        head = blockIdx.x / a.tiles;
-        if (warp == 0) {
-            locate(a.q_ranges, a.sequences, a.q_rows, 128, a.tiles - 1 - (int)(blockIdx.x % a.tiles), seq, tile);
-            if (lane == 0) place_of[0] = seq, place_of[1] = tile;
-        }
-    } else {
-        tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);
-        head = blockIdx.x / a.tiles % a.q_heads;
-        seq = blockIdx.x / a.tiles / a.q_heads;
-    }
     fence_before();
     __syncthreads();
     fence_after();
-    release_next_grid(); // not before this CTA has its TMEM: the next kernel's CTAs may want some, and wait for this one's end
     const uint32_t tmem = tmem_at;
-    if (a.packed_q) seq = place_of[0], tile = place_of[1];
-    Range qr{0, 0}, kr{0, 0};
-    if (seq >= 0) qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
-    const int i0 = tile * 128, p0 = i0 + kr.count - qr.count;
-    const int rows = min(128, qr.count - i0); // of this CTA
-    const Blocks blocks(p0, rows > 0 ? p0 + rows - 1 : -1, a.window, a.sinks, kBlock);
+    wait_prior_grid();
+    release_next_grid(); // not before this CTA has its TMEM: the next kernel's CTAs may want some, and wait for this one's end
 
     if (warp == 4) {
-        // ---------------------------------------------------------- tiles in
+        // ---------------------------------------------------------- tiles in: keys two blocks ahead of values
         const bool chosen = elect_one();
-        int stage = 0;
+        int stage = 0, item = blockIdx.x - gridDim.x, kt = -1, vt = -1; // tiles begun
         uint32_t phase = 0, tails = 0;
         bool ok = true;
-        if (blocks.count > 0 && chosen) {
-            bar_expect(q_full, Shape::kTile);
-            for (int c = 0; c < kChunks; ++c) tma_load4(base + c * 16384u, &a.q, 64 * c, qr.first + i0, head, a.q_planes > 1 ? seq : 0, q_full);
-        }
-        const auto bring = [&](const CUtensorMap *map, int planes, int block, bool clear) {
+        Tile k, v;
+        int kn = 0, vn = 0;
+        k.blocks.count = v.blocks.count = 0;
+        const auto bring = [&](const CUtensorMap *map, int planes, const Tile &t, int n, bool clear) {
             ok = ok && bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
             if (!ok) return;
             const uint32_t dst = ring + stage * kSlice;
-            const int valid = kr.count - block * kBlock;
+            const int block = t.blocks[n], valid = t.k_count - block * kBlock;
             clear = clear && a.k_ranges && valid < kBlock;
             const uint32_t bar = clear ? tail : full(stage);
             if (chosen) {
                 bar_expect(bar, kSlice);
-                for (int c = 0; c < kChunks; ++c)
-                    tma_load4(dst + c * 8192u, map, 64 * c, kr.first + block * kBlock, head / a.group, planes > 1 ? seq : 0, bar);
+                for (int c = 0; c < kChunks; ++c) tma_load4(dst + c * 8192u, map, 64 * c, t.k_row + block * kBlock, t.head / a.group, planes > 1 ? t.seq : 0, bar);
             }
             __syncwarp();
             if (clear) {
@@ -297,10 +311,54 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             }
             if (++stage == kStages) stage = 0, phase ^= 1u;
         };
-        for (int n = 0; ok && n < min(kBuffers, blocks.count); ++n) bring(&a.k, a.k_planes, blocks[n], false);
-        for (int n = 0; ok && n < blocks.count; ++n) {
-            bring(&a.v, a.v_planes, blocks[n], true);
-            if (n + kBuffers < blocks.count) bring(&a.k, a.k_planes, blocks[n + kBuffers], false);
+        // a block of keys, with the tile and its queries where it is the first; false at the end
+        const auto bring_k = [&] {
+            if (kn == k.blocks.count) {
+                for (;;) {
+                    item += gridDim.x;
+                    if (item >= a.items) k.rows = 0, k.blocks.count = 0;
+                    else if (!find_tile(a, item, k)) continue;
+                    if (k.rows == 0 || k.blocks.count > 0) break;
+                    for (int r = 0; r < k.rows; ++r) { // queries that see nothing
+                        T *o = at<T>(a.o, k.seq, k.q_row + r, k.head);
+                        for (int c = lane; c < a.d; c += 32) o[c] = from_f32<T>(0.0f);
+                        if (a.lse && lane == 0) a.lse[lse_of(a, k, r)] = -INFINITY;
+                    }
+                }
+                ++kt;
+                kn = 0;
+                ok = ok && bar_wait_cta(tile_empty(kt), (kt / kTiles & 1) ^ 1, &gave_up);
+                if (!ok) return false;
+                if (lane == 0) tiles[kt % kTiles] = k;
+                __syncwarp();
+                if (chosen) bar_arrive(tile_full(kt));
+                __syncwarp();
+                if (k.rows == 0) {
+                    item = a.items; // the end, from now on
+                    return false;
+                }
+                ok = bar_wait_cta(q_empty, (kt & 1) ^ 1, &gave_up); // the last tile's queries have been read
+                if (ok && chosen) {
+                    bar_expect(q_full, Shape::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load4(base + c * 16384u, &a.q, 64 * c, k.q_row, k.head, a.q_planes > 1 ? k.seq : 0, q_full);
+                }
+                __syncwarp();
+            }
+            bring(&a.k, a.k_planes, k, kn, false);
+            ++kn;
+            return true;
+        };
+        bool keys = bring_k() && bring_k();
+        for (;;) {
+            if (vn == v.blocks.count) {
+                if (vt == kt || !ok) break;
+                v = tiles[++vt % kTiles];
+                vn = 0;
+                if (v.rows == 0) break;
+            }
+            bring(&a.v, a.v_planes, v, vn, true);
+            ++vn;
+            keys = keys && ok && bring_k();
         }
         // every tile has been consumed: nothing is in flight towards this CTA any more
         for (int s = 0; ok && s < kStages; ++s) {
@@ -308,148 +366,190 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             if (++stage == kStages) stage = 0, phase ^= 1u;
         }
     } else if (warp == 5) {
-        // ---------------------------------------------------------- products
+        // ---------------------------------------------------------- products: scores two blocks ahead
         const bool chosen = elect_one();
         const int steps = (a.d + 15) / 16; // of 16 elements of the head
         const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
         const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
-        int stage = 0;
+        const uint64_t dq = operand_desc(base, 16);
+        int stage = 0, formed = 0, kt = -1, vt = -1, kn = 0, vn = 0; // blocks left of the tiles begun
         uint32_t phase = 0;
-        bool ok = blocks.count > 0 && bar_wait_cta(q_full, 0, &gave_up);
-        const auto form_s = [&](int n) {
-            ok = ok && bar_wait_cta(full(stage), phase, &gave_up);
-            if (!ok) return;
-            fence_after();
-            if (chosen) {
-                const uint64_t dq = operand_desc(base, 16), dk = operand_desc(ring + stage * kSlice, 16);
-                for (int j = 0; j < steps; ++j) // 64 elements a chunk
-                    mma_ss(tmem + 64 * (n % kBuffers), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc_s, j > 0);
-                commit(empty(stage));
-                commit(s_full(n % kBuffers));
-            }
-            __syncwarp();
+        bool ok = true;
+        const auto next = [&] {
             if (++stage == kStages) stage = 0, phase ^= 1u;
         };
-        for (int n = 0; ok && n < min(kBuffers, blocks.count); ++n) form_s(n);
-        for (int n = 0; ok && n < blocks.count; ++n) {
-            ok = bar_wait_cta(full(stage), phase, &gave_up) && bar_wait_cta(p_full(n % kBuffers), n / kBuffers & 1, &gave_up);
+        const auto form_s = [&] { // false at the end
+            if (kn == 0) {
+                ++kt;
+                ok = ok && bar_wait_cta(tile_full(kt), kt / kTiles & 1, &gave_up);
+                if (!ok) return false;
+                kn = tiles[kt % kTiles].blocks.count;
+                if (kn == 0) return false;
+                ok = bar_wait_cta(q_full, kt & 1, &gave_up);
+            }
+            ok = ok && bar_wait_cta(full(stage), phase, &gave_up);
+            if (!ok) return false;
+            fence_after();
+            --kn;
+            if (chosen) {
+                const uint64_t dk = operand_desc(ring + stage * kSlice, 16);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) // 64 elements a chunk
+                    if (j < steps)
+                        mma_ss(tmem + 64 * (formed & 1), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc_s, j > 0);
+                commit(s_full(formed));
+                commit(empty(stage));
+                if (kn == 0) commit(q_empty);
+            }
+            __syncwarp();
+            ++formed;
+            next();
+            return true;
+        };
+        bool keys = form_s() && form_s();
+        for (int g = 0; ok && g < formed; ++g) {
+            const bool first = vn == 0;
+            if (first) {
+                vn = tiles[++vt % kTiles].blocks.count;
+                ok = bar_wait_cta(o_empty, (vt & 1) ^ 1, &gave_up); // the last tile's output has been read
+            }
+            ok = ok && bar_wait_cta(full(stage), phase, &gave_up) && bar_wait_cta(p_full(g), g >> 1 & 1, &gave_up);
             if (!ok) break;
             fence_after();
+            --vn;
             if (chosen) {
                 const uint64_t dv = operand_desc(ring + stage * kSlice, 8192);
 #pragma unroll
                 for (int j = 0; j < kBlock / 16; ++j)
-                    mma_ts(tmem + Shape::kO, tmem + 64 * (n % kBuffers) + 8 * j, dv + j * (2048 >> 4), desc_o, n > 0 || j > 0);
-                commit(empty(stage));
+                    mma_ts(tmem + Shape::kO, tmem + 64 * (g & 1) + 8 * j, dv + j * (2048 >> 4), desc_o, !first || j > 0);
                 commit(pv_done);
-                if (n + 1 == blocks.count) commit(o_full);
+                commit(empty(stage));
+                if (vn == 0) {
+                    commit(o_full);
+                    bar_arrive(tile_empty(vt));
+                }
             }
             __syncwarp();
-            if (++stage == kStages) stage = 0, phase ^= 1u;
-            if (n + kBuffers < blocks.count) {
-                ok = bar_wait_cta(pv_done, n & 1, &gave_up);
-                form_s(n + kBuffers);
+            next();
+            if (keys) {
+                ok = bar_wait_cta(pv_done, g & 1, &gave_up); // P has been read where the next S goes
+                keys = form_s();
             }
         }
-    } else if (rows > 0) {
+    } else {
         // ---------------------------------------------------------- softmax, a thread a query
-        const int row = warp * 32 + lane, place = p0 + row;
-        const int w0 = p0 + warp * 32, w1 = w0 + 31; // the warp's places
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16), to = lanes + Shape::kO;
         const float c = a.scale_log2;
-        float ref = -INFINITY, total = 0.0f;
-        bool ok = true;
-        const auto some_seen = [&](int g0) { return g0 <= w1 && (g0 + 31 > w0 - a.window || g0 < a.sinks); }; // of 32 keys, by the warp
-        const auto seen_by = [&](int g0) { return below(place + 1 - g0) & (~below(place - a.window + 1 - g0) | below(a.sinks - g0)); };
-        for (int n = 0; n < blocks.count; ++n) {
-            const int k0 = blocks[n] * kBlock;
-            const uint32_t ts = lanes + 64 * (n % kBuffers); // S, and P over it
-            ok = bar_wait_cta(s_full(n % kBuffers), n / kBuffers & 1, &gave_up);
-            if (!ok) break;
-            fence_after();
-            const bool inside = k0 + 63 <= w0 && (k0 > w1 - a.window || k0 + 63 < a.sinks); // every row sees all 64
-            const bool first = inside || some_seen(k0), second = inside || some_seen(k0 + 32);
-            // 32 keys at a time; the second 32 are read for the maximum, and again for P: four CTAs an SM leave 80 registers
-            float x[32], top = -INFINITY;
-            if (second) {
-                tmem_ld32(ts + 32, x);
-                tmem_wait_ld();
-                if (!inside) hide(x, seen_by(k0 + 32));
-                top = most_of<32>(x);
-            }
-            if (first) {
-                tmem_ld32(ts, x);
-                tmem_wait_ld();
-                if (!inside) hide(x, seen_by(k0));
-                top = fmaxf(top, most_of<32>(x));
-            }
-            const bool moves = top > ref && (top - ref) * c > 8.0f; // from -infinity, too
-            float shrink = 1.0f;
-            if (moves) {
-                shrink = exp2_approx((ref - top) * c);
-                ref = top;
-                total *= shrink;
-            }
-            if (n > 0 && __any_sync(0xffffffffu, moves)) {
-                if (kBuffers > 1) { // O is at rest
-                    ok = bar_wait_cta(pv_done, (n - 1) & 1, &gave_up);
-                    if (!ok) break;
-                    fence_after();
-                }
-#pragma unroll 1
-                for (int e = 0; 16 * e < a.d; ++e) {
-                    uint32_t r[16];
-                    tmem_ld16(to + 16 * e, r);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * shrink);
-                    tmem_st16(to + 16 * e, r);
-                }
-            }
-            const float off = ref == -INFINITY ? 0.0f : -ref * c;
-            f32x2 sum = pair(0.0f);
-            uint32_t p[16] = {};
-            if (first) exponentials<T>(x, c, off, sum, p);
-            tmem_st16(ts, p);
-            if (second) {
-                tmem_ld32(ts + 32, x);
-                tmem_wait_ld();
-                if (!inside) hide(x, seen_by(k0 + 32));
-                exponentials<T>(x, c, off, sum, p);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[i] = 0;
-            }
-            tmem_st16(ts + 16, p);
-            total += sum2(sum);
-            tmem_wait_st();
-            fence_before();
+        int g = 0; // blocks so far
+        for (int vt = 0;; ++vt) {
+            bar_pass_cta(tile_full(vt), vt / kTiles & 1, &gave_up);
+            if (__any_sync(0xffffffffu, gave_up)) break;
+            const Tile tile = tiles[vt % kTiles];
             __syncwarp();
-            if (lane == 0) bar_arrive(p_full(n % kBuffers));
-        }
-        if (ok && blocks.count > 0) {
-            ok = bar_wait_cta(o_full, 0, &gave_up);
+            if (lane == 0) bar_arrive(tile_empty(vt));
+            if (tile.rows == 0) break;
+            const int row = warp * 32 + lane, place = tile.p0 + row;
+            const int w0 = tile.p0 + warp * 32, w1 = w0 + 31; // the warp's places
+            const bool live = row < tile.rows;
+            // P = 2^(c s - ref); a row's reference is a whole number, so that what was summed about one is taken to another exactly
+            float ref = live ? -INFINITY : 0.0f, total = 0.0f;
+            bool ready = false; // every row of the warp has a reference
+            const auto some_seen = [&](int g0) { return g0 <= w1 && (g0 + 31 > w0 - a.window || g0 < a.sinks); }; // of 32 keys, by the warp
+            const auto seen_by = [&](int g0) { return below(place + 1 - g0) & (~below(place - a.window + 1 - g0) | below(a.sinks - g0)); };
+            for (int n = 0; n < tile.blocks.count; ++n, ++g) {
+                const int k0 = tile.blocks[n] * kBlock;
+                const uint32_t ts = lanes + 64 * (g & 1); // S, and P over it
+                const bool inside = k0 + 63 <= w0 && (k0 > w1 - a.window || k0 + 63 < a.sinks); // every row sees all 64
+                bar_pass_cta(s_full(g), g >> 1 & 1, &gave_up);
+                fence_after();
+                bool done = false;
+                if (inside && ready) {
+                    // No maximum is taken: a sum of more than 2^13 says that the row has risen too far above its reference.
+                    uint32_t p[32];
+                    float x[32], y[32];
+                    tmem_ld32(ts, x);
+                    tmem_ld32(ts + 32, y);
+                    tmem_wait_ld();
+                    const float sum = exponentials<T>(x, c, -ref, reinterpret_cast<uint32_t(&)[16]>(p[0])) +
+                                      exponentials<T>(y, c, -ref, reinterpret_cast<uint32_t(&)[16]>(p[16]));
+                    done = !__any_sync(0xffffffffu, live && sum > 8192.0f);
+                    if (done) {
+                        tmem_st32(ts, p);
+                        total += sum;
+                    }
+                }
+                if (!done) {
+                    // 32 keys at a time, read twice: for the maximum, and for P, which lies over scores that have been read
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int e = 0; e < 64; e += 32) {
+                        if (!some_seen(k0 + e)) continue;
+                        float x[32];
+                        tmem_ld32(ts + e, x);
+                        tmem_wait_ld();
+                        hide(x, seen_by(k0 + e));
+                        top = fmaxf(top, most_of<32>(x));
+                    }
+                    const float next = live && top * c > ref + 8.0f ? ceilf(top * c) : ref;
+                    const bool moves = next > ref;
+                    if (__any_sync(0xffffffffu, moves)) {
+                        const float shrink = moves ? exp2_approx(ref - next) : 1.0f; // 0 from -infinity
+                        ref = next;
+                        total *= shrink;
+                        if (n > 0) {
+                            bar_pass_cta(pv_done, (g - 1) & 1, &gave_up); // O is at rest
+                            fence_after();
+#pragma unroll 1
+                            for (int e = 0; 16 * e < a.d; ++e) {
+                                uint32_t r[16];
+                                tmem_ld16(to + 16 * e, r);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * shrink);
+                                tmem_st16(to + 16 * e, r);
+                            }
+                        }
+                    }
+                    ready = __all_sync(0xffffffffu, ref != -INFINITY);
+                    const float off = ref == -INFINITY ? 0.0f : -ref;
+#pragma unroll 1
+                    for (int e = 0; e < 64; e += 32) {
+                        uint32_t p[16] = {};
+                        if (some_seen(k0 + e)) {
+                            float x[32];
+                            tmem_ld32(ts + e, x);
+                            tmem_wait_ld();
+                            hide(x, seen_by(k0 + e));
+                            total += exponentials<T>(x, c, off, p);
+                        }
+                        tmem_st16(ts + e / 2, p);
+                    }
+                }
+                tmem_wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full(g));
+            }
+            const bool some = total > 0.0f || total != total; // not a number: neither is the output
+            const float inverse = some ? 1.0f / total : 0.0f;
+            T *p = live ? at<T>(a.o, tile.seq, tile.q_row + row, tile.head) : nullptr;
+            if (live && a.lse) a.lse[lse_of(a, tile, row)] = some ? (ref + log2f(total)) * kLn2 : -INFINITY;
+            bar_pass_cta(o_full, vt & 1, &gave_up);
             fence_after();
-        }
-        if (ok) {
-            const bool live = row < rows;
-            const int64_t out_row = qr.first + i0 + row;
-            const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
-            T *p = live ? at<T>(a.o, seq, out_row, head) : nullptr;
 #pragma unroll 1
             for (int e = 0; 32 * e < a.d; ++e) {
                 float o[32];
-                if (blocks.count > 0) {
-                    tmem_ld32(to + 32 * e, o);
-                    tmem_wait_ld();
+                tmem_ld32(to + 32 * e, o);
+                tmem_wait_ld();
+                if (32 * e + 32 >= a.d) { // all of it has been read
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(o_empty);
                 }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = total > 0.0f || total != total ? o[i] * (total != total ? total : inverse) : 0.0f;
+                for (int i = 0; i < 32; ++i) o[i] = some ? o[i] * inverse : 0.0f;
                 if (live) store_row(p + 32 * e, o, a.d - 32 * e, a.wide_o);
             }
-            if (live && a.lse)
-                a.lse[((int64_t)(a.packed_q ? 0 : seq) * a.q_heads + head) * a.q_rows + out_row] =
-                    total > 0.0f ? ref * (c * kLn2) + logf(total) : total != total ? total : -INFINITY;
         }
     }
     __syncwarp();
@@ -736,16 +836,22 @@ struct Packer {
 };
 
 template <typename T, int D>
-int launch_forward(ForwardArgs &f, int64_t rows, cudaStream_t s)
+int launch_forward(ForwardArgs &f, int64_t rows, int sms, cudaStream_t s)
 {
     using Shape = ForwardShape<D>;
     f.tiles = (int)(f.packed_q ? rows / 128 + f.sequences : (rows + 127) / 128);
-    const int64_t ctas = (int64_t)f.tiles * f.q_heads * (f.packed_q ? 1 : f.sequences);
-    if (ctas > 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
+    const int64_t lanes = (int64_t)f.q_heads * (f.packed_q ? 1 : f.sequences), items = lanes * f.tiles;
+    if (items > 0x3fffffff) return A2SGD_ERR_TOO_LARGE;
+    f.lanes = (int)lanes;
+    // Heads that are worked on side by side: as many as their keys and values fit into L2 with (48 MB of 126), those that some tile of a wave
+    // sees.  8 x 4096, 25 heads of 128, no window: all 200 at once 1089 us.
+    const int64_t live = std::min<int64_t>(f.k_rows, (int64_t)f.window + 2048);
+    f.together = (int)std::min<int64_t>(lanes, std::max<int64_t>(8, (48ll << 20) * f.group / std::max<int64_t>(1, live * D * 4)));
+    f.items = (int)items;
     const void *fn = reinterpret_cast<const void *>(&k_forward<T, D>);
     A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
     void *params[] = {&f};
-    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)ctas), Shape::kThreads, Shape::kSmem, params, s));
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)std::min<int64_t>(items, (int64_t)sms * Shape::kCtas)), Shape::kThreads, Shape::kSmem, params, s));
     return A2SGD_OK;
 }
 
@@ -773,7 +879,7 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     f.sequences = (int)shape->sequences;
     f.wide_o = wide(o);
     f.scale_log2 = (float)(shape->scale * 1.4426950408889634);
-    return q.d <= 64 ? launch_forward<T, 64>(f, q.rows, s) : launch_forward<T, 128>(f, q.rows, s);
+    return q.d <= 64 ? launch_forward<T, 64>(f, q.rows, sms, s) : launch_forward<T, 128>(f, q.rows, sms, s);
 }
 
 Args common(const a2sgd_attention *s, const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *v, const a2sgd_heads *o)
