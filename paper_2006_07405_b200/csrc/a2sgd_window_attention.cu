@@ -17,16 +17,6 @@ struct Heads {
     int64_t seq, row, head;
 };
 
-struct Args {
-    Heads q, k, v, o, dout, dq, dk, dv;
-    float *lse, *delta;
-    const int32_t *q_ranges, *k_ranges;
-    int sequences, q_heads, kv_heads, d, group;
-    int q_rows, k_rows, window, sinks;
-    int packed_q; // one lse plane
-    float scale;
-};
-
 struct Range {
     int first, count;
 };
@@ -41,16 +31,6 @@ __device__ __forceinline__ T *at(const Heads &h, int b, int64_t row, int head)
 {
     return static_cast<T *>(h.p) + (int64_t)b * h.seq + row * h.row + (int64_t)head * h.head;
 }
-__device__ __forceinline__ int64_t lse_at(const Args &a, int b, int head, int64_t row)
-{
-    return ((int64_t)(a.packed_q ? 0 : b) * a.q_heads + head) * a.q_rows + row;
-}
-__device__ __forceinline__ bool sees(int place, int key, int window, int sinks)
-{
-    return key <= place && (key > place - window || key < sinks);
-}
-
-
 // CTAs whose bounded wait ran out, since the library was loaded: only ever counted up.
 __device__ unsigned int g_waits_run_out = 0;
 
@@ -272,7 +252,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     }
     if (warp == 5) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
     const int beyond = (int)threadIdx.x - 128;
-    if (beyond >= 0 && beyond < 3) tma_prefetch_map(beyond == 0 ? &a.q : beyond == 1 ? &a.k : &a.v); // parameters: no need to wait for the launch before
+    if (beyond >= 0 && beyond < 3 && a.k_rows > 0) tma_prefetch_map(beyond == 0 ? &a.q : beyond == 1 ? &a.k : &a.v); // parameters: no need to wait for the launch before
     fence_before();
     __syncthreads();
     fence_after();
@@ -563,119 +543,519 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     if (warp == 5) tmem_free(tmem, Shape::kColumns);
 }
 
-// A warp a query: 32 keys at a time, a lane each, then the lanes share out the head's elements.
-template <typename T, bool BACKWARD>
-__global__ void __launch_bounds__(128) k_query(const __grid_constant__ Args a)
+struct DeltaArgs {
+    Heads o, dout;
+    const float *lse;
+    float *lse2, *delta;
+    int64_t rows;
+    int planes, heads, d, wide;
+};
+
+// ------------------------------------------------------------------ backward
+// Two launches of one template, so that nothing is added up by atomics (S and dP are formed twice: 14 D operations a pair in place of 10).
+//   KEYS false: 128 queries stay, blocks of 64 keys pass:        dQ += dS K
+//   KEYS true:  128 keys stay, blocks of 64 queries pass, of all query heads of the key head:   dK += dS^T Q,  dV += P^T dO
+// In either, with A, A' the tiles that stay and B, B' those that pass:  S = A B^T, dP = A' B'^T into TMEM; a thread reads its row, forms
+// P = exp(scale S - lse) and dS = P (dP - delta) and writes them over S and dP in 16 bits; then out += dS B, out' += P B'.
+// Roles and tiles as in the forward pass.  D = 64: two CTAs an SM; 128: one, with two buffers of S and dP and two groups of four softmax warps
+// that take the blocks in turn.
+// The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.
+struct BackwardArgs {
+    CUtensorMap stay0, stay1, pass0, pass1;
+    Heads out0, out1; // dq; or dk, dv
+    int wide0, wide1;
+    const float *lse2, *delta; // [q_heads][q_rows] a plane: log2 e times lse, delta
+    float *partials;           // [lanes][sink_rows][parts][2][D]
+    const int32_t *q_ranges, *k_ranges;
+    int q_heads, kv_heads, group, d, q_rows, k_rows, window, sinks;
+    int packed_q, packed_k, sequences; // packed_q: one plane of lse2 and delta
+    int stay0_planes, stay1_planes, pass0_planes, pass1_planes;
+    int tiles, lanes, items, together;
+    int parts, part_blocks, sink_tiles, sink_rows, extra; // parts of a first tokens' tile, blocks of each; tiles and keys; items of a lane beyond its tiles
+    float scale, scale_log2;
+};
+template <int D, bool KEYS>
+struct BackwardShape {
+    static constexpr int kBuffers = D / 64, kThreads = 128 * kBuffers + 64, kCtas = D == 64 ? 2 : 1;
+    static constexpr int kStages = 4;
+    static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u, kStage = 2 * kSlice; // 128 rows, 64 rows, both tensors' 64
+    static constexpr uint32_t kSmem = 2 * kTile + kStages * kStage + 1024;
+    static constexpr uint32_t kColumns = D == 64 ? 256 : 512, kOut = kBuffers * 128; // of dK or dQ; dV's behind
+};
+
+struct BackwardTile {
+    int seq, head;         // KEYS: key head
+    int row, rows, place0; // in the plane, number; KEYS: first key, else place of the first query
+    int q_row, q_count, k_row, k_count;
+    int first, count;      // KEYS: first query of the first block; blocks (times heads) of this part
+    int part, begin;       // KEYS: part, and its first block
+    Blocks blocks;         // of keys
+};
+
+// KEYS: the blocks of queries, times heads, that see the keys kb to kb + 127 (within the range), from query `first` on.
+__device__ __forceinline__ int query_blocks(int kb, int q_count, int k_count, int window, int sinks, int group, int &first)
 {
-    wait_prior_grid();
-    release_next_grid();
-    const int lane = threadIdx.x & 31, head = blockIdx.y, b = blockIdx.z, i = blockIdx.x * 4 + (threadIdx.x >> 5);
-    const Range qr = range_of(a.q_ranges, b, a.q_rows), kr = range_of(a.k_ranges, b, a.k_rows);
-    if (i >= qr.count) return;
-    const int64_t row = qr.first + i;
-    const int place = i + kr.count - qr.count;
-    const T *q = at<T>(a.q, b, row, head), *g = BACKWARD ? at<T>(a.dout, b, row, head) : nullptr;
-    const T *o = BACKWARD ? at<T>(a.o, b, row, head) : nullptr;
-    float delta = 0.0f, lse = 0.0f;
-    if (BACKWARD) {
-        for (int c = lane; c < a.d; c += 32) delta += to_f32(g[c]) * to_f32(o[c]);
-        for (int s = 16; s; s >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, s);
-        lse = a.lse[lse_at(a, b, head, row)];
-        if (lane == 0) a.delta[lse_at(a, b, head, row)] = delta;
-    }
-    float acc[4] = {}, top = -INFINITY, total = 0.0f;
-    const int lo = max(0, place - a.window + 1), end = min(place + 1, kr.count);
-    for (int j0 = 0; j0 < end; j0 += 32) {
-        if (j0 + 32 <= lo && j0 >= a.sinks) {
-            j0 = lo / 32 * 32 - 32;
-            continue;
-        }
-        const int j = j0 + lane;
-        const bool on = j < end && sees(place, j, a.window, a.sinks);
-        float s = -INFINITY, dp = 0.0f;
-        if (on) {
-            const T *k = at<T>(a.k, b, kr.first + j, head / a.group), *v = at<T>(a.v, b, kr.first + j, head / a.group);
-            s = 0.0f;
-            for (int c = 0; c < a.d; ++c) {
-                s += to_f32(q[c]) * to_f32(k[c]);
-                if (BACKWARD) dp += to_f32(g[c]) * to_f32(v[c]);
-            }
-            s *= a.scale;
-        }
-        float p;
-        if (BACKWARD) {
-            p = on ? expf(s - lse) * (dp - delta) * a.scale : 0.0f;
-        } else {
-            float most = s;
-            for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-            const float next = fmaxf(top, most), base = next == -INFINITY ? 0.0f : next, shrink = expf(top - base);
-            p = expf(s - base);
-            total *= shrink;
-            for (float &x : acc) x *= shrink;
-            top = next;
-            float sum = p;
-            for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-            total += sum;
-        }
-        for (int r = 0; r < 32 && j0 + r < end; ++r) {
-            const float w = __shfl_sync(0xffffffffu, p, r);
-            if (!sees(place, j0 + r, a.window, a.sinks)) continue;
-            const T *x = at<T>(BACKWARD ? a.k : a.v, b, kr.first + j0 + r, head / a.group);
-            for (int e = 0; e < 4; ++e)
-                if (lane + 32 * e < a.d) acc[e] += w * to_f32(x[lane + 32 * e]);
-        }
-    }
-    if (BACKWARD && !a.dq.p) return;
-    T *out = at<T>(BACKWARD ? a.dq : a.o, b, row, head);
-    for (int e = 0; e < 4; ++e)
-        if (lane + 32 * e < a.d) out[lane + 32 * e] = from_f32<T>(BACKWARD ? acc[e] : total > 0.0f ? acc[e] / total : 0.0f);
-    if (!BACKWARD && a.lse && lane == 0) a.lse[lse_at(a, b, head, row)] = top + logf(total);
+    const int ahead = k_count - q_count, last_key = min(kb + 127, k_count - 1);
+    first = max(0, kb - ahead);
+    const int end = kb < sinks ? q_count : (int)min((int64_t)q_count, (int64_t)last_key + window - ahead);
+    return end > first ? (end - first + 63) / 64 * group : 0;
 }
 
-// A warp a key and key head: the queries that see it, 32 at a time.
-template <typename T>
-__global__ void __launch_bounds__(128) k_key(const __grid_constant__ Args a)
+template <bool KEYS>
+__device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, BackwardTile &t)
+{
+    const int each = a.tiles + a.extra;
+    const int part = item / (a.together * each), rest = item - part * a.together * each;
+    const int wide = min(a.together, a.lanes - part * a.together), lane = part * a.together + rest % wide;
+    const int heads = KEYS ? a.kv_heads : a.q_heads;
+    int tile = rest / wide;
+    t.head = lane % heads;
+    t.seq = lane / heads;
+    t.part = 0;
+    if (KEYS && tile < a.extra) {
+        const int more = a.parts - 1;
+        t.part = 1 + tile % more;
+        tile /= more;
+        if (a.packed_k) t.seq = tile / a.sink_tiles, tile %= a.sink_tiles;
+    } else {
+        tile = KEYS ? tile - a.extra : a.tiles - 1 - tile;
+        if (KEYS ? a.packed_k : a.packed_q) locate(KEYS ? a.k_ranges : a.q_ranges, a.sequences, KEYS ? a.k_rows : a.q_rows, 128, tile, t.seq, tile);
+        if (t.seq < 0) return false;
+    }
+    const Range qr = range_of(a.q_ranges, t.seq, a.q_rows), kr = range_of(a.k_ranges, t.seq, a.k_rows);
+    t.q_row = qr.first, t.q_count = qr.count, t.k_row = kr.first, t.k_count = kr.count;
+    t.rows = min(128, (KEYS ? kr.count : qr.count) - tile * 128);
+    if (t.rows <= 0) return false;
+    t.row = (KEYS ? kr.first : qr.first) + tile * 128;
+    t.begin = 0;
+    if (KEYS) {
+        t.place0 = tile * 128;
+        const int all = query_blocks(tile * 128, qr.count, kr.count, a.window, a.sinks, a.group, t.first);
+        t.begin = t.part * a.part_blocks;
+        t.count = min(all - t.begin, a.parts > 1 ? a.part_blocks : all);
+        if (t.part && t.count <= 0) return false;
+        t.count = max(t.count, 0);
+    } else {
+        t.place0 = tile * 128 + kr.count - qr.count;
+        t.blocks = Blocks(t.place0, t.place0 + t.rows - 1, a.window, a.sinks, kBlock);
+        t.count = t.blocks.count;
+    }
+    return true;
+}
+
+template <typename T, int D, bool KEYS>
+__global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, BackwardShape<D, KEYS>::kCtas) k_backward(const __grid_constant__ BackwardArgs a)
+{
+    using Shape = BackwardShape<D, KEYS>;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kLoad = 4 * kBuffers, kProducts = kLoad + 1;
+    constexpr uint32_t kSlice = Shape::kSlice, kTile = Shape::kTile;
+    extern __shared__ char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * kTile;
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 6 + 2 * kBuffers];
+    __shared__ BackwardTile tiles[kTiles];
+    __shared__ __align__(16) float columns[KEYS ? kStages : 1][2][64]; // KEYS: lse2 and delta of the queries that pass
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int gave_up;
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 8u * s; };
+    const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+    const uint32_t tile0 = bar0 + 16u * kStages, more0 = tile0 + 16u * kTiles;
+    const auto tile_full = [&](int t) { return tile0 + 8u * (t % kTiles); };
+    const auto tile_empty = [&](int t) { return tile0 + 8u * (kTiles + t % kTiles); };
+    const uint32_t stay_full = more0, stay_empty = more0 + 8, tail = more0 + 16, out_done = more0 + 24, out_full = more0 + 32, out_empty = more0 + 40;
+    const auto s_full = [&](int g) { return more0 + 48 + 8u * (g % kBuffers); };
+    const auto p_full = [&](int g) { return more0 + 48 + 8u * (kBuffers + g % kBuffers); };
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < 2 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
+        for (int t = 0; t < kTiles; ++t) {
+            bar_init(tile_full(t), 1);
+            bar_init(tile_empty(t), 4 * kBuffers + 1);
+        }
+        for (uint32_t b : {stay_full, stay_empty, tail, out_done, out_full}) bar_init(b, 1);
+        bar_init(out_empty, 4 * kBuffers);
+        for (int i = 0; i < kBuffers; ++i) {
+            bar_init(s_full(i), 1);
+            bar_init(p_full(i), 4);
+        }
+        gave_up = 0;
+        bar_init_fence();
+    }
+    if (warp == kProducts) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
+    const int beyond = (int)threadIdx.x - 32 * kLoad;
+    if (beyond >= 0 && beyond < 4 && a.q_rows > 0 && a.k_rows > 0) tma_prefetch_map(beyond == 0 ? &a.stay0 : beyond == 1 ? &a.stay1 : beyond == 2 ? &a.pass0 : &a.pass1);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_at;
+    wait_prior_grid();
+    release_next_grid(); // as in the forward pass
+
+    if (warp == kLoad) {
+        // ---------------------------------------------------------- tiles in
+        const bool chosen = elect_one();
+        int stage = 0, kt = -1;
+        uint32_t phase = 0, tails = 0;
+        bool ok = true;
+        for (int item = blockIdx.x; ok; item += gridDim.x) {
+            BackwardTile t;
+            t.rows = t.count = 0;
+            const bool end = item >= a.items;
+            if (!end && !find_tile<KEYS>(a, item, t)) continue;
+            if (!end && t.count == 0) { // rows that nothing sees, or that see nothing
+                for (int r = 0; r < t.rows; ++r) {
+                    for (int o = 0; o < (KEYS ? 2 : 1); ++o) {
+                        const Heads &h = o ? a.out1 : a.out0;
+                        if (!h.p) continue;
+                        T *p = at<T>(h, t.seq, t.row + r, t.head);
+                        for (int c = lane; c < a.d; c += 32) p[c] = from_f32<T>(0.0f);
+                    }
+                }
+                continue;
+            }
+            ++kt;
+            ok = bar_wait_cta(tile_empty(kt), (kt / kTiles & 1) ^ 1, &gave_up);
+            if (!ok) break;
+            if (lane == 0) tiles[kt % kTiles] = t;
+            __syncwarp();
+            if (chosen) bar_arrive(tile_full(kt));
+            __syncwarp();
+            if (end) break;
+            ok = bar_wait_cta(stay_empty, (kt & 1) ^ 1, &gave_up); // the last tile's have been read
+            if (!ok) break;
+            if (chosen) {
+                const int head = t.head;
+                bar_expect(stay_full, 2 * kTile);
+                for (int c = 0; c < kChunks; ++c) {
+                    tma_load4(base + c * 16384u, &a.stay0, 64 * c, t.row, head, a.stay0_planes > 1 ? t.seq : 0, stay_full);
+                    tma_load4(base + kTile + c * 16384u, &a.stay1, 64 * c, t.row, head, a.stay1_planes > 1 ? t.seq : 0, stay_full);
+                }
+            }
+            __syncwarp();
+            for (int n = 0; ok && n < t.count; ++n) {
+                ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
+                if (!ok) break;
+                const int it = t.begin + n;
+                const int head = KEYS ? t.head * a.group + it % a.group : t.head / a.group;
+                const int at_row = KEYS ? t.first + it / a.group * 64 : t.blocks[n] * kBlock; // in the sequence
+                const int row = (KEYS ? t.q_row : t.k_row) + at_row, valid = (KEYS ? t.q_count : t.k_count) - at_row;
+                const uint32_t dst = ring + stage * Shape::kStage;
+                const bool clear = (KEYS ? a.q_ranges : a.k_ranges) && valid < kBlock;
+                if (KEYS) {
+                    const int64_t line = ((int64_t)(a.packed_q ? 0 : t.seq) * a.q_heads + head) * a.q_rows + row;
+#pragma unroll
+                    for (int i = 0; i < 64; i += 32) {
+                        const bool in = i + lane < valid;
+                        columns[stage][0][i + lane] = in ? a.lse2[line + i + lane] : INFINITY;
+                        columns[stage][1][i + lane] = in ? a.delta[line + i + lane] : 0.0f;
+                    }
+                    __syncwarp();
+                }
+                const uint32_t bar = clear ? tail : full(stage);
+                if (chosen) {
+                    bar_expect(bar, Shape::kStage);
+                    for (int c = 0; c < kChunks; ++c) {
+                        tma_load4(dst + c * 8192u, &a.pass0, 64 * c, row, head, a.pass0_planes > 1 ? t.seq : 0, bar);
+                        tma_load4(dst + kSlice + c * 8192u, &a.pass1, 64 * c, row, head, a.pass1_planes > 1 ? t.seq : 0, bar);
+                    }
+                }
+                __syncwarp();
+                if (clear) {
+                    ok = bar_wait_cta(tail, tails & 1u, &gave_up);
+                    ++tails;
+                    if (!ok) break;
+                    clear_rows(dst, 2 * kChunks, kBlock, valid);
+                    if (chosen) bar_arrive(full(stage));
+                    __syncwarp();
+                }
+                if (++stage == kStages) stage = 0, phase ^= 1u;
+            }
+        }
+        // every tile has been consumed: nothing is in flight towards this CTA any more
+        for (int s = 0; ok && s < kStages; ++s) {
+            ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+        }
+    } else if (warp == kProducts) {
+        // ---------------------------------------------------------- products: S and dP a buffer's turn ahead
+        const bool chosen = elect_one();
+        const int steps = (a.d + 15) / 16;
+        const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
+        const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
+        const uint64_t d0 = operand_desc(base, 16), d1 = operand_desc(base + kTile, 16);
+        const bool with0 = a.out0.p != nullptr, with1 = KEYS && a.out1.p != nullptr;
+        int stage = 0, last_stage = 0, formed = 0, kt = -1, vt = -1, kn = 0, vn = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const auto form = [&] { // false at the end
+            if (kn == 0) {
+                ++kt;
+                ok = ok && bar_wait_cta(tile_full(kt), kt / kTiles & 1, &gave_up);
+                if (!ok) return false;
+                kn = tiles[kt % kTiles].count;
+                if (kn == 0) return false;
+                ok = bar_wait_cta(stay_full, kt & 1, &gave_up);
+            }
+            ok = ok && bar_wait_cta(full(stage), phase, &gave_up);
+            if (!ok) return false;
+            fence_after();
+            --kn;
+            if (chosen) {
+                const uint32_t s = tmem + 128 * (formed % kBuffers);
+                const uint64_t b0 = operand_desc(ring + stage * Shape::kStage, 16), b1 = operand_desc(ring + stage * Shape::kStage + kSlice, 16);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) { // 64 elements a chunk
+                    const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
+                    if (j < steps) mma_ss(s, d0 + oa, b0 + ob, desc_s, j > 0);
+                }
+                if (with0) {
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
+                        if (j < steps) mma_ss(s + 64, d1 + oa, b1 + ob, desc_s, j > 0);
+                    }
+                }
+                commit(s_full(formed));
+                if (kn == 0) commit(stay_empty);
+            }
+            __syncwarp();
+            ++formed;
+            if (++stage == kStages) stage = 0, phase ^= 1u;
+            return true;
+        };
+        bool more = form() && (kBuffers == 1 || form());
+        for (int g = 0; ok && g < formed; ++g) {
+            const bool first = vn == 0;
+            if (first) {
+                vn = tiles[++vt % kTiles].count;
+                ok = bar_wait_cta(out_empty, (vt & 1) ^ 1, &gave_up); // the last tile's outputs have been read
+            }
+            ok = ok && bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
+            if (!ok) break;
+            fence_after();
+            --vn;
+            if (chosen) {
+                const uint32_t s = tmem + 128 * (g % kBuffers), ds = KEYS ? s + 64 : s;
+                const uint64_t b0 = operand_desc(ring + last_stage * Shape::kStage, 8192), b1 = operand_desc(ring + last_stage * Shape::kStage + kSlice, 8192);
+                if (with1) {
+#pragma unroll
+                    for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 8 * j, b1 + j * (2048 >> 4), desc_o, !first || j > 0);
+                }
+                if (with0) {
+#pragma unroll
+                    for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 8 * j, b0 + j * (2048 >> 4), desc_o, !first || j > 0);
+                }
+                commit(out_done);
+                commit(empty(last_stage));
+                if (vn == 0) {
+                    commit(out_full);
+                    bar_arrive(tile_empty(vt));
+                }
+            }
+            __syncwarp();
+            if (++last_stage == kStages) last_stage = 0;
+            if (more) {
+                ok = bar_wait_cta(out_done, g & 1, &gave_up); // P and dS have been read where the next S and dP go
+                more = form();
+            }
+        }
+    } else {
+        // ---------------------------------------------------------- P and dS, a thread a row
+        const int buffer = warp >> 2, quarter = warp & 3;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), ts = lanes + 128 * buffer;
+        const float c = a.scale_log2;
+        int g = 0; // blocks so far
+        for (int vt = 0;; ++vt) {
+            bar_pass_cta(tile_full(vt), vt / kTiles & 1, &gave_up);
+            if (__any_sync(0xffffffffu, gave_up)) break;
+            const BackwardTile tile = tiles[vt % kTiles];
+            __syncwarp();
+            if (lane == 0) bar_arrive(tile_empty(vt));
+            if (tile.rows == 0) break;
+            const int row = quarter * 32 + lane, place = tile.place0 + row; // KEYS: the key
+            const int w0 = tile.place0 + quarter * 32, w1 = w0 + 31;
+            const bool live = row < tile.rows;
+            const int ahead = tile.k_count - tile.q_count;
+            float lse2 = INFINITY, delta = 0.0f;
+            if (!KEYS && live) {
+                const int64_t line = ((int64_t)(a.packed_q ? 0 : tile.seq) * a.q_heads + tile.head) * a.q_rows + tile.row + row;
+                lse2 = a.lse2[line];
+                delta = a.delta[line];
+            }
+            for (int n = 0; n < tile.count; ++n, ++g) {
+                if (kBuffers > 1 && (g & 1) != buffer) continue;
+                const int g0 = KEYS ? tile.first + (tile.begin + n) / a.group * 64 : tile.blocks[n] * kBlock; // first query (KEYS) or key
+                const int stage = g % kStages;
+                if (KEYS) bar_pass_cta(full(stage), g / kStages & 1, &gave_up);
+                bar_pass_cta(s_full(g), g / kBuffers & 1, &gave_up);
+                fence_after();
+#pragma unroll 1
+                for (int e = 0; e < 64; e += 32) {
+                    const int o0 = g0 + e, o1 = o0 + 31;
+                    bool some, all;
+                    if (KEYS) { // queries at places o0 + ahead on
+                        some = o1 + ahead >= w0 && o0 < tile.q_count && (o0 + ahead - a.window < w1 || w0 < a.sinks);
+                        all = o0 + ahead >= w1 && o1 < tile.q_count && (o1 + ahead - a.window < w0 || w1 < a.sinks);
+                    } else {
+                        some = o0 <= w1 && (o1 > w0 - a.window || o0 < a.sinks);
+                        all = o1 <= w0 && (o0 > w1 - a.window || o1 < a.sinks);
+                    }
+                    uint32_t p[16] = {}, ds[16] = {};
+                    if (some) {
+                        float x[32], y[32];
+                        tmem_ld32(ts + e, x);
+                        tmem_ld32(ts + 64 + e, y);
+                        tmem_wait_ld();
+                        const f32x2 c2 = pair(c);
+                        const float4 *l4 = reinterpret_cast<const float4 *>(&columns[KEYS ? stage : 0][0][KEYS ? e : 0]);
+                        const float4 *d4 = reinterpret_cast<const float4 *>(&columns[KEYS ? stage : 0][1][KEYS ? e : 0]);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            float4 l = make_float4(lse2, lse2, lse2, lse2), dl = make_float4(delta, delta, delta, delta);
+                            if (KEYS) l = l4[i / 4], dl = d4[i / 4];
+                            unpair(fma2(pair(x[i], x[i + 1]), c2, pair(-l.x, -l.y)), x[i], x[i + 1]);
+                            unpair(fma2(pair(x[i + 2], x[i + 3]), c2, pair(-l.z, -l.w)), x[i + 2], x[i + 3]);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) x[i + k] = exp2_approx(x[i + k]);
+                            unpair(mul2(pair(x[i], x[i + 1]), add2(pair(y[i], y[i + 1]), pair(-dl.x, -dl.y))), y[i], y[i + 1]);
+                            unpair(mul2(pair(x[i + 2], x[i + 3]), add2(pair(y[i + 2], y[i + 3]), pair(-dl.z, -dl.w))), y[i + 2], y[i + 3]);
+                        }
+                        if (!all) {
+                            uint32_t seen;
+                            if (KEYS) seen = ~below(place - ahead - o0) & below(tile.q_count - o0) & (place < a.sinks ? ~0u : below(place + a.window - ahead - o0));
+                            else seen = below(place + 1 - o0) & (~below(place - a.window + 1 - o0) | below(a.sinks - o0));
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                if (KEYS) x[i] = seen >> i & 1u ? x[i] : 0.0f;
+                                y[i] = seen >> i & 1u ? y[i] : 0.0f;
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (KEYS) p[i] = pack2(x[2 * i], x[2 * i + 1], T());
+                            ds[i] = pack2(y[2 * i], y[2 * i + 1], T());
+                        }
+                    }
+                    // over scores that have been read
+                    if (KEYS) tmem_st16(ts + e / 2, p);
+                    tmem_st16((KEYS ? ts + 64 : ts) + e / 2, ds);
+                }
+                tmem_wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full(g));
+            }
+            bar_pass_cta(out_full, vt & 1, &gave_up);
+            fence_after();
+            // the outputs: KEYS: dK and dV, one a group where there are two; else dQ, half of the elements a group
+            const uint32_t to = lanes + Shape::kOut;
+            const bool partial = KEYS && a.parts > 1 && live && place < a.sinks; // another part of this tile has some, too
+            constexpr int kOuts = KEYS ? 2 : 1, kSpan = !KEYS && kBuffers == 2 ? D / 2 : D;
+            const int o0 = KEYS && kBuffers == 2 ? buffer : 0, o1 = KEYS && kBuffers == 2 ? buffer + 1 : kOuts;
+            const int c0 = !KEYS && kBuffers == 2 ? buffer * kSpan : 0, c1 = min(a.d, c0 + kSpan);
+#pragma unroll 1
+            for (int o = o0; o < o1; ++o) {
+                const Heads &h = o ? a.out1 : a.out0;
+                if (!h.p) continue;
+                const float factor = o ? 1.0f : a.scale;
+#pragma unroll 1
+                for (int cc = c0; cc < c1; cc += 32) {
+                    float v[32];
+                    tmem_ld32(to + D * o + cc, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] *= factor;
+                    if (partial) {
+                        float *q = a.partials + ((((int64_t)(tile.seq * a.kv_heads + tile.head) * a.sink_rows + place) * a.parts + tile.part) * 2 + o) * D + cc;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(q + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    } else if (live && tile.part == 0) {
+                        store_row(at<T>(h, tile.seq, tile.row + row, tile.head) + cc, v, c1 - cc, o ? a.wide1 : a.wide0);
+                    }
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(out_empty);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (gave_up) {
+        // leave the copies and products in flight a bounded time to end, and say so
+        if (threadIdx.x == 0) atomicAdd(&g_waits_run_out, 1u);
+        const uint64_t begin = now_ns();
+        while (now_ns() - begin < 5000000ull) __nanosleep(1000);
+    }
+    if (warp == kProducts) tmem_free(tmem, Shape::kColumns);
+}
+
+// The parts' sums of the first tokens' keys, in order.  A warp a key and key head.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ BackwardArgs a)
 {
     wait_prior_grid();
     release_next_grid();
-    const int lane = threadIdx.x & 31, kv = blockIdx.y, b = blockIdx.z, j = blockIdx.x * 4 + (threadIdx.x >> 5);
-    const Range qr = range_of(a.q_ranges, b, a.q_rows), kr = range_of(a.k_ranges, b, a.k_rows);
-    if (j >= kr.count) return;
-    const T *k = at<T>(a.k, b, kr.first + j, kv), *v = at<T>(a.v, b, kr.first + j, kv);
-    const int ahead = kr.count - qr.count;
-    const int first = max(0, j - ahead);
-    const int end = j < a.sinks ? qr.count : (int)min((int64_t)qr.count, (int64_t)j - ahead + a.window);
-    float dk[4] = {}, dv[4] = {};
-    for (int head = kv * a.group; head < (kv + 1) * a.group; ++head) {
-        for (int i0 = first; i0 < end; i0 += 32) {
-            const int i = i0 + lane;
-            float p = 0.0f, ds = 0.0f;
-            if (i < end) {
-                const T *q = at<T>(a.q, b, qr.first + i, head), *g = at<T>(a.dout, b, qr.first + i, head);
-                float s = 0.0f, dp = 0.0f;
-                for (int c = 0; c < a.d; ++c) {
-                    s += to_f32(q[c]) * to_f32(k[c]);
-                    dp += to_f32(g[c]) * to_f32(v[c]);
-                }
-                const int64_t at_row = lse_at(a, b, head, qr.first + i);
-                p = expf(s * a.scale - a.lse[at_row]);
-                ds = p * (dp - a.delta[at_row]) * a.scale;
-            }
-            for (int r = 0; r < 32 && i0 + r < end; ++r) {
-                const float wp = __shfl_sync(0xffffffffu, p, r), ws = __shfl_sync(0xffffffffu, ds, r);
-                const T *q = at<T>(a.q, b, qr.first + i0 + r, head), *g = at<T>(a.dout, b, qr.first + i0 + r, head);
-                for (int e = 0; e < 4; ++e) {
-                    if (lane + 32 * e >= a.d) break;
-                    dk[e] += ws * to_f32(q[lane + 32 * e]);
-                    dv[e] += wp * to_f32(g[lane + 32 * e]);
-                }
-            }
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (item >= (int64_t)a.sequences * a.kv_heads * a.sink_rows) return;
+    const int key = (int)(item % a.sink_rows), lane = (int)(item / a.sink_rows), head = lane % a.kv_heads, seq = lane / a.kv_heads;
+    const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
+    if (key >= kr.count) return;
+    int first;
+    const int all = query_blocks(key / 128 * 128, qr.count, kr.count, a.window, a.sinks, a.group, first);
+    const int parts = (all + a.part_blocks - 1) / a.part_blocks;
+    if (parts == 0) return; // cleared where the tile was found
+    for (int o = 0; o < 2; ++o) {
+        const Heads &h = o ? a.out1 : a.out0;
+        if (!h.p) continue;
+        T *p = at<T>(h, seq, kr.first + key, head);
+        for (int c = threadIdx.x & 31; c < a.d; c += 32) {
+            float sum = 0.0f;
+            for (int k = 0; k < parts; ++k) sum += a.partials[((item * a.parts + k) * 2 + o) * D + c];
+            p[c] = from_f32<T>(sum);
         }
     }
-    for (int e = 0; e < 4; ++e) {
-        if (lane + 32 * e >= a.d) break;
-        if (a.dk.p) at<T>(a.dk, b, kr.first + j, kv)[lane + 32 * e] = from_f32<T>(dk[e]);
-        if (a.dv.p) at<T>(a.dv, b, kr.first + j, kv)[lane + 32 * e] = from_f32<T>(dv[e]);
+}
+
+// lse in units of log 2 and delta of every query: sixteen lanes a query and head.
+template <typename T>
+__global__ void __launch_bounds__(256) k_delta(const __grid_constant__ DeltaArgs a)
+{
+    wait_prior_grid();
+    release_next_grid();
+    const int lane = threadIdx.x & 15;
+    const int64_t all = (int64_t)a.planes * a.rows * a.heads;
+    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < (all + 1) / 2 * 2; i += (int64_t)gridDim.x * 16) {
+        const int64_t flat = i / a.heads, plane = flat / a.rows, row = flat - plane * a.rows;
+        const int head = (int)(i - flat * a.heads);
+        float sum = 0.0f;
+        if (i < all) {
+            const T *o = static_cast<const T *>(a.o.p) + plane * a.o.seq + row * a.o.row + (int64_t)head * a.o.head;
+            const T *g = static_cast<const T *>(a.dout.p) + plane * a.dout.seq + row * a.dout.row + (int64_t)head * a.dout.head;
+            if (a.wide) {
+                if (lane * 8 < a.d) {
+                    Raw8<T> x, y;
+                    float u[8], v[8];
+                    x.load(o + lane * 8);
+                    y.load(g + lane * 8);
+                    x.unpack(u);
+                    y.unpack(v);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum = fmaf(u[k], v[k], sum);
+                }
+            } else {
+                for (int c = lane; c < a.d; c += 16) sum = fmaf(to_f32(o[c]), to_f32(g[c]), sum);
+            }
+        }
+#pragma unroll
+        for (int s = 8; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+        if (lane == 0 && i < all) {
+            const int64_t line = (plane * a.heads + head) * a.rows + row;
+            const float l = a.lse[line];
+            a.lse2[line] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
+            a.delta[line] = sum;
+        }
     }
 }
 
@@ -882,32 +1262,130 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     return q.d <= 64 ? launch_forward<T, 64>(f, q.rows, sms, s) : launch_forward<T, 128>(f, q.rows, sms, s);
 }
 
-Args common(const a2sgd_attention *s, const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *v, const a2sgd_heads *o)
+// How the first tokens' tiles are cut: the blocks of an ordinary tile's pass each, or 32 at least.
+struct Parts {
+    int parts = 1, blocks = 0, sink_tiles = 0, sink_rows = 0;
+};
+Parts parts_of(const a2sgd_attention *s)
 {
-    Args a{};
-    a.q = heads_of(q), a.k = heads_of(k), a.v = heads_of(v), a.o = heads_of(o);
-    a.q_ranges = s->q_ranges, a.k_ranges = s->k_ranges;
-    a.sequences = (int)s->sequences, a.q_heads = (int)s->q_heads, a.kv_heads = (int)s->kv_heads, a.d = (int)s->head_dim;
-    a.group = a.q_heads / a.kv_heads;
-    a.q_rows = (int)s->q_rows, a.k_rows = (int)s->k_rows;
-    a.window = (int)std::min<uint64_t>(s->window, 1u << 30);
-    a.sinks = (int)std::min<uint64_t>(s->sinks, 1u << 30);
-    a.packed_q = s->q_ranges && q->sequence_stride == 0;
-    a.scale = (float)s->scale;
-    return a;
+    Parts p;
+    const int64_t group = s->q_heads / s->kv_heads, q_rows = (int64_t)s->q_rows, k_rows = (int64_t)s->k_rows;
+    const int64_t sinks = std::min<int64_t>(s->sinks, k_rows), window = (int64_t)std::min<uint64_t>(s->window, 1u << 30);
+    if (sinks == 0 || window >= q_rows) return p;
+    const int64_t ordinary = ((127 + window + 63) / 64 + 1) * group, each = std::max<int64_t>(ordinary, 32), all = (q_rows + 63) / 64 * group;
+    if (all <= each) return p;
+    p.parts = (int)((all + each - 1) / each);
+    p.blocks = (int)each;
+    p.sink_tiles = (int)((sinks + 127) / 128);
+    p.sink_rows = (int)sinks;
+    return p;
+}
+uint64_t partial_bytes(const a2sgd_attention *s)
+{
+    const Parts p = parts_of(s);
+    return p.parts > 1 ? up256((uint64_t)s->sequences * s->kv_heads * p.sink_rows * p.parts * 2 * (s->head_dim <= 64 ? 64 : 128) * 4) : 0;
+}
+
+template <typename T, int D, bool KEYS>
+int launch_backward(BackwardArgs &b, int64_t rows, int sms, cudaStream_t s)
+{
+    using Shape = BackwardShape<D, KEYS>;
+    const bool packed = KEYS ? b.packed_k : b.packed_q;
+    b.tiles = (int)(packed ? rows / 128 + b.sequences : (rows + 127) / 128);
+    const int64_t lanes = (int64_t)(KEYS ? b.kv_heads : b.q_heads) * (packed ? 1 : b.sequences);
+    const int64_t extra = KEYS ? (int64_t)b.sink_tiles * (b.parts - 1) * (packed ? b.sequences : 1) : 0;
+    const int64_t items = lanes * (b.tiles + extra);
+    if (items > 0x3fffffff) return A2SGD_ERR_TOO_LARGE;
+    b.lanes = (int)lanes;
+    b.extra = (int)extra;
+    b.items = (int)items;
+    // as in the forward pass: what the tiles of a wave read at the same time stays in L2
+    const int64_t live = std::min<int64_t>(KEYS ? b.q_rows : b.k_rows, (int64_t)b.window + 2048);
+    b.together = (int)std::min<int64_t>(lanes, std::max<int64_t>(8, (48ll << 20) * (KEYS ? 1 : b.group) / std::max<int64_t>(1, live * D * 4 * (KEYS ? b.group : 1))));
+    const void *fn = reinterpret_cast<const void *>(&k_backward<T, D, KEYS>);
+    A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
+    void *params[] = {&b};
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)std::min<int64_t>(items, (int64_t)sms * Shape::kCtas)), Shape::kThreads, Shape::kSmem, params, s));
+    return A2SGD_OK;
+}
+
+template <typename T, int D>
+int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &dout, const Tensor &dq, const Tensor &dk,
+                 const Tensor &dv, int dtype, int sms, cudaStream_t s)
+{
+    int rc = A2SGD_OK;
+    if (dq.h.p && q.rows) {
+        const auto maps = [&] {
+            return make_map(&b.stay0, q, dtype, 128) && make_map(&b.stay1, dout, dtype, 128) &&
+                   (k.rows == 0 || (make_map(&b.pass0, k, dtype, kBlock) && make_map(&b.pass1, v, dtype, kBlock)));
+        };
+        if (!maps()) return A2SGD_ERR_CUDA;
+        b.stay0_planes = q.planes, b.stay1_planes = dout.planes, b.pass0_planes = k.planes, b.pass1_planes = v.planes;
+        b.out0 = dq.h, b.out1 = Heads{nullptr, 0, 0, 0};
+        b.wide0 = wide(dq);
+        rc = launch_backward<T, D, false>(b, q.rows, sms, s);
+        if (rc != A2SGD_OK) return rc;
+    }
+    if ((dk.h.p || dv.h.p) && k.rows) {
+        const auto maps = [&] {
+            return make_map(&b.stay0, k, dtype, 128) && make_map(&b.stay1, v, dtype, 128) &&
+                   (q.rows == 0 || (make_map(&b.pass0, q, dtype, kBlock) && make_map(&b.pass1, dout, dtype, kBlock)));
+        };
+        if (!maps()) return A2SGD_ERR_CUDA;
+        b.stay0_planes = k.planes, b.stay1_planes = v.planes, b.pass0_planes = q.planes, b.pass1_planes = dout.planes;
+        b.out0 = dk.h, b.out1 = dv.h;
+        b.wide0 = wide(dk), b.wide1 = wide(dv);
+        rc = launch_backward<T, D, true>(b, k.rows, sms, s);
+        if (rc != A2SGD_OK) return rc;
+        if (b.parts > 1) {
+            const int64_t keys = (int64_t)b.sequences * b.kv_heads * b.sink_rows;
+            void *params[] = {&b};
+            A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold_keys<T, D>), dim3((unsigned)((keys + 7) / 8)), 256, 0, params, s));
+        }
+    }
+    return rc;
 }
 
 template <typename T>
-int backward(Args &a, cudaStream_t s)
+int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &o, const float *lse,
+             const Tensor &dq, const Tensor &dk, const Tensor &dv, void *workspace, uint64_t workspace_bytes, int sms, cudaStream_t s)
 {
-    void *params[] = {&a};
-    if (a.q_rows)
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_query<T, true>),
-                             dim3((unsigned)(a.q_rows + 3) / 4, (unsigned)a.q_heads, (unsigned)a.sequences), 128, 0, params, s));
-    if (a.k_rows && (a.dk.p || a.dv.p))
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_key<T>),
-                             dim3((unsigned)(a.k_rows + 3) / 4, (unsigned)a.kv_heads, (unsigned)a.sequences), 128, 0, params, s));
-    return A2SGD_OK;
+    Packer pack(workspace);
+    const bool packed_q = shape->q_ranges && q.h.seq == 0, packed_k = shape->k_ranges && k.h.seq == 0;
+    const uint64_t lines = (uint64_t)(packed_q ? 1 : shape->sequences) * shape->q_heads * shape->q_rows;
+    BackwardArgs b{};
+    float *lse2 = static_cast<float *>(pack.take(lines * 4)), *delta = static_cast<float *>(pack.take(lines * 4));
+    b.lse2 = lse2, b.delta = delta;
+    b.partials = static_cast<float *>(pack.take(partial_bytes(shape)));
+    const Tensor pq = pack.usable(q), pk = pack.usable(k), pv = pack.usable(v), pdout = pack.usable(dout);
+    if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
+    int rc = pack.run(sms, s);
+    if (rc != A2SGD_OK) return rc;
+    if (lines) {
+        DeltaArgs d{};
+        d.o = o.h, d.dout = dout.h;
+        d.lse = lse;
+        d.lse2 = lse2, d.delta = delta;
+        d.rows = q.rows;
+        d.planes = packed_q ? 1 : (int)shape->sequences;
+        d.heads = q.heads, d.d = q.d;
+        d.wide = wide(o) && wide(dout);
+        void *params[] = {&d};
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_delta<T>), dim3((unsigned)std::min<uint64_t>((lines + 15) / 16, (uint64_t)sms * 16)), 256, 0, params, s));
+    }
+    const Parts parts = parts_of(shape);
+    b.q_ranges = shape->q_ranges, b.k_ranges = shape->k_ranges;
+    b.q_heads = q.heads, b.kv_heads = k.heads, b.group = q.heads / k.heads, b.d = q.d;
+    b.q_rows = (int)q.rows, b.k_rows = (int)k.rows;
+    b.window = (int)std::min<uint64_t>(shape->window, 1u << 30);
+    b.sinks = (int)std::min<uint64_t>(shape->sinks, 1u << 30);
+    b.packed_q = packed_q, b.packed_k = packed_k;
+    b.sequences = (int)shape->sequences;
+    b.parts = parts.parts, b.part_blocks = parts.blocks, b.sink_tiles = parts.sink_tiles, b.sink_rows = parts.sink_rows;
+    b.scale = (float)shape->scale;
+    b.scale_log2 = (float)(shape->scale * 1.4426950408889634);
+    return q.d <= 64 ? run_backward<T, 64>(b, pq, pk, pv, pdout, dq, dk, dv, shape->dtype, sms, s)
+                     : run_backward<T, 128>(b, pq, pk, pv, pdout, dq, dk, dv, shape->dtype, sms, s);
 }
 
 } // namespace
@@ -918,7 +1396,8 @@ extern "C" uint64_t a2sgd_window_attention_workspace(const a2sgd_attention *shap
     const int64_t q_planes = flags & A2SGD_ATTENTION_PACKED_Q ? 1 : shape->sequences, k_planes = flags & A2SGD_ATTENTION_PACKED_K ? 1 : shape->sequences;
     const int d = (int)shape->head_dim;
     uint64_t bytes = 0;
-    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4);
+    if (shape->kv_heads == 0) return 0;
+    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += 2 * up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4) + partial_bytes(shape);
     if (!(flags & A2SGD_ATTENTION_ALIGNED))
         bytes += (flags & A2SGD_ATTENTION_BACKWARD ? 2 : 1) * room(q_planes, (int64_t)shape->q_rows, (int)shape->q_heads, d) +
                  2 * room(k_planes, (int64_t)shape->k_rows, (int)shape->kv_heads, d);
@@ -962,17 +1441,14 @@ extern "C" int a2sgd_window_attention_backward(const a2sgd_attention *shape, con
     if ((rc = check_heads(shape, dq, shape->q_heads, shape->q_rows, shape->q_ranges, false, true)) != A2SGD_OK) return rc;
     if (!lse && shape->q_rows) return A2SGD_ERR_ARG;
     if (!aligned(workspace, 256) || !aligned(lse, 4)) return A2SGD_ERR_ALIGN;
-    if (workspace_bytes < a2sgd_window_attention_workspace(shape, A2SGD_ATTENTION_BACKWARD | A2SGD_ATTENTION_ALIGNED |
-                                                                      (shape->q_ranges && q->sequence_stride == 0 ? A2SGD_ATTENTION_PACKED_Q : 0)))
-        return A2SGD_ERR_ARG;
     DeviceGuard guard(device);
-    if (!guard.ok) return A2SGD_ERR_CUDA;
-    Args a = common(shape, q, k, v, o);
-    a.dout = heads_of(dout), a.dq = heads_of(dq), a.dk = heads_of(dk), a.dv = heads_of(dv);
-    a.lse = const_cast<float *>(lse);
-    a.delta = static_cast<float *>(workspace);
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms < 1) return A2SGD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return shape->dtype == A2SGD_BF16 ? backward<__nv_bfloat16>(a, s) : backward<__half>(a, s);
+    const Tensor tdo = tensor_of(shape, dout, false), tq = tensor_of(shape, q, false), tk = tensor_of(shape, k, true), tv = tensor_of(shape, v, true),
+                 to = tensor_of(shape, o, false), tdq = tensor_of(shape, dq, false), tdk = tensor_of(shape, dk, true), tdv = tensor_of(shape, dv, true);
+    return shape->dtype == A2SGD_BF16 ? backward<__nv_bfloat16>(shape, tdo, tq, tk, tv, to, lse, tdq, tdk, tdv, workspace, workspace_bytes, sms, s)
+                                      : backward<__half>(shape, tdo, tq, tk, tv, to, lse, tdq, tdk, tdv, workspace, workspace_bytes, sms, s);
 }
 
 extern "C" int a2sgd_window_attention_status(int device, int *device_status, void *stream)
