@@ -209,6 +209,18 @@ __device__ __forceinline__ bool bar_try_cta(uint32_t bar, uint32_t parity)
                  : "memory");
     return done != 0;
 }
+// Whether the barrier's phase is complete, without waiting; the whole warp gets one answer.
+__device__ __forceinline__ bool bar_test_cta(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return __all_sync(0xffffffffu, done);
+}
 // bar_wait for a barrier that only this CTA's threads, copies and products arrive on.
 __device__ __forceinline__ bool bar_wait_cta(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
@@ -216,7 +228,7 @@ __device__ __forceinline__ bool bar_wait_cta(uint32_t bar, uint32_t parity, vola
     const uint64_t begin = now_ns();
     for (uint32_t polls = 1;; ++polls) {
         if (__all_sync(0xffffffffu, bar_try_cta(bar, parity))) return true;
-        if ((polls & 255u) == 0u && __any_sync(0xffffffffu, *gave_up || now_ns() - begin > kWaitLimitNs)) {
+        if (__any_sync(0xffffffffu, *gave_up || ((polls & 255u) == 0u && now_ns() - begin > kWaitLimitNs))) {
             *gave_up = 1;
             return false;
         }
@@ -229,7 +241,7 @@ __device__ __forceinline__ void bar_pass_cta(uint32_t bar, uint32_t parity, vola
     if (!bar_try_cta(bar, parity)) {
         const uint64_t begin = now_ns();
         for (uint32_t polls = 1; !bar_try_cta(bar, parity); ++polls) {
-            if ((polls & 63u) == 0u && (*gave_up || now_ns() - begin > kWaitLimitNs)) {
+            if (*gave_up || ((polls & 63u) == 0u && now_ns() - begin > kWaitLimitNs)) {
                 *gave_up = 1;
                 break;
             }

@@ -41,7 +41,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // keys that any of its queries sees: the first tokens' blocks, then those of the window.  One warp brings tiles in by TMA, one issues the
 // products, four hold the softmax, a thread a query.
 //   S = Q K^T into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  O += P V, P read from TMEM.
-// Two buffers of S: the next block's, be it the next tile's, is formed while the present one's P is.
+// Three buffers of S (two where O has 128 columns): the next block's, be it the next tile's, is formed while the present one's P is.
 // P is taken about a reference that is moved, and O and the sum with it, only where P would grow beyond 2^13: nearly no
 // block touches O, and blocks without a mask need no maximum.
 struct ForwardArgs {
@@ -63,7 +63,8 @@ struct ForwardShape {
     static constexpr int kThreads = 192, kCtas = 2, kStages = D == 64 ? 8 : 4;
     static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u; // 128 rows, 64 rows
     static constexpr uint32_t kSmem = kTile + kStages * kSlice + 1024;
-    static constexpr uint32_t kColumns = 256, kO = 128;
+    static constexpr int kBuffers = D == 64 ? 3 : 2; // of S
+    static constexpr uint32_t kColumns = 256, kO = 64 * kBuffers;
 };
 
 // The sequence and the tile of `unit` rows that a CTA has among packed sequences; count 0: none.  One warp.
@@ -181,6 +182,24 @@ __device__ __forceinline__ float exponentials(const float (&x)[32], float c, flo
     return sum2(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])));
 }
 
+// A warp that looks for work in turn: how long it has found none.
+struct Idle {
+    uint32_t polls = 0;
+    uint64_t begin = 0;
+    __device__ __forceinline__ bool go_on(bool went, volatile int *gave_up)
+    {
+        if (went) {
+            polls = 0;
+            return true;
+        }
+        if ((++polls & 255u) != 0u) return true;
+        if (polls == 256u) begin = now_ns();
+        if (!__any_sync(0xffffffffu, *gave_up || now_ns() - begin > kWaitLimitNs)) return true;
+        *gave_up = 1;
+        return false;
+    }
+};
+
 // A tile: whose it is, its queries and the blocks of keys that they see.  The loading warp works them out and leaves them in shared memory.
 struct Tile {
     int seq, head, p0, rows;     // place of the first query; queries, at least 1
@@ -220,11 +239,11 @@ template <typename T, int D>
 __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kCtas) k_forward(const __grid_constant__ ForwardArgs a)
 {
     using Shape = ForwardShape<D>;
-    constexpr int kStages = Shape::kStages, kChunks = D / 64;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers;
     constexpr uint32_t kSlice = Shape::kSlice;
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + Shape::kTile;
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 10];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 5 + 3 * kBuffers];
     __shared__ Tile tiles[kTiles];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
@@ -234,9 +253,10 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     const uint32_t tile0 = bar0 + 16u * kStages, more0 = tile0 + 16u * kTiles;
     const auto tile_full = [&](int t) { return tile0 + 8u * (t % kTiles); };
     const auto tile_empty = [&](int t) { return tile0 + 8u * (kTiles + t % kTiles); };
-    const uint32_t q_full = more0, q_empty = more0 + 8, tail = more0 + 16, pv_done = more0 + 24, o_full = more0 + 32, o_empty = more0 + 40;
-    const auto s_full = [&](int g) { return more0 + 48 + 8u * (g & 1); };
-    const auto p_full = [&](int g) { return more0 + 64 + 8u * (g & 1); };
+    const uint32_t q_full = more0, q_empty = more0 + 8, tail = more0 + 16, o_full = more0 + 24, o_empty = more0 + 32;
+    const auto s_full = [&](int g) { return more0 + 40 + 8u * (g % kBuffers); };
+    const auto p_full = [&](int g) { return more0 + 40 + 8u * (kBuffers + g % kBuffers); };
+    const auto pv_done = [&](int g) { return more0 + 40 + 8u * (2 * kBuffers + g % kBuffers); };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -245,8 +265,13 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             bar_init(tile_full(t), 1);
             bar_init(tile_empty(t), 5);
         }
-        for (uint32_t b : {q_full, q_empty, tail, pv_done, o_full, s_full(0), s_full(1)}) bar_init(b, 1);
-        for (uint32_t b : {o_empty, p_full(0), p_full(1)}) bar_init(b, 4);
+        for (uint32_t b : {q_full, q_empty, tail, o_full}) bar_init(b, 1);
+        bar_init(o_empty, 4);
+        for (int i = 0; i < kBuffers; ++i) {
+            bar_init(s_full(i), 1);
+            bar_init(p_full(i), 4);
+            bar_init(pv_done(i), 1);
+        }
         gave_up = 0;
         bar_init_fence();
     }
@@ -346,75 +371,74 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             if (++stage == kStages) stage = 0, phase ^= 1u;
         }
     } else if (warp == 5) {
-        // ---------------------------------------------------------- products: scores two blocks ahead
+        // ---------------------------------------------------------- products: whichever can go, so that they do not pause
         const bool chosen = elect_one();
         const int steps = (a.d + 15) / 16; // of 16 elements of the head
         const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
         const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
         const uint64_t dq = operand_desc(base, 16);
-        int stage = 0, formed = 0, kt = -1, vt = -1, kn = 0, vn = 0; // blocks left of the tiles begun
+        // tiles are consumed in the order in which they were loaded: K, K, then V and K in turn (the loading warp's order)
+        int stage = 0, formed = 0, added = 0, kt = 0, vt = -1, kn = 0, vn = 0; // blocks; the next tile; blocks left of the tiles begun
         uint32_t phase = 0;
-        bool ok = true;
+        bool more = true, fresh = false; // keys to come; the tile's queries have not been waited for
+        Idle idle;
         const auto next = [&] {
             if (++stage == kStages) stage = 0, phase ^= 1u;
         };
-        const auto form_s = [&] { // false at the end
-            if (kn == 0) {
-                ++kt;
-                ok = ok && bar_wait_cta(tile_full(kt), kt / kTiles & 1, &gave_up);
-                if (!ok) return false;
+        while (more || added < formed) {
+            bool went = false;
+            if (more && kn == 0 && bar_test_cta(tile_full(kt), kt / kTiles & 1)) {
                 kn = tiles[kt % kTiles].blocks.count;
-                if (kn == 0) return false;
-                ok = bar_wait_cta(q_full, kt & 1, &gave_up);
+                more = kn > 0;
+                fresh = true;
+                ++kt;
             }
-            ok = ok && bar_wait_cta(full(stage), phase, &gave_up);
-            if (!ok) return false;
-            fence_after();
-            --kn;
-            if (chosen) {
-                const uint64_t dk = operand_desc(ring + stage * kSlice, 16);
+            // S of the next block: where its place is free, and its keys have come, which lie behind V of two blocks before
+            if (kn > 0 && formed < added + 2 && (formed < kBuffers || bar_test_cta(pv_done(formed), (formed / kBuffers + 1) & 1)) && bar_test_cta(full(stage), phase) &&
+                (!fresh || bar_test_cta(q_full, (kt & 1) ^ 1))) {
+                fresh = false;
+                went = true;
+                fence_after();
+                --kn;
+                if (chosen) {
+                    const uint64_t dk = operand_desc(ring + stage * kSlice, 16);
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) // 64 elements a chunk
-                    if (j < steps)
-                        mma_ss(tmem + 64 * (formed & 1), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc_s, j > 0);
-                commit(s_full(formed));
-                commit(empty(stage));
-                if (kn == 0) commit(q_empty);
-            }
-            __syncwarp();
-            ++formed;
-            next();
-            return true;
-        };
-        bool keys = form_s() && form_s();
-        for (int g = 0; ok && g < formed; ++g) {
-            const bool first = vn == 0;
-            if (first) {
-                vn = tiles[++vt % kTiles].blocks.count;
-                ok = bar_wait_cta(o_empty, (vt & 1) ^ 1, &gave_up); // the last tile's output has been read
-            }
-            ok = ok && bar_wait_cta(full(stage), phase, &gave_up) && bar_wait_cta(p_full(g), g >> 1 & 1, &gave_up);
-            if (!ok) break;
-            fence_after();
-            --vn;
-            if (chosen) {
-                const uint64_t dv = operand_desc(ring + stage * kSlice, 8192);
-#pragma unroll
-                for (int j = 0; j < kBlock / 16; ++j)
-                    mma_ts(tmem + Shape::kO, tmem + 64 * (g & 1) + 8 * j, dv + j * (2048 >> 4), desc_o, !first || j > 0);
-                commit(pv_done);
-                commit(empty(stage));
-                if (vn == 0) {
-                    commit(o_full);
-                    bar_arrive(tile_empty(vt));
+                    for (int j = 0; j < D / 16; ++j) // 64 elements a chunk
+                        if (j < steps)
+                            mma_ss(tmem + 64 * (formed % kBuffers), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc_s, j > 0);
+                    commit(s_full(formed));
+                    commit(empty(stage));
+                    if (kn == 0) commit(q_empty);
                 }
+                __syncwarp();
+                ++formed;
+                next();
             }
-            __syncwarp();
-            next();
-            if (keys) {
-                ok = bar_wait_cta(pv_done, g & 1, &gave_up); // P has been read where the next S goes
-                keys = form_s();
+            // O += P V of the oldest block
+            if (added < formed && (formed == added + 2 || !more) && bar_test_cta(p_full(added), added / kBuffers & 1) && bar_test_cta(full(stage), phase) &&
+                (vn > 0 || bar_test_cta(o_empty, vt & 1))) {
+                went = true;
+                fence_after();
+                const bool first = vn == 0;
+                if (first) vn = tiles[++vt % kTiles].blocks.count; // the last tile's output has been read
+                --vn;
+                if (chosen) {
+                    const uint64_t dv = operand_desc(ring + stage * kSlice, 8192);
+#pragma unroll
+                    for (int j = 0; j < kBlock / 16; ++j)
+                        mma_ts(tmem + Shape::kO, tmem + 64 * (added % kBuffers) + 8 * j, dv + j * (2048 >> 4), desc_o, !first || j > 0);
+                    commit(pv_done(added));
+                    commit(empty(stage));
+                    if (vn == 0) {
+                        commit(o_full);
+                        bar_arrive(tile_empty(vt));
+                    }
+                }
+                __syncwarp();
+                ++added;
+                next();
             }
+            if (!idle.go_on(went, &gave_up)) break;
         }
     } else {
         // ---------------------------------------------------------- softmax, a thread a query
@@ -438,9 +462,9 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             const auto seen_by = [&](int g0) { return below(place + 1 - g0) & (~below(place - a.window + 1 - g0) | below(a.sinks - g0)); };
             for (int n = 0; n < tile.blocks.count; ++n, ++g) {
                 const int k0 = tile.blocks[n] * kBlock;
-                const uint32_t ts = lanes + 64 * (g & 1); // S, and P over it
+                const uint32_t ts = lanes + 64 * (g % kBuffers); // S, and P over it
                 const bool inside = k0 + 63 <= w0 && (k0 > w1 - a.window || k0 + 63 < a.sinks); // every row sees all 64
-                bar_pass_cta(s_full(g), g >> 1 & 1, &gave_up);
+                bar_pass_cta(s_full(g), g / kBuffers & 1, &gave_up);
                 fence_after();
                 bool done = false;
                 if (inside && ready) {
@@ -477,7 +501,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                         ref = next;
                         total *= shrink;
                         if (n > 0) {
-                            bar_pass_cta(pv_done, (g - 1) & 1, &gave_up); // O is at rest
+                            bar_pass_cta(pv_done(g - 1), (g - 1) / kBuffers & 1, &gave_up); // O is at rest
                             fence_after();
 #pragma unroll 1
                             for (int e = 0; 16 * e < a.d; ++e) {
@@ -548,7 +572,7 @@ struct DeltaArgs {
     const float *lse;
     float *lse2, *delta;
     int64_t rows;
-    int planes, heads, d, wide;
+    int blocks, heads, d, wide; // CTAs of a plane
 };
 
 // ------------------------------------------------------------------ backward
@@ -557,8 +581,8 @@ struct DeltaArgs {
 //   KEYS true:  128 keys stay, blocks of 64 queries pass, of all query heads of the key head:   dK += dS^T Q,  dV += P^T dO
 // In either, with A, A' the tiles that stay and B, B' those that pass:  S = A B^T, dP = A' B'^T into TMEM; a thread reads its row, forms
 // P = exp(scale S - lse) and dS = P (dP - delta) and writes them over S and dP in 16 bits; then out += dS B, out' += P B'.
-// Roles and tiles as in the forward pass.  D = 64: two CTAs an SM; 128: one, with two buffers of S and dP and two groups of four softmax warps
-// that take the blocks in turn.
+// Roles and tiles as in the forward pass, one CTA an SM, with three buffers of S and dP (two where dK and dV of 128 elements leave no more) and
+// groups of four warps that take the blocks in turn.
 // The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.
 struct BackwardArgs {
     CUtensorMap stay0, stay1, pass0, pass1;
@@ -576,11 +600,11 @@ struct BackwardArgs {
 };
 template <int D, bool KEYS>
 struct BackwardShape {
-    static constexpr int kBuffers = D / 64, kThreads = 128 * kBuffers + 64, kCtas = D == 64 ? 2 : 1;
-    static constexpr int kStages = 4;
+    static constexpr int kBuffers = KEYS && D == 128 ? 2 : 3, kGroups = 2, kThreads = 128 * kGroups + 64;
+    static constexpr int kStages = D == 64 ? 8 : 4;
     static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u, kStage = 2 * kSlice; // 128 rows, 64 rows, both tensors' 64
     static constexpr uint32_t kSmem = 2 * kTile + kStages * kStage + 1024;
-    static constexpr uint32_t kColumns = D == 64 ? 256 : 512, kOut = kBuffers * 128; // of dK or dQ; dV's behind
+    static constexpr uint32_t kColumns = 512, kOut = kBuffers * 128; // of dK or dQ; dV's behind
 };
 
 struct BackwardTile {
@@ -644,14 +668,14 @@ __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, Backw
 }
 
 template <typename T, int D, bool KEYS>
-__global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, BackwardShape<D, KEYS>::kCtas) k_backward(const __grid_constant__ BackwardArgs a)
+__global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backward(const __grid_constant__ BackwardArgs a)
 {
     using Shape = BackwardShape<D, KEYS>;
-    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kLoad = 4 * kBuffers, kProducts = kLoad + 1;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kGroups = Shape::kGroups, kLoad = 4 * kGroups, kProducts = kLoad + 1;
     constexpr uint32_t kSlice = Shape::kSlice, kTile = Shape::kTile;
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * kTile;
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 6 + 2 * kBuffers];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 5 + 3 * kBuffers];
     __shared__ BackwardTile tiles[kTiles];
     __shared__ __align__(16) float columns[KEYS ? kStages : 1][2][64]; // KEYS: lse2 and delta of the queries that pass
     __shared__ uint32_t tmem_at;
@@ -662,22 +686,24 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, BackwardShap
     const uint32_t tile0 = bar0 + 16u * kStages, more0 = tile0 + 16u * kTiles;
     const auto tile_full = [&](int t) { return tile0 + 8u * (t % kTiles); };
     const auto tile_empty = [&](int t) { return tile0 + 8u * (kTiles + t % kTiles); };
-    const uint32_t stay_full = more0, stay_empty = more0 + 8, tail = more0 + 16, out_done = more0 + 24, out_full = more0 + 32, out_empty = more0 + 40;
-    const auto s_full = [&](int g) { return more0 + 48 + 8u * (g % kBuffers); };
-    const auto p_full = [&](int g) { return more0 + 48 + 8u * (kBuffers + g % kBuffers); };
+    const uint32_t stay_full = more0, stay_empty = more0 + 8, tail = more0 + 16, out_full = more0 + 24, out_empty = more0 + 32;
+    const auto s_full = [&](int g) { return more0 + 40 + 8u * (g % kBuffers); };
+    const auto p_full = [&](int g) { return more0 + 40 + 8u * (kBuffers + g % kBuffers); };
+    const auto out_done = [&](int g) { return more0 + 40 + 8u * (2 * kBuffers + g % kBuffers); };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
         for (int t = 0; t < kTiles; ++t) {
             bar_init(tile_full(t), 1);
-            bar_init(tile_empty(t), 4 * kBuffers + 1);
+            bar_init(tile_empty(t), 4 * kGroups + 1);
         }
-        for (uint32_t b : {stay_full, stay_empty, tail, out_done, out_full}) bar_init(b, 1);
-        bar_init(out_empty, 4 * kBuffers);
+        for (uint32_t b : {stay_full, stay_empty, tail, out_full}) bar_init(b, 1);
+        bar_init(out_empty, 4 * kGroups);
         for (int i = 0; i < kBuffers; ++i) {
             bar_init(s_full(i), 1);
             bar_init(p_full(i), 4);
+            bar_init(out_done(i), 1);
         }
         gave_up = 0;
         bar_init_fence();
@@ -778,92 +804,89 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, BackwardShap
             if (++stage == kStages) stage = 0, phase ^= 1u;
         }
     } else if (warp == kProducts) {
-        // ---------------------------------------------------------- products: S and dP a buffer's turn ahead
+        // ---------------------------------------------------------- products: whichever can go, so that they do not pause
         const bool chosen = elect_one();
         const int steps = (a.d + 15) / 16;
         const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
         const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
         const uint64_t d0 = operand_desc(base, 16), d1 = operand_desc(base + kTile, 16);
         const bool with0 = a.out0.p != nullptr, with1 = KEYS && a.out1.p != nullptr;
-        int stage = 0, last_stage = 0, formed = 0, kt = -1, vt = -1, kn = 0, vn = 0;
+        int stage = 0, last_stage = 0, formed = 0, added = 0, kt = 0, vt = -1, kn = 0, vn = 0; // blocks; the next tile; blocks left of the tiles begun
         uint32_t phase = 0;
-        bool ok = true;
-        const auto form = [&] { // false at the end
-            if (kn == 0) {
-                ++kt;
-                ok = ok && bar_wait_cta(tile_full(kt), kt / kTiles & 1, &gave_up);
-                if (!ok) return false;
+        bool more = true, fresh = false; // blocks to come; the tile that stays has not been waited for
+        Idle idle;
+        while (more || added < formed) {
+            bool went = false;
+            if (more && kn == 0 && bar_test_cta(tile_full(kt), kt / kTiles & 1)) {
                 kn = tiles[kt % kTiles].count;
-                if (kn == 0) return false;
-                ok = bar_wait_cta(stay_full, kt & 1, &gave_up);
+                more = kn > 0;
+                fresh = true;
+                ++kt;
             }
-            ok = ok && bar_wait_cta(full(stage), phase, &gave_up);
-            if (!ok) return false;
-            fence_after();
-            --kn;
-            if (chosen) {
-                const uint32_t s = tmem + 128 * (formed % kBuffers);
-                const uint64_t b0 = operand_desc(ring + stage * Shape::kStage, 16), b1 = operand_desc(ring + stage * Shape::kStage + kSlice, 16);
+            // S and dP of the next block, where their places are free
+            if (kn > 0 && formed < added + kBuffers && (formed < kBuffers || bar_test_cta(out_done(formed), (formed / kBuffers + 1) & 1)) &&
+                bar_test_cta(full(stage), phase) && (!fresh || bar_test_cta(stay_full, (kt & 1) ^ 1))) {
+                fresh = false;
+                went = true;
+                fence_after();
+                --kn;
+                if (chosen) {
+                    const uint32_t s = tmem + 128 * (formed % kBuffers);
+                    const uint64_t b0 = operand_desc(ring + stage * Shape::kStage, 16), b1 = operand_desc(ring + stage * Shape::kStage + kSlice, 16);
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) { // 64 elements a chunk
-                    const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
-                    if (j < steps) mma_ss(s, d0 + oa, b0 + ob, desc_s, j > 0);
-                }
-                if (with0) {
-#pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
+                    for (int j = 0; j < D / 16; ++j) { // 64 elements a chunk
                         const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
-                        if (j < steps) mma_ss(s + 64, d1 + oa, b1 + ob, desc_s, j > 0);
+                        if (j < steps) mma_ss(s, d0 + oa, b0 + ob, desc_s, j > 0);
+                    }
+                    if (with0) {
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j) {
+                            const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
+                            if (j < steps) mma_ss(s + 64, d1 + oa, b1 + ob, desc_s, j > 0);
+                        }
+                    }
+                    commit(s_full(formed));
+                    if (kn == 0) commit(stay_empty);
+                }
+                __syncwarp();
+                ++formed;
+                if (++stage == kStages) stage = 0, phase ^= 1u;
+            }
+            // the outputs' share of the oldest block
+            if (added < formed && bar_test_cta(p_full(added), added / kBuffers & 1) && (vn > 0 || bar_test_cta(out_empty, vt & 1))) {
+                went = true;
+                fence_after();
+                const bool first = vn == 0;
+                if (first) vn = tiles[++vt % kTiles].count; // the last tile's outputs have been read
+                --vn;
+                if (chosen) {
+                    const uint32_t s = tmem + 128 * (added % kBuffers), ds = KEYS ? s + 64 : s;
+                    const uint64_t b0 = operand_desc(ring + last_stage * Shape::kStage, 8192), b1 = operand_desc(ring + last_stage * Shape::kStage + kSlice, 8192);
+                    if (with1) {
+#pragma unroll
+                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 8 * j, b1 + j * (2048 >> 4), desc_o, !first || j > 0);
+                    }
+                    if (with0) {
+#pragma unroll
+                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 8 * j, b0 + j * (2048 >> 4), desc_o, !first || j > 0);
+                    }
+                    commit(out_done(added));
+                    commit(empty(last_stage));
+                    if (vn == 0) {
+                        commit(out_full);
+                        bar_arrive(tile_empty(vt));
                     }
                 }
-                commit(s_full(formed));
-                if (kn == 0) commit(stay_empty);
+                __syncwarp();
+                ++added;
+                if (++last_stage == kStages) last_stage = 0;
             }
-            __syncwarp();
-            ++formed;
-            if (++stage == kStages) stage = 0, phase ^= 1u;
-            return true;
-        };
-        bool more = form() && (kBuffers == 1 || form());
-        for (int g = 0; ok && g < formed; ++g) {
-            const bool first = vn == 0;
-            if (first) {
-                vn = tiles[++vt % kTiles].count;
-                ok = bar_wait_cta(out_empty, (vt & 1) ^ 1, &gave_up); // the last tile's outputs have been read
-            }
-            ok = ok && bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
-            if (!ok) break;
-            fence_after();
-            --vn;
-            if (chosen) {
-                const uint32_t s = tmem + 128 * (g % kBuffers), ds = KEYS ? s + 64 : s;
-                const uint64_t b0 = operand_desc(ring + last_stage * Shape::kStage, 8192), b1 = operand_desc(ring + last_stage * Shape::kStage + kSlice, 8192);
-                if (with1) {
-#pragma unroll
-                    for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 8 * j, b1 + j * (2048 >> 4), desc_o, !first || j > 0);
-                }
-                if (with0) {
-#pragma unroll
-                    for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 8 * j, b0 + j * (2048 >> 4), desc_o, !first || j > 0);
-                }
-                commit(out_done);
-                commit(empty(last_stage));
-                if (vn == 0) {
-                    commit(out_full);
-                    bar_arrive(tile_empty(vt));
-                }
-            }
-            __syncwarp();
-            if (++last_stage == kStages) last_stage = 0;
-            if (more) {
-                ok = bar_wait_cta(out_done, g & 1, &gave_up); // P and dS have been read where the next S and dP go
-                more = form();
-            }
+            if (!idle.go_on(went, &gave_up)) break;
         }
     } else {
         // ---------------------------------------------------------- P and dS, a thread a row
-        const int buffer = warp >> 2, quarter = warp & 3;
-        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), ts = lanes + 128 * buffer;
+        const int group = warp >> 2, quarter = warp & 3;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         const float c = a.scale_log2;
         int g = 0; // blocks so far
         for (int vt = 0;; ++vt) {
@@ -884,7 +907,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, BackwardShap
                 delta = a.delta[line];
             }
             for (int n = 0; n < tile.count; ++n, ++g) {
-                if (kBuffers > 1 && (g & 1) != buffer) continue;
+                if (g % kGroups != group) continue;
+                const uint32_t ts = lanes + 128 * (g % kBuffers);
                 const int g0 = KEYS ? tile.first + (tile.begin + n) / a.group * 64 : tile.blocks[n] * kBlock; // first query (KEYS) or key
                 const int stage = g % kStages;
                 if (KEYS) bar_pass_cta(full(stage), g / kStages & 1, &gave_up);
@@ -948,31 +972,26 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, BackwardShap
             }
             bar_pass_cta(out_full, vt & 1, &gave_up);
             fence_after();
-            // the outputs: KEYS: dK and dV, one a group where there are two; else dQ, half of the elements a group
+            // the outputs, 32 columns of each a group of warps in turn
             const uint32_t to = lanes + Shape::kOut;
             const bool partial = KEYS && a.parts > 1 && live && place < a.sinks; // another part of this tile has some, too
-            constexpr int kOuts = KEYS ? 2 : 1, kSpan = !KEYS && kBuffers == 2 ? D / 2 : D;
-            const int o0 = KEYS && kBuffers == 2 ? buffer : 0, o1 = KEYS && kBuffers == 2 ? buffer + 1 : kOuts;
-            const int c0 = !KEYS && kBuffers == 2 ? buffer * kSpan : 0, c1 = min(a.d, c0 + kSpan);
 #pragma unroll 1
-            for (int o = o0; o < o1; ++o) {
+            for (int i = group; i < (KEYS ? 2 : 1) * (D / 32); i += kGroups) {
+                const int o = i / (D / 32), cc = i % (D / 32) * 32;
                 const Heads &h = o ? a.out1 : a.out0;
-                if (!h.p) continue;
+                if (!h.p || cc >= a.d) continue;
                 const float factor = o ? 1.0f : a.scale;
-#pragma unroll 1
-                for (int cc = c0; cc < c1; cc += 32) {
-                    float v[32];
-                    tmem_ld32(to + D * o + cc, v);
-                    tmem_wait_ld();
+                float v[32];
+                tmem_ld32(to + D * o + cc, v);
+                tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= factor;
-                    if (partial) {
-                        float *q = a.partials + ((((int64_t)(tile.seq * a.kv_heads + tile.head) * a.sink_rows + place) * a.parts + tile.part) * 2 + o) * D + cc;
+                for (int k = 0; k < 32; ++k) v[k] *= factor;
+                if (partial) {
+                    float *q = a.partials + ((((int64_t)(tile.seq * a.kv_heads + tile.head) * a.sink_rows + place) * a.parts + tile.part) * 2 + o) * D + cc;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(q + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                    } else if (live && tile.part == 0) {
-                        store_row(at<T>(h, tile.seq, tile.row + row, tile.head) + cc, v, c1 - cc, o ? a.wide1 : a.wide0);
-                    }
+                    for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4 *>(q + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                } else if (live && tile.part == 0) {
+                    store_row(at<T>(h, tile.seq, tile.row + row, tile.head) + cc, v, a.d - cc, o ? a.wide1 : a.wide0);
                 }
             }
             fence_before();
@@ -1018,43 +1037,51 @@ __global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ Backw
     }
 }
 
-// lse in units of log 2 and delta of every query: sixteen lanes a query and head.
-template <typename T>
+// lse in units of log 2 and delta of every query: eight or sixteen lanes a query and head; a CTA takes 16 rows of a plane.
+constexpr int kDeltaRows = 16;
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_delta(const __grid_constant__ DeltaArgs a)
 {
     wait_prior_grid();
     release_next_grid();
-    const int lane = threadIdx.x & 15;
-    const int64_t all = (int64_t)a.planes * a.rows * a.heads;
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < (all + 1) / 2 * 2; i += (int64_t)gridDim.x * 16) {
-        const int64_t flat = i / a.heads, plane = flat / a.rows, row = flat - plane * a.rows;
-        const int head = (int)(i - flat * a.heads);
-        float sum = 0.0f;
-        if (i < all) {
+    constexpr int kEach = 256 / LANES, kAhead = 4; // queries at a time, whose reads come before their sums
+    const int lane = threadIdx.x % LANES, plane = blockIdx.x / a.blocks;
+    const int64_t row0 = (int64_t)(blockIdx.x % a.blocks) * kDeltaRows;
+    const int count = (int)min((int64_t)kDeltaRows, a.rows - row0) * a.heads;
+    for (int i0 = threadIdx.x / LANES; i0 - (int)threadIdx.x / LANES < count; i0 += kEach * kAhead) {
+        Raw8<T> x[kAhead], y[kAhead];
+        float sum[kAhead] = {};
+        int64_t line[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int i = min(i0 + e * kEach, count - 1), r = i / a.heads, head = i - r * a.heads;
+            const int64_t row = row0 + r;
             const T *o = static_cast<const T *>(a.o.p) + plane * a.o.seq + row * a.o.row + (int64_t)head * a.o.head;
             const T *g = static_cast<const T *>(a.dout.p) + plane * a.dout.seq + row * a.dout.row + (int64_t)head * a.dout.head;
+            line[e] = ((int64_t)plane * a.heads + head) * a.rows + row;
             if (a.wide) {
-                if (lane * 8 < a.d) {
-                    Raw8<T> x, y;
-                    float u[8], v[8];
-                    x.load(o + lane * 8);
-                    y.load(g + lane * 8);
-                    x.unpack(u);
-                    y.unpack(v);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) sum = fmaf(u[k], v[k], sum);
-                }
+                if (lane * 8 < a.d) x[e].load(o + lane * 8), y[e].load(g + lane * 8);
+                else x[e].zero(), y[e].zero();
             } else {
-                for (int c = lane; c < a.d; c += 16) sum = fmaf(to_f32(o[c]), to_f32(g[c]), sum);
+                for (int c = lane; c < a.d; c += LANES) sum[e] = fmaf(to_f32(o[c]), to_f32(g[c]), sum[e]);
             }
         }
 #pragma unroll
-        for (int s = 8; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-        if (lane == 0 && i < all) {
-            const int64_t line = (plane * a.heads + head) * a.rows + row;
-            const float l = a.lse[line];
-            a.lse2[line] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
-            a.delta[line] = sum;
+        for (int e = 0; e < kAhead; ++e) {
+            if (a.wide) {
+                float u[8], v[8];
+                x[e].unpack(u);
+                y[e].unpack(v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[e] = fmaf(u[k], v[k], sum[e]);
+            }
+#pragma unroll
+            for (int s = LANES / 2; s; s >>= 1) sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], s);
+            if (lane == 0 && i0 + e * kEach < count) {
+                const float l = a.lse[line[e]];
+                a.lse2[line[e]] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
+                a.delta[line[e]] = sum[e];
+            }
         }
     }
 }
@@ -1305,7 +1332,7 @@ int launch_backward(BackwardArgs &b, int64_t rows, int sms, cudaStream_t s)
     const void *fn = reinterpret_cast<const void *>(&k_backward<T, D, KEYS>);
     A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
     void *params[] = {&b};
-    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)std::min<int64_t>(items, (int64_t)sms * Shape::kCtas)), Shape::kThreads, Shape::kSmem, params, s));
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)std::min<int64_t>(items, sms)), Shape::kThreads, Shape::kSmem, params, s));
     return A2SGD_OK;
 }
 
@@ -1367,11 +1394,14 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
         d.lse = lse;
         d.lse2 = lse2, d.delta = delta;
         d.rows = q.rows;
-        d.planes = packed_q ? 1 : (int)shape->sequences;
+        const int64_t planes = packed_q ? 1 : (int64_t)shape->sequences, blocks = (q.rows + kDeltaRows - 1) / kDeltaRows;
+        if (planes * blocks > 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
+        d.blocks = (int)blocks;
         d.heads = q.heads, d.d = q.d;
         d.wide = wide(o) && wide(dout);
         void *params[] = {&d};
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_delta<T>), dim3((unsigned)std::min<uint64_t>((lines + 15) / 16, (uint64_t)sms * 16)), 256, 0, params, s));
+        const void *fn = q.d <= 64 ? reinterpret_cast<const void *>(&k_delta<T, 8>) : reinterpret_cast<const void *>(&k_delta<T, 16>);
+        A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(planes * blocks)), 256, 0, params, s));
     }
     const Parts parts = parts_of(shape);
     b.q_ranges = shape->q_ranges, b.k_ranges = shape->k_ranges;
