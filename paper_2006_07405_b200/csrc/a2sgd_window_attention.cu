@@ -38,7 +38,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ forward
 // Persistent CTAs, two an SM, deal out the tiles of 128 queries of one head, the longest first.  For each tile a CTA walks the blocks of 64
-// keys that any of its queries sees: the first tokens' blocks, then those of the window.  One warp brings tiles in by TMA, one issues the
+// keys that any of its queries sees: the first tokens' blocks, then those of the window.  One warp brings tiles in by TMA, two issue the
 // products, four hold the softmax, a thread a query.
 //   S = Q K^T into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  O += P V, P read from TMEM.
 // Three buffers of S (two where O has 128 columns): the next block's, be it the next tile's, is formed while the present one's P is.
@@ -60,9 +60,9 @@ struct ForwardArgs {
 constexpr int kBlock = 64; // keys
 template <int D>
 struct ForwardShape {
-    static constexpr int kThreads = 192, kCtas = 2, kStages = D == 64 ? 8 : 4;
+    static constexpr int kThreads = 256, kCtas = 2, kStages = D == 64 ? 4 : 2; // of keys, and of values
     static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u; // 128 rows, 64 rows
-    static constexpr uint32_t kSmem = kTile + kStages * kSlice + 1024;
+    static constexpr uint32_t kSmem = kTile + 2 * kStages * kSlice + 1024;
     static constexpr int kBuffers = D == 64 ? 3 : 2; // of S
     static constexpr uint32_t kColumns = 256, kO = 64 * kBuffers;
 };
@@ -182,24 +182,6 @@ __device__ __forceinline__ float exponentials(const float (&x)[32], float c, flo
     return sum2(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])));
 }
 
-// A warp that looks for work in turn: how long it has found none.
-struct Idle {
-    uint32_t polls = 0;
-    uint64_t begin = 0;
-    __device__ __forceinline__ bool go_on(bool went, volatile int *gave_up)
-    {
-        if (went) {
-            polls = 0;
-            return true;
-        }
-        if ((++polls & 255u) != 0u) return true;
-        if (polls == 256u) begin = now_ns();
-        if (!__any_sync(0xffffffffu, *gave_up || now_ns() - begin > kWaitLimitNs)) return true;
-        *gave_up = 1;
-        return false;
-    }
-};
-
 // A tile: whose it is, its queries and the blocks of keys that they see.  The loading warp works them out and leaves them in shared memory.
 struct Tile {
     int seq, head, p0, rows;     // place of the first query; queries, at least 1
@@ -243,14 +225,15 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     constexpr uint32_t kSlice = Shape::kSlice;
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + Shape::kTile;
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 5 + 3 * kBuffers];
+    __shared__ __align__(8) uint64_t bars[4 * kStages + 2 * kTiles + 5 + 3 * kBuffers];
     __shared__ Tile tiles[kTiles];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
     const uint32_t bar0 = smem_u32(bars);
+    // keys' stages, then values'
     const auto full = [&](int s) { return bar0 + 8u * s; };
-    const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
-    const uint32_t tile0 = bar0 + 16u * kStages, more0 = tile0 + 16u * kTiles;
+    const auto empty = [&](int s) { return bar0 + 8u * (2 * kStages + s); };
+    const uint32_t tile0 = bar0 + 32u * kStages, more0 = tile0 + 16u * kTiles;
     const auto tile_full = [&](int t) { return tile0 + 8u * (t % kTiles); };
     const auto tile_empty = [&](int t) { return tile0 + 8u * (kTiles + t % kTiles); };
     const uint32_t q_full = more0, q_empty = more0 + 8, tail = more0 + 16, o_full = more0 + 24, o_empty = more0 + 32;
@@ -260,7 +243,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < 2 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
+        for (int s = 0; s < 4 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
         for (int t = 0; t < kTiles; ++t) {
             bar_init(tile_full(t), 1);
             bar_init(tile_empty(t), 5);
@@ -288,18 +271,20 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     if (warp == 4) {
         // ---------------------------------------------------------- tiles in: keys two blocks ahead of values
         const bool chosen = elect_one();
-        int stage = 0, item = blockIdx.x - gridDim.x, kt = -1, vt = -1; // tiles begun
-        uint32_t phase = 0, tails = 0;
+        int item = blockIdx.x - gridDim.x, kt = -1, vt = -1, kb = 0, vb = 0; // tiles begun, blocks
+        uint32_t tails = 0;
         bool ok = true;
         Tile k, v;
         int kn = 0, vn = 0;
         k.blocks.count = v.blocks.count = 0;
-        const auto bring = [&](const CUtensorMap *map, int planes, const Tile &t, int n, bool clear) {
-            ok = ok && bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
+        // block `count` of keys or values
+        const auto bring = [&](const CUtensorMap *map, int planes, const Tile &t, int n, int count, bool values) {
+            const int stage = (values ? kStages : 0) + count % kStages;
+            ok = ok && bar_wait_cta(empty(stage), (count / kStages & 1) ^ 1, &gave_up);
             if (!ok) return;
             const uint32_t dst = ring + stage * kSlice;
             const int block = t.blocks[n], valid = t.k_count - block * kBlock;
-            clear = clear && a.k_ranges && valid < kBlock;
+            const bool clear = values && a.k_ranges && valid < kBlock;
             const uint32_t bar = clear ? tail : full(stage);
             if (chosen) {
                 bar_expect(bar, kSlice);
@@ -314,7 +299,6 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                 if (chosen) bar_arrive(full(stage));
                 __syncwarp();
             }
-            if (++stage == kStages) stage = 0, phase ^= 1u;
         };
         // a block of keys, with the tile and its queries where it is the first; false at the end
         const auto bring_k = [&] {
@@ -349,8 +333,9 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                 }
                 __syncwarp();
             }
-            bring(&a.k, a.k_planes, k, kn, false);
+            bring(&a.k, a.k_planes, k, kn, kb, false);
             ++kn;
+            ++kb;
             return true;
         };
         bool keys = bring_k() && bring_k();
@@ -361,86 +346,80 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                 vn = 0;
                 if (v.rows == 0) break;
             }
-            bring(&a.v, a.v_planes, v, vn, true);
+            bring(&a.v, a.v_planes, v, vn, vb, true);
             ++vn;
+            ++vb;
             keys = keys && ok && bring_k();
         }
         // every tile has been consumed: nothing is in flight towards this CTA any more
-        for (int s = 0; ok && s < kStages; ++s) {
-            ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
-            if (++stage == kStages) stage = 0, phase ^= 1u;
+        for (int s = 0; s < kStages; ++s) {
+            ok = ok && bar_wait_cta(empty((kb + s) % kStages), ((kb + s) / kStages & 1) ^ 1, &gave_up);
+            ok = ok && bar_wait_cta(empty(kStages + (vb + s) % kStages), ((vb + s) / kStages & 1) ^ 1, &gave_up);
         }
     } else if (warp == 5) {
-        // ---------------------------------------------------------- products: whichever can go, so that they do not pause
+        // ---------------------------------------------------------- S = Q K^T, as far ahead as there are buffers
         const bool chosen = elect_one();
         const int steps = (a.d + 15) / 16; // of 16 elements of the head
-        const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
-        const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
+        const uint32_t desc = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
         const uint64_t dq = operand_desc(base, 16);
-        // tiles are consumed in the order in which they were loaded: K, K, then V and K in turn (the loading warp's order)
-        int stage = 0, formed = 0, added = 0, kt = 0, vt = -1, kn = 0, vn = 0; // blocks; the next tile; blocks left of the tiles begun
-        uint32_t phase = 0;
-        bool more = true, fresh = false; // keys to come; the tile's queries have not been waited for
-        Idle idle;
-        const auto next = [&] {
-            if (++stage == kStages) stage = 0, phase ^= 1u;
-        };
-        while (more || added < formed) {
-            bool went = false;
-            if (more && kn == 0 && bar_test_cta(tile_full(kt), kt / kTiles & 1)) {
-                kn = tiles[kt % kTiles].blocks.count;
-                more = kn > 0;
-                fresh = true;
-                ++kt;
-            }
-            // S of the next block: where its place is free, and its keys have come, which lie behind V of two blocks before
-            if (kn > 0 && formed < added + 2 && (formed < kBuffers || bar_test_cta(pv_done(formed), (formed / kBuffers + 1) & 1)) && bar_test_cta(full(stage), phase) &&
-                (!fresh || bar_test_cta(q_full, (kt & 1) ^ 1))) {
-                fresh = false;
-                went = true;
+        int g = 0;
+        bool ok = true;
+        for (int t = 0; ok; ++t) {
+            ok = bar_wait_cta(tile_full(t), t / kTiles & 1, &gave_up);
+            const int count = ok ? tiles[t % kTiles].blocks.count : 0;
+            if (count == 0) break;
+            ok = bar_wait_cta(q_full, t & 1, &gave_up);
+            for (int n = 0; ok && n < count; ++n, ++g) {
+                const int stage = g % kStages;
+                ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up);
+                if (g >= kBuffers) ok = ok && bar_wait_cta(pv_done(g), (g / kBuffers + 1) & 1, &gave_up); // P has been read where S goes
+                if (!ok) break;
                 fence_after();
-                --kn;
                 if (chosen) {
                     const uint64_t dk = operand_desc(ring + stage * kSlice, 16);
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) // 64 elements a chunk
                         if (j < steps)
-                            mma_ss(tmem + 64 * (formed % kBuffers), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc_s, j > 0);
-                    commit(s_full(formed));
+                            mma_ss(tmem + 64 * (g % kBuffers), dq + (((j >> 2) * 16384u + (j & 3) * 32u) >> 4), dk + (((j >> 2) * 8192u + (j & 3) * 32u) >> 4), desc, j > 0);
+                    commit(s_full(g));
                     commit(empty(stage));
-                    if (kn == 0) commit(q_empty);
+                    if (n + 1 == count) commit(q_empty);
                 }
                 __syncwarp();
-                ++formed;
-                next();
             }
-            // O += P V of the oldest block
-            if (added < formed && (formed == added + 2 || !more) && bar_test_cta(p_full(added), added / kBuffers & 1) && bar_test_cta(full(stage), phase) &&
-                (vn > 0 || bar_test_cta(o_empty, vt & 1))) {
-                went = true;
+        }
+    } else if (warp == 6) {
+        // ---------------------------------------------------------- O += P V
+        const bool chosen = elect_one();
+        const uint32_t desc = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * ((a.d + 15) / 16)) << 17;
+        int g = 0;
+        bool ok = true;
+        for (int t = 0; ok; ++t) {
+            ok = bar_wait_cta(tile_full(t), t / kTiles & 1, &gave_up);
+            const int count = ok ? tiles[t % kTiles].blocks.count : 0;
+            if (count == 0) break;
+            ok = bar_wait_cta(o_empty, (t & 1) ^ 1, &gave_up); // the last tile's output has been read
+            for (int n = 0; ok && n < count; ++n, ++g) {
+                const int stage = kStages + g % kStages;
+                ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up) && bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
+                if (!ok) break;
                 fence_after();
-                const bool first = vn == 0;
-                if (first) vn = tiles[++vt % kTiles].blocks.count; // the last tile's output has been read
-                --vn;
                 if (chosen) {
                     const uint64_t dv = operand_desc(ring + stage * kSlice, 8192);
 #pragma unroll
                     for (int j = 0; j < kBlock / 16; ++j)
-                        mma_ts(tmem + Shape::kO, tmem + 64 * (added % kBuffers) + 8 * j, dv + j * (2048 >> 4), desc_o, !first || j > 0);
-                    commit(pv_done(added));
+                        mma_ts(tmem + Shape::kO, tmem + 64 * (g % kBuffers) + 8 * j, dv + j * (2048 >> 4), desc, n > 0 || j > 0);
+                    commit(pv_done(g));
                     commit(empty(stage));
-                    if (vn == 0) {
+                    if (n + 1 == count) {
                         commit(o_full);
-                        bar_arrive(tile_empty(vt));
+                        bar_arrive(tile_empty(t));
                     }
                 }
                 __syncwarp();
-                ++added;
-                next();
             }
-            if (!idle.go_on(went, &gave_up)) break;
         }
-    } else {
+    } else if (warp < 4) {
         // ---------------------------------------------------------- softmax, a thread a query
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16), to = lanes + Shape::kO;
         const float c = a.scale_log2;
@@ -600,7 +579,7 @@ struct BackwardArgs {
 };
 template <int D, bool KEYS>
 struct BackwardShape {
-    static constexpr int kBuffers = KEYS && D == 128 ? 2 : 3, kGroups = 2, kThreads = 128 * kGroups + 64;
+    static constexpr int kBuffers = KEYS && D == 128 ? 2 : 3, kGroups = 2, kThreads = 128 * kGroups + 128;
     static constexpr int kStages = D == 64 ? 8 : 4;
     static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u, kStage = 2 * kSlice; // 128 rows, 64 rows, both tensors' 64
     static constexpr uint32_t kSmem = 2 * kTile + kStages * kStage + 1024;
@@ -671,7 +650,7 @@ template <typename T, int D, bool KEYS>
 __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backward(const __grid_constant__ BackwardArgs a)
 {
     using Shape = BackwardShape<D, KEYS>;
-    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kGroups = Shape::kGroups, kLoad = 4 * kGroups, kProducts = kLoad + 1;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kGroups = Shape::kGroups, kLoad = 4 * kGroups, kForm = kLoad + 1, kAdd = kLoad + 2;
     constexpr uint32_t kSlice = Shape::kSlice, kTile = Shape::kTile;
     extern __shared__ char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * kTile;
@@ -708,7 +687,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
         gave_up = 0;
         bar_init_fence();
     }
-    if (warp == kProducts) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
+    if (warp == kForm) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
     const int beyond = (int)threadIdx.x - 32 * kLoad;
     if (beyond >= 0 && beyond < 4 && a.q_rows > 0 && a.k_rows > 0) tma_prefetch_map(beyond == 0 ? &a.stay0 : beyond == 1 ? &a.stay1 : beyond == 2 ? &a.pass0 : &a.pass1);
     fence_before();
@@ -759,23 +738,29 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 }
             }
             __syncwarp();
+            int member = KEYS ? t.begin % a.group : 0, block = KEYS ? t.begin / a.group : 0; // KEYS: of the key head's query heads; of queries
             for (int n = 0; ok && n < t.count; ++n) {
-                ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
-                if (!ok) break;
-                const int it = t.begin + n;
-                const int head = KEYS ? t.head * a.group + it % a.group : t.head / a.group;
-                const int at_row = KEYS ? t.first + it / a.group * 64 : t.blocks[n] * kBlock; // in the sequence
+                const int head = KEYS ? t.head * a.group + member : t.head / a.group;
+                const int at_row = KEYS ? t.first + block * 64 : t.blocks[n] * kBlock; // in the sequence
                 const int row = (KEYS ? t.q_row : t.k_row) + at_row, valid = (KEYS ? t.q_count : t.k_count) - at_row;
                 const uint32_t dst = ring + stage * Shape::kStage;
                 const bool clear = (KEYS ? a.q_ranges : a.k_ranges) && valid < kBlock;
+                float lines[2][2]; // on their way while the stage is waited for
                 if (KEYS) {
                     const int64_t line = ((int64_t)(a.packed_q ? 0 : t.seq) * a.q_heads + head) * a.q_rows + row;
 #pragma unroll
-                    for (int i = 0; i < 64; i += 32) {
-                        const bool in = i + lane < valid;
-                        columns[stage][0][i + lane] = in ? a.lse2[line + i + lane] : INFINITY;
-                        columns[stage][1][i + lane] = in ? a.delta[line + i + lane] : 0.0f;
+                    for (int i = 0; i < 2; ++i) {
+                        const bool in = 32 * i + lane < valid;
+                        lines[0][i] = in ? a.lse2[line + 32 * i + lane] : INFINITY;
+                        lines[1][i] = in ? a.delta[line + 32 * i + lane] : 0.0f;
                     }
+                    if (++member == a.group) member = 0, ++block;
+                }
+                ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
+                if (!ok) break;
+                if (KEYS) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) columns[stage][0][32 * i + lane] = lines[0][i], columns[stage][1][32 * i + lane] = lines[1][i];
                     __syncwarp();
                 }
                 const uint32_t bar = clear ? tail : full(stage);
@@ -803,87 +788,86 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
             if (++stage == kStages) stage = 0, phase ^= 1u;
         }
-    } else if (warp == kProducts) {
-        // ---------------------------------------------------------- products: whichever can go, so that they do not pause
+    } else if (warp == kForm) {
+        // ---------------------------------------------------------- S and dP, as far ahead as there are buffers
         const bool chosen = elect_one();
         const int steps = (a.d + 15) / 16;
-        const uint32_t desc_s = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
-        const uint32_t desc_o = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * steps) << 17;
+        const uint32_t desc = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
         const uint64_t d0 = operand_desc(base, 16), d1 = operand_desc(base + kTile, 16);
-        const bool with0 = a.out0.p != nullptr, with1 = KEYS && a.out1.p != nullptr;
-        int stage = 0, last_stage = 0, formed = 0, added = 0, kt = 0, vt = -1, kn = 0, vn = 0; // blocks; the next tile; blocks left of the tiles begun
-        uint32_t phase = 0;
-        bool more = true, fresh = false; // blocks to come; the tile that stays has not been waited for
-        Idle idle;
-        while (more || added < formed) {
-            bool went = false;
-            if (more && kn == 0 && bar_test_cta(tile_full(kt), kt / kTiles & 1)) {
-                kn = tiles[kt % kTiles].count;
-                more = kn > 0;
-                fresh = true;
-                ++kt;
-            }
-            // S and dP of the next block, where their places are free
-            if (kn > 0 && formed < added + kBuffers && (formed < kBuffers || bar_test_cta(out_done(formed), (formed / kBuffers + 1) & 1)) &&
-                bar_test_cta(full(stage), phase) && (!fresh || bar_test_cta(stay_full, (kt & 1) ^ 1))) {
-                fresh = false;
-                went = true;
+        const bool with0 = a.out0.p != nullptr;
+        int g = 0;
+        bool ok = true;
+        for (int t = 0; ok; ++t) {
+            ok = bar_wait_cta(tile_full(t), t / kTiles & 1, &gave_up);
+            const int count = ok ? tiles[t % kTiles].count : 0;
+            if (count == 0) break;
+            ok = bar_wait_cta(stay_full, t & 1, &gave_up);
+            for (int n = 0; ok && n < count; ++n, ++g) {
+                const int stage = g % kStages;
+                ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up);
+                if (g >= kBuffers) ok = ok && bar_wait_cta(out_done(g), (g / kBuffers + 1) & 1, &gave_up); // P and dS have been read where S and dP go
+                if (!ok) break;
                 fence_after();
-                --kn;
                 if (chosen) {
-                    const uint32_t s = tmem + 128 * (formed % kBuffers);
+                    const uint32_t s = tmem + 128 * (g % kBuffers);
                     const uint64_t b0 = operand_desc(ring + stage * Shape::kStage, 16), b1 = operand_desc(ring + stage * Shape::kStage + kSlice, 16);
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) { // 64 elements a chunk
                         const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
-                        if (j < steps) mma_ss(s, d0 + oa, b0 + ob, desc_s, j > 0);
+                        if (j < steps) mma_ss(s, d0 + oa, b0 + ob, desc, j > 0);
                     }
                     if (with0) {
 #pragma unroll
                         for (int j = 0; j < D / 16; ++j) {
                             const uint32_t oa = ((j >> 2) * 16384u + (j & 3) * 32u) >> 4, ob = ((j >> 2) * 8192u + (j & 3) * 32u) >> 4;
-                            if (j < steps) mma_ss(s + 64, d1 + oa, b1 + ob, desc_s, j > 0);
+                            if (j < steps) mma_ss(s + 64, d1 + oa, b1 + ob, desc, j > 0);
                         }
                     }
-                    commit(s_full(formed));
-                    if (kn == 0) commit(stay_empty);
+                    commit(s_full(g));
+                    if (n + 1 == count) commit(stay_empty);
                 }
                 __syncwarp();
-                ++formed;
-                if (++stage == kStages) stage = 0, phase ^= 1u;
             }
-            // the outputs' share of the oldest block
-            if (added < formed && bar_test_cta(p_full(added), added / kBuffers & 1) && (vn > 0 || bar_test_cta(out_empty, vt & 1))) {
-                went = true;
+        }
+    } else if (warp == kAdd) {
+        // ---------------------------------------------------------- the outputs
+        const bool chosen = elect_one();
+        const uint32_t desc = instruction_desc(type_bits<T>(), false, true, 128, 0) | (uint32_t)(2 * ((a.d + 15) / 16)) << 17;
+        const bool with0 = a.out0.p != nullptr, with1 = KEYS && a.out1.p != nullptr;
+        int g = 0;
+        bool ok = true;
+        for (int t = 0; ok; ++t) {
+            ok = bar_wait_cta(tile_full(t), t / kTiles & 1, &gave_up);
+            const int count = ok ? tiles[t % kTiles].count : 0;
+            if (count == 0) break;
+            ok = bar_wait_cta(out_empty, (t & 1) ^ 1, &gave_up); // the last tile's outputs have been read
+            for (int n = 0; ok && n < count; ++n, ++g) {
+                const int stage = g % kStages;
+                ok = bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
+                if (!ok) break;
                 fence_after();
-                const bool first = vn == 0;
-                if (first) vn = tiles[++vt % kTiles].count; // the last tile's outputs have been read
-                --vn;
                 if (chosen) {
-                    const uint32_t s = tmem + 128 * (added % kBuffers), ds = KEYS ? s + 64 : s;
-                    const uint64_t b0 = operand_desc(ring + last_stage * Shape::kStage, 8192), b1 = operand_desc(ring + last_stage * Shape::kStage + kSlice, 8192);
+                    const uint32_t s = tmem + 128 * (g % kBuffers), ds = KEYS ? s + 64 : s;
+                    const uint64_t b0 = operand_desc(ring + stage * Shape::kStage, 8192), b1 = operand_desc(ring + stage * Shape::kStage + kSlice, 8192);
                     if (with1) {
 #pragma unroll
-                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 8 * j, b1 + j * (2048 >> 4), desc_o, !first || j > 0);
+                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 8 * j, b1 + j * (2048 >> 4), desc, n > 0 || j > 0);
                     }
                     if (with0) {
 #pragma unroll
-                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 8 * j, b0 + j * (2048 >> 4), desc_o, !first || j > 0);
+                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 8 * j, b0 + j * (2048 >> 4), desc, n > 0 || j > 0);
                     }
-                    commit(out_done(added));
-                    commit(empty(last_stage));
-                    if (vn == 0) {
+                    commit(out_done(g));
+                    commit(empty(stage)); // S and dP, which had read it, too, are done: P came of them
+                    if (n + 1 == count) {
                         commit(out_full);
-                        bar_arrive(tile_empty(vt));
+                        bar_arrive(tile_empty(t));
                     }
                 }
                 __syncwarp();
-                ++added;
-                if (++last_stage == kStages) last_stage = 0;
             }
-            if (!idle.go_on(went, &gave_up)) break;
         }
-    } else {
+    } else if (warp < kLoad) {
         // ---------------------------------------------------------- P and dS, a thread a row
         const int group = warp >> 2, quarter = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -906,11 +890,16 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 lse2 = a.lse2[line];
                 delta = a.delta[line];
             }
-            for (int n = 0; n < tile.count; ++n, ++g) {
-                if (g % kGroups != group) continue;
+            const int begun = g, skip = (group + kGroups - g % kGroups) % kGroups; // this group's first block of the tile
+            int member = KEYS ? (tile.begin + skip) % a.group : 0, block = KEYS ? (tile.begin + skip) / a.group : 0;
+            for (int n = skip; n < tile.count; n += kGroups) {
+                g = begun + n;
                 const uint32_t ts = lanes + 128 * (g % kBuffers);
-                const int g0 = KEYS ? tile.first + (tile.begin + n) / a.group * 64 : tile.blocks[n] * kBlock; // first query (KEYS) or key
+                const int g0 = KEYS ? tile.first + block * 64 : tile.blocks[n] * kBlock; // first query (KEYS) or key
                 const int stage = g % kStages;
+                if (KEYS) {
+                    for (member += kGroups; member >= a.group; member -= a.group) ++block;
+                }
                 if (KEYS) bar_pass_cta(full(stage), g / kStages & 1, &gave_up);
                 bar_pass_cta(s_full(g), g / kBuffers & 1, &gave_up);
                 fence_after();
@@ -970,6 +959,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full(g));
             }
+            g = begun + tile.count;
             bar_pass_cta(out_full, vt & 1, &gave_up);
             fence_after();
             // the outputs, 32 columns of each a group of warps in turn
@@ -1007,7 +997,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
         const uint64_t begin = now_ns();
         while (now_ns() - begin < 5000000ull) __nanosleep(1000);
     }
-    if (warp == kProducts) tmem_free(tmem, Shape::kColumns);
+    if (warp == kForm) tmem_free(tmem, Shape::kColumns);
 }
 
 // The parts' sums of the first tokens' keys, in order.  A warp a key and key head.
