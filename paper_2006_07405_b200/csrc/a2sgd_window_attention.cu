@@ -561,7 +561,7 @@ struct DeltaArgs {
 // In either, with A, A' the tiles that stay and B, B' those that pass:  S = A B^T, dP = A' B'^T into TMEM; a thread reads its row, forms
 // P = exp(scale S - lse) and dS = P (dP - delta) and writes them over S and dP in 16 bits; then out += dS B, out' += P B'.
 // Roles and tiles as in the forward pass, one CTA an SM, with three buffers of S and dP (two where dK and dV of 128 elements leave no more) and
-// groups of four warps that take the blocks in turn.
+// two groups of four warps, each with half of a block.
 // The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.
 struct BackwardArgs {
     CUtensorMap stay0, stay1, pass0, pass1;
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * kTile;
     __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 5 + 3 * kBuffers];
     __shared__ BackwardTile tiles[kTiles];
-    __shared__ __align__(16) float columns[KEYS ? kStages : 1][2][64]; // KEYS: lse2 and delta of the queries that pass
+    __shared__ __align__(16) float columns[KEYS ? kStages : 1][2][64]; // KEYS: -lse2 and -delta of the queries that pass
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
     const uint32_t bar0 = smem_u32(bars);
@@ -681,7 +681,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
         bar_init(out_empty, 4 * kGroups);
         for (int i = 0; i < kBuffers; ++i) {
             bar_init(s_full(i), 1);
-            bar_init(p_full(i), 4);
+            bar_init(p_full(i), 4 * kGroups);
             bar_init(out_done(i), 1);
         }
         gave_up = 0;
@@ -760,7 +760,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 if (!ok) break;
                 if (KEYS) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) columns[stage][0][32 * i + lane] = lines[0][i], columns[stage][1][32 * i + lane] = lines[1][i];
+                    for (int i = 0; i < 2; ++i) columns[stage][0][32 * i + lane] = -lines[0][i], columns[stage][1][32 * i + lane] = -lines[1][i];
                     __syncwarp();
                 }
                 const uint32_t bar = clear ? tail : full(stage);
@@ -851,11 +851,11 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                     const uint64_t b0 = operand_desc(ring + stage * Shape::kStage, 8192), b1 = operand_desc(ring + stage * Shape::kStage + kSlice, 8192);
                     if (with1) {
 #pragma unroll
-                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 8 * j, b1 + j * (2048 >> 4), desc, n > 0 || j > 0);
+                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut + D, s + 32 * (j >> 1) + 8 * (j & 1), b1 + j * (2048 >> 4), desc, n > 0 || j > 0);
                     }
                     if (with0) {
 #pragma unroll
-                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 8 * j, b0 + j * (2048 >> 4), desc, n > 0 || j > 0);
+                        for (int j = 0; j < kBlock / 16; ++j) mma_ts(tmem + Shape::kOut, ds + 32 * (j >> 1) + 8 * (j & 1), b0 + j * (2048 >> 4), desc, n > 0 || j > 0);
                     }
                     commit(out_done(g));
                     commit(empty(stage)); // S and dP, which had read it, too, are done: P came of them
@@ -884,82 +884,73 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             const int w0 = tile.place0 + quarter * 32, w1 = w0 + 31;
             const bool live = row < tile.rows;
             const int ahead = tile.k_count - tile.q_count;
-            float lse2 = INFINITY, delta = 0.0f;
+            float minus_lse = -INFINITY, minus_delta = 0.0f;
             if (!KEYS && live) {
                 const int64_t line = ((int64_t)(a.packed_q ? 0 : tile.seq) * a.q_heads + tile.head) * a.q_rows + tile.row + row;
-                lse2 = a.lse2[line];
-                delta = a.delta[line];
+                minus_lse = -a.lse2[line];
+                minus_delta = -a.delta[line];
             }
-            const int begun = g, skip = (group + kGroups - g % kGroups) % kGroups; // this group's first block of the tile
-            int member = KEYS ? (tile.begin + skip) % a.group : 0, block = KEYS ? (tile.begin + skip) / a.group : 0;
-            for (int n = skip; n < tile.count; n += kGroups) {
-                g = begun + n;
-                const uint32_t ts = lanes + 128 * (g % kBuffers);
-                const int g0 = KEYS ? tile.first + block * 64 : tile.blocks[n] * kBlock; // first query (KEYS) or key
+            int member = KEYS ? tile.begin % a.group : 0, block = KEYS ? tile.begin / a.group : 0;
+            for (int n = 0; n < tile.count; ++n, ++g) {
+                const uint32_t ts = lanes + 128 * (g % kBuffers) + 32 * group;
+                const int o0 = (KEYS ? tile.first + block * 64 : tile.blocks[n] * kBlock) + 32 * group, o1 = o0 + 31; // this group's queries (KEYS) or keys
                 const int stage = g % kStages;
-                if (KEYS) {
-                    for (member += kGroups; member >= a.group; member -= a.group) ++block;
+                if (KEYS && ++member == a.group) member = 0, ++block;
+                bool some, all;
+                if (KEYS) { // queries at places o0 + ahead on
+                    some = o1 + ahead >= w0 && o0 < tile.q_count && (o0 + ahead - a.window < w1 || w0 < a.sinks);
+                    all = o0 + ahead >= w1 && o1 < tile.q_count && (o1 + ahead - a.window < w0 || w1 < a.sinks);
+                } else {
+                    some = o0 <= w1 && (o1 > w0 - a.window || o0 < a.sinks);
+                    all = o1 <= w0 && (o0 > w1 - a.window || o1 < a.sinks);
                 }
+                uint32_t p[16] = {}, ds[16] = {};
                 if (KEYS) bar_pass_cta(full(stage), g / kStages & 1, &gave_up);
                 bar_pass_cta(s_full(g), g / kBuffers & 1, &gave_up);
                 fence_after();
-#pragma unroll 1
-                for (int e = 0; e < 64; e += 32) {
-                    const int o0 = g0 + e, o1 = o0 + 31;
-                    bool some, all;
-                    if (KEYS) { // queries at places o0 + ahead on
-                        some = o1 + ahead >= w0 && o0 < tile.q_count && (o0 + ahead - a.window < w1 || w0 < a.sinks);
-                        all = o0 + ahead >= w1 && o1 < tile.q_count && (o1 + ahead - a.window < w0 || w1 < a.sinks);
-                    } else {
-                        some = o0 <= w1 && (o1 > w0 - a.window || o0 < a.sinks);
-                        all = o1 <= w0 && (o0 > w1 - a.window || o1 < a.sinks);
+                if (some) {
+                    float x[32], y[32];
+                    tmem_ld32(ts, x);
+                    tmem_ld32(ts + 64, y);
+                    tmem_wait_ld();
+                    const f32x2 c2 = pair(c);
+                    const float4 *l4 = reinterpret_cast<const float4 *>(&columns[KEYS ? stage : 0][0][KEYS ? 32 * group : 0]);
+                    const float4 *d4 = reinterpret_cast<const float4 *>(&columns[KEYS ? stage : 0][1][KEYS ? 32 * group : 0]);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        float4 l = make_float4(minus_lse, minus_lse, minus_lse, minus_lse), dl = make_float4(minus_delta, minus_delta, minus_delta, minus_delta);
+                        if (KEYS) l = l4[i / 4], dl = d4[i / 4];
+                        unpair(fma2(pair(x[i], x[i + 1]), c2, pair(l.x, l.y)), x[i], x[i + 1]);
+                        unpair(fma2(pair(x[i + 2], x[i + 3]), c2, pair(l.z, l.w)), x[i + 2], x[i + 3]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[i + k] = exp2_approx(x[i + k]);
+                        unpair(mul2(pair(x[i], x[i + 1]), add2(pair(y[i], y[i + 1]), pair(dl.x, dl.y))), y[i], y[i + 1]);
+                        unpair(mul2(pair(x[i + 2], x[i + 3]), add2(pair(y[i + 2], y[i + 3]), pair(dl.z, dl.w))), y[i + 2], y[i + 3]);
                     }
-                    uint32_t p[16] = {}, ds[16] = {};
-                    if (some) {
-                        float x[32], y[32];
-                        tmem_ld32(ts + e, x);
-                        tmem_ld32(ts + 64 + e, y);
-                        tmem_wait_ld();
-                        const f32x2 c2 = pair(c);
-                        const float4 *l4 = reinterpret_cast<const float4 *>(&columns[KEYS ? stage : 0][0][KEYS ? e : 0]);
-                        const float4 *d4 = reinterpret_cast<const float4 *>(&columns[KEYS ? stage : 0][1][KEYS ? e : 0]);
+                    if (!all) {
+                        uint32_t seen;
+                        if (KEYS) seen = ~below(place - ahead - o0) & below(tile.q_count - o0) & (place < a.sinks ? ~0u : below(place + a.window - ahead - o0));
+                        else seen = below(place + 1 - o0) & (~below(place - a.window + 1 - o0) | below(a.sinks - o0));
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            float4 l = make_float4(lse2, lse2, lse2, lse2), dl = make_float4(delta, delta, delta, delta);
-                            if (KEYS) l = l4[i / 4], dl = d4[i / 4];
-                            unpair(fma2(pair(x[i], x[i + 1]), c2, pair(-l.x, -l.y)), x[i], x[i + 1]);
-                            unpair(fma2(pair(x[i + 2], x[i + 3]), c2, pair(-l.z, -l.w)), x[i + 2], x[i + 3]);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) x[i + k] = exp2_approx(x[i + k]);
-                            unpair(mul2(pair(x[i], x[i + 1]), add2(pair(y[i], y[i + 1]), pair(-dl.x, -dl.y))), y[i], y[i + 1]);
-                            unpair(mul2(pair(x[i + 2], x[i + 3]), add2(pair(y[i + 2], y[i + 3]), pair(-dl.z, -dl.w))), y[i + 2], y[i + 3]);
-                        }
-                        if (!all) {
-                            uint32_t seen;
-                            if (KEYS) seen = ~below(place - ahead - o0) & below(tile.q_count - o0) & (place < a.sinks ? ~0u : below(place + a.window - ahead - o0));
-                            else seen = below(place + 1 - o0) & (~below(place - a.window + 1 - o0) | below(a.sinks - o0));
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                if (KEYS) x[i] = seen >> i & 1u ? x[i] : 0.0f;
-                                y[i] = seen >> i & 1u ? y[i] : 0.0f;
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (KEYS) p[i] = pack2(x[2 * i], x[2 * i + 1], T());
-                            ds[i] = pack2(y[2 * i], y[2 * i + 1], T());
+                        for (int i = 0; i < 32; ++i) {
+                            if (KEYS) x[i] = seen >> i & 1u ? x[i] : 0.0f;
+                            y[i] = seen >> i & 1u ? y[i] : 0.0f;
                         }
                     }
-                    // over scores that have been read
-                    if (KEYS) tmem_st16(ts + e / 2, p);
-                    tmem_st16((KEYS ? ts + 64 : ts) + e / 2, ds);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (KEYS) p[i] = pack2(x[2 * i], x[2 * i + 1], T());
+                        ds[i] = pack2(y[2 * i], y[2 * i + 1], T());
+                    }
                 }
+                // over scores that this thread has read
+                if (KEYS) tmem_st16(ts, p);
+                tmem_st16(KEYS ? ts + 64 : ts, ds);
                 tmem_wait_st();
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full(g));
             }
-            g = begun + tile.count;
             bar_pass_cta(out_full, vt & 1, &gave_up);
             fence_after();
             // the outputs, 32 columns of each a group of warps in turn
