@@ -872,7 +872,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
         const int group = warp >> 2, quarter = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         const float c = a.scale_log2;
-        int g = 0; // blocks so far
+        int buffer = 0, stage = 0;
+        uint32_t phase = 0, stage_phase = 0;
         for (int vt = 0;; ++vt) {
             bar_pass_cta(tile_full(vt), vt / kTiles & 1, &gave_up);
             if (__any_sync(0xffffffffu, gave_up)) break;
@@ -891,10 +892,9 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 minus_delta = -a.delta[line];
             }
             int member = KEYS ? tile.begin % a.group : 0, block = KEYS ? tile.begin / a.group : 0;
-            for (int n = 0; n < tile.count; ++n, ++g) {
-                const uint32_t ts = lanes + 128 * (g % kBuffers) + 32 * group;
+            for (int n = 0; n < tile.count; ++n) {
+                const uint32_t ts = lanes + 128 * buffer + 32 * group;
                 const int o0 = (KEYS ? tile.first + block * 64 : tile.blocks[n] * kBlock) + 32 * group, o1 = o0 + 31; // this group's queries (KEYS) or keys
-                const int stage = g % kStages;
                 if (KEYS && ++member == a.group) member = 0, ++block;
                 bool some, all;
                 if (KEYS) { // queries at places o0 + ahead on
@@ -904,9 +904,9 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                     some = o0 <= w1 && (o1 > w0 - a.window || o0 < a.sinks);
                     all = o1 <= w0 && (o0 > w1 - a.window || o1 < a.sinks);
                 }
-                uint32_t p[16] = {}, ds[16] = {};
-                if (KEYS) bar_pass_cta(full(stage), g / kStages & 1, &gave_up);
-                bar_pass_cta(s_full(g), g / kBuffers & 1, &gave_up);
+                uint32_t p[16], ds[16];
+                if (KEYS) bar_pass_cta(full(stage), stage_phase, &gave_up);
+                bar_pass_cta(s_full(buffer), phase, &gave_up);
                 fence_after();
                 if (some) {
                     float x[32], y[32];
@@ -942,6 +942,9 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                         if (KEYS) p[i] = pack2(x[2 * i], x[2 * i + 1], T());
                         ds[i] = pack2(y[2 * i], y[2 * i + 1], T());
                     }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[i] = ds[i] = 0;
                 }
                 // over scores that this thread has read
                 if (KEYS) tmem_st16(ts, p);
@@ -949,7 +952,9 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 tmem_wait_st();
                 fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(p_full(g));
+                if (lane == 0) bar_arrive(p_full(buffer));
+                if (++buffer == kBuffers) buffer = 0, phase ^= 1u;
+                if (++stage == kStages) stage = 0, stage_phase ^= 1u;
             }
             bar_pass_cta(out_full, vt & 1, &gave_up);
             fence_after();
