@@ -546,6 +546,259 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     if (warp == 5) tmem_free(tmem, Shape::kColumns);
 }
 
+// ------------------------------------------------------------------ few queries
+// A query or a few over a long cache are bound by the cache's bytes.  A CTA takes up to 16 rows, the queries of all heads of one key
+// head, and a share of the keys that they see; its four warps take 16 keys at a time, each a run of its own, with mma.sync (m16n8k16): the
+// scores leave a warp's registers as the left operand of P V.  Keys come by cp.async into places that the lane alone reads: the order of a head's elements is
+// free as long as q has the same.  Values come in rows, and through ldmatrix.trans.  Every warp has its own maximum, sum and output; they meet in shared
+// memory, and those of a row's CTAs in a second launch.
+constexpr int kFewRows = 16, kFewWarps = 4, kFewKeys = 16, kMostShares = 320; // CTAs of a call whose rows are shared out
+template <int D>
+struct FewShape {
+    static constexpr int kStages = D == 64 ? 6 : 3;
+    static constexpr uint32_t kKeys = kFewKeys * D * 2, kStage = 2 * kKeys, kSmem = kFewWarps * kStages * kStage;
+    static constexpr int kPartial = kFewRows * (D + 2); // floats: outputs, maxima, sums
+};
+struct FewArgs {
+    Heads q, k, v, o;
+    float *lse, *partials;
+    const int32_t *q_ranges, *k_ranges;
+    int q_heads, kv_heads, group, d, q_rows, k_rows, window, sinks;
+    int tiles, shares; // of 16 rows, of a row's keys
+    float scale_log2;
+};
+
+template <typename T>
+__device__ __forceinline__ void mma_rows(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+
+// Sums about different references joined: `n` of them, `stride` floats apart, of 16 rows of D outputs, then 16 references (log 2) and 16 sums each.
+template <typename T, int D>
+__device__ __forceinline__ void join(const FewArgs &a, const float *parts, int n, int stride, int seq, int kv, int tile, float *partial)
+{
+    const Range qr = range_of(a.q_ranges, seq, a.q_rows);
+    const int r = threadIdx.x >> 3, c0 = threadIdx.x & 7, row = tile * kFewRows + r; // eight threads a row
+    float most = -INFINITY, sum = 0.0f, out[D / 8] = {};
+    for (int k = 0; k < n; ++k) most = fmaxf(most, parts[k * stride + kFewRows * D + r]);
+    for (int k = 0; k < n; ++k) {
+        const float *p = parts + k * stride, ref = p[kFewRows * D + r];
+        if (ref == -INFINITY) continue;
+        const float f = exp2_approx(ref - most);
+        sum = fmaf(f, p[kFewRows * (D + 1) + r], sum);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) out[i] = fmaf(f, p[r * D + c0 + 8 * i], out[i]);
+    }
+    if (partial) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) partial[r * D + c0 + 8 * i] = out[i];
+        if (c0 == 0) {
+            partial[kFewRows * D + r] = most;
+            partial[kFewRows * (D + 1) + r] = sum;
+        }
+        return;
+    }
+    const int t = row / a.group, head = kv * a.group + row % a.group;
+    if (t >= qr.count) return;
+    const bool some = sum > 0.0f || sum != sum;
+    T *o = at<T>(a.o, seq, qr.first + t, head);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+        if (c0 + 8 * i < a.d) o[c0 + 8 * i] = from_f32<T>(some ? out[i] / sum : 0.0f);
+    if (a.lse && c0 == 0) a.lse[((int64_t)seq * a.q_heads + head) * a.q_rows + qr.first + t] = some ? (most + log2f(sum)) * kLn2 : -INFINITY;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ FewArgs a)
+{
+    using Shape = FewShape<D>;
+    constexpr int kSteps = D / 32, kPieces = D / 8;
+    extern __shared__ __align__(128) char smem_raw[];
+    wait_prior_grid();
+    release_next_grid();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, c = lane & 3;
+    const int share = blockIdx.x % a.shares, item = blockIdx.x / a.shares, tile = item % a.tiles, kv = item / a.tiles % a.kv_heads, seq = item / a.tiles / a.kv_heads;
+    const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
+    const int rows = min(kFewRows, qr.count * a.group - tile * kFewRows), ahead = kr.count - qr.count;
+    // what some row sees: the first tokens up to `first`, and the keys from lo to end
+    const int t0 = tile * kFewRows / a.group, t1 = rows > 0 ? (tile * kFewRows + rows - 1) / a.group : t0;
+    int lo = max(0, t0 + ahead - a.window + 1), first = min(a.sinks, lo);
+    const int end = rows > 0 ? max(0, t1 + ahead + 1) : 0;
+    if (first == lo) lo = first = 0; // one run
+    first = min(first, end);
+    const int units0 = (first + kFewKeys - 1) / kFewKeys, units = units0 + (max(0, end - lo) + kFewKeys - 1) / kFewKeys;
+    const int worker = share * kFewWarps + warp, workers = a.shares * kFewWarps;
+    const int u0 = (int)((int64_t)units * worker / workers), u1 = (int)((int64_t)units * (worker + 1) / workers);
+
+    // q: rows quad and quad + 8, elements 32 s + 8 c on
+    uint32_t q[kSteps][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = tile * kFewRows + quad + 8 * h, t = r / a.group;
+        const bool live = quad + 8 * h < rows;
+        const uint16_t *p = live ? at<uint16_t>(a.q, seq, qr.first + t, kv * a.group + r - t * a.group) : nullptr;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            const int at0 = 32 * s + 8 * c;
+            if (live && at0 + 8 <= a.d) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(p + at0);
+                w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+            } else if (live) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (at0 + i < a.d) w[i / 2] |= (uint32_t)p[at0 + i] << (16 * (i & 1));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[s][2 * i + h] = w[i];
+        }
+    }
+    const uint32_t mine = smem_u32(smem_raw) + warp * Shape::kStages * Shape::kStage;
+    const T *keys = at<T>(a.k, seq, kr.first, kv), *values = at<T>(a.v, seq, kr.first, kv);
+    const auto bring = [&](int u, int stage) {
+        if (u < u1) {
+            const int k0 = u < units0 ? u * kFewKeys : lo + (u - units0) * kFewKeys, stop = u < units0 ? first : end;
+            const uint32_t place = mine + stage * Shape::kStage;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int key = k0 + 8 * n + quad;
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const int at0 = 32 * s + 8 * c, there = key < stop ? max(0, min(8, a.d - at0)) : 0;
+                    async_copy16(place + ((n * kSteps + s) * 32 + lane) * 16, there ? keys + (int64_t)key * a.k.row + at0 : keys, 2 * there);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) { // 16 rows of D / 8 pieces
+                const int piece = i * 32 + lane, r = piece / kPieces, e = piece % kPieces, key = k0 + r, there = key < stop ? max(0, min(8, a.d - 8 * e)) : 0;
+                async_copy16(place + Shape::kKeys + r * (D * 2) + ((e ^ (r & 7)) << 4), there ? values + (int64_t)key * a.v.row + 8 * e : values, 2 * there);
+            }
+        }
+        async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < Shape::kStages - 1; ++i) bring(u0 + i, i);
+
+    float o[kPieces][4] = {}, ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
+    const int place0 = (tile * kFewRows + quad) / a.group + ahead, place1 = (tile * kFewRows + quad + 8) / a.group + ahead;
+    const float cl = a.scale_log2;
+    int stage = 0;
+    for (int u = u0; u < u1; ++u) {
+        async_wait<Shape::kStages - 2>();
+        __syncwarp();
+        const uint32_t place = mine + stage * Shape::kStage;
+        {
+            const int ahead_stage = stage == 0 ? Shape::kStages - 1 : stage - 1; // the one before: read by all lanes
+            bring(u + Shape::kStages - 1, ahead_stage);
+        }
+        float s[2][4] = {};
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e) {
+                const uint4 b = ld_shared(place + ((n * kSteps + e) * 32 + lane) * 16);
+                mma_rows<T>(s[n], q[e][0], q[e][1], q[e][2], q[e][3], b.x, b.y);
+                mma_rows<T>(s[n], q[e][4], q[e][5], q[e][6], q[e][7], b.z, b.w);
+            }
+        }
+        const int k0 = u < units0 ? u * kFewKeys : lo + (u - units0) * kFewKeys, stop = u < units0 ? first : end;
+        const bool all = k0 + kFewKeys <= stop && k0 + kFewKeys - 1 <= t0 + ahead && (k0 > t1 + ahead - a.window || k0 + kFewKeys <= a.sinks);
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!all) {
+                    const int key = k0 + 8 * n + 2 * c + (i & 1), at_place = i < 2 ? place0 : place1;
+                    if (key >= stop || !(key <= at_place && (key > at_place - a.window || key < a.sinks))) s[n][i] = -INFINITY;
+                }
+                top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
+            }
+        float shrink[2];
+        bool moves = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2)) * cl;
+            shrink[h] = 1.0f;
+            if (top[h] > ref[h] + 8.0f) { // from -infinity, too
+                shrink[h] = exp2_approx(ref[h] - top[h]);
+                ref[h] = top[h];
+                moves = true;
+            }
+        }
+        if (__any_sync(0xffffffffu, moves)) {
+            sum[0] *= shrink[0], sum[1] *= shrink[1];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) o[j][0] *= shrink[0], o[j][1] *= shrink[0], o[j][2] *= shrink[1], o[j][3] *= shrink[1];
+        }
+        const float off0 = ref[0] == -INFINITY ? 0.0f : -ref[0], off1 = ref[1] == -INFINITY ? 0.0f : -ref[1];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[n][i] = exp2_approx(fmaf(s[n][i], cl, i < 2 ? off0 : off1));
+            sum[0] += s[n][0] + s[n][1];
+            sum[1] += s[n][2] + s[n][3];
+        }
+        const uint32_t a0 = pack2(s[0][0], s[0][1], T()), a1 = pack2(s[0][2], s[0][3], T()), a2 = pack2(s[1][0], s[1][1], T()), a3 = pack2(s[1][2], s[1][3], T());
+        const int r = (lane & 7) + (lane & 8); // the row whose address this lane gives: keys 0 to 15, twice
+#pragma unroll
+        for (int j = 0; j < kPieces; j += 2) {
+            uint32_t b[4];
+            const int e = j + (lane >> 4);
+            load_transposed(place + Shape::kKeys + r * (D * 2) + ((e ^ (r & 7)) << 4), b);
+            mma_rows<T>(o[j], a0, a1, a2, a3, b[0], b[1]);
+            mma_rows<T>(o[j + 1], a0, a1, a2, a3, b[2], b[3]);
+        }
+        __syncwarp();
+        if (++stage == Shape::kStages) stage = 0;
+    }
+    async_wait<0>();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
+        sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
+    }
+    __syncthreads(); // the keys' places are free
+    float *parts = reinterpret_cast<float *>(smem_raw), *own = parts + warp * Shape::kPartial;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) own[(quad + 8 * (i >> 1)) * D + 8 * j + 2 * c + (i & 1)] = o[j][i];
+    if (c == 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            own[kFewRows * D + quad + 8 * h] = ref[h];
+            own[kFewRows * (D + 1) + quad + 8 * h] = sum[h];
+        }
+    }
+    __syncthreads();
+    join<T, D>(a, parts, kFewWarps, Shape::kPartial, seq, kv, tile, a.shares > 1 ? a.partials + (int64_t)blockIdx.x * Shape::kPartial : nullptr);
+}
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * kFewWarps) k_few_join(const __grid_constant__ FewArgs a)
+{
+    wait_prior_grid();
+    release_next_grid();
+    const int item = blockIdx.x, tile = item % a.tiles, kv = item / a.tiles % a.kv_heads, seq = item / a.tiles / a.kv_heads;
+    join<T, D>(a, a.partials + (int64_t)item * a.shares * FewShape<D>::kPartial, a.shares, FewShape<D>::kPartial, seq, kv, tile, nullptr);
+}
+
 struct DeltaArgs {
     Heads o, dout;
     const float *lse;
@@ -1228,6 +1481,32 @@ struct Packer {
     }
 };
 
+// Queries that are few enough: the rows of a key head's queries, in sequences that are not packed (whose lengths the host does not know).
+constexpr int kFewMost = 48;
+inline bool few(const a2sgd_attention *s, bool packed_q) { return !packed_q && s->q_rows * (s->q_heads / s->kv_heads) <= kFewMost; }
+inline uint64_t share_bytes(const a2sgd_attention *s) { return (uint64_t)kMostShares * kFewRows * ((s->head_dim <= 64 ? 64 : 128) + 2) * 4; }
+
+template <typename T, int D>
+int launch_few(FewArgs &f, int sequences, float *partials, int sms, cudaStream_t s)
+{
+    using Shape = FewShape<D>;
+    f.tiles = (f.q_rows * f.group + kFewRows - 1) / kFewRows;
+    const int64_t items = (int64_t)f.tiles * f.kv_heads * sequences;
+    if (items > 0x7fffffff / kMostShares) return A2SGD_ERR_TOO_LARGE;
+    // a row's keys are shared out until there are two CTAs an SM, as long as a warp keeps four runs of 16 keys
+    const int64_t seen = std::min<int64_t>(f.k_rows, (int64_t)std::min(f.window, 1 << 29) + f.sinks), units = (seen + kFewKeys - 1) / kFewKeys;
+    f.shares = 1;
+    if (partials && items < 2 * sms)
+        f.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(2 * sms, kMostShares) / items, units / (kFewWarps * 4)));
+    f.partials = partials;
+    void *params[] = {&f};
+    const void *fn = reinterpret_cast<const void *>(&k_few<T, D>);
+    A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(items * f.shares)), 32 * kFewWarps, Shape::kSmem, params, s));
+    if (f.shares > 1) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), dim3((unsigned)items), 32 * kFewWarps, 0, params, s));
+    return A2SGD_OK;
+}
+
 template <typename T, int D>
 int launch_forward(ForwardArgs &f, int64_t rows, int sms, cudaStream_t s)
 {
@@ -1257,6 +1536,20 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
     const int rc = pack.run(sms, s);
     if (rc != A2SGD_OK) return rc;
+    if (few(shape, shape->q_ranges && q.h.seq == 0)) {
+        FewArgs f{};
+        f.q = pq.h, f.k = pk.h, f.v = pv.h, f.o = o.h;
+        f.lse = lse;
+        f.q_ranges = shape->q_ranges, f.k_ranges = shape->k_ranges;
+        f.q_heads = q.heads, f.kv_heads = k.heads, f.group = q.heads / k.heads, f.d = q.d;
+        f.q_rows = (int)q.rows, f.k_rows = (int)k.rows;
+        f.window = (int)std::min<uint64_t>(shape->window, 1u << 30);
+        f.sinks = (int)std::min<uint64_t>(shape->sinks, 1u << 30);
+        f.scale_log2 = (float)(shape->scale * 1.4426950408889634);
+        const bool room_for_shares = pack.begin && (uint64_t)(pack.at - pack.begin) + share_bytes(shape) <= workspace_bytes;
+        float *partials = room_for_shares ? reinterpret_cast<float *>(pack.at) : nullptr;
+        return q.d <= 64 ? launch_few<T, 64>(f, (int)shape->sequences, partials, sms, s) : launch_few<T, 128>(f, (int)shape->sequences, partials, sms, s);
+    }
     ForwardArgs f{};
     if (!make_map(&f.q, pq, shape->dtype, 128)) return A2SGD_ERR_CUDA;
     if (k.rows && (!make_map(&f.k, pk, shape->dtype, kBlock) || !make_map(&f.v, pv, shape->dtype, kBlock))) return A2SGD_ERR_CUDA;
@@ -1414,6 +1707,7 @@ extern "C" uint64_t a2sgd_window_attention_workspace(const a2sgd_attention *shap
     uint64_t bytes = 0;
     if (shape->kv_heads == 0) return 0;
     if (flags & A2SGD_ATTENTION_BACKWARD) bytes += 2 * up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4) + partial_bytes(shape);
+    else if (few(shape, flags & A2SGD_ATTENTION_PACKED_Q)) bytes += share_bytes(shape);
     if (!(flags & A2SGD_ATTENTION_ALIGNED))
         bytes += (flags & A2SGD_ATTENTION_BACKWARD ? 2 : 1) * room(q_planes, (int64_t)shape->q_rows, (int)shape->q_heads, d) +
                  2 * room(k_planes, (int64_t)shape->k_rows, (int)shape->kv_heads, d);
