@@ -4,8 +4,8 @@
 //   backward  t = dz + back(du w2; z),  dx = t,  dn = alpha gate t,  dy = back(dn w1; y),  and the columns' sums
 //
 // Bound by memory: forward reads x, y and writes z, u; backward reads dz, du, y, z and writes dx, dy.  A CTA takes a run of
-// consecutive rows, one after another, a row's elements in its threads' registers; the next row's are on their way while the present
-// one is worked on.  Each norm costs one barrier: a warp forms its own mean and sum of squares about it by shuffles, and
+// consecutive rows, one after another, a row's elements in its threads' registers, the parameters in shared memory; the next row's are on
+// their way while the present one is worked on.  Each norm costs one barrier: a warp forms its own mean and sum of squares about it by shuffles, and
 // the warps' are joined from shared memory (Chan's formula), so that no element is squared about anything but a mean near its own.
 //
 // The columns' sums: t hat1 and t (from which the gate's, the post weight's and the post bias' gradients follow, a gate at a time), du hat2
@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kMostThreads = 512;
 constexpr int kSums = 4; // t hat1, t, du hat2, du
+constexpr int kStrips = 32;
 
 struct Rows {
     void *p;
@@ -104,16 +105,30 @@ __device__ __forceinline__ int column(int chunk, int i)
 {
     return VEC == 8 ? (chunk * (int)blockDim.x + (int)threadIdx.x) * 8 + i : (chunk * 8 + i) * (int)blockDim.x + (int)threadIdx.x;
 }
-// Eight columns of a vector of parameters, or `other` without one.
-template <int VEC>
-__device__ __forceinline__ void params8(float (&f)[8], const void *p, int type, int64_t base, int chunk, int d, float other)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = column<VEC>(chunk, i);
-        f[i] = p && c < d ? param_at(p, type, base + c) : other;
+// Parameters as the rows need them, in fp32, in shared memory: vector k of a CTA's columns, zeros past the end.  Eight columns of a thread lie
+// together where its elements do, so that they come in two 128-bit accesses; the parameters' own accesses are a CTA's start, or a gate's.
+template <int VEC, int C>
+struct Columns {
+    float *p;
+    __device__ __forceinline__ int span() const { return C * 8 * (int)blockDim.x; }
+    template <typename F>
+    __device__ __forceinline__ void fill(int k, int d, F value) const
+    {
+        for (int c = threadIdx.x; c < span(); c += blockDim.x) // VEC 8: the first four of each eight columns, then the second four: no bank twice
+            p[k * span() + (VEC == 8 ? (c >> 2 & 1) * (span() / 2) + (c >> 3) * 4 + (c & 3) : c)] = c < d ? value(c) : 0.0f;
     }
-}
+    __device__ __forceinline__ void read(int k, int chunk, float (&f)[8]) const
+    {
+        if constexpr (VEC == 8) {
+            const float4 *q = reinterpret_cast<const float4 *>(p + k * span() + column<8>(chunk, 0) / 2);
+            const float4 x = q[0], y = q[span() / 8];
+            f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w, f[4] = y.x, f[5] = y.y, f[6] = y.z, f[7] = y.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = p[k * span() + column<1>(chunk, i)];
+        }
+    }
+};
 
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -195,14 +210,18 @@ __device__ __forceinline__ void moments(const float (&v)[C][8], const Args &a, f
     rstd = 1.0f / sqrtf(square / (float)a.d + a.eps);
 }
 
-template <typename T, typename R, int VEC, int C>
-__global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant__ Args a)
+template <typename T, typename R, int VEC, int C, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) k_forward(const __grid_constant__ Args a)
 {
+    extern __shared__ __align__(16) float columns[]; // alpha gate w1, alpha gate b1, w2, b2
     __shared__ float slots[2][48];
     wait_prior_grid();
     release_next_grid();
     const int64_t row0 = (int64_t)blockIdx.x * a.run, end = min(a.rows, row0 + a.run);
     if (row0 >= end) return;
+    const Columns<VEC, C> cols{columns};
+    cols.fill(2, a.d, [&](int c) { return a.w2 ? param_at(a.w2, a.param, c) : 1.0f; });
+    cols.fill(3, a.d, [&](int c) { return a.b2 ? param_at(a.b2, a.param, c) : 0.0f; });
     Eight<T, VEC> y[C];
     Eight<R, VEC> x[C];
     const auto bring = [&](int64_t r) {
@@ -213,6 +232,7 @@ __global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant_
         }
     };
     bring(row0);
+    int64_t gate_end = row0; // rows from here on have another gate
     for (int64_t r = row0; r < end; ++r) {
         float n[C][8], z[C][8];
 #pragma unroll
@@ -221,6 +241,15 @@ __global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant_
             x[k].unpack(z[k]);
         }
         if (r + 1 < end) bring(r + 1);
+        if (r == gate_end) {
+            const int64_t group = a.gate ? r / a.gate_rows : 0;
+            gate_end = a.gate ? min(end, (group + 1) * a.gate_rows) : end;
+            __syncthreads();
+            const auto gate = [&](int c) { return a.gate ? a.alpha * param_at(a.gate, a.param, group * a.d + c) : a.alpha; };
+            cols.fill(0, a.d, [&](int c) { return gate(c) * (a.post && a.w1 ? param_at(a.w1, a.param, c) : 1.0f); });
+            cols.fill(1, a.d, [&](int c) { return a.post && a.b1 ? gate(c) * param_at(a.b1, a.param, c) : 0.0f; });
+            __syncthreads();
+        }
         float mean = 0.0f, rstd = 1.0f;
         if (a.post) {
             moments<VEC, C>(n, a, slots[0], mean, rstd);
@@ -229,19 +258,16 @@ __global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant_
                 if (a.rstd1) a.rstd1[r] = rstd;
             }
         }
-        const int64_t gate = a.gate ? r / a.gate_rows * a.d : 0;
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], b[8], g[8];
-            params8<VEC>(g, a.gate, a.param, gate, k, a.d, 1.0f);
-            if (a.post) {
-                params8<VEC>(w, a.w1, a.param, 0, k, a.d, 1.0f);
-                params8<VEC>(b, a.b1, a.param, 0, k, a.d, 0.0f);
-            }
+            float w[8], b[8];
+            cols.read(0, k, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (a.post) n[k][i] = fmaf((n[k][i] - mean) * rstd, w[i], b[i]);
-                z[k][i] = column<VEC>(k, i) < a.d ? fmaf(a.alpha * g[i], n[k][i], z[k][i]) : 0.0f;
+            for (int i = 0; i < 8; ++i) z[k][i] = fmaf((n[k][i] - mean) * rstd, w[i], z[k][i]); // past the end: w is 0
+            if (a.post && a.b1) {
+                cols.read(1, k, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[k][i] += b[i];
             }
             Eight<R, VEC>::store(static_cast<R *>(a.z.p) + r * a.z.ld, k, a.d, z[k]);
         }
@@ -252,9 +278,9 @@ __global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant_
         }
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], b[8], u[8];
-            params8<VEC>(w, a.w2, a.param, 0, k, a.d, 1.0f);
-            params8<VEC>(b, a.b2, a.param, 0, k, a.d, 0.0f);
+            float w[8], b[8] = {}, u[8];
+            cols.read(2, k, w);
+            if (a.b2) cols.read(3, k, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = fmaf((z[k][i] - mean) * rstd, w[i], b[i]);
             Eight<T, VEC>::store(static_cast<T *>(a.u.p) + r * a.u.ld, k, a.d, u);
@@ -262,158 +288,150 @@ __global__ void __launch_bounds__(kMostThreads) k_forward(const __grid_constant_
     }
 }
 
-template <typename T, typename R, int VEC, int C>
-__global__ void __launch_bounds__(kMostThreads) k_backward(const __grid_constant__ Args a)
+template <typename T, typename R, int VEC, int C, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(const __grid_constant__ Args a)
 {
-    extern __shared__ float sums[]; // [4][columns of the CTA], for C > 1
+    extern __shared__ __align__(16) float columns[]; // w2, alpha gate w1 (alpha gate without a norm), and for C > 1 the four sums
     __shared__ float slots[2][48];
     wait_prior_grid();
     release_next_grid();
     const int64_t row0 = (int64_t)blockIdx.x * a.run, end = min(a.rows, row0 + a.run);
     if (row0 >= end) return;
-    const int span = C * 8 * (int)blockDim.x;
+    const Columns<VEC, C> cols{columns};
+    float *sums = columns + 2 * cols.span();
     const bool want = a.partials != nullptr;
     float acc[kSums][8] = {};
-    const auto sum_at = [&](int s, int k, int i) -> float & { return sums[s * span + (k * 8 + i) * (int)blockDim.x + (int)threadIdx.x]; };
+    const auto sum_at = [&](int s, int k, int i) -> float & { return sums[s * cols.span() + (k * 8 + i) * (int)blockDim.x + (int)threadIdx.x]; };
     if constexpr (C > 1) {
         for (int s = 0; s < kSums; ++s)
             for (int k = 0; k < C; ++k)
                 for (int i = 0; i < 8; ++i) sum_at(s, k, i) = 0.0f;
     }
+    cols.fill(0, a.d, [&](int c) { return a.w2 ? param_at(a.w2, a.param, c) : 1.0f; });
     Eight<T, VEC> y[C], du[C];
     Eight<R, VEC> z[C], dz[C];
     const auto bring = [&](int64_t r) {
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            y[k].load(static_cast<const T *>(a.y.p) + r * a.y.ld, k, a.d);
             du[k].load(static_cast<const T *>(a.du.p) + r * a.du.ld, k, a.d);
             z[k].load(static_cast<const R *>(a.z.p) + r * a.z.ld, k, a.d);
+            y[k].load(static_cast<const T *>(a.y.p) + r * a.y.ld, k, a.d);
             if (a.dz.p) dz[k].load(static_cast<const R *>(a.dz.p) + r * a.dz.ld, k, a.d);
         }
     };
     bring(row0);
     bool flushed = false; // this CTA's partial sums hold earlier gates' rows
+    int64_t gate_end = row0, group = 0; // rows from here on have another gate
+    const float per = 1.0f / (float)a.d;
     for (int64_t r = row0; r < end; ++r) {
         const float mean2 = a.rms ? 0.0f : a.mean2[r], rstd2 = a.rstd2[r];
         const float mean1 = a.rms || !a.post ? 0.0f : a.mean1[r], rstd1 = a.post ? a.rstd1[r] : 1.0f;
-        const int64_t group = a.gate ? r / a.gate_rows : 0;
-        float h1[C][8], t[C][8], s0 = 0.0f, s1 = 0.0f;
-        Eight<T, VEC> g2[C];
-        Eight<R, VEC> zz[C], res[C];
-#pragma unroll
-        for (int k = 0; k < C; ++k) {
-            y[k].unpack(h1[k]);
-            g2[k] = du[k];
-            zz[k] = z[k];
-            res[k] = dz[k];
+        if (r == gate_end) {
+            group = a.gate ? r / a.gate_rows : 0;
+            gate_end = a.gate ? min(end, (group + 1) * a.gate_rows) : end;
+            __syncthreads();
+            cols.fill(1, a.d, [&](int c) {
+                const float g = a.gate ? a.alpha * param_at(a.gate, a.param, group * a.d + c) : a.alpha;
+                return g * (a.post && a.w1 ? param_at(a.w1, a.param, c) : 1.0f);
+            });
+            __syncthreads();
         }
-        if (r + 1 < end) bring(r + 1);
-        // the norm before the next block
+        // the norm before the next block: hat = norm(z), g = du w2
+        float hat[C][8], t[C][8], s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], g[8], h[8];
-            params8<VEC>(w, a.w2, a.param, 0, k, a.d, 1.0f);
-            g2[k].unpack(g);
-            zz[k].unpack(h);
+            float w[8];
+            cols.read(0, k, w);
+            z[k].unpack(hat[k]);
+            du[k].unpack(t[k]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool in = column<VEC>(k, i) < a.d;
-                h[i] = in ? (h[i] - mean2) * rstd2 : 0.0f;
+                hat[k][i] = (hat[k][i] - mean2) * rstd2; // past the end t is 0
                 if (want) {
                     if constexpr (C == 1) {
-                        acc[2][i] = fmaf(g[i], h[i], acc[2][i]);
-                        acc[3][i] += g[i];
+                        acc[2][i] = fmaf(t[k][i], hat[k][i], acc[2][i]);
+                        acc[3][i] += t[k][i];
                     } else {
-                        sum_at(2, k, i) += g[i] * h[i];
-                        sum_at(3, k, i) += g[i];
+                        sum_at(2, k, i) += t[k][i] * hat[k][i];
+                        sum_at(3, k, i) += t[k][i];
                     }
                 }
-                const float gw = in ? g[i] * w[i] : 0.0f;
-                s0 += gw;
-                s1 = fmaf(gw, h[i], s1);
+                t[k][i] *= w[i];
+                s0 += t[k][i];
+                s1 = fmaf(t[k][i], hat[k][i], s1);
             }
         }
         cta_sums(s0, s1, slots[0]);
-        s0 = a.rms ? 0.0f : s0 / (float)a.d;
-        s1 /= (float)a.d;
+        s0 = a.rms ? 0.0f : s0 * per;
+        s1 *= per;
+        // t, dx, and the norm after the block
         float p0 = 0.0f, p1 = 0.0f;
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], g[8], h[8], e[8];
-            params8<VEC>(w, a.w2, a.param, 0, k, a.d, 1.0f);
-            g2[k].unpack(g);
-            zz[k].unpack(h);
-            if (a.dz.p) res[k].unpack(e);
-            float w1[8], gt[8];
-            if (a.post) params8<VEC>(w1, a.w1, a.param, 0, k, a.d, 1.0f);
-            params8<VEC>(gt, a.gate, a.param, group * a.d, k, a.d, 1.0f);
+            float w[8], e[8];
+            if (a.dz.p) dz[k].unpack(e);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool in = column<VEC>(k, i) < a.d;
-                const float hat = (h[i] - mean2) * rstd2;
-                const float v = (g[i] * w[i] - s0 - hat * s1) * rstd2;
-                t[k][i] = in ? v + (a.dz.p ? e[i] : 0.0f) : 0.0f;
-                h1[k][i] = in ? (h1[k][i] - mean1) * rstd1 : 0.0f;
+                t[k][i] = (t[k][i] - s0 - hat[k][i] * s1) * rstd2 + (a.dz.p ? e[i] : 0.0f);
+                if (column<VEC>(k, i) >= a.d) t[k][i] = 0.0f;
+            }
+            if (a.dx.p) Eight<R, VEC>::store(static_cast<R *>(a.dx.p) + r * a.dx.ld, k, a.d, t[k]);
+            y[k].unpack(hat[k]);
+            cols.read(1, k, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                hat[k][i] = (hat[k][i] - mean1) * rstd1;
                 if (want) {
                     if constexpr (C == 1) {
-                        acc[0][i] = fmaf(t[k][i], h1[k][i], acc[0][i]);
+                        acc[0][i] = fmaf(t[k][i], hat[k][i], acc[0][i]);
                         acc[1][i] += t[k][i];
                     } else {
-                        sum_at(0, k, i) += t[k][i] * h1[k][i];
+                        sum_at(0, k, i) += t[k][i] * hat[k][i];
                         sum_at(1, k, i) += t[k][i];
                     }
                 }
-            }
-            if (a.dx.p) Eight<R, VEC>::store(static_cast<R *>(a.dx.p) + r * a.dx.ld, k, a.d, t[k]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                t[k][i] *= a.alpha * gt[i];
-                if (a.post) {
-                    t[k][i] *= w1[i];
-                    p0 += t[k][i];
-                    p1 = fmaf(t[k][i], h1[k][i], p1);
-                }
+                t[k][i] *= w[i];
+                p0 += t[k][i];
+                p1 = fmaf(t[k][i], hat[k][i], p1);
             }
         }
+        if (r + 1 < end) bring(r + 1);
         if (a.post) {
             cta_sums(p0, p1, slots[1]);
-            p0 = a.rms ? 0.0f : p0 / (float)a.d;
-            p1 /= (float)a.d;
+            p0 = a.rms ? 0.0f : p0 * per;
+            p1 *= per;
         }
         if (a.dy.p) {
 #pragma unroll
             for (int k = 0; k < C; ++k) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[k][i] = a.post ? (t[k][i] - p0 - h1[k][i] * p1) * rstd1 : t[k][i];
+                for (int i = 0; i < 8; ++i) t[k][i] = a.post ? (t[k][i] - p0 - hat[k][i] * p1) * rstd1 : t[k][i];
                 Eight<T, VEC>::store(static_cast<T *>(a.dy.p) + r * a.dy.ld, k, a.d, t[k]);
             }
         }
         // a gate's last row in this CTA: what its rows give to the gate, the post weight and the post bias
         const bool last = r + 1 == end;
-        if (want && (last || (a.gate && (r + 1) / a.gate_rows != group))) {
+        if (want && r + 1 == gate_end) {
             const bool whole = a.gate && group * a.gate_rows >= row0 && min(a.rows, (group + 1) * a.gate_rows) <= end;
             const int slot = a.gate && group != row0 / a.gate_rows;
             float *mine = a.partials + (int64_t)blockIdx.x * kSums * a.d;
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < C; ++k) {
-                float w1[8], b1[8], gt[8];
-                params8<VEC>(w1, a.post ? a.w1 : nullptr, a.param, 0, k, a.d, 1.0f);
-                params8<VEC>(b1, a.post ? a.b1 : nullptr, a.param, 0, k, a.d, 0.0f);
-                params8<VEC>(gt, a.gate, a.param, group * a.d, k, a.d, 1.0f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int c = column<VEC>(k, i);
                     if (c >= a.d) continue;
-                    float hat, one;
-                    if constexpr (C == 1) hat = acc[0][i], one = acc[1][i], acc[0][i] = acc[1][i] = 0.0f;
-                    else hat = sum_at(0, k, i), one = sum_at(1, k, i), sum_at(0, k, i) = sum_at(1, k, i) = 0.0f;
+                    float one_hat, one;
+                    if constexpr (C == 1) one_hat = acc[0][i], one = acc[1][i], acc[0][i] = acc[1][i] = 0.0f;
+                    else one_hat = sum_at(0, k, i), one = sum_at(1, k, i), sum_at(0, k, i) = sum_at(1, k, i) = 0.0f;
                     if (a.dgate) {
-                        const float v = a.alpha * fmaf(w1[i], hat, b1[i] * one);
+                        const float w1 = a.post && a.w1 ? param_at(a.w1, a.param, c) : 1.0f, b1 = a.post && a.b1 ? param_at(a.b1, a.param, c) : 0.0f;
+                        const float v = a.alpha * fmaf(w1, one_hat, b1 * one);
                         if (whole) param_put(a.dgate, a.param, group * a.d + c, v);
                         else a.gate_partials[((int64_t)blockIdx.x * 2 + slot) * a.d + c] = v;
                     }
-                    const float f = a.alpha * gt[i];
-                    mine[c] = (flushed ? mine[c] : 0.0f) + f * hat;
+                    const float f = a.gate ? a.alpha * param_at(a.gate, a.param, group * a.d + c) : a.alpha;
+                    mine[c] = (flushed ? mine[c] : 0.0f) + f * one_hat;
                     mine[a.d + c] = (flushed ? mine[a.d + c] : 0.0f) + f * one;
                     if (last) {
                         if constexpr (C == 1) mine[2 * a.d + c] = acc[2][i], mine[3 * a.d + c] = acc[3][i];
@@ -426,10 +444,10 @@ __global__ void __launch_bounds__(kMostThreads) k_backward(const __grid_constant
     }
 }
 
-// The CTAs' sums, added up in order: blocks of 32 columns, eight strips of CTAs each.  blockIdx.y: dw1, db1, dw2, db2, then the gates.
-__global__ void __launch_bounds__(256) k_fold(const __grid_constant__ Args a)
+// The CTAs' sums, added up in order: blocks of 32 columns, 32 strips of CTAs each.  blockIdx.y: dw1, db1, dw2, db2, then the gates.
+__global__ void __launch_bounds__(1024) k_fold(const __grid_constant__ Args a)
 {
-    __shared__ float part[8][32];
+    __shared__ float part[kStrips][32];
     wait_prior_grid();
     release_next_grid();
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), strip = threadIdx.x >> 5;
@@ -451,7 +469,7 @@ __global__ void __launch_bounds__(256) k_fold(const __grid_constant__ Args a)
         if (!out) continue;
         float sum = 0.0f;
         if (c < a.d) {
-            const int count = last - first + 1, lo = first + count * strip / 8, hi = first + count * (strip + 1) / 8;
+            const int count = last - first + 1, lo = first + count * strip / kStrips, hi = first + count * (strip + 1) / kStrips;
 #pragma unroll 4
             for (int k = lo; k < hi; ++k) {
                 if (job < kSums) sum += __ldcg(a.partials + ((int64_t)k * kSums + job) * a.d + c);
@@ -461,7 +479,7 @@ __global__ void __launch_bounds__(256) k_fold(const __grid_constant__ Args a)
         part[strip][threadIdx.x & 31] = sum;
         __syncthreads();
         if (strip == 0 && c < a.d) {
-            for (int k = 1; k < 8; ++k) sum += part[k][threadIdx.x];
+            for (int k = 1; k < kStrips; ++k) sum += part[k][threadIdx.x];
             param_put(out, a.param, at, sum);
         }
         __syncthreads();
@@ -470,7 +488,7 @@ __global__ void __launch_bounds__(256) k_fold(const __grid_constant__ Args a)
 
 // ------------------------------------------------------------------ host
 struct Plan {
-    int threads, chunks, vec;
+    int threads, chunks, vec, most; // threads that the kernel is compiled for
 };
 Plan plan_of(uint32_t d, bool vec)
 {
@@ -479,19 +497,22 @@ Plan plan_of(uint32_t d, bool vec)
     p.chunks = d > 8u * kMostThreads ? 2 : 1;
     const int pieces = (int)(d + 8 * p.chunks - 1) / (8 * p.chunks);
     p.threads = (pieces + 31) / 32 * 32;
+    p.most = p.threads <= 256 ? 256 : 512;
     return p;
 }
 
 template <typename T, typename R>
 const void *pick(const Plan &p, bool backward)
 {
-#define A2_PICK(V, K)                                                                                         \
-    if (p.vec == V && p.chunks == K)                                                                          \
-        return backward ? reinterpret_cast<const void *>(&k_backward<T, R, V, K>) : reinterpret_cast<const void *>(&k_forward<T, R, V, K>);
-    A2_PICK(8, 1)
-    A2_PICK(8, 2)
-    A2_PICK(1, 1)
-    A2_PICK(1, 2)
+#define A2_PICK(V, K, N)                                                                                         \
+    if (p.vec == V && p.chunks == K && p.most == N)                                                              \
+        return backward ? reinterpret_cast<const void *>(&k_backward<T, R, V, K, N>) : reinterpret_cast<const void *>(&k_forward<T, R, V, K, N>);
+    A2_PICK(8, 1, 256)
+    A2_PICK(8, 1, 512)
+    A2_PICK(8, 2, 512)
+    A2_PICK(1, 1, 256)
+    A2_PICK(1, 1, 512)
+    A2_PICK(1, 2, 512)
 #undef A2_PICK
     return nullptr;
 }
@@ -501,7 +522,10 @@ const void *pick_types(int dtype, int residual, const Plan &p, bool backward)
     if (dtype == A2SGD_BF16) return residual == A2SGD_F32 ? pick<__nv_bfloat16, float>(p, backward) : pick<__nv_bfloat16, __nv_bfloat16>(p, backward);
     return residual == A2SGD_F32 ? pick<__half, float>(p, backward) : pick<__half, __half>(p, backward);
 }
-size_t smem_of(const Plan &p, bool backward) { return backward && p.chunks > 1 ? (size_t)kSums * p.chunks * 8 * p.threads * 4 : 0; }
+size_t smem_of(const Plan &p, bool backward)
+{
+    return (size_t)(backward ? 2 + (p.chunks > 1 ? kSums : 0) : 4) * p.chunks * 8 * p.threads * 4;
+}
 
 int check_shape(const a2sgd_residual *s)
 {
@@ -569,10 +593,12 @@ extern "C" int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2
     a.x = rows_of(x), a.y = rows_of(y), a.z = rows_of(z), a.u = rows_of(u);
     const Plan p = plan_of(shape->d, shape->d % 8 == 0 && wide(x, shape, r) && wide(y, shape, t) && wide(z, shape, r) && wide(u, shape, t));
     const void *fn = pick_types(t, r, p, false);
-    const int64_t most = (int64_t)sms * resident_ctas(fn, (unsigned)p.threads, 0, device);
+    const size_t smem = smem_of(p, false);
+    A2_TRAIN_CUDA(allow_smem(fn, smem));
+    const int64_t most = (int64_t)sms * resident_ctas(fn, (unsigned)p.threads, smem, device);
     a.run = (a.rows + most - 1) / most;
     void *params[] = {&a};
-    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)((a.rows + a.run - 1) / a.run)), (unsigned)p.threads, 0, params, static_cast<cudaStream_t>(stream)));
+    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)((a.rows + a.run - 1) / a.run)), (unsigned)p.threads, smem, params, static_cast<cudaStream_t>(stream)));
     return A2SGD_OK;
 }
 
@@ -640,7 +666,7 @@ extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a
     if (want) {
         const int64_t groups = a.dgate ? (a.rows + a.gate_rows - 1) / a.gate_rows : 0;
         A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold), dim3((unsigned)(a.d + 31) / 32, (unsigned)std::min<int64_t>(kSums + groups, 1024)),
-                             256, 0, params, s));
+                             32 * kStrips, 0, params, s));
     }
     return A2SGD_OK;
 }

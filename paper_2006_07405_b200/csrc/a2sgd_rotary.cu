@@ -39,25 +39,20 @@ struct Args {
     int split, heads_each; // threads that share a token's heads, and heads of each
 };
 
-// VEC consecutive elements
+// VEC consecutive elements as they are in memory
 template <typename T, int VEC>
 struct Piece {
-    float v[VEC];
-    __device__ __forceinline__ void load(const T *p)
-    {
-        if constexpr (VEC == 8) {
-            Raw8<T> raw;
-            raw.load(p);
-            raw.unpack(v);
-        } else {
-            v[0] = to_f32(*p);
-        }
-    }
-    __device__ __forceinline__ void store(T *p) const
-    {
-        if constexpr (VEC == 8) store8(p, v);
-        else *p = from_f32<T>(v[0]);
-    }
+    Raw8<T> raw;
+    __device__ __forceinline__ void load(const T *p) { raw.load(p); }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const { raw.unpack(f); }
+    __device__ static __forceinline__ void store(T *p, const float (&f)[8]) { store8(p, f); }
+};
+template <typename T>
+struct Piece<T, 1> {
+    T raw;
+    __device__ __forceinline__ void load(const T *p) { raw = *p; }
+    __device__ __forceinline__ void unpack(float (&f)[1]) const { f[0] = to_f32(raw); }
+    __device__ static __forceinline__ void store(T *p, const float (&f)[1]) { *p = from_f32<T>(f[0]); }
 };
 
 template <typename T, int VEC, bool INTERLEAVED>
@@ -118,26 +113,26 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Arg
         for (int e = 0; e < kAhead; ++e) {
             if (h0 + e >= last) break;
             T *p = target(h0 + e);
+            float m[VEC], n[VEC], x[VEC], y[VEC];
+            u[e].unpack(m);
             if (turns) {
-                Piece<T, VEC> x, y;
+                v[e].unpack(n);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     if constexpr (INTERLEAVED && VEC > 1) {
                         // pair j of the unit is elements 2 j and 2 j + 1 of u and v one after another
-                        const float m = j < VEC / 2 ? u[e].v[(2 * j) % VEC] : v[e].v[(2 * j) % VEC];
-                        const float n = j < VEC / 2 ? u[e].v[(2 * j + 1) % VEC] : v[e].v[(2 * j + 1) % VEC];
-                        const float m1 = m * c[j] - n * s[j], n1 = m * s[j] + n * c[j];
-                        (j < VEC / 2 ? x : y).v[(2 * j) % VEC] = m1;
-                        (j < VEC / 2 ? x : y).v[(2 * j + 1) % VEC] = n1;
+                        const float f = j < VEC / 2 ? m[(2 * j) % VEC] : n[(2 * j) % VEC], g = j < VEC / 2 ? m[(2 * j + 1) % VEC] : n[(2 * j + 1) % VEC];
+                        (j < VEC / 2 ? x : y)[(2 * j) % VEC] = f * c[j] - g * s[j];
+                        (j < VEC / 2 ? x : y)[(2 * j + 1) % VEC] = f * s[j] + g * c[j];
                     } else {
-                        x.v[j] = u[e].v[j] * c[j] - v[e].v[j] * s[j];
-                        y.v[j] = u[e].v[j] * s[j] + v[e].v[j] * c[j];
+                        x[j] = m[j] * c[j] - n[j] * s[j];
+                        y[j] = m[j] * s[j] + n[j] * c[j];
                     }
                 }
-                x.store(p + at0);
-                y.store(p + at1);
+                Piece<T, VEC>::store(p + at0, x);
+                Piece<T, VEC>::store(p + at1, y);
             } else {
-                u[e].store(p + at0);
+                Piece<T, VEC>::store(p + at0, m);
             }
         }
     }
