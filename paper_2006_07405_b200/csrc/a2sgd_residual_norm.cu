@@ -117,18 +117,30 @@ struct Columns {
         for (int c = threadIdx.x; c < span(); c += blockDim.x) // VEC 8: the first four of each eight columns, then the second four: no bank twice
             p[k * span() + (VEC == 8 ? (c >> 2 & 1) * (span() / 2) + (c >> 3) * 4 + (c & 3) : c)] = c < d ? value(c) : 0.0f;
     }
-    __device__ __forceinline__ void read(int k, int chunk, float (&f)[8]) const
+    __device__ __forceinline__ void read(int k, int chunk, f32x2 (&f)[4]) const
     {
         if constexpr (VEC == 8) {
-            const float4 *q = reinterpret_cast<const float4 *>(p + k * span() + column<8>(chunk, 0) / 2);
-            const float4 x = q[0], y = q[span() / 8];
-            f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w, f[4] = y.x, f[5] = y.y, f[6] = y.z, f[7] = y.w;
+            const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(p + k * span() + column<8>(chunk, 0) / 2);
+            const ulonglong2 x = q[0], y = q[span() / 8];
+            f[0] = x.x, f[1] = x.y, f[2] = y.x, f[3] = y.y;
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = p[k * span() + column<1>(chunk, i)];
+            for (int i = 0; i < 4; ++i) f[i] = pair(p[k * span() + column<1>(chunk, 2 * i)], p[k * span() + column<1>(chunk, 2 * i + 1)]);
         }
     }
 };
+
+// Eight numbers as four pairs.
+__device__ __forceinline__ void pairs8(f32x2 (&p)[4], const float (&f)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = pair(f[2 * i], f[2 * i + 1]);
+}
+__device__ __forceinline__ void singles8(float (&f)[8], const f32x2 (&p)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpair(p[i], f[2 * i], f[2 * i + 1]);
+}
 
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -157,17 +169,19 @@ __device__ __forceinline__ void cta_sums(float &a, float &b, float *slot)
     }
 }
 
-// The mean (0 for RMS) and 1 / sqrt(variance or mean square + eps) of a row whose elements the threads hold.
+// The mean (0 for RMS) and 1 / sqrt(variance or mean square + eps) of a row whose elements the threads hold, zeros past its end.
 template <int VEC, int C>
-__device__ __forceinline__ void moments(const float (&v)[C][8], const Args &a, float *slot, float &mean, float &rstd)
+__device__ __forceinline__ void moments(const f32x2 (&v)[C][4], const Args &a, float *slot, float &mean, float &rstd)
 {
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
-    float sum = 0.0f, square = 0.0f;
+    f32x2 pairs = pair(0.0f);
+    float sum = 0.0f, square;
     if (a.rms) {
 #pragma unroll
         for (int k = 0; k < C; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) square = fmaf(v[k][i], v[k][i], square); // zeros past the row's end
+            for (int i = 0; i < 4; ++i) pairs = fma2(v[k][i], v[k][i], pairs);
+        square = sum2(pairs);
         cta_sums(sum, square, slot);
         mean = 0.0f;
         rstd = 1.0f / sqrtf(square / (float)a.d + a.eps);
@@ -175,22 +189,33 @@ __device__ __forceinline__ void moments(const float (&v)[C][8], const Args &a, f
     }
     int count = 0;
 #pragma unroll
-    for (int k = 0; k < C; ++k)
+    for (int k = 0; k < C; ++k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sum += v[k][i];
-            count += column<VEC>(k, i) < a.d;
+        for (int i = 0; i < 4; ++i) pairs = add2(pairs, v[k][i]);
+        if (VEC == 8) {
+            count += column<VEC>(k, 0) < a.d ? 8 : 0;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) count += column<VEC>(k, i) < a.d;
         }
-    sum = warp_sum(sum);
+    }
+    sum = warp_sum(sum2(pairs));
     const float n = (float)__reduce_add_sync(0xffffffffu, count), own = n > 0.0f ? sum / n : 0.0f;
+    const f32x2 minus = pair(-own);
+    pairs = pair(0.0f);
 #pragma unroll
     for (int k = 0; k < C; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float e = column<VEC>(k, i) < a.d ? v[k][i] - own : 0.0f;
-            square = fmaf(e, e, square);
+        for (int i = 0; i < 4; ++i) {
+            f32x2 e = add2(v[k][i], minus);
+            if (VEC == 8 ? column<VEC>(k, 0) >= a.d : column<VEC>(k, 2 * i + 1) >= a.d) { // past the end
+                float x, y;
+                unpair(e, x, y);
+                e = pair(column<VEC>(k, 2 * i) < a.d ? x : 0.0f, 0.0f);
+            }
+            pairs = fma2(e, e, pairs);
         }
-    square = warp_sum(square);
+    square = warp_sum(sum2(pairs));
     mean = own;
     if (warps > 1) {
         if ((threadIdx.x & 31) == 0) {
@@ -234,11 +259,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) 
     bring(row0);
     int64_t gate_end = row0; // rows from here on have another gate
     for (int64_t r = row0; r < end; ++r) {
-        float n[C][8], z[C][8];
+        f32x2 n[C][4], z[C][4];
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            y[k].unpack(n[k]);
-            x[k].unpack(z[k]);
+            float f[8];
+            y[k].unpack(f);
+            pairs8(n[k], f);
+            x[k].unpack(f);
+            pairs8(z[k], f);
         }
         if (r + 1 < end) bring(r + 1);
         if (r == gate_end) {
@@ -260,16 +288,19 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) 
         }
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], b[8];
+            const f32x2 by = pair(rstd);
+            f32x2 w[4], b[4];
             cols.read(0, k, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[k][i] = fmaf((n[k][i] - mean) * rstd, w[i], z[k][i]); // past the end: w is 0
+            for (int i = 0; i < 4; ++i) z[k][i] = fma2(a.rms ? mul2(n[k][i], by) : mul2(add2(n[k][i], pair(-mean)), by), w[i], z[k][i]); // past the end: w is 0
             if (a.post && a.b1) {
                 cols.read(1, k, b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[k][i] += b[i];
+                for (int i = 0; i < 4; ++i) z[k][i] = add2(z[k][i], b[i]);
             }
-            Eight<R, VEC>::store(static_cast<R *>(a.z.p) + r * a.z.ld, k, a.d, z[k]);
+            float f[8];
+            singles8(f, z[k]);
+            Eight<R, VEC>::store(static_cast<R *>(a.z.p) + r * a.z.ld, k, a.d, f);
         }
         moments<VEC, C>(z, a, slots[1], mean, rstd);
         if (threadIdx.x == 0) {
@@ -278,18 +309,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) 
         }
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], b[8] = {}, u[8];
+            f32x2 w[4], b[4] = {};
+            float u[8];
             cols.read(2, k, w);
             if (a.b2) cols.read(3, k, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = fmaf((z[k][i] - mean) * rstd, w[i], b[i]);
+            for (int i = 0; i < 4; ++i) w[i] = fma2(mul2(add2(z[k][i], pair(-mean)), pair(rstd)), w[i], b[i]);
+            singles8(u, w);
             Eight<T, VEC>::store(static_cast<T *>(a.u.p) + r * a.u.ld, k, a.d, u);
         }
     }
 }
 
 template <typename T, typename R, int VEC, int C, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(const __grid_constant__ Args a)
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(const __grid_constant__ Args a)
 {
     extern __shared__ __align__(16) float columns[]; // w2, alpha gate w1 (alpha gate without a norm), and for C > 1 the four sums
     __shared__ float slots[2][48];
@@ -300,7 +333,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
     const Columns<VEC, C> cols{columns};
     float *sums = columns + 2 * cols.span();
     const bool want = a.partials != nullptr;
-    float acc[kSums][8] = {};
+    f32x2 acc[kSums][4] = {};
     const auto sum_at = [&](int s, int k, int i) -> float & { return sums[s * cols.span() + (k * 8 + i) * (int)blockDim.x + (int)threadIdx.x]; };
     if constexpr (C > 1) {
         for (int s = 0; s < kSums; ++s)
@@ -310,22 +343,37 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
     cols.fill(0, a.d, [&](int c) { return a.w2 ? param_at(a.w2, a.param, c) : 1.0f; });
     Eight<T, VEC> y[C], du[C];
     Eight<R, VEC> z[C], dz[C];
-    const auto bring = [&](int64_t r) {
+    // what the next row starts with is asked for as soon as its place is free
+    const auto bring_pre = [&](int64_t r) {
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             du[k].load(static_cast<const T *>(a.du.p) + r * a.du.ld, k, a.d);
             z[k].load(static_cast<const R *>(a.z.p) + r * a.z.ld, k, a.d);
+        }
+    };
+    const auto bring_post = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
             y[k].load(static_cast<const T *>(a.y.p) + r * a.y.ld, k, a.d);
             if (a.dz.p) dz[k].load(static_cast<const R *>(a.dz.p) + r * a.dz.ld, k, a.d);
         }
     };
-    bring(row0);
+    float next_mean1 = 0.0f, next_rstd1 = 1.0f, next_mean2 = 0.0f, next_rstd2;
+    const auto bring_stats = [&](int64_t r) {
+        next_rstd2 = a.rstd2[r];
+        if (!a.rms) next_mean2 = a.mean2[r];
+        if (a.post) next_rstd1 = a.rstd1[r];
+        if (a.post && !a.rms) next_mean1 = a.mean1[r];
+    };
+    bring_stats(row0);
+    bring_pre(row0);
+    bring_post(row0);
     bool flushed = false; // this CTA's partial sums hold earlier gates' rows
     int64_t gate_end = row0, group = 0; // rows from here on have another gate
     const float per = 1.0f / (float)a.d;
     for (int64_t r = row0; r < end; ++r) {
-        const float mean2 = a.rms ? 0.0f : a.mean2[r], rstd2 = a.rstd2[r];
-        const float mean1 = a.rms || !a.post ? 0.0f : a.mean1[r], rstd1 = a.post ? a.rstd1[r] : 1.0f;
+        const float mean1 = next_mean1, rstd1 = next_rstd1, mean2 = next_mean2, rstd2 = next_rstd2;
+        if (r + 1 < end) bring_stats(r + 1);
         if (r == gate_end) {
             group = a.gate ? r / a.gate_rows : 0;
             gate_end = a.gate ? min(end, (group + 1) * a.gate_rows) : end;
@@ -337,65 +385,74 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
             __syncthreads();
         }
         // the norm before the next block: hat = norm(z), g = du w2
-        float hat[C][8], t[C][8], s0 = 0.0f, s1 = 0.0f;
+        f32x2 hat[C][4], t[C][4], s0s = pair(0.0f), s1s = pair(0.0f);
+        const auto add_up = [&](int which, int k, int i, f32x2 v, f32x2 h) { // v h and v
+            if constexpr (C == 1) {
+                acc[which][i] = fma2(v, h, acc[which][i]);
+                acc[which + 1][i] = add2(acc[which + 1][i], v);
+            } else {
+                float x, y, m, n;
+                unpair(v, x, y);
+                unpair(h, m, n);
+                sum_at(which, k, 2 * i) += x * m;
+                sum_at(which, k, 2 * i + 1) += y * n;
+                sum_at(which + 1, k, 2 * i) += x;
+                sum_at(which + 1, k, 2 * i + 1) += y;
+            }
+        };
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8];
+            f32x2 w[4];
+            float f[8];
             cols.read(0, k, w);
-            z[k].unpack(hat[k]);
-            du[k].unpack(t[k]);
+            z[k].unpack(f);
+            pairs8(hat[k], f);
+            du[k].unpack(f);
+            pairs8(t[k], f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                hat[k][i] = (hat[k][i] - mean2) * rstd2; // past the end t is 0
-                if (want) {
-                    if constexpr (C == 1) {
-                        acc[2][i] = fmaf(t[k][i], hat[k][i], acc[2][i]);
-                        acc[3][i] += t[k][i];
-                    } else {
-                        sum_at(2, k, i) += t[k][i] * hat[k][i];
-                        sum_at(3, k, i) += t[k][i];
-                    }
-                }
-                t[k][i] *= w[i];
-                s0 += t[k][i];
-                s1 = fmaf(t[k][i], hat[k][i], s1);
+            for (int i = 0; i < 4; ++i) {
+                hat[k][i] = mul2(add2(hat[k][i], pair(-mean2)), pair(rstd2)); // past the end t is 0
+                if (want) add_up(2, k, i, t[k][i], hat[k][i]);
+                t[k][i] = mul2(t[k][i], w[i]);
+                s0s = add2(s0s, t[k][i]);
+                s1s = fma2(t[k][i], hat[k][i], s1s);
             }
         }
+        float s0 = sum2(s0s), s1 = sum2(s1s);
+        if (r + 1 < end) bring_pre(r + 1);
         cta_sums(s0, s1, slots[0]);
         s0 = a.rms ? 0.0f : s0 * per;
         s1 *= per;
         // t, dx, and the norm after the block
-        float p0 = 0.0f, p1 = 0.0f;
+        f32x2 p0s = pair(0.0f), p1s = pair(0.0f);
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            float w[8], e[8];
-            if (a.dz.p) dz[k].unpack(e);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                t[k][i] = (t[k][i] - s0 - hat[k][i] * s1) * rstd2 + (a.dz.p ? e[i] : 0.0f);
-                if (column<VEC>(k, i) >= a.d) t[k][i] = 0.0f;
+            f32x2 w[4], e[4] = {};
+            float f[8];
+            if (a.dz.p) {
+                dz[k].unpack(f);
+                pairs8(e, f);
             }
-            if (a.dx.p) Eight<R, VEC>::store(static_cast<R *>(a.dx.p) + r * a.dx.ld, k, a.d, t[k]);
-            y[k].unpack(hat[k]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[k][i] = fma2(fma2(hat[k][i], pair(-s1), add2(t[k][i], pair(-s0))), pair(rstd2), e[i]);
+            if (a.dx.p) {
+                singles8(f, t[k]);
+                Eight<R, VEC>::store(static_cast<R *>(a.dx.p) + r * a.dx.ld, k, a.d, f);
+            }
+            y[k].unpack(f);
+            pairs8(hat[k], f);
             cols.read(1, k, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                hat[k][i] = (hat[k][i] - mean1) * rstd1;
-                if (want) {
-                    if constexpr (C == 1) {
-                        acc[0][i] = fmaf(t[k][i], hat[k][i], acc[0][i]);
-                        acc[1][i] += t[k][i];
-                    } else {
-                        sum_at(0, k, i) += t[k][i] * hat[k][i];
-                        sum_at(1, k, i) += t[k][i];
-                    }
-                }
-                t[k][i] *= w[i];
-                p0 += t[k][i];
-                p1 = fmaf(t[k][i], hat[k][i], p1);
+            for (int i = 0; i < 4; ++i) {
+                hat[k][i] = mul2(add2(hat[k][i], pair(-mean1)), pair(rstd1));
+                if (want) add_up(0, k, i, t[k][i], hat[k][i]);
+                t[k][i] = mul2(t[k][i], w[i]); // past the end w is 0
+                p0s = add2(p0s, t[k][i]);
+                p1s = fma2(t[k][i], hat[k][i], p1s);
             }
         }
-        if (r + 1 < end) bring(r + 1);
+        float p0 = sum2(p0s), p1 = sum2(p1s);
+        if (r + 1 < end) bring_post(r + 1);
         if (a.post) {
             cta_sums(p0, p1, slots[1]);
             p0 = a.rms ? 0.0f : p0 * per;
@@ -404,9 +461,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
         if (a.dy.p) {
 #pragma unroll
             for (int k = 0; k < C; ++k) {
+                if (a.post) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[k][i] = a.post ? (t[k][i] - p0 - hat[k][i] * p1) * rstd1 : t[k][i];
-                Eight<T, VEC>::store(static_cast<T *>(a.dy.p) + r * a.dy.ld, k, a.d, t[k]);
+                    for (int i = 0; i < 4; ++i) t[k][i] = mul2(fma2(hat[k][i], pair(-p1), add2(t[k][i], pair(-p0))), pair(rstd1));
+                }
+                float f[8];
+                singles8(f, t[k]);
+                Eight<T, VEC>::store(static_cast<T *>(a.dy.p) + r * a.dy.ld, k, a.d, f);
             }
         }
         // a gate's last row in this CTA: what its rows give to the gate, the post weight and the post bias
@@ -415,6 +476,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
             const bool whole = a.gate && group * a.gate_rows >= row0 && min(a.rows, (group + 1) * a.gate_rows) <= end;
             const int slot = a.gate && group != row0 / a.gate_rows;
             float *mine = a.partials + (int64_t)blockIdx.x * kSums * a.d;
+            float mine4[kSums][8];
+            if constexpr (C == 1) {
+#pragma unroll
+                for (int q = 0; q < kSums; ++q) singles8(mine4[q], acc[q]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[0][i] = acc[1][i] = pair(0.0f);
+            }
 #pragma unroll 1
             for (int k = 0; k < C; ++k) {
 #pragma unroll
@@ -422,7 +490,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
                     const int c = column<VEC>(k, i);
                     if (c >= a.d) continue;
                     float one_hat, one;
-                    if constexpr (C == 1) one_hat = acc[0][i], one = acc[1][i], acc[0][i] = acc[1][i] = 0.0f;
+                    if constexpr (C == 1) one_hat = mine4[0][i], one = mine4[1][i];
                     else one_hat = sum_at(0, k, i), one = sum_at(1, k, i), sum_at(0, k, i) = sum_at(1, k, i) = 0.0f;
                     if (a.dgate) {
                         const float w1 = a.post && a.w1 ? param_at(a.w1, a.param, c) : 1.0f, b1 = a.post && a.b1 ? param_at(a.b1, a.param, c) : 0.0f;
@@ -434,7 +502,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) k_backward(co
                     mine[c] = (flushed ? mine[c] : 0.0f) + f * one_hat;
                     mine[a.d + c] = (flushed ? mine[a.d + c] : 0.0f) + f * one;
                     if (last) {
-                        if constexpr (C == 1) mine[2 * a.d + c] = acc[2][i], mine[3 * a.d + c] = acc[3][i];
+                        if constexpr (C == 1) mine[2 * a.d + c] = mine4[2][i], mine[3 * a.d + c] = mine4[3][i];
                         else mine[2 * a.d + c] = sum_at(2, k, i), mine[3 * a.d + c] = sum_at(3, k, i);
                     }
                 }
