@@ -551,8 +551,9 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 // head, and a share of the keys that they see; its four warps take 16 keys at a time, each a run of its own, with mma.sync (m16n8k16): the
 // scores leave a warp's registers as the left operand of P V.  Keys come by cp.async into places that the lane alone reads: the order of a head's elements is
 // free as long as q has the same.  Values come in rows, and through ldmatrix.trans.  Every warp has its own maximum, sum and output; they meet in shared
-// memory, and those of a row's CTAs in a second launch.
-constexpr int kFewRows = 16, kFewWarps = 4, kFewKeys = 16, kMostShares = 320; // CTAs of a call whose rows are shared out
+// memory, and those of a row's CTAs in a cluster's, or beyond eight CTAs in a second launch.
+constexpr int kFewRows = 16, kFewWarps = 4, kFewKeys = 16, kMostShares = 320; // CTAs of a call whose rows are shared out beyond a cluster
+constexpr int kFewCluster = 8;
 template <int D>
 struct FewShape {
     static constexpr int kStages = D == 64 ? 6 : 3;
@@ -564,7 +565,7 @@ struct FewArgs {
     float *lse, *partials;
     const int32_t *q_ranges, *k_ranges;
     int q_heads, kv_heads, group, d, q_rows, k_rows, window, sinks;
-    int tiles, shares; // of 16 rows, of a row's keys
+    int tiles, shares, cluster; // of 16 rows; of a row's keys, which are a cluster's CTAs
     float scale_log2;
 };
 
@@ -588,32 +589,34 @@ __device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t (&r)[4])
                  : "memory");
 }
 
-// Sums about different references joined: `n` of them, `stride` floats apart, of 16 rows of D outputs, then 16 references (log 2) and 16 sums each.
-template <typename T, int D>
-__device__ __forceinline__ void join(const FewArgs &a, const float *parts, int n, int stride, int seq, int kv, int tile, float *partial)
+// Sums about different references joined: at(k, i) is float i of share k of `n`, each 16 rows of D outputs, then 16 references (log 2) and 16
+// sums.  Rows r0 to r1, as another such share, or as the output.
+template <typename T, int D, typename At>
+__device__ __forceinline__ void join(const FewArgs &a, const At &at_share, int n, int seq, int kv, int tile, int r0, int r1, float *joined)
 {
-    const Range qr = range_of(a.q_ranges, seq, a.q_rows);
-    const int r = threadIdx.x >> 3, c0 = threadIdx.x & 7, row = tile * kFewRows + r; // eight threads a row
+    const int r = r0 + (threadIdx.x >> 3), c0 = threadIdx.x & 7; // eight threads a row
+    if (r >= r1) return;
     float most = -INFINITY, sum = 0.0f, out[D / 8] = {};
-    for (int k = 0; k < n; ++k) most = fmaxf(most, parts[k * stride + kFewRows * D + r]);
+    for (int k = 0; k < n; ++k) most = fmaxf(most, at_share(k, kFewRows * D + r));
     for (int k = 0; k < n; ++k) {
-        const float *p = parts + k * stride, ref = p[kFewRows * D + r];
+        const float ref = at_share(k, kFewRows * D + r);
         if (ref == -INFINITY) continue;
         const float f = exp2_approx(ref - most);
-        sum = fmaf(f, p[kFewRows * (D + 1) + r], sum);
+        sum = fmaf(f, at_share(k, kFewRows * (D + 1) + r), sum);
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) out[i] = fmaf(f, p[r * D + c0 + 8 * i], out[i]);
+        for (int i = 0; i < D / 8; ++i) out[i] = fmaf(f, at_share(k, r * D + c0 + 8 * i), out[i]);
     }
-    if (partial) {
+    if (joined) {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) partial[r * D + c0 + 8 * i] = out[i];
+        for (int i = 0; i < D / 8; ++i) joined[r * D + c0 + 8 * i] = out[i];
         if (c0 == 0) {
-            partial[kFewRows * D + r] = most;
-            partial[kFewRows * (D + 1) + r] = sum;
+            joined[kFewRows * D + r] = most;
+            joined[kFewRows * (D + 1) + r] = sum;
         }
         return;
     }
-    const int t = row / a.group, head = kv * a.group + row % a.group;
+    const Range qr = range_of(a.q_ranges, seq, a.q_rows);
+    const int row = tile * kFewRows + r, t = row / a.group, head = kv * a.group + row - t * a.group;
     if (t >= qr.count) return;
     const bool some = sum > 0.0f || sum != sum;
     T *o = at<T>(a.o, seq, qr.first + t, head);
@@ -632,7 +635,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     wait_prior_grid();
     release_next_grid();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, c = lane & 3;
-    const int share = blockIdx.x % a.shares, item = blockIdx.x / a.shares, tile = item % a.tiles, kv = item / a.tiles % a.kv_heads, seq = item / a.tiles / a.kv_heads;
+    const int tile = blockIdx.x / a.shares, share = blockIdx.x - tile * a.shares, kv = blockIdx.y, seq = blockIdx.z;
     const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
     const int rows = min(kFewRows, qr.count * a.group - tile * kFewRows), ahead = kr.count - qr.count;
     // what some row sees: the first tokens up to `first`, and the keys from lo to end
@@ -643,7 +646,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     first = min(first, end);
     const int units0 = (first + kFewKeys - 1) / kFewKeys, units = units0 + (max(0, end - lo) + kFewKeys - 1) / kFewKeys;
     const int worker = share * kFewWarps + warp, workers = a.shares * kFewWarps;
-    const int u0 = (int)((int64_t)units * worker / workers), u1 = (int)((int64_t)units * (worker + 1) / workers);
+    const int each = units / workers, rest = units - each * workers, u0 = each * worker + min(worker, rest), u1 = u0 + each + (worker < rest);
 
     // q: rows quad and quad + 8, elements 32 s + 8 c on
     uint32_t q[kSteps][8];
@@ -788,15 +791,34 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
         }
     }
     __syncthreads();
-    join<T, D>(a, parts, kFewWarps, Shape::kPartial, seq, kv, tile, a.shares > 1 ? a.partials + (int64_t)blockIdx.x * Shape::kPartial : nullptr);
+    if (a.shares == 1) {
+        join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, kFewWarps, seq, kv, tile, 0, kFewRows, nullptr);
+        return;
+    }
+    // the shares of a row: the CTAs of a cluster read one another's, or a second launch joins them
+    float *joined = a.cluster ? parts + kFewWarps * Shape::kPartial : a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + blockIdx.x) * Shape::kPartial;
+    join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, kFewWarps, seq, kv, tile, 0, kFewRows, joined);
+    if (!a.cluster) return;
+    cluster_sync();
+    const uint32_t here = smem_u32(joined);
+    join<T, D>(a,
+               [&](int k, int i) {
+                   float v;
+                   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to(here + 4 * i, k)) : "memory");
+                   return v;
+               },
+               a.shares, seq, kv, tile, kFewRows * share / a.shares, kFewRows * (share + 1) / a.shares, nullptr);
+    __syncwarp();
+    cluster_sync(); // no CTA leaves while another reads its share
 }
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kFewWarps) k_few_join(const __grid_constant__ FewArgs a)
 {
     wait_prior_grid();
     release_next_grid();
-    const int item = blockIdx.x, tile = item % a.tiles, kv = item / a.tiles % a.kv_heads, seq = item / a.tiles / a.kv_heads;
-    join<T, D>(a, a.partials + (int64_t)item * a.shares * FewShape<D>::kPartial, a.shares, FewShape<D>::kPartial, seq, kv, tile, nullptr);
+    const int tile = blockIdx.x, kv = blockIdx.y, seq = blockIdx.z;
+    const float *parts = a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + tile) * a.shares * FewShape<D>::kPartial;
+    join<T, D>(a, [&](int k, int i) { return parts[(int64_t)k * FewShape<D>::kPartial + i]; }, a.shares, seq, kv, tile, 0, kFewRows, nullptr);
 }
 
 struct DeltaArgs {
@@ -1491,19 +1513,22 @@ int launch_few(FewArgs &f, int sequences, float *partials, int sms, cudaStream_t
 {
     using Shape = FewShape<D>;
     f.tiles = (f.q_rows * f.group + kFewRows - 1) / kFewRows;
+    if (f.kv_heads > 65535 || sequences > 65535) return A2SGD_ERR_TOO_LARGE;
     const int64_t items = (int64_t)f.tiles * f.kv_heads * sequences;
-    if (items > 0x7fffffff / kMostShares) return A2SGD_ERR_TOO_LARGE;
     // a row's keys are shared out until there are two CTAs an SM, as long as a warp keeps four runs of 16 keys
     const int64_t seen = std::min<int64_t>(f.k_rows, (int64_t)std::min(f.window, 1 << 29) + f.sinks), units = (seen + kFewKeys - 1) / kFewKeys;
-    f.shares = 1;
-    if (partials && items < 2 * sms)
-        f.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(2 * sms, kMostShares) / items, units / (kFewWarps * 4)));
+    int64_t shares = 1;
+    if (items < 2 * sms) shares = std::max<int64_t>(1, std::min<int64_t>(std::min(2 * sms, kMostShares) / items, units / (kFewWarps * 4)));
+    if (!partials) shares = std::min<int64_t>(shares, kFewCluster);
+    f.shares = (int)shares;
+    f.cluster = shares > 1 && shares <= kFewCluster;
     f.partials = partials;
     void *params[] = {&f};
     const void *fn = reinterpret_cast<const void *>(&k_few<T, D>);
     A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
-    A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(items * f.shares)), 32 * kFewWarps, Shape::kSmem, params, s));
-    if (f.shares > 1) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), dim3((unsigned)items), 32 * kFewWarps, 0, params, s));
+    const dim3 rows((unsigned)f.tiles, (unsigned)f.kv_heads, (unsigned)sequences);
+    A2_TRAIN_CUDA(launch(fn, dim3(rows.x * (unsigned)f.shares, rows.y, rows.z), 32 * kFewWarps, Shape::kSmem, params, s, f.cluster ? (unsigned)f.shares : 1));
+    if (f.shares > 1 && !f.cluster) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), rows, 32 * kFewWarps, 0, params, s));
     return A2SGD_OK;
 }
 
