@@ -548,16 +548,15 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 
 // ------------------------------------------------------------------ few queries
 // A query or a few over a long cache are bound by the cache's bytes.  A CTA takes up to 16 rows, the queries of all heads of one key
-// head, and a share of the keys that they see; its four warps take 16 keys at a time, each a run of its own, with mma.sync (m16n8k16): the
+// head, and a share of the keys that they see; its warps take 16 keys at a time, each a run of its own, with mma.sync (m16n8k16): the
 // scores leave a warp's registers as the left operand of P V.  Keys come by cp.async into places that the lane alone reads: the order of a head's elements is
 // free as long as q has the same.  Values come in rows, and through ldmatrix.trans.  Every warp has its own maximum, sum and output; they meet in shared
 // memory, and those of a row's CTAs in a cluster's, or beyond eight CTAs in a second launch.
-constexpr int kFewRows = 16, kFewWarps = 4, kFewKeys = 16, kMostShares = 320; // CTAs of a call whose rows are shared out beyond a cluster
-constexpr int kFewCluster = 8;
+constexpr int kFewRows = 16, kFewKeys = 16, kFewCluster = 8, kMostShares = 320; // the last: CTAs of a call whose rows are shared out beyond a cluster
 template <int D>
 struct FewShape {
-    static constexpr int kStages = D == 64 ? 6 : 3;
-    static constexpr uint32_t kKeys = kFewKeys * D * 2, kStage = 2 * kKeys, kSmem = kFewWarps * kStages * kStage;
+    static constexpr int kWarps = D == 64 ? 8 : 4, kStages = 3;
+    static constexpr uint32_t kKeys = kFewKeys * D * 2, kStage = 2 * kKeys, kSmem = kWarps * kStages * kStage;
     static constexpr int kPartial = kFewRows * (D + 2); // floats: outputs, maxima, sums
 };
 struct FewArgs {
@@ -627,7 +626,7 @@ __device__ __forceinline__ void join(const FewArgs &a, const At &at_share, int n
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ FewArgs a)
+__global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_constant__ FewArgs a)
 {
     using Shape = FewShape<D>;
     constexpr int kSteps = D / 32, kPieces = D / 8;
@@ -645,7 +644,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     if (first == lo) lo = first = 0; // one run
     first = min(first, end);
     const int units0 = (first + kFewKeys - 1) / kFewKeys, units = units0 + (max(0, end - lo) + kFewKeys - 1) / kFewKeys;
-    const int worker = share * kFewWarps + warp, workers = a.shares * kFewWarps;
+    const int worker = share * Shape::kWarps + warp, workers = a.shares * Shape::kWarps;
     const int each = units / workers, rest = units - each * workers, u0 = each * worker + min(worker, rest), u1 = u0 + each + (worker < rest);
 
     // q: rows quad and quad + 8, elements 32 s + 8 c on
@@ -672,24 +671,30 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
         }
     }
     const uint32_t mine = smem_u32(smem_raw) + warp * Shape::kStages * Shape::kStage;
+    // a lane's pieces of a run: keys quad and quad + 8, elements 8 c and every 32 on; values: elements 8 e of every (32 / kPieces)th row
+    const int e = lane % kPieces, r0 = lane / kPieces;
     const T *keys = at<T>(a.k, seq, kr.first, kv), *values = at<T>(a.v, seq, kr.first, kv);
+    const T *lane_keys = keys + (int64_t)quad * a.k.row + 8 * c, *lane_values = values + (int64_t)r0 * a.v.row + 8 * e;
+    const int64_t keys8 = 8 * a.k.row, values_step = (32 / kPieces) * a.v.row;
+    const int value_bytes = 2 * max(0, min(8, a.d - 8 * e));
     const auto bring = [&](int u, int stage) {
         if (u < u1) {
-            const int k0 = u < units0 ? u * kFewKeys : lo + (u - units0) * kFewKeys, stop = u < units0 ? first : end;
-            const uint32_t place = mine + stage * Shape::kStage;
+            const int k0 = u < units0 ? u * kFewKeys : lo + (u - units0) * kFewKeys, left = (u < units0 ? first : end) - k0;
+            const uint32_t place = mine + stage * Shape::kStage + lane * 16, value_place = mine + stage * Shape::kStage + Shape::kKeys;
+            const T *k = lane_keys + (int64_t)k0 * a.k.row, *v = lane_values + (int64_t)k0 * a.v.row;
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const int key = k0 + 8 * n + quad;
+                const bool in = quad + 8 * n < left;
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s) {
-                    const int at0 = 32 * s + 8 * c, there = key < stop ? max(0, min(8, a.d - at0)) : 0;
-                    async_copy16(place + ((n * kSteps + s) * 32 + lane) * 16, there ? keys + (int64_t)key * a.k.row + at0 : keys, 2 * there);
+                    const int there = in ? 2 * max(0, min(8, a.d - 32 * s - 8 * c)) : 0;
+                    async_copy16(place + (n * kSteps + s) * 512, there ? k + n * keys8 + 32 * s : keys, there);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kPieces / 2; ++i) { // 16 rows of D / 8 pieces
-                const int piece = i * 32 + lane, r = piece / kPieces, e = piece % kPieces, key = k0 + r, there = key < stop ? max(0, min(8, a.d - 8 * e)) : 0;
-                async_copy16(place + Shape::kKeys + r * (D * 2) + ((e ^ (r & 7)) << 4), there ? values + (int64_t)key * a.v.row + 8 * e : values, 2 * there);
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int r = i * (32 / kPieces) + r0, there = r < left ? value_bytes : 0;
+                async_copy16(value_place + r * (D * 2) + ((e ^ (r & 7)) << 4), there ? v + i * values_step : values, there);
             }
         }
         async_commit();
@@ -713,10 +718,10 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
 #pragma unroll
-            for (int e = 0; e < kSteps; ++e) {
-                const uint4 b = ld_shared(place + ((n * kSteps + e) * 32 + lane) * 16);
-                mma_rows<T>(s[n], q[e][0], q[e][1], q[e][2], q[e][3], b.x, b.y);
-                mma_rows<T>(s[n], q[e][4], q[e][5], q[e][6], q[e][7], b.z, b.w);
+            for (int x = 0; x < kSteps; ++x) {
+                const uint4 b = ld_shared(place + ((n * kSteps + x) * 32 + lane) * 16);
+                mma_rows<T>(s[n], q[x][0], q[x][1], q[x][2], q[x][3], b.x, b.y);
+                mma_rows<T>(s[n], q[x][4], q[x][5], q[x][6], q[x][7], b.z, b.w);
             }
         }
         const int k0 = u < units0 ? u * kFewKeys : lo + (u - units0) * kFewKeys, stop = u < units0 ? first : end;
@@ -759,12 +764,11 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
             sum[1] += s[n][2] + s[n][3];
         }
         const uint32_t a0 = pack2(s[0][0], s[0][1], T()), a1 = pack2(s[0][2], s[0][3], T()), a2 = pack2(s[1][0], s[1][1], T()), a3 = pack2(s[1][2], s[1][3], T());
-        const int r = (lane & 7) + (lane & 8); // the row whose address this lane gives: keys 0 to 15, twice
+        const int r = lane & 15; // the row whose address this lane gives: keys 0 to 15, twice
 #pragma unroll
         for (int j = 0; j < kPieces; j += 2) {
             uint32_t b[4];
-            const int e = j + (lane >> 4);
-            load_transposed(place + Shape::kKeys + r * (D * 2) + ((e ^ (r & 7)) << 4), b);
+            load_transposed(place + Shape::kKeys + r * (D * 2) + (((j + (lane >> 4)) ^ (r & 7)) << 4), b);
             mma_rows<T>(o[j], a0, a1, a2, a3, b[0], b[1]);
             mma_rows<T>(o[j + 1], a0, a1, a2, a3, b[2], b[3]);
         }
@@ -792,12 +796,12 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     }
     __syncthreads();
     if (a.shares == 1) {
-        join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, kFewWarps, seq, kv, tile, 0, kFewRows, nullptr);
+        join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, Shape::kWarps, seq, kv, tile, 0, kFewRows, nullptr);
         return;
     }
     // the shares of a row: the CTAs of a cluster read one another's, or a second launch joins them
-    float *joined = a.cluster ? parts + kFewWarps * Shape::kPartial : a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + blockIdx.x) * Shape::kPartial;
-    join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, kFewWarps, seq, kv, tile, 0, kFewRows, joined);
+    float *joined = a.cluster ? parts + Shape::kWarps * Shape::kPartial : a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + blockIdx.x) * Shape::kPartial;
+    join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, Shape::kWarps, seq, kv, tile, 0, kFewRows, joined);
     if (!a.cluster) return;
     cluster_sync();
     const uint32_t here = smem_u32(joined);
@@ -812,7 +816,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few(const __grid_constant__ 
     cluster_sync(); // no CTA leaves while another reads its share
 }
 template <typename T, int D>
-__global__ void __launch_bounds__(32 * kFewWarps) k_few_join(const __grid_constant__ FewArgs a)
+__global__ void __launch_bounds__(128) k_few_join(const __grid_constant__ FewArgs a)
 {
     wait_prior_grid();
     release_next_grid();
@@ -1518,7 +1522,7 @@ int launch_few(FewArgs &f, int sequences, float *partials, int sms, cudaStream_t
     // a row's keys are shared out until there are two CTAs an SM, as long as a warp keeps four runs of 16 keys
     const int64_t seen = std::min<int64_t>(f.k_rows, (int64_t)std::min(f.window, 1 << 29) + f.sinks), units = (seen + kFewKeys - 1) / kFewKeys;
     int64_t shares = 1;
-    if (items < 2 * sms) shares = std::max<int64_t>(1, std::min<int64_t>(std::min(2 * sms, kMostShares) / items, units / (kFewWarps * 4)));
+    if (items < 2 * sms) shares = std::max<int64_t>(1, std::min<int64_t>(std::min(2 * sms, kMostShares) / items, units / (Shape::kWarps * 4)));
     if (!partials) shares = std::min<int64_t>(shares, kFewCluster);
     f.shares = (int)shares;
     f.cluster = shares > 1 && shares <= kFewCluster;
@@ -1527,8 +1531,8 @@ int launch_few(FewArgs &f, int sequences, float *partials, int sms, cudaStream_t
     const void *fn = reinterpret_cast<const void *>(&k_few<T, D>);
     A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
     const dim3 rows((unsigned)f.tiles, (unsigned)f.kv_heads, (unsigned)sequences);
-    A2_TRAIN_CUDA(launch(fn, dim3(rows.x * (unsigned)f.shares, rows.y, rows.z), 32 * kFewWarps, Shape::kSmem, params, s, f.cluster ? (unsigned)f.shares : 1));
-    if (f.shares > 1 && !f.cluster) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), rows, 32 * kFewWarps, 0, params, s));
+    A2_TRAIN_CUDA(launch(fn, dim3(rows.x * (unsigned)f.shares, rows.y, rows.z), 32 * Shape::kWarps, Shape::kSmem, params, s, f.cluster ? (unsigned)f.shares : 1));
+    if (f.shares > 1 && !f.cluster) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), rows, 128, 0, params, s));
     return A2SGD_OK;
 }
 
