@@ -38,7 +38,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ forward
 // Persistent CTAs, two an SM, deal out the tiles of 128 queries of one head, the longest first.  For each tile a CTA walks the blocks of 64
-// keys that any of its queries sees: the first tokens' blocks, then those of the window.  One warp brings tiles in by TMA, two issue the
+// keys that any of its queries sees: the first tokens' blocks, then those of the window.  Two warps bring tiles in by TMA, two issue the
 // products, four hold the softmax, a thread a query.
 //   S = Q K^T into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  O += P V, P read from TMEM.
 // Three buffers of S (two where O has 128 columns): the next block's, be it the next tile's, is formed while the present one's P is.
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
         for (int s = 0; s < 4 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
         for (int t = 0; t < kTiles; ++t) {
             bar_init(tile_full(t), 1);
-            bar_init(tile_empty(t), 5);
+            bar_init(tile_empty(t), 6);
         }
         for (uint32_t b : {q_full, q_empty, tail, o_full}) bar_init(b, 1);
         bar_init(o_empty, 4);
@@ -269,93 +269,90 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     release_next_grid(); // not before this CTA has its TMEM: the next kernel's CTAs may want some, and wait for this one's end
 
     if (warp == 4) {
-        // ---------------------------------------------------------- tiles in: keys two blocks ahead of values
+        // ---------------------------------------------------------- tiles, queries and keys in
         const bool chosen = elect_one();
-        int item = blockIdx.x - gridDim.x, kt = -1, vt = -1, kb = 0, vb = 0; // tiles begun, blocks
-        uint32_t tails = 0;
+        int t = -1, g = 0; // tiles and blocks so far
         bool ok = true;
-        Tile k, v;
-        int kn = 0, vn = 0;
-        k.blocks.count = v.blocks.count = 0;
-        // block `count` of keys or values
-        const auto bring = [&](const CUtensorMap *map, int planes, const Tile &t, int n, int count, bool values) {
-            const int stage = (values ? kStages : 0) + count % kStages;
-            ok = ok && bar_wait_cta(empty(stage), (count / kStages & 1) ^ 1, &gave_up);
-            if (!ok) return;
-            const uint32_t dst = ring + stage * kSlice;
-            const int block = t.blocks[n], valid = t.k_count - block * kBlock;
-            const bool clear = values && a.k_ranges && valid < kBlock;
-            const uint32_t bar = clear ? tail : full(stage);
-            if (chosen) {
-                bar_expect(bar, kSlice);
-                for (int c = 0; c < kChunks; ++c) tma_load4(dst + c * 8192u, map, 64 * c, t.k_row + block * kBlock, t.head / a.group, planes > 1 ? t.seq : 0, bar);
+        for (int item = blockIdx.x; ok; item += gridDim.x) {
+            Tile k;
+            k.rows = k.blocks.count = 0;
+            const bool end = item >= a.items;
+            if (!end && !find_tile(a, item, k)) continue;
+            if (!end && k.blocks.count == 0) { // queries that see nothing
+                for (int r = 0; r < k.rows; ++r) {
+                    T *o = at<T>(a.o, k.seq, k.q_row + r, k.head);
+                    for (int c = lane; c < a.d; c += 32) o[c] = from_f32<T>(0.0f);
+                    if (a.lse && lane == 0) a.lse[lse_of(a, k, r)] = -INFINITY;
+                }
+                continue;
+            }
+            ++t;
+            ok = bar_wait_cta(tile_empty(t), (t / kTiles & 1) ^ 1, &gave_up);
+            if (!ok) break;
+            if (lane == 0) tiles[t % kTiles] = k;
+            __syncwarp();
+            if (chosen) bar_arrive(tile_full(t));
+            __syncwarp();
+            if (end) break;
+            ok = bar_wait_cta(q_empty, (t & 1) ^ 1, &gave_up); // the last tile's queries have been read
+            if (ok && chosen) {
+                bar_expect(q_full, Shape::kTile);
+                for (int c = 0; c < kChunks; ++c) tma_load4(base + c * 16384u, &a.q, 64 * c, k.q_row, k.head, a.q_planes > 1 ? k.seq : 0, q_full);
             }
             __syncwarp();
-            if (clear) {
-                ok = bar_wait_cta(tail, tails & 1u, &gave_up);
-                ++tails;
-                if (!ok) return;
-                clear_rows(dst, kChunks, kBlock, valid);
-                if (chosen) bar_arrive(full(stage));
-                __syncwarp();
-            }
-        };
-        // a block of keys, with the tile and its queries where it is the first; false at the end
-        const auto bring_k = [&] {
-            if (kn == k.blocks.count) {
-                for (;;) {
-                    item += gridDim.x;
-                    if (item >= a.items) k.rows = 0, k.blocks.count = 0;
-                    else if (!find_tile(a, item, k)) continue;
-                    if (k.rows == 0 || k.blocks.count > 0) break;
-                    for (int r = 0; r < k.rows; ++r) { // queries that see nothing
-                        T *o = at<T>(a.o, k.seq, k.q_row + r, k.head);
-                        for (int c = lane; c < a.d; c += 32) o[c] = from_f32<T>(0.0f);
-                        if (a.lse && lane == 0) a.lse[lse_of(a, k, r)] = -INFINITY;
-                    }
-                }
-                ++kt;
-                kn = 0;
-                ok = ok && bar_wait_cta(tile_empty(kt), (kt / kTiles & 1) ^ 1, &gave_up);
-                if (!ok) return false;
-                if (lane == 0) tiles[kt % kTiles] = k;
-                __syncwarp();
-                if (chosen) bar_arrive(tile_full(kt));
-                __syncwarp();
-                if (k.rows == 0) {
-                    item = a.items; // the end, from now on
-                    return false;
-                }
-                ok = bar_wait_cta(q_empty, (kt & 1) ^ 1, &gave_up); // the last tile's queries have been read
+            const int head = k.head / a.group, plane = a.k_planes > 1 ? k.seq : 0;
+            for (int n = 0; ok && n < k.blocks.count; ++n, ++g) {
+                const int stage = g % kStages;
+                ok = bar_wait_cta(empty(stage), (g / kStages & 1) ^ 1, &gave_up);
                 if (ok && chosen) {
-                    bar_expect(q_full, Shape::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load4(base + c * 16384u, &a.q, 64 * c, k.q_row, k.head, a.q_planes > 1 ? k.seq : 0, q_full);
+                    bar_expect(full(stage), kSlice);
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) tma_load4(ring + stage * kSlice + c * 8192u, &a.k, 64 * c, k.k_row + k.blocks[n] * kBlock, head, plane, full(stage));
                 }
                 __syncwarp();
             }
-            bring(&a.k, a.k_planes, k, kn, kb, false);
-            ++kn;
-            ++kb;
-            return true;
-        };
-        bool keys = bring_k() && bring_k();
-        for (;;) {
-            if (vn == v.blocks.count) {
-                if (vt == kt || !ok) break;
-                v = tiles[++vt % kTiles];
-                vn = 0;
-                if (v.rows == 0) break;
-            }
-            bring(&a.v, a.v_planes, v, vn, vb, true);
-            ++vn;
-            ++vb;
-            keys = keys && ok && bring_k();
         }
         // every tile has been consumed: nothing is in flight towards this CTA any more
-        for (int s = 0; s < kStages; ++s) {
-            ok = ok && bar_wait_cta(empty((kb + s) % kStages), ((kb + s) / kStages & 1) ^ 1, &gave_up);
-            ok = ok && bar_wait_cta(empty(kStages + (vb + s) % kStages), ((vb + s) / kStages & 1) ^ 1, &gave_up);
+        for (int s = 0; ok && s < kStages; ++s) ok = bar_wait_cta(empty((g + s) % kStages), ((g + s) / kStages & 1) ^ 1, &gave_up);
+    } else if (warp == 7) {
+        // ---------------------------------------------------------- values in
+        const bool chosen = elect_one();
+        int g = 0;
+        uint32_t tails = 0;
+        bool ok = true;
+        for (int t = 0; ok; ++t) {
+            ok = bar_wait_cta(tile_full(t), t / kTiles & 1, &gave_up);
+            if (!ok) break;
+            const Tile v = tiles[t % kTiles];
+            __syncwarp();
+            if (chosen) bar_arrive(tile_empty(t));
+            __syncwarp();
+            if (v.rows == 0) break;
+            const int head = v.head / a.group, plane = a.v_planes > 1 ? v.seq : 0;
+            for (int n = 0; ok && n < v.blocks.count; ++n, ++g) {
+                const int stage = kStages + g % kStages;
+                const int block = v.blocks[n], valid = v.k_count - block * kBlock;
+                const bool clear = a.k_ranges && valid < kBlock;
+                const uint32_t dst = ring + stage * kSlice, bar = clear ? tail : full(stage);
+                ok = bar_wait_cta(empty(stage), (g / kStages & 1) ^ 1, &gave_up);
+                if (!ok) break;
+                if (chosen) {
+                    bar_expect(bar, kSlice);
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) tma_load4(dst + c * 8192u, &a.v, 64 * c, v.k_row + block * kBlock, head, plane, bar);
+                }
+                __syncwarp();
+                if (clear) {
+                    ok = bar_wait_cta(tail, tails & 1u, &gave_up);
+                    ++tails;
+                    if (!ok) break;
+                    clear_rows(dst, kChunks, kBlock, valid);
+                    if (chosen) bar_arrive(full(stage));
+                    __syncwarp();
+                }
+            }
         }
+        for (int s = 0; ok && s < kStages; ++s) ok = bar_wait_cta(empty(kStages + (g + s) % kStages), ((g + s) / kStages & 1) ^ 1, &gave_up);
     } else if (warp == 5) {
         // ---------------------------------------------------------- S = Q K^T, as far ahead as there are buffers
         const bool chosen = elect_one();
@@ -859,9 +856,9 @@ struct BackwardArgs {
 template <int D, bool KEYS>
 struct BackwardShape {
     static constexpr int kBuffers = KEYS && D == 128 ? 2 : 3, kGroups = 2, kThreads = 128 * kGroups + 128;
-    static constexpr int kStages = D == 64 ? 8 : 4;
+    static constexpr int kStages = D == 64 ? 8 : 4, kStay = D == 64 ? 2 : 1; // kStay: the next tile's come while this one's are read
     static constexpr uint32_t kTile = (D / 64) * 16384u, kSlice = (D / 64) * 8192u, kStage = 2 * kSlice; // 128 rows, 64 rows, both tensors' 64
-    static constexpr uint32_t kSmem = 2 * kTile + kStages * kStage + 1024;
+    static constexpr uint32_t kSmem = kStay * 2 * kTile + kStages * kStage + 1024;
     static constexpr uint32_t kColumns = 512, kOut = kBuffers * 128; // of dK or dQ; dV's behind
 };
 
@@ -929,11 +926,11 @@ template <typename T, int D, bool KEYS>
 __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backward(const __grid_constant__ BackwardArgs a)
 {
     using Shape = BackwardShape<D, KEYS>;
-    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kGroups = Shape::kGroups, kLoad = 4 * kGroups, kForm = kLoad + 1, kAdd = kLoad + 2;
+    constexpr int kStages = Shape::kStages, kChunks = D / 64, kBuffers = Shape::kBuffers, kGroups = Shape::kGroups, kStay = Shape::kStay, kLoad = 4 * kGroups, kForm = kLoad + 1, kAdd = kLoad + 2;
     constexpr uint32_t kSlice = Shape::kSlice, kTile = Shape::kTile;
     extern __shared__ char smem_raw[];
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * kTile;
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 5 + 3 * kBuffers];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + kStay * 2 * kTile;
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kTiles + 4 + 2 * kStay + 3 * kBuffers];
     __shared__ BackwardTile tiles[kTiles];
     __shared__ __align__(16) float columns[KEYS ? kStages : 1][2][64]; // KEYS: -lse2 and -delta of the queries that pass
     __shared__ uint32_t tmem_at;
@@ -944,19 +941,27 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     const uint32_t tile0 = bar0 + 16u * kStages, more0 = tile0 + 16u * kTiles;
     const auto tile_full = [&](int t) { return tile0 + 8u * (t % kTiles); };
     const auto tile_empty = [&](int t) { return tile0 + 8u * (kTiles + t % kTiles); };
-    const uint32_t stay_full = more0, stay_empty = more0 + 8, tail = more0 + 16, out_full = more0 + 24, out_empty = more0 + 32;
-    const auto s_full = [&](int g) { return more0 + 40 + 8u * (g % kBuffers); };
-    const auto p_full = [&](int g) { return more0 + 40 + 8u * (kBuffers + g % kBuffers); };
-    const auto out_done = [&](int g) { return more0 + 40 + 8u * (2 * kBuffers + g % kBuffers); };
+    const uint32_t out_full = more0, out_empty = more0 + 8;
+    const auto tail = [&](int i) { return more0 + 16 + 8u * i; };
+    const auto stay_full = [&](int t) { return more0 + 32 + 8u * (t % kStay); };
+    const auto stay_empty = [&](int t) { return more0 + 32 + 8u * (kStay + t % kStay); };
+    const uint32_t more1 = more0 + 32 + 16u * kStay;
+    const auto s_full = [&](int g) { return more1 + 8u * (g % kBuffers); };
+    const auto p_full = [&](int g) { return more1 + 8u * (kBuffers + g % kBuffers); };
+    const auto out_done = [&](int g) { return more1 + 8u * (2 * kBuffers + g % kBuffers); };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * kStages; ++s) bar_init(bar0 + 8u * s, 1);
         for (int t = 0; t < kTiles; ++t) {
             bar_init(tile_full(t), 1);
-            bar_init(tile_empty(t), 4 * kGroups + 1);
+            bar_init(tile_empty(t), 4 * kGroups + 2);
         }
-        for (uint32_t b : {stay_full, stay_empty, tail, out_full}) bar_init(b, 1);
+        for (uint32_t b : {tail(0), tail(1), out_full}) bar_init(b, 1);
+        for (int i = 0; i < kStay; ++i) {
+            bar_init(stay_full(i), 1);
+            bar_init(stay_empty(i), 1);
+        }
         bar_init(out_empty, 4 * kGroups);
         for (int i = 0; i < kBuffers; ++i) {
             bar_init(s_full(i), 1);
@@ -976,11 +981,57 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     wait_prior_grid();
     release_next_grid(); // as in the forward pass
 
+    // Blocks come by two warps, every second one each: what a warp does for a block takes as long as its products.  `g`: blocks before this tile.
+    const auto bring_blocks = [&](const BackwardTile &t, int g, int which, uint32_t tail_bar, uint32_t &tails, bool chosen) {
+        const int first = (g ^ which) & 1, begin = t.begin + first;
+        int member = KEYS ? begin % a.group : 0, block = KEYS ? begin / a.group : 0; // KEYS: of the key head's query heads; of queries
+        const int plane0 = a.pass0_planes > 1 ? t.seq : 0, plane1 = a.pass1_planes > 1 ? t.seq : 0, count = KEYS ? t.q_count : t.k_count;
+        const int64_t lines = KEYS ? ((int64_t)(a.packed_q ? 0 : t.seq) * a.q_heads + t.head * a.group) * a.q_rows + t.q_row + lane : 0;
+        for (int n = first; n < t.count; n += 2) {
+            const int stage = (g + n) % kStages;
+            const int head = KEYS ? t.head * a.group + member : t.head / a.group;
+            const int at_row = KEYS ? t.first + block * 64 : t.blocks[n] * kBlock; // in the sequence
+            const int row = (KEYS ? t.q_row : t.k_row) + at_row, valid = count - at_row;
+            const uint32_t dst = ring + stage * Shape::kStage;
+            const bool clear = (KEYS ? a.q_ranges : a.k_ranges) && valid < kBlock;
+            float lse0 = -INFINITY, lse1 = -INFINITY, delta0 = 0.0f, delta1 = 0.0f; // on their way while the stage is waited for
+            if (KEYS) {
+                const int64_t line = lines + (int64_t)member * a.q_rows + at_row;
+                if (lane < valid) lse0 = -a.lse2[line], delta0 = -a.delta[line];
+                if (lane + 32 < valid) lse1 = -a.lse2[line + 32], delta1 = -a.delta[line + 32];
+                for (member += 2; member >= a.group; member -= a.group) ++block;
+            }
+            if (!bar_wait_cta(empty(stage), ((g + n) / kStages & 1) ^ 1, &gave_up)) return false;
+            if (KEYS) {
+                columns[stage][0][lane] = lse0, columns[stage][0][32 + lane] = lse1;
+                columns[stage][1][lane] = delta0, columns[stage][1][32 + lane] = delta1;
+                __syncwarp();
+            }
+            const uint32_t bar = clear ? tail_bar : full(stage);
+            if (chosen) {
+                bar_expect(bar, Shape::kStage);
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    tma_load4(dst + c * 8192u, &a.pass0, 64 * c, row, head, plane0, bar);
+                    tma_load4(dst + kSlice + c * 8192u, &a.pass1, 64 * c, row, head, plane1, bar);
+                }
+            }
+            __syncwarp();
+            if (clear) {
+                if (!bar_wait_cta(tail_bar, tails & 1u, &gave_up)) return false;
+                ++tails;
+                clear_rows(dst, 2 * kChunks, kBlock, valid);
+                if (chosen) bar_arrive(full(stage));
+                __syncwarp();
+            }
+        }
+        return true;
+    };
     if (warp == kLoad) {
         // ---------------------------------------------------------- tiles in
         const bool chosen = elect_one();
-        int stage = 0, kt = -1;
-        uint32_t phase = 0, tails = 0;
+        int kt = -1, g = 0;
+        uint32_t tails = 0;
         bool ok = true;
         for (int item = blockIdx.x; ok; item += gridDim.x) {
             BackwardTile t;
@@ -1006,73 +1057,42 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             if (chosen) bar_arrive(tile_full(kt));
             __syncwarp();
             if (end) break;
-            ok = bar_wait_cta(stay_empty, (kt & 1) ^ 1, &gave_up); // the last tile's have been read
+            ok = bar_wait_cta(stay_empty(kt), (kt / kStay & 1) ^ 1, &gave_up); // those that were there have been read
             if (!ok) break;
             if (chosen) {
-                const int head = t.head;
-                bar_expect(stay_full, 2 * kTile);
+                const int head = t.head, plane0 = a.stay0_planes > 1 ? t.seq : 0, plane1 = a.stay1_planes > 1 ? t.seq : 0;
+                const uint32_t stay = base + (kt % kStay) * 2 * kTile;
+                bar_expect(stay_full(kt), 2 * kTile);
+#pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
-                    tma_load4(base + c * 16384u, &a.stay0, 64 * c, t.row, head, a.stay0_planes > 1 ? t.seq : 0, stay_full);
-                    tma_load4(base + kTile + c * 16384u, &a.stay1, 64 * c, t.row, head, a.stay1_planes > 1 ? t.seq : 0, stay_full);
+                    tma_load4(stay + c * 16384u, &a.stay0, 64 * c, t.row, head, plane0, stay_full(kt));
+                    tma_load4(stay + kTile + c * 16384u, &a.stay1, 64 * c, t.row, head, plane1, stay_full(kt));
                 }
             }
             __syncwarp();
-            int member = KEYS ? t.begin % a.group : 0, block = KEYS ? t.begin / a.group : 0; // KEYS: of the key head's query heads; of queries
-            for (int n = 0; ok && n < t.count; ++n) {
-                const int head = KEYS ? t.head * a.group + member : t.head / a.group;
-                const int at_row = KEYS ? t.first + block * 64 : t.blocks[n] * kBlock; // in the sequence
-                const int row = (KEYS ? t.q_row : t.k_row) + at_row, valid = (KEYS ? t.q_count : t.k_count) - at_row;
-                const uint32_t dst = ring + stage * Shape::kStage;
-                const bool clear = (KEYS ? a.q_ranges : a.k_ranges) && valid < kBlock;
-                float lines[2][2]; // on their way while the stage is waited for
-                if (KEYS) {
-                    const int64_t line = ((int64_t)(a.packed_q ? 0 : t.seq) * a.q_heads + head) * a.q_rows + row;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const bool in = 32 * i + lane < valid;
-                        lines[0][i] = in ? a.lse2[line + 32 * i + lane] : INFINITY;
-                        lines[1][i] = in ? a.delta[line + 32 * i + lane] : 0.0f;
-                    }
-                    if (++member == a.group) member = 0, ++block;
-                }
-                ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
-                if (!ok) break;
-                if (KEYS) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) columns[stage][0][32 * i + lane] = -lines[0][i], columns[stage][1][32 * i + lane] = -lines[1][i];
-                    __syncwarp();
-                }
-                const uint32_t bar = clear ? tail : full(stage);
-                if (chosen) {
-                    bar_expect(bar, Shape::kStage);
-                    for (int c = 0; c < kChunks; ++c) {
-                        tma_load4(dst + c * 8192u, &a.pass0, 64 * c, row, head, a.pass0_planes > 1 ? t.seq : 0, bar);
-                        tma_load4(dst + kSlice + c * 8192u, &a.pass1, 64 * c, row, head, a.pass1_planes > 1 ? t.seq : 0, bar);
-                    }
-                }
-                __syncwarp();
-                if (clear) {
-                    ok = bar_wait_cta(tail, tails & 1u, &gave_up);
-                    ++tails;
-                    if (!ok) break;
-                    clear_rows(dst, 2 * kChunks, kBlock, valid);
-                    if (chosen) bar_arrive(full(stage));
-                    __syncwarp();
-                }
-                if (++stage == kStages) stage = 0, phase ^= 1u;
-            }
+            ok = bring_blocks(t, g, 0, tail(0), tails, chosen);
+            g += t.count;
         }
         // every tile has been consumed: nothing is in flight towards this CTA any more
-        for (int s = 0; ok && s < kStages; ++s) {
-            ok = bar_wait_cta(empty(stage), phase ^ 1u, &gave_up);
-            if (++stage == kStages) stage = 0, phase ^= 1u;
+        for (int s = 0; ok && s < kStages; ++s) ok = bar_wait_cta(empty((g + s) % kStages), ((g + s) / kStages & 1) ^ 1, &gave_up);
+    } else if (warp == kLoad + 3) {
+        const bool chosen = elect_one();
+        int g = 0;
+        uint32_t tails = 0;
+        for (int vt = 0;; ++vt) {
+            if (!bar_wait_cta(tile_full(vt), vt / kTiles & 1, &gave_up)) break;
+            const BackwardTile t = tiles[vt % kTiles];
+            __syncwarp();
+            if (chosen) bar_arrive(tile_empty(vt));
+            __syncwarp();
+            if (t.rows == 0 || !bring_blocks(t, g, 1, tail(1), tails, chosen)) break;
+            g += t.count;
         }
     } else if (warp == kForm) {
         // ---------------------------------------------------------- S and dP, as far ahead as there are buffers
         const bool chosen = elect_one();
         const int steps = (a.d + 15) / 16;
         const uint32_t desc = instruction_desc(type_bits<T>(), false, false, 128, kBlock);
-        const uint64_t d0 = operand_desc(base, 16), d1 = operand_desc(base + kTile, 16);
         const bool with0 = a.out0.p != nullptr;
         int g = 0;
         bool ok = true;
@@ -1080,7 +1100,9 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             ok = bar_wait_cta(tile_full(t), t / kTiles & 1, &gave_up);
             const int count = ok ? tiles[t % kTiles].count : 0;
             if (count == 0) break;
-            ok = bar_wait_cta(stay_full, t & 1, &gave_up);
+            ok = bar_wait_cta(stay_full(t), t / kStay & 1, &gave_up);
+            const uint32_t stay = base + (t % kStay) * 2 * kTile;
+            const uint64_t d0 = operand_desc(stay, 16), d1 = operand_desc(stay + kTile, 16);
             for (int n = 0; ok && n < count; ++n, ++g) {
                 const int stage = g % kStages;
                 ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up);
@@ -1103,7 +1125,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                         }
                     }
                     commit(s_full(g));
-                    if (n + 1 == count) commit(stay_empty);
+                    if (n + 1 == count) commit(stay_empty(t));
                 }
                 __syncwarp();
             }
