@@ -53,7 +53,7 @@ struct ForwardArgs {
     int packed_q, q_planes, k_planes, v_planes; // planes: more than one: by sequence
     int sequences, tiles;                       // tiles of a sequence, or of all packed ones
     int items, lanes, together;                 // tiles of all heads; heads, times sequences that are not packed; of them at a time
-    int wide_o;                                 // 16-byte stores
+    int wide_o;                                 // bytes of a store
     float scale_log2;
 };
 
@@ -126,10 +126,22 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int chunks, int rows, 
     __syncwarp();
 }
 
+// Up to 32 elements of a row: 32 or 16 bytes at a time (a thread's own sectors: 16-byte stores half fill them), or one element.
 template <typename T>
-__device__ __forceinline__ void store_row(T *p, const float *v, int count, bool wide) // up to 32 elements
+__device__ __forceinline__ void store_row(T *p, const float *v, int count, int bytes)
 {
-    if (wide) {
+    if (bytes == 32) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 16) {
+            if (i >= count) break;
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = pack2(v[i + 2 * k], v[i + 2 * k + 1], T());
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + i), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                         "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
+        }
+    } else if (bytes == 16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (8 * i < count)
@@ -1490,6 +1502,13 @@ bool make_map(CUtensorMap *map, const Tensor &t, int dtype, int box)
 }
 // 16-byte accesses to whole rows of heads
 bool wide(const Tensor &t) { return t.d % 8 == 0 && tma_ok(t); }
+// The widest stores to them, in bytes.
+int store_bytes(const Tensor &t)
+{
+    const auto step = [](int64_t extent, int64_t stride) { return extent <= 1 || stride % 16 == 0; };
+    if (!t.h.p || !wide(t)) return 2;
+    return t.d % 16 == 0 && aligned(t.h.p, 32) && step(t.rows, t.h.row) && step(t.heads, t.h.head) && step(t.planes, t.h.seq) ? 32 : 16;
+}
 
 struct Packer {
     PackArgs args{};
@@ -1614,7 +1633,7 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     f.packed_q = shape->q_ranges && q.h.seq == 0;
     f.q_planes = pq.planes, f.k_planes = pk.planes, f.v_planes = pv.planes;
     f.sequences = (int)shape->sequences;
-    f.wide_o = wide(o);
+    f.wide_o = store_bytes(o);
     f.scale_log2 = (float)(shape->scale * 1.4426950408889634);
     return q.d <= 64 ? launch_forward<T, 64>(f, q.rows, sms, s) : launch_forward<T, 128>(f, q.rows, sms, s);
 }
@@ -1679,7 +1698,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         if (!maps()) return A2SGD_ERR_CUDA;
         b.stay0_planes = q.planes, b.stay1_planes = dout.planes, b.pass0_planes = k.planes, b.pass1_planes = v.planes;
         b.out0 = dq.h, b.out1 = Heads{nullptr, 0, 0, 0};
-        b.wide0 = wide(dq);
+        b.wide0 = store_bytes(dq);
         rc = launch_backward<T, D, false>(b, q.rows, sms, s);
         if (rc != A2SGD_OK) return rc;
     }
@@ -1691,7 +1710,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         if (!maps()) return A2SGD_ERR_CUDA;
         b.stay0_planes = k.planes, b.stay1_planes = v.planes, b.pass0_planes = q.planes, b.pass1_planes = dout.planes;
         b.out0 = dk.h, b.out1 = dv.h;
-        b.wide0 = wide(dk), b.wide1 = wide(dv);
+        b.wide0 = store_bytes(dk), b.wide1 = store_bytes(dv);
         rc = launch_backward<T, D, true>(b, k.rows, sms, s);
         if (rc != A2SGD_OK) return rc;
         if (b.parts > 1) {
