@@ -239,7 +239,8 @@ template <typename T, typename R, int VEC, int C, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) k_forward(const __grid_constant__ Args a)
 {
     extern __shared__ __align__(16) float columns[]; // alpha gate w1, alpha gate b1, w2, b2
-    __shared__ float slots[2][48];
+    __shared__ float slots[2][48]; // in turn: one barrier a norm leaves no time to empty them
+    int turn = 0;
     wait_prior_grid();
     release_next_grid();
     const int64_t row0 = (int64_t)blockIdx.x * a.run, end = min(a.rows, row0 + a.run);
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) 
         }
         float mean = 0.0f, rstd = 1.0f;
         if (a.post) {
-            moments<VEC, C>(n, a, slots[0], mean, rstd);
+            moments<VEC, C>(n, a, slots[turn ^= 1], mean, rstd);
             if (threadIdx.x == 0) {
                 if (a.mean1) a.mean1[r] = mean;
                 if (a.rstd1) a.rstd1[r] = rstd;
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) 
             singles8(f, z[k]);
             Eight<R, VEC>::store(static_cast<R *>(a.z.p) + r * a.z.ld, k, a.d, f);
         }
-        moments<VEC, C>(z, a, slots[1], mean, rstd);
+        moments<VEC, C>(z, a, slots[turn ^= 1], mean, rstd);
         if (threadIdx.x == 0) {
             if (a.mean2) a.mean2[r] = mean;
             if (a.rstd2) a.rstd2[r] = rstd;
@@ -325,7 +326,8 @@ template <typename T, typename R, int VEC, int C, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(const __grid_constant__ Args a)
 {
     extern __shared__ __align__(16) float columns[]; // w2, alpha gate w1 (alpha gate without a norm), and for C > 1 the four sums
-    __shared__ float slots[2][48];
+    __shared__ float slots[2][48]; // in turn: one barrier a norm leaves no time to empty them
+    int turn = 0;
     wait_prior_grid();
     release_next_grid();
     const int64_t row0 = (int64_t)blockIdx.x * a.run, end = min(a.rows, row0 + a.run);
@@ -420,7 +422,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
         }
         float s0 = sum2(s0s), s1 = sum2(s1s);
         if (r + 1 < end) bring_pre(r + 1);
-        cta_sums(s0, s1, slots[0]);
+        cta_sums(s0, s1, slots[turn ^= 1]);
         s0 = a.rms ? 0.0f : s0 * per;
         s1 *= per;
         // t, dx, and the norm after the block
@@ -454,7 +456,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
         float p0 = sum2(p0s), p1 = sum2(p1s);
         if (r + 1 < end) bring_post(r + 1);
         if (a.post) {
-            cta_sums(p0, p1, slots[1]);
+            cta_sums(p0, p1, slots[turn ^= 1]);
             p0 = a.rms ? 0.0f : p0 * per;
             p1 *= per;
         }

@@ -130,6 +130,28 @@ def test_on_another_stream_and_side_by_side():
         assert torch.equal(w[0], g[0]) and torch.equal(w[1], g[1]) and all(torch.equal(a, b) for a, b in zip(w[2], g[2]))
 
 
+@pytest.mark.parametrize("d", [1600, 4096, 8192])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_residual_without_the_first_norm_again_and_again(kind, d):
+    """One norm a row: its warps' sums have two places, in turn, as a warp may be a row ahead of another."""
+    gen = torch.Generator("cuda").manual_seed(9)
+    x, y, dz, du = (torch.empty((6007, d), device="cuda").normal_(generator=gen).to(BF16) for _ in range(4))
+    first = None
+    for _ in range(20):
+        z, u, dx, dy = (torch.empty_like(x) for _ in range(4))
+        mean, rstd = torch.empty(6007, device="cuda"), torch.empty(6007, device="cuda")
+        B.a2sgd_residual_norm_forward(x, y, z, u, kind, post=False, pre_mean=mean, pre_rstd=rstd)
+        B.a2sgd_residual_norm_backward(dz, du, y, z, dx, dy, kind, post=False, pre_mean=mean, pre_rstd=rstd)
+        out = [z, u, dx, dy, mean, rstd]
+        first = first or out
+        assert all(torch.equal(a, b) for a, b in zip(first, out))
+    # 64-bit: the statistics are of z before its rounding; d products and sums in fp32, the root's and the quotient's rounding
+    zz = x.double() + y.double()
+    m = zz.mean(1, keepdim=True) if kind == "layer" else torch.zeros_like(zz[:, :1])
+    r = ((zz - m).square().mean(1) + 1e-5).rsqrt()
+    assert ((rstd.double() - r).abs() <= (d + 8) * 2.0 ** -24 * r).all()
+
+
 def test_rotary_beyond_two_to_the_31():
     gen = torch.Generator("cuda").manual_seed(1)
     q = far_rows(gen, 140, 2, 64, BF16)
