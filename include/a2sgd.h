@@ -514,7 +514,8 @@ int a2sgd_gated_ffn_status(int device, int *device_status, void *stream);
  * The conventions above hold.
  *
  * A tensor of heads: element c of head h in row t of sequence b is at p[b sequence_stride + t row_stride + h head_stride + c],
- * strides in ELEMENTS.  Packed sequences share one plane: sequence_stride 0, and ranges say which rows are whose. */
+ * strides in ELEMENTS.  Packed sequences share one plane: sequence_stride 0, and ranges say which rows are whose; what is written (o, dq like
+ * q; dk, dv like k) is then packed, too, and else it is not.  Without ranges sequence_stride 0 says that all sequences read the same plane. */
 typedef struct a2sgd_heads {
     void *p;
     int64_t sequence_stride, row_stride, head_stride;
@@ -540,7 +541,9 @@ typedef struct a2sgd_heads {
  * as long as it lies in its sequence's range.
  *   workspace   DEVICE, 256-byte aligned, a2sgd_window_attention_workspace bytes: flags A2SGD_ATTENTION_BACKWARD,
  *               A2SGD_ATTENTION_ALIGNED when every tensor that is read is laid out as above, and A2SGD_ATTENTION_PACKED_Q, _PACKED_K
- *               when the q and the k tensors hold packed sequences (else room is needed for each sequence's plane)
+ *               when the q and the k tensors hold packed sequences (else room is needed for each sequence's plane).  Few queries
+ *               over long caches: the room asked for lets a row's keys be shared out over the whole device; with less than that the call
+ *               works, too, by at most eight CTAs a row
  * Outputs must not overlap an input or one another. */
 #define A2SGD_ATTENTION_MAX_HEAD_DIM 128
 #define A2SGD_ATTENTION_BACKWARD 1u

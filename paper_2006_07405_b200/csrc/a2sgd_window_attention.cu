@@ -1427,15 +1427,18 @@ int check_shape(const a2sgd_attention *s)
     return A2SGD_OK;
 }
 
-// A tensor of `heads` heads and `rows` rows a sequence.  written: no two elements may share a place.
+// A tensor of `heads` heads and `rows` rows a sequence.  like: it is written, as the tensor `like` is read: no two elements may share a place, and it
+// is packed where that is.
 int check_heads(const a2sgd_attention *s, const a2sgd_heads *h, uint32_t heads, uint64_t rows, const int32_t *ranges, bool needed,
-                bool written)
+                const a2sgd_heads *like)
 {
     if (!h || !h->p) return needed && rows ? A2SGD_ERR_ARG : A2SGD_OK;
     if (h->sequence_stride < 0 || h->row_stride < 0 || h->head_stride < 0) return A2SGD_ERR_ARG;
-    if (written && ((h->sequence_stride == 0 && s->sequences > 1 && !ranges) || (h->row_stride == 0 && rows > 1) ||
-                    (h->head_stride == 0 && heads > 1)))
-        return A2SGD_ERR_ARG;
+    if (like) {
+        const bool packed = ranges && (!like->p || like->sequence_stride == 0);
+        if ((s->sequences > 1 && (h->sequence_stride == 0) != packed) || (h->row_stride == 0 && rows > 1) || (h->head_stride == 0 && heads > 1))
+            return A2SGD_ERR_ARG;
+    }
     return aligned(h->p, 2) ? A2SGD_OK : A2SGD_ERR_ALIGN;
 }
 
@@ -1790,10 +1793,10 @@ extern "C" int a2sgd_window_attention_forward(const a2sgd_attention *shape, cons
 {
     int rc = check_shape(shape);
     if (rc != A2SGD_OK || shape->sequences == 0 || shape->q_rows == 0) return rc;
-    if ((rc = check_heads(shape, q, shape->q_heads, shape->q_rows, shape->q_ranges, true, false)) != A2SGD_OK ||
-        (rc = check_heads(shape, k, shape->kv_heads, shape->k_rows, shape->k_ranges, true, false)) != A2SGD_OK ||
-        (rc = check_heads(shape, v, shape->kv_heads, shape->k_rows, shape->k_ranges, true, false)) != A2SGD_OK ||
-        (rc = check_heads(shape, o, shape->q_heads, shape->q_rows, shape->q_ranges, true, true)) != A2SGD_OK)
+    if ((rc = check_heads(shape, q, shape->q_heads, shape->q_rows, shape->q_ranges, true, nullptr)) != A2SGD_OK ||
+        (rc = check_heads(shape, k, shape->kv_heads, shape->k_rows, shape->k_ranges, true, nullptr)) != A2SGD_OK ||
+        (rc = check_heads(shape, v, shape->kv_heads, shape->k_rows, shape->k_ranges, true, nullptr)) != A2SGD_OK ||
+        (rc = check_heads(shape, o, shape->q_heads, shape->q_rows, shape->q_ranges, true, q)) != A2SGD_OK)
         return rc;
     if (!aligned(workspace, 256) || !aligned(lse, 4)) return A2SGD_ERR_ALIGN;
     DeviceGuard guard(device);
@@ -1813,12 +1816,12 @@ extern "C" int a2sgd_window_attention_backward(const a2sgd_attention *shape, con
     int rc = check_shape(shape);
     if (rc != A2SGD_OK || shape->sequences == 0) return rc;
     for (const a2sgd_heads *h : {dout, q, o})
-        if ((rc = check_heads(shape, h, shape->q_heads, shape->q_rows, shape->q_ranges, true, false)) != A2SGD_OK) return rc;
+        if ((rc = check_heads(shape, h, shape->q_heads, shape->q_rows, shape->q_ranges, true, nullptr)) != A2SGD_OK) return rc;
     for (const a2sgd_heads *h : {k, v})
-        if ((rc = check_heads(shape, h, shape->kv_heads, shape->k_rows, shape->k_ranges, true, false)) != A2SGD_OK) return rc;
+        if ((rc = check_heads(shape, h, shape->kv_heads, shape->k_rows, shape->k_ranges, true, nullptr)) != A2SGD_OK) return rc;
     for (const a2sgd_heads *h : {dk, dv})
-        if ((rc = check_heads(shape, h, shape->kv_heads, shape->k_rows, shape->k_ranges, false, true)) != A2SGD_OK) return rc;
-    if ((rc = check_heads(shape, dq, shape->q_heads, shape->q_rows, shape->q_ranges, false, true)) != A2SGD_OK) return rc;
+        if ((rc = check_heads(shape, h, shape->kv_heads, shape->k_rows, shape->k_ranges, false, k)) != A2SGD_OK) return rc;
+    if ((rc = check_heads(shape, dq, shape->q_heads, shape->q_rows, shape->q_ranges, false, q)) != A2SGD_OK) return rc;
     if (!lse && shape->q_rows) return A2SGD_ERR_ARG;
     if (!aligned(workspace, 256) || !aligned(lse, 4)) return A2SGD_ERR_ALIGN;
     DeviceGuard guard(device);

@@ -52,6 +52,8 @@ def test_attention_tensors():
     assert forward(s, q=heads(p=FAKE + 1)) == B.ERR_ALIGN
     assert forward(s, lse=FAKE + 2) == B.ERR_ALIGN
     assert forward(s, workspace=FAKE + 64, bytes_=1 << 20) == B.ERR_ALIGN
+    # packed queries and an output that is not, and the other way round
+    assert forward(shape(q_ranges=FAKE), q=heads(seq=0)) == B.ERR_ARG and forward(shape(q_ranges=FAKE), o=heads(seq=0)) == B.ERR_ARG
     # outputs whose elements share a place
     assert forward(s, o=heads(seq=0)) == B.ERR_ARG and forward(s, o=heads(row=0)) == B.ERR_ARG and forward(s, o=heads(head=0)) == B.ERR_ARG
     assert B.lib().a2sgd_window_attention_forward(None, at(heads()), at(heads()), at(heads()), at(heads()), None, None, 0, 0, None) == B.ERR_ARG
@@ -66,6 +68,9 @@ def test_attention_backward():
     assert go(shape(), [t] * 8, lse=None) == B.ERR_ARG
     assert go(shape(), [t] * 5 + [heads(head=0), None, None]) == B.ERR_ARG
     assert go(shape(), [t] * 5 + [None, heads(row=0), None]) == B.ERR_ARG
+    assert go(shape(k_ranges=FAKE), [t, t, heads(seq=0), heads(seq=0), t, None, t, None]) == B.ERR_ARG
+    assert go(shape(k_ranges=FAKE), [t] * 7 + [heads(seq=0)]) == B.ERR_ARG
+    assert go(shape(q_ranges=FAKE), [t, heads(seq=0), t, t, t, t, None, None]) == B.ERR_ARG
     assert go(shape(), [t] * 8, ws=FAKE + 8) == B.ERR_ALIGN
     assert go(shape(window=0), [t] * 8) == B.ERR_ARG
 
