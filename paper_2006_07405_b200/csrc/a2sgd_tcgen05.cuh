@@ -187,12 +187,6 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// A warpgroup's registers a thread from here on.  The warpgroups' shares add up to at most what the launch gave the block.
-template <int N>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
 // ------------------------------------------------------------------ a CTA by itself
 __device__ __forceinline__ void bar_arrive(uint32_t bar)
 {
@@ -208,18 +202,6 @@ __device__ __forceinline__ bool bar_try_cta(uint32_t bar, uint32_t parity)
                  : "r"(bar), "r"(parity)
                  : "memory");
     return done != 0;
-}
-// Whether the barrier's phase is complete, without waiting; the whole warp gets one answer.
-__device__ __forceinline__ bool bar_test_cta(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\t"
-                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                 "selp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
-    return __all_sync(0xffffffffu, done);
 }
 // bar_wait for a barrier that only this CTA's threads, copies and products arrive on.
 __device__ __forceinline__ bool bar_wait_cta(uint32_t bar, uint32_t parity, volatile int *gave_up)
