@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -822,15 +823,22 @@ class _ResidualShape(ctypes.Structure):
                                     "pre_mean", "pre_rstd")]
 
 
-def _heads(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int):
+# a2sgd_heads and a2sgd_rows as bytes, which ctypes passes by address: a quarter of what an array of its own costs
+_pack_heads = struct.Struct("4q").pack
+_pack_rows = struct.Struct("2q").pack
+
+
+def _heads(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> bytes:
     """CUDA [sequences, rows, heads, head_dim], or [rows, heads, head_dim] of packed sequences, unit inner stride ->
-    (address, sequence stride, row stride, head stride)."""
+    address, sequence stride, row stride, head stride."""
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
         raise ValueError(f"{name}: need a {dtype} tensor {list(shape)} on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
     stride = t.stride()
     if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: need unit inner stride")
-    return (t.data_ptr(), 0, stride[0], stride[1]) if len(shape) == 3 else (t.data_ptr(), *stride[:3])
+    if len(shape) == 3:
+        return _pack_heads(t.data_ptr(), 0, stride[0], stride[1])
+    return _pack_heads(t.data_ptr(), stride[0], stride[1], stride[2])
 
 
 def _ranges(t: Optional[torch.Tensor], name: str, sequences: int, index: int) -> Optional[int]:
@@ -876,14 +884,6 @@ def _lse(t, q, dev):
     return _vector(t, "lse", t.numel(), torch.float32, dev)
 
 
-def _table(*heads):
-    """The tensors' (address, strides) one after another in memory, as the header's structures, and where each begins."""
-    flat = [x for h in heads for x in (h if h is not None else (0, 0, 0, 0))]
-    table = (_i64 * len(flat))(*flat)
-    at = ctypes.addressof(table)
-    return table, [at + 32 * i for i in range(len(heads))]
-
-
 def a2sgd_window_attention_workspace(q: torch.Tensor, k: torch.Tensor, window: Optional[int], sinks: int, sequences: int,
                                      backward: bool = False, aligned: bool = False) -> int:
     """Bytes of workspace of a2sgd_window_attention_forward (or _backward).  aligned: every tensor that is read starts at a multiple
@@ -906,11 +906,10 @@ def a2sgd_window_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Te
     [sequences, 2], first row and number of rows, or None for all.  workspace: uint8 CUDA tensor of
     a2sgd_window_attention_workspace bytes."""
     dev, shape = _attention_shape(q, k, window, sinks, scale, q_ranges, k_ranges)
-    dt, wb = q.dtype, 0 if workspace is None else workspace.numel()
-    table, (qa, ka, va, oa) = _table(_heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev),
-                                     _heads(v, "v", k.shape, dt, dev), _heads(o, "o", q.shape, dt, dev))
+    dt, wb, qs, ks = q.dtype, 0 if workspace is None else workspace.numel(), q.shape, k.shape
     _check(lib().a2sgd_window_attention_forward(
-        ctypes.addressof(shape), qa, ka, va, oa, _lse(lse, q, dev), _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev,
+        ctypes.addressof(shape), _heads(q, "q", qs, dt, dev), _heads(k, "k", ks, dt, dev), _heads(v, "v", ks, dt, dev),
+        _heads(o, "o", qs, dt, dev), _lse(lse, q, dev), _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev,
         _stream_on(dev, stream)), "a2sgd_window_attention_forward")
 
 
@@ -925,12 +924,11 @@ def a2sgd_window_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torc
     dev, shape = _attention_shape(q, k, window, sinks, scale, q_ranges, k_ranges)
     dt, wb = q.dtype, 0 if workspace is None else workspace.numel()
     maybe = lambda t, name, like: None if t is None else _heads(t, name, like.shape, dt, dev)  # noqa: E731
-    table, at = _table(_heads(dout, "dout", q.shape, dt, dev), _heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev),
-                       _heads(v, "v", k.shape, dt, dev), _heads(o, "o", q.shape, dt, dev), maybe(dq, "dq", q), maybe(dk, "dk", k),
-                       maybe(dv, "dv", k))
     _check(lib().a2sgd_window_attention_backward(
-        ctypes.addressof(shape), *at[:5], _lse(lse, q, dev), *at[5:], _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev,
-        _stream_on(dev, stream)), "a2sgd_window_attention_backward")
+        ctypes.addressof(shape), _heads(dout, "dout", q.shape, dt, dev), _heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev),
+        _heads(v, "v", k.shape, dt, dev), _heads(o, "o", q.shape, dt, dev), _lse(lse, q, dev), maybe(dq, "dq", q), maybe(dk, "dk", k),
+        maybe(dv, "dv", k), _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev, _stream_on(dev, stream)),
+        "a2sgd_window_attention_backward")
 
 
 def a2sgd_window_attention_status(device: Optional[int] = None, stream=None) -> int:
@@ -961,12 +959,15 @@ def a2sgd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor
     pos = _vector(positions, "positions", axes * tokens, torch.int32, dev)
     if axes and min(sections) < 1:
         raise ValueError("sections: need at least one pair each")
-    none = (0, 0, 0, 0)
-    table, at = _table(_heads(q, "q", q.shape, q.dtype, dev), none if k is None else _heads(k, "k", k.shape, q.dtype, dev),
-                       _heads(q_out, "q_out", q.shape, q.dtype, dev), none if k is None else _heads(k_out, "k_out", k.shape, q.dtype, dev))
+    shape, dt = q.shape, q.dtype
+    k_shape, k_in, k_turned = None, None, None
+    if k is not None:
+        k_shape = k.shape
+        k_in, k_turned = _heads(k, "k", k_shape, dt, dev), _heads(k_out, "k_out", k_shape, dt, dev)
     flags = (ROTARY_INTERLEAVED if interleaved else 0) | (ROTARY_LADDER_PER_AXIS if ladder_per_axis else 0) | (ROTARY_INVERSE if inverse else 0)
-    _check(lib().a2sgd_rotary(*at, pos, axes, (ctypes.c_uint32 * axes)(*sections), base, flags, tokens, heads,
-                              0 if k is None else k.shape[1], d, code, dev, _stream_on(dev, stream)), "a2sgd_rotary")
+    _check(lib().a2sgd_rotary(_heads(q, "q", shape, dt, dev), k_in, _heads(q_out, "q_out", shape, dt, dev), k_turned, pos, axes,
+                              struct.pack(f"{axes}I", *sections), base, flags, tokens, heads, k_shape[1] if k_shape else 0, d, code, dev,
+                              _stream_on(dev, stream)), "a2sgd_rotary")
 
 
 _NORM_KINDS = {"layer": 0, "rms": RESIDUAL_RMS}
@@ -985,20 +986,18 @@ def _residual_shape(y, residual, kind, post, post_weight, post_bias, gate, gate_
         if gate_rows < 1:
             raise ValueError("gate_rows: at least 1 with a gate")
         groups = -(-rows // gate_rows)
-    rest = [_vector(t, name, n, dtype, dev) for t, name, n, dtype in
-            ((post_weight, "post_weight", d, pt), (post_bias, "post_bias", d, pt), (gate, "gate", groups * d, pt),
-             (pre_weight, "pre_weight", d, pt), (pre_bias, "pre_bias", d, pt))]
-    rest += [_vector(t, name, rows, torch.float32, dev) for t, name in zip(stats, ("post_mean", "post_rstd", "pre_mean", "pre_rstd"))]
+    rest = [None if t is None else _vector(t, name, n, pt, dev) for t, name, n in
+            ((post_weight, "post_weight", d), (post_bias, "post_bias", d), (gate, "gate", groups * d), (pre_weight, "pre_weight", d),
+             (pre_bias, "pre_bias", d))]
+    rest += [None if t is None else _vector(t, name, rows, torch.float32, dev)
+             for t, name in zip(stats, ("post_mean", "post_rstd", "pre_mean", "pre_rstd"))]
     shape = _ResidualShape(rows, gate_rows if gate is not None else 0, d, _NORM_KINDS[kind] | (RESIDUAL_POST_NORM if post else 0), code,
                            _dtype_code(residual, "x or z"), _DTYPE_CODES.get(pt, -1), 0, alpha, eps, *rest)
     return dev, shape, pt, groups
 
 
-def _rows_table(dev, shape, *tensors):
-    flat = [x for t, name, dtype in tensors for x in ((0, 0) if t is None else _matrix(t, name, shape, dtype, dev))]
-    table = (_i64 * len(flat))(*flat)
-    at = ctypes.addressof(table)
-    return table, [at + 16 * i for i in range(len(tensors))]
+def _row_matrix(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, index: int) -> Optional[bytes]:
+    return None if t is None else _pack_rows(*_matrix(t, name, shape, dtype, index))
 
 
 def a2sgd_residual_norm_forward(x: torch.Tensor, y: torch.Tensor, z: torch.Tensor, u: torch.Tensor, kind: str = "rms",
@@ -1013,8 +1012,10 @@ def a2sgd_residual_norm_forward(x: torch.Tensor, y: torch.Tensor, z: torch.Tenso
     of float32 or y's type, each may be None.  post_mean ... pre_rstd: float32 [rows], out, or None."""
     dev, shape, _, _ = _residual_shape(y, x, kind, post, post_weight, post_bias, gate, gate_rows, alpha, pre_weight, pre_bias,
                                        (post_mean, post_rstd, pre_mean, pre_rstd), eps)
-    table, at = _rows_table(dev, y.shape, (x, "x", x.dtype), (y, "y", y.dtype), (z, "z", x.dtype), (u, "u", y.dtype))
-    _check(lib().a2sgd_residual_norm_forward(ctypes.addressof(shape), *at, dev, _stream_on(dev, stream)), "a2sgd_residual_norm_forward")
+    rows_d, yt, xt = y.shape, y.dtype, x.dtype
+    _check(lib().a2sgd_residual_norm_forward(
+        ctypes.addressof(shape), _row_matrix(x, "x", rows_d, xt, dev), _row_matrix(y, "y", rows_d, yt, dev), _row_matrix(z, "z", rows_d, xt, dev),
+        _row_matrix(u, "u", rows_d, yt, dev), dev, _stream_on(dev, stream)), "a2sgd_residual_norm_forward")
 
 
 def a2sgd_residual_norm_workspace(rows: int, d: int, gate_rows: int = 0, device: Optional[int] = None) -> int:
@@ -1040,12 +1041,12 @@ def a2sgd_residual_norm_backward(dz: Optional[torch.Tensor], du: torch.Tensor, y
                                              (post_mean, post_rstd, pre_mean, pre_rstd), 0.0, dpost_weight, dpost_bias, dgate,
                                              dpre_weight, dpre_bias)
     d = y.shape[1]
-    table, at = _rows_table(dev, y.shape, (dz, "dz", z.dtype), (du, "du", y.dtype), (y, "y", y.dtype), (z, "z", z.dtype),
-                            (dx, "dx", z.dtype), (dy, "dy", y.dtype))
+    tensors = [_row_matrix(t, name, y.shape, dtype, dev) for t, name, dtype in
+               ((dz, "dz", z.dtype), (du, "du", y.dtype), (y, "y", y.dtype), (z, "z", z.dtype), (dx, "dx", z.dtype), (dy, "dy", y.dtype))]
     sums = (_vp * 5)(_vector(dpost_weight, "dpost_weight", d, pt, dev), _vector(dpost_bias, "dpost_bias", d, pt, dev),
                      _vector(dgate, "dgate", groups * d, pt, dev), _vector(dpre_weight, "dpre_weight", d, pt, dev),
                      _vector(dpre_bias, "dpre_bias", d, pt, dev))
     wb = 0 if workspace is None else workspace.numel()
-    _check(lib().a2sgd_residual_norm_backward(ctypes.addressof(shape), *at, ctypes.addressof(sums),
+    _check(lib().a2sgd_residual_norm_backward(ctypes.addressof(shape), *tensors, ctypes.addressof(sums),
                                               _vector(workspace, "workspace", wb, torch.uint8, dev), wb, dev, _stream_on(dev, stream)),
            "a2sgd_residual_norm_backward")
