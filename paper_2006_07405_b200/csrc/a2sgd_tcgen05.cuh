@@ -28,6 +28,9 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The two halves of it: this CTA has begun (nothing written before is meant), and so have all others.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // The same place in the shared memory of the cluster's CTA `rank`.
 __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank)
 {
@@ -35,6 +38,7 @@ __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
 
 // ------------------------------------------------------------------ mbarriers
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)

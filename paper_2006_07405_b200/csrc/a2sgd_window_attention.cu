@@ -565,8 +565,9 @@ constexpr int kFewRows = 16, kFewKeys = 16, kFewCluster = 8, kMostShares = 320; 
 template <int D>
 struct FewShape {
     static constexpr int kWarps = D == 64 ? 8 : 4, kStages = 3;
-    static constexpr uint32_t kKeys = kFewKeys * D * 2, kStage = 2 * kKeys, kSmem = kWarps * kStages * kStage;
-    static constexpr int kPartial = kFewRows * (D + 2); // floats: outputs, maxima, sums
+    static constexpr int kRow = D + 2, kPartial = kFewRows * kRow; // floats of a row's share: outputs, reference (log 2), sum
+    static constexpr uint32_t kKeys = kFewKeys * D * 2, kStage = 2 * kKeys, kRing = kWarps * kStages * kStage;
+    static constexpr uint32_t kSmem = kRing + (kFewRows + kFewCluster - 1) * kRow * 4; // with a cluster's shares of this CTA's rows
 };
 struct FewArgs {
     Heads q, k, v, o;
@@ -597,41 +598,33 @@ __device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t (&r)[4])
                  : "memory");
 }
 
-// Sums about different references joined: at(k, i) is float i of share k of `n`, each 16 rows of D outputs, then 16 references (log 2) and 16
-// sums.  Rows r0 to r1, as another such share, or as the output.
-template <typename T, int D, typename At>
-__device__ __forceinline__ void join(const FewArgs &a, const At &at_share, int n, int seq, int kv, int tile, int r0, int r1, float *joined)
+// Column c of a row's shares, sums about different references, joined: at(k, i) is float i of the row in share k of `n`.
+struct Joined {
+    float out, ref, sum;
+};
+template <int D, typename At>
+__device__ __forceinline__ Joined join(const At &at_share, int n, int c)
 {
-    const int r = r0 + (threadIdx.x >> 3), c0 = threadIdx.x & 7; // eight threads a row
-    if (r >= r1) return;
-    float most = -INFINITY, sum = 0.0f, out[D / 8] = {};
-    for (int k = 0; k < n; ++k) most = fmaxf(most, at_share(k, kFewRows * D + r));
+    Joined x{0.0f, -INFINITY, 0.0f};
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) x.ref = fmaxf(x.ref, at_share(k, D));
+#pragma unroll 8
     for (int k = 0; k < n; ++k) {
-        const float ref = at_share(k, kFewRows * D + r);
-        if (ref == -INFINITY) continue;
-        const float f = exp2_approx(ref - most);
-        sum = fmaf(f, at_share(k, kFewRows * (D + 1) + r), sum);
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) out[i] = fmaf(f, at_share(k, r * D + c0 + 8 * i), out[i]);
-    }
-    if (joined) {
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) joined[r * D + c0 + 8 * i] = out[i];
-        if (c0 == 0) {
-            joined[kFewRows * D + r] = most;
-            joined[kFewRows * (D + 1) + r] = sum;
+        const float ref = at_share(k, D), f = exp2_approx(ref - x.ref), sum = at_share(k, D + 1), out = at_share(k, c);
+        if (ref != -INFINITY) { // else it has seen nothing
+            x.sum = fmaf(f, sum, x.sum);
+            x.out = fmaf(f, out, x.out);
         }
-        return;
     }
-    const Range qr = range_of(a.q_ranges, seq, a.q_rows);
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ void put_joined(const FewArgs &a, const Range &qr, int seq, int kv, int tile, int r, int c, const Joined &x)
+{
     const int row = tile * kFewRows + r, t = row / a.group, head = kv * a.group + row - t * a.group;
-    if (t >= qr.count) return;
-    const bool some = sum > 0.0f || sum != sum;
-    T *o = at<T>(a.o, seq, qr.first + t, head);
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i)
-        if (c0 + 8 * i < a.d) o[c0 + 8 * i] = from_f32<T>(some ? out[i] / sum : 0.0f);
-    if (a.lse && c0 == 0) a.lse[((int64_t)seq * a.q_heads + head) * a.q_rows + qr.first + t] = some ? (most + log2f(sum)) * kLn2 : -INFINITY;
+    const bool some = x.sum > 0.0f || x.sum != x.sum;
+    if (c < a.d) at<T>(a.o, seq, qr.first + t, head)[c] = from_f32<T>(some ? x.out / x.sum : 0.0f);
+    if (a.lse && c == 0) a.lse[((int64_t)seq * a.q_heads + head) * a.q_rows + qr.first + t] = some ? (x.ref + log2f(x.sum)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int D>
@@ -640,10 +633,11 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
     using Shape = FewShape<D>;
     constexpr int kSteps = D / 32, kPieces = D / 8;
     extern __shared__ __align__(128) char smem_raw[];
-    wait_prior_grid();
-    release_next_grid();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, c = lane & 3;
     const int tile = blockIdx.x / a.shares, share = blockIdx.x - tile * a.shares, kv = blockIdx.y, seq = blockIdx.z;
+    if (a.cluster) cluster_arrive(); // has begun: its memory may be written to
+    wait_prior_grid();
+    release_next_grid();
     const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
     const int rows = min(kFewRows, qr.count * a.group - tile * kFewRows), ahead = kr.count - qr.count;
     // what some row sees: the first tokens up to `first`, and the keys from lo to end
@@ -795,43 +789,60 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
 #pragma unroll
     for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) own[(quad + 8 * (i >> 1)) * D + 8 * j + 2 * c + (i & 1)] = o[j][i];
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<float2 *>(own + (quad + 8 * h) * Shape::kRow + 8 * j + 2 * c) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
     if (c == 0) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            own[kFewRows * D + quad + 8 * h] = ref[h];
-            own[kFewRows * (D + 1) + quad + 8 * h] = sum[h];
-        }
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<float2 *>(own + (quad + 8 * h) * Shape::kRow + D) = make_float2(ref[h], sum[h]);
     }
     __syncthreads();
-    if (a.shares == 1) {
-        join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, Shape::kWarps, seq, kv, tile, 0, kFewRows, nullptr);
-        return;
+    // the warps' sums are joined, a thread a column of a row; then, if other CTAs have shares of the row, they go to the CTA of the cluster that
+    // joins this row, or to memory
+    const int slots = (kFewRows + a.shares - 1) / a.shares; // rows that a CTA of a cluster joins
+    const uint32_t got = smem_u32(smem_raw) + Shape::kRing;
+    if (a.cluster) cluster_wait();
+    for (int i = threadIdx.x; i < rows * D; i += 32 * Shape::kWarps) {
+        const int r = i / D, col = i % D;
+        const Joined x = join<D>([&](int k, int f) { return parts[k * Shape::kPartial + r * Shape::kRow + f]; }, Shape::kWarps, col);
+        if (a.shares == 1) {
+            put_joined<T>(a, qr, seq, kv, tile, r, col, x);
+        } else if (a.cluster) {
+            const int slot = r / a.shares;
+            const uint32_t to = map_to(got + 4u * ((share * slots + slot) * Shape::kRow), r - slot * a.shares);
+            st_cluster(to + 4u * col, x.out);
+            if (col == 0) {
+                st_cluster(to + 4u * D, x.ref);
+                st_cluster(to + 4u * (D + 1), x.sum);
+            }
+        } else {
+            float *to = a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + blockIdx.x) * Shape::kPartial + r * Shape::kRow;
+            to[col] = x.out;
+            if (col == 0) to[D] = x.ref, to[D + 1] = x.sum;
+        }
     }
-    // the shares of a row: the CTAs of a cluster read one another's, or a second launch joins them
-    float *joined = a.cluster ? parts + Shape::kWarps * Shape::kPartial : a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + blockIdx.x) * Shape::kPartial;
-    join<T, D>(a, [&](int k, int i) { return parts[k * Shape::kPartial + i]; }, Shape::kWarps, seq, kv, tile, 0, kFewRows, joined);
     if (!a.cluster) return;
-    cluster_sync();
-    const uint32_t here = smem_u32(joined);
-    join<T, D>(a,
-               [&](int k, int i) {
-                   float v;
-                   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to(here + 4 * i, k)) : "memory");
-                   return v;
-               },
-               a.shares, seq, kv, tile, kFewRows * share / a.shares, kFewRows * (share + 1) / a.shares, nullptr);
     __syncwarp();
-    cluster_sync(); // no CTA leaves while another reads its share
+    cluster_sync();
+    const float *shares = reinterpret_cast<const float *>(smem_raw + Shape::kRing);
+    for (int i = threadIdx.x; i < slots * D; i += 32 * Shape::kWarps) {
+        const int slot = i / D, r = slot * a.shares + share;
+        if (r >= rows) break;
+        put_joined<T>(a, qr, seq, kv, tile, r, i % D, join<D>([&](int k, int f) { return shares[(k * slots + slot) * Shape::kRow + f]; }, a.shares, i % D));
+    }
 }
 template <typename T, int D>
 __global__ void __launch_bounds__(128) k_few_join(const __grid_constant__ FewArgs a)
 {
+    using Shape = FewShape<D>;
     wait_prior_grid();
     release_next_grid();
     const int tile = blockIdx.x, kv = blockIdx.y, seq = blockIdx.z;
-    const float *parts = a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + tile) * a.shares * FewShape<D>::kPartial;
-    join<T, D>(a, [&](int k, int i) { return parts[(int64_t)k * FewShape<D>::kPartial + i]; }, a.shares, seq, kv, tile, 0, kFewRows, nullptr);
+    const Range qr = range_of(a.q_ranges, seq, a.q_rows);
+    const int rows = min(kFewRows, qr.count * a.group - tile * kFewRows);
+    const float *parts = a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + tile) * a.shares * Shape::kPartial;
+    for (int i = threadIdx.x; i < rows * D; i += 128) {
+        const int r = i / D;
+        put_joined<T>(a, qr, seq, kv, tile, r, i % D, join<D>([&](int k, int f) { return parts[(int64_t)k * Shape::kPartial + r * Shape::kRow + f]; }, a.shares, i % D));
+    }
 }
 
 struct DeltaArgs {
