@@ -650,29 +650,6 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
     const int worker = share * Shape::kWarps + warp, workers = a.shares * Shape::kWarps;
     const int each = units / workers, rest = units - each * workers, u0 = each * worker + min(worker, rest), u1 = u0 + each + (worker < rest);
 
-    // q: rows quad and quad + 8, elements 32 s + 8 c on
-    uint32_t q[kSteps][8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = tile * kFewRows + quad + 8 * h, t = r / a.group;
-        const bool live = quad + 8 * h < rows;
-        const uint16_t *p = live ? at<uint16_t>(a.q, seq, qr.first + t, kv * a.group + r - t * a.group) : nullptr;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            uint32_t w[4] = {0, 0, 0, 0};
-            const int at0 = 32 * s + 8 * c;
-            if (live && at0 + 8 <= a.d) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(p + at0);
-                w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-            } else if (live) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (at0 + i < a.d) w[i / 2] |= (uint32_t)p[at0 + i] << (16 * (i & 1));
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[s][2 * i + h] = w[i];
-        }
-    }
     const uint32_t mine = smem_u32(smem_raw) + warp * Shape::kStages * Shape::kStage;
     // a lane's pieces of a run: keys quad and quad + 8, elements 8 c and every 32 on; values: elements 8 e of every (32 / kPieces)th row
     const int e = lane % kPieces, r0 = lane / kPieces;
@@ -703,8 +680,31 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
         async_commit();
     };
 #pragma unroll
-    for (int i = 0; i < Shape::kStages - 1; ++i) bring(u0 + i, i);
+    for (int i = 0; i < Shape::kStages - 1; ++i) bring(u0 + i, i); // the long way is memory's: q comes meanwhile
 
+    // q: rows quad and quad + 8, elements 32 s + 8 c on
+    uint32_t q[kSteps][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = tile * kFewRows + quad + 8 * h, t = r / a.group;
+        const bool live = quad + 8 * h < rows;
+        const uint16_t *p = live ? at<uint16_t>(a.q, seq, qr.first + t, kv * a.group + r - t * a.group) : nullptr;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            const int at0 = 32 * s + 8 * c;
+            if (live && at0 + 8 <= a.d) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(p + at0);
+                w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+            } else if (live) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (at0 + i < a.d) w[i / 2] |= (uint32_t)p[at0 + i] << (16 * (i & 1));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[s][2 * i + h] = w[i];
+        }
+    }
     float o[kPieces][4] = {}, ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
     const int place0 = (tile * kFewRows + quad) / a.group + ahead, place1 = (tile * kFewRows + quad + 8) / a.group + ahead;
     const float cl = a.scale_log2;
