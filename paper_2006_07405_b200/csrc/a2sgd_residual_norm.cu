@@ -540,11 +540,13 @@ __global__ void __launch_bounds__(1024) k_fold(const __grid_constant__ Args a)
         float sum = 0.0f;
         if (c < a.d) {
             const int count = last - first + 1, lo = first + count * strip / kStrips, hi = first + count * (strip + 1) / kStrips;
-#pragma unroll 4
-            for (int k = lo; k < hi; ++k) {
-                if (job < kSums) sum += __ldcg(a.partials + ((int64_t)k * kSums + job) * a.d + c);
-                else sum += __ldcg(a.gate_partials + ((int64_t)k * 2 + (k * a.run / a.gate_rows != job - kSums)) * a.d + c);
-            }
+            const bool gate = job >= kSums;
+            const float *p = (gate ? a.gate_partials : a.partials + job * a.d) + c;
+            const int64_t step = (int64_t)(gate ? 2 : kSums) * a.d;
+            // of a gate's CTAs only the first may have begun with another gate's rows, and then this gate's sums are its second ones
+            const bool second = gate && first * a.run < (job - kSums) * a.gate_rows;
+#pragma unroll 8
+            for (int k = lo; k < hi; ++k) sum += __ldcg(p + k * step + (second && k == first ? a.d : 0));
         }
         part[strip][threadIdx.x & 31] = sum;
         __syncthreads();
