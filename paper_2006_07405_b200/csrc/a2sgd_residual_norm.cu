@@ -10,6 +10,13 @@
 //
 // The columns' sums: t hat1 and t (from which the gate's, the post weight's and the post bias' gradients follow, a gate at a time), du hat2
 // and du.  A CTA adds its rows up in registers or shared memory, leaves one partial sum a column, and a second kernel adds the CTAs' in order.
+//
+// Statistics, sums and z before its rounding are fp32; z and u (dx and dy) are rounded once, as they are written.
+//
+// B200, 65536 x 1600, bfloat16: forward with an fp32 residual stream 256 us (4.9 TB/s, 75 % of a copy's), four CTAs of 224 threads an SM: a row's two
+// barriers and the little that is on its way meanwhile bound it (two rows on their way take the registers of a CTA: 306 us; parameters read from
+// memory for each row 761).  Backward of a layer norm 364 us (3.5 TB/s), of which the fold is 20: three CTAs an SM (80 registers, of which 8 bytes a
+// thread spill; two CTAs 405 us).  16 rows: 7.0 us on the device, 11.9 a call.
 #include "a2sgd_train.cuh"
 
 #include <algorithm>

@@ -1,4 +1,14 @@
 // Attention with a sliding window and first tokens that stay visible, forward and backward.
+//
+//   forward    S = scale Q K^T where a query sees a key,  P = exp(S - lse),  lse = log sum exp S,  O = P V
+//   backward   delta = sum_c dO O,  dP = dO V^T,  dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// Three kernels: tiles of 128 queries on the tensor cores (k_forward), a few queries over a long cache (k_few), and the backward pass, twice the
+// same template (k_backward).  S, dP, sums, references and outputs are fp32.  P and dS are rounded once to the 16-bit type, since they are operands
+// of products of 16-bit values; the sum that divides P is taken before that rounding, so that a row's error is P's alone (half a step of each term).
+// Scores are kept in units of log 2: one fused multiply-add and one exp2 an element.
+//
+// Every wait on an mbarrier ends after two seconds at most; the kernel then says so (a2sgd_window_attention_status) and leaves.
 #include "a2sgd_tcgen05.cuh"
 #include "a2sgd_train.cuh"
 
@@ -38,12 +48,18 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ forward
 // Persistent CTAs, two an SM, deal out the tiles of 128 queries of one head, the longest first.  For each tile a CTA walks the blocks of 64
-// keys that any of its queries sees: the first tokens' blocks, then those of the window.  Two warps bring tiles in by TMA, two issue the
-// products, four hold the softmax, a thread a query.
-//   S = Q K^T into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  O += P V, P read from TMEM.
+// keys that any of its queries sees: the first tokens' blocks, then those of the window.  Warp 4 brings tiles, queries and keys in by TMA, warp 7 the
+// values, warp 5 issues S = Q K^T, warp 6 O += P V, warps 0 to 3 hold the softmax, a thread a query.
+//   S goes into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  P is read from TMEM by its product with V.
 // Three buffers of S (two where O has 128 columns): the next block's, be it the next tile's, is formed while the present one's P is.
 // P is taken about a reference that is moved, and O and the sum with it, only where P would grow beyond 2^13: nearly no
 // block touches O, and blocks without a mask need no maximum.
+//
+// Bound, for heads of 64, by the softmax' warps: 16 exponentials a clock and SM are 164 us of 8 x 4096 queries, 25 heads of 64, window 1024 (737 M
+// pairs), and with the loads from and stores to TMEM, the sums and the rounding to 16 bits a block takes a warp twice that; the products alone are
+// 116 us.  B200: 344 us (550 TFLOP/s, tensor pipe 31 % busy); 20011 packed rows, 16 heads of 128, window 4096, float16: 225 us (871 TFLOP/s,
+// 54 %).  One CTA an SM with 16 softmax warps, and every second exponential as a polynomial on the multiply-add pipe, measured the same; one
+// loading warp for keys and values 364 and 240 us; 16-byte stores 348 and 230.
 struct ForwardArgs {
     CUtensorMap q, k, v;
     Heads o;
@@ -57,7 +73,7 @@ struct ForwardArgs {
     float scale_log2;
 };
 
-constexpr int kBlock = 64; // keys
+constexpr int kBlock = 64; // keys: of 128, two buffers of S and an O of 64 columns leave no second CTA on the SM
 template <int D>
 struct ForwardShape {
     static constexpr int kThreads = 256, kCtas = 2, kStages = D == 64 ? 4 : 2; // of keys, and of values
@@ -560,7 +576,11 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 // head, and a share of the keys that they see; its warps take 16 keys at a time, each a run of its own, with mma.sync (m16n8k16): the
 // scores leave a warp's registers as the left operand of P V.  Keys come by cp.async into places that the lane alone reads: the order of a head's elements is
 // free as long as q has the same.  Values come in rows, and through ldmatrix.trans.  Every warp has its own maximum, sum and output; they meet in shared
-// memory, and those of a row's CTAs in a cluster's, or beyond eight CTAs in a second launch.
+// memory, and those of a row's CTAs in that of a cluster's CTA, or beyond eight CTAs in memory and a second launch.
+//
+// B200: 64 sequences, 32 heads of 128, 8 key heads, 4112 of 8192 keys visible, 1079 MB: 179 us (6.0 TB/s, 92 % of a copy's).  4 sequences, 25 heads of
+// 64, 1028 keys, 26 MB: 10.8 us on the device, 11.9 a call: 2 until the first keys are asked for, 5 until the last are used, 1.2 and 0.9 for the two
+// joins (with threads of eight columns each, and a cluster's CTAs reading one another, 13.0 us); the call itself is 10.5 us on the host.
 constexpr int kFewRows = 16, kFewKeys = 16, kFewCluster = 8, kMostShares = 320; // the last: CTAs of a call whose rows are shared out beyond a cluster
 template <int D>
 struct FewShape {
@@ -854,7 +874,8 @@ struct DeltaArgs {
 };
 
 // ------------------------------------------------------------------ backward
-// Two launches of one template, so that nothing is added up by atomics (S and dP are formed twice: 14 D operations a pair in place of 10).
+// Two launches of one template, so that nothing is added up by atomics (S and dP are formed twice: 14 D operations a pair in place of 10, and
+// two exponentials in place of one): the same call gives the same bits.
 //   KEYS false: 128 queries stay, blocks of 64 keys pass:        dQ += dS K
 //   KEYS true:  128 keys stay, blocks of 64 queries pass, of all query heads of the key head:   dK += dS^T Q,  dV += P^T dO
 // In either, with A, A' the tiles that stay and B, B' those that pass:  S = A B^T, dP = A' B'^T into TMEM; a thread reads its row, forms
@@ -862,6 +883,11 @@ struct DeltaArgs {
 // Roles and tiles as in the forward pass, one CTA an SM, with three buffers of S and dP (two where dK and dV of 128 elements leave no more) and
 // two groups of four warps, each with half of a block.
 // The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.
+//
+// Bound by the softmax' warps and what lies between them and the products: S and dP come out of TMEM, P and dS go back, 1100 to 1400 clocks a block of
+// 64, in which the products take 611 and the exponentials 560.  B200, 8 x 4096 queries, 25 heads of 64, window 1024: dq 490 us, dk and dv 610,
+// delta 54, together 1160 (405 TFLOP/s of the 10 D operations a pair); 5003 packed rows, 12 heads of 80: 118 us.  Measured and not taken: blocks of
+// 128 with places of their own for P and dS (1240 us: one buffer only), 16 softmax warps, two CTAs an SM, exponentials by polynomials (no change).
 struct BackwardArgs {
     CUtensorMap stay0, stay1, pass0, pass1;
     Heads out0, out1; // dq; or dk, dv
@@ -874,6 +900,7 @@ struct BackwardArgs {
     int stay0_planes, stay1_planes, pass0_planes, pass1_planes;
     int tiles, lanes, items, together;
     int parts, part_blocks, sink_tiles, sink_rows, extra; // parts of a first tokens' tile, blocks of each; tiles and keys; items of a lane beyond its tiles
+    int beside; // KEYS: the launch before is that of dq, whose CTAs have all waited for what this one reads: it needs no wait but for its end
     float scale, scale_log2;
 };
 template <int D, bool KEYS>
@@ -1001,7 +1028,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     __syncthreads();
     fence_after();
     const uint32_t tmem = tmem_at;
-    wait_prior_grid();
+    if (!a.beside) wait_prior_grid();
     release_next_grid(); // as in the forward pass
 
     // Blocks come by two warps, every second one each: what a warp does for a block takes as long as its products.  `g`: blocks before this tile.
@@ -1020,8 +1047,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             float lse0 = -INFINITY, lse1 = -INFINITY, delta0 = 0.0f, delta1 = 0.0f; // on their way while the stage is waited for
             if (KEYS) {
                 const int64_t line = lines + (int64_t)member * a.q_rows + at_row;
-                if (lane < valid) lse0 = -a.lse2[line], delta0 = -a.delta[line];
-                if (lane + 32 < valid) lse1 = -a.lse2[line + 32], delta1 = -a.delta[line + 32];
+                if (lane < valid) lse0 = -__ldcg(a.lse2 + line), delta0 = -__ldcg(a.delta + line);
+                if (lane + 32 < valid) lse1 = -__ldcg(a.lse2 + line + 32), delta1 = -__ldcg(a.delta + line + 32);
                 for (member += 2; member >= a.group; member -= a.group) ++block;
             }
             if (!bar_wait_cta(empty(stage), ((g + n) / kStages & 1) ^ 1, &gave_up)) return false;
@@ -1318,6 +1345,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
         while (now_ns() - begin < 5000000ull) __nanosleep(1000);
     }
     if (warp == kForm) tmem_free(tmem, Shape::kColumns);
+    if (a.beside) wait_prior_grid(); // who waits for this launch waits for dq, too
 }
 
 // The parts' sums of the first tokens' keys, in order.  A warp a key and key head.
@@ -1562,7 +1590,8 @@ struct Packer {
     }
 };
 
-// Queries that are few enough: the rows of a key head's queries, in sequences that are not packed (whose lengths the host does not know).
+// Queries that are few enough: the rows of a key head's queries, in sequences that are not packed (whose lengths the host does not know).  64 sequences,
+// 32 heads of 128, 8 key heads, 4112 keys: 32 rows 304 us here and 48 rows 452, where tiles of 128 queries take 533; 64 rows 539 and 488.
 constexpr int kFewMost = 48;
 inline bool few(const a2sgd_attention *s, bool packed_q) { return !packed_q && s->q_rows * (s->q_heads / s->kv_heads) <= kFewMost; }
 inline uint64_t share_bytes(const a2sgd_attention *s) { return (uint64_t)kMostShares * kFewRows * ((s->head_dim <= 64 ? 64 : 128) + 2) * 4; }
@@ -1704,6 +1733,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
                  const Tensor &dv, int dtype, int sms, cudaStream_t s)
 {
     int rc = A2SGD_OK;
+    bool beside = false;
     if (dq.h.p && q.rows) {
         const auto maps = [&] {
             return make_map(&b.stay0, q, dtype, 128) && make_map(&b.stay1, dout, dtype, 128) &&
@@ -1715,6 +1745,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         b.wide0 = store_bytes(dq);
         rc = launch_backward<T, D, false>(b, q.rows, sms, s);
         if (rc != A2SGD_OK) return rc;
+        beside = true;
     }
     if ((dk.h.p || dv.h.p) && k.rows) {
         const auto maps = [&] {
@@ -1722,6 +1753,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
                    (q.rows == 0 || (make_map(&b.pass0, q, dtype, kBlock) && make_map(&b.pass1, dout, dtype, kBlock)));
         };
         if (!maps()) return A2SGD_ERR_CUDA;
+        b.beside = beside;
         b.stay0_planes = k.planes, b.stay1_planes = v.planes, b.pass0_planes = q.planes, b.pass1_planes = dout.planes;
         b.out0 = dk.h, b.out1 = dv.h;
         b.wide0 = store_bytes(dk), b.wide1 = store_bytes(dv);
