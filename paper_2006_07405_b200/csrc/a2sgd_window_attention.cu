@@ -581,6 +581,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 // B200: 64 sequences, 32 heads of 128, 8 key heads, 4112 of 8192 keys visible, 1079 MB: 179 us (6.0 TB/s, 92 % of a copy's).  4 sequences, 25 heads of
 // 64, 1028 keys, 26 MB: 10.8 us on the device, 11.9 a call: 2 until the first keys are asked for, 5 until the last are used, 1.2 and 0.9 for the two
 // joins (with threads of eight columns each, and a cluster's CTAs reading one another, 13.0 us); the call itself is 10.5 us on the host.
+// 1 sequence, 32 heads of 128, 8 key heads: 8192 keys (34 MB) 14.4 us, 131072 keys (537 MB) 77 us (7.0 TB/s: part of it stays in L2).
 constexpr int kFewRows = 16, kFewKeys = 16, kFewCluster = 8, kMostShares = 320; // the last: CTAs of a call whose rows are shared out beyond a cluster
 template <int D>
 struct FewShape {
@@ -849,20 +850,50 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
         put_joined<T>(a, qr, seq, kv, tile, r, i % D, join<D>([&](int k, int f) { return shares[(k * slots + slot) * Shape::kRow + f]; }, a.shares, i % D));
     }
 }
+// The shares of a row that are more than a cluster's: a CTA a row, a thread a column, the shares' factors in shared memory.
+constexpr int kJoinThreads = 128;
 template <typename T, int D>
-__global__ void __launch_bounds__(128) k_few_join(const __grid_constant__ FewArgs a)
+__global__ void __launch_bounds__(kJoinThreads) k_few_join(const __grid_constant__ FewArgs a)
 {
     using Shape = FewShape<D>;
+    constexpr int kWarps = kJoinThreads / 32;
+    __shared__ float refs[kMostShares], factors[kMostShares], tops[kWarps], sums[kWarps];
     wait_prior_grid();
     release_next_grid();
-    const int tile = blockIdx.x, kv = blockIdx.y, seq = blockIdx.z;
+    const int tile = blockIdx.x / kFewRows, r = blockIdx.x % kFewRows, kv = blockIdx.y, seq = blockIdx.z, n = a.shares;
     const Range qr = range_of(a.q_ranges, seq, a.q_rows);
-    const int rows = min(kFewRows, qr.count * a.group - tile * kFewRows);
-    const float *parts = a.partials + (((int64_t)seq * a.kv_heads + kv) * gridDim.x + tile) * a.shares * Shape::kPartial;
-    for (int i = threadIdx.x; i < rows * D; i += 128) {
-        const int r = i / D;
-        put_joined<T>(a, qr, seq, kv, tile, r, i % D, join<D>([&](int k, int f) { return parts[(int64_t)k * Shape::kPartial + r * Shape::kRow + f]; }, a.shares, i % D));
+    if (r >= qr.count * a.group - tile * kFewRows) return;
+    const float *parts = a.partials + (((int64_t)seq * a.kv_heads + kv) * a.tiles + tile) * n * Shape::kPartial + r * Shape::kRow;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    Joined x{0.0f, -INFINITY, 0.0f};
+    for (int k = threadIdx.x; k < n; k += kJoinThreads) {
+        refs[k] = parts[k * Shape::kPartial + D];
+        x.ref = fmaxf(x.ref, refs[k]);
     }
+#pragma unroll
+    for (int m = 16; m; m >>= 1) x.ref = fmaxf(x.ref, __shfl_xor_sync(0xffffffffu, x.ref, m));
+    if (lane == 0) tops[warp] = x.ref;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) x.ref = fmaxf(x.ref, tops[w]);
+    for (int k = threadIdx.x; k < n; k += kJoinThreads) {
+        factors[k] = exp2_approx(refs[k] - x.ref);
+        if (refs[k] != -INFINITY) x.sum = fmaf(factors[k], parts[k * Shape::kPartial + D + 1], x.sum); // else it has seen nothing
+    }
+#pragma unroll
+    for (int m = 16; m; m >>= 1) x.sum += __shfl_xor_sync(0xffffffffu, x.sum, m);
+    if (lane == 0) sums[warp] = x.sum;
+    __syncthreads();
+    x.sum = sums[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) x.sum += sums[w];
+    if (threadIdx.x >= D) return;
+#pragma unroll 16
+    for (int k = 0; k < n; ++k) {
+        const float out = parts[k * Shape::kPartial + (int)threadIdx.x];
+        if (refs[k] != -INFINITY) x.out = fmaf(factors[k], out, x.out);
+    }
+    put_joined<T>(a, qr, seq, kv, tile, r, threadIdx.x, x);
 }
 
 struct DeltaArgs {
@@ -1603,11 +1634,15 @@ int launch_few(FewArgs &f, int sequences, float *partials, int sms, cudaStream_t
     f.tiles = (f.q_rows * f.group + kFewRows - 1) / kFewRows;
     if (f.kv_heads > 65535 || sequences > 65535) return A2SGD_ERR_TOO_LARGE;
     const int64_t items = (int64_t)f.tiles * f.kv_heads * sequences;
-    // a row's keys are shared out until there are two CTAs an SM, as long as a warp keeps four runs of 16 keys
+    // a row's keys are shared out until there are two CTAs an SM, as long as a warp keeps four runs of 16 keys (4 sequences, 25 heads of 64, 1028 keys:
+    // two CTAs a row 11.8 us, one 14.5)
     const int64_t seen = std::min<int64_t>(f.k_rows, (int64_t)std::min(f.window, 1 << 29) + f.sinks), units = (seen + kFewKeys - 1) / kFewKeys;
     int64_t shares = 1;
     if (items < 2 * sms) shares = std::max<int64_t>(1, std::min<int64_t>(std::min(2 * sms, kMostShares) / items, units / (Shape::kWarps * 4)));
-    if (!partials) shares = std::min<int64_t>(shares, kFewCluster);
+    // Beyond a cluster there is a second launch: only where the warps of a cluster's CTAs would have more than twelve runs each.  One sequence, 32
+    // heads of 128, 8 key heads: 4096 keys (8 runs) 14.3 us with 16 CTAs a row and 13.0 with eight, 8192 keys 14.4 (32 CTAs) and 18.8,
+    // 131072 keys 76.7 (37) and 198; 4 heads of 64: 8192 keys (8 runs) 13.5 and 11.4, 32768 14.2 and 22.7.
+    if (!partials || units <= 12 * kFewCluster * Shape::kWarps) shares = std::min<int64_t>(shares, kFewCluster);
     f.shares = (int)shares;
     f.cluster = shares > 1 && shares <= kFewCluster;
     f.partials = partials;
@@ -1616,7 +1651,7 @@ int launch_few(FewArgs &f, int sequences, float *partials, int sms, cudaStream_t
     A2_TRAIN_CUDA(allow_smem(fn, Shape::kSmem));
     const dim3 rows((unsigned)f.tiles, (unsigned)f.kv_heads, (unsigned)sequences);
     A2_TRAIN_CUDA(launch(fn, dim3(rows.x * (unsigned)f.shares, rows.y, rows.z), 32 * Shape::kWarps, Shape::kSmem, params, s, f.cluster ? (unsigned)f.shares : 1));
-    if (f.shares > 1 && !f.cluster) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), rows, 128, 0, params, s));
+    if (f.shares > 1 && !f.cluster) A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_few_join<T, D>), dim3(rows.x * kFewRows, rows.y, rows.z), kJoinThreads, 0, params, s));
     return A2SGD_OK;
 }
 
@@ -1629,7 +1664,7 @@ int launch_forward(ForwardArgs &f, int64_t rows, int sms, cudaStream_t s)
     if (items > 0x3fffffff) return A2SGD_ERR_TOO_LARGE;
     f.lanes = (int)lanes;
     // Heads that are worked on side by side: as many as their keys and values fit into L2 with (48 MB of 126), those that some tile of a wave
-    // sees.  8 x 4096, 25 heads of 128, no window: all 200 at once 1089 us.
+    // sees.  8 x 4096, 25 heads of 128, no window: 862 us, all 200 at once 971.
     const int64_t live = std::min<int64_t>(f.k_rows, (int64_t)f.window + 2048);
     f.together = (int)std::min<int64_t>(lanes, std::max<int64_t>(8, (48ll << 20) * f.group / std::max<int64_t>(1, live * D * 4)));
     f.items = (int)items;

@@ -109,6 +109,23 @@ def test_few_queries_shared_out_and_not():
             check_all(q[0], k[0], v[0], None, 1 << 30, 0, o[0], lse[0], None)
 
 
+@pytest.mark.parametrize("d, window, sinks", [(64, 1 << 30, 0), (128, 20000, 40), (72, 17000, 2)])
+def test_shares_of_caches_of_all_lengths(d, window, sinks):
+    """Two tiles of rows a key head, caches of 30000, 5 and no keys in one call: most shares of the short ones see nothing."""
+    gen = torch.Generator("cuda").manual_seed(6)
+    q = torch.empty((3, 2, 24, d), device="cuda").normal_(generator=gen).to(BF16)
+    k, v = (torch.empty((3, 30000, 2, d), device="cuda").normal_(generator=gen).to(BF16) for _ in range(2))
+    ranges = torch.tensor([[0, 30000], [7, 5], [0, 0]], dtype=torch.int32, device="cuda")
+    work = torch.empty(B.a2sgd_window_attention_workspace(q, k, window, sinks, 3, aligned=True), dtype=torch.uint8, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty((3, 24, 2), device="cuda")
+    again = torch.empty_like(q)
+    B.a2sgd_window_attention_forward(q, k, v, o, lse, window=window, sinks=sinks, k_ranges=ranges, workspace=work)
+    B.a2sgd_window_attention_forward(q, k, v, again, None, window=window, sinks=sinks, k_ranges=ranges, workspace=work)
+    assert torch.equal(o, again)
+    for b, (first, count) in enumerate(ranges.tolist()):
+        check_all(q[b], k[b, first:first + count], v[b, first:first + count], None, window, sinks, o[b], lse[b], None)
+
+
 def test_on_another_stream_and_side_by_side():
     """Two calls at once on two streams, with a workspace each."""
     gen = torch.Generator("cuda").manual_seed(5)
