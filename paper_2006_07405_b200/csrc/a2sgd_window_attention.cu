@@ -901,6 +901,7 @@ struct DeltaArgs {
     const float *lse;
     float *lse2, *delta;
     int64_t rows;
+    unsigned int *next; // two, cleared
     int blocks, heads, d, wide; // CTAs of a plane
 };
 
@@ -916,9 +917,11 @@ struct DeltaArgs {
 // The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.
 //
 // Bound by the softmax' warps and what lies between them and the products: S and dP come out of TMEM, P and dS go back, 1100 to 1400 clocks a block of
-// 64, in which the products take 611 and the exponentials 560.  B200, 8 x 4096 queries, 25 heads of 64, window 1024: dq 490 us, dk and dv 610,
-// delta 54, together 1160 (405 TFLOP/s of the 10 D operations a pair); 5003 packed rows, 12 heads of 80: 118 us.  Measured and not taken: blocks of
-// 128 with places of their own for P and dS (1240 us: one buffer only), 16 softmax warps, two CTAs an SM, exponentials by polynomials (no change).
+// 64, in which the products take 611 and the exponentials 560.  B200, 8 x 4096 queries, 25 heads of 64, window 1024: dk and dv 610 us, dq 490,
+// delta 54, together 1131 (416 TFLOP/s of the 10 D operations a pair); 5003 packed rows, 12 heads of 80: 80 us.  CTAs take their tiles from a counter,
+// and dq's begin where dk and dv's end (tiles dealt out by number, dq first: 1140 and 113 us; one launch after the other 1160 and 118).  Which
+// CTA has a tile changes nothing in its result.  Measured and not taken: blocks of 128 with places of their own for P and dS (1240 us: one buffer
+// only), 16 softmax warps, two CTAs an SM, exponentials by polynomials (no change).
 struct BackwardArgs {
     CUtensorMap stay0, stay1, pass0, pass1;
     Heads out0, out1; // dq; or dk, dv
@@ -931,7 +934,8 @@ struct BackwardArgs {
     int stay0_planes, stay1_planes, pass0_planes, pass1_planes;
     int tiles, lanes, items, together;
     int parts, part_blocks, sink_tiles, sink_rows, extra; // parts of a first tokens' tile, blocks of each; tiles and keys; items of a lane beyond its tiles
-    int beside; // KEYS: the launch before is that of dq, whose CTAs have all waited for what this one reads: it needs no wait but for its end
+    unsigned int *next; // items taken beyond every CTA's first one
+    int beside;         // dq: the launch before is that of dk and dv, whose CTAs have all waited for what this one reads: it waits for its end only
     float scale, scale_log2;
 };
 template <int D, bool KEYS>
@@ -1114,7 +1118,11 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
         int kt = -1, g = 0;
         uint32_t tails = 0;
         bool ok = true;
-        for (int item = blockIdx.x; ok; item += gridDim.x) {
+        const auto take = [&] {
+            unsigned int n = lane == 0 ? atomicAdd(a.next, 1u) : 0;
+            return (int)(gridDim.x + __shfl_sync(0xffffffffu, n, 0));
+        };
+        for (int item = blockIdx.x; ok; item = take()) {
             BackwardTile t;
             t.rows = t.count = 0;
             const bool end = item >= a.items;
@@ -1270,8 +1278,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             float minus_lse = -INFINITY, minus_delta = 0.0f;
             if (!KEYS && live) {
                 const int64_t line = ((int64_t)(a.packed_q ? 0 : tile.seq) * a.q_heads + tile.head) * a.q_rows + tile.row + row;
-                minus_lse = -a.lse2[line];
-                minus_delta = -a.delta[line];
+                minus_lse = -__ldcg(a.lse2 + line);
+                minus_delta = -__ldcg(a.delta + line);
             }
             int member = KEYS ? tile.begin % a.group : 0, block = KEYS ? tile.begin / a.group : 0;
             for (int n = 0; n < tile.count; ++n) {
@@ -1413,6 +1421,7 @@ __global__ void __launch_bounds__(256) k_delta(const __grid_constant__ DeltaArgs
 {
     wait_prior_grid();
     release_next_grid();
+    if (blockIdx.x == 0 && threadIdx.x < 2) a.next[threadIdx.x] = 0;
     constexpr int kEach = 256 / LANES, kAhead = 4; // queries at a time, whose reads come before their sums
     const int lane = threadIdx.x % LANES, plane = blockIdx.x / a.blocks;
     const int64_t row0 = (int64_t)(blockIdx.x % a.blocks) * kDeltaRows;
@@ -1734,6 +1743,7 @@ Parts parts_of(const a2sgd_attention *s)
     p.sink_rows = (int)sinks;
     return p;
 }
+constexpr uint64_t kCounters = 256; // bytes: of items taken, by dk and dv, and by dq
 uint64_t partial_bytes(const a2sgd_attention *s)
 {
     const Parts p = parts_of(s);
@@ -1768,37 +1778,38 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
                  const Tensor &dv, int dtype, int sms, cudaStream_t s)
 {
     int rc = A2SGD_OK;
-    bool beside = false;
-    if (dq.h.p && q.rows) {
-        const auto maps = [&] {
-            return make_map(&b.stay0, q, dtype, 128) && make_map(&b.stay1, dout, dtype, 128) &&
-                   (k.rows == 0 || (make_map(&b.pass0, k, dtype, kBlock) && make_map(&b.pass1, v, dtype, kBlock)));
-        };
-        if (!maps()) return A2SGD_ERR_CUDA;
-        b.stay0_planes = q.planes, b.stay1_planes = dout.planes, b.pass0_planes = k.planes, b.pass1_planes = v.planes;
-        b.out0 = dq.h, b.out1 = Heads{nullptr, 0, 0, 0};
-        b.wide0 = store_bytes(dq);
-        rc = launch_backward<T, D, false>(b, q.rows, sms, s);
-        if (rc != A2SGD_OK) return rc;
-        beside = true;
-    }
-    if ((dk.h.p || dv.h.p) && k.rows) {
+    const bool keys = (dk.h.p || dv.h.p) && k.rows;
+    if (keys) {
         const auto maps = [&] {
             return make_map(&b.stay0, k, dtype, 128) && make_map(&b.stay1, v, dtype, 128) &&
                    (q.rows == 0 || (make_map(&b.pass0, q, dtype, kBlock) && make_map(&b.pass1, dout, dtype, kBlock)));
         };
         if (!maps()) return A2SGD_ERR_CUDA;
-        b.beside = beside;
         b.stay0_planes = k.planes, b.stay1_planes = v.planes, b.pass0_planes = q.planes, b.pass1_planes = dout.planes;
         b.out0 = dk.h, b.out1 = dv.h;
         b.wide0 = store_bytes(dk), b.wide1 = store_bytes(dv);
         rc = launch_backward<T, D, true>(b, k.rows, sms, s);
         if (rc != A2SGD_OK) return rc;
-        if (b.parts > 1) {
-            const int64_t keys = (int64_t)b.sequences * b.kv_heads * b.sink_rows;
-            void *params[] = {&b};
-            A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold_keys<T, D>), dim3((unsigned)((keys + 7) / 8)), 256, 0, params, s));
-        }
+    }
+    if (dq.h.p && q.rows) {
+        BackwardArgs c = b;
+        const auto maps = [&] {
+            return make_map(&c.stay0, q, dtype, 128) && make_map(&c.stay1, dout, dtype, 128) &&
+                   (k.rows == 0 || (make_map(&c.pass0, k, dtype, kBlock) && make_map(&c.pass1, v, dtype, kBlock)));
+        };
+        if (!maps()) return A2SGD_ERR_CUDA;
+        c.stay0_planes = q.planes, c.stay1_planes = dout.planes, c.pass0_planes = k.planes, c.pass1_planes = v.planes;
+        c.out0 = dq.h, c.out1 = Heads{nullptr, 0, 0, 0};
+        c.wide0 = store_bytes(dq);
+        c.next = b.next + 1;
+        c.beside = keys;
+        rc = launch_backward<T, D, false>(c, q.rows, sms, s);
+        if (rc != A2SGD_OK) return rc;
+    }
+    if (keys && b.parts > 1) {
+        const int64_t rows = (int64_t)b.sequences * b.kv_heads * b.sink_rows;
+        void *params[] = {&b};
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold_keys<T, D>), dim3((unsigned)((rows + 7) / 8)), 256, 0, params, s));
     }
     return rc;
 }
@@ -1813,6 +1824,7 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
     BackwardArgs b{};
     float *lse2 = static_cast<float *>(pack.take(lines * 4)), *delta = static_cast<float *>(pack.take(lines * 4));
     b.lse2 = lse2, b.delta = delta;
+    b.next = static_cast<unsigned int *>(pack.take(kCounters));
     b.partials = static_cast<float *>(pack.take(partial_bytes(shape)));
     const Tensor pq = pack.usable(q), pk = pack.usable(k), pv = pack.usable(v), pdout = pack.usable(dout);
     if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
@@ -1822,7 +1834,7 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
         DeltaArgs d{};
         d.o = o.h, d.dout = dout.h;
         d.lse = lse;
-        d.lse2 = lse2, d.delta = delta;
+        d.lse2 = lse2, d.delta = delta, d.next = b.next;
         d.rows = q.rows;
         const int64_t planes = packed_q ? 1 : (int64_t)shape->sequences, blocks = (q.rows + kDeltaRows - 1) / kDeltaRows;
         if (planes * blocks > 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
@@ -1832,6 +1844,8 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
         void *params[] = {&d};
         const void *fn = q.d <= 64 ? reinterpret_cast<const void *>(&k_delta<T, 8>) : reinterpret_cast<const void *>(&k_delta<T, 16>);
         A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(planes * blocks)), 256, 0, params, s));
+    } else {
+        A2_TRAIN_CUDA(cudaMemsetAsync(b.next, 0, kCounters, s));
     }
     const Parts parts = parts_of(shape);
     b.q_ranges = shape->q_ranges, b.k_ranges = shape->k_ranges;
@@ -1857,7 +1871,7 @@ extern "C" uint64_t a2sgd_window_attention_workspace(const a2sgd_attention *shap
     const int d = (int)shape->head_dim;
     uint64_t bytes = 0;
     if (shape->kv_heads == 0) return 0;
-    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += 2 * up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4) + partial_bytes(shape);
+    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += 2 * up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4) + kCounters + partial_bytes(shape);
     else if (few(shape, flags & A2SGD_ATTENTION_PACKED_Q)) bytes += share_bytes(shape);
     if (!(flags & A2SGD_ATTENTION_ALIGNED))
         bytes += (flags & A2SGD_ATTENTION_BACKWARD ? 2 : 1) * room(q_planes, (int64_t)shape->q_rows, (int)shape->q_heads, d) +
