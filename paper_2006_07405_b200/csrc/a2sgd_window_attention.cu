@@ -1387,13 +1387,15 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     if (a.beside) wait_prior_grid(); // who waits for this launch waits for dq, too
 }
 
-// The parts' sums of the first tokens' keys, in order.  A warp a key and key head.
+// The parts' sums of the first tokens' keys, in order.  A warp 32 columns of one output of a key and key head.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ BackwardArgs a)
 {
     wait_prior_grid();
     release_next_grid();
-    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    constexpr int kPieces = 2 * (D / 32);
+    const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), item = warp / kPieces;
+    const int piece = (int)(warp % kPieces), o = piece / (D / 32), c = piece % (D / 32) * 32 + (threadIdx.x & 31);
     if (item >= (int64_t)a.sequences * a.kv_heads * a.sink_rows) return;
     const int key = (int)(item % a.sink_rows), lane = (int)(item / a.sink_rows), head = lane % a.kv_heads, seq = lane / a.kv_heads;
     const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
@@ -1402,16 +1404,12 @@ __global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ Backw
     const int all = query_blocks(key / 128 * 128, qr.count, kr.count, a.window, a.sinks, a.group, first);
     const int parts = (all + a.part_blocks - 1) / a.part_blocks;
     if (parts == 0) return; // cleared where the tile was found
-    for (int o = 0; o < 2; ++o) {
-        const Heads &h = o ? a.out1 : a.out0;
-        if (!h.p) continue;
-        T *p = at<T>(h, seq, kr.first + key, head);
-        for (int c = threadIdx.x & 31; c < a.d; c += 32) {
-            float sum = 0.0f;
-            for (int k = 0; k < parts; ++k) sum += a.partials[((item * a.parts + k) * 2 + o) * D + c];
-            p[c] = from_f32<T>(sum);
-        }
-    }
+    const Heads &h = o ? a.out1 : a.out0;
+    if (!h.p || c >= a.d) return;
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) sum += a.partials[((item * a.parts + k) * 2 + o) * D + c];
+    at<T>(h, seq, kr.first + key, head)[c] = from_f32<T>(sum);
 }
 
 // lse in units of log 2 and delta of every query: eight or sixteen lanes a query and head; a CTA takes 16 rows of a plane.
@@ -1807,9 +1805,9 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         if (rc != A2SGD_OK) return rc;
     }
     if (keys && b.parts > 1) {
-        const int64_t rows = (int64_t)b.sequences * b.kv_heads * b.sink_rows;
+        const int64_t rows = (int64_t)b.sequences * b.kv_heads * b.sink_rows; // far below a grid's limit: their partial sums fit the workspace
         void *params[] = {&b};
-        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold_keys<T, D>), dim3((unsigned)((rows + 7) / 8)), 256, 0, params, s));
+        A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold_keys<T, D>), dim3((unsigned)(rows * 2 * (D / 32) / 8 + 1)), 256, 0, params, s));
     }
     return rc;
 }
