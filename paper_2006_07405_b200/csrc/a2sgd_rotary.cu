@@ -203,7 +203,7 @@ extern "C" int a2sgd_rotary(const a2sgd_heads *q, const a2sgd_heads *k, const a2
             ratio = powl((long double)base, -1.0L / (long double)sections[i]);
         }
         for (uint32_t l = 0; l < sections[i]; ++l, ++j, omega *= ratio) {
-            const long double t = omega / kTurn, part = t - floorl(t);
+            const long double t = omega / kTurn, part = t < 1.0L ? t : t - floorl(t);
             a.turn[j] = part >= 1.0L ? 0 : (uint64_t)(part * 18446744073709551616.0L);
             a.axis[j] = (uint8_t)i;
         }
