@@ -1359,6 +1359,6 @@ extern "C" int a2sgd_gated_ffn_status(int device, int *device_status, void *stre
     unsigned int count = 0;
     A2_TRAIN_CUDA(cudaMemcpyFromSymbolAsync(&count, g_waits_run_out, sizeof count, 0, cudaMemcpyDeviceToHost, s));
     A2_TRAIN_CUDA(cudaStreamSynchronize(s));
-    *device_status = count_moved(device, s, count) ? A2SGD_ERR_TIMEOUT : A2SGD_OK;
+    *device_status = count_moved(device, s, count, &g_waits_run_out) ? A2SGD_ERR_TIMEOUT : A2SGD_OK;
     return A2SGD_OK;
 }

@@ -69,14 +69,14 @@ cudaError_t allow_smem(const void *fn, size_t bytes)
     return cudaSuccess;
 }
 
-bool count_moved(int device, cudaStream_t stream, unsigned int count)
+bool count_moved(int device, cudaStream_t stream, unsigned int count, const void *counter)
 {
     static std::mutex lock;
-    static std::map<std::tuple<int, cudaStream_t, std::thread::id>, unsigned int> seen;
+    static std::map<std::tuple<const void *, int, cudaStream_t, std::thread::id>, unsigned int> seen;
     if (count == 0) return false;
     const std::thread::id thread = stream == cudaStreamPerThread ? std::this_thread::get_id() : std::thread::id();
     std::lock_guard<std::mutex> hold(lock);
-    const auto key = std::make_tuple(device, stream, thread);
+    const auto key = std::make_tuple(counter, device, stream, thread);
     const auto it = seen.find(key);
     if (it != seen.end() && it->second == count) return false;
     try {

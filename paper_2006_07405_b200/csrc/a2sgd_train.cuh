@@ -234,8 +234,9 @@ int resident_ctas(const void *fn, unsigned threads, size_t smem, int device);
 cudaError_t allow_smem(const void *fn, size_t bytes);
 
 // Whether a device's count has moved since this was last asked with the same stream (before the first time: since 0).
-// Each stream is told for itself, and each thread for its own per-thread default stream.
-bool count_moved(int device, cudaStream_t stream, unsigned int count);
+// Each stream is told for itself, and each thread for its own per-thread default stream.  counter: an address that says which of the device's counts is
+// meant, where there are several.
+bool count_moved(int device, cudaStream_t stream, unsigned int count, const void *counter = nullptr);
 
 } // namespace a2sgd_train
 
