@@ -632,7 +632,7 @@ __device__ __forceinline__ Joined join(const At &at_share, int n, int c)
 #pragma unroll 8
     for (int k = 0; k < n; ++k) {
         const float ref = at_share(k, D), f = exp2_approx(ref - x.ref), sum = at_share(k, D + 1), out = at_share(k, c);
-        if (ref != -INFINITY) { // else it has seen nothing
+        if (ref != -INFINITY || sum != 0.0f) { // else it has seen nothing; scores that are not numbers leave no reference, but a sum
             x.sum = fmaf(f, sum, x.sum);
             x.out = fmaf(f, out, x.out);
         }
@@ -877,8 +877,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const __grid_constant
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) x.ref = fmaxf(x.ref, tops[w]);
     for (int k = threadIdx.x; k < n; k += kJoinThreads) {
-        factors[k] = exp2_approx(refs[k] - x.ref);
-        if (refs[k] != -INFINITY) x.sum = fmaf(factors[k], parts[k * Shape::kPartial + D + 1], x.sum); // else it has seen nothing
+        const float sum = parts[k * Shape::kPartial + D + 1];
+        const bool some = refs[k] != -INFINITY || sum != 0.0f; // as in join
+        factors[k] = some ? exp2_approx(refs[k] - x.ref) : -1.0f;
+        if (some) x.sum = fmaf(factors[k], sum, x.sum);
     }
 #pragma unroll
     for (int m = 16; m; m >>= 1) x.sum += __shfl_xor_sync(0xffffffffu, x.sum, m);
@@ -891,7 +893,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const __grid_constant
 #pragma unroll 16
     for (int k = 0; k < n; ++k) {
         const float out = parts[k * Shape::kPartial + (int)threadIdx.x];
-        if (refs[k] != -INFINITY) x.out = fmaf(factors[k], out, x.out);
+        if (!(factors[k] < 0.0f)) x.out = fmaf(factors[k], out, x.out);
     }
     put_joined<T>(a, qr, seq, kv, tile, r, threadIdx.x, x);
 }
