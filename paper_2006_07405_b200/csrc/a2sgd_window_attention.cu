@@ -45,6 +45,8 @@ __device__ __forceinline__ T *at(const Heads &h, int b, int64_t row, int head)
 __device__ unsigned int g_waits_run_out = 0;
 
 constexpr float kLn2 = 0.6931471805599453f;
+// log sum exp of a row that sees some key, from the sum about 2^ref.  No sum: every score was -infinity, and the softmax of that is not a number.
+__device__ __forceinline__ float lse_from(float ref, float sum) { return sum > 0.0f ? (ref + log2f(sum)) * kLn2 : NAN; }
 
 // ------------------------------------------------------------------ forward
 // Persistent CTAs, two an SM, deal out the tiles of 128 queries of one head, the longest first.  For each tile a CTA walks the blocks of 64
@@ -538,10 +540,10 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full(g));
             }
-            const bool some = total > 0.0f || total != total; // not a number: neither is the output
-            const float inverse = some ? 1.0f / total : 0.0f;
+            const bool some = place >= 0; // the row sees a key: that at its own place, at least
+            const float inverse = 1.0f / total; // not a number: neither is the output
             T *p = live ? at<T>(a.o, tile.seq, tile.q_row + row, tile.head) : nullptr;
-            if (live && a.lse) a.lse[lse_of(a, tile, row)] = some ? (ref + log2f(total)) * kLn2 : -INFINITY;
+            if (live && a.lse) a.lse[lse_of(a, tile, row)] = some ? lse_from(ref, total) : -INFINITY;
             bar_pass_cta(o_full, vt & 1, &gave_up);
             fence_after();
 #pragma unroll 1
@@ -640,12 +642,12 @@ __device__ __forceinline__ Joined join(const At &at_share, int n, int c)
     return x;
 }
 template <typename T>
-__device__ __forceinline__ void put_joined(const FewArgs &a, const Range &qr, int seq, int kv, int tile, int r, int c, const Joined &x)
+__device__ __forceinline__ void put_joined(const FewArgs &a, const Range &qr, int ahead, int seq, int kv, int tile, int r, int c, const Joined &x)
 {
     const int row = tile * kFewRows + r, t = row / a.group, head = kv * a.group + row - t * a.group;
-    const bool some = x.sum > 0.0f || x.sum != x.sum;
+    const bool some = t + ahead >= 0; // the key at its own place, at least
     if (c < a.d) at<T>(a.o, seq, qr.first + t, head)[c] = from_f32<T>(some ? x.out / x.sum : 0.0f);
-    if (a.lse && c == 0) a.lse[((int64_t)seq * a.q_heads + head) * a.q_rows + qr.first + t] = some ? (x.ref + log2f(x.sum)) * kLn2 : -INFINITY;
+    if (a.lse && c == 0) a.lse[((int64_t)seq * a.q_heads + head) * a.q_rows + qr.first + t] = some ? lse_from(x.ref, x.sum) : -INFINITY;
 }
 
 template <typename T, int D>
@@ -825,7 +827,7 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
         const int r = i / D, col = i % D;
         const Joined x = join<D>([&](int k, int f) { return parts[k * Shape::kPartial + r * Shape::kRow + f]; }, Shape::kWarps, col);
         if (a.shares == 1) {
-            put_joined<T>(a, qr, seq, kv, tile, r, col, x);
+            put_joined<T>(a, qr, ahead, seq, kv, tile, r, col, x);
         } else if (a.cluster) {
             const int slot = r / a.shares;
             const uint32_t to = map_to(got + 4u * ((share * slots + slot) * Shape::kRow), r - slot * a.shares);
@@ -847,7 +849,7 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
     for (int i = threadIdx.x; i < slots * D; i += 32 * Shape::kWarps) {
         const int slot = i / D, r = slot * a.shares + share;
         if (r >= rows) break;
-        put_joined<T>(a, qr, seq, kv, tile, r, i % D, join<D>([&](int k, int f) { return shares[(k * slots + slot) * Shape::kRow + f]; }, a.shares, i % D));
+        put_joined<T>(a, qr, ahead, seq, kv, tile, r, i % D, join<D>([&](int k, int f) { return shares[(k * slots + slot) * Shape::kRow + f]; }, a.shares, i % D));
     }
 }
 // The shares of a row that are more than a cluster's: a CTA a row, a thread a column, the shares' factors in shared memory.
@@ -895,7 +897,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_few_join(const __grid_constant
         const float out = parts[k * Shape::kPartial + (int)threadIdx.x];
         if (!(factors[k] < 0.0f)) x.out = fmaf(factors[k], out, x.out);
     }
-    put_joined<T>(a, qr, seq, kv, tile, r, threadIdx.x, x);
+    put_joined<T>(a, qr, range_of(a.k_ranges, seq, a.k_rows).count - qr.count, seq, kv, tile, r, threadIdx.x, x);
 }
 
 struct DeltaArgs {

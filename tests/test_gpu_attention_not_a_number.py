@@ -30,3 +30,16 @@ def test_a_query_that_is_not_a_number_over_caches_of_all_lengths(keys, d, room):
     k[0, keys // 2 - 20:keys // 2 + 20] = math.nan
     B.a2sgd_window_attention_forward(q, k, v, o, lse, workspace=work)
     assert torch.isnan(o).all() and torch.isnan(lse).all()
+
+
+def test_a_query_that_sees_only_scores_of_minus_infinity():
+    """Not one that sees nothing: the softmax of such scores is not a number, by either kernel."""
+    for lq in (2, 200):
+        q, k = torch.ones((1, lq, 1, 64), dtype=torch.bfloat16, device="cuda"), -torch.ones((1, 150, 1, 64), dtype=torch.bfloat16, device="cuda")
+        q[0, -1] = math.inf
+        o, lse = torch.zeros_like(q), torch.zeros((1, 1, lq), device="cuda")
+        work = torch.empty(B.a2sgd_window_attention_workspace(q, k, 40, 1, 1), dtype=torch.uint8, device="cuda")
+        B.a2sgd_window_attention_forward(q, k, k, o, lse, window=40, sinks=1, workspace=work)
+        assert torch.isnan(o[0, -1]).all() and torch.isnan(lse[0, 0, -1]) and torch.isfinite(o[0, :-1]).all()
+        empty = max(0, lq - 150)
+        assert torch.isneginf(lse[0, 0, :empty]).all() and torch.isfinite(lse[0, 0, empty:-1]).all() and not o[0, :empty].any()
