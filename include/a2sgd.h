@@ -537,8 +537,9 @@ typedef struct a2sgd_heads {
  *   scale       finite, > 0;   dtype  A2SGD_BF16 or A2SGD_F16
  *   lse         fp32 [sequences][q_heads][q_rows] (packed: [q_heads][q_rows]), out, for the backward pass; may be NULL
  * Tensors whose address is a multiple of 16 bytes and whose strides are multiples of 8 elements are read where they are; others are
- * first copied to the workspace.  A key or value that is not finite reaches every query whose tile of keys it is in, masked or not,
- * as long as it lies in its sequence's range.
+ * first copied to the workspace.  What is not finite reaches what sees it only, in the backward pass, too: a query that sees a value that is
+ * not finite has an output that is not in that column, one that sees a score that is infinite or not a number an output that is not a number.
+ * (A tile of queries or keys with an output that is not finite is worked on twice: a call with such a place in every tile takes some times as long.)
  *   workspace   DEVICE, 256-byte aligned, a2sgd_window_attention_workspace bytes: flags A2SGD_ATTENTION_BACKWARD,
  *               A2SGD_ATTENTION_ALIGNED when every tensor that is read is laid out as above, and A2SGD_ATTENTION_PACKED_Q, _PACKED_K
  *               when the q and the k tensors hold packed sequences (else room is needed for each sequence's plane).  Few queries

@@ -64,7 +64,7 @@ __device__ __forceinline__ float lse_from(float ref, float sum) { return sum > 0
 // loading warp for keys and values 364 and 240 us; 16-byte stores 348 and 230.
 struct ForwardArgs {
     CUtensorMap q, k, v;
-    Heads o;
+    Heads o, values; // values: what v is read from
     float *lse;
     const int32_t *q_ranges, *k_ranges;
     int q_heads, group, d, q_rows, k_rows, window, sinks;
@@ -144,6 +144,115 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int chunks, int rows, 
     __syncwarp();
 }
 
+// A hidden pair's P (or dS) is 0, and 0 times infinity is not a number: an operand that is not finite reaches rows that do not see it.  So a tile
+// with an output that is not finite is done once more, with care: blocks that not every row sees are looked through before their product with P, what is
+// not finite in them is put to 0, and the rows that do see it are given it by mend_row.  A tile without such an output pays for the question: 8 x 4096,
+// 25 heads of 64, forward 346 -> 350 us, backward 1165 -> 1181, 5003 packed rows 80 -> 83.5 (looked through at once: 366, 1201 and 92).  With a first
+// token's value and a third of the gradients not finite in every sequence, 1.7 ms and 2.5 ms.
+constexpr int kAgain = 64;
+struct Again { // in shared memory: the tiles to be done again, in turn
+    int last;  // of those that have been put down, the tile's number among the CTA's
+    volatile int count, items[kAgain];
+    // One lane of each warp that has found something; a CTA's warps are never a tile apart.
+    __device__ __forceinline__ void put(int tile, int item)
+    {
+        if (atomicMax(&last, tile) >= tile) return;
+        items[count % kAgain] = item;
+        __threadfence_block();
+        count = count + 1;
+    }
+    // By the loading warp: whether the next tile is to be one of these, `done` of which have been taken; as long as there are others, not before half a list.
+    __device__ __forceinline__ bool due(int done, bool others)
+    {
+        const int waiting = __shfl_sync(0xffffffffu, count, 0) - done;
+        return waiting > 0 && (!others || waiting >= kAgain / 2);
+    }
+};
+// Not a number where some element of v, of `count` that matter, is not finite.
+__device__ __forceinline__ float judge(const float (&v)[32], int count)
+{
+    f32x2 z[2] = {};
+    if (count >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) z[0] = fma2(pair(v[i], v[i + 1]), pair(0.0f), z[0]), z[1] = fma2(pair(v[i + 2], v[i + 3]), pair(0.0f), z[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) z[0] = fma2(pair(i < count ? v[i] : 0.0f, i + 1 < count ? v[i + 1] : 0.0f), pair(0.0f), z[0]);
+    }
+    return sum2(add2(z[0], z[1]));
+}
+template <typename T>
+__host__ __device__ constexpr uint32_t infinity_bits() { return std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u; }
+__device__ __forceinline__ uint32_t larger_halves(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ void add_size(uint32_t &top, const uint4 &w)
+{
+    top = larger_halves(larger_halves(larger_halves(top, w.x & 0x7fff7fffu), w.y & 0x7fff7fffu), larger_halves(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+}
+template <typename T>
+__device__ __forceinline__ bool not_finite(uint32_t sizes) { return (sizes & 0x7fffu) >= infinity_bits<T>() || (sizes >> 16 & 0x7fffu) >= infinity_bits<T>(); }
+template <typename T>
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w)
+{
+    const uint32_t low = (w & 0x7fffu) >= infinity_bits<T>() ? 0u : w & 0xffffu, high = (w >> 16 & 0x7fffu) >= infinity_bits<T>() ? 0u : w & 0xffff0000u;
+    return low | high;
+}
+// Of `pieces` times 16 bytes of shared memory.  The whole warp.
+template <typename T>
+__device__ __forceinline__ bool some_not_finite(uint32_t tile, int pieces)
+{
+    uint32_t top = 0;
+#pragma unroll 8
+    for (int i = threadIdx.x & 31; i < pieces; i += 32) add_size(top, ld_shared(tile + 16u * i));
+    return __any_sync(0xffffffffu, not_finite<T>(top));
+}
+// Puts what is not finite in the 64 rows of a block, `chunks` times 128 bytes each, to 0; returns the rows that had some.  The whole warp.
+template <typename T>
+__device__ __forceinline__ uint64_t clear_not_finite(uint32_t tile, int chunks)
+{
+    uint32_t low = 0, high = 0;
+#pragma unroll 1
+    for (int i = threadIdx.x & 31; i < chunks * 512; i += 32) {
+        const uint4 w = ld_shared(tile + 16u * i), f = make_uint4(finite_halves<T>(w.x), finite_halves<T>(w.y), finite_halves<T>(w.z), finite_halves<T>(w.w));
+        if (f.x != w.x || f.y != w.y || f.z != w.z || f.w != w.w) {
+            st_shared(tile + 16u * i, f);
+            const int row = i >> 3 & 63;
+            (row < 32 ? low : high) |= 1u << (row & 31);
+        }
+    }
+    fence_async();
+    low = __reduce_or_sync(0xffffffffu, low), high = __reduce_or_sync(0xffffffffu, high);
+    return (uint64_t)high << 32 | low;
+}
+// The rows that were put to 0, of a tile's blocks, in shared memory: for who sees them.
+constexpr int kMarred = 32;
+struct Marred {
+    int count; // beyond kMarred: all rows of all blocks may be
+    int block[kMarred];
+    uint64_t rows[kMarred];
+    __device__ __forceinline__ void put(int n, int b, uint64_t r)
+    {
+        if (n < kMarred) block[n] = b, rows[n] = r;
+    }
+};
+// Column c of an output, as this thread wrote it, and those of the rows that it sees: what is not finite there is not finite here.  As a product with
+// 0 < P: plus itself; with dS, whose sign may be any: not a number.  of(x): row x of the block's, or NULL where it is not seen.
+template <bool SIGNED, typename T, typename Row>
+__device__ __forceinline__ void add_not_finite(float &out, uint64_t rows, int c, const Row &of)
+{
+    while (rows && out == out) {
+        const int x = __ffsll((long long)rows) - 1;
+        rows &= rows - 1;
+        const T *row = of(x);
+        const float v = row ? to_f32(row[c]) : 0.0f;
+        if (!isfinite(v)) out = SIGNED ? out + v : NAN;
+    }
+}
+
 // Up to 32 elements of a row: 32 or 16 bytes at a time (a thread's own sectors: 16-byte stores half fill them), or one element.
 template <typename T>
 __device__ __forceinline__ void store_row(T *p, const float *v, int count, int bytes)
@@ -216,9 +325,12 @@ __device__ __forceinline__ float exponentials(const float (&x)[32], float c, flo
 struct Tile {
     int seq, head, p0, rows;     // place of the first query; queries, at least 1
     int q_row, k_row, k_count;   // rows of the plane, keys
+    int item, careful;
     Blocks blocks;
+    // Whether every query sees every key of the 64 from k0 on.
+    __device__ __forceinline__ bool all_seen(int k0, int window, int sinks) const { return k0 + kBlock - 1 <= p0 && (k0 > p0 + rows - 1 - window || k0 + kBlock <= sinks); }
 };
-constexpr int kTiles = 4; // kept in shared memory, in turn
+constexpr int kTiles = 8; // kept in shared memory, in turn (fewer than half of kAgain: as many may be put down while the loading warp does not look)
 // The whole warp (packed sequences are searched through by its lanes).  False where there are no queries.
 __device__ __forceinline__ bool find_tile(const ForwardArgs &a, int item, Tile &t)
 {
@@ -247,6 +359,26 @@ __device__ __forceinline__ int64_t lse_of(const ForwardArgs &a, const Tile &t, i
     return ((int64_t)(a.packed_q ? 0 : t.seq) * a.q_heads + t.head) * a.q_rows + t.q_row + row;
 }
 
+// What a query sees that is not finite, in blocks that not all of its tile's see.
+template <typename T>
+__device__ __noinline__ void mend_row(T *out, const ForwardArgs &a, const Tile &tile, int place, const Marred &marred)
+{
+    const T *values = at<T>(a.values, tile.seq, tile.k_row, tile.head / a.group);
+    const bool listed = marred.count <= kMarred;
+    for (int c = 0; c < a.d; ++c) {
+        float f = to_f32(out[c]);
+        for (int i = 0; i < (listed ? marred.count : tile.blocks.count) && f == f; ++i) {
+            const int k0 = tile.blocks[listed ? marred.block[i] : i] * kBlock;
+            if (tile.all_seen(k0, a.window, a.sinks)) continue;
+            add_not_finite<true, T>(f, listed ? marred.rows[i] : ~0ull, c, [&](int x) {
+                const int key = k0 + x;
+                return key <= place && (key > place - a.window || key < a.sinks) ? values + (int64_t)key * a.values.row : nullptr;
+            });
+        }
+        if (!isfinite(f)) out[c] = from_f32<T>(f);
+    }
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kCtas) k_forward(const __grid_constant__ ForwardArgs a)
 {
@@ -259,6 +391,8 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     __shared__ Tile tiles[kTiles];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
+    __shared__ Marred marred;
+    __shared__ Again again;
     const uint32_t bar0 = smem_u32(bars);
     // keys' stages, then values'
     const auto full = [&](int s) { return bar0 + 8u * s; };
@@ -278,7 +412,8 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             bar_init(tile_full(t), 1);
             bar_init(tile_empty(t), 6);
         }
-        for (uint32_t b : {q_full, q_empty, tail, o_full}) bar_init(b, 1);
+        for (uint32_t b : {q_full, q_empty, tail}) bar_init(b, 1);
+        bar_init(o_full, 2); // the products, and what is to be known about them
         bar_init(o_empty, 4);
         for (int i = 0; i < kBuffers; ++i) {
             bar_init(s_full(i), 1);
@@ -286,6 +421,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             bar_init(pv_done(i), 1);
         }
         gave_up = 0;
+        again.last = -1, again.count = 0;
         bar_init_fence();
     }
     if (warp == 5) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
@@ -301,13 +437,22 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
     if (warp == 4) {
         // ---------------------------------------------------------- tiles, queries and keys in
         const bool chosen = elect_one();
-        int t = -1, g = 0; // tiles and blocks so far
-        bool ok = true;
-        for (int item = blockIdx.x; ok; item += gridDim.x) {
+        int t = -1, g = 0, done_again = 0; // tiles and blocks so far
+        bool ok = true, judged = false;
+        for (int item = blockIdx.x; ok;) {
             Tile k;
             k.rows = k.blocks.count = 0;
-            const bool end = item >= a.items;
-            if (!end && !find_tile(a, item, k)) continue;
+            const bool others = item < a.items;
+            if (!others && !judged) { // what the last tiles came out as
+                for (int u = max(0, t - kTiles + 1); ok && u <= t; ++u) ok = bar_wait_cta(tile_empty(u), u / kTiles & 1, &gave_up);
+                if (!ok) break;
+                judged = true;
+            }
+            k.careful = again.due(done_again, others);
+            const bool end = !others && !k.careful;
+            k.item = k.careful ? again.items[done_again++ % kAgain] : item;
+            if (!k.careful) item += gridDim.x;
+            if (!end && !find_tile(a, k.item, k)) continue;
             if (!end && k.blocks.count == 0) { // queries that see nothing
                 for (int r = 0; r < k.rows; ++r) {
                     T *o = at<T>(a.o, k.seq, k.q_row + r, k.head);
@@ -426,9 +571,19 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             const int count = ok ? tiles[t % kTiles].blocks.count : 0;
             if (count == 0) break;
             ok = bar_wait_cta(o_empty, (t & 1) ^ 1, &gave_up); // the last tile's output has been read
+            const Tile &tile = tiles[t % kTiles];
+            const bool careful = tile.careful;
+            int bad = 0;
             for (int n = 0; ok && n < count; ++n, ++g) {
                 const int stage = kStages + g % kStages;
-                ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up) && bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
+                ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up);
+                if (!ok) break;
+                if (careful && !tile.all_seen(tile.blocks[n] * kBlock, a.window, a.sinks) && some_not_finite<T>(ring + stage * kSlice, (int)(kSlice / 16))) { // while P is formed
+                    const uint64_t rows = clear_not_finite<T>(ring + stage * kSlice, kChunks);
+                    if (chosen) marred.put(bad, n, rows);
+                    ++bad;
+                }
+                ok = bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
                 if (!ok) break;
                 fence_after();
                 if (chosen) {
@@ -439,6 +594,8 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                     commit(pv_done(g));
                     commit(empty(stage));
                     if (n + 1 == count) {
+                        marred.count = bad;
+                        bar_arrive(o_full);
                         commit(o_full);
                         bar_arrive(tile_empty(t));
                     }
@@ -455,8 +612,6 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             bar_pass_cta(tile_full(vt), vt / kTiles & 1, &gave_up);
             if (__any_sync(0xffffffffu, gave_up)) break;
             const Tile tile = tiles[vt % kTiles];
-            __syncwarp();
-            if (lane == 0) bar_arrive(tile_empty(vt));
             if (tile.rows == 0) break;
             const int row = warp * 32 + lane, place = tile.p0 + row;
             const int w0 = tile.p0 + warp * 32, w1 = w0 + 31; // the warp's places
@@ -546,6 +701,8 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
             if (live && a.lse) a.lse[lse_of(a, tile, row)] = some ? lse_from(ref, total) : -INFINITY;
             bar_pass_cta(o_full, vt & 1, &gave_up);
             fence_after();
+            const bool mend = tile.careful && marred.count;
+            float sound = 0.0f;
 #pragma unroll 1
             for (int e = 0; 32 * e < a.d; ++e) {
                 float o[32];
@@ -554,12 +711,21 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                 if (32 * e + 32 >= a.d) { // all of it has been read
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(o_empty);
+                    if (lane == 0 && !mend) bar_arrive(o_empty);
                 }
+                sound += judge(o, a.d - 32 * e);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = some ? o[i] * inverse : 0.0f;
                 if (live) store_row(p + 32 * e, o, a.d - 32 * e, a.wide_o);
             }
+            if (mend) { // the next tile's list may not be begun before this one has been read
+                if (live) mend_row(p, a, tiles[vt % kTiles], place, marred);
+                __syncwarp();
+                if (lane == 0) bar_arrive(o_empty);
+            }
+            if (__any_sync(0xffffffffu, live && sound != sound && total < INFINITY && !tile.careful) && lane == 0) again.put(vt, tile.item);
+            __syncwarp();
+            if (lane == 0) bar_arrive(tile_empty(vt));
         }
     }
     __syncwarp();
@@ -789,6 +955,38 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
             sum[0] += s[n][0] + s[n][1];
             sum[1] += s[n][2] + s[n][3];
         }
+        if (!all) { // as in the kernel for many queries
+            const uint32_t values_at = place + Shape::kKeys;
+            uint32_t sizes = 0;
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int r = i * (32 / kPieces) + r0;
+                add_size(sizes, ld_shared(values_at + r * (D * 2) + ((e ^ (r & 7)) << 4)));
+            }
+            if (__any_sync(0xffffffffu, not_finite<T>(sizes))) {
+#pragma unroll 1
+                for (int r = 0; r < kFewKeys && k0 + r < stop; ++r) {
+                    const int key = k0 + r;
+                    const bool sees0 = key <= place0 && (key > place0 - a.window || key < a.sinks), sees1 = key <= place1 && (key > place1 - a.window || key < a.sinks);
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j) {
+                        const uint32_t w = ld_shared32(values_at + r * (D * 2) + ((j ^ (r & 7)) << 4) + 4 * c);
+                        const float x = lo_f32(w, T()), y = hi_f32(w, T());
+                        if (!isfinite(x)) o[j][0] += sees0 ? x : 0.0f, o[j][2] += sees1 ? x : 0.0f;
+                        if (!isfinite(y)) o[j][1] += sees0 ? y : 0.0f, o[j][3] += sees1 ? y : 0.0f;
+                    }
+                }
+                __syncwarp();
+#pragma unroll 1
+                for (int i = 0; i < kPieces / 2; ++i) {
+                    const int r = i * (32 / kPieces) + r0;
+                    const uint32_t piece = values_at + r * (D * 2) + ((e ^ (r & 7)) << 4);
+                    const uint4 w = ld_shared(piece);
+                    st_shared(piece, make_uint4(finite_halves<T>(w.x), finite_halves<T>(w.y), finite_halves<T>(w.z), finite_halves<T>(w.w)));
+                }
+                __syncwarp();
+            }
+        }
         const uint32_t a0 = pack2(s[0][0], s[0][1], T()), a1 = pack2(s[0][2], s[0][3], T()), a2 = pack2(s[1][0], s[1][1], T()), a3 = pack2(s[1][2], s[1][3], T());
         const int r = lane & 15; // the row whose address this lane gives: keys 0 to 15, twice
 #pragma unroll
@@ -929,6 +1127,7 @@ struct DeltaArgs {
 struct BackwardArgs {
     CUtensorMap stay0, stay1, pass0, pass1;
     Heads out0, out1; // dq; or dk, dv
+    Heads passing;    // what k, or dout, is read from
     int wide0, wide1;
     const float *lse2, *delta; // [q_heads][q_rows] a plane: log2 e times lse, delta
     float *partials;           // [lanes][sink_rows][parts][2][D]
@@ -957,7 +1156,16 @@ struct BackwardTile {
     int q_row, q_count, k_row, k_count;
     int first, count;      // KEYS: first query of the first block; blocks (times heads) of this part
     int part, begin;       // KEYS: part, and its first block
+    int item, careful;
     Blocks blocks;         // of keys
+    // Whether every row that stays sees, or is seen by, every row of the 64 that pass from o0 on.
+    template <bool KEYS>
+    __device__ __forceinline__ bool all_seen(int o0, int window, int sinks) const
+    {
+        if (!KEYS) return o0 + kBlock - 1 <= place0 && (o0 > place0 + rows - 1 - window || o0 + kBlock <= sinks);
+        const int ahead = k_count - q_count, last_key = place0 + rows - 1;
+        return o0 + ahead >= last_key && (min(o0 + kBlock, q_count) - 1 + ahead - window < place0 || last_key < sinks);
+    }
 };
 
 // KEYS: the blocks of queries, times heads, that see the keys kb to kb + 127 (within the range), from query `first` on.
@@ -1011,6 +1219,43 @@ __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, Backw
     return true;
 }
 
+// Where a key's row of partial sums begins, of dk; dv's are behind.
+template <int D>
+__device__ __forceinline__ float *partial_row(const BackwardArgs &a, int seq, int head, int key, int part)
+{
+    return a.partials + (((int64_t)(seq * a.kv_heads + head) * a.sink_rows + key) * a.parts + part) * 2 * D;
+}
+
+// As in the forward pass: dq from the keys, dv from the outputs' gradients (what is not finite of a query is in its lse, and so in P and dk already).
+// `row`, at `place`, is the thread's, of the tile's; so are `columns` of it on, 32 in `step`.
+template <typename T, int D, bool KEYS>
+__device__ __noinline__ void mend_row(const BackwardArgs &a, const BackwardTile &tile, int place, int row, int columns, int step, bool partial, const Marred &marred)
+{
+    if (!partial && tile.part) return;
+    const int ahead = tile.k_count - tile.q_count;
+    float *sums = partial ? partial_row<D>(a, tile.seq, tile.head, place, tile.part) + D : nullptr;
+    T *out = partial ? nullptr : at<T>(KEYS ? a.out1 : a.out0, tile.seq, tile.row + row, tile.head);
+    const bool listed = marred.count <= kMarred;
+    for (int c0 = columns; c0 < a.d; c0 += step)
+        for (int c = c0; c < min(c0 + 32, a.d); ++c) {
+            float f = partial ? sums[c] : to_f32(out[c]);
+            for (int i = 0; i < (listed ? marred.count : tile.count) && f == f; ++i) {
+                const int n = listed ? marred.block[i] : i, at_block = tile.begin + n, o0 = KEYS ? tile.first + at_block / a.group * 64 : tile.blocks[n] * kBlock;
+                if (tile.template all_seen<KEYS>(o0, a.window, a.sinks)) continue;
+                const int head = KEYS ? tile.head * a.group + at_block % a.group : tile.head / a.group;
+                const T *passing = at<T>(a.passing, tile.seq, KEYS ? tile.q_row : tile.k_row, head);
+                add_not_finite<KEYS, T>(f, listed ? marred.rows[i] : ~0ull, c, [&](int x) {
+                    const int o = o0 + x, q_place = KEYS ? o + ahead : place, key = KEYS ? place : o;
+                    return o < (KEYS ? tile.q_count : tile.k_count) && key <= q_place && (key > q_place - a.window || key < a.sinks) ? passing + (int64_t)o * a.passing.row
+                                                                                                                                     : nullptr;
+                });
+            }
+            if (isfinite(f)) continue;
+            if (partial) sums[c] = f;
+            else out[c] = from_f32<T>(f);
+        }
+}
+
 template <typename T, int D, bool KEYS>
 __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backward(const __grid_constant__ BackwardArgs a)
 {
@@ -1024,6 +1269,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     __shared__ __align__(16) float columns[KEYS ? kStages : 1][2][64]; // KEYS: -lse2 and -delta of the queries that pass
     __shared__ uint32_t tmem_at;
     __shared__ volatile int gave_up;
+    __shared__ Marred marred;
+    __shared__ Again again;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
     const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
@@ -1046,7 +1293,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             bar_init(tile_full(t), 1);
             bar_init(tile_empty(t), 4 * kGroups + 2);
         }
-        for (uint32_t b : {tail(0), tail(1), out_full}) bar_init(b, 1);
+        for (uint32_t b : {tail(0), tail(1)}) bar_init(b, 1);
+        bar_init(out_full, 2); // the products, and what is to be known about them
         for (int i = 0; i < kStay; ++i) {
             bar_init(stay_full(i), 1);
             bar_init(stay_empty(i), 1);
@@ -1058,6 +1306,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             bar_init(out_done(i), 1);
         }
         gave_up = 0;
+        again.last = -1, again.count = 0;
         bar_init_fence();
     }
     if (warp == kForm) tmem_alloc(smem_u32(&tmem_at), Shape::kColumns);
@@ -1119,18 +1368,30 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
     if (warp == kLoad) {
         // ---------------------------------------------------------- tiles in
         const bool chosen = elect_one();
-        int kt = -1, g = 0;
+        int kt = -1, g = 0, done_again = 0;
         uint32_t tails = 0;
-        bool ok = true;
+        bool ok = true, judged = false;
         const auto take = [&] {
             unsigned int n = lane == 0 ? atomicAdd(a.next, 1u) : 0;
             return (int)(gridDim.x + __shfl_sync(0xffffffffu, n, 0));
         };
-        for (int item = blockIdx.x; ok; item = take()) {
+        bool taken = true;
+        for (int item = blockIdx.x; ok;) { // as in the forward pass
+            if (!taken) item = take(); // not before the last tile's blocks are on their way
+            taken = true;
             BackwardTile t;
             t.rows = t.count = 0;
-            const bool end = item >= a.items;
-            if (!end && !find_tile<KEYS>(a, item, t)) continue;
+            const bool others = item < a.items;
+            if (!others && !judged) {
+                for (int u = max(0, kt - kTiles + 1); ok && u <= kt; ++u) ok = bar_wait_cta(tile_empty(u), u / kTiles & 1, &gave_up);
+                if (!ok) break;
+                judged = true;
+            }
+            t.careful = again.due(done_again, others);
+            const bool end = !others && !t.careful;
+            t.item = t.careful ? again.items[done_again++ % kAgain] : item;
+            if (!t.careful && others) taken = false;
+            if (!end && !find_tile<KEYS>(a, t.item, t)) continue;
             if (!end && t.count == 0) { // rows that nothing sees, or that see nothing
                 for (int r = 0; r < t.rows; ++r) {
                     for (int o = 0; o < (KEYS ? 2 : 1); ++o) {
@@ -1235,10 +1496,27 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             const int count = ok ? tiles[t % kTiles].count : 0;
             if (count == 0) break;
             ok = bar_wait_cta(out_empty, (t & 1) ^ 1, &gave_up); // the last tile's outputs have been read
+            const BackwardTile &tile = tiles[t % kTiles];
+            const bool careful = tile.careful;
+            int bad = 0;
             for (int n = 0; ok && n < count; ++n, ++g) {
                 const int stage = g % kStages;
+                // as in the forward pass; S and dP are formed of what is there
+                bool clear = false;
+                constexpr int kPieces = (int)((KEYS ? Shape::kStage : kSlice) / 16);
+                if (careful && !tile.template all_seen<KEYS>(KEYS ? tile.first + (tile.begin + n) / a.group * 64 : tile.blocks[n] * kBlock, a.window, a.sinks)) {
+                    ok = bar_wait_cta(full(stage), g / kStages & 1, &gave_up);
+                    if (!ok) break;
+                    clear = some_not_finite<T>(ring + stage * Shape::kStage, kPieces); // while P is formed
+                }
                 ok = bar_wait_cta(p_full(g), g / kBuffers & 1, &gave_up);
                 if (!ok) break;
+                if (clear) {
+                    uint64_t rows = clear_not_finite<T>(ring + stage * Shape::kStage, kChunks);
+                    if (KEYS) rows = clear_not_finite<T>(ring + stage * Shape::kStage + kSlice, kChunks);
+                    if (chosen) marred.put(bad, n, rows);
+                    ++bad;
+                }
                 fence_after();
                 if (chosen) {
                     const uint32_t s = tmem + 128 * (g % kBuffers), ds = KEYS ? s + 64 : s;
@@ -1254,6 +1532,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                     commit(out_done(g));
                     commit(empty(stage)); // S and dP, which had read it, too, are done: P came of them
                     if (n + 1 == count) {
+                        marred.count = bad;
+                        bar_arrive(out_full);
                         commit(out_full);
                         bar_arrive(tile_empty(t));
                     }
@@ -1272,8 +1552,6 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             bar_pass_cta(tile_full(vt), vt / kTiles & 1, &gave_up);
             if (__any_sync(0xffffffffu, gave_up)) break;
             const BackwardTile tile = tiles[vt % kTiles];
-            __syncwarp();
-            if (lane == 0) bar_arrive(tile_empty(vt));
             if (tile.rows == 0) break;
             const int row = quarter * 32 + lane, place = tile.place0 + row; // KEYS: the key
             const int w0 = tile.place0 + quarter * 32, w1 = w0 + 31;
@@ -1352,6 +1630,8 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             }
             bar_pass_cta(out_full, vt & 1, &gave_up);
             fence_after();
+            const bool mend = tile.careful && marred.count;
+            float sound = 0.0f;
             // the outputs, 32 columns of each a group of warps in turn
             const uint32_t to = lanes + Shape::kOut;
             const bool partial = KEYS && a.parts > 1 && live && place < a.sinks; // another part of this tile has some, too
@@ -1364,10 +1644,11 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
                 float v[32];
                 tmem_ld32(to + D * o + cc, v);
                 tmem_wait_ld();
+                sound += judge(v, a.d - cc);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] *= factor;
                 if (partial) {
-                    float *q = a.partials + ((((int64_t)(tile.seq * a.kv_heads + tile.head) * a.sink_rows + place) * a.parts + tile.part) * 2 + o) * D + cc;
+                    float *q = partial_row<D>(a, tile.seq, tile.head, place, tile.part) + o * D + cc;
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4 *>(q + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                 } else if (live && tile.part == 0) {
@@ -1376,7 +1657,12 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             }
             fence_before();
             __syncwarp();
+            if (mend && live && (!KEYS || a.out1.p)) mend_row<T, D, KEYS>(a, tiles[vt % kTiles], place, row, 32 * group, 32 * kGroups, partial, marred);
+            __syncwarp();
             if (lane == 0) bar_arrive(out_empty);
+            if (__any_sync(0xffffffffu, live && sound != sound && minus_lse == minus_lse && !tile.careful) && lane == 0) again.put(vt, tile.item);
+            __syncwarp();
+            if (lane == 0) bar_arrive(tile_empty(vt));
         }
     }
     __syncwarp();
@@ -1712,7 +1998,7 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
     ForwardArgs f{};
     if (!make_map(&f.q, pq, shape->dtype, 128)) return A2SGD_ERR_CUDA;
     if (k.rows && (!make_map(&f.k, pk, shape->dtype, kBlock) || !make_map(&f.v, pv, shape->dtype, kBlock))) return A2SGD_ERR_CUDA;
-    f.o = o.h;
+    f.o = o.h, f.values = pv.h;
     f.lse = lse;
     f.q_ranges = shape->q_ranges, f.k_ranges = shape->k_ranges;
     f.q_heads = q.heads, f.group = q.heads / k.heads, f.d = q.d;
@@ -1789,6 +2075,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         if (!maps()) return A2SGD_ERR_CUDA;
         b.stay0_planes = k.planes, b.stay1_planes = v.planes, b.pass0_planes = q.planes, b.pass1_planes = dout.planes;
         b.out0 = dk.h, b.out1 = dv.h;
+        b.passing = dout.h;
         b.wide0 = store_bytes(dk), b.wide1 = store_bytes(dv);
         rc = launch_backward<T, D, true>(b, k.rows, sms, s);
         if (rc != A2SGD_OK) return rc;
@@ -1802,6 +2089,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         if (!maps()) return A2SGD_ERR_CUDA;
         c.stay0_planes = q.planes, c.stay1_planes = dout.planes, c.pass0_planes = k.planes, c.pass1_planes = v.planes;
         c.out0 = dq.h, c.out1 = Heads{nullptr, 0, 0, 0};
+        c.passing = k.h;
         c.wide0 = store_bytes(dq);
         c.next = b.next + 1;
         c.beside = keys;
