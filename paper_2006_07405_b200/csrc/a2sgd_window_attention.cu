@@ -1105,6 +1105,10 @@ struct DeltaArgs {
     int64_t rows;
     unsigned int *next; // two, cleared
     int blocks, heads, d, wide; // CTAs of a plane
+    // packed queries whose first tokens' passes are cut into parts (see PartsList)
+    const int32_t *q_ranges;
+    int *list;
+    int sequences, group, part_blocks, more, listed;
 };
 
 // ------------------------------------------------------------------ backward
@@ -1116,7 +1120,8 @@ struct DeltaArgs {
 // P = exp(scale S - lse) and dS = P (dP - delta) and writes them over S and dP in 16 bits; then out += dS B, out' += P B'.
 // Roles and tiles as in the forward pass, one CTA an SM, with three buffers of S and dP (two where dK and dV of 128 elements leave no more) and
 // two groups of four warps, each with half of a block.
-// The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.
+// The first tokens' keys are seen by every query: their tiles' passes are cut into parts, whose sums are joined in order by k_fold_keys.  Sequences of packed
+// queries are cut by their own lengths, which the device knows: see PartsList.
 //
 // Bound by the softmax' warps and what lies between them and the products: S and dP come out of TMEM, P and dS go back, 1100 to 1400 clocks a block of
 // 64, in which the products take 611 and the exponentials 560.  B200, 8 x 4096 queries, 25 heads of 64, window 1024: dk and dv 610 us, dq 490,
@@ -1137,6 +1142,8 @@ struct BackwardArgs {
     int stay0_planes, stay1_planes, pass0_planes, pass1_planes;
     int tiles, lanes, items, together;
     int parts, part_blocks, sink_tiles, sink_rows, extra; // parts of a first tokens' tile, blocks of each; tiles and keys; items of a lane beyond its tiles
+    const int *list;   // packed queries: PartsList, and then `extra` are a key head's and come before all others
+    int listed, slots; // room in it; parts of a key head that it can have
     unsigned int *next; // items taken beyond every CTA's first one
     int beside;         // dq: the launch before is that of dk and dv, whose CTAs have all waited for what this one reads: it waits for its end only
     float scale, scale_log2;
@@ -1150,12 +1157,83 @@ struct BackwardShape {
     static constexpr uint32_t kColumns = 512, kOut = kBuffers * 128; // of dK or dQ; dV's behind
 };
 
+// Sequences of packed queries whose first tokens' passes have more than one part, in order: their number, the sequences, and for each how many parts
+// beyond a first one the sequences before it have (and, last, all have).  Every query is in one sequence, so that the parts of all together are bound by
+// the rows (`more` beyond the first ones); a sequence beyond that bound, as overlapping ranges could have it, keeps one part.
+struct PartsList {
+    const int *p;
+    int room; // sequences
+    __device__ __forceinline__ int count() const { return __ldcg(p); }
+    __device__ __forceinline__ int sequence(int m) const { return __ldcg(p + 1 + m); }
+    __device__ __forceinline__ int before(int m) const { return __ldcg(p + 1 + room + m); }
+    // The first of n numbers in order that is at least x.  The whole warp.
+    __device__ static __forceinline__ int search(const int *v, int n, int x)
+    {
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const int i = i0 + (int)(threadIdx.x & 31);
+            const unsigned hit = __ballot_sync(0xffffffffu, i < n && __ldcg(v + i) >= x);
+            if (hit) return i0 + __ffs(hit) - 1;
+        }
+        return n;
+    }
+    __device__ __forceinline__ int of_sequence(int seq) const // -1: not in the list
+    {
+        const int n = count(), m = search(p + 1, n, seq);
+        return m < n && sequence(m) == seq ? m : -1;
+    }
+    __device__ __forceinline__ int of_part(int x) const // x-th of the parts beyond first ones
+    {
+        const int n = count(), m = search(p + 2 + room, n, x + 1);
+        return m < n ? m : -1;
+    }
+    static uint64_t bytes(int64_t room) { return (uint64_t)(2 * room + 2) * 4; }
+};
+// Its making, by one CTA of 256 threads.
+__device__ __forceinline__ void list_parts(const DeltaArgs &a)
+{
+    __shared__ int64_t sums[8];
+    __shared__ int ranks[8], count;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int64_t sum_before = 0;
+    int rank_before = 0;
+    if (tid == 0) count = 0, a.list[1 + a.listed] = 0;
+    for (int b0 = 0; b0 < a.sequences; b0 += 256) {
+        const int b = b0 + tid;
+        const int64_t blocks = b < a.sequences ? (int64_t)((range_of(a.q_ranges, b, (int)a.rows).count + 63) / 64) * a.group : 0;
+        const int64_t mine = blocks ? (blocks - 1) / a.part_blocks : 0;
+        int64_t sum = mine;
+        int rank = mine > 0;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, sum, s);
+            const int r = __shfl_up_sync(0xffffffffu, rank, s);
+            if (lane >= s) sum += v, rank += r;
+        }
+        __syncthreads();
+        if (lane == 31) sums[warp] = sum, ranks[warp] = rank;
+        __syncthreads();
+        for (int w = 0; w < 8; ++w) {
+            if (w < warp) sum += sums[w], rank += ranks[w];
+        }
+        if (mine > 0 && sum_before + sum <= a.more) { // and so rank_before + rank, at least one each, is not more either
+            const int m = rank_before + rank - 1;
+            a.list[1 + m] = b;
+            a.list[2 + a.listed + m] = (int)(sum_before + sum);
+            atomicMax(&count, m + 1);
+        }
+        for (int w = 0; w < 8; ++w) sum_before += sums[w], rank_before += ranks[w];
+    }
+    __syncthreads();
+    if (tid == 0) a.list[0] = count;
+}
+
 struct BackwardTile {
     int seq, head;         // KEYS: key head
     int row, rows, place0; // in the plane, number; KEYS: first key, else place of the first query
     int q_row, q_count, k_row, k_count;
     int first, count;      // KEYS: first query of the first block; blocks (times heads) of this part
     int part, begin;       // KEYS: part, and its first block
+    int parts, slot;       // KEYS: parts that the tile may have; with a list, the sequence's first place among the parts of all
     int item, careful;
     Blocks blocks;         // of keys
     // Whether every row that stays sees, or is seen by, every row of the 64 that pass from o0 on.
@@ -1180,23 +1258,41 @@ __device__ __forceinline__ int query_blocks(int kb, int q_count, int k_count, in
 template <bool KEYS>
 __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, BackwardTile &t)
 {
-    const int each = a.tiles + a.extra;
-    const int part = item / (a.together * each), rest = item - part * a.together * each;
-    const int wide = min(a.together, a.lanes - part * a.together), lane = part * a.together + rest % wide;
     const int heads = KEYS ? a.kv_heads : a.q_heads;
-    int tile = rest / wide;
-    t.head = lane % heads;
-    t.seq = lane / heads;
-    t.part = 0;
-    if (KEYS && tile < a.extra) {
-        const int more = a.parts - 1;
-        t.part = 1 + tile % more;
-        tile /= more;
-        if (a.packed_k) t.seq = tile / a.sink_tiles, tile %= a.sink_tiles;
+    int tile;
+    t.part = 0, t.parts = KEYS ? a.parts : 1, t.slot = 0;
+    const int listed = KEYS && a.list ? a.extra * heads : 0; // of all key heads together, first
+    const PartsList list{a.list, a.listed};
+    if (KEYS && item < listed) {
+        t.head = item % heads;
+        tile = item / heads % a.sink_tiles;
+        const int x = item / heads / a.sink_tiles, m = list.of_part(x);
+        if (m < 0) return false;
+        const int before = list.before(m);
+        t.seq = list.sequence(m), t.part = 1 + x - before, t.parts = 1 + list.before(m + 1) - before, t.slot = before + m;
     } else {
-        tile = KEYS ? tile - a.extra : a.tiles - 1 - tile;
-        if (KEYS ? a.packed_k : a.packed_q) locate(KEYS ? a.k_ranges : a.q_ranges, a.sequences, KEYS ? a.k_rows : a.q_rows, 128, tile, t.seq, tile);
-        if (t.seq < 0) return false;
+        item -= listed;
+        const int each = a.tiles + (KEYS && !a.list ? a.extra : 0);
+        const int group = item / (a.together * each), rest = item - group * a.together * each;
+        const int wide = min(a.together, a.lanes - group * a.together), lane = group * a.together + rest % wide;
+        tile = rest / wide;
+        t.head = lane % heads;
+        t.seq = lane / heads;
+        if (KEYS && !a.list && tile < a.extra) {
+            const int more = a.parts - 1;
+            t.part = 1 + tile % more;
+            tile /= more;
+            if (a.packed_k) t.seq = tile / a.sink_tiles, tile %= a.sink_tiles;
+        } else {
+            tile = KEYS ? tile - (a.list ? 0 : a.extra) : a.tiles - 1 - tile;
+            if (KEYS ? a.packed_k : a.packed_q) locate(KEYS ? a.k_ranges : a.q_ranges, a.sequences, KEYS ? a.k_rows : a.q_rows, 128, tile, t.seq, tile);
+            if (t.seq < 0) return false;
+            if (KEYS && a.list) {
+                const int m = tile < a.sink_tiles ? list.of_sequence(t.seq) : -1;
+                t.parts = 1;
+                if (m >= 0) t.parts += list.before(m + 1) - list.before(m), t.slot = list.before(m) + m;
+            }
+        }
     }
     const Range qr = range_of(a.q_ranges, t.seq, a.q_rows), kr = range_of(a.k_ranges, t.seq, a.k_rows);
     t.q_row = qr.first, t.q_count = qr.count, t.k_row = kr.first, t.k_count = kr.count;
@@ -1208,7 +1304,7 @@ __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, Backw
         t.place0 = tile * 128;
         const int all = query_blocks(tile * 128, qr.count, kr.count, a.window, a.sinks, a.group, t.first);
         t.begin = t.part * a.part_blocks;
-        t.count = min(all - t.begin, a.parts > 1 ? a.part_blocks : all);
+        t.count = min(all - t.begin, t.parts > 1 ? a.part_blocks : all);
         if (t.part && t.count <= 0) return false;
         t.count = max(t.count, 0);
     } else {
@@ -1219,11 +1315,12 @@ __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, Backw
     return true;
 }
 
-// Where a key's row of partial sums begins, of dk; dv's are behind.
+// Where a key's row of partial sums of a part begins, of dk; dv's are behind.  slot: with a list, the sequence's.
 template <int D>
-__device__ __forceinline__ float *partial_row(const BackwardArgs &a, int seq, int head, int key, int part)
+__device__ __forceinline__ float *partial_row(const BackwardArgs &a, int seq, int slot, int head, int key, int part)
 {
-    return a.partials + (((int64_t)(seq * a.kv_heads + head) * a.sink_rows + key) * a.parts + part) * 2 * D;
+    const int64_t row = a.list ? ((int64_t)head * a.slots + slot + part) * a.sink_rows + key : ((int64_t)(seq * a.kv_heads + head) * a.sink_rows + key) * a.parts + part;
+    return a.partials + row * 2 * D;
 }
 
 // As in the forward pass: dq from the keys, dv from the outputs' gradients (what is not finite of a query is in its lse, and so in P and dk already).
@@ -1233,7 +1330,7 @@ __device__ __noinline__ void mend_row(const BackwardArgs &a, const BackwardTile 
 {
     if (!partial && tile.part) return;
     const int ahead = tile.k_count - tile.q_count;
-    float *sums = partial ? partial_row<D>(a, tile.seq, tile.head, place, tile.part) + D : nullptr;
+    float *sums = partial ? partial_row<D>(a, tile.seq, tile.slot, tile.head, place, tile.part) + D : nullptr;
     T *out = partial ? nullptr : at<T>(KEYS ? a.out1 : a.out0, tile.seq, tile.row + row, tile.head);
     const bool listed = marred.count <= kMarred;
     for (int c0 = columns; c0 < a.d; c0 += step)
@@ -1634,7 +1731,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
             float sound = 0.0f;
             // the outputs, 32 columns of each a group of warps in turn
             const uint32_t to = lanes + Shape::kOut;
-            const bool partial = KEYS && a.parts > 1 && live && place < a.sinks; // another part of this tile has some, too
+            const bool partial = KEYS && tile.parts > 1 && live && place < a.sinks; // another part of this tile has some, too
 #pragma unroll 1
             for (int i = group; i < (KEYS ? 2 : 1) * (D / 32); i += kGroups) {
                 const int o = i / (D / 32), cc = i % (D / 32) * 32;
@@ -1648,7 +1745,7 @@ __global__ void __launch_bounds__(BackwardShape<D, KEYS>::kThreads, 1) k_backwar
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] *= factor;
                 if (partial) {
-                    float *q = partial_row<D>(a, tile.seq, tile.head, place, tile.part) + o * D + cc;
+                    float *q = partial_row<D>(a, tile.seq, tile.slot, tile.head, place, tile.part) + o * D + cc;
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4 *>(q + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                 } else if (live && tile.part == 0) {
@@ -1686,8 +1783,15 @@ __global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ Backw
     constexpr int kPieces = 2 * (D / 32);
     const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), item = warp / kPieces;
     const int piece = (int)(warp % kPieces), o = piece / (D / 32), c = piece % (D / 32) * 32 + (threadIdx.x & 31);
-    if (item >= (int64_t)a.sequences * a.kv_heads * a.sink_rows) return;
-    const int key = (int)(item % a.sink_rows), lane = (int)(item / a.sink_rows), head = lane % a.kv_heads, seq = lane / a.kv_heads;
+    if (item >= (int64_t)(a.list ? a.listed : a.sequences) * a.kv_heads * a.sink_rows) return;
+    const int key = (int)(item % a.sink_rows), lane = (int)(item / a.sink_rows), head = lane % a.kv_heads;
+    int seq = lane / a.kv_heads, slot = 0;
+    if (a.list) {
+        const PartsList list{a.list, a.listed};
+        const int m = seq;
+        if (m >= list.count()) return;
+        seq = list.sequence(m), slot = list.before(m) + m;
+    }
     const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
     if (key >= kr.count) return;
     int first;
@@ -1698,7 +1802,7 @@ __global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ Backw
     if (!h.p || c >= a.d) return;
     float sum = 0.0f;
 #pragma unroll 4
-    for (int k = 0; k < parts; ++k) sum += a.partials[((item * a.parts + k) * 2 + o) * D + c];
+    for (int k = 0; k < parts; ++k) sum += partial_row<D>(a, seq, slot, head, key, k)[o * D + c];
     at<T>(h, seq, kr.first + key, head)[c] = from_f32<T>(sum);
 }
 
@@ -1710,6 +1814,7 @@ __global__ void __launch_bounds__(256) k_delta(const __grid_constant__ DeltaArgs
     wait_prior_grid();
     release_next_grid();
     if (blockIdx.x == 0 && threadIdx.x < 2) a.next[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && a.list) list_parts(a);
     constexpr int kEach = 256 / LANES, kAhead = 4; // queries at a time, whose reads come before their sums
     const int lane = threadIdx.x % LANES, plane = blockIdx.x / a.blocks;
     const int64_t row0 = (int64_t)(blockIdx.x % a.blocks) * kDeltaRows;
@@ -2016,8 +2121,9 @@ int forward(const a2sgd_attention *shape, const Tensor &q, const Tensor &k, cons
 // How the first tokens' tiles are cut: the blocks of an ordinary tile's pass each, or 32 at least.
 struct Parts {
     int parts = 1, blocks = 0, sink_tiles = 0, sink_rows = 0;
+    int more = 0, listed = 0; // packed queries: parts of all sequences beyond a first one each; sequences that have some
 };
-Parts parts_of(const a2sgd_attention *s)
+Parts parts_of(const a2sgd_attention *s, bool packed_q)
 {
     Parts p;
     const int64_t group = s->q_heads / s->kv_heads, q_rows = (int64_t)s->q_rows, k_rows = (int64_t)s->k_rows;
@@ -2029,13 +2135,21 @@ Parts parts_of(const a2sgd_attention *s)
     p.blocks = (int)each;
     p.sink_tiles = (int)((sinks + 127) / 128);
     p.sink_rows = (int)sinks;
+    if (packed_q) {
+        // A sequence with a second part has more than `each` >= 3 group blocks times heads, so four blocks of 64 or more and 193 rows at least: there are
+        // at most q_rows / 193 of them, with q_rows / 64 blocks and one for each that is not full.
+        p.more = (int)(((q_rows + 63) / 64 + std::min<int64_t>(s->sequences, q_rows / 193)) * group / each);
+        p.listed = (int)std::min<int64_t>(s->sequences, p.more);
+    }
     return p;
 }
 constexpr uint64_t kCounters = 256; // bytes: of items taken, by dk and dv, and by dq
-uint64_t partial_bytes(const a2sgd_attention *s)
+uint64_t partial_bytes(const a2sgd_attention *s, bool packed_q)
 {
-    const Parts p = parts_of(s);
-    return p.parts > 1 ? up256((uint64_t)s->sequences * s->kv_heads * p.sink_rows * p.parts * 2 * (s->head_dim <= 64 ? 64 : 128) * 4) : 0;
+    const Parts p = parts_of(s, packed_q);
+    if (p.parts == 1) return 0;
+    const uint64_t rows = (packed_q ? (uint64_t)(p.more + p.listed) : (uint64_t)s->sequences * p.parts) * s->kv_heads * p.sink_rows;
+    return up256(rows * 2 * (s->head_dim <= 64 ? 64 : 128) * 4) + (packed_q ? up256(PartsList::bytes(p.listed)) : 0);
 }
 
 template <typename T, int D, bool KEYS>
@@ -2045,8 +2159,9 @@ int launch_backward(BackwardArgs &b, int64_t rows, int sms, cudaStream_t s)
     const bool packed = KEYS ? b.packed_k : b.packed_q;
     b.tiles = (int)(packed ? rows / 128 + b.sequences : (rows + 127) / 128);
     const int64_t lanes = (int64_t)(KEYS ? b.kv_heads : b.q_heads) * (packed ? 1 : b.sequences);
-    const int64_t extra = KEYS ? (int64_t)b.sink_tiles * (b.parts - 1) * (packed ? b.sequences : 1) : 0;
-    const int64_t items = lanes * (b.tiles + extra);
+    // with a list, of a key head; else of a lane
+    const int64_t extra = !KEYS ? 0 : b.list ? (int64_t)b.sink_tiles * (b.slots - b.listed) : (int64_t)b.sink_tiles * (b.parts - 1) * (packed ? b.sequences : 1);
+    const int64_t items = lanes * b.tiles + (KEYS && b.list ? b.kv_heads : lanes) * extra;
     if (items > 0x3fffffff) return A2SGD_ERR_TOO_LARGE;
     b.lanes = (int)lanes;
     b.extra = (int)extra;
@@ -2097,7 +2212,7 @@ int run_backward(BackwardArgs &b, const Tensor &q, const Tensor &k, const Tensor
         if (rc != A2SGD_OK) return rc;
     }
     if (keys && b.parts > 1) {
-        const int64_t rows = (int64_t)b.sequences * b.kv_heads * b.sink_rows; // far below a grid's limit: their partial sums fit the workspace
+        const int64_t rows = (int64_t)(b.list ? b.listed : b.sequences) * b.kv_heads * b.sink_rows; // far below a grid's limit: their partial sums fit the workspace
         void *params[] = {&b};
         A2_TRAIN_CUDA(launch(reinterpret_cast<const void *>(&k_fold_keys<T, D>), dim3((unsigned)(rows * 2 * (D / 32) / 8 + 1)), 256, 0, params, s));
     }
@@ -2115,7 +2230,10 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
     float *lse2 = static_cast<float *>(pack.take(lines * 4)), *delta = static_cast<float *>(pack.take(lines * 4));
     b.lse2 = lse2, b.delta = delta;
     b.next = static_cast<unsigned int *>(pack.take(kCounters));
-    b.partials = static_cast<float *>(pack.take(partial_bytes(shape)));
+    const Parts parts = parts_of(shape, packed_q);
+    const uint64_t for_parts = partial_bytes(shape, packed_q), for_list = parts.listed ? up256(PartsList::bytes(parts.listed)) : 0;
+    int *list = for_list ? static_cast<int *>(pack.take(for_list)) : nullptr;
+    b.partials = static_cast<float *>(pack.take(for_parts - for_list));
     const Tensor pq = pack.usable(q), pk = pack.usable(k), pv = pack.usable(v), pdout = pack.usable(dout);
     if (!pack.fits(workspace_bytes)) return A2SGD_ERR_ARG;
     int rc = pack.run(sms, s);
@@ -2131,13 +2249,17 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
         d.blocks = (int)blocks;
         d.heads = q.heads, d.d = q.d;
         d.wide = wide(o) && wide(dout);
+        if (dk.h.p || dv.h.p) {
+            d.list = list, d.q_ranges = shape->q_ranges;
+            d.sequences = (int)shape->sequences, d.group = q.heads / k.heads;
+            d.part_blocks = parts.blocks, d.more = parts.more, d.listed = parts.listed;
+        }
         void *params[] = {&d};
         const void *fn = q.d <= 64 ? reinterpret_cast<const void *>(&k_delta<T, 8>) : reinterpret_cast<const void *>(&k_delta<T, 16>);
         A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(planes * blocks)), 256, 0, params, s));
     } else {
         A2_TRAIN_CUDA(cudaMemsetAsync(b.next, 0, kCounters, s));
     }
-    const Parts parts = parts_of(shape);
     b.q_ranges = shape->q_ranges, b.k_ranges = shape->k_ranges;
     b.q_heads = q.heads, b.kv_heads = k.heads, b.group = q.heads / k.heads, b.d = q.d;
     b.q_rows = (int)q.rows, b.k_rows = (int)k.rows;
@@ -2146,6 +2268,7 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
     b.packed_q = packed_q, b.packed_k = packed_k;
     b.sequences = (int)shape->sequences;
     b.parts = parts.parts, b.part_blocks = parts.blocks, b.sink_tiles = parts.sink_tiles, b.sink_rows = parts.sink_rows;
+    b.list = list, b.listed = parts.listed, b.slots = parts.more + parts.listed;
     b.scale = (float)shape->scale;
     b.scale_log2 = (float)(shape->scale * 1.4426950408889634);
     return q.d <= 64 ? run_backward<T, 64>(b, pq, pk, pv, pdout, dq, dk, dv, shape->dtype, sms, s)
@@ -2161,7 +2284,8 @@ extern "C" uint64_t a2sgd_window_attention_workspace(const a2sgd_attention *shap
     const int d = (int)shape->head_dim;
     uint64_t bytes = 0;
     if (shape->kv_heads == 0) return 0;
-    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += 2 * up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4) + kCounters + partial_bytes(shape);
+    if (flags & A2SGD_ATTENTION_BACKWARD) bytes += 2 * up256((uint64_t)q_planes * shape->q_heads * shape->q_rows * 4) + kCounters +
+                                                  (flags & A2SGD_ATTENTION_PACKED_Q ? partial_bytes(shape, true) : std::max(partial_bytes(shape, false), partial_bytes(shape, true)));
     else if (few(shape, flags & A2SGD_ATTENTION_PACKED_Q)) bytes += share_bytes(shape);
     if (!(flags & A2SGD_ATTENTION_ALIGNED))
         bytes += (flags & A2SGD_ATTENTION_BACKWARD ? 2 : 1) * room(q_planes, (int64_t)shape->q_rows, (int)shape->q_heads, d) +
