@@ -1106,9 +1106,9 @@ struct DeltaArgs {
     unsigned int *next; // two, cleared
     int blocks, heads, d, wide; // CTAs of a plane
     // packed queries whose first tokens' passes are cut into parts (see PartsList)
-    const int32_t *q_ranges;
+    const int32_t *q_ranges, *k_ranges;
     int *list;
-    int sequences, group, part_blocks, more, listed;
+    int sequences, k_rows, group, part_blocks, more, listed;
 };
 
 // ------------------------------------------------------------------ backward
@@ -1158,35 +1158,35 @@ struct BackwardShape {
 };
 
 // Sequences of packed queries whose first tokens' passes have more than one part, in order: their number, the sequences, and for each how many parts
-// beyond a first one the sequences before it have (and, last, all have).  Every query is in one sequence, so that the parts of all together are bound by
+// beyond a first one the sequences before it have (and, last, all have); and for the fold their queries, and their keys' first row and number.  Every query is in one sequence, so that the parts of all together are bound by
 // the rows (`more` beyond the first ones); a sequence beyond that bound, as overlapping ranges could have it, keeps one part.
 struct PartsList {
     const int *p;
-    int room; // sequences
-    __device__ __forceinline__ int count() const { return __ldcg(p); }
-    __device__ __forceinline__ int sequence(int m) const { return __ldcg(p + 1 + m); }
-    __device__ __forceinline__ int before(int m) const { return __ldcg(p + 1 + room + m); }
-    // The first of n numbers in order that is at least x.  The whole warp.
-    __device__ static __forceinline__ int search(const int *v, int n, int x)
+    int room; // sequences; read through L1: thousands of warps of the fold ask for the same few lines
+    __device__ __forceinline__ int count() const { return p[0]; }
+    __device__ __forceinline__ int sequence(int m) const { return p[1 + m]; }
+    __device__ __forceinline__ int before(int m) const { return p[1 + room + m]; }
+    struct Entry {
+        int m, seq, before, next; // m -1: there is none; next: `before` of the entry behind
+    };
+    // The first entry whose sequence is at least x, or (parts) the one that has the x-th of the parts beyond first ones.  The whole warp; what it reads
+    // is asked for at once.
+    __device__ __forceinline__ Entry find(int x, bool parts) const
     {
-        for (int i0 = 0; i0 < n; i0 += 32) {
-            const int i = i0 + (int)(threadIdx.x & 31);
-            const unsigned hit = __ballot_sync(0xffffffffu, i < n && __ldcg(v + i) >= x);
-            if (hit) return i0 + __ffs(hit) - 1;
+        const int n = count(), lane = threadIdx.x & 31;
+        for (int i0 = 0; i0 < room; i0 += 32) {
+            const int i = min(i0 + lane, room - 1), seq = sequence(i), first = before(i), next = before(i + 1);
+            if (i0 >= n) break;
+            const unsigned hit = __ballot_sync(0xffffffffu, i0 + lane < n && (parts ? next > x : seq >= x));
+            if (hit) {
+                const int who = __ffs(hit) - 1;
+                return {i0 + who, __shfl_sync(0xffffffffu, seq, who), __shfl_sync(0xffffffffu, first, who), __shfl_sync(0xffffffffu, next, who)};
+            }
         }
-        return n;
+        return {-1, -1, 0, 0};
     }
-    __device__ __forceinline__ int of_sequence(int seq) const // -1: not in the list
-    {
-        const int n = count(), m = search(p + 1, n, seq);
-        return m < n && sequence(m) == seq ? m : -1;
-    }
-    __device__ __forceinline__ int of_part(int x) const // x-th of the parts beyond first ones
-    {
-        const int n = count(), m = search(p + 2 + room, n, x + 1);
-        return m < n ? m : -1;
-    }
-    static uint64_t bytes(int64_t room) { return (uint64_t)(2 * room + 2) * 4; }
+    __device__ __forceinline__ int fact(int which, int m) const { return p[2 + (2 + which) * room + m]; } // queries, first key, keys
+    static uint64_t bytes(int64_t room) { return (uint64_t)(5 * room + 2) * 4; }
 };
 // Its making, by one CTA of 256 threads.
 __device__ __forceinline__ void list_parts(const DeltaArgs &a)
@@ -1219,6 +1219,9 @@ __device__ __forceinline__ void list_parts(const DeltaArgs &a)
             const int m = rank_before + rank - 1;
             a.list[1 + m] = b;
             a.list[2 + a.listed + m] = (int)(sum_before + sum);
+            const Range kr = range_of(a.k_ranges, b, a.k_rows);
+            int *fact = a.list + 2 + 2 * a.listed + m;
+            fact[0] = range_of(a.q_ranges, b, (int)a.rows).count, fact[a.listed] = kr.first, fact[2 * a.listed] = kr.count;
             atomicMax(&count, m + 1);
         }
         for (int w = 0; w < 8; ++w) sum_before += sums[w], rank_before += ranks[w];
@@ -1266,10 +1269,10 @@ __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, Backw
     if (KEYS && item < listed) {
         t.head = item % heads;
         tile = item / heads % a.sink_tiles;
-        const int x = item / heads / a.sink_tiles, m = list.of_part(x);
-        if (m < 0) return false;
-        const int before = list.before(m);
-        t.seq = list.sequence(m), t.part = 1 + x - before, t.parts = 1 + list.before(m + 1) - before, t.slot = before + m;
+        const int x = item / heads / a.sink_tiles;
+        const PartsList::Entry its = list.find(x, true);
+        if (its.m < 0) return false;
+        t.seq = its.seq, t.part = 1 + x - its.before, t.parts = 1 + its.next - its.before, t.slot = its.before + its.m;
     } else {
         item -= listed;
         const int each = a.tiles + (KEYS && !a.list ? a.extra : 0);
@@ -1288,9 +1291,11 @@ __device__ __forceinline__ bool find_tile(const BackwardArgs &a, int item, Backw
             if (KEYS ? a.packed_k : a.packed_q) locate(KEYS ? a.k_ranges : a.q_ranges, a.sequences, KEYS ? a.k_rows : a.q_rows, 128, tile, t.seq, tile);
             if (t.seq < 0) return false;
             if (KEYS && a.list) {
-                const int m = tile < a.sink_tiles ? list.of_sequence(t.seq) : -1;
                 t.parts = 1;
-                if (m >= 0) t.parts += list.before(m + 1) - list.before(m), t.slot = list.before(m) + m;
+                if (tile < a.sink_tiles) {
+                    const PartsList::Entry its = list.find(t.seq, false);
+                    if (its.seq == t.seq) t.parts += its.next - its.before, t.slot = its.before + its.m;
+                }
             }
         }
     }
@@ -1781,28 +1786,34 @@ __global__ void __launch_bounds__(256) k_fold_keys(const __grid_constant__ Backw
     wait_prior_grid();
     release_next_grid();
     constexpr int kPieces = 2 * (D / 32);
-    const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), item = warp / kPieces;
+    // 32 bits hold a key, a head and a sequence: each has a row of partial sums
+    const uint32_t warp = blockIdx.x * 8 + (threadIdx.x >> 5), item = warp / kPieces;
     const int piece = (int)(warp % kPieces), o = piece / (D / 32), c = piece % (D / 32) * 32 + (threadIdx.x & 31);
-    if (item >= (int64_t)(a.list ? a.listed : a.sequences) * a.kv_heads * a.sink_rows) return;
     const int key = (int)(item % a.sink_rows), lane = (int)(item / a.sink_rows), head = lane % a.kv_heads;
-    int seq = lane / a.kv_heads, slot = 0;
+    int seq = lane / a.kv_heads, slot = 0, q_count;
+    if (seq >= (a.list ? a.listed : a.sequences)) return;
+    Range kr;
     if (a.list) {
         const PartsList list{a.list, a.listed};
-        const int m = seq;
-        if (m >= list.count()) return;
+        const int m = seq, n = list.count();
         seq = list.sequence(m), slot = list.before(m) + m;
+        q_count = list.fact(0, m), kr = {list.fact(1, m), list.fact(2, m)};
+        if (m >= n) return;
+    } else {
+        q_count = range_of(a.q_ranges, seq, a.q_rows).count, kr = range_of(a.k_ranges, seq, a.k_rows);
     }
-    const Range qr = range_of(a.q_ranges, seq, a.q_rows), kr = range_of(a.k_ranges, seq, a.k_rows);
     if (key >= kr.count) return;
     int first;
-    const int all = query_blocks(key / 128 * 128, qr.count, kr.count, a.window, a.sinks, a.group, first);
+    const int all = query_blocks(key / 128 * 128, q_count, kr.count, a.window, a.sinks, a.group, first);
     const int parts = (all + a.part_blocks - 1) / a.part_blocks;
     if (parts == 0) return; // cleared where the tile was found
     const Heads &h = o ? a.out1 : a.out0;
     if (!h.p || c >= a.d) return;
+    const float *p = partial_row<D>(a, seq, slot, head, key, 0) + o * D + c;
+    const int64_t step = (a.list ? a.sink_rows : 1) * 2 * D;
     float sum = 0.0f;
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k) sum += partial_row<D>(a, seq, slot, head, key, k)[o * D + c];
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) sum += p[k * step];
     at<T>(h, seq, kr.first + key, head)[c] = from_f32<T>(sum);
 }
 
@@ -1814,7 +1825,10 @@ __global__ void __launch_bounds__(256) k_delta(const __grid_constant__ DeltaArgs
     wait_prior_grid();
     release_next_grid();
     if (blockIdx.x == 0 && threadIdx.x < 2) a.next[threadIdx.x] = 0;
-    if (blockIdx.x == 0 && a.list) list_parts(a);
+    if (a.list && blockIdx.x == gridDim.x - 1) { // a CTA for it alone
+        list_parts(a);
+        return;
+    }
     constexpr int kEach = 256 / LANES, kAhead = 4; // queries at a time, whose reads come before their sums
     const int lane = threadIdx.x % LANES, plane = blockIdx.x / a.blocks;
     const int64_t row0 = (int64_t)(blockIdx.x % a.blocks) * kDeltaRows;
@@ -2245,18 +2259,18 @@ int backward(const a2sgd_attention *shape, const Tensor &dout, const Tensor &q, 
         d.lse2 = lse2, d.delta = delta, d.next = b.next;
         d.rows = q.rows;
         const int64_t planes = packed_q ? 1 : (int64_t)shape->sequences, blocks = (q.rows + kDeltaRows - 1) / kDeltaRows;
-        if (planes * blocks > 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
+        if (planes * blocks >= 0x7fffffff) return A2SGD_ERR_TOO_LARGE;
         d.blocks = (int)blocks;
         d.heads = q.heads, d.d = q.d;
         d.wide = wide(o) && wide(dout);
         if (dk.h.p || dv.h.p) {
-            d.list = list, d.q_ranges = shape->q_ranges;
-            d.sequences = (int)shape->sequences, d.group = q.heads / k.heads;
+            d.list = list, d.q_ranges = shape->q_ranges, d.k_ranges = shape->k_ranges;
+            d.sequences = (int)shape->sequences, d.k_rows = (int)k.rows, d.group = q.heads / k.heads;
             d.part_blocks = parts.blocks, d.more = parts.more, d.listed = parts.listed;
         }
         void *params[] = {&d};
         const void *fn = q.d <= 64 ? reinterpret_cast<const void *>(&k_delta<T, 8>) : reinterpret_cast<const void *>(&k_delta<T, 16>);
-        A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(planes * blocks)), 256, 0, params, s));
+        A2_TRAIN_CUDA(launch(fn, dim3((unsigned)(planes * blocks) + (d.list != nullptr)), 256, 0, params, s));
     } else {
         A2_TRAIN_CUDA(cudaMemsetAsync(b.next, 0, kCounters, s));
     }
