@@ -514,8 +514,8 @@ int a2sgd_gated_ffn_status(int device, int *device_status, void *stream);
  * The conventions above hold.
  *
  * A tensor of heads: element c of head h in row t of sequence b is at p[b sequence_stride + t row_stride + h head_stride + c],
- * strides in ELEMENTS.  Packed sequences share one plane: sequence_stride 0, and ranges say which rows are whose; what is written (o, dq like
- * q; dk, dv like k) is then packed, too, and else it is not.  Without ranges sequence_stride 0 says that all sequences read the same plane. */
+ * strides in ELEMENTS.  Packed sequences share one plane: sequence_stride 0, and ranges say which rows are whose; what belongs to it (o, dout,
+ * dq to q; dk, dv to k) is then packed, too, and what is written is not else.  Without ranges sequence_stride 0 says that all sequences read the same plane. */
 typedef struct a2sgd_heads {
     void *p;
     int64_t sequence_stride, row_stride, head_stride;

@@ -2335,8 +2335,11 @@ extern "C" int a2sgd_window_attention_backward(const a2sgd_attention *shape, con
 {
     int rc = check_shape(shape);
     if (rc != A2SGD_OK || shape->sequences == 0) return rc;
-    for (const a2sgd_heads *h : {dout, q, o})
+    for (const a2sgd_heads *h : {q, dout, o}) {
         if ((rc = check_heads(shape, h, shape->q_heads, shape->q_rows, shape->q_ranges, true, nullptr)) != A2SGD_OK) return rc;
+        // what belongs to packed queries lies as they do
+        if (shape->sequences > 1 && shape->q_ranges && shape->q_rows && q->sequence_stride == 0 && h->sequence_stride != 0) return A2SGD_ERR_ARG;
+    }
     for (const a2sgd_heads *h : {k, v})
         if ((rc = check_heads(shape, h, shape->kv_heads, shape->k_rows, shape->k_ranges, true, nullptr)) != A2SGD_OK) return rc;
     for (const a2sgd_heads *h : {dk, dv})

@@ -1,0 +1,20 @@
+"""More of what the attention's and the residual connection's entry points refuse, through the C ABI, before anything is launched: no GPU is needed."""
+import math
+
+import pytest
+
+from paper_2006_07405_b200 import binding as B
+from test_block_operators_refusals import FAKE, at, heads, shape
+
+
+def backward(s, dout=None, q=None, k=None, v=None, o=None, dq=None, dk=None, dv=None):
+    t = heads()
+    first, rest = [dout or t, q or t, k or t, v or t, o or t], [dq, dk, dv]
+    return B.lib().a2sgd_window_attention_backward(at(s), *(at(x) for x in first), FAKE, *(at(x) for x in rest), FAKE, 1 << 30, 0, None)
+
+
+def test_packed_queries_with_gradients_or_outputs_that_are_not():
+    packed, s = heads(seq=0), shape(q_ranges=FAKE)
+    assert backward(s, q=packed, dq=packed, o=packed) == B.ERR_ARG                      # dout has a plane for each sequence
+    assert backward(s, q=packed, dq=packed, dout=packed) == B.ERR_ARG                   # o has
+    assert backward(s, q=packed, dk=heads(), o=packed) == B.ERR_ARG
