@@ -534,7 +534,7 @@ typedef struct a2sgd_heads {
  *               its own plane.  Rows outside are neither read into a result nor written; what they hold does not matter.  Ranges of
  *               different sequences in one plane must not overlap where they are written, and are clipped to the plane.
  *   window      at least 1; 2^31 and more: every key up to the query's own place
- *   scale       finite, > 0;   dtype  A2SGD_BF16 or A2SGD_F16
+ *   scale       finite, > 0, and so in fp32, and times log2 e;   dtype  A2SGD_BF16 or A2SGD_F16
  *   lse         fp32 [sequences][q_heads][q_rows] (packed: [q_heads][q_rows]), out, for the backward pass; may be NULL
  * Tensors whose address is a multiple of 16 bytes and whose strides are multiples of 8 elements are read where they are; others are
  * first copied to the workspace.  What is not finite reaches what sees it only, in the backward pass, too: a query that sees a value that is

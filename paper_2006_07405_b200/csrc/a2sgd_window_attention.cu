@@ -1906,7 +1906,9 @@ int check_shape(const a2sgd_attention *s)
 {
     if (!s || (s->dtype != A2SGD_BF16 && s->dtype != A2SGD_F16)) return A2SGD_ERR_ARG;
     if (s->kv_heads == 0 || s->q_heads == 0 || s->q_heads % s->kv_heads || s->head_dim == 0) return A2SGD_ERR_ARG;
-    if (s->window == 0 || !std::isfinite(s->scale) || !(s->scale > 0.0)) return A2SGD_ERR_ARG;
+    // as the kernels have it: 0 times a hidden score's -infinity, or infinity times a score of 0, is not a number
+    const float scale = (float)s->scale, scale_log2 = (float)(s->scale * 1.4426950408889634);
+    if (s->window == 0 || !(scale > 0.0f) || !(scale_log2 > 0.0f) || !std::isfinite(scale_log2)) return A2SGD_ERR_ARG;
     if (s->head_dim > A2SGD_ATTENTION_MAX_HEAD_DIM || s->q_heads > 65535u || s->sequences > 65535u || s->q_rows >= (1ull << 30) ||
         s->k_rows >= (1ull << 30))
         return A2SGD_ERR_TOO_LARGE;

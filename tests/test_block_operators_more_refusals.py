@@ -18,3 +18,11 @@ def test_packed_queries_with_gradients_or_outputs_that_are_not():
     assert backward(s, q=packed, dq=packed, o=packed) == B.ERR_ARG                      # dout has a plane for each sequence
     assert backward(s, q=packed, dq=packed, dout=packed) == B.ERR_ARG                   # o has
     assert backward(s, q=packed, dk=heads(), o=packed) == B.ERR_ARG
+
+
+@pytest.mark.parametrize("scale", [1e-46, 5e-324, 2.5e38, 3.5e38, 1e308])
+def test_scales_that_fp32_does_not_hold(scale):
+    """In fp32, and times log2 e in fp32, a scale is neither 0 nor infinite."""
+    t, s = heads(), shape(scale=scale)
+    assert B.lib().a2sgd_window_attention_forward(at(s), at(t), at(t), at(t), at(t), None, None, 0, 0, None) == B.ERR_ARG
+    assert backward(s, dq=t, dk=t, dv=t) == B.ERR_ARG
