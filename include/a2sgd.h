@@ -604,6 +604,7 @@ int a2sgd_rotary(const a2sgd_heads *q, const a2sgd_heads *k, const a2sgd_heads *
  *   y, u        [rows] rows of `dtype`, stride in ELEMENTS (>= d);   x, z  the same of residual_dtype (A2SGD_F32, or dtype)
  *   gate        [ceil(rows / gate_rows)][d], contiguous, or NULL;  gate_rows >= 1 with a gate
  *   weights, biases  [d] or NULL (1 and 0), and gate: of param_dtype (A2SGD_F32, or dtype)
+ *   alpha, eps  finite in fp32; eps >= 0
  *   post_mean, post_rstd, pre_mean, pre_rstd  out, fp32 [rows], for the backward pass; each may be NULL
  *   d           up to A2SGD_RESIDUAL_MAX_COLUMNS;   z may be x, u may be y (where the types agree, with the same stride) */
 #define A2SGD_RESIDUAL_MAX_COLUMNS 8192

@@ -609,7 +609,7 @@ size_t smem_of(const Plan &p, bool backward)
 int check_shape(const a2sgd_residual *s)
 {
     if (!s || !known(s->dtype) || (s->residual_dtype != A2SGD_F32 && s->residual_dtype != s->dtype) ||
-        (s->param_dtype != A2SGD_F32 && s->param_dtype != s->dtype) || s->d == 0 || (s->flags & ~3u) || !std::isfinite(s->alpha) ||
+        (s->param_dtype != A2SGD_F32 && s->param_dtype != s->dtype) || s->d == 0 || (s->flags & ~3u) || !std::isfinite((float)s->alpha) ||
         (s->gate && s->gate_rows == 0))
         return A2SGD_ERR_ARG;
     if (s->d > A2SGD_RESIDUAL_MAX_COLUMNS || s->rows >= (1ull << 40) || s->gate_rows >= (1ull << 62)) return A2SGD_ERR_TOO_LARGE;
@@ -659,7 +659,7 @@ extern "C" int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2
 {
     int rc = check_shape(shape);
     if (rc != A2SGD_OK) return rc;
-    if (!std::isfinite(shape->eps) || shape->eps < 0.0) return A2SGD_ERR_ARG;
+    if (!std::isfinite((float)shape->eps) || shape->eps < 0.0) return A2SGD_ERR_ARG;
     if (shape->rows == 0) return A2SGD_OK;
     const int t = shape->dtype, r = shape->residual_dtype;
     if ((rc = check_rows(x, shape, r, true)) != A2SGD_OK || (rc = check_rows(y, shape, t, true)) != A2SGD_OK ||

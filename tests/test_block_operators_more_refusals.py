@@ -4,7 +4,7 @@ import math
 import pytest
 
 from paper_2006_07405_b200 import binding as B
-from test_block_operators_refusals import FAKE, at, heads, shape
+from test_block_operators_refusals import FAKE, at, heads, residual, rows, shape
 
 
 def backward(s, dout=None, q=None, k=None, v=None, o=None, dq=None, dk=None, dv=None):
@@ -26,3 +26,11 @@ def test_scales_that_fp32_does_not_hold(scale):
     t, s = heads(), shape(scale=scale)
     assert B.lib().a2sgd_window_attention_forward(at(s), at(t), at(t), at(t), at(t), None, None, 0, 0, None) == B.ERR_ARG
     assert backward(s, dq=t, dk=t, dv=t) == B.ERR_ARG
+
+
+@pytest.mark.parametrize("bad", [dict(alpha=1e39), dict(alpha=-1e300), dict(eps=1e39), dict(alpha=math.inf)])
+def test_factors_that_fp32_does_not_hold(bad):
+    r, s = rows(), residual(pre_rstd=FAKE, **bad)
+    assert B.lib().a2sgd_residual_norm_forward(at(s), at(r), at(r), at(r), at(r), 0, None) == B.ERR_ARG
+    if "alpha" in bad:      # eps is not read by the backward pass
+        assert B.lib().a2sgd_residual_norm_backward(at(s), at(r), at(r), at(r), at(r), at(r), at(r), None, FAKE, 1 << 30, 0, None) == B.ERR_ARG
