@@ -54,7 +54,7 @@ __device__ __forceinline__ float lse_from(float ref, float sum) { return sum > 0
 // values, warp 5 issues S = Q K^T, warp 6 O += P V, warps 0 to 3 hold the softmax, a thread a query.
 //   S goes into TMEM;  a thread reads its row, forms P and writes it over S in 16 bits;  P is read from TMEM by its product with V.
 // Three buffers of S (two where O has 128 columns): the next block's, be it the next tile's, is formed while the present one's P is.
-// P is taken about a reference that is moved, and O and the sum with it, only where P would grow beyond 2^13: nearly no
+// P is taken about a reference that is moved, and O and the sum with it, only where P would grow beyond a limit (Probabilities): nearly no
 // block touches O, and blocks without a mask need no maximum.
 //
 // Bound, for heads of 64, by the softmax' warps: 16 exponentials a clock and SM are 164 us of 8 x 4096 queries, 25 heads of 64, window 1024 (737 M
@@ -280,6 +280,19 @@ __device__ __forceinline__ void store_row(T *p, const float *v, int count, int b
             if (i < count) p[i] = from_f32<T>(v[i]);
     }
 }
+
+// The powers of 2 between which P is held: a reference is put so that its row's largest P is 2^(kFirst - 1) to 2^kFirst, and moved when one is above
+// 2^kMost, or the sum over a block of 64 without a mask above 2^kSum (kMost + 6 at least, so that a block of equal scores does not ask for what does not
+// come).  bfloat16 has fp32's range.  float16 loses what is below 2^-25, while the row's sum keeps it: P is lifted, so that this is 2^-31 of the
+// largest, and 2^17 far keys take no more than 2^-14 from an output.  (Few queries: the maximum is known in every run of keys.)
+template <typename T>
+struct Probabilities {
+    static constexpr float kFirst = 0.0f, kMost = 8.0f, kSum = 8192.0f, kMostFew = 8.0f;
+};
+template <>
+struct Probabilities<__half> {
+    static constexpr float kFirst = 7.0f, kMost = 9.0f, kSum = 32768.0f, kMostFew = 15.0f;
+};
 
 template <typename T>
 __host__ __device__ constexpr uint32_t type_bits() { return std::is_same<T, __nv_bfloat16>::value ? 1u : 0u; }
@@ -629,7 +642,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                 fence_after();
                 bool done = false;
                 if (inside && ready) {
-                    // No maximum is taken: a sum of more than 2^13 says that the row has risen too far above its reference.
+                    // No maximum is taken: too large a sum says that the row has risen too far above its reference.
                     uint32_t p[32];
                     float x[32], y[32];
                     tmem_ld32(ts, x);
@@ -637,7 +650,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                     tmem_wait_ld();
                     const float sum = exponentials<T>(x, c, -ref, reinterpret_cast<uint32_t(&)[16]>(p[0])) +
                                       exponentials<T>(y, c, -ref, reinterpret_cast<uint32_t(&)[16]>(p[16]));
-                    done = !__any_sync(0xffffffffu, live && sum > 8192.0f);
+                    done = !__any_sync(0xffffffffu, live && sum > Probabilities<T>::kSum);
                     if (done) {
                         tmem_st32(ts, p);
                         total += sum;
@@ -655,7 +668,7 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
                         hide(x, seen_by(k0 + e));
                         top = fmaxf(top, most_of<32>(x));
                     }
-                    const float next = live && top * c > ref + 8.0f ? ceilf(top * c) : ref;
+                    const float next = live && top * c > ref + Probabilities<T>::kMost ? ceilf(top * c) - Probabilities<T>::kFirst : ref;
                     const bool moves = next > ref;
                     if (__any_sync(0xffffffffu, moves)) {
                         const float shrink = moves ? exp2_approx(ref - next) : 1.0f; // 0 from -infinity
@@ -936,9 +949,10 @@ __global__ void __launch_bounds__(32 * FewShape<D>::kWarps) k_few(const __grid_c
             top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
             top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2)) * cl;
             shrink[h] = 1.0f;
-            if (top[h] > ref[h] + 8.0f) { // from -infinity, too
-                shrink[h] = exp2_approx(ref[h] - top[h]);
-                ref[h] = top[h];
+            if (top[h] > ref[h] + Probabilities<T>::kMostFew) { // from -infinity, too
+                const float next = top[h] - Probabilities<T>::kFirst;
+                shrink[h] = exp2_approx(ref[h] - next);
+                ref[h] = next;
                 moves = true;
             }
         }
