@@ -630,6 +630,8 @@ int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2sgd_rows *x
  *     back(g; a) = rstd (g - mean_c(g) - hat mean_c(g hat)),  hat = norm(a);  RMS: without mean_c(g)
  *     dpre_weight = sum du norm(z),  dpre_bias = sum du,  dpost_weight = sum dn norm(y),  dpost_bias = sum dn,
  *     dgate = sum over its rows of alpha t n
+ * Sums: fp32 in chains of at most 512 terms (rows, then sums of 512 rows, then CTAs').  Each gate costs a CTA's sums a way to memory: gates of
+ * few rows are slow.
  * dx may be dz, dy may be du or y (where the types agree, with the same stride).  dx.p and dy.p may be NULL, and so may each of the sums, which are of param_dtype
  * and are zero when there are no rows.  shape->pre_bias and eps are not read.
  *   workspace   DEVICE, 256-byte aligned, a2sgd_residual_norm_workspace bytes (needed for any of the sums) */

@@ -9,7 +9,8 @@
 // the warps' are joined from shared memory (Chan's formula), so that no element is squared about anything but a mean near its own.
 //
 // The columns' sums: t hat1 and t (from which the gate's, the post weight's and the post bias' gradients follow, a gate at a time), du hat2
-// and du.  A CTA adds its rows up in registers or shared memory, leaves one partial sum a column, and a second kernel adds the CTAs' in order.
+// and du.  A CTA adds its rows up in registers or shared memory, leaves one partial sum a column, and a second kernel adds the CTAs' in order.  No chain
+// of additions has more than 512 terms: after 512 rows, or at a gate's end, a sum goes to memory, after 512 of those to the next place.
 //
 // Statistics, sums and z before its rounding are fp32; z and u (dx and dy) are rounded once, as they are written.
 //
@@ -31,6 +32,7 @@ namespace {
 constexpr int kMostThreads = 512;
 constexpr int kSums = 4; // t hat1, t, du hat2, du
 constexpr int kStrips = 32;
+constexpr int kRun = 512; // terms of a running sum (7812 equal terms in one chain were off by 1.2e-4 of their sum)
 
 struct Rows {
     void *p;
@@ -46,6 +48,7 @@ struct Args {
     // backward
     void *dw1, *db1, *dgate, *dw2, *db2;
     float *partials;      // [CTAs][4][d]: dw1, db1, dw2, db2
+    float *runs;          // [CTAs][4][d]: up to kRun terms of those each; NULL where every CTA puts its sums down but once
     float *gate_partials; // [CTAs][2][d]
     int ctas;
 };
@@ -377,8 +380,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
     bring_stats(row0);
     bring_pre(row0);
     bring_post(row0);
-    bool flushed = false; // this CTA's partial sums hold earlier gates' rows
     int64_t gate_end = row0, group = 0; // rows from here on have another gate
+    int since = 0, puts = 0; // rows since the sums were last put down, and how often they were
     const float per = 1.0f / (float)a.d;
     for (int64_t r = row0; r < end; ++r) {
         const float mean1 = next_mean1, rstd1 = next_rstd1, mean2 = next_mean2, rstd2 = next_rstd2;
@@ -479,18 +482,26 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
                 Eight<T, VEC>::store(static_cast<T *>(a.dy.p) + r * a.dy.ld, k, a.d, f);
             }
         }
-        // a gate's last row in this CTA: what its rows give to the gate, the post weight and the post bias
-        const bool last = r + 1 == end;
-        if (want && r + 1 == gate_end) {
+        // what the rows since the last time give to the gate, the post weight and the post bias, and to the pre weight and bias
+        if (want && (++since == kRun || r + 1 == gate_end)) {
+            const bool last = r + 1 == end, gate_over = r + 1 == gate_end, begun = r + 1 - max(row0, group * a.gate_rows) > since; // some of the gate's rows have been
             const bool whole = a.gate && group * a.gate_rows >= row0 && min(a.rows, (group + 1) * a.gate_rows) <= end;
-            const int slot = a.gate && group != row0 / a.gate_rows;
-            float *mine = a.partials + (int64_t)blockIdx.x * kSums * a.d;
+            const int slot = a.gate && group != row0 / a.gate_rows, place = puts % kRun;
+            const int64_t mine = (int64_t)blockIdx.x * kSums * a.d;
+            const auto put = [&](int s, int c, float v) {
+                float *sum = a.partials + mine + s * a.d + c, *run = a.runs + mine + s * a.d + c;
+                if (place) v += *run;
+                if (last || place == kRun - 1) *sum = puts >= kRun ? *sum + v : v;
+                else *run = v;
+            };
             float mine4[kSums][8];
             if constexpr (C == 1) {
 #pragma unroll
-                for (int q = 0; q < kSums; ++q) singles8(mine4[q], acc[q]);
+                for (int q = 0; q < kSums; ++q) {
+                    singles8(mine4[q], acc[q]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[0][i] = acc[1][i] = pair(0.0f);
+                    for (int i = 0; i < 4; ++i) acc[q][i] = pair(0.0f);
+                }
             }
 #pragma unroll 1
             for (int k = 0; k < C; ++k) {
@@ -498,25 +509,29 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
                 for (int i = 0; i < 8; ++i) {
                     const int c = column<VEC>(k, i);
                     if (c >= a.d) continue;
-                    float one_hat, one;
-                    if constexpr (C == 1) one_hat = mine4[0][i], one = mine4[1][i];
-                    else one_hat = sum_at(0, k, i), one = sum_at(1, k, i), sum_at(0, k, i) = sum_at(1, k, i) = 0.0f;
+                    const auto take = [&](int q) {
+                        if constexpr (C == 1) return mine4[q][i];
+                        const float v = sum_at(q, k, i);
+                        sum_at(q, k, i) = 0.0f;
+                        return v;
+                    };
+                    const float one_hat = take(0), one = take(1);
                     if (a.dgate) {
                         const float w1 = a.post && a.w1 ? param_at(a.w1, a.param, c) : 1.0f, b1 = a.post && a.b1 ? param_at(a.b1, a.param, c) : 0.0f;
-                        const float v = a.alpha * fmaf(w1, one_hat, b1 * one);
-                        if (whole) param_put(a.dgate, a.param, group * a.d + c, v);
-                        else a.gate_partials[((int64_t)blockIdx.x * 2 + slot) * a.d + c] = v;
+                        float *part = a.gate_partials + ((int64_t)blockIdx.x * 2 + slot) * a.d + c, v = a.alpha * fmaf(w1, one_hat, b1 * one);
+                        if (begun) v += *part;
+                        if (whole && gate_over) param_put(a.dgate, a.param, group * a.d + c, v);
+                        else *part = v; // a whole gate's place is free: a first gate that has rows before this CTA, or a last one behind it, is another
                     }
                     const float f = a.gate ? a.alpha * param_at(a.gate, a.param, group * a.d + c) : a.alpha;
-                    mine[c] = (flushed ? mine[c] : 0.0f) + f * one_hat;
-                    mine[a.d + c] = (flushed ? mine[a.d + c] : 0.0f) + f * one;
-                    if (last) {
-                        if constexpr (C == 1) mine[2 * a.d + c] = mine4[2][i], mine[3 * a.d + c] = mine4[3][i];
-                        else mine[2 * a.d + c] = sum_at(2, k, i), mine[3 * a.d + c] = sum_at(3, k, i);
-                    }
+                    put(0, c, f * one_hat);
+                    put(1, c, f * one);
+                    put(2, c, take(2));
+                    put(3, c, take(3));
                 }
             }
-            flushed = true;
+            since = 0;
+            ++puts;
         }
     }
 }
@@ -649,8 +664,14 @@ Args common(const a2sgd_residual *s)
 }
 
 constexpr int kMostCtas = 1024; // that leave partial sums
-inline uint64_t sums_bytes(int64_t ctas, uint32_t d, bool gate) { return (uint64_t)ctas * (kSums + (gate ? 2 : 0)) * d * 4; }
 int64_t most_ctas(uint64_t rows) { return (int64_t)std::min<uint64_t>(rows, kMostCtas); }
+// Whether a CTA may put its sums down more than once: with several gates, or where rows are many on any number of CTAs from one an SM on.
+bool several_puts(uint64_t rows, uint64_t gate_rows, int device)
+{
+    const int sms = sm_count(device);
+    return (gate_rows && gate_rows < rows) || sms < 1 || rows > (uint64_t)std::min(sms, kMostCtas) * kRun;
+}
+inline uint64_t sums_bytes(int64_t ctas, uint32_t d, bool several, bool gate) { return (uint64_t)ctas * ((several ? 2 : 1) * kSums + (gate ? 2 : 0)) * d * 4; }
 
 } // namespace
 
@@ -683,8 +704,7 @@ extern "C" int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2
 
 extern "C" uint64_t a2sgd_residual_norm_workspace(uint64_t rows, uint32_t d, uint64_t gate_rows, int device)
 {
-    (void)device;
-    return sums_bytes(most_ctas(rows), d, gate_rows != 0);
+    return sums_bytes(most_ctas(rows), d, several_puts(rows, gate_rows, device), gate_rows != 0);
 }
 
 extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a2sgd_rows *dz, const a2sgd_rows *du, const a2sgd_rows *y,
@@ -737,8 +757,11 @@ extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a
     a.run = (a.rows + most - 1) / most;
     a.ctas = (int)((a.rows + a.run - 1) / a.run);
     if (want) {
+        const int64_t each = (int64_t)a.ctas * kSums * a.d;
+        const bool several = several_puts(shape->rows, shape->gate ? shape->gate_rows : 0, device);
         a.partials = static_cast<float *>(workspace);
-        a.gate_partials = a.partials + (int64_t)a.ctas * kSums * a.d;
+        a.runs = several ? a.partials + each : nullptr;
+        a.gate_partials = a.partials + (several ? 2 : 1) * each;
     }
     void *params[] = {&a};
     A2_TRAIN_CUDA(launch(fn, dim3((unsigned)a.ctas), (unsigned)p.threads, smem, params, s));
