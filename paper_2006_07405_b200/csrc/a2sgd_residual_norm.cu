@@ -664,7 +664,24 @@ Args common(const a2sgd_residual *s)
 }
 
 constexpr int kMostCtas = 1024; // that leave partial sums
-int64_t most_ctas(uint64_t rows) { return (int64_t)std::min<uint64_t>(rows, kMostCtas); }
+// CTAs of the backward pass on a device, by the kernel that fits it most often; without a device, all that may be.
+int64_t most_ctas(uint64_t rows, uint32_t d, int device)
+{
+    DeviceGuard guard(device);
+    const int sms = guard.ok ? sm_count(device) : 0;
+    if (sms < 1 || d == 0 || d > A2SGD_RESIDUAL_MAX_COLUMNS) return std::min<int64_t>((int64_t)rows, kMostCtas);
+    int most = 1;
+    for (int dtype : {A2SGD_F32, A2SGD_BF16, A2SGD_F16})
+        for (int residual : {(int)A2SGD_F32, dtype})
+            for (bool vec : {false, true}) {
+                const Plan p = plan_of(d, vec);
+                const void *fn = pick_types(dtype, residual, p, true);
+                const size_t smem = smem_of(p, true);
+                if (allow_smem(fn, smem) != cudaSuccess) (void)cudaGetLastError();
+                most = std::max(most, resident_ctas(fn, (unsigned)p.threads, smem, device));
+            }
+    return std::min<int64_t>((int64_t)rows, std::min<int64_t>((int64_t)sms * most, kMostCtas));
+}
 // Whether a CTA may put its sums down more than once: with several gates, or where rows are many on any number of CTAs from one an SM on.
 bool several_puts(uint64_t rows, uint64_t gate_rows, int device)
 {
@@ -704,7 +721,7 @@ extern "C" int a2sgd_residual_norm_forward(const a2sgd_residual *shape, const a2
 
 extern "C" uint64_t a2sgd_residual_norm_workspace(uint64_t rows, uint32_t d, uint64_t gate_rows, int device)
 {
-    return sums_bytes(most_ctas(rows), d, several_puts(rows, gate_rows, device), gate_rows != 0);
+    return sums_bytes(most_ctas(rows, d, device), d, several_puts(rows, gate_rows, device), gate_rows != 0);
 }
 
 extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a2sgd_rows *dz, const a2sgd_rows *du, const a2sgd_rows *y,

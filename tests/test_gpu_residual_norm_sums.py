@@ -82,3 +82,14 @@ def test_one_norm_a_row_with_the_sums_again_and_again(kind, d):
     # fp32: a term's own roundings and at most 512 + 600 additions
     assert ((out[2].double() - terms.sum(0)).abs() <= (1112 + 8) * U * (du.double().abs() * (hat.abs() + (mean.double().abs() * rstd.double())[:, None])).sum(0)).all()
     assert ((out[3].double() - du.double().sum(0)).abs() <= 1112 * U * du.double().abs().sum(0)).all()
+
+
+@pytest.mark.parametrize("d, ctas", [(8192, 1), (5000, 2), (2048, 4)])
+def test_room_is_what_the_device_uses(d, ctas):
+    """Four sums and, with a gate, two more of each CTA; a CTA an SM at d = 8192 (196 KB of shared memory each), few at other widths.  Several gates, or many
+    rows: four sums more."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert B.a2sgd_residual_norm_workspace(65536, d) <= sms * ctas * 4 * d * 4
+    assert B.a2sgd_residual_norm_workspace(65536, d, 1000) <= sms * ctas * 10 * d * 4
+    assert B.a2sgd_residual_norm_workspace(1 << 24, d) <= sms * ctas * 8 * d * 4
+    assert B.a2sgd_residual_norm_workspace(3, d) == 3 * 4 * d * 4 and B.a2sgd_residual_norm_workspace(0, d) == 0
