@@ -1949,24 +1949,6 @@ Heads heads_of(const a2sgd_heads *h)
     return h && h->p ? Heads{h->p, h->sequence_stride, h->row_stride, h->head_stride} : Heads{nullptr, 0, 0, 0};
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled()
-{
-    static const EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
 // A tensor of heads with its extents; planes: 1 where all sequences lie in one, or read the same.
 struct Tensor {
     Heads h;
