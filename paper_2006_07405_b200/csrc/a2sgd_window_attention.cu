@@ -239,18 +239,29 @@ struct Marred {
         if (n < kMarred) block[n] = b, rows[n] = r;
     }
 };
-// Column c of an output, as this thread wrote it, and those of the rows that it sees: what is not finite there is not finite here.  As a product with
-// 0 < P: plus itself; with dS, whose sign may be any: not a number.  of(x): row x of the block's, or NULL where it is not seen.
-template <bool SIGNED, typename T, typename Row>
-__device__ __forceinline__ void add_not_finite(float &out, uint64_t rows, int c, const Row &of)
+// Columns first to last (first a multiple of 8) of an output that this thread wrote, and of a row that it sees, in a tensor that TMA can read: what is not
+// finite there is not finite here.  As a product with 0 < P: plus itself; with dS, whose sign may be any: not a number.  Returns whether no column
+// is a number any more.
+template <bool SIGNED, typename T, typename O>
+__device__ __forceinline__ bool add_not_finite(O *out, const T *row, int first, int last)
 {
-    while (rows && out == out) {
-        const int x = __ffsll((long long)rows) - 1;
-        rows &= rows - 1;
-        const T *row = of(x);
-        const float v = row ? to_f32(row[c]) : 0.0f;
-        if (!isfinite(v)) out = SIGNED ? out + v : NAN;
+    bool none = true;
+    for (int c = first; c < last; c += 8) {
+        if (c + 8 <= last) {
+            uint32_t top = 0;
+            add_size(top, *reinterpret_cast<const uint4 *>(row + c));
+            if (!not_finite<T>(top)) {
+                none = false;
+                continue;
+            }
+        }
+        for (int i = c; i < min(c + 8, last); ++i) {
+            const float v = to_f32(row[i]), sum = isfinite(v) ? 0.0f : SIGNED ? to_f32(out[i]) + v : NAN;
+            if (!isfinite(v)) out[i] = from_f32<O>(sum);
+            none = none && sum != sum;
+        }
     }
+    return none;
 }
 
 // Up to 32 elements of a row: 32 or 16 bytes at a time (a thread's own sectors: 16-byte stores half fill them), or one element.
@@ -378,17 +389,14 @@ __device__ __noinline__ void mend_row(T *out, const ForwardArgs &a, const Tile &
 {
     const T *values = at<T>(a.values, tile.seq, tile.k_row, tile.head / a.group);
     const bool listed = marred.count <= kMarred;
-    for (int c = 0; c < a.d; ++c) {
-        float f = to_f32(out[c]);
-        for (int i = 0; i < (listed ? marred.count : tile.blocks.count) && f == f; ++i) {
-            const int k0 = tile.blocks[listed ? marred.block[i] : i] * kBlock;
-            if (tile.all_seen(k0, a.window, a.sinks)) continue;
-            add_not_finite<true, T>(f, listed ? marred.rows[i] : ~0ull, c, [&](int x) {
-                const int key = k0 + x;
-                return key <= place && (key > place - a.window || key < a.sinks) ? values + (int64_t)key * a.values.row : nullptr;
-            });
+    for (int i = 0; i < (listed ? marred.count : tile.blocks.count); ++i) {
+        const int k0 = tile.blocks[listed ? marred.block[i] : i] * kBlock;
+        if (tile.all_seen(k0, a.window, a.sinks)) continue;
+        for (uint64_t rows = listed ? marred.rows[i] : ~0ull; rows; rows &= rows - 1) {
+            const int key = k0 + __ffsll((long long)rows) - 1;
+            if (!(key <= place && (key > place - a.window || key < a.sinks))) continue;
+            if (add_not_finite<true>(out, values + (int64_t)key * a.values.row, 0, a.d)) return;
         }
-        if (!isfinite(f)) out[c] = from_f32<T>(f);
     }
 }
 
@@ -1352,24 +1360,22 @@ __device__ __noinline__ void mend_row(const BackwardArgs &a, const BackwardTile 
     float *sums = partial ? partial_row<D>(a, tile.seq, tile.slot, tile.head, place, tile.part) + D : nullptr;
     T *out = partial ? nullptr : at<T>(KEYS ? a.out1 : a.out0, tile.seq, tile.row + row, tile.head);
     const bool listed = marred.count <= kMarred;
-    for (int c0 = columns; c0 < a.d; c0 += step)
-        for (int c = c0; c < min(c0 + 32, a.d); ++c) {
-            float f = partial ? sums[c] : to_f32(out[c]);
-            for (int i = 0; i < (listed ? marred.count : tile.count) && f == f; ++i) {
-                const int n = listed ? marred.block[i] : i, at_block = tile.begin + n, o0 = KEYS ? tile.first + at_block / a.group * 64 : tile.blocks[n] * kBlock;
-                if (tile.template all_seen<KEYS>(o0, a.window, a.sinks)) continue;
-                const int head = KEYS ? tile.head * a.group + at_block % a.group : tile.head / a.group;
-                const T *passing = at<T>(a.passing, tile.seq, KEYS ? tile.q_row : tile.k_row, head);
-                add_not_finite<KEYS, T>(f, listed ? marred.rows[i] : ~0ull, c, [&](int x) {
-                    const int o = o0 + x, q_place = KEYS ? o + ahead : place, key = KEYS ? place : o;
-                    return o < (KEYS ? tile.q_count : tile.k_count) && key <= q_place && (key > q_place - a.window || key < a.sinks) ? passing + (int64_t)o * a.passing.row
-                                                                                                                                     : nullptr;
-                });
+    for (int i = 0; i < (listed ? marred.count : tile.count); ++i) {
+        const int n = listed ? marred.block[i] : i, at_block = tile.begin + n, o0 = KEYS ? tile.first + at_block / a.group * 64 : tile.blocks[n] * kBlock;
+        if (tile.template all_seen<KEYS>(o0, a.window, a.sinks)) continue;
+        const int head = KEYS ? tile.head * a.group + at_block % a.group : tile.head / a.group, end = KEYS ? tile.q_count : tile.k_count;
+        const T *passing = at<T>(a.passing, tile.seq, KEYS ? tile.q_row : tile.k_row, head);
+        for (uint64_t rows = listed ? marred.rows[i] : ~0ull; rows; rows &= rows - 1) {
+            const int o = o0 + __ffsll((long long)rows) - 1, q_place = KEYS ? o + ahead : place, key = KEYS ? place : o;
+            if (!(o < end && key <= q_place && (key > q_place - a.window || key < a.sinks))) continue;
+            bool none = true;
+            for (int c = columns; c < a.d; c += step) {
+                const T *from = passing + (int64_t)o * a.passing.row;
+                none = (partial ? add_not_finite<KEYS>(sums, from, c, min(c + 32, a.d)) : add_not_finite<KEYS>(out, from, c, min(c + 32, a.d))) && none;
             }
-            if (isfinite(f)) continue;
-            if (partial) sums[c] = f;
-            else out[c] = from_f32<T>(f);
+            if (none) return;
         }
+    }
 }
 
 template <typename T, int D, bool KEYS>

@@ -204,3 +204,34 @@ def test_more_tiles_than_are_remembered():
     assert torch.equal(clean[1], got[1])
     for name, lost, a, b in (("o", o, clean[0], got[0]), ("dq", dq, clean[2], got[2]), ("dk", dk, clean[3], got[3]), ("dv", dv, clean[4], got[4])):
         assert torch.isnan(b[lost]).all() and torch.equal(a[~lost], b[~lost]), name
+
+
+@pytest.mark.parametrize("bads", [[math.inf], [math.inf, -math.inf, math.nan]])
+def test_more_blocks_of_a_pass_than_are_remembered(bads):
+    """A first token's pass of 44 blocks (4 heads of 11) a part, a gradient that is not finite in each: 32 of them are listed."""
+    gen = torch.Generator("cuda").manual_seed(6)
+    n, d, h = 2100, 16, 4
+    q, dout, k, v = (normal(gen, 1, n, x, d, dtype=torch.bfloat16) for x in (h, h, 1, 1))
+    for i, row in enumerate(range(7, n, 50)):
+        dout[0, row, :, 3] = bads[i % len(bads)]
+    o, lse = forward(q, k, v, 500, 3)
+    grads = backward(dout, q, k, v, o, lse, 500, 3)
+    check_backward(dout[0], q[0], k[0], v[0], o[0], lse[0], 500, 3, [g[0] for g in grads])
+    dout[0, 1500:, :, :] = math.nan
+    grads = backward(dout, q, k, v, o, lse, 500, 3)
+    check_backward(dout[0], q[0], k[0], v[0], o[0], lse[0], 500, 3, [g[0] for g in grads])
+
+
+@pytest.mark.parametrize("d, wide", [(63, 64), (33, 40), (100, 104), (8, 9)])
+def test_heads_inside_wider_ones(d, wide):
+    """Rows whose last elements are not eight, and ones that are copied first; what lies behind a head is not a number and does not count."""
+    gen = torch.Generator("cuda").manual_seed(d)
+    new = lambda h: torch.full((1, 150, h, wide), math.nan, device="cuda", dtype=torch.bfloat16)[..., :d].copy_(normal(gen, 1, 150, h, d, dtype=torch.bfloat16))  # noqa: E731
+    q, k, v, dout = new(4), new(2), new(2), new(4)
+    v[0, 70, 0, d - 1], v[0, 149, 1, 0], dout[0, 90, 1, d - 1], k[0, 20, 1, d - 1] = math.inf, math.nan, -math.inf, math.nan
+    o, lse = forward(q, k, v, 50, 2)
+    check_forward(q[0], k[0], v[0], 50, 2, o[0], lse[0])
+    grads = backward(dout, q, k, v, o, lse, 50, 2)
+    check_backward(dout[0], q[0], k[0], v[0], o[0], lse[0], 50, 2, [g[0] for g in grads])
+    o, lse = forward(q[:, :3], k, v, 50, 2)
+    check_forward(q[0, :3], k[0], v[0], 50, 2, o[0], lse[0])
