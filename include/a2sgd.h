@@ -538,7 +538,8 @@ typedef struct a2sgd_heads {
  *   lse         fp32 [sequences][q_heads][q_rows] (packed: [q_heads][q_rows]), out, for the backward pass; may be NULL
  * Tensors whose address is a multiple of 16 bytes and whose strides are multiples of 8 elements are read where they are; others are
  * first copied to the workspace.  What is not finite reaches what sees it only, in the backward pass, too: a query that sees a value that is
- * not finite has an output that is not in that column, one that sees a score that is infinite or not a number an output that is not a number.
+ * not finite has an output that is not in that column, one that sees a score of +infinity or not a number (or none but -infinity) an output that is
+ * not a number.  Scores (scaled) are meant to stay below 2^24: fp32 does not tell larger ones apart.
  * (A tile of queries or keys with an output that is not finite is worked on twice: a call with such a place in every tile takes some times as long.)
  *   workspace   DEVICE, 256-byte aligned, a2sgd_window_attention_workspace bytes: flags A2SGD_ATTENTION_BACKWARD,
  *               A2SGD_ATTENTION_ALIGNED when every tensor that is read is laid out as above, and A2SGD_ATTENTION_PACKED_Q, _PACKED_K
@@ -569,7 +570,7 @@ int a2sgd_window_attention_forward(const a2sgd_attention *shape, const a2sgd_hea
  *     delta = sum_c dout o,   P = exp(scale q . k - lse),   dS = P (dout . v - delta)
  *     dq = scale sum_j dS k,   dk = scale sum_i dS q,   dv = sum_i P dout      (dk, dv over the query heads of the key head, too)
  * P and dS are rounded once to the 16-bit type, as operands of the products; with float16 scale dout so that dS stays between 2^-14 and
- * 65504.  dq, dk, dv may each be NULL, and what only they need is then not computed.  Rows in a range that no query sees get zeros. */
+ * 65504; a P below 2^-25 gives nothing to dv there.  dq, dk, dv may each be NULL, and what only they need is then not computed.  Rows in a range that no query sees get zeros. */
 int a2sgd_window_attention_backward(const a2sgd_attention *shape, const a2sgd_heads *dout, const a2sgd_heads *q, const a2sgd_heads *k,
                                     const a2sgd_heads *v, const a2sgd_heads *o, const float *lse, const a2sgd_heads *dq,
                                     const a2sgd_heads *dk, const a2sgd_heads *dv, void *workspace, uint64_t workspace_bytes, int device,
@@ -580,12 +581,13 @@ int a2sgd_window_attention_backward(const a2sgd_attention *shape, const a2sgd_he
  *     (u, v) <- (u cos - v sin, u sin + v cos)      (A2SGD_ROTARY_INVERSE: by the opposite angle, which is the backward pass)
  *     omega_j = base^(-j / n);   A2SGD_ROTARY_LADDER_PER_AXIS: base^(-l / sections[a]), l counted from the axis' first pair
  * Pair j is the elements j and j + n; A2SGD_ROTARY_INTERLEAVED: 2 j and 2 j + 1.  Elements past the pairs are copied.  Angles are kept as
- * 64-bit fractions of a turn (pos times a 64-bit frequency, modulo one turn), so that far positions lose nothing.
+ * 64-bit fractions of a turn (pos times a 64-bit frequency, modulo one turn), so that far positions lose nothing (with a base below 1, frequencies
+ * above a turn a step have fewer bits by those before their point).
  *   q, k        [tokens] rows of q_heads and k_heads heads (sequence_stride is not read); outputs q_out, k_out the same; an output may be its
  *               input.  k_heads may be 0
  *   positions   DEVICE, int32 [axes][tokens];   sections  HOST [axes], each at least 1;   axes 1 to A2SGD_ROTARY_MAX_AXES
  *   head_dim    1 to A2SGD_ROTARY_MAX_HEAD_DIM, >= 2 n;   base  finite, > 0;   dtype  any
- * Heads that start at multiples of 16 bytes, with n a multiple of 16 bytes too where pairs are not interleaved, take 128-bit accesses. */
+ * Heads that start at multiples of 16 bytes, with n and head_dim - 2 n multiples of 8, take 128-bit accesses, others one element an access. */
 #define A2SGD_ROTARY_MAX_AXES 4
 #define A2SGD_ROTARY_MAX_HEAD_DIM 512
 #define A2SGD_ROTARY_INTERLEAVED 1u

@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : C == 1 ? 2 : 1) 
 template <typename T, typename R, int VEC, int C, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(const __grid_constant__ Args a)
 {
-    extern __shared__ __align__(16) float columns[]; // w2, alpha gate w1 (alpha gate without a norm), and for C > 1 the four sums
+    extern __shared__ __align__(16) float columns[]; // w2, alpha gate w1 (alpha gate without a norm), and the four sums: for C == 1 on their way out
     __shared__ float slots[2][48]; // in turn: one barrier a norm leaves no time to empty them
     int turn = 0;
     wait_prior_grid();
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
     bring_pre(row0);
     bring_post(row0);
     int64_t gate_end = row0, group = 0; // rows from here on have another gate
-    int since = 0, puts = 0; // rows since the sums were last put down, and how often they were
+    int puts = 0; // how often the sums of t were put down; those of du are after every kRun-th row
     const float per = 1.0f / (float)a.d;
     for (int64_t r = row0; r < end; ++r) {
         const float mean1 = next_mean1, rstd1 = next_rstd1, mean2 = next_mean2, rstd2 = next_rstd2;
@@ -483,36 +483,41 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
             }
         }
         // what the rows since the last time give to the gate, the post weight and the post bias, and to the pre weight and bias
-        if (want && (++since == kRun || r + 1 == gate_end)) {
-            const bool last = r + 1 == end, gate_over = r + 1 == gate_end, begun = r + 1 - max(row0, group * a.gate_rows) > since; // some of the gate's rows have been
+        if (want && ((r + 1 - row0) % kRun == 0 || r + 1 == gate_end)) {
+            const int64_t runs = (r - row0) / kRun; // before this one
+            const bool last = r + 1 == end, gate_over = r + 1 == gate_end, begun = runs * kRun + row0 > max(row0, group * a.gate_rows); // some of the gate's rows have been
+            const bool du_due = last || (r + 1 - row0) % kRun == 0;
             const bool whole = a.gate && group * a.gate_rows >= row0 && min(a.rows, (group + 1) * a.gate_rows) <= end;
-            const int slot = a.gate && group != row0 / a.gate_rows, place = puts % kRun;
+            const int slot = a.gate && group != row0 / a.gate_rows;
             const int64_t mine = (int64_t)blockIdx.x * kSums * a.d;
-            const auto put = [&](int s, int c, float v) {
+            const auto put = [&](int s, int c, int64_t n, float v) { // the n-th of a sum's runs
                 float *sum = a.partials + mine + s * a.d + c, *run = a.runs + mine + s * a.d + c;
+                const int place = (int)(n % kRun);
                 if (place) v += *run;
-                if (last || place == kRun - 1) *sum = puts >= kRun ? *sum + v : v;
+                if (last || place == kRun - 1) *sum = n >= kRun ? *sum + v : v;
                 else *run = v;
             };
-            float mine4[kSums][8];
-            if constexpr (C == 1) {
+            if constexpr (C == 1) { // through shared memory: a column at a time takes few registers
 #pragma unroll
-                for (int q = 0; q < kSums; ++q) {
-                    singles8(mine4[q], acc[q]);
+                for (int q = 0; q < kSums; ++q)
+                    if (q < 2 || du_due) {
+                        float f[8];
+                        singles8(f, acc[q]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[q][i] = pair(0.0f);
-                }
+                        for (int i = 0; i < 8; ++i) sum_at(q, 0, i) = f[i];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[q][i] = pair(0.0f);
+                    }
             }
 #pragma unroll 1
             for (int k = 0; k < C; ++k) {
-#pragma unroll
+#pragma unroll 1
                 for (int i = 0; i < 8; ++i) {
                     const int c = column<VEC>(k, i);
                     if (c >= a.d) continue;
                     const auto take = [&](int q) {
-                        if constexpr (C == 1) return mine4[q][i];
                         const float v = sum_at(q, k, i);
-                        sum_at(q, k, i) = 0.0f;
+                        if (C > 1) sum_at(q, k, i) = 0.0f;
                         return v;
                     };
                     const float one_hat = take(0), one = take(1);
@@ -524,13 +529,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) k_backward(co
                         else *part = v; // a whole gate's place is free: a first gate that has rows before this CTA, or a last one behind it, is another
                     }
                     const float f = a.gate ? a.alpha * param_at(a.gate, a.param, group * a.d + c) : a.alpha;
-                    put(0, c, f * one_hat);
-                    put(1, c, f * one);
-                    put(2, c, take(2));
-                    put(3, c, take(3));
+                    put(0, c, puts, f * one_hat);
+                    put(1, c, puts, f * one);
+                    if (du_due) {
+                        put(2, c, runs, take(2));
+                        put(3, c, runs, take(3));
+                    }
                 }
             }
-            since = 0;
             ++puts;
         }
     }
@@ -618,7 +624,7 @@ const void *pick_types(int dtype, int residual, const Plan &p, bool backward)
 }
 size_t smem_of(const Plan &p, bool backward)
 {
-    return (size_t)(backward ? 2 + (p.chunks > 1 ? kSums : 0) : 4) * p.chunks * 8 * p.threads * 4;
+    return (size_t)(backward ? 2 + kSums : 4) * p.chunks * 8 * p.threads * 4;
 }
 
 int check_shape(const a2sgd_residual *s)
@@ -749,8 +755,7 @@ extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a
     }
     if ((sums->dgate && !shape->gate) || (!post && (sums->dpost_weight || sums->dpost_bias))) return A2SGD_ERR_ARG;
     if (!aligned(workspace, 256)) return A2SGD_ERR_ALIGN;
-    if (want && some && (!workspace || workspace_bytes < a2sgd_residual_norm_workspace(shape->rows, shape->d, shape->gate ? shape->gate_rows : 0, device)))
-        return A2SGD_ERR_ARG;
+    if (want && some && (!workspace || workspace_bytes < sums_bytes(1, shape->d, false, shape->gate))) return A2SGD_ERR_ARG;
     DeviceGuard guard(device);
     const int sms = guard.ok ? sm_count(device) : 0;
     if (sms < 1) return A2SGD_ERR_CUDA;
@@ -776,6 +781,7 @@ extern "C" int a2sgd_residual_norm_backward(const a2sgd_residual *shape, const a
     if (want) {
         const int64_t each = (int64_t)a.ctas * kSums * a.d;
         const bool several = several_puts(shape->rows, shape->gate ? shape->gate_rows : 0, device);
+        if (workspace_bytes < sums_bytes(a.ctas, shape->d, several, shape->gate)) return A2SGD_ERR_ARG; // no more than a2sgd_residual_norm_workspace
         a.partials = static_cast<float *>(workspace);
         a.runs = several ? a.partials + each : nullptr;
         a.gate_partials = a.partials + (several ? 2 : 1) * each;

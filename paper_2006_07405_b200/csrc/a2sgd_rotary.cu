@@ -9,8 +9,8 @@
 //
 // An angle is a 64-bit fraction of a turn, the product of the position and the frequency in turns modulo 2^64: whole turns fall
 // off by themselves, so that a position of 2^30 is turned as exactly as one of 1.  (In fp32 the product alone would be off by
-// position * 2^-24 radians.)  The upper bits say the quarter of a turn; what is left, at most an eighth either way, is exact to 2^-33
-// of a turn and goes through sincospif, whose error is two units in the last place.
+// position * 2^-24 radians.)  The upper bits say the quarter of a turn; what is left, at most an eighth either way, is rounded
+// to fp32, at most 2^-28 of a turn off, and goes through sincospif, whose error is two units in the last place.
 #include "a2sgd_train.cuh"
 
 #include <algorithm>

@@ -93,3 +93,16 @@ def test_room_is_what_the_device_uses(d, ctas):
     assert B.a2sgd_residual_norm_workspace(65536, d, 1000) <= sms * ctas * 10 * d * 4
     assert B.a2sgd_residual_norm_workspace(1 << 24, d) <= sms * ctas * 8 * d * 4
     assert B.a2sgd_residual_norm_workspace(3, d) == 3 * 4 * d * 4 and B.a2sgd_residual_norm_workspace(0, d) == 0
+
+
+def test_too_little_room_is_refused():
+    one = torch.ones((2000, 64), dtype=torch.bfloat16, device="cuda")
+    rstd, sums = torch.ones(2000, device="cuda"), torch.empty(64, device="cuda")
+    n = B.a2sgd_residual_norm_workspace(2000, 64)
+    work = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for size in (4 * 64 * 4, n // 4 // 256 * 256):
+        with pytest.raises(B.A2SGDError) as e:
+            B.a2sgd_residual_norm_backward(one, one, one, one, None, None, "rms", post=False, pre_rstd=rstd, dpre_weight=sums, workspace=work[:size])
+        assert e.value.status == B.ERR_ARG
+    B.a2sgd_residual_norm_backward(one, one, one, one, None, None, "rms", post=False, pre_rstd=rstd, dpre_weight=sums, workspace=work)
+    assert (sums == 2000).all()
