@@ -14,10 +14,11 @@
 //
 // Statistics, sums and z before its rounding are fp32; z and u (dx and dy) are rounded once, as they are written.
 //
-// B200, 65536 x 1600, bfloat16: forward with an fp32 residual stream 256 us (4.9 TB/s, 75 % of a copy's), four CTAs of 224 threads an SM: a row's two
+// B200, 65536 x 1600, bfloat16: forward with an fp32 residual stream 256 us (4.9 TB/s, 75 % of a copy's; 280 among other work), four CTAs of 224 threads an SM: a row's two
 // barriers and the little that is on its way meanwhile bound it (two rows on their way take the registers of a CTA: 306 us; parameters read from
-// memory for each row 761).  Backward of a layer norm 364 us (3.5 TB/s), of which the fold is 20: three CTAs an SM (80 registers, of which 8 bytes a
-// thread spill; two CTAs 405 us).  16 rows: 7.0 us on the device, 11.9 a call.
+// memory for each row 761).  Backward of a layer norm 361 us (3.5 TB/s), of which the fold is 15: three CTAs an SM (80 registers, beyond which 8 bytes a
+// thread spill; with an fp32 stream 40, all in fp32 136, one element an access 184 to 216, and above 4096 columns 108 to 132 there; two CTAs 405
+// us).  16 rows: 7.0 us on the device, 11 a call.  A gate of few rows costs its sums' way to memory: 64 rows a gate 878 us.
 #include "a2sgd_train.cuh"
 
 #include <algorithm>

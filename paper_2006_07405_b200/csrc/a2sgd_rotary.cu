@@ -4,8 +4,8 @@
 //
 // Bound by memory: every element of q and k is read and written once.  A thread takes eight pairs of one token (one where addresses, strides or
 // pairs do not allow 128-bit accesses), works out their sines and cosines once, and walks the heads with them; few tokens share their heads out
-// among threads, until the SMs are full.  B200, 65531 tokens, 32 and 8 heads of 128: 213 us (6.3 TB/s, 96 % of a copy's); 4097 tokens, 13 and 13 heads
-// of 80 in fp32, odd rows: 20.5 us (3.3 TB/s: a single element an access); 16 tokens: 2.8 us on the device, 10.9 a call.
+// among threads, until the SMs are full.  B200, 65531 tokens, 32 and 8 heads of 128: 215 us (6.2 TB/s, 95 % of a copy's; fp32 464); 4097 tokens, 13 and 13 heads
+// of 80 in fp32, odd rows: 20.5 us (3.3 TB/s: a single element an access); 16 tokens: 2.8 us on the device, 9.7 a call.
 //
 // An angle is a 64-bit fraction of a turn, the product of the position and the frequency in turns modulo 2^64: whole turns fall
 // off by themselves, so that a position of 2^30 is turned as exactly as one of 1.  (In fp32 the product alone would be off by

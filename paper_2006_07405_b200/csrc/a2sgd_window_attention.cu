@@ -59,9 +59,9 @@ __device__ __forceinline__ float lse_from(float ref, float sum) { return sum > 0
 //
 // Bound, for heads of 64, by the softmax' warps: 16 exponentials a clock and SM are 164 us of 8 x 4096 queries, 25 heads of 64, window 1024 (737 M
 // pairs), and with the loads from and stores to TMEM, the sums and the rounding to 16 bits a block takes a warp twice that; the products alone are
-// 116 us.  B200: 344 us (550 TFLOP/s, tensor pipe 31 % busy); 20011 packed rows, 16 heads of 128, window 4096, float16: 225 us (871 TFLOP/s,
-// 54 %).  One CTA an SM with 16 softmax warps, and every second exponential as a polynomial on the multiply-add pipe, measured the same; one
-// loading warp for keys and values 364 and 240 us; 16-byte stores 348 and 230.
+// 116 us.  B200: 349 us (541 TFLOP/s, tensor pipe 30 % busy); 20011 packed rows, 16 heads of 128, window 4096, float16: 234 us (838 TFLOP/s,
+// 53 %); among other work 381 and 267.  One CTA an SM with 16 softmax warps, and every second exponential as a polynomial on the multiply-add pipe,
+// measured the same; one loading warp for keys and values 6 % more, 16-byte stores 1 to 2 %.
 struct ForwardArgs {
     CUtensorMap q, k, v;
     Heads o, values; // values: what v is read from
@@ -767,8 +767,8 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 // free as long as q has the same.  Values come in rows, and through ldmatrix.trans.  Every warp has its own maximum, sum and output; they meet in shared
 // memory, and those of a row's CTAs in that of a cluster's CTA, or beyond eight CTAs in memory and a second launch.
 //
-// B200: 64 sequences, 32 heads of 128, 8 key heads, 4112 of 8192 keys visible, 1079 MB: 179 us (6.0 TB/s, 92 % of a copy's).  4 sequences, 25 heads of
-// 64, 1028 keys, 26 MB: 10.8 us on the device, 11.9 a call: 2 until the first keys are asked for, 5 until the last are used, 1.2 and 0.9 for the two
+// B200: 64 sequences, 32 heads of 128, 8 key heads, 4112 of 8192 keys visible, 1079 MB: 171 us (6.3 TB/s, 96 % of a copy's), among other work 182.
+// 4 sequences, 25 heads of 64, 1028 keys, 26 MB: 10.8 us on the device, 11 to 13.5 a call: 2 until the first keys are asked for, 5 until the last are used, 1.2 and 0.9 for the two
 // joins (with threads of eight columns each, and a cluster's CTAs reading one another, 13.0 us); the call itself is 10.5 us on the host.
 // 1 sequence, 32 heads of 128, 8 key heads: 8192 keys (34 MB) 14.4 us, 131072 keys (537 MB) 77 us (7.0 TB/s: part of it stays in L2).
 constexpr int kFewRows = 16, kFewKeys = 16, kFewCluster = 8, kMostShares = 320; // the last: CTAs of a call whose rows are shared out beyond a cluster
@@ -1134,8 +1134,8 @@ struct DeltaArgs {
 };
 
 // ------------------------------------------------------------------ backward
-// Two launches of one template, so that nothing is added up by atomics (S and dP are formed twice: 14 D operations a pair in place of 10, and
-// two exponentials in place of one): the same call gives the same bits.
+// Two launches of one template, so that each output is added up by one CTA, in order, and the same call gives the same bits.  (S and dP are formed twice:
+// 14 D operations a pair in place of 10, and two exponentials in place of one.  One launch would have to keep dq's parts and join them in order.)
 //   KEYS false: 128 queries stay, blocks of 64 keys pass:        dQ += dS K
 //   KEYS true:  128 keys stay, blocks of 64 queries pass, of all query heads of the key head:   dK += dS^T Q,  dV += P^T dO
 // In either, with A, A' the tiles that stay and B, B' those that pass:  S = A B^T, dP = A' B'^T into TMEM; a thread reads its row, forms
@@ -1146,9 +1146,10 @@ struct DeltaArgs {
 // queries are cut by their own lengths, which the device knows: see PartsList.
 //
 // Bound by the softmax' warps and what lies between them and the products: S and dP come out of TMEM, P and dS go back, 1100 to 1400 clocks a block of
-// 64, in which the products take 611 and the exponentials 560.  B200, 8 x 4096 queries, 25 heads of 64, window 1024: dk and dv 610 us, dq 490,
-// delta 54, together 1131 (416 TFLOP/s of the 10 D operations a pair); 5003 packed rows, 12 heads of 80: 80 us.  CTAs take their tiles from a counter,
-// and dq's begin where dk and dv's end (tiles dealt out by number, dq first: 1140 and 113 us; one launch after the other 1160 and 118).  Which
+// 64, in which the products take 611 and the exponentials 560.  B200, 8 x 4096 queries, 25 heads of 64, window 1024: 1152 us (409 TFLOP/s of the 10 D
+// operations a pair), among other work 1230; by themselves, cold, dk and dv 653, dq 500, delta 55, the fold 5.  5003 packed rows, 12 heads of 80: 77
+// us.  CTAs take their tiles from a counter, and dq's begin where dk and dv's end (tiles dealt out by number, dq first: 113 us for the packed rows, 1 %
+// more for the others; one launch after the other 118, and 3 %).  Which
 // CTA has a tile changes nothing in its result.  Measured and not taken: blocks of 128 with places of their own for P and dS (1240 us: one buffer
 // only), 16 softmax warps, two CTAs an SM, exponentials by polynomials (no change).
 struct BackwardArgs {
