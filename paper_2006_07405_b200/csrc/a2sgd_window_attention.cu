@@ -241,7 +241,7 @@ struct Marred {
 };
 // Columns first to last (first a multiple of 8) of an output that this thread wrote, and of a row that it sees, in a tensor that TMA can read: what is not
 // finite there is not finite here.  As a product with 0 < P: plus itself; with dS, whose sign may be any: not a number.  Returns whether no column
-// is a number any more.
+// is finite any more.
 template <bool SIGNED, typename T, typename O>
 __device__ __forceinline__ bool add_not_finite(O *out, const T *row, int first, int last)
 {
@@ -258,7 +258,7 @@ __device__ __forceinline__ bool add_not_finite(O *out, const T *row, int first, 
         for (int i = c; i < min(c + 8, last); ++i) {
             const float v = to_f32(row[i]), sum = isfinite(v) ? 0.0f : SIGNED ? to_f32(out[i]) + v : NAN;
             if (!isfinite(v)) out[i] = from_f32<O>(sum);
-            none = none && sum != sum;
+            none = none && !isfinite(v);
         }
     }
     return none;
