@@ -115,3 +115,9 @@ def test_more_sequences_than_a_list_is_made_of_at_once():
 def test_one_long_sequence_among_packed_rows():
     run([5000], [5000], True, True, 1, 1, 64, 70, 3)
     run([1, 5000, 1], [1, 5000, 1], True, True, 1, 1, 64, 70, 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("packed", [True, False])
+def test_many_queries_and_no_keys(packed):
+    run([200, 3, 130], [0, 0, 1], packed, packed, 2, 1, 64, 30, 2)
