@@ -147,8 +147,8 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int chunks, int rows, 
 // A hidden pair's P (or dS) is 0, and 0 times infinity is not a number: an operand that is not finite reaches rows that do not see it.  So a tile
 // with an output that is not finite is done once more, with care: blocks that not every row sees are looked through before their product with P, what is
 // not finite in them is put to 0, and the rows that do see it are given it by mend_row.  A tile without such an output pays for the question: 8 x 4096,
-// 25 heads of 64, forward 346 -> 350 us, backward 1165 -> 1181, 5003 packed rows 80 -> 83.5 (looked through at once: 366, 1201 and 92).  With a first
-// token's value and a third of the gradients not finite in every sequence, 1.7 ms and 2.5 ms.
+// 25 heads of 64, forward 345 -> 349 us, backward 1140 -> 1152, 5003 packed rows 3 us (looked through at once: 366, 1183 and 11 us).  With a first
+// token's value, and 67 queries' gradients, not finite in every sequence: 1.2 ms and 2.8 ms.
 constexpr int kAgain = 64;
 struct Again { // in shared memory: the tiles to be done again, in turn
     int last;  // of those that have been put down, the tile's number among the CTA's
@@ -768,8 +768,9 @@ __global__ void __launch_bounds__(ForwardShape<D>::kThreads, ForwardShape<D>::kC
 // memory, and those of a row's CTAs in that of a cluster's CTA, or beyond eight CTAs in memory and a second launch.
 //
 // B200: 64 sequences, 32 heads of 128, 8 key heads, 4112 of 8192 keys visible, 1079 MB: 171 us (6.3 TB/s, 96 % of a copy's), among other work 182.
-// 4 sequences, 25 heads of 64, 1028 keys, 26 MB: 10.8 us on the device, 11 to 13.5 a call: 2 until the first keys are asked for, 5 until the last are used, 1.2 and 0.9 for the two
-// joins (with threads of eight columns each, and a cluster's CTAs reading one another, 13.0 us); the call itself is 10.5 us on the host.
+// 4 sequences, 25 heads of 64, 1028 keys, 26 MB: 10.8 us on the device, 11 to 13.5 a call: 2 until the first keys are asked for, 5 until the last are
+// used, 1.2 and 0.9 for the two joins (with threads of eight columns each, and a cluster's CTAs reading one another, 13.0 us); the call itself is 10.5
+// us on the host.
 // 1 sequence, 32 heads of 128, 8 key heads: 8192 keys (34 MB) 14.4 us, 131072 keys (537 MB) 77 us (7.0 TB/s: part of it stays in L2).
 constexpr int kFewRows = 16, kFewKeys = 16, kFewCluster = 8, kMostShares = 320; // the last: CTAs of a call whose rows are shared out beyond a cluster
 template <int D>
@@ -1158,7 +1159,7 @@ struct BackwardArgs {
     Heads passing;    // what k, or dout, is read from
     int wide0, wide1;
     const float *lse2, *delta; // [q_heads][q_rows] a plane: log2 e times lse, delta
-    float *partials;           // [lanes][sink_rows][parts][2][D]
+    float *partials;           // rows of dk and of dv, [2][D] each: see partial_row
     const int32_t *q_ranges, *k_ranges;
     int q_heads, kv_heads, group, d, q_rows, k_rows, window, sinks;
     int packed_q, packed_k, sequences; // packed_q: one plane of lse2 and delta
@@ -1181,8 +1182,9 @@ struct BackwardShape {
 };
 
 // Sequences of packed queries whose first tokens' passes have more than one part, in order: their number, the sequences, and for each how many parts
-// beyond a first one the sequences before it have (and, last, all have); and for the fold their queries, and their keys' first row and number.  Every query is in one sequence, so that the parts of all together are bound by
-// the rows (`more` beyond the first ones); a sequence beyond that bound, as overlapping ranges could have it, keeps one part.
+// beyond a first one the sequences before it have (and, last, all have); and for the fold their queries, and their keys' first row and number.  Every
+// query is in one sequence, so that the parts of all together are bound by the rows (`more` beyond the first ones); a sequence beyond that bound, as
+// overlapping ranges could have it, keeps one part.
 struct PartsList {
     const int *p;
     int room; // sequences; read through L1: thousands of warps of the fold ask for the same few lines

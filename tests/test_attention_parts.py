@@ -121,3 +121,35 @@ def test_one_long_sequence_among_packed_rows():
 @pytest.mark.parametrize("packed", [True, False])
 def test_many_queries_and_no_keys(packed):
     run([200, 3, 130], [0, 0, 1], packed, packed, 2, 1, 64, 30, 2)
+
+
+@pytest.mark.gpu
+def test_captured_and_replayed_with_other_lengths():
+    """The list of parts is the device's: a replay goes by the ranges as they are then."""
+    gen, rows, window, sinks = torch.Generator("cuda").manual_seed(3), 5200, 60, 9
+    q, dout = (normal(gen, rows, 4, 64) for _ in range(2))
+    k, v = (normal(gen, rows, 2, 64) for _ in range(2))
+    ranges = torch.tensor([[0, 200], [200, 5000], [5200, 0]], dtype=torch.int32, device="cuda")
+    kw = dict(window=window, sinks=sinks, q_ranges=ranges, k_ranges=ranges)
+    work = torch.empty(B.a2sgd_window_attention_workspace(q, k, window, sinks, 3, backward=True), dtype=torch.uint8, device="cuda")
+    o, lse, grads = torch.zeros_like(q), torch.zeros((4, rows), device="cuda"), [torch.zeros_like(t) for t in (q, k, v)]
+
+    def both(o, lse, grads, work):
+        B.a2sgd_window_attention_forward(q, k, v, o, lse, workspace=work, **kw)
+        B.a2sgd_window_attention_backward(dout, q, k, v, o, lse, *grads, workspace=work, **kw)
+
+    both(o, lse, grads, work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(o, lse, grads, work)
+    other = torch.empty_like(work)
+    for lens in ([5000, 200, 0], [2500, 100, 2600], [1, 1, 5198], [1700, 1700, 1800]):
+        first = [0, lens[0], lens[0] + lens[1]]
+        ranges.copy_(torch.tensor(list(zip(first, lens)), dtype=torch.int32, device="cuda"))
+        graph.replay()
+        want = torch.zeros_like(q), torch.zeros((4, rows), device="cuda"), [torch.zeros_like(t) for t in (q, k, v)]
+        both(*want, other)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and all(torch.equal(a, b) for a, b in zip(grads, want[2]))
+    assert B.a2sgd_window_attention_status() == B.OK
